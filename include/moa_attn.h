@@ -40,7 +40,9 @@ enum moa_status {
     MOA_ERR_UNSUPPORTED_SHAPE = 3, /* head dimensions or sizes outside what the kernels take */
     MOA_ERR_MISALIGNED = 4,        /* a pointer not 16-byte aligned, or a row not a multiple of 16 bytes */
     MOA_ERR_CUDA = 5,              /* a CUDA runtime/driver call failed (message in moa_last_error) */
-    MOA_ERR_DEVICE_TIMEOUT = 6     /* a kernel gave up on a wait and recorded it in the status word */
+    MOA_ERR_DEVICE_TIMEOUT = 6,    /* a kernel gave up on a wait and recorded it in the status word */
+    MOA_ERR_DEVICE_INDEX = 7       /* a kernel met a position, length or page number outside its table
+                                      and recorded it in the status word */
 };
 
 /*
@@ -335,6 +337,139 @@ int moa_attn_fwd_splitkv_noalloc(const void* Q, const void* K, const void* V, vo
                                  int64_t d_v, float scale, int dtype, int num_splits,
                                  void* stream);
 
+/* ------------------------------------------------------------------------------------------
+ * Operators around attention: per-head norms with rotation, and a 4-bit cache.
+ *
+ * The paper has no counterpart to these; they carry a projected token to the attention above
+ * (training) or to a cache and back out of it (generation).  Common rules:
+ *   * Tensors [B, H, N, d] have unit stride along d and any strides along B, H and N, in
+ *     elements: `strides` points to host memory holding (b, h, n) for each tensor in the order
+ *     named.  Every row starts on a 16-byte boundary.  Strides of an input may be 0 (broadcast);
+ *     an output's rows must not overlap one another.
+ *   * Asynchronous on `stream`; arguments are checked before anything is launched, and on a
+ *     non-OK return nothing was launched.  Nothing is allocated.  B, H, N >= 1.
+ *   * Values that live on the device (positions, lengths, page numbers) are checked by the
+ *     kernels: one outside its table reads and writes nothing there and is recorded for
+ *     moa_get_device_status (MOA_ERR_DEVICE_INDEX); what the outputs hold then is said below.
+ * ------------------------------------------------------------------------------------------ */
+
+/*
+ * moa_qk_norm_rope -- RMS norm of every head of Q and K and the rotation of its position, one pass.
+ *
+ * Defines, for each row x of d features (one token of one head) with the weight w of its tensor,
+ * r = (mean_j x_j^2 + eps)^(-1/2) and u_j = w_j x_j r.  Each pair (a, b) of the first d_rot
+ * features is then rotated by the angle of the row's position p = pos[b, n]:
+ *     y_a = u_a cos[p, i] - u_b sin[p, i],   y_b = u_b cos[p, i] + u_a sin[p, i],   i < d_rot / 2,
+ * with (a, b) = (i, i + d_rot/2), or (2 i, 2 i + 1) if `interleaved`; the other features pass.
+ * A negative position marks padding: its rows are written as zeros.
+ *
+ *   Q  [B, H_q, N, d], K  [B, H_k, N, d]  inputs;  Qo, Ko  outputs of the same shapes
+ *   W_q, W_k   [d], contiguous, the element type of Q
+ *   cos, sin   float32 [n_pos, d_rot / 2], contiguous;  pos  int32 [B, N], contiguous
+ *   strides    12 values: Q, K, Qo, Ko
+ *   eps        > 0 and finite;   dtype  MOA_BF16 or MOA_FP32
+ * d a multiple of 8 up to 256; d_rot a multiple of 16, 16 <= d_rot <= d.  Qo may be Q and Ko may
+ * be K with the same strides (in place); no other overlap.  Q and K may be slices of one buffer.
+ * Computed in fp32, rounded once.  Position >= n_pos: the row is NaN, MOA_ERR_DEVICE_INDEX.
+ */
+int moa_qk_norm_rope(const void* Q, const void* K, const void* W_q, const void* W_k,
+                     const float* cos, const float* sin, const int32_t* pos, void* Qo, void* Ko,
+                     int64_t B, int64_t H_q, int64_t H_k, int64_t N, int64_t d, int64_t d_rot,
+                     int64_t n_pos, const int64_t* strides, float eps, int interleaved, int dtype,
+                     void* stream);
+
+/*
+ * moa_qk_norm_rope_bwd -- the gradients of moa_qk_norm_rope.
+ *
+ * With g the gradient of a row's output, t = g rotated by the opposite angle:
+ *     dW = sum over rows of t x r,    dx = r (W t - x r mean(W t x r)).
+ *   Q, K, W_q, W_k, cos, sin, pos  as in the forward;  dQo, dKo  gradients of its outputs
+ *   dQ, dK     outputs, element type of Q;   dW_q, dW_k  outputs, float32 [d]
+ *   strides    18 values: Q, K, dQo, dKo, dQ, dK
+ *   workspace  device, 16-byte aligned, moa_qk_norm_rope_bwd_workspace_bytes(...) bytes
+ * Padding rows get zero gradients and add nothing to dW; rows with a position >= n_pos get NaN
+ * gradients and add nothing.  dQ may be dQo (and dK dKo) with the same strides.  Two launches;
+ * bitwise reproducible.
+ */
+int moa_qk_norm_rope_bwd(const void* Q, const void* K, const void* W_q, const void* W_k,
+                         const float* cos, const float* sin, const int32_t* pos, const void* dQo,
+                         const void* dKo, void* dQ, void* dK, float* dW_q, float* dW_k, int64_t B,
+                         int64_t H_q, int64_t H_k, int64_t N, int64_t d, int64_t d_rot,
+                         int64_t n_pos, const int64_t* strides, float eps, int interleaved,
+                         int dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Scratch bytes of moa_qk_norm_rope_bwd on the current device (0 for sizes < 1 or no device). */
+size_t moa_qk_norm_rope_bwd_workspace_bytes(int64_t B, int64_t H_q, int64_t H_k, int64_t N,
+                                            int64_t d);
+
+/*
+ * The 4-bit cache.  A pool holds n_pages pages of page_tokens tokens (a multiple of 16) for H key
+ * heads; sequence b's token at position p lies in page pages[b, p / page_tokens], at place
+ * p % page_tokens.  32 neighbouring features of one head and token share a scale
+ * s = bf16(max |x| / 7); a feature is stored as code = rint(x / s) in [-7, 7] (ties to even) and
+ * stands for code * s: 4.5 bits a value.  A group with a member that is not finite reads as NaN.
+ *
+ * moa_kv4_pool_bytes -- size of a pool: 9 (d_k + d_v) bytes for 16 tokens of one head (0 for
+ * unsupported sizes).  d_k, d_v in {64, 128}.  The pool is 16-byte aligned device memory, owned by
+ * the caller; its contents need no initial value.
+ */
+size_t moa_kv4_pool_bytes(int64_t n_pages, int64_t H, int64_t page_tokens, int64_t d_k,
+                          int64_t d_v);
+
+/*
+ * moa_kv4_write -- quantises rows of keys and values into the pool.
+ *   K [B, H, N, d_k], V [B, H, N, d_v]  inputs;  strides  6 values: K, V;  dtype MOA_BF16 or MOA_FP32
+ *   pool   written at the rows' places only
+ *   pages  int32 [B, max_pages];  pos  int32 [B, N], the tokens' positions; negative: not written
+ * No two rows of a call may name the same place.  A position or page outside its table: that row
+ * is not written, MOA_ERR_DEVICE_INDEX.
+ */
+int moa_kv4_write(const void* K, const void* V, void* pool, const int32_t* pages,
+                  const int32_t* pos, int64_t B, int64_t H, int64_t N, int64_t d_k, int64_t d_v,
+                  int64_t n_pages, int64_t page_tokens, int64_t max_pages, const int64_t* strides,
+                  int dtype, void* stream);
+
+/*
+ * moa_kv4_read -- the rows at given positions, widened: code * s, rounded once to dtype.
+ * Arguments of moa_kv4_write, with K and V written and the pool read.  A negative position gives
+ * zeros; one outside its table (or a page outside the pool) gives NaN and MOA_ERR_DEVICE_INDEX.
+ */
+int moa_kv4_read(void* K, void* V, const void* pool, const int32_t* pages, const int32_t* pos,
+                 int64_t B, int64_t H, int64_t N, int64_t d_k, int64_t d_v, int64_t n_pages,
+                 int64_t page_tokens, int64_t max_pages, const int64_t* strides, int dtype,
+                 void* stream);
+
+/*
+ * moa_kv4_attn -- attention of N query rows of each sequence over its cached tokens.
+ *
+ * Defines: the softmax attention of moa_attn_fwd with keys and values as the cache holds them
+ * (code * s, not rounded to bf16), query head j reading key head j / (H_q / H_k).  lens[b] tokens of
+ * sequence b are cached, the N query rows being the last N of them: row i sees the first
+ * lens[b] - N + i + 1 tokens if `causal`, else all lens[b].  A row that sees no token gives O = 0
+ * and LSE = -infinity; what the pool holds past lens[b] has no influence.
+ *   Q  [B, H_q, N, d_k] input, O  [B, H_q, N, d_v] output;  strides  6 values: Q, O
+ *   LSE    float32 [B, H_q, N] contiguous, or null: ln of the sum of exp of the row's scaled scores
+ *   lens   int32 [B] on the device, 0 <= lens[b] <= max_len
+ *   max_len  what the host knows of the lengths: it decides how the work is divided
+ *            (1 <= max_len <= max_pages * page_tokens, below 2^31 - 64)
+ *   scale  any finite value;  dtype  MOA_BF16 (weights rounded to bf16 once) or MOA_FP32 (every
+ *          product of 24 bits, fp32 accumulation)
+ *   workspace  device, 16-byte aligned, moa_kv4_attn_workspace_bytes(...) bytes (null if that is 0)
+ * H_q a multiple of H_k.  A length outside [0, max_len] is clamped, a page outside the pool counts
+ * as hidden tokens; both record MOA_ERR_DEVICE_INDEX.  Bounded waits as moa_attn_fwd.  Bitwise
+ * reproducible.
+ */
+int moa_kv4_attn(const void* Q, const void* pool, const int32_t* pages, const int32_t* lens, void* O,
+                 float* LSE, int64_t B, int64_t H_q, int64_t H_k, int64_t N, int64_t d_k,
+                 int64_t d_v, int64_t n_pages, int64_t page_tokens, int64_t max_pages,
+                 int64_t max_len, const int64_t* strides, float scale, int causal, int dtype,
+                 void* workspace, size_t workspace_bytes, void* stream);
+
+/* Scratch bytes of moa_kv4_attn on the current device: partial rows of split token ranges (0 when
+ * nothing is split, for invalid sizes or without a device). */
+size_t moa_kv4_attn_workspace_bytes(int64_t B, int64_t H_q, int64_t H_k, int64_t N, int64_t d_k,
+                                    int64_t d_v, int64_t max_len, int dtype);
+
 /*
  * moa_last_error -- human-readable reason for the last non-OK status returned
  * on the calling thread ("" if none).  The string is owned by the library and
@@ -346,6 +481,8 @@ const char* moa_last_error(void);
  * moa_get_device_status -- synchronises `stream`, then returns and clears the
  * device status word that bounded waits write on timeout: MOA_OK if no kernel
  * timed out since the last call, MOA_ERR_DEVICE_TIMEOUT otherwise,
+ * MOA_ERR_DEVICE_INDEX if no wait ran out but a kernel of the operators around
+ * attention met a position, length or page number outside its table,
  * MOA_ERR_CUDA if the synchronisation itself failed.
  */
 int moa_get_device_status(void* stream);

@@ -19,7 +19,12 @@ from ._lib import (MOA_BF16, MOA_FP32, MoaError, check, lib, moa_attn_dnf_bytes,
                    moa_attn_fwd_splitkv, moa_attn_splitkv_workspace_bytes, moa_attn_fwd_lse,
                    moa_attn_bwd, moa_attn_bwd_workspace_bytes, moa_qkv_proj,
                    moa_attn_split_plan, MOA_SPLITS_AUTO, moa_attn_bwd_fused,
-                   moa_attn_bwd_fused_workspace_bytes)
+                   moa_attn_bwd_fused_workspace_bytes, moa_kv4_attn,
+                   moa_kv4_attn_workspace_bytes, moa_kv4_pool_bytes, moa_kv4_read,
+                   moa_kv4_write, moa_qk_norm_rope, moa_qk_norm_rope_bwd,
+                   moa_qk_norm_rope_bwd_workspace_bytes)
+from .ops import (kv4_attn, kv4_attn_lse, kv4_pool, kv4_read, kv4_write, qk_norm_rope,  # noqa: F401
+                  qk_norm_rope_bwd, rope_table)
 
 __all__ = ["attn_fwd", "attn_fwd_staged", "get_device_status", "attn_flops", "dnf_bytes",
            "MOA_FP32", "MOA_BF16", "MoaError", "moa_attn_fwd", "moa_attn_fwd_staged",
@@ -28,7 +33,11 @@ __all__ = ["attn_fwd", "attn_fwd_staged", "get_device_status", "attn_flops", "dn
            "moa_attn_fwd_splitkv", "moa_attn_splitkv_workspace_bytes", "attn_fwd_lse",
            "moa_attn_fwd_lse", "attn_bwd", "moa_attn_bwd", "moa_attn_bwd_workspace_bytes",
            "qkv_proj", "moa_qkv_proj", "moa_attn_split_plan", "MOA_SPLITS_AUTO",
-           "moa_attn_bwd_fused", "moa_attn_bwd_fused_workspace_bytes"]
+           "moa_attn_bwd_fused", "moa_attn_bwd_fused_workspace_bytes", "qk_norm_rope",
+           "qk_norm_rope_bwd", "rope_table", "kv4_pool", "kv4_write", "kv4_read", "kv4_attn",
+           "kv4_attn_lse", "moa_qk_norm_rope", "moa_qk_norm_rope_bwd",
+           "moa_qk_norm_rope_bwd_workspace_bytes", "moa_kv4_pool_bytes", "moa_kv4_write",
+           "moa_kv4_read", "moa_kv4_attn", "moa_kv4_attn_workspace_bytes"]
 
 
 def _dtype_code(t) -> int:

@@ -20,6 +20,7 @@ MOA_ERR_UNSUPPORTED_SHAPE = 3
 MOA_ERR_MISALIGNED = 4
 MOA_ERR_CUDA = 5
 MOA_ERR_DEVICE_TIMEOUT = 6
+MOA_ERR_DEVICE_INDEX = 7
 
 STATUS_NAMES = {
     MOA_OK: "MOA_OK",
@@ -29,6 +30,7 @@ STATUS_NAMES = {
     MOA_ERR_MISALIGNED: "MOA_ERR_MISALIGNED",
     MOA_ERR_CUDA: "MOA_ERR_CUDA",
     MOA_ERR_DEVICE_TIMEOUT: "MOA_ERR_DEVICE_TIMEOUT",
+    MOA_ERR_DEVICE_INDEX: "MOA_ERR_DEVICE_INDEX",
 }
 
 # Every function declared in include/moa_attn.h: name -> (restype, argtypes).
@@ -66,6 +68,18 @@ SIGNATURES = {
                                            ctypes.POINTER(ctypes.c_int),
                                            ctypes.POINTER(ctypes.c_int),
                                            ctypes.POINTER(ctypes.c_int64)]),
+    "moa_qk_norm_rope": (ctypes.c_int, [_VP] * 9 + [_I64] * 7 + [_VP, ctypes.c_float, ctypes.c_int,
+                                                                ctypes.c_int, _VP]),
+    "moa_qk_norm_rope_bwd": (ctypes.c_int, [_VP] * 13 + [_I64] * 7 +
+                             [_VP, ctypes.c_float, ctypes.c_int, ctypes.c_int, _VP,
+                              ctypes.c_size_t, _VP]),
+    "moa_qk_norm_rope_bwd_workspace_bytes": (ctypes.c_size_t, [_I64] * 5),
+    "moa_kv4_pool_bytes": (ctypes.c_size_t, [_I64] * 5),
+    "moa_kv4_write": (ctypes.c_int, [_VP] * 5 + [_I64] * 8 + [_VP, ctypes.c_int, _VP]),
+    "moa_kv4_read": (ctypes.c_int, [_VP] * 5 + [_I64] * 8 + [_VP, ctypes.c_int, _VP]),
+    "moa_kv4_attn": (ctypes.c_int, [_VP] * 6 + [_I64] * 10 +
+                     [_VP, ctypes.c_float, ctypes.c_int, ctypes.c_int, _VP, ctypes.c_size_t, _VP]),
+    "moa_kv4_attn_workspace_bytes": (ctypes.c_size_t, [_I64] * 7 + [ctypes.c_int]),
     "moa_last_error": (ctypes.c_char_p, []),
     "moa_get_device_status": (ctypes.c_int, [_VP]),
     "moa_selftest_wait_timeout": (ctypes.c_int, [ctypes.c_uint64, _VP]),
@@ -174,6 +188,56 @@ def moa_attn_split_plan(B, H, N_q, N_k, num_splits, sm_count) -> tuple[int, int,
     rc = lib().moa_attn_split_plan(B, H, N_q, N_k, num_splits, sm_count, ctypes.byref(s),
                                    ctypes.byref(per), ctypes.byref(whole))
     return rc, s.value, per.value, whole.value
+
+
+def _strides(values):
+    return (ctypes.c_int64 * len(values))(*values)
+
+
+def moa_qk_norm_rope(Q, K, W_q, W_k, cos, sin, pos, Qo, Ko, B, H_q, H_k, N, d, d_rot, n_pos,
+                     strides, eps, interleaved, dtype, stream) -> int:
+    return lib().moa_qk_norm_rope(Q, K, W_q, W_k, cos, sin, pos, Qo, Ko, B, H_q, H_k, N, d, d_rot,
+                                  n_pos, _strides(strides), eps, interleaved, dtype, stream)
+
+
+def moa_qk_norm_rope_bwd(Q, K, W_q, W_k, cos, sin, pos, dQo, dKo, dQ, dK, dW_q, dW_k, B, H_q, H_k,
+                         N, d, d_rot, n_pos, strides, eps, interleaved, dtype, workspace,
+                         workspace_bytes, stream) -> int:
+    return lib().moa_qk_norm_rope_bwd(Q, K, W_q, W_k, cos, sin, pos, dQo, dKo, dQ, dK, dW_q, dW_k,
+                                      B, H_q, H_k, N, d, d_rot, n_pos, _strides(strides), eps,
+                                      interleaved, dtype, workspace, workspace_bytes, stream)
+
+
+def moa_qk_norm_rope_bwd_workspace_bytes(B, H_q, H_k, N, d) -> int:
+    return lib().moa_qk_norm_rope_bwd_workspace_bytes(B, H_q, H_k, N, d)
+
+
+def moa_kv4_pool_bytes(n_pages, H, page_tokens, d_k, d_v) -> int:
+    return lib().moa_kv4_pool_bytes(n_pages, H, page_tokens, d_k, d_v)
+
+
+def moa_kv4_write(K, V, pool, pages, pos, B, H, N, d_k, d_v, n_pages, page_tokens, max_pages,
+                  strides, dtype, stream) -> int:
+    return lib().moa_kv4_write(K, V, pool, pages, pos, B, H, N, d_k, d_v, n_pages, page_tokens,
+                               max_pages, _strides(strides), dtype, stream)
+
+
+def moa_kv4_read(K, V, pool, pages, pos, B, H, N, d_k, d_v, n_pages, page_tokens, max_pages,
+                 strides, dtype, stream) -> int:
+    return lib().moa_kv4_read(K, V, pool, pages, pos, B, H, N, d_k, d_v, n_pages, page_tokens,
+                              max_pages, _strides(strides), dtype, stream)
+
+
+def moa_kv4_attn(Q, pool, pages, lens, O, LSE, B, H_q, H_k, N, d_k, d_v, n_pages, page_tokens,
+                 max_pages, max_len, strides, scale, causal, dtype, workspace, workspace_bytes,
+                 stream) -> int:
+    return lib().moa_kv4_attn(Q, pool, pages, lens, O, LSE, B, H_q, H_k, N, d_k, d_v, n_pages,
+                              page_tokens, max_pages, max_len, _strides(strides), scale, causal,
+                              dtype, workspace, workspace_bytes, stream)
+
+
+def moa_kv4_attn_workspace_bytes(B, H_q, H_k, N, d_k, d_v, max_len, dtype) -> int:
+    return lib().moa_kv4_attn_workspace_bytes(B, H_q, H_k, N, d_k, d_v, max_len, dtype)
 
 
 # MOA_NOALLOC_SCRATCH_BYTES and MOA_SPLITS_AUTO of include/moa_attn.h

@@ -13,6 +13,7 @@
 
 #include "../../include/moa_attn.h"
 #include "internal.h"
+#include "ops_internal.h"
 
 namespace moa {
 
@@ -158,18 +159,34 @@ bool debug_sync() {
   return v;
 }
 
+// Reads and clears the status words of every translation unit (after a synchronisation): MOA_OK,
+// or the error that a kernel recorded (a wait that ran out before an index out of range).
+int read_status(const char* where) {
+  cudaError_t (*const readers[])(unsigned*) = {
+      bf16_read_and_clear_status, bwd_read_and_clear_status,  proj_read_and_clear_status,
+      norm_read_and_clear_status, kv4_read_and_clear_status, kv4_attn_read_and_clear_status};
+  unsigned timeout = 0, index = 0;
+  for (auto read : readers) {
+    unsigned v = 0;
+    const cudaError_t e = read(&v);
+    if (e != cudaSuccess)
+      return fail(MOA_ERR_CUDA, "%s: status word read: %s", where, cudaGetErrorString(e));
+    if (v == unsigned(MOA_ERR_DEVICE_INDEX)) index = v;
+    else if (v != 0) timeout = v;
+  }
+  if (timeout != 0)
+    return fail(MOA_ERR_DEVICE_TIMEOUT, "%s: a kernel wait ran out (status %u)", where, timeout);
+  if (index != 0)
+    return fail(MOA_ERR_DEVICE_INDEX,
+                "%s: a position, length or page number was outside its table", where);
+  return MOA_OK;
+}
+
 int debug_check(void* stream) {
   if (!debug_sync()) return MOA_OK;
   cudaError_t e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return fail(MOA_ERR_CUDA, "debug sync: %s", cudaGetErrorString(e));
-  unsigned v = 0, vb = 0, vp = 0;
-  e = bf16_read_and_clear_status(&v);
-  if (e == cudaSuccess) e = bwd_read_and_clear_status(&vb);
-  if (e == cudaSuccess) e = proj_read_and_clear_status(&vp);
-  if (e != cudaSuccess) return fail(MOA_ERR_CUDA, "debug status read: %s", cudaGetErrorString(e));
-  if ((v | vb | vp) != 0)
-    return fail(MOA_ERR_DEVICE_TIMEOUT, "debug sync: a kernel wait ran out (status %u)", v | vb | vp);
-  return MOA_OK;
+  return read_status("debug sync");
 }
 
 int dispatch(const void* Q, const void* K, const void* V, void* O, int64_t B, int64_t H,
@@ -326,6 +343,17 @@ int bwd_call(const void* Q, const void* K, const void* V, const void* O, const v
 }
 
 }  // namespace
+
+int api_fail(int code, const char* fmt, ...) {
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(t_last_error, sizeof(t_last_error), fmt, ap);
+  va_end(ap);
+  return code;
+}
+void api_clear() { t_last_error[0] = '\0'; }
+int api_debug_check(void* stream) { return debug_check(stream); }
+
 }  // namespace moa
 
 extern "C" {
@@ -605,16 +633,7 @@ int moa_get_device_status(void* stream) {
   cudaError_t e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess)
     return moa::fail(MOA_ERR_CUDA, "stream synchronize: %s", cudaGetErrorString(e));
-  unsigned v = 0, vb = 0, vp = 0;
-  e = moa::bf16_read_and_clear_status(&v);
-  if (e == cudaSuccess) e = moa::bwd_read_and_clear_status(&vb);
-  if (e == cudaSuccess) e = moa::proj_read_and_clear_status(&vp);
-  if (e != cudaSuccess)
-    return moa::fail(MOA_ERR_CUDA, "status word read: %s", cudaGetErrorString(e));
-  v |= vb | vp;
-  if (v != 0)
-    return moa::fail(MOA_ERR_DEVICE_TIMEOUT, "a kernel wait ran out (status %u)", v);
-  return MOA_OK;
+  return moa::read_status("device status");
 }
 
 int moa_selftest_wait_timeout(uint64_t limit_ns, void* stream) {

@@ -1,0 +1,396 @@
+// Per-head RMS norm of queries and keys with the rotation of positions in the same pass, and its
+// gradients, sm_103a.
+//
+// Mathematics, per row x of d features with weight w:  r = (mean x^2 + eps)^(-1/2),  u = w x r,
+// and each pair (a, b) of the first d_rot features turns by its position's angle:
+//     y_a = u_a c - u_b s,   y_b = u_b c + u_a s.
+// Backward, g = dL/dy:  t = R^T g (the same turn by the opposite angle),
+//     dw = sum over rows of t x r,    dx = r (w t - x r * mean(w t x r)).
+// Everything is computed in fp32; outputs are rounded once, the weights' gradients stay fp32.
+//
+// What bounds it: memory.  Every element is read once and written once (backward: x and g read,
+// dx written), with about ten operations for each.
+//
+// Layout of the work: a group of 8, 16 or 32 lanes owns one token and walks over a range of its
+// heads, eight features a lane (one 16-byte load of bf16, two of fp32).  The token's cosines and
+// sines are loaded once and serve all heads of the range.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <cstdio>
+
+#include "internal.h"
+#include "ops_internal.h"
+
+namespace moa {
+
+__device__ unsigned int g_moa_norm_status = 0;
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kV = 8;  // features of a lane
+constexpr unsigned kErrIndex = 7u;  // MOA_ERR_DEVICE_INDEX
+
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, float* x) {
+  const uint4 v = *reinterpret_cast<const uint4*>(p);
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(w[i] << 16);
+    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void load8(const float* p, float* x) {
+  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+  x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+}
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float* x) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    __nv_bfloat162 v = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+    w[i] = *reinterpret_cast<uint32_t*>(&v);
+  }
+  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void store8(float* p, const float* x) {
+  *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+  *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+}
+
+template <int LPR>
+__device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+  for (int o = LPR / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o, LPR);
+  return v;
+}
+
+// One lane's share of a token's rotation: cosine and (signed) sine of its features' pairs.  With
+// neighbouring pairs a lane holds four pairs; with halves its eight features meet the same eight
+// of the lane half a rotation away.
+struct Turn {
+  float c[kV], s[kV];
+};
+
+// Turned features: y = x * c + partner * s, where s carries the sign of the member.
+template <int LPR, bool PAIRS>
+__device__ __forceinline__ void turn(float* x, const Turn& t, int partner) {
+  if constexpr (PAIRS) {
+#pragma unroll
+    for (int i = 0; i < kV; i += 2) {
+      const float a = x[i], b = x[i + 1];
+      x[i] = a * t.c[i] + b * t.s[i];
+      x[i + 1] = b * t.c[i + 1] + a * t.s[i + 1];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kV; ++i) {
+      const float o = __shfl_sync(0xffffffffu, x[i], partner, LPR);
+      x[i] = x[i] * t.c[i] + o * t.s[i];
+    }
+  }
+}
+
+struct Dims {
+  int64_t tokens;    // B * N
+  int64_t N, n_pos;
+  int Hq, Hk, d, d_rot;
+  int hp;            // heads of one range
+  int nq;            // ranges of query heads (the ranges of key heads follow)
+  float eps;
+};
+
+// The rotation of the token's position for this lane.  `dir` +1 forward, -1 backward.
+template <bool PAIRS>
+__device__ __forceinline__ void load_turn(Turn& t, const float* cosines, const float* sines,
+                                          int64_t pos, const Dims& p, int f0, float dir) {
+#pragma unroll
+  for (int i = 0; i < kV; ++i) t.c[i] = 1.f, t.s[i] = 0.f;
+  if (f0 >= p.d_rot) return;
+  const int half = p.d_rot / 2;
+  const float* c = cosines + pos * half;
+  const float* s = sines + pos * half;
+  if constexpr (PAIRS) {
+    const float4 cc = *reinterpret_cast<const float4*>(c + f0 / 2);
+    const float4 ss = *reinterpret_cast<const float4*>(s + f0 / 2);
+    const float cv[4] = {cc.x, cc.y, cc.z, cc.w}, sv[4] = {ss.x, ss.y, ss.z, ss.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      t.c[2 * i] = t.c[2 * i + 1] = cv[i];
+      t.s[2 * i] = -dir * sv[i];
+      t.s[2 * i + 1] = dir * sv[i];
+    }
+  } else {
+    const bool first = f0 < half;
+    const int i0 = first ? f0 : f0 - half;
+    const float sign = first ? -dir : dir;
+    load8(c + i0, t.c);
+    load8(s + i0, t.s);
+#pragma unroll
+    for (int i = 0; i < kV; ++i) t.s[i] *= sign;
+  }
+}
+
+template <typename T, int LPR, bool PAIRS>
+__global__ void __launch_bounds__(kThreads)
+norm_rope_kernel(View q, View k, View oq, View ok, const T* wq, const T* wk, const float* cosines,
+                 const float* sines, const int32_t* pos, Dims p) {
+  constexpr int kGroups = kThreads / LPR;
+  const int lane = threadIdx.x % LPR;
+  const int64_t token = int64_t(blockIdx.x) * kGroups + threadIdx.x / LPR;
+  const bool is_q = int(blockIdx.y) < p.nq;
+  const int range = is_q ? int(blockIdx.y) : int(blockIdx.y) - p.nq;
+  const View in = is_q ? q : k, out = is_q ? oq : ok;
+  const int H = is_q ? p.Hq : p.Hk;
+  const int h0 = range * p.hp, h1 = h0 + p.hp < H ? h0 + p.hp : H;
+  const int f0 = lane * kV;
+  const bool live = token < p.tokens;
+  const bool mine = live && f0 < p.d;
+  const int64_t b = live ? token / p.N : 0, n = live ? token % p.N : 0;
+  const int32_t at = live ? pos[token] : -1;
+  const bool bad = live && at >= p.n_pos;
+  if (bad && lane == 0) atomicExch(&g_moa_norm_status, kErrIndex);
+  Turn t;
+  load_turn<PAIRS>(t, cosines, sines, at >= 0 && !bad ? at : 0, p, f0, 1.f);
+  float w[kV];
+#pragma unroll
+  for (int i = 0; i < kV; ++i) w[i] = 0.f;
+  if (f0 < p.d) load8((is_q ? wq : wk) + f0, w);
+  const int half_lanes = p.d_rot / 2 / kV;
+  const int partner = f0 >= p.d_rot ? lane : (f0 < p.d_rot / 2 ? lane + half_lanes : lane - half_lanes);
+  const T* src = static_cast<const T*>(in.p) + b * in.sb + n * in.sn + f0;
+  T* dst = static_cast<T*>(out.p) + b * out.sb + n * out.sn + f0;
+  const float inv_d = 1.f / float(p.d);
+  for (int h = h0; h < h1; ++h) {
+    float x[kV];
+#pragma unroll
+    for (int i = 0; i < kV; ++i) x[i] = 0.f;
+    if (mine) load8(src + h * in.sh, x);
+    float ss = 0.f;
+#pragma unroll
+    for (int i = 0; i < kV; ++i) ss += x[i] * x[i];
+    const float r = 1.f / sqrtf(group_sum<LPR>(ss) * inv_d + p.eps);
+#pragma unroll
+    for (int i = 0; i < kV; ++i) x[i] = x[i] * r * w[i];
+    turn<LPR, PAIRS>(x, t, partner);
+    if (at < 0 || bad) {
+      const float fill = bad ? __int_as_float(0x7fc00000) : 0.f;
+#pragma unroll
+      for (int i = 0; i < kV; ++i) x[i] = fill;
+    }
+    if (mine) store8(dst + h * out.sh, x);
+  }
+}
+
+// The gradients: one launch for dx and, for each CTA, the sum of its rows' t x r; a second one
+// adds the CTAs' sums in a fixed order.
+template <typename T, int LPR, bool PAIRS>
+__global__ void __launch_bounds__(kThreads)
+norm_rope_bwd_kernel(View q, View k, View gq, View gk, View oq, View ok, const T* wq, const T* wk,
+                     const float* cosines, const float* sines, const int32_t* pos, float* partial,
+                     Dims p) {
+  constexpr int kGroups = kThreads / LPR;
+  __shared__ float sums[kGroups][LPR * kV];
+  const int lane = threadIdx.x % LPR, group = threadIdx.x / LPR;
+  const bool is_q = int(blockIdx.y) < p.nq;
+  const int range = is_q ? int(blockIdx.y) : int(blockIdx.y) - p.nq;
+  const View in = is_q ? q : k, gin = is_q ? gq : gk, out = is_q ? oq : ok;
+  const int H = is_q ? p.Hq : p.Hk;
+  const int h0 = range * p.hp, h1 = h0 + p.hp < H ? h0 + p.hp : H;
+  const int f0 = lane * kV;
+  float w[kV], acc[kV];
+#pragma unroll
+  for (int i = 0; i < kV; ++i) w[i] = acc[i] = 0.f;
+  if (f0 < p.d) load8((is_q ? wq : wk) + f0, w);
+  const int half_lanes = p.d_rot / 2 / kV;
+  const int partner = f0 >= p.d_rot ? lane : (f0 < p.d_rot / 2 ? lane + half_lanes : lane - half_lanes);
+  const float inv_d = 1.f / float(p.d);
+  // every lane of a warp takes part in each turn of the loop (shuffles), whether its token exists
+  for (int64_t base = int64_t(blockIdx.x) * kGroups; base < p.tokens; base += int64_t(gridDim.x) * kGroups) {
+    const int64_t token = base + group;
+    const bool live = token < p.tokens;
+    const bool mine = live && f0 < p.d;
+    const int64_t b = live ? token / p.N : 0, n = live ? token % p.N : 0;
+    const int32_t at = live ? pos[token] : -1;
+    const bool bad = live && at >= p.n_pos;
+    if (bad && lane == 0) atomicExch(&g_moa_norm_status, kErrIndex);
+    const bool counts = mine && at >= 0 && !bad;
+    Turn t;
+    load_turn<PAIRS>(t, cosines, sines, at >= 0 && !bad ? at : 0, p, f0, -1.f);
+    const T* src = static_cast<const T*>(in.p) + b * in.sb + n * in.sn + f0;
+    const T* gsrc = static_cast<const T*>(gin.p) + b * gin.sb + n * gin.sn + f0;
+    T* dst = static_cast<T*>(out.p) + b * out.sb + n * out.sn + f0;
+    for (int h = h0; h < h1; ++h) {
+      float x[kV], g[kV];
+#pragma unroll
+      for (int i = 0; i < kV; ++i) x[i] = g[i] = 0.f;
+      if (mine) {
+        load8(src + h * in.sh, x);
+        load8(gsrc + h * gin.sh, g);
+      }
+      float ss = 0.f;
+#pragma unroll
+      for (int i = 0; i < kV; ++i) ss += x[i] * x[i];
+      const float r = 1.f / sqrtf(group_sum<LPR>(ss) * inv_d + p.eps);
+      turn<LPR, PAIRS>(g, t, partner);
+      float dot = 0.f;
+#pragma unroll
+      for (int i = 0; i < kV; ++i) {
+        x[i] *= r;
+        if (counts) acc[i] += g[i] * x[i];
+        g[i] *= w[i];
+        dot += g[i] * x[i];
+      }
+      const float mean = group_sum<LPR>(dot) * inv_d;
+#pragma unroll
+      for (int i = 0; i < kV; ++i) {
+        x[i] = r * (g[i] - x[i] * mean);
+        if (at < 0 || bad) x[i] = bad ? __int_as_float(0x7fc00000) : 0.f;
+      }
+      if (mine) store8(dst + h * out.sh, x);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kV; ++i) sums[group][f0 + i] = acc[i];
+  __syncthreads();
+  const int64_t row = int64_t(blockIdx.y) * gridDim.x + blockIdx.x;
+  for (int f = threadIdx.x; f < p.d; f += kThreads) {
+    float s = 0.f;
+#pragma unroll 4
+    for (int g = 0; g < kGroups; ++g) s += sums[g][f];
+    partial[row * p.d + f] = s;
+  }
+}
+
+// Sums of partial rows: block (column block, 0 = queries / 1 = keys); warp w adds rows w, w+32, ...
+// of 32 columns, then the warps' sums are added in order.
+__global__ void __launch_bounds__(1024)
+norm_rope_bwd_sum_kernel(const float* partial, float* dwq, float* dwk, int64_t rows_q, int64_t rows,
+                         int d) {
+  __shared__ float sums[32][33];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int f = blockIdx.x * 32 + lane;
+  const int64_t r0 = blockIdx.y == 0 ? 0 : rows_q, r1 = blockIdx.y == 0 ? rows_q : rows;
+  float s = 0.f;
+  if (f < d) {
+#pragma unroll 8
+    for (int64_t r = r0 + warp; r < r1; r += 32) s += partial[r * d + f];
+  }
+  sums[warp][lane] = s;
+  __syncthreads();
+  if (warp == 0 && f < d) {
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) s += sums[i][lane];
+    (blockIdx.y == 0 ? dwq : dwk)[f] = s;
+  }
+}
+
+int lanes_per_row(int64_t d) { return d <= 64 ? 8 : d <= 128 ? 16 : 32; }
+
+// Heads of one range: as many as leave every SM about 2048 threads, eight at most (the token's
+// angles, 64 bytes a lane, are then a quarter of the loads of a bf16 row's lane).
+int heads_per_range(int64_t tokens, int64_t Hq, int64_t Hk, int lpr, int sms) {
+  const int64_t groups = int64_t(sms) * 2048 / lpr;
+  int64_t hp = tokens * (Hq + Hk) / groups;
+  const int64_t most = Hq > Hk ? Hq : Hk;
+  hp = hp < 1 ? 1 : hp > 8 ? 8 : hp;
+  return int(hp < most ? hp : most);
+}
+
+struct Grid {
+  int64_t x;
+  int y, hp, nq;
+};
+Grid plan(int64_t tokens, int64_t Hq, int64_t Hk, int64_t d, int sms, bool bwd) {
+  const int lpr = lanes_per_row(d);
+  Grid g;
+  g.hp = heads_per_range(tokens, Hq, Hk, lpr, sms);
+  g.nq = int((Hq + g.hp - 1) / g.hp);
+  g.y = g.nq + int((Hk + g.hp - 1) / g.hp);
+  const int64_t per = kThreads / lpr;
+  g.x = (tokens + per - 1) / per;
+  if (bwd) {  // each CTA leaves one row of sums: a few waves of CTAs walk over the tokens
+    int64_t most = int64_t(sms) * 16 / g.y;
+    most = most < 1 ? 1 : most;
+    if (g.x > most) g.x = most;
+  }
+  return g;
+}
+
+template <typename T, int LPR, bool PAIRS>
+int run(const NormRopeArgs& a, const Grid& g, const Dims& p, bool bwd, char* msg, size_t msglen) {
+  const T* wq = static_cast<const T*>(a.wq);
+  const T* wk = static_cast<const T*>(a.wk);
+  const dim3 grid{unsigned(g.x), unsigned(g.y), 1};
+  if (!bwd) {
+    norm_rope_kernel<T, LPR, PAIRS><<<grid, kThreads, 0, a.stream>>>(
+        a.q, a.k, a.oq, a.ok, wq, wk, a.cosines, a.sines, a.pos, p);
+  } else {
+    norm_rope_bwd_kernel<T, LPR, PAIRS><<<grid, kThreads, 0, a.stream>>>(
+        a.q, a.k, a.gq, a.gk, a.oq, a.ok, wq, wk, a.cosines, a.sines, a.pos, a.partial, p);
+    norm_rope_bwd_sum_kernel<<<dim3(unsigned((a.d + 31) / 32), 2), 1024, 0, a.stream>>>(
+        a.partial, a.dwq, a.dwk, g.x * g.nq, g.x * g.y, a.d);
+  }
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) {
+    snprintf(msg, msglen, "norm and rotation launch: %s", cudaGetErrorString(e));
+    return 5;
+  }
+  return 0;
+}
+
+template <typename T, int LPR>
+int run_style(const NormRopeArgs& a, const Grid& g, const Dims& p, bool bwd, char* msg, size_t n) {
+  return a.pairs ? run<T, LPR, true>(a, g, p, bwd, msg, n) : run<T, LPR, false>(a, g, p, bwd, msg, n);
+}
+
+template <typename T>
+int run_type(const NormRopeArgs& a, const Grid& g, const Dims& p, bool bwd, char* msg, size_t n) {
+  switch (lanes_per_row(a.d)) {
+    case 8: return run_style<T, 8>(a, g, p, bwd, msg, n);
+    case 16: return run_style<T, 16>(a, g, p, bwd, msg, n);
+    default: return run_style<T, 32>(a, g, p, bwd, msg, n);
+  }
+}
+
+int launch(const NormRopeArgs& a, bool bwd, char* msg, size_t msglen) {
+  int sms = 0;
+  const cudaError_t e = device_sm_count(&sms);
+  if (e != cudaSuccess) {
+    snprintf(msg, msglen, "norm and rotation: SM count: %s", cudaGetErrorString(e));
+    return 5;
+  }
+  const Grid g = plan(a.B * a.N, a.Hq, a.Hk, a.d, sms, bwd);
+  if (g.x > 0x7fffffffLL || g.y > 65535) {
+    snprintf(msg, msglen, "norm and rotation: too many tokens or heads for one launch");
+    return 3;
+  }
+  const Dims p{a.B * a.N, a.N, a.n_pos, int(a.Hq), int(a.Hk), a.d, a.d_rot, g.hp, g.nq, a.eps};
+  return a.f32 ? run_type<float>(a, g, p, bwd, msg, msglen)
+               : run_type<__nv_bfloat16>(a, g, p, bwd, msg, msglen);
+}
+
+}  // namespace
+
+int64_t norm_rope_partial_rows(int64_t B, int64_t Hq, int64_t Hk, int64_t N, int64_t d, int sms) {
+  const Grid g = plan(B * N, Hq, Hk, d, sms, true);
+  return g.x * g.y;
+}
+
+int launch_norm_rope(const NormRopeArgs& a, char* msg, size_t msglen) {
+  return launch(a, false, msg, msglen);
+}
+int launch_norm_rope_bwd(const NormRopeArgs& a, char* msg, size_t msglen) {
+  return launch(a, true, msg, msglen);
+}
+
+cudaError_t norm_read_and_clear_status(unsigned* value) {
+  cudaError_t e = cudaMemcpyFromSymbol(value, g_moa_norm_status, sizeof(unsigned));
+  if (e != cudaSuccess || *value == 0) return e;
+  const unsigned zero = 0;
+  return cudaMemcpyToSymbol(g_moa_norm_status, &zero, sizeof(unsigned));
+}
+
+}  // namespace moa
