@@ -454,7 +454,7 @@ int moa_kv4_read(void* K, void* V, const void* pool, const int32_t* pages, const
  *            (1 <= max_len <= max_pages * page_tokens, below 2^31 - 64)
  *   scale  any finite value;  dtype  MOA_BF16 (weights rounded to bf16 once) or MOA_FP32 (every
  *          product of 24 bits, fp32 accumulation)
- *   workspace  device, 16-byte aligned, moa_kv4_attn_workspace_bytes(...) bytes (null if that is 0)
+ *   workspace  device, 16-byte aligned, moa_kv4_attn_workspace_bytes(...) bytes
  * H_q a multiple of H_k.  A length outside [0, max_len] is clamped, a page outside the pool counts
  * as hidden tokens; both record MOA_ERR_DEVICE_INDEX.  Bounded waits as moa_attn_fwd.  Bitwise
  * reproducible.
@@ -465,8 +465,8 @@ int moa_kv4_attn(const void* Q, const void* pool, const int32_t* pages, const in
                  int64_t max_len, const int64_t* strides, float scale, int causal, int dtype,
                  void* workspace, size_t workspace_bytes, void* stream);
 
-/* Scratch bytes of moa_kv4_attn on the current device: partial rows of split token ranges (0 when
- * nothing is split, for invalid sizes or without a device). */
+/* Scratch bytes of moa_kv4_attn on the current device: the pieces of rows whose tokens several CTAs
+ * share (0 for invalid sizes or without a device). */
 size_t moa_kv4_attn_workspace_bytes(int64_t B, int64_t H_q, int64_t H_k, int64_t N, int64_t d_k,
                                     int64_t d_v, int64_t max_len, int dtype);
 

@@ -11,7 +11,7 @@
 // joined by o = sum_s e^(m_s - M) o_s / sum_s e^(m_s - M) l_s.
 //
 // Rounding: bf16 queries enter exactly; the weights p sv are rounded to bf16 once (relative
-// 2^-9, as in the other bf16 forward).  fp32 queries and weights enter as three bf16 terms each
+// 2^-8, as in the other bf16 forward).  fp32 queries and weights enter as three bf16 terms each
 // (24 bits), so the fp32 form is fp32-accurate on the same instructions.  Scores, maxima, sums
 // and outputs accumulate in fp32.
 //
@@ -20,13 +20,18 @@
 // mma.m16n8k16 and queries on its 8 columns: a decoding step has few queries, and the other way
 // round half of the tensor work would be padding.
 //
-// Layout of the work: a CTA owns up to 8 NT query rows of one key head and a range of 16-token
-// blocks; its four warps take turns at tiles of SUB blocks, each with its own ring of bulk copies,
-// running maximum, sum and output, joined through shared memory at the end.
+// Layout of the work: a work item is a tile of up to 8 NT query rows of one key head of one
+// sequence; its visible tokens count in units of 64.  The units of all items, in a row, are cut into
+// equal shares, one for each resident CTA, so uneven lengths leave no SM idle; a CTA walks over the
+// items of its share.  An item inside one share is written at once; the pieces of a cut item go to
+// the workspace and a second kernel joins them.  Within a CTA four warps take turns at tiles of
+// kSub blocks, each with its own ring of bulk copies, running maximum, sum and output, joined
+// through shared memory at the end of the item.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
 #include <cstdio>
+#include <type_traits>
 
 #include "internal.h"
 #include "kv4.cuh"
@@ -63,13 +68,19 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t a) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
   return d;
 }
-// Four pairs of codes of a word as bf16 pairs of integers -8 .. 7: 0x4300 | n is 128 + n.
+// Four pairs of codes of a word as bf16 pairs of code / 64.  The bits 0 .. 255 of a bf16 are the
+// numbers 0 .. 255 times 2^-133 (subnormals and the first binade share their spacing), so a nibble
+// n = code + 8 masked out at bits 0-3 is n 2^-133 and at bits 4-7 is n 2^-129: one fused multiply-add
+// makes (n - 8) / 64 of either, exactly, and half of the nibbles need no shift.
+constexpr float kCodeUnit = 64.f;
 __device__ __forceinline__ void widen(uint32_t w, uint32_t* r) {
-  const __nv_bfloat162 bias = __halves2bfloat162(__ushort_as_bfloat16(0x4308), __ushort_as_bfloat16(0x4308));
+  const __nv_bfloat162 low = __halves2bfloat162(__ushort_as_bfloat16(0x7f00), __ushort_as_bfloat16(0x7f00));    // 2^127
+  const __nv_bfloat162 high = __halves2bfloat162(__ushort_as_bfloat16(0x7d00), __ushort_as_bfloat16(0x7d00));   // 2^123
+  const __nv_bfloat162 bias = __halves2bfloat162(__ushort_as_bfloat16(0xbe00), __ushort_as_bfloat16(0xbe00));   // -1/8
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    uint32_t x = ((w >> (4 * j)) & 0x000f000fu) | 0x43004300u;
-    const __nv_bfloat162 y = __hsub2(*reinterpret_cast<__nv_bfloat162*>(&x), bias);
+    const uint32_t x = (j < 2 ? w : w >> 8) & (j % 2 ? 0x00f000f0u : 0x000f000fu);
+    const __nv_bfloat162 y = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&x), j % 2 ? high : low, bias);
     r[j] = *reinterpret_cast<const uint32_t*>(&y);
   }
 }
@@ -111,34 +122,50 @@ __device__ __forceinline__ void split_pair(float x, float y, uint32_t* t) {
   }
 }
 
+constexpr int kUnit = 64;              // tokens of a unit of work
+constexpr int kUnitBlocks = kUnit / kBlock;
+constexpr float kSlack = 8.f;          // the running maximum may lag by this (log2): weights up to 2^8
+
 struct Params {
   int64_t q_sb, q_sh, q_sn, o_sb, o_sh, o_sn;
   int64_t n_pages, max_pages;
-  int64_t N, max_len;
+  int64_t N;
+  int max_len;
+  int n_tiles, n_pairs;                // query tiles of a key head; B * n_tiles
   int Hk, G, blocks_per_page;
-  int n_splits, chunk_blocks;
-  int64_t n_tiles;
   float scale;
   bool causal;
   uint64_t wait_limit_ns;
 };
 
+// One cut item for the joining kernel: written by the CTA that has its first piece.
+struct Cut {
+  int pair, h;
+  int pieces;   // 0: this CTA begins no cut item
+  int unused;
+};
+
 template <int DK, int DV, int NT, int TERMS>
 struct Cfg {
-  static constexpr int kSub = NT == 1 ? 4 : NT == 2 ? 2 : 1;  // 16-token blocks of a tile
+  static constexpr int kSub = NT == 4 ? 1 : 2;                  // 16-token blocks of a tile
   static constexpr int kBytes = block_bytes(DK, DV);
-  static constexpr int kStages = 12 / kSub;
+  static constexpr int kStages = (NT * TERMS == 1 ? 13824 : 18432) / (kSub * kBytes);
+  static constexpr int kBatch = 32 / kSub;                      // tiles whose places are looked up at once
   static constexpr int kRing = kSub * kStages * kBytes;         // one warp's ring
   static constexpr int kOStride = DV + 4;                       // padded row of the final join
   static constexpr int kJoin = kWarps * 8 * NT * (kOStride + 2) * 4;
   static constexpr int kData = kWarps * kRing > kJoin ? kWarps * kRing : kJoin;
+  static constexpr bool kQRegs = NT * TERMS == 1;               // queries in registers
   // queries in the order of the matrix operands: [nt][term][group][lane] 16 bytes
-  static constexpr int kQ = NT * TERMS * (DK / 32) * 32 * 16;
+  static constexpr int kQ = kQRegs ? 0 : NT * TERMS * (DK / 32) * 32 * 16;
   static constexpr int kOffQ = kData;
   static constexpr int kOffBar = kOffQ + kQ;
   static constexpr int kOffMisc = kOffBar + kWarps * kStages * 8;
-  static constexpr int kSmem = kOffMisc + 16;
+  static constexpr int kSmem = kOffMisc + 64;
+  // resident CTAs: registers (128 or 255 a thread) and 228 KB of shared memory
+  static constexpr int kCtas = NT * TERMS == 1 ? 4 : 2;
   static_assert(kBytes % 16 == 0, "bulk copies are whole 16-byte units");
+  static_assert(kCtas * (kSmem + 1024) <= 233472, "shared memory of the resident CTAs");
 };
 
 template <typename T>
@@ -151,46 +178,71 @@ template <>
 __device__ __forceinline__ void store4(__nv_bfloat16* p, const float* x) {
   *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
 }
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, float* x) {
+  const uint4 v = *reinterpret_cast<const uint4*>(p);
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(w[i] << 16);
+    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void load8(const float* p, float* x) {
+  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+  x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+}
+
+// The cached tokens of sequence b, its length clamped to what the call allows.
+__device__ __forceinline__ int length_of(const int32_t* lens, int64_t b, const Params& p, bool report) {
+  const int len = lens[b];
+  if (len >= 0 && len <= p.max_len) return len;
+  if (report) atomicExch(&g_moa_kv4_attn_status, kErrIndex);
+  return len < 0 ? 0 : p.max_len;
+}
+// Tokens that row r of a sequence of `len` tokens sees.
+__device__ __forceinline__ int limit_of(int len, int r, const Params& p) {
+  if (!p.causal) return len;
+  const int n = len - int(p.N) + int(unsigned(r) / unsigned(p.G)) + 1;
+  return n < 0 ? 0 : n;
+}
+__device__ __forceinline__ int sequence_of(int pair, const Params& p) {
+  return p.n_tiles == 1 ? pair : int(unsigned(pair) / unsigned(p.n_tiles));
+}
+// Units of an item of a pair (sequence, query tile): at least one, so that every item is written.
+template <int NT>
+__device__ __forceinline__ int units_of(const int32_t* lens, int pair, const Params& p, bool report) {
+  const int rows = int(p.N) * p.G, b = sequence_of(pair, p);
+  const int last = (pair - b * p.n_tiles + 1) * (8 * NT) - 1;
+  const int n = limit_of(length_of(lens, b, p, report), last < rows ? last : rows - 1, p);
+  return n <= kUnit ? 1 : (n + kUnit - 1) / kUnit;
+}
+
+// Equal shares of `total` units: share c begins at start(c).
+struct Shares {
+  int64_t each;
+  uint32_t rest, n;
+  __device__ __forceinline__ Shares(int64_t total, uint32_t ctas) {
+    n = total < ctas ? uint32_t(total) : ctas;   // none without a unit
+    each = total < 0x7fffffff ? int64_t(uint32_t(total) / n) : total / n;
+    rest = uint32_t(total - each * n);
+  }
+  __device__ __forceinline__ int64_t start(uint32_t c) const { return each * c + rest * c / n; }
+};
 
 template <typename T, int DK, int DV, int NT, int TERMS>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, Cfg<DK, DV, NT, TERMS>::kCtas)
 kv4_attn_kernel(const T* __restrict__ Q, const uint8_t* __restrict__ pool,
                 const int32_t* __restrict__ table, const int32_t* __restrict__ lens,
                 T* __restrict__ O, float* __restrict__ lse, float* __restrict__ part_o,
-                float* __restrict__ part_ml, Params p) {
+                float* __restrict__ part_ml, Cut* __restrict__ cuts, Params p) {
   using C = Cfg<DK, DV, NT, TERMS>;
   constexpr int GK = DK / 32, GV = DV / 32;
   extern __shared__ __align__(128) uint8_t smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = lane >> 2, t = lane & 3;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::kOffMisc);
+  int64_t* scan = reinterpret_cast<int64_t*>(smem + C::kOffMisc + 8);   // [kWarps], then a pair found
   const WaitCtl wc{abort_flag, p.wait_limit_ns, 0u, &g_moa_kv4_attn_status};
-
-  const int split = int(blockIdx.x % unsigned(p.n_splits));
-  const int64_t item = blockIdx.x / unsigned(p.n_splits);
-  const int64_t tile = item % p.n_tiles;
-  const int h = int(item / p.n_tiles % p.Hk);
-  const int64_t b = item / p.n_tiles / p.Hk;
-  const int64_t rows = p.N * p.G;
-  const int64_t r0 = tile * (8 * NT);
-
-  // tokens that the tile's rows may see
-  int64_t len = lens[b];
-  if (len < 0 || len > p.max_len) {
-    if (threadIdx.x == 0) atomicExch(&g_moa_kv4_attn_status, kErrIndex);
-    len = len < 0 ? 0 : p.max_len;
-  }
-  auto limit = [&](int64_t r) -> int64_t {  // visible tokens of row r
-    if (!p.causal) return len;
-    const int64_t n = len - p.N + r / p.G + 1;
-    return n < 0 ? 0 : n;
-  };
-  const int64_t last_row = r0 + 8 * NT < rows ? r0 + 8 * NT - 1 : rows - 1;
-  const int all_limit = int(limit(r0));          // every row sees these
-  const int any_limit = int(limit(last_row));    // no row sees more
-  const int n_blocks = (any_limit + kBlock - 1) / kBlock;
-  const int first = split * p.chunk_blocks;
-  const int end = first + p.chunk_blocks < n_blocks ? first + p.chunk_blocks : n_blocks;
 
   uint8_t* ring = smem + warp * C::kRing;
   const uint32_t ring_s = smem_u32(ring);
@@ -200,177 +252,253 @@ kv4_attn_kernel(const T* __restrict__ Q, const uint8_t* __restrict__ pool,
     fence_barrier_init();
   }
   if (threadIdx.x == 0) *abort_flag = 0;
-  // queries -> shared memory, split into their terms, in operand order
-  for (int i = threadIdx.x; i < NT * GK * 32; i += kThreads) {
-    const int ln = i & 31, gi = (i >> 5) % GK, nt = (i >> 5) / GK;
-    const int64_t r = r0 + nt * 8 + (ln >> 2);
-    float x[8];
+  wait_for_previous();
+
+  // this CTA's share of all units, and the pair in which it begins
+  int64_t sum = 0;
+  for (int i = threadIdx.x; i < p.n_pairs; i += kThreads) sum += units_of<NT>(lens, i, p, true);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = 0.f;
-    if (r < rows) {
-      const T* src = Q + b * p.q_sb + (int64_t(h) * p.G + r % p.G) * p.q_sh + (r / p.G) * p.q_sn +
-                     32 * gi + 8 * (ln & 3);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = float(src[e]);
-    }
-    uint32_t w[4][TERMS];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) split_pair<TERMS>(x[2 * e], x[2 * e + 1], w[e]);
-#pragma unroll
-    for (int k = 0; k < TERMS; ++k)
-      *reinterpret_cast<uint4*>(smem + C::kOffQ + (((nt * TERMS + k) * GK + gi) * 32 + ln) * 16) =
-          make_uint4(w[0][k], w[1][k], w[2][k], w[3][k]);
-  }
+  for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+  if (lane == 0) scan[warp] = sum;
   __syncthreads();
-
-  float o[NT][DV / 16][4];
-  float m[NT][2], l[NT][2];
+  int64_t total = 0;
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    m[n][0] = m[n][1] = -INFINITY;
-    l[n][0] = l[n][1] = 0.f;
+  for (int w = 0; w < kWarps; ++w) total += scan[w];
+  total *= p.Hk;
+  const Shares shares(total, gridDim.x);
+  int64_t at = blockIdx.x < shares.n ? shares.start(blockIdx.x) : total;
+  const int64_t stop = blockIdx.x < shares.n ? shares.start(blockIdx.x + 1) : total;
+  int pair = 0;
+  int64_t before = 0;   // the pair of unit `at`, the units of all heads in the pairs before it
+  int64_t done = 0;
+  for (int base = 0; p.n_pairs > 1 && at < stop; base += kThreads) {
+    const int i = base + threadIdx.x;
+    const int64_t mine = i < p.n_pairs ? int64_t(units_of<NT>(lens, i, p, false)) * p.Hk : 0;
+    int64_t incl = mine;
 #pragma unroll
-    for (int i = 0; i < DV / 16; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.f;
+    for (int d = 1; d < 32; d <<= 1) {
+      const int64_t o = __shfl_up_sync(0xffffffffu, incl, d);
+      if (lane >= d) incl += o;
+    }
+    __syncthreads();
+    if (lane == 31) scan[warp] = incl;
+    __syncthreads();
+    int64_t all = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      if (w < warp) incl += scan[w];
+      all += scan[w];
+    }
+    incl += done;
+    done += all;
+    __syncthreads();
+    if (at >= incl - mine && at < incl) {
+      scan[0] = i;
+      scan[1] = incl - mine;
+    }
+    if (at < done) {
+      __syncthreads();
+      pair = int(scan[0]);
+      before = scan[1];
+      break;
+    }
   }
-  int lim[NT][2];
-#pragma unroll
-  for (int n = 0; n < NT; ++n)
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const int64_t r = r0 + n * 8 + 2 * t + c;
-      lim[n][c] = r < rows ? int(limit(r)) : any_limit;
-    }
 
-  const int n_mine = end - first;                       // blocks of this CTA's range
-  const int n_tiles = n_mine <= 0 ? 0 : (n_mine + C::kSub - 1) / C::kSub;
-  const float c2 = p.scale * kLog2e;
-  const int32_t* pages = table + b * p.max_pages;
-  // The page of block `lane` (< kSub) of this warp's tile number `it` (0, 1, ...), -1 if none.
-  auto page_of = [&](int it) -> int {
-    const int blk = first + (warp + it * kWarps) * C::kSub + lane;
-    if (lane >= C::kSub || blk >= end) return -2;
-    const int pg = pages[blk / p.blocks_per_page];
-    if (pg < 0 || pg >= p.n_pages) {
-      atomicExch(&g_moa_kv4_attn_status, kErrIndex);
-      return -1;
-    }
-    return pg;
-  };
-  // Starts the copies of tile `it` into its stage; returns the blocks copied, one bit each.
-  auto issue = [&](int it, int pg) -> uint32_t {
-    const uint32_t got = __ballot_sync(0xffffffffu, pg >= 0);
-    const int s = it % C::kStages;
-    if (lane == 0) mbar_arrive_expect_tx(bars + 8 * s, __popc(got) * C::kBytes);
-    __syncwarp();
-    if (pg >= 0) {
-      const int blk = first + (warp + it * kWarps) * C::kSub + lane;
-      const int64_t at = (int64_t(pg) * p.Hk + h) * p.blocks_per_page + blk % p.blocks_per_page;
-      bulk_load(ring_s + (s * C::kSub + lane) * C::kBytes, pool + at * C::kBytes, C::kBytes, bars + 8 * s);
-    }
-    return got;
-  };
-  const int my_tiles = n_tiles > warp ? (n_tiles - warp + kWarps - 1) / kWarps : 0;
-  uint64_t present = 0;  // copied blocks of the tiles in flight, kSub bits a stage
-  int issued = 0;
-  for (; issued < my_tiles && issued < C::kStages; ++issued)
-    present |= uint64_t(issue(issued, page_of(issued))) << (issued * C::kSub);
-  int next_page = issued < my_tiles ? page_of(issued) : -2;
-
+  if (threadIdx.x == 0) cuts[blockIdx.x].pieces = 0;
+  const float c2 = fabsf(p.scale) * kLog2e * kCodeUnit, slack = c2 > 0.f ? kSlack / c2 : INFINITY;
+  const int rows = int(p.N) * p.G;
+  uint32_t count = 0;     // tiles this warp has taken so far: its place in the ring and the phases
   bool ok = true;
-  for (int it = 0; it < my_tiles; ++it) {
-    const int s = it % C::kStages;
-    ok = wait_bounded(bars + 8 * s, uint32_t(it / C::kStages) & 1u, wc);
-    ok = __all_sync(0xffffffffu, ok);
-    if (!ok) break;
-    const uint8_t* st = ring + s * C::kSub * C::kBytes;
-    const int tok0 = (first + (warp + it * kWarps) * C::kSub) * kBlock;
-    const uint32_t got = uint32_t(present >> (s * C::kSub)) & ((1u << C::kSub) - 1);
-    const bool plain = got == (1u << C::kSub) - 1 && tok0 + C::kSub * kBlock <= all_limit;
+  while (at < stop) {
+    // the item and this CTA's units of it
+    const int units = units_of<NT>(lens, pair, p, false);
+    const uint32_t local = uint32_t(at - before);
+    const int h = int(local / uint32_t(units));
+    const int u0 = int(local - uint32_t(h * units));
+    const int u1 = int(units - u0 < stop - at ? units : u0 + (stop - at));
+    const int64_t b = sequence_of(pair, p);
+    const int r0 = (pair - int(b) * p.n_tiles) * (8 * NT);
+    const int len = length_of(lens, b, p, false);
+    const int last_row = r0 + 8 * NT < rows ? r0 + 8 * NT - 1 : rows - 1;
+    const int all_limit = limit_of(len, r0, p);          // every row sees these
+    const int any_limit = limit_of(len, last_row, p);    // no row sees more
+    const int n_blocks = (any_limit + kBlock - 1) / kBlock;
+    const int first = u0 * kUnitBlocks;
+    const int end = u1 * kUnitBlocks < n_blocks ? u1 * kUnitBlocks : n_blocks;
 
-    // scores of the tile, in log2 units: sc[sub][nt]: (token g, rows 2t, 2t+1), (token g+8, ...)
-    float sc[C::kSub][NT][4];
-#pragma unroll
-    for (int sub = 0; sub < C::kSub; ++sub) {
-      const uint8_t* blk = st + sub * C::kBytes;
-      uint32_t kw[2][GK];
-      float ks[2][GK];
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        load_words<GK>(kw[r], blk + ((g + 8 * r) * 4 + t) * GK * 4);
-        load_scales<GK>(ks[r], blk + key_scales(DK, DV) + (g + 8 * r) * GK * 2);
+    // This warp's tiles: kSub blocks each, every kWarps-th one.  Places are looked up for kBatch
+    // tiles at once: lane i finds where block i of the batch lies, and starts its copy when the
+    // turn of its tile comes.
+    const int n_tiles = end <= first ? 0 : (end - first + C::kSub - 1) / C::kSub;
+    const int my_tiles = ok && n_tiles > warp ? (n_tiles - warp + kWarps - 1) / kWarps : 0;
+    const int32_t* pages = table + b * p.max_pages;
+    const uint8_t* src = nullptr;      // this lane's block of the batch being started
+    uint32_t dst = 0, bar = 0, here = 0, here_next = 0;   // blocks that are there: batch in use, batch started
+    auto look_up = [&](int batch) {
+      const int i = batch * C::kBatch + lane / C::kSub;
+      const int blk = first + (warp + i * kWarps) * C::kSub + lane % C::kSub;
+      src = nullptr;
+      if (blk < end) {
+        const int slot = blk / p.blocks_per_page;
+        const int pg = pages[slot];
+        if (pg >= 0 && pg < p.n_pages)
+          src = pool + ((int64_t(pg) * p.Hk + h) * p.blocks_per_page + (blk - slot * p.blocks_per_page)) * C::kBytes;
+        else
+          atomicExch(&g_moa_kv4_attn_status, kErrIndex);
       }
+      const uint32_t st = (count + i) % C::kStages;
+      dst = ring_s + (st * C::kSub + lane % C::kSub) * C::kBytes;
+      bar = bars + 8 * st;
+      here_next = __ballot_sync(0xffffffffu, src != nullptr);
+    };
+    constexpr uint32_t kTileBits = (1u << C::kSub) - 1;
+    auto start = [&](int it) {         // starts the copies of tile `it`, of the batch looked up last
+      const int j = it % C::kBatch;
+      const uint32_t bytes = __popc(here_next >> (j * C::kSub) & kTileBits) * C::kBytes;
+      if (lane == j * C::kSub) mbar_arrive_expect_tx(bar, bytes);
+      __syncwarp();
+      if (lane / C::kSub == j && src != nullptr) bulk_load(dst, src, C::kBytes, bar);
+    };
+    int issued = 0;
+    if (my_tiles > 0) {
+      look_up(0);
+      here = here_next;
+      for (; issued < my_tiles && issued < C::kStages; ++issued) start(issued);
+      static_assert(C::kStages <= C::kBatch, "the first tiles are of one batch");
+    }
+
+    // queries: registers or shared memory, in operand order; a negative scale turns their signs
+    uint4 qreg[C::kQRegs ? GK : 1];
+    {
+      const uint32_t sign = p.scale < 0.f ? 0x80008000u : 0u;
+      for (int i = C::kQRegs ? warp * GK * 32 + lane : threadIdx.x; i < (C::kQRegs ? (warp + 1) * GK : NT * GK) * 32;
+           i += C::kQRegs ? 32 : kThreads) {
+        const int gi = (i >> 5) % GK, nt = C::kQRegs ? 0 : (i >> 5) / GK;
+        const int r = r0 + nt * 8 + g, i_n = int(unsigned(r) / unsigned(p.G));
+        float x[8];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) sc[sub][n][0] = sc[sub][n][1] = sc[sub][n][2] = sc[sub][n][3] = 0.f;
+        for (int e = 0; e < 8; ++e) x[e] = 0.f;
+        if (r < rows)
+          load8(Q + b * p.q_sb + (int64_t(h) * p.G + r - i_n * p.G) * p.q_sh + i_n * p.q_sn + 32 * gi + 8 * t, x);
+        uint32_t w[4][TERMS];
 #pragma unroll
-      for (int gi = 0; gi < GK; ++gi) {
-        uint32_t lo[4], hi[4];
-        widen(kw[0][gi], lo);
-        widen(kw[1][gi], hi);
-        const uint32_t a0[4] = {lo[0], hi[0], lo[1], hi[1]}, a1[4] = {lo[2], hi[2], lo[3], hi[3]};
+        for (int e = 0; e < 4; ++e) {
+          split_pair<TERMS>(x[2 * e], x[2 * e + 1], w[e]);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          float acc[4] = {0.f, 0.f, 0.f, 0.f};
+          for (int k = 0; k < TERMS; ++k) w[e][k] ^= sign;
+        }
+        if constexpr (C::kQRegs) {
 #pragma unroll
-          for (int k = 0; k < TERMS; ++k) {
-            const uint4 q = *reinterpret_cast<const uint4*>(
-                smem + C::kOffQ + (((n * TERMS + k) * GK + gi) * 32 + lane) * 16);
-            mma_16816(acc, a0, q.x, q.y);
-            mma_16816(acc, a1, q.z, q.w);
-          }
-          sc[sub][n][0] += ks[0][gi] * acc[0];
-          sc[sub][n][1] += ks[0][gi] * acc[1];
-          sc[sub][n][2] += ks[1][gi] * acc[2];
-          sc[sub][n][3] += ks[1][gi] * acc[3];
+          for (int j = 0; j < GK; ++j)
+            if (j == gi) qreg[j] = make_uint4(w[0][0], w[1][0], w[2][0], w[3][0]);
+        } else {
+#pragma unroll
+          for (int k = 0; k < TERMS; ++k)
+            *reinterpret_cast<uint4*>(smem + C::kOffQ + (((nt * TERMS + k) * GK + gi) * 32 + lane) * 16) =
+                make_uint4(w[0][k], w[1][k], w[2][k], w[3][k]);
         }
       }
+      if constexpr (!C::kQRegs) __syncthreads();
+    }
+
+    float o[NT][DV / 16][4];
+    // maximum, sum, where the maximum has to move, and what weights subtract: -m c2
+    float m[NT][2], l[NT][2], above[NT][2], mb[NT][2];
+    int lim[NT][2];
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+    for (int n = 0; n < NT; ++n) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sc[sub][n][e] *= c2;
-      if (!plain) {
-        const int tok = tok0 + sub * kBlock + g;
-        const bool here = (got >> sub) & 1u;
+      for (int c = 0; c < 2; ++c) {
+        m[n][c] = above[n][c] = -INFINITY;
+        l[n][c] = mb[n][c] = 0.f;
+        const int r = r0 + n * 8 + 2 * t + c;
+        lim[n][c] = r < rows ? limit_of(len, r, p) : any_limit;
+      }
+#pragma unroll
+      for (int i = 0; i < DV / 16; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.f;
+    }
+
+    // One block of 16 tokens.  PLAIN: it is there and every row sees every token of it.
+    auto block = [&](auto plain_tag, const uint8_t* blk, int tok0, bool there) {
+      constexpr bool PLAIN = decltype(plain_tag)::value;
+      // scores: sc[nt]: (token g, rows 2t, 2t+1), (token g+8, ...)
+      float sc[NT][4];
+      {
+        uint32_t kw[2][GK];
+        float ks[2][GK];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          load_words<GK>(kw[r], blk + ((g + 8 * r) * 4 + t) * GK * 4);
+          load_scales<GK>(ks[r], blk + key_scales(DK, DV) + (g + 8 * r) * GK * 2);
+        }
+#pragma unroll
+        for (int gi = 0; gi < GK; ++gi) {
+          uint32_t lo[4], hi[4];
+          widen(kw[0][gi], lo);
+          widen(kw[1][gi], hi);
+          const uint32_t a0[4] = {lo[0], hi[0], lo[1], hi[1]}, a1[4] = {lo[2], hi[2], lo[3], hi[3]};
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < TERMS; ++k) {
+              uint4 q;
+              if constexpr (C::kQRegs) q = qreg[gi];
+              else q = *reinterpret_cast<const uint4*>(smem + C::kOffQ + (((n * TERMS + k) * GK + gi) * 32 + lane) * 16);
+              mma_16816(acc, a0, q.x, q.y);
+              mma_16816(acc, a1, q.z, q.w);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              sc[n][e] = gi == 0 ? ks[e >> 1][gi] * acc[e] : fmaf(ks[e >> 1][gi], acc[e], sc[n][e]);
+          }
+        }
+      }
+      if constexpr (!PLAIN) {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (!here || tok + (e >> 1) * 8 >= lim[n][e & 1]) sc[sub][n][e] = -INFINITY;
+            if (!there || tok0 + g + (e >> 1) * 8 >= lim[n][e & 1]) sc[n][e] = -INFINITY;
       }
-    }
-    // running maximum and sum
+      // The maximum moves only when a score passes it by more than kSlack (in log2): until then
+      // the weights stay below 2^kSlack and nothing is rescaled.
+      bool moves = false;
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        float x = -INFINITY;
+        for (int c = 0; c < 2; ++c) moves |= fmaxf(sc[n][c], sc[n][2 + c]) > above[n][c];
+      if (__any_sync(0xffffffffu, moves)) {
 #pragma unroll
-        for (int sub = 0; sub < C::kSub; ++sub) x = fmaxf(x, fmaxf(sc[sub][n][c], sc[sub][n][2 + c]));
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
-        const float mn = fmaxf(m[n][c], x);
-        const float base = mn == -INFINITY ? 0.f : mn;  // no visible token yet: weights stay 0
-        const float alpha = ex2_approx(m[n][c] - base);
-        m[n][c] = mn;
-        float sum = 0.f;
+          for (int c = 0; c < 2; ++c) {
+            float x = fmaxf(sc[n][c], sc[n][2 + c]);
 #pragma unroll
-        for (int sub = 0; sub < C::kSub; ++sub)
+            for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
+            const float mn = fmaxf(m[n][c], x);
+            const float alpha = m[n][c] == -INFINITY ? 0.f : ex2_approx((m[n][c] - mn) * c2);
+            m[n][c] = mn;
+            above[n][c] = mn == -INFINITY ? -INFINITY : mn + slack;
+            mb[n][c] = mn == -INFINITY ? 0.f : -mn * c2;
+            l[n][c] *= alpha;
 #pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            const float e = ex2_approx(sc[sub][n][2 * r + c] - base);
-            sc[sub][n][2 * r + c] = e;
-            sum += e;
+            for (int i = 0; i < DV / 16; ++i) {
+              o[n][i][c] *= alpha;
+              o[n][i][2 + c] *= alpha;
+            }
           }
-        l[n][c] = l[n][c] * alpha + sum;
-#pragma unroll
-        for (int i = 0; i < DV / 16; ++i) {
-          o[n][i][c] *= alpha;
-          o[n][i][2 + c] *= alpha;
-        }
       }
-    // o += (p sv) codes
 #pragma unroll
-    for (int sub = 0; sub < C::kSub; ++sub) {
-      const uint8_t* blk = st + sub * C::kBytes;
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float w = ex2_approx(fmaf(sc[n][e], c2, mb[n][e & 1]));
+          if (!PLAIN && sc[n][e] == -INFINITY) w = 0.f;
+          sc[n][e] = w;
+          l[n][e & 1] += w;
+        }
+      // o += (p sv) codes
       uint32_t vw[2][GV];
       float vs[2][GV];
 #pragma unroll
@@ -389,9 +517,9 @@ kv4_attn_kernel(const T* __restrict__ Q, const uint8_t* __restrict__ pool,
           float w[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            w[e] = sc[sub][n][e] * vs[e >> 1][gi];
+            w[e] = sc[n][e] * vs[e >> 1][gi];
             // a hidden token's scale may be anything: its weight is zero whatever that is
-            if (!plain && sc[sub][n][e] == 0.f) w[e] = 0.f;
+            if (!PLAIN && sc[n][e] == 0.f) w[e] = 0.f;
           }
           uint32_t p0[TERMS], p1[TERMS];
           split_pair<TERMS>(w[0], w[1], p0);
@@ -404,121 +532,195 @@ kv4_attn_kernel(const T* __restrict__ Q, const uint8_t* __restrict__ pool,
           }
         }
       }
-    }
-    // the stage is free again: start its next tile
-    __syncwarp();
-    if (issued < my_tiles) {
-      const uint64_t bits = ((uint64_t(1) << C::kSub) - 1) << (s * C::kSub);
-      present = (present & ~bits) | (uint64_t(issue(issued, next_page)) << (s * C::kSub));
-      ++issued;
-      next_page = issued < my_tiles ? page_of(issued) : -2;
-    }
-  }
-  if (!ok) {  // a wait ran out: let the copies in flight land before the memory is reused
-    for (int s = 0; s < C::kStages; ++s) {
-      const int it = issued - 1 - ((issued - 1 - s) % C::kStages + C::kStages) % C::kStages;
-      if (it >= 0) wait_quiesce(bars + 8 * s, uint32_t(it / C::kStages) & 1u, p.wait_limit_ns, &g_moa_kv4_attn_status);
-    }
-  }
-#pragma unroll
-  for (int n = 0; n < NT; ++n)
-#pragma unroll
-    for (int c = 0; c < 2; ++c)
-#pragma unroll
-      for (int d = 4; d < 32; d <<= 1) l[n][c] += __shfl_xor_sync(0xffffffffu, l[n][c], d);
+    };
 
-  // join the warps
-  __syncthreads();
-  float* jo = reinterpret_cast<float*>(smem);                      // [warp][row][kOStride]
-  float* jm = jo + kWarps * 8 * NT * C::kOStride;                  // [warp][row]
-  float* jl = jm + kWarps * 8 * NT;
-#pragma unroll
-  for (int n = 0; n < NT; ++n)
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const int row = warp * 8 * NT + n * 8 + 2 * t + c;
-      if (g == 0) {
-        jm[row] = m[n][c];
-        jl[row] = l[n][c];
+    uint32_t s = count % C::kStages, phase = count / C::kStages & 1u;
+    for (int it = 0; it < my_tiles; ++it) {
+      ok = wait_bounded(bars + 8 * s, phase, wc);
+      if (__any_sync(0xffffffffu, !ok)) {
+        ok = false;
+        break;
       }
-#pragma unroll
-      for (int gi = 0; gi < GV; ++gi)
-        *reinterpret_cast<float4*>(jo + row * C::kOStride + 32 * gi + 4 * g) = make_float4(
-            o[n][2 * gi][c], o[n][2 * gi][2 + c], o[n][2 * gi + 1][c], o[n][2 * gi + 1][2 + c]);
-    }
-  __syncthreads();
-  for (int i = threadIdx.x; i < 8 * NT * (DV / 4); i += kThreads) {
-    const int row = i / (DV / 4), col = i % (DV / 4) * 4;
-    const int64_t r = r0 + row;
-    if (r >= rows) continue;
-    float M = -INFINITY, L = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) M = fmaxf(M, jm[w * 8 * NT + row]);
-    const float base = M == -INFINITY ? 0.f : M;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      const float f = ex2_approx(jm[w * 8 * NT + row] - base);
-      const float4 v = *reinterpret_cast<const float4*>(jo + (w * 8 * NT + row) * C::kOStride + col);
-      L += f * jl[w * 8 * NT + row];
-      x[0] += f * v.x, x[1] += f * v.y, x[2] += f * v.z, x[3] += f * v.w;
-    }
-    if (p.n_splits > 1) {
-      const int64_t at = (item * p.n_splits + split) * (8 * NT) + row;
-      store4(part_o + at * DV + col, x);
-      if (col == 0) {
-        part_ml[2 * at] = M;
-        part_ml[2 * at + 1] = L;
+      const uint8_t* st = ring + s * C::kSub * C::kBytes;
+      const int tok0 = (first + (warp + it * kWarps) * C::kSub) * kBlock;
+      const uint32_t got = here >> (it % C::kBatch * C::kSub) & kTileBits;
+#pragma unroll 1
+      for (int sub = 0; sub < C::kSub; ++sub) {
+        const int tok = tok0 + sub * kBlock;
+        const bool there = got >> sub & 1u;
+        if (there && tok + kBlock <= all_limit)
+          block(std::true_type{}, st + sub * C::kBytes, tok, true);
+        else
+          block(std::false_type{}, st + sub * C::kBytes, tok, there);
       }
-    } else {
-      const float inv = L == 0.f ? 0.f : 1.f / L;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] *= inv;
-      const int64_t head = int64_t(h) * p.G + r % p.G, i_n = r / p.G;
-      store4(O + b * p.o_sb + head * p.o_sh + i_n * p.o_sn + col, x);
-      if (lse != nullptr && col == 0)
-        lse[(b * p.Hk * p.G + head) * p.N + i_n] = L == 0.f ? -INFINITY : (M + lg2_approx(L)) * kLn2;
+      if (it % C::kBatch == C::kBatch - 1) here = here_next;
+      // the stage is free again: start its next tile
+      __syncwarp();
+      if (issued < my_tiles) {
+        if (issued % C::kBatch == 0) look_up(issued / C::kBatch);
+        start(issued);
+        ++issued;
+      }
+      if (++s == C::kStages) {
+        s = 0;
+        phase ^= 1u;
+      }
     }
+    if (!ok) {  // a wait ran out: let the copies in flight land before the memory is reused
+      for (int i = issued > C::kStages ? issued - C::kStages : 0; i < issued; ++i)
+        wait_quiesce(bars + 8 * ((count + i) % C::kStages), (count + i) / C::kStages & 1u, p.wait_limit_ns,
+                     &g_moa_kv4_attn_status);
+    }
+    count += my_tiles;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) l[n][c] += __shfl_xor_sync(0xffffffffu, l[n][c], d);
+
+    // join the warps; maxima in log2 from here on
+    __syncthreads();
+    float* jo = reinterpret_cast<float*>(smem);                      // [warp][row][kOStride]
+    float* jm = jo + kWarps * 8 * NT * C::kOStride;                  // [warp][row]
+    float* jl = jm + kWarps * 8 * NT;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const int row = warp * 8 * NT + n * 8 + 2 * t + c;
+        if (g == 0) {
+          jm[row] = m[n][c] == -INFINITY ? -INFINITY : m[n][c] * c2;
+          jl[row] = l[n][c];
+        }
+#pragma unroll
+        for (int gi = 0; gi < GV; ++gi)
+          *reinterpret_cast<float4*>(jo + row * C::kOStride + 32 * gi + 4 * g) = make_float4(
+              o[n][2 * gi][c], o[n][2 * gi][2 + c], o[n][2 * gi + 1][c], o[n][2 * gi + 1][2 + c]);
+      }
+    __syncthreads();
+    const bool whole = u0 == 0 && u1 == units;
+    // pieces of a cut item: the first one in the CTA's second place, others in the first
+    const int64_t place = (int64_t(blockIdx.x) * 2 + (u0 == 0)) * (8 * NT);
+    for (int i = threadIdx.x; i < 8 * NT * (DV / 4); i += kThreads) {
+      const int row = i / (DV / 4), col = i % (DV / 4) * 4;
+      const int r = r0 + row;
+      if (r >= rows) continue;
+      float M = -INFINITY, L = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) M = fmaxf(M, jm[w * 8 * NT + row]);
+      const float base = M == -INFINITY ? 0.f : M;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float f = ex2_approx(jm[w * 8 * NT + row] - base);
+        const float4 v = *reinterpret_cast<const float4*>(jo + (w * 8 * NT + row) * C::kOStride + col);
+        L += f * jl[w * 8 * NT + row];
+        x[0] += f * v.x, x[1] += f * v.y, x[2] += f * v.z, x[3] += f * v.w;
+      }
+      if (!whole) {
+        store4(part_o + (place + row) * DV + col, x);
+        if (col == 0) *reinterpret_cast<float2*>(part_ml + 2 * (place + row)) = make_float2(M, L);
+      } else {
+        const float inv = L == 0.f ? 0.f : kCodeUnit / L;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] *= inv;
+        const int64_t i_n = unsigned(r) / unsigned(p.G), head = int64_t(h) * p.G + r - i_n * p.G;
+        store4(O + b * p.o_sb + head * p.o_sh + i_n * p.o_sn + col, x);
+        if (lse != nullptr && col == 0)
+          lse[(b * p.Hk * p.G + head) * p.N + i_n] = L == 0.f ? -INFINITY : (M + lg2_approx(L)) * kLn2;
+      }
+    }
+    if (u0 == 0 && !whole && threadIdx.x == 0) {
+      // the CTA that has the item's last unit
+      const int64_t last = before + int64_t(h + 1) * units - 1;
+      uint32_t c = blockIdx.x;
+      while (shares.start(c + 1) <= last) ++c;
+      cuts[blockIdx.x] = Cut{pair, h, int(c - blockIdx.x) + 1, 0};
+    }
+    at += u1 - u0;
+    if (at == before + int64_t(units) * p.Hk) {
+      before = at;
+      ++pair;
+    }
+    // the joined values have been read: copies may write the memory again
+    __syncthreads();
+    fence_proxy_async_smem();
   }
 }
 
-// Joins the ranges of one query row: one warp a row.
-template <typename T, int DV>
-__global__ void __launch_bounds__(128)
+// Joins the pieces of cut items: one CTA for each CTA of the kernel above that began one, sixteen
+// warps for its rows; several warps share a row's pieces when there are fewer rows than warps.
+template <typename T, int DV, int ROWS>
+__global__ void __launch_bounds__(512)
 kv4_attn_join_kernel(const float* __restrict__ part_o, const float* __restrict__ part_ml,
-                     T* __restrict__ O, float* __restrict__ lse, int rows_tile, int64_t n_rows_all,
-                     Params p) {
-  const int64_t id = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31;
-  if (id >= n_rows_all) return;
-  const int64_t rows = p.N * p.G;
-  const int64_t r = id % rows, bh = id / rows;
-  const int h = int(bh % p.Hk);
-  const int64_t b = bh / p.Hk;
-  const int64_t item = bh * p.n_tiles + r / rows_tile;
-  const int64_t at0 = item * p.n_splits * rows_tile + r % rows_tile;
-  float M = -INFINITY;
-  for (int s = lane; s < p.n_splits; s += 32) M = fmaxf(M, part_ml[2 * (at0 + int64_t(s) * rows_tile)]);
+                     const Cut* __restrict__ cuts, T* __restrict__ O, float* __restrict__ lse, Params p) {
+  constexpr int kShare = ROWS >= 16 ? 1 : 16 / ROWS;    // warps of one row
+  __shared__ float so[16][DV], sm[16], sl[16];
+  wait_for_previous();
+  const Cut cut = cuts[blockIdx.x];
+  if (cut.pieces == 0) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rows = int(p.N) * p.G;
+  const int64_t b = sequence_of(cut.pair, p);
+  const int r0 = (cut.pair - int(b) * p.n_tiles) * ROWS;
+  const int64_t c0 = blockIdx.x;
+  auto place = [&](int i, int row) -> int64_t { return ((c0 + i) * 2 + (i == 0)) * ROWS + row; };
+  for (int row = warp / kShare; row < ROWS; row += 16 / kShare) {
+    const int r = r0 + row;
+    float M = -INFINITY, L = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+    if (r < rows) {
+      for (int i = warp % kShare + kShare * lane; i < cut.pieces; i += kShare * 32)
+        M = fmaxf(M, part_ml[2 * place(i, row)]);
 #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
-  const float base = M == -INFINITY ? 0.f : M;
-  float L = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < p.n_splits; ++s) {
-    const int64_t at = at0 + int64_t(s) * rows_tile;
-    const float f = ex2_approx(part_ml[2 * at] - base);
-    L += f * part_ml[2 * at + 1];
-    if (lane * 4 < DV) {
-      const float4 v = *reinterpret_cast<const float4*>(part_o + at * DV + lane * 4);
-      x[0] += f * v.x, x[1] += f * v.y, x[2] += f * v.z, x[3] += f * v.w;
+      for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+      const float base = M == -INFINITY ? 0.f : M;
+#pragma unroll 8
+      for (int i = warp % kShare; i < cut.pieces; i += kShare) {
+        const int64_t at = place(i, row);
+        const float2 ml = *reinterpret_cast<const float2*>(part_ml + 2 * at);
+        const float f = ex2_approx(ml.x - base);
+        L += f * ml.y;
+        if (lane * 4 < DV) {
+          const float4 v = *reinterpret_cast<const float4*>(part_o + at * DV + lane * 4);
+          x[0] += f * v.x, x[1] += f * v.y, x[2] += f * v.z, x[3] += f * v.w;
+        }
+      }
     }
-  }
-  const float inv = L == 0.f ? 0.f : 1.f / L;
+    if constexpr (kShare > 1) {   // rows of one pass only: every warp comes here once
+      if (lane * 4 < DV) *reinterpret_cast<float4*>(&so[warp][lane * 4]) = make_float4(x[0], x[1], x[2], x[3]);
+      if (lane == 0) sm[warp] = M, sl[warp] = L;
+      __syncthreads();
+      if (warp % kShare != 0) continue;
+      M = -INFINITY, L = 0.f, x[0] = x[1] = x[2] = x[3] = 0.f;
+      for (int w = warp; w < warp + kShare; ++w) M = fmaxf(M, sm[w]);
+      const float base = M == -INFINITY ? 0.f : M;
+      for (int w = warp; w < warp + kShare; ++w) {
+        const float f = ex2_approx(sm[w] - base);
+        L += f * sl[w];
+        if (lane * 4 < DV) {
+          const float4 v = *reinterpret_cast<const float4*>(&so[w][lane * 4]);
+          x[0] += f * v.x, x[1] += f * v.y, x[2] += f * v.z, x[3] += f * v.w;
+        }
+      }
+    }
+    if (r >= rows) continue;
+    const float inv = L == 0.f ? 0.f : kCodeUnit / L;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) x[e] *= inv;
-  const int64_t head = int64_t(h) * p.G + r % p.G, i_n = r / p.G;
-  if (lane * 4 < DV) store4(O + b * p.o_sb + head * p.o_sh + i_n * p.o_sn + lane * 4, x);
-  if (lse != nullptr && lane == 0)
-    lse[(b * p.Hk * p.G + head) * p.N + i_n] = L == 0.f ? -INFINITY : (M + lg2_approx(L)) * kLn2;
+    for (int e = 0; e < 4; ++e) x[e] *= inv;
+    const int64_t i_n = unsigned(r) / unsigned(p.G), head = int64_t(cut.h) * p.G + r - i_n * p.G;
+    if (lane * 4 < DV) store4(O + b * p.o_sb + head * p.o_sh + i_n * p.o_sn + lane * 4, x);
+    if (lse != nullptr && lane == 0)
+      lse[(b * p.Hk * p.G + head) * p.N + i_n] = L == 0.f ? -INFINITY : (M + lg2_approx(L)) * kLn2;
+  }
 }
+
+// Workspace: the pieces' rows, their maxima and sums, and the list of cut items.
+struct Work {
+  size_t o, ml, cuts;   // bytes of each
+  Work(int64_t ctas, int64_t rows, int64_t dv)
+      : o(size_t(ctas) * 2 * rows * dv * 4), ml(size_t(ctas) * 2 * rows * 8), cuts(size_t(ctas) * sizeof(Cut)) {}
+  size_t bytes() const { return o + ml + cuts; }
+};
 
 template <typename T, int DK, int DV, int NT, int TERMS>
 cudaError_t run(const Kv4AttnArgs& a, const Kv4Plan& plan, const Params& p) {
@@ -526,18 +728,17 @@ cudaError_t run(const Kv4AttnArgs& a, const Kv4Plan& plan, const Params& p) {
   const void* f = reinterpret_cast<const void*>(kv4_attn_kernel<T, DK, DV, NT, TERMS>);
   cudaError_t e = ensure_smem_limit(f, C::kSmem);
   if (e != cudaSuccess) return e;
-  const int64_t items = a.B * a.c.H * plan.n_tiles;
-  float* part_o = static_cast<float*>(a.ws);
-  float* part_ml = part_o + items * plan.n_splits * plan.rows_tile * DV;
-  kv4_attn_kernel<T, DK, DV, NT, TERMS><<<unsigned(items * plan.n_splits), kThreads, C::kSmem, a.stream>>>(
-      static_cast<const T*>(a.q.p), static_cast<const uint8_t*>(a.c.pool), a.c.table, a.lens,
-      static_cast<T*>(a.o.p), a.lse, part_o, part_ml, p);
-  e = cudaGetLastError();
-  if (e != cudaSuccess || plan.n_splits == 1) return e;
-  const int64_t n_rows = a.B * a.Hq * a.N;
-  kv4_attn_join_kernel<T, DV><<<unsigned((n_rows + 3) / 4), 128, 0, a.stream>>>(
-      part_o, part_ml, static_cast<T*>(a.o.p), a.lse, plan.rows_tile, n_rows, p);
-  return cudaGetLastError();
+  const Work w(plan.ctas, plan.rows_tile, DV);
+  uint8_t* ws = static_cast<uint8_t*>(a.ws);
+  float* part_o = reinterpret_cast<float*>(ws);
+  float* part_ml = reinterpret_cast<float*>(ws + w.o);
+  Cut* cuts = reinterpret_cast<Cut*>(ws + w.o + w.ml);
+  e = launch_overlapped(kv4_attn_kernel<T, DK, DV, NT, TERMS>, dim3(unsigned(plan.ctas)), dim3(kThreads), C::kSmem,
+                        a.stream, static_cast<const T*>(a.q.p), static_cast<const uint8_t*>(a.c.pool), a.c.table,
+                        a.lens, static_cast<T*>(a.o.p), a.lse, part_o, part_ml, cuts, p);
+  if (e != cudaSuccess) return e;
+  return launch_overlapped(kv4_attn_join_kernel<T, DV, 8 * NT>, dim3(unsigned(plan.ctas)), dim3(512), 0, a.stream,
+                           part_o, part_ml, cuts, static_cast<T*>(a.o.p), a.lse, p);
 }
 
 template <typename T, int DK, int DV, int TERMS>
@@ -558,49 +759,38 @@ cudaError_t run_d(const Kv4AttnArgs& a, const Kv4Plan& plan, const Params& p) {
 
 }  // namespace
 
-Kv4Plan kv4_attn_plan(int64_t B, int64_t Hk, int64_t G, int64_t N, int64_t max_len, int sms) {
+Kv4Plan kv4_attn_plan(int64_t B, int64_t Hk, int64_t G, int64_t N, int64_t max_len, bool f32, int sms) {
   Kv4Plan p;
   const int64_t rows = G * N;
   p.rows_tile = rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
   p.n_tiles = (rows + p.rows_tile - 1) / p.rows_tile;
+  // resident CTAs, but none with less than two units if every length is max_len
+  const int64_t resident = int64_t(sms) * (p.rows_tile == 8 && !f32 ? 4 : 2);
+  const int64_t units = (max_len + kUnit - 1) / kUnit;
   const int64_t items = B * Hk * p.n_tiles;
-  const int64_t blocks = (max_len + kv4::kBlock - 1) / kv4::kBlock;
-  // enough ranges for four CTAs on every SM, none shorter than one tile of 64 tokens a warp
-  int64_t splits = (int64_t(sms) * 4 + items - 1) / items;
-  const int64_t most = (blocks + 15) / 16;
-  splits = splits < 1 ? 1 : splits > most ? most : splits;
-  if (splits < 1) splits = 1;
-  int64_t chunk = (blocks + splits - 1) / splits;
-  chunk = (chunk + 3) / 4 * 4;
-  if (chunk < 1) chunk = 1;
-  p.chunk_blocks = int(chunk);
-  p.n_splits = int((blocks + chunk - 1) / chunk);
-  if (p.n_splits < 1) p.n_splits = 1;
+  const int64_t most = items * ((units + 1) / 2);
+  p.ctas = most < resident ? most : resident;
   return p;
 }
 
-size_t kv4_attn_workspace(int64_t B, int64_t Hk, int64_t dv, const Kv4Plan& p) {
-  if (p.n_splits <= 1) return 0;
-  return size_t(B) * Hk * p.n_tiles * p.n_splits * p.rows_tile * (4 * dv + 8);
-}
+size_t kv4_attn_workspace(int64_t dv, const Kv4Plan& p) { return Work(p.ctas, p.rows_tile, dv).bytes(); }
 
 int launch_kv4_attn(const Kv4AttnArgs& a, const Kv4Plan& plan, char* msg, size_t msglen) {
   Params p{};
   p.q_sb = a.q.sb, p.q_sh = a.q.sh, p.q_sn = a.q.sn;
   p.o_sb = a.o.sb, p.o_sh = a.o.sh, p.o_sn = a.o.sn;
   p.n_pages = a.c.n_pages, p.max_pages = a.c.max_pages;
-  p.N = a.N, p.max_len = a.max_len;
+  p.N = a.N, p.max_len = int(a.max_len);
   p.Hk = a.c.H, p.G = int(a.Hq / a.c.H);
   p.blocks_per_page = a.c.page / kv4::kBlock;
-  p.n_splits = plan.n_splits, p.chunk_blocks = plan.chunk_blocks;
-  p.n_tiles = plan.n_tiles;
+  p.n_tiles = int(plan.n_tiles), p.n_pairs = int(a.B * plan.n_tiles);
+  if ((a.max_len / kUnit + 1) * a.c.H > 0x7fffffffLL) {
+    snprintf(msg, msglen, "cache attention: max_len times the key heads is too large");
+    return 3;
+  }
   p.scale = a.scale;
   p.causal = a.causal;
   p.wait_limit_ns = wait_limit_ns();
-  if (a.B * a.c.H * plan.n_tiles > 0x7fffffffLL / plan.n_splits || (a.B * a.Hq * a.N + 3) / 4 > 0x7fffffffLL) {
-    snprintf(msg, msglen, "cache attention: too many query rows for one launch");
-    return 3;
-  }
   const cudaError_t e = a.f32 ? run_d<float, 3>(a, plan, p) : run_d<__nv_bfloat16, 1>(a, plan, p);
   if (e != cudaSuccess) {
     snprintf(msg, msglen, "cache attention launch: %s", cudaGetErrorString(e));

@@ -111,6 +111,7 @@ __device__ __forceinline__ uint8_t* find_block(uint8_t* pool, const int32_t* tab
 template <typename T, int LPR>
 __global__ void __launch_bounds__(kThreads)
 kv4_write_kernel(View k, View v, uint8_t* pool, const int32_t* table, const int32_t* pos, Dims p) {
+  wait_for_previous();
   const int lane = threadIdx.x % LPR;
   const int64_t row = int64_t(blockIdx.x) * (kThreads / LPR) + threadIdx.x / LPR;
   const bool live = row < p.rows;
@@ -158,6 +159,7 @@ kv4_write_kernel(View k, View v, uint8_t* pool, const int32_t* table, const int3
 template <typename T, int LPR>
 __global__ void __launch_bounds__(kThreads)
 kv4_read_kernel(View k, View v, uint8_t* pool, const int32_t* table, const int32_t* pos, Dims p) {
+  wait_for_previous();
   const int lane = threadIdx.x % LPR;
   const int64_t row = int64_t(blockIdx.x) * (kThreads / LPR) + threadIdx.x / LPR;
   if (row >= p.rows) return;
@@ -206,11 +208,8 @@ kv4_read_kernel(View k, View v, uint8_t* pool, const int32_t* table, const int32
 template <typename T, int LPR>
 cudaError_t run(const Kv4MoveArgs& a, const Dims& p, bool write, int64_t grid) {
   uint8_t* pool = static_cast<uint8_t*>(a.c.pool);
-  if (write)
-    kv4_write_kernel<T, LPR><<<unsigned(grid), kThreads, 0, a.stream>>>(a.k, a.v, pool, a.c.table, a.pos, p);
-  else
-    kv4_read_kernel<T, LPR><<<unsigned(grid), kThreads, 0, a.stream>>>(a.k, a.v, pool, a.c.table, a.pos, p);
-  return cudaGetLastError();
+  return launch_overlapped(write ? kv4_write_kernel<T, LPR> : kv4_read_kernel<T, LPR>, dim3(unsigned(grid)),
+                           dim3(kThreads), 0, a.stream, a.k, a.v, pool, a.c.table, a.pos, p);
 }
 
 int launch(const Kv4MoveArgs& a, bool write, char* msg, size_t msglen) {

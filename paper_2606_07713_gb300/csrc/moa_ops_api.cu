@@ -338,8 +338,8 @@ int attn_call(const void* Q, const void* pool, const int32_t* pages, const int32
   const cudaError_t e = device_sm_count(&sms);
   if (e != cudaSuccess)
     return api_fail(MOA_ERR_CUDA, "SM count of the current device: %s", cudaGetErrorString(e));
-  const Kv4Plan plan = kv4_attn_plan(B, H_k, H_q / H_k, N, max_len, sms);
-  const size_t need = kv4_attn_workspace(B, H_k, d_v, plan);
+  const Kv4Plan plan = kv4_attn_plan(B, H_k, H_q / H_k, N, max_len, dtype == MOA_FP32, sms);
+  const size_t need = kv4_attn_workspace(d_v, plan);
   if (need > 0) {
     if (workspace == nullptr || workspace_bytes < need)
       return api_fail(MOA_ERR_INVALID_ARG, "workspace too small: need %zu bytes, got %zu", need,
@@ -466,7 +466,7 @@ size_t moa_kv4_attn_workspace_bytes(int64_t B, int64_t H_q, int64_t H_k, int64_t
   if (!moa::mul(B, H_q, &rows) || !moa::mul(rows, N, &rows) || rows > moa::kMax31) return 0;
   int sms = 0;
   if (moa::device_sm_count(&sms) != cudaSuccess) return 0;
-  return moa::kv4_attn_workspace(B, H_k, d_v, moa::kv4_attn_plan(B, H_k, H_q / H_k, N, max_len, sms));
+  return moa::kv4_attn_workspace(d_v, moa::kv4_attn_plan(B, H_k, H_q / H_k, N, max_len, dtype == MOA_FP32, sms));
 }
 
 }  // extern "C"

@@ -1,11 +1,32 @@
 // Declarations shared by the translation units of the operators around attention: per-head norms
-// with rotation, the 4-bit cache and attention over it (host side only).
+// with rotation, the 4-bit cache and attention over it.
 #pragma once
 #include <cstddef>
 #include <cstdint>
 #include <cuda_runtime.h>
+#include <utility>
 
 namespace moa {
+
+// Launches a kernel that may be set up while the kernel before it on the stream still runs.  Every
+// thread of such a kernel calls wait_for_previous() before its first access to global memory.
+template <typename... P, typename... A>
+cudaError_t launch_overlapped(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, A&&... args) {
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t c{};
+  c.gridDim = grid;
+  c.blockDim = block;
+  c.dynamicSmemBytes = smem;
+  c.stream = stream;
+  c.attrs = &attr;
+  c.numAttrs = 1;
+  return cudaLaunchKernelEx(&c, kernel, P(std::forward<A>(args))...);
+}
+#ifdef __CUDACC__
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+#endif
 
 // Defined beside the attention entry points: the per-thread error text, and MOA_DEBUG_SYNC.
 int api_fail(int code, const char* fmt, ...);
@@ -72,16 +93,15 @@ struct Kv4AttnArgs {
   void* ws;
   cudaStream_t stream;
 };
-// How the cached tokens of one work item are divided: n_splits ranges of chunk_blocks 16-token
-// blocks.
+// How the work is divided: tiles of the G * N query rows of one key head, and the CTAs that share
+// the tokens of all tiles.
 struct Kv4Plan {
-  int rows_tile = 8;        // query rows of one CTA
-  int64_t n_tiles = 1;      // tiles of the G * N query rows of one key head
-  int n_splits = 1;
-  int chunk_blocks = 1;
+  int rows_tile = 8;        // query rows of one tile
+  int64_t n_tiles = 1;
+  int64_t ctas = 1;
 };
-Kv4Plan kv4_attn_plan(int64_t B, int64_t Hk, int64_t G, int64_t N, int64_t max_len, int sms);
-size_t kv4_attn_workspace(int64_t B, int64_t Hk, int64_t dv, const Kv4Plan& p);
+Kv4Plan kv4_attn_plan(int64_t B, int64_t Hk, int64_t G, int64_t N, int64_t max_len, bool f32, int sms);
+size_t kv4_attn_workspace(int64_t dv, const Kv4Plan& p);
 int launch_kv4_attn(const Kv4AttnArgs& a, const Kv4Plan& p, char* msg, size_t msglen);
 
 // Status words of the three translation units (0, MOA_ERR_DEVICE_TIMEOUT or

@@ -137,6 +137,7 @@ __global__ void __launch_bounds__(kThreads)
 norm_rope_kernel(View q, View k, View oq, View ok, const T* wq, const T* wk, const float* cosines,
                  const float* sines, const int32_t* pos, Dims p) {
   constexpr int kGroups = kThreads / LPR;
+  wait_for_previous();
   const int lane = threadIdx.x % LPR;
   const int64_t token = int64_t(blockIdx.x) * kGroups + threadIdx.x / LPR;
   const bool is_q = int(blockIdx.y) < p.nq;
@@ -192,6 +193,7 @@ norm_rope_bwd_kernel(View q, View k, View gq, View gk, View oq, View ok, const T
                      Dims p) {
   constexpr int kGroups = kThreads / LPR;
   __shared__ float sums[kGroups][LPR * kV];
+  wait_for_previous();
   const int lane = threadIdx.x % LPR, group = threadIdx.x / LPR;
   const bool is_q = int(blockIdx.y) < p.nq;
   const int range = is_q ? int(blockIdx.y) : int(blockIdx.y) - p.nq;
@@ -269,6 +271,7 @@ __global__ void __launch_bounds__(1024)
 norm_rope_bwd_sum_kernel(const float* partial, float* dwq, float* dwk, int64_t rows_q, int64_t rows,
                          int d) {
   __shared__ float sums[32][33];
+  wait_for_previous();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int f = blockIdx.x * 32 + lane;
   const int64_t r0 = blockIdx.y == 0 ? 0 : rows_q, r1 = blockIdx.y == 0 ? rows_q : rows;
@@ -324,16 +327,17 @@ int run(const NormRopeArgs& a, const Grid& g, const Dims& p, bool bwd, char* msg
   const T* wq = static_cast<const T*>(a.wq);
   const T* wk = static_cast<const T*>(a.wk);
   const dim3 grid{unsigned(g.x), unsigned(g.y), 1};
+  cudaError_t e;
   if (!bwd) {
-    norm_rope_kernel<T, LPR, PAIRS><<<grid, kThreads, 0, a.stream>>>(
-        a.q, a.k, a.oq, a.ok, wq, wk, a.cosines, a.sines, a.pos, p);
+    e = launch_overlapped(norm_rope_kernel<T, LPR, PAIRS>, grid, dim3(kThreads), 0, a.stream, a.q, a.k, a.oq, a.ok, wq,
+                          wk, a.cosines, a.sines, a.pos, p);
   } else {
-    norm_rope_bwd_kernel<T, LPR, PAIRS><<<grid, kThreads, 0, a.stream>>>(
-        a.q, a.k, a.gq, a.gk, a.oq, a.ok, wq, wk, a.cosines, a.sines, a.pos, a.partial, p);
-    norm_rope_bwd_sum_kernel<<<dim3(unsigned((a.d + 31) / 32), 2), 1024, 0, a.stream>>>(
-        a.partial, a.dwq, a.dwk, g.x * g.nq, g.x * g.y, a.d);
+    e = launch_overlapped(norm_rope_bwd_kernel<T, LPR, PAIRS>, grid, dim3(kThreads), 0, a.stream, a.q, a.k, a.gq, a.gk,
+                          a.oq, a.ok, wq, wk, a.cosines, a.sines, a.pos, a.partial, p);
+    if (e == cudaSuccess)
+      e = launch_overlapped(norm_rope_bwd_sum_kernel, dim3(unsigned((a.d + 31) / 32), 2), dim3(1024), 0, a.stream,
+                            a.partial, a.dwq, a.dwk, g.x * g.nq, g.x * g.y, a.d);
   }
-  const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) {
     snprintf(msg, msglen, "norm and rotation launch: %s", cudaGetErrorString(e));
     return 5;
