@@ -62,6 +62,14 @@ __device__ __forceinline__ void mma_16816(float* d, const uint32_t* a, uint32_t 
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// D = A B: the same without an addend.
+__device__ __forceinline__ void mma_16816_first(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7},"
+      " {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
 // Transpose of an 8 x 8 matrix of 16-bit values held one row (two values a lane) per four lanes.
 __device__ __forceinline__ uint32_t transpose8(uint32_t a) {
   uint32_t d;
@@ -138,11 +146,12 @@ struct Params {
   uint64_t wait_limit_ns;
 };
 
-// One cut item for the joining kernel: written by the CTA that has its first piece.
+// An item for the joining kernel: the list has one for every item if there are no more items than
+// CTAs, else one for every CTA (the item that it begins and does not end).
 struct Cut {
   int pair, h;
-  int pieces;   // 0: this CTA begins no cut item
-  int unused;
+  int first;    // the CTA of its first piece
+  int pieces;   // 0: written whole, nothing to join
 };
 
 template <int DK, int DV, int NT, int TERMS>
@@ -304,7 +313,8 @@ kv4_attn_kernel(const T* __restrict__ Q, const uint8_t* __restrict__ pool,
     }
   }
 
-  if (threadIdx.x == 0) cuts[blockIdx.x].pieces = 0;
+  const bool by_item = int64_t(p.n_pairs) * p.Hk <= gridDim.x;
+  if (threadIdx.x == 0 && !by_item) cuts[blockIdx.x].pieces = 0;
   const float c2 = fabsf(p.scale) * kLog2e * kCodeUnit, slack = c2 > 0.f ? kSlack / c2 : INFINITY;
   const int rows = int(p.N) * p.G;
   uint32_t count = 0;     // tiles this warp has taken so far: its place in the ring and the phases
@@ -439,13 +449,14 @@ kv4_attn_kernel(const T* __restrict__ Q, const uint8_t* __restrict__ pool,
           const uint32_t a0[4] = {lo[0], hi[0], lo[1], hi[1]}, a1[4] = {lo[2], hi[2], lo[3], hi[3]};
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            float acc[4] = {0.f, 0.f, 0.f, 0.f};
+            float acc[4];
 #pragma unroll
             for (int k = 0; k < TERMS; ++k) {
               uint4 q;
               if constexpr (C::kQRegs) q = qreg[gi];
               else q = *reinterpret_cast<const uint4*>(smem + C::kOffQ + (((n * TERMS + k) * GK + gi) * 32 + lane) * 16);
-              mma_16816(acc, a0, q.x, q.y);
+              if (k == 0) mma_16816_first(acc, a0, q.x, q.y);
+              else mma_16816(acc, a0, q.x, q.y);
               mma_16816(acc, a1, q.z, q.w);
             }
 #pragma unroll
@@ -630,12 +641,13 @@ kv4_attn_kernel(const T* __restrict__ Q, const uint8_t* __restrict__ pool,
           lse[(b * p.Hk * p.G + head) * p.N + i_n] = L == 0.f ? -INFINITY : (M + lg2_approx(L)) * kLn2;
       }
     }
-    if (u0 == 0 && !whole && threadIdx.x == 0) {
+    if (u0 == 0 && (by_item || !whole) && threadIdx.x == 0) {
       // the CTA that has the item's last unit
       const int64_t last = before + int64_t(h + 1) * units - 1;
       uint32_t c = blockIdx.x;
       while (shares.start(c + 1) <= last) ++c;
-      cuts[blockIdx.x] = Cut{pair, h, int(c - blockIdx.x) + 1, 0};
+      cuts[by_item ? uint32_t(pair) * p.Hk + h : blockIdx.x] =
+          Cut{pair, h, int(blockIdx.x), whole ? 0 : int(c - blockIdx.x) + 1};
     }
     at += u1 - u0;
     if (at == before + int64_t(units) * p.Hk) {
@@ -648,70 +660,80 @@ kv4_attn_kernel(const T* __restrict__ Q, const uint8_t* __restrict__ pool,
   }
 }
 
-// Joins the pieces of cut items: one CTA for each CTA of the kernel above that began one, sixteen
-// warps for its rows; several warps share a row's pieces when there are fewer rows than warps.
+// Joins the pieces of cut items: CTA (item, row); its eight warps share the pieces, each with its
+// first eight on their way before the largest maximum is known (the call is all latency).
 template <typename T, int DV, int ROWS>
-__global__ void __launch_bounds__(512)
+__global__ void __launch_bounds__(256)
 kv4_attn_join_kernel(const float* __restrict__ part_o, const float* __restrict__ part_ml,
                      const Cut* __restrict__ cuts, T* __restrict__ O, float* __restrict__ lse, Params p) {
-  constexpr int kShare = ROWS >= 16 ? 1 : 16 / ROWS;    // warps of one row
-  __shared__ float so[16][DV], sm[16], sl[16];
+  constexpr int kJoinWarps = 8, kAhead = 8;
+  __shared__ float so[kJoinWarps][DV], sl[kJoinWarps];
   wait_for_previous();
   const Cut cut = cuts[blockIdx.x];
   if (cut.pieces == 0) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rows = int(p.N) * p.G;
   const int64_t b = sequence_of(cut.pair, p);
-  const int r0 = (cut.pair - int(b) * p.n_tiles) * ROWS;
-  const int64_t c0 = blockIdx.x;
-  auto place = [&](int i, int row) -> int64_t { return ((c0 + i) * 2 + (i == 0)) * ROWS + row; };
-  for (int row = warp / kShare; row < ROWS; row += 16 / kShare) {
-    const int r = r0 + row;
-    float M = -INFINITY, L = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
-    if (r < rows) {
-      for (int i = warp % kShare + kShare * lane; i < cut.pieces; i += kShare * 32)
-        M = fmaxf(M, part_ml[2 * place(i, row)]);
+  const int row = int(blockIdx.y), r = (cut.pair - int(b) * p.n_tiles) * ROWS + row;
+  if (r >= int(p.N) * p.G) return;
+  // piece 0 lies in its CTA's second place, the others in the first
+  auto place = [&](int i) -> int64_t { return (int64_t(cut.first + i) * 2 + (i == 0)) * ROWS + row; };
+  float4 v[kAhead];
+  float2 ml[kAhead];
 #pragma unroll
-      for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
-      const float base = M == -INFINITY ? 0.f : M;
-#pragma unroll 8
-      for (int i = warp % kShare; i < cut.pieces; i += kShare) {
-        const int64_t at = place(i, row);
-        const float2 ml = *reinterpret_cast<const float2*>(part_ml + 2 * at);
-        const float f = ex2_approx(ml.x - base);
-        L += f * ml.y;
-        if (lane * 4 < DV) {
-          const float4 v = *reinterpret_cast<const float4*>(part_o + at * DV + lane * 4);
-          x[0] += f * v.x, x[1] += f * v.y, x[2] += f * v.z, x[3] += f * v.w;
-        }
-      }
+  for (int j = 0; j < kAhead; ++j) {
+    const int i = warp + j * kJoinWarps;
+    ml[j] = make_float2(-INFINITY, 0.f);
+    v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (i < cut.pieces) {
+      ml[j] = *reinterpret_cast<const float2*>(part_ml + 2 * place(i));
+      if (lane * 4 < DV) v[j] = *reinterpret_cast<const float4*>(part_o + place(i) * DV + lane * 4);
     }
-    if constexpr (kShare > 1) {   // rows of one pass only: every warp comes here once
-      if (lane * 4 < DV) *reinterpret_cast<float4*>(&so[warp][lane * 4]) = make_float4(x[0], x[1], x[2], x[3]);
-      if (lane == 0) sm[warp] = M, sl[warp] = L;
-      __syncthreads();
-      if (warp % kShare != 0) continue;
-      M = -INFINITY, L = 0.f, x[0] = x[1] = x[2] = x[3] = 0.f;
-      for (int w = warp; w < warp + kShare; ++w) M = fmaxf(M, sm[w]);
-      const float base = M == -INFINITY ? 0.f : M;
-      for (int w = warp; w < warp + kShare; ++w) {
-        const float f = ex2_approx(sm[w] - base);
-        L += f * sl[w];
-        if (lane * 4 < DV) {
-          const float4 v = *reinterpret_cast<const float4*>(&so[w][lane * 4]);
-          x[0] += f * v.x, x[1] += f * v.y, x[2] += f * v.z, x[3] += f * v.w;
-        }
-      }
+  }
+  float M = -INFINITY;
+  for (int i = lane; i < cut.pieces; i += 32) M = fmaxf(M, part_ml[2 * place(i)]);
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+  const float base = M == -INFINITY ? 0.f : M;
+  float L = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int j = 0; j < kAhead; ++j) {
+    const float f = ex2_approx(ml[j].x - base);
+    L += f * ml[j].y;
+    x[0] += f * v[j].x, x[1] += f * v[j].y, x[2] += f * v[j].z, x[3] += f * v[j].w;
+  }
+#pragma unroll 4
+  for (int i = warp + kAhead * kJoinWarps; i < cut.pieces; i += kJoinWarps) {
+    const int64_t at = place(i);
+    const float2 q = *reinterpret_cast<const float2*>(part_ml + 2 * at);
+    const float f = ex2_approx(q.x - base);
+    L += f * q.y;
+    if (lane * 4 < DV) {
+      const float4 u = *reinterpret_cast<const float4*>(part_o + at * DV + lane * 4);
+      x[0] += f * u.x, x[1] += f * u.y, x[2] += f * u.z, x[3] += f * u.w;
     }
-    if (r >= rows) continue;
-    const float inv = L == 0.f ? 0.f : kCodeUnit / L;
+  }
+  if (lane * 4 < DV) *reinterpret_cast<float4*>(&so[warp][lane * 4]) = make_float4(x[0], x[1], x[2], x[3]);
+  if (lane == 0) sl[warp] = L;
+  __syncthreads();
+  if (warp != 0) return;
+  L = 0.f;
+#pragma unroll
+  for (int w = 0; w < kJoinWarps; ++w) L += sl[w];
+  const float inv = L == 0.f ? 0.f : kCodeUnit / L;
+  const int64_t i_n = unsigned(r) / unsigned(p.G), head = int64_t(cut.h) * p.G + r - i_n * p.G;
+  if (lane * 4 < DV) {
+    x[0] = x[1] = x[2] = x[3] = 0.f;
+#pragma unroll
+    for (int w = 0; w < kJoinWarps; ++w) {
+      const float4 u = *reinterpret_cast<const float4*>(&so[w][lane * 4]);
+      x[0] += u.x, x[1] += u.y, x[2] += u.z, x[3] += u.w;
+    }
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] *= inv;
-    const int64_t i_n = unsigned(r) / unsigned(p.G), head = int64_t(cut.h) * p.G + r - i_n * p.G;
-    if (lane * 4 < DV) store4(O + b * p.o_sb + head * p.o_sh + i_n * p.o_sn + lane * 4, x);
-    if (lse != nullptr && lane == 0)
-      lse[(b * p.Hk * p.G + head) * p.N + i_n] = L == 0.f ? -INFINITY : (M + lg2_approx(L)) * kLn2;
+    store4(O + b * p.o_sb + head * p.o_sh + i_n * p.o_sn + lane * 4, x);
   }
+  if (lse != nullptr && lane == 0)
+    lse[(b * p.Hk * p.G + head) * p.N + i_n] = L == 0.f ? -INFINITY : (M + lg2_approx(L)) * kLn2;
 }
 
 // Workspace: the pieces' rows, their maxima and sums, and the list of cut items.
@@ -737,7 +759,9 @@ cudaError_t run(const Kv4AttnArgs& a, const Kv4Plan& plan, const Params& p) {
                         a.stream, static_cast<const T*>(a.q.p), static_cast<const uint8_t*>(a.c.pool), a.c.table,
                         a.lens, static_cast<T*>(a.o.p), a.lse, part_o, part_ml, cuts, p);
   if (e != cudaSuccess) return e;
-  return launch_overlapped(kv4_attn_join_kernel<T, DV, 8 * NT>, dim3(unsigned(plan.ctas)), dim3(512), 0, a.stream,
+  const int64_t items = a.B * a.c.H * plan.n_tiles, rows = a.N * (a.Hq / a.c.H);
+  const dim3 grid(unsigned(items < plan.ctas ? items : plan.ctas), unsigned(rows < 8 * NT ? rows : 8 * NT));
+  return launch_overlapped(kv4_attn_join_kernel<T, DV, 8 * NT>, grid, dim3(256), 0, a.stream,
                            part_o, part_ml, cuts, static_cast<T*>(a.o.p), a.lse, p);
 }
 
