@@ -20,7 +20,7 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(BUILD, "libmoa_attn.so")
 SOURCES = ["moa_attn_api.cu", "attn_fwd_f32_cc.cu", "attn_fwd_bf16_tc.cu", "attn_bwd_bf16_tc.cu",
            "attn_bwd_f32_cc.cu", "qkv_proj_bf16_tc.cu", "moa_ops_api.cu", "qk_norm_rope.cu",
-           "kv4_cache.cu", "kv4_attn.cu"]
+           "kv4_cache.cu", "kv4_attn.cu", "kv4_attn_tc.cu"]
 BINDING = os.path.join(BUILD, "moa_torch.so")
 BINDING_SOURCE = "torch_binding.cpp"
 HEADERS = ["internal.h", "ops_internal.h", "kv4.cuh", "ptx.cuh", "tc_common.cuh"]

@@ -132,6 +132,7 @@ __device__ __forceinline__ void split_pair(float x, float y, uint32_t* t) {
 
 constexpr int kUnit = 64;              // tokens of a unit of work
 constexpr int kUnitBlocks = kUnit / kBlock;
+constexpr int64_t kTcRows = 32;        // more bf16 query rows of a key head than this go to kv4_attn_tc.cu
 constexpr float kSlack = 8.f;          // the running maximum may lag by this (log2): weights up to 2^8
 
 struct Params {
@@ -786,6 +787,7 @@ cudaError_t run_d(const Kv4AttnArgs& a, const Kv4Plan& plan, const Params& p) {
 Kv4Plan kv4_attn_plan(int64_t B, int64_t Hk, int64_t G, int64_t N, int64_t max_len, bool f32, int sms) {
   Kv4Plan p;
   const int64_t rows = G * N;
+  p.tc = !f32 && rows > kTcRows;
   p.rows_tile = rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
   p.n_tiles = (rows + p.rows_tile - 1) / p.rows_tile;
   // resident CTAs, but none with less than two units if every length is max_len
@@ -797,9 +799,12 @@ Kv4Plan kv4_attn_plan(int64_t B, int64_t Hk, int64_t G, int64_t N, int64_t max_l
   return p;
 }
 
-size_t kv4_attn_workspace(int64_t dv, const Kv4Plan& p) { return Work(p.ctas, p.rows_tile, dv).bytes(); }
+size_t kv4_attn_workspace(int64_t B, int64_t Hk, int64_t max_len, int64_t dk, int64_t dv, const Kv4Plan& p, int sms) {
+  return p.tc ? kv4_attn_tc_workspace(B * Hk, max_len, dk, dv, sms) : Work(p.ctas, p.rows_tile, dv).bytes();
+}
 
 int launch_kv4_attn(const Kv4AttnArgs& a, const Kv4Plan& plan, char* msg, size_t msglen) {
+  if (plan.tc) return launch_kv4_attn_tc(a, msg, msglen);
   Params p{};
   p.q_sb = a.q.sb, p.q_sh = a.q.sh, p.q_sn = a.q.sn;
   p.o_sb = a.o.sb, p.o_sh = a.o.sh, p.o_sn = a.o.sn;

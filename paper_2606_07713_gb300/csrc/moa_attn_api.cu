@@ -164,7 +164,8 @@ bool debug_sync() {
 int read_status(const char* where) {
   cudaError_t (*const readers[])(unsigned*) = {
       bf16_read_and_clear_status, bwd_read_and_clear_status,  proj_read_and_clear_status,
-      norm_read_and_clear_status, kv4_read_and_clear_status, kv4_attn_read_and_clear_status};
+      norm_read_and_clear_status, kv4_read_and_clear_status, kv4_attn_read_and_clear_status,
+      kv4_tc_read_and_clear_status};
   unsigned timeout = 0, index = 0;
   for (auto read : readers) {
     unsigned v = 0;

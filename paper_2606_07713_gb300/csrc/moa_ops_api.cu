@@ -339,7 +339,7 @@ int attn_call(const void* Q, const void* pool, const int32_t* pages, const int32
   if (e != cudaSuccess)
     return api_fail(MOA_ERR_CUDA, "SM count of the current device: %s", cudaGetErrorString(e));
   const Kv4Plan plan = kv4_attn_plan(B, H_k, H_q / H_k, N, max_len, dtype == MOA_FP32, sms);
-  const size_t need = kv4_attn_workspace(d_v, plan);
+  const size_t need = kv4_attn_workspace(B, H_k, max_len, d_k, d_v, plan, sms);
   if (need > 0) {
     if (workspace == nullptr || workspace_bytes < need)
       return api_fail(MOA_ERR_INVALID_ARG, "workspace too small: need %zu bytes, got %zu", need,
@@ -459,14 +459,14 @@ int moa_kv4_attn(const void* Q, const void* pool, const int32_t* pages, const in
 
 size_t moa_kv4_attn_workspace_bytes(int64_t B, int64_t H_q, int64_t H_k, int64_t N, int64_t d_k,
                                     int64_t d_v, int64_t max_len, int dtype) {
-  (void)d_k;
   if ((dtype != MOA_BF16 && dtype != MOA_FP32) || B < 1 || H_q < 1 || H_k < 1 || N < 1 || max_len < 1) return 0;
-  if (H_q % H_k != 0 || d_v < 1 || d_v > 128 || max_len > moa::kMax31) return 0;
+  if (H_q % H_k != 0 || (d_k != 64 && d_k != 128) || (d_v != 64 && d_v != 128) || max_len > moa::kMax31 - 64) return 0;
   int64_t rows;
   if (!moa::mul(B, H_q, &rows) || !moa::mul(rows, N, &rows) || rows > moa::kMax31) return 0;
   int sms = 0;
   if (moa::device_sm_count(&sms) != cudaSuccess) return 0;
-  return moa::kv4_attn_workspace(d_v, moa::kv4_attn_plan(B, H_k, H_q / H_k, N, max_len, dtype == MOA_FP32, sms));
+  return moa::kv4_attn_workspace(B, H_k, max_len, d_k, d_v,
+                                 moa::kv4_attn_plan(B, H_k, H_q / H_k, N, max_len, dtype == MOA_FP32, sms), sms);
 }
 
 }  // extern "C"

@@ -96,18 +96,22 @@ struct Kv4AttnArgs {
 // How the work is divided: tiles of the G * N query rows of one key head, and the CTAs that share
 // the tokens of all tiles.
 struct Kv4Plan {
+  bool tc = false;          // many rows: kv4_attn_tc.cu (the rest of the plan is then unused)
   int rows_tile = 8;        // query rows of one tile
   int64_t n_tiles = 1;
   int64_t ctas = 1;
 };
 Kv4Plan kv4_attn_plan(int64_t B, int64_t Hk, int64_t G, int64_t N, int64_t max_len, bool f32, int sms);
-size_t kv4_attn_workspace(int64_t dv, const Kv4Plan& p);
+size_t kv4_attn_workspace(int64_t B, int64_t Hk, int64_t max_len, int64_t dk, int64_t dv, const Kv4Plan& p, int sms);
+size_t kv4_attn_tc_workspace(int64_t bh, int64_t max_len, int64_t dk, int64_t dv, int sms);
+int launch_kv4_attn_tc(const Kv4AttnArgs& a, char* msg, size_t msglen);
 int launch_kv4_attn(const Kv4AttnArgs& a, const Kv4Plan& p, char* msg, size_t msglen);
 
-// Status words of the three translation units (0, MOA_ERR_DEVICE_TIMEOUT or
+// Status words of the four translation units (0, MOA_ERR_DEVICE_TIMEOUT or
 // MOA_ERR_DEVICE_INDEX); read and cleared after a synchronisation.
 cudaError_t norm_read_and_clear_status(unsigned* value);
 cudaError_t kv4_read_and_clear_status(unsigned* value);
 cudaError_t kv4_attn_read_and_clear_status(unsigned* value);
+cudaError_t kv4_tc_read_and_clear_status(unsigned* value);
 
 }  // namespace moa
