@@ -14,8 +14,10 @@
 //            A token whose value is not finite gets zeros and a NaN key: the rows that see it
 //            read NaN, the others nothing (0 * NaN would reach them through the second product).
 //   attend   query rows, as fp16 with each row's power of two taken out (bf16 queries fit exactly),
-//            against 128-token tiles: S = Q K^T (fp16), running maximum and sum per row, P (bf16)
-//            V (bf16) accumulated in TMEM.  Maximum, exponentials, sum in fp32.
+//            against 128-token tiles: S = Q K^T (fp16), running maximum and sum per row, O += P V
+//            (bf16) in TMEM.  Maximum, exponentials, sum in fp32.  P and V in fp16 (11 bits, V then
+//            exact) would halve the rounding of ordinary rows, but weights below 2^-31 of the largest
+//            would be lost, and they are all there is of a feature that the larger ones leave at zero.
 //   join     the pieces of cut work items.
 //
 // Rows of a key head are counted head by head: row r is query r % N of query head r / N of the
@@ -27,7 +29,7 @@
 //
 // CTA organisation (12 warps): warps 0-3 and 4-7 softmax and epilogue of row tiles 0 and 1 (thread
 // = row), warp 8 TMEM allocation and the products of tile 0, warp 9 TMA, warp 10 the products of
-// tile 1, warp 11 completes the warpgroup whose registers move to the softmax.  TMEM columns: two
+// tile 1, warp 11 the share's items, one after another, for the other roles.  TMEM columns: two
 // S, P and O at d_v = 64; one S for both tiles at d_v = 128.  K and V tiles stream through a
 // shared-memory ring in the order of use, K0 K1 V0 K2 V1 ...
 // Waits are bounded: on expiry MOA_ERR_DEVICE_TIMEOUT is recorded and every role leaves its loop.
@@ -37,6 +39,7 @@
 #include <cuda_runtime.h>
 
 #include <atomic>
+#include <cfloat>
 #include <cstdio>
 
 #include "internal.h"
@@ -59,7 +62,7 @@ constexpr int kBM = 128;              // query rows of a row tile (= TMEM lanes)
 constexpr int kRows = 2 * kBM;        // query rows of a work item
 constexpr int kBN = 128;              // tokens of a tile
 constexpr int kThreads = 384;
-constexpr int kMmaWarp0 = 8, kLoadWarp = 9, kMmaWarp1 = 10;
+constexpr int kMmaWarp0 = 8, kLoadWarp = 9, kMmaWarp1 = 10, kWalkWarp = 11;
 constexpr float kRescaleLog2 = 8.f;   // the running maximum may lag by this: weights up to 2^8
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -76,10 +79,12 @@ struct Cfg {
   static constexpr int kStages = DK == 64 ? (DV == 64 ? 8 : 6) : (DV == 64 ? 4 : 5);
   static constexpr int kOffKV = 2 * kQTileBytes;
   static constexpr int kOffBar = kOffKV + kStages * kStageBytes;
-  // barriers: full[NS], empty[NS], q_full, s_full[2], p_ready[2], o_done[2], s_free[2], p_free[2], drain
-  static constexpr int kNumBars = 2 * kStages + 12;
+  // barriers: full[NS], empty[NS], q_full, s_full[2], p_ready[2], o_done[2], s_free[2], p_free[2], drain,
+  // item_full[2], item_empty[2]
+  static constexpr int kNumBars = 2 * kStages + 16;
   static constexpr int kOffMisc = kOffBar + kNumBars * 8;
-  static constexpr int kSmemBytes = kOffMisc + 16 + 12 * 8 + 32 + 1024;
+  static constexpr int kOffItems = (kOffMisc + 8 + 15) / 16 * 16;    // two items, then scan[12] and found[2]
+  static constexpr int kSmemBytes = kOffItems + 2 * 16 + 14 * 8 + 1024;
   static constexpr int kEarlyChunks = DV == 64 ? 2 : 3;
   static constexpr uint32_t kTmemCols = 512;
   static constexpr uint32_t kTmemS0 = 0, kTmemS1 = kSharedS ? 0 : 128;
@@ -145,6 +150,10 @@ struct Cut {
 // ------------------------------------------------------------------------------------------------
 // Widening
 // ------------------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+  const __half2 x = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&x);
+}
 __device__ __forceinline__ float bf16_value(const uint8_t* p) {
   return __uint_as_float(uint32_t(*reinterpret_cast<const uint16_t*>(p)) << 16);
 }
@@ -226,8 +235,7 @@ kv4_widen_kernel(const uint8_t* __restrict__ pool, const int32_t* __restrict__ t
     uint32_t o[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const __half2 x = __floats2half2_rn(float(int(w >> (4 * j) & 15u) - 8) * s, float(int(w >> (4 * j + 16) & 15u) - 8) * s);
-      o[j] = *reinterpret_cast<const uint32_t*>(&x);
+      o[j] = pack_f16x2(float(int(w >> (4 * j) & 15u) - 8) * s, float(int(w >> (4 * j + 16) & 15u) - 8) * s);
     }
     *reinterpret_cast<uint4*>(wk + (row0 + token) * DK + f8 * 8) = make_uint4(o[0], o[1], o[2], o[3]);
   }
@@ -298,25 +306,9 @@ __host__ __device__ constexpr uint32_t make_idesc_f16(int M, int N) {
   return (1u << 4) | (uint32_t(N >> 3) << 17) | (uint32_t(M >> 4) << 24);
 }
 
-// The items of this CTA's share, one after another: every role walks over the same ones.
-struct Walk {
-  int64_t at, stop, before;   // the next unit, the share's end, the first unit of `item`
-  int item;
-  int u0, u1, units;          // the tiles of the item that are this CTA's, of so many
-  bool begun;
-  __device__ __forceinline__ bool next(const int32_t* lens, const Params& p) {
-    if (at >= stop) return false;
-    if (begun) {   // a share goes on only past an item's end
-      before = at;
-      ++item;
-    }
-    begun = true;
-    units = units_of(lens, item, p, false);
-    u0 = int(at - before);
-    u1 = int(units - u0 < stop - at ? units : u0 + (stop - at));
-    at += u1 - u0;
-    return true;
-  }
+// One item of a CTA's share: its tiles [u0, u1) of `units` are this CTA's.  item < 0: no more.
+struct Item {
+  int item, u0, u1, units;
 };
 
 template <int DK, int DV>
@@ -340,9 +332,11 @@ kv4_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   const uint32_t drain = bar0 + 8u * (2 * C::kStages + 11);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::kOffMisc);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::kOffMisc + 4);
-  // scan[0..11] warp sums; found[0..3]: item, its first unit, start and end of the share
-  int64_t* scan = reinterpret_cast<int64_t*>(smem + ((C::kOffMisc + 8 + 7) & ~7));
-  int64_t* found = scan + 12;
+  auto item_full = [&](int i) { return bar0 + 8u * (2 * C::kStages + 12 + i); };
+  auto item_empty = [&](int i) { return bar0 + 8u * (2 * C::kStages + 14 + i); };
+  volatile Item* items = reinterpret_cast<volatile Item*>(smem + C::kOffItems);
+  int64_t* scan = reinterpret_cast<int64_t*>(smem + C::kOffItems + 2 * sizeof(Item));   // warp sums
+  int64_t* found = scan + 12;                                                           // item, its first unit
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const WaitCtl wc{abort_flag, p.wait_limit_ns, 0u, &g_moa_kv4_tc_status};
 
@@ -353,6 +347,10 @@ kv4_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     }
     mbar_init(q_full, 256);
     mbar_init(drain, 2);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(item_full(i), 1);
+      mbar_init(item_empty(i), 11);   // the softmax warps, both issuers, the loads
+    }
     for (int j = 0; j < 2; ++j) {
       mbar_init(s_full(j), 1);
       mbar_init(p_ready(j), 128);
@@ -380,11 +378,10 @@ kv4_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
 #pragma unroll
   for (int w = 0; w < 12; ++w) total += scan[w];
   const Shares shares(total, gridDim.x);
-  Walk walk{};
-  walk.at = blockIdx.x < shares.n ? shares.start(blockIdx.x) : total;
-  walk.stop = blockIdx.x < shares.n ? shares.start(blockIdx.x + 1) : total;
+  const int64_t first_unit = blockIdx.x < shares.n ? shares.start(blockIdx.x) : total;
+  const int64_t stop = blockIdx.x < shares.n ? shares.start(blockIdx.x + 1) : total;
   int64_t done = 0;
-  for (int base = 0; walk.at < walk.stop; base += kThreads) {
+  for (int base = 0; first_unit < stop; base += kThreads) {
     const int i = base + threadIdx.x;
     const int64_t mine = i < n_items ? units_of(lens, i, p, false) : 0;
     int64_t incl = mine;
@@ -404,22 +401,23 @@ kv4_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     }
     incl += done;
     done += all;
-    if (walk.at >= incl - mine && walk.at < incl) {
+    if (first_unit >= incl - mine && first_unit < incl) {
       found[0] = i;
       found[1] = incl - mine;
     }
-    if (walk.at < done) break;
+    if (first_unit < done) break;
   }
   if (threadIdx.x == 0) cuts[blockIdx.x].pieces = 0;
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = *tmem_slot;
-  if (walk.at < walk.stop) {
-    walk.item = int(found[0]);
-    walk.before = found[1];
-  }
-  const int rows = p.N * p.G;
+  // Item number i of the share, as every role sees it: valid until the role's release.
+  auto get_item = [&](uint32_t i, bool& ok) {
+    ok = ok && wait_bounded(item_full(i & 1), i >> 1 & 1u, wc);
+    const volatile Item& x = items[i & 1];
+    return ok ? Item{x.item, x.u0, x.u1, x.units} : Item{-1, 0, 0, 0};
+  };
 
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRegsCtrl));
@@ -431,8 +429,11 @@ kv4_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         int slot = 0;
         uint32_t phase = 0, issued = 0, issued_phase = 0;
         bool ok = true;
-        while (ok && walk.next(lens, p)) {
-          const int bh = int(unsigned(walk.item) / unsigned(p.n_tiles)), n_kt = walk.u1 - walk.u0;
+        for (uint32_t seg = 0; ok; ++seg) {
+          const Item x = get_item(seg, ok);
+          if (x.item < 0) break;
+          mbar_arrive(item_empty(seg & 1));
+          const int bh = int(unsigned(x.item) / unsigned(p.n_tiles)), n_kt = x.u1 - x.u0;
           for (int t = 0; t < 2 * n_kt; ++t) {
             // K0 K1 V0 K2 V1 ... (tile n + 1's scores come before tile n's P V)
             const int u = t - 1, nn = u >> 1;
@@ -445,7 +446,7 @@ kv4_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
             issued |= 1u << slot;
             issued_phase = (issued_phase & ~(1u << slot)) | (phase << slot);
             const uint32_t dst = sKV + slot * C::kStageBytes;
-            const int row = (walk.u0 + n) * kBN;
+            const int row = (x.u0 + n) * kBN;
             mbar_arrive_expect_tx(full_bar(slot), is_k ? C::kKTileBytes : C::kVTileBytes);
             if (is_k) {
 #pragma unroll
@@ -479,7 +480,7 @@ kv4_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         const uint32_t tO = tmem + (j ? C::kTmemO1 : C::kTmemO0);
         const uint32_t sQj = sQ + j * C::kQTileBytes;
         int slot = 0;
-        uint32_t phase = 0, seg = 0;
+        uint32_t phase = 0;
         uint32_t t = 0;   // tiles so far: the phases of the barriers between the roles
         auto next = [&]() {
           if (++slot == C::kStages) {
@@ -509,8 +510,11 @@ kv4_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
           return u == 0 || wait_bounded(s_free(j), (u - 1) & 1u, wc);
         };
         bool ok = true;
-        while (ok && walk.next(lens, p)) {
-          const int n_kt = walk.u1 - walk.u0;
+        for (uint32_t seg = 0; ok; ++seg) {
+          const Item x = get_item(seg, ok);
+          if (x.item < 0) break;
+          mbar_arrive(item_empty(seg & 1));
+          const int n_kt = x.u1 - x.u0;
           ok = wait_bounded(q_full, seg & 1u, wc) && wait_bounded(full_bar(slot), phase, wc) && s_buffer(t);
           if (ok) {
             tc_fence_after_sync();
@@ -542,9 +546,37 @@ kv4_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
           }
           // arrives when the item's products are complete
           mma_commit(o_done(j));
-          ++seg;
         }
         mma_commit(drain);
+      }
+    } else if (warp == kWalkWarp && lane == 0) {
+      // ------------------------------------------------------------ the items of the share
+      int64_t at = first_unit, before = 0;
+      int item = 0;
+      if (at < stop) {
+        item = int(found[0]);
+        before = found[1];
+      }
+      for (uint32_t seg = 0;; ++seg) {
+        if (seg >= 2 && !wait_bounded(item_empty(seg & 1), ((seg >> 1) - 1) & 1u, wc)) break;
+        volatile Item& x = items[seg & 1];
+        if (at >= stop) {
+          x.item = -1;
+          mbar_arrive(item_full(seg & 1));
+          break;
+        }
+        const int units = units_of(lens, item, p, false), u0 = int(at - before);
+        const int u1 = int(units - u0 < stop - at ? units : u0 + (stop - at));
+        x.item = item, x.u0 = u0, x.u1 = u1, x.units = units;
+        mbar_arrive(item_full(seg & 1));
+        at += u1 - u0;
+        if (u0 == 0 && u1 < units) {   // begun here, ended by a later CTA
+          uint32_t c = blockIdx.x;
+          while (shares.start(c + 1) < before + units) ++c;
+          cuts[blockIdx.x] = Cut{item, int(c - blockIdx.x) + 1};
+        }
+        before += units;
+        ++item;
       }
     }
   } else {
@@ -556,27 +588,44 @@ kv4_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     const uint32_t tO = tmem + (uint32_t(lane_base) << 16) + (j ? C::kTmemO1 : C::kTmemO0);
     const uint32_t tP = tmem + (uint32_t(lane_base) << 16) + (j ? C::kTmemP1 : C::kTmemP0);
     bool ok = true;
-    uint32_t t = 0, seg = 0;
-    while (ok && walk.next(lens, p)) {
-      const int bh = int(unsigned(walk.item) / unsigned(p.n_tiles));
-      const int r = (walk.item - bh * p.n_tiles) * kRows + j * kBM + row;
-      const int b = int(unsigned(p.bh0 + bh) / unsigned(p.Hk)), h = p.bh0 + bh - b * p.Hk;
-      const int rh = int(unsigned(r) / unsigned(p.N)), ri = r - rh * p.N;   // query head of the group, query
-      const int lim = r < rows ? limit_of(length_of(lens, b, p, false), ri, p) : 0;
-      // the row as fp16, its power of two taken out, into the swizzled tile
+    uint32_t t = 0;
+    for (uint32_t seg = 0;; ++seg) {
+      const Item x0 = get_item(seg, ok);
+      if (x0.item < 0) break;
+      int u0 = x0.u0, u1 = x0.u1;
+      // where the thread's row lies: row r of key head bh is query ri of its query head rh
+      struct Place {
+        int r, b, h, rh, ri;
+        bool live;
+      };
+      auto place = [&](int item) {
+        Place w;
+        const int bh = int(unsigned(item) / unsigned(p.n_tiles));
+        w.r = (item - bh * p.n_tiles) * kRows + j * kBM + row;
+        w.b = int(unsigned(p.bh0 + bh) / unsigned(p.Hk)), w.h = p.bh0 + bh - w.b * p.Hk;
+        w.rh = int(unsigned(w.r) / unsigned(p.N)), w.ri = w.r - w.rh * p.N;
+        w.live = w.r < p.N * p.G;
+        return w;
+      };
+      int lim;
       float c_row = p.c_log2;
+      const float2* fac;
       {
+        const Place w = place(x0.item);
+        lim = w.live ? limit_of(length_of(lens, w.b, p, false), w.ri, p) : 0;
+        fac = factor + int64_t(w.b * p.Hk + w.h - p.bh0) * p.tiles_pad;
+        // the row as fp16, its power of two taken out, into the swizzled tile
         uint4 x[DK / 8];
-        const __nv_bfloat16* src = Q + int64_t(b) * p.q_sb + (int64_t(h) * p.G + rh) * p.q_sh + int64_t(ri) * p.q_sn;
+        const __nv_bfloat16* src = Q + int64_t(w.b) * p.q_sb + (int64_t(w.h) * p.G + w.rh) * p.q_sh + int64_t(w.ri) * p.q_sn;
         uint32_t top = 0;
 #pragma unroll
         for (int i = 0; i < DK / 8; ++i) {
-          x[i] = r < rows ? *reinterpret_cast<const uint4*>(src + 8 * i) : make_uint4(0, 0, 0, 0);
-          const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+          x[i] = w.live ? *reinterpret_cast<const uint4*>(src + 8 * i) : make_uint4(0, 0, 0, 0);
+          const uint32_t q[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            top = max(top, w[k] & 0x7fffu);
-            top = max(top, (w[k] >> 16) & 0x7fffu);
+            top = max(top, q[k] & 0x7fffu);
+            top = max(top, (q[k] >> 16) & 0x7fffu);
           }
         }
         // the largest magnitude in [2^14, 2^15); a row with a member that is not finite as it is
@@ -587,26 +636,23 @@ kv4_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         c_row *= __uint_as_float(uint32_t(127 + e) << 23);
 #pragma unroll
         for (int i = 0; i < DK / 8; ++i) {
-          const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+          const uint32_t q[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
           uint32_t o[4];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const __half2 y = __floats2half2_rn(__uint_as_float(w[k] << 16) * down, __uint_as_float(w[k] & 0xffff0000u) * down);
-            o[k] = *reinterpret_cast<const uint32_t*>(&y);
-          }
+          for (int k = 0; k < 4; ++k)
+            o[k] = pack_f16x2(__uint_as_float(q[k] << 16) * down, __uint_as_float(q[k] & 0xffff0000u) * down);
           *reinterpret_cast<uint4*>(smem + j * C::kQTileBytes + (i >> 3) * C::kPanelBytes + row * 128 +
                                     (((i & 7) ^ (row & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
         }
         fence_proxy_async_smem();
         mbar_arrive(q_full);
       }
-      const float2* fac = factor + int64_t(bh) * p.tiles_pad;
       float m = -INFINITY, l = 0.f;
-      float2 f_next = fac[walk.u0];
-      for (int n = walk.u0; n < walk.u1; ++n, ++t) {
-        const float c = c_row * f_next.x;
+      float2 f_next = fac[u0];
+      for (int n = u0; n < u1; ++n, ++t) {
+        const float c = fmaxf(c_row * f_next.x, FLT_MIN);   // not zero: c * -infinity hides a token
         const uint32_t gone = __float_as_uint(f_next.y);   // blocks whose page is not there
-        if (n + 1 < walk.u1) f_next = fac[n + 1];
+        if (n + 1 < u1) f_next = fac[n + 1];
         if (!wait_bounded(s_full(j), t & 1u, wc)) {
           ok = false;
           break;
@@ -619,19 +665,14 @@ kv4_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         float* s = reinterpret_cast<float*>(sr);
         const int valid = lim - n * kBN;   // of this row
         const bool full = __all_sync(0xffffffffu, valid >= kBN) && gone == 0;
-        float tmax;
-        if (full) {
-          tmax = row_max128(s);
-        } else {
-          tmax = -INFINITY;
+        if (!full) {   // hidden tokens: -infinity, and the rest is the same code
 #pragma unroll
-          for (int i = 0; i < kBN; ++i)
-            if (i < valid && !(gone >> (i / kBlock) & 1u)) tmax = fmaxf(tmax, s[i]);
+          for (int i = 0; i < kBN; ++i) s[i] = i < valid && !(gone >> (i / kBlock) & 1u) ? s[i] : -INFINITY;
         }
-        const float m_tile = tmax == -INFINITY ? -INFINITY : c * tmax;
+        const float m_tile = c * row_max128(s);
         bool rescale = false;   // warp-uniform
         float alpha = 1.f;
-        if (n == walk.u0) {
+        if (n == u0) {
           m = m_tile;
         } else if (__any_sync(0xffffffffu, m_tile > m + kRescaleLog2)) {
           const float m_new = fmaxf(m, m_tile);
@@ -651,13 +692,6 @@ kv4_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
             float x0, x1, x2, x3;
             ffma2(x0, x1, s[k], s[k + 1], cc, mm);
             ffma2(x2, x3, s[k + 2], s[k + 3], cc, mm);
-            if (!full) {
-              const int n_seen = gone >> (k / kBlock) & 1u ? 0 : valid;
-              x0 = k < n_seen ? x0 : -INFINITY;
-              x1 = k + 1 < n_seen ? x1 : -INFINITY;
-              x2 = k + 2 < n_seen ? x2 : -INFINITY;
-              x3 = k + 3 < n_seen ? x3 : -INFINITY;
-            }
             const float p0 = ex2_approx(x0), p1 = ex2_approx(x1), p2 = ex2_approx(x2), p3 = ex2_approx(x3);
             fadd2(l0, l1, p0, p1);
             fadd2(l2, l3, p2, p3);
@@ -690,16 +724,14 @@ kv4_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         tc_fence_before_sync();
         mbar_arrive(p_ready(j));
       }
-      if (!ok || !wait_bounded(o_done(j), seg & 1u, wc)) {
-        ok = false;
-        break;
-      }
-      ++seg;
+      if (!ok || !wait_bounded(o_done(j), seg & 1u, wc)) break;
       tc_fence_after_sync();
       // the item is written, or this CTA's piece of it
-      const bool whole = walk.u0 == 0 && walk.u1 == walk.units;
+      const volatile Item& xi = items[seg & 1];
+      const Place w = place(xi.item);
+      const bool first_piece = xi.u0 == 0, whole = first_piece && xi.u1 == xi.units;
       if (!whole) {
-        const int64_t at = (int64_t(blockIdx.x) * 2 + (walk.u0 == 0)) * kRows + j * kBM + row;
+        const int64_t at = (int64_t(blockIdx.x) * 2 + first_piece) * kRows + j * kBM + row;
 #pragma unroll
         for (int c = 0; c < DV; c += 16) {
           uint32_t o[16];
@@ -713,33 +745,30 @@ kv4_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
                                  __uint_as_float(o[4 * i + 3]));
         }
         part_ml[at] = make_float2(m, l);
-        if (walk.u0 == 0 && threadIdx.x == 0) {
-          uint32_t c = blockIdx.x;
-          while (shares.start(c + 1) < walk.before + walk.units) ++c;
-          cuts[blockIdx.x] = Cut{walk.item, int(c - blockIdx.x) + 1};
-        }
       } else {
         const float inv = l == 0.f ? 0.f : 1.f / l;
-        __nv_bfloat16* orow = O + int64_t(b) * p.o_sb + (int64_t(h) * p.G + rh) * p.o_sh + int64_t(ri) * p.o_sn;
-        if (lse != nullptr && r < rows)
-          lse[(int64_t(b) * p.Hk * p.G + int64_t(h) * p.G + rh) * p.N + ri] = l == 0.f ? -INFINITY : (m + lg2_approx(l)) * kLn2;
+        __nv_bfloat16* orow = O + int64_t(w.b) * p.o_sb + (int64_t(w.h) * p.G + w.rh) * p.o_sh + int64_t(w.ri) * p.o_sn;
+        if (lse != nullptr && w.live)
+          lse[(int64_t(w.b) * p.Hk * p.G + int64_t(w.h) * p.G + w.rh) * p.N + w.ri] = l == 0.f ? -INFINITY : (m + lg2_approx(l)) * kLn2;
 #pragma unroll
         for (int c = 0; c < DV; c += 16) {
           uint32_t o[16];
           tmem_ld_32x32b_x16(tO + c, o);
           tmem_wait_ld();
           reg_anchor_x16(o);
-          if (r < rows) {
-            uint32_t w[8];
+          if (w.live) {
+            uint32_t y[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-              w[i] = pack_bf16x2(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv);
-            reinterpret_cast<uint4*>(orow + c)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-            reinterpret_cast<uint4*>(orow + c)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+              y[i] = pack_bf16x2(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv);
+            reinterpret_cast<uint4*>(orow + c)[0] = make_uint4(y[0], y[1], y[2], y[3]);
+            reinterpret_cast<uint4*>(orow + c)[1] = make_uint4(y[4], y[5], y[6], y[7]);
           }
         }
       }
       tc_fence_before_sync();   // O is read: the next item's first product (after p_ready) may write it
+      __syncwarp();
+      if (lane == 0) mbar_arrive(item_empty(seg & 1));
     }
   }
 
