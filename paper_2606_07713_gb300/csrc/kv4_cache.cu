@@ -1,13 +1,18 @@
 // Writing keys and values into the 4-bit cache, and reading them back, sm_103a.
 //
 // Mathematics and layout: kv4.cuh.  Write: per row and 32 features, s = bf16(max|x| / 7),
-// code = rint(x / s) (ties to even, IEEE division: the same codes as the definition in exact
-// arithmetic for bf16 inputs).  Read: code * s in fp32, rounded once to the output's type.
+// code = rint(x / s) (ties to even; for bf16 inputs the same codes as in exact arithmetic).  Read:
+// code * s in fp32, rounded once to the output's type.
 //
 // What bounds it: memory.  A bf16 value is 2 bytes on one side and 9/16 on the other.
 //
-// Layout of the work: 8 or 16 lanes own one row (head, token), eight features a lane, so that the
-// four lanes of a scale group are neighbours.
+// Layout of the work: a unit is 16 tokens of a sequence that fall into one 16-token block of the cache
+// when the call's positions are consecutive (a prompt): a head's block is then put together (or taken
+// apart) in shared memory and crosses to or from global memory in whole 16-byte pieces.  Rows that do
+// not fill a block (single tokens, the ends of a prompt, positions in another order) go straight to
+// their places, in 2- and 4-byte pieces.  A CTA takes a unit through a range of heads: its places are
+// looked up once, and the next head's rows are on their way while one is worked on.  8 or 16 lanes own
+// one row, eight features a lane, so the four lanes of a scale group are neighbours.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -27,19 +32,45 @@ using namespace kv4;
 
 constexpr int kThreads = 256;
 
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, float* x) {
-  const uint4 v = *reinterpret_cast<const uint4*>(p);
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+// A lane's eight features as they lie in memory.
+template <typename T>
+struct Raw {
+  uint4 w[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(w[i] << 16);
-    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    for (int i = 0; i < int(sizeof(T) / 2); ++i) w[i] = p ? reinterpret_cast<const uint4*>(p)[i] : make_uint4(0, 0, 0, 0);
   }
-}
-__device__ __forceinline__ void load8(const float* p, float* x) {
-  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-  x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-}
+  __device__ __forceinline__ void widen(float* x) const {
+    if constexpr (sizeof(T) == 2) {
+      const uint32_t v[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(v[i] << 16);
+        x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+      }
+    } else {
+      const uint32_t v[8] = {w[0].x, w[0].y, w[0].z, w[0].w, w[1].x, w[1].y, w[1].z, w[1].w};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(v[i]);
+    }
+  }
+  // The largest magnitude's bits, as a float's: a NaN's are above every number's.
+  __device__ __forceinline__ uint32_t top() const {
+    if constexpr (sizeof(T) == 2) {
+      uint32_t m = 0;   // of each half; as integers, since they are magnitudes
+      const uint32_t v[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) m = __vmaxu2(m, v[i] & 0x7fff7fffu);
+      return max(m << 16, m & 0xffff0000u);
+    } else {
+      uint32_t m = 0;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        m = max(max(m, max(w[i].x & 0x7fffffffu, w[i].y & 0x7fffffffu)), max(w[i].z & 0x7fffffffu, w[i].w & 0x7fffffffu));
+      return m;
+    }
+  }
+};
 __device__ __forceinline__ void store8(__nv_bfloat16* p, const float* x) {
   uint32_t w[4];
 #pragma unroll
@@ -55,19 +86,16 @@ __device__ __forceinline__ void store8(float* p, const float* x) {
 }
 
 // Codes + 8 of this lane's eight features, and the group's scale (bits of a bf16).
-__device__ __forceinline__ uint32_t quantise8(const float* x, uint32_t* code) {
-  // the maximum of the magnitudes' bits: a NaN's are above every number's
-  uint32_t m = 0;
+// The quotient of bf16 inputs: x (1/s), then one residual step (Markstein's correction), which is
+// exact where x / s is a half-integer; where it is not, it is at least 2^-12 away from one (8-bit
+// significands), so the code is that of the exact quotient.  fp32 inputs take the IEEE division.
+// `code` holds them as integers plus a multiple of 2^16 (of 2^20 and more once shifted): only the low
+// 16 bits of a sum of four, shifted by nibbles, count.
+template <typename T>
+__device__ __forceinline__ uint32_t quantise8(const Raw<T>& raw, uint32_t* code) {
+  uint32_t m = raw.top();
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t a = __float_as_uint(x[i]) & 0x7fffffffu;
-    m = a > m ? a : m;
-  }
-#pragma unroll
-  for (int o = 1; o < 4; o <<= 1) {
-    const uint32_t a = __shfl_xor_sync(0xffffffffu, m, o);
-    m = a > m ? a : m;
-  }
+  for (int o = 1; o < 4; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
   uint32_t bits = 0x7fc0u;
   float s = 0.f;
   if (m < 0x7f800000u) {
@@ -75,152 +103,262 @@ __device__ __forceinline__ uint32_t quantise8(const float* x, uint32_t* code) {
     bits = __bfloat16_as_ushort(h);
     s = __bfloat162float(h);
   }
+  float x[8];
+  raw.widen(x);
+  // rint and the bias of 8 at once: 1.5 * 2^23 + 8 makes an integer of the sum, ties to even
+  constexpr float kRound = 12582920.f;
+  if (sizeof(T) == 2 && s > 1.2e-38f && s < 8.0e37f) {   // 1/s is a normal number
+    const float inv = __frcp_rn(s);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    float c = 0.f;
-    if (s > 0.f) c = fminf(fmaxf(rintf(__fdiv_rn(x[i], s)), -7.f), 7.f);
-    code[i] = uint32_t(int(c) + 8);
+    for (int i = 0; i < 8; ++i) {
+      // |x / s| <= 7 (1 + 2^-8): the code needs no bound
+      const float q = x[i] * inv;
+      code[i] = __float_as_uint(fmaf(fmaf(-q, s, x[i]), inv, q) + kRound);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float q = s > 0.f ? __fdiv_rn(x[i], s) : 0.f;
+      code[i] = __float_as_uint(fminf(fmaxf(q, -7.f), 7.f) + kRound);
+    }
   }
   return bits;
+}
+// Four codes as a 16-bit word.
+__device__ __forceinline__ uint32_t pack4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return a + (b << 4) + (c << 8) + (d << 12);
 }
 
 struct Dims {
   int64_t B, N;
   int64_t n_pages, max_pages;
-  int64_t rows;     // B * H * N
+  uint32_t units;   // of a sequence: 16 tokens each, the first one short of the first position's offset
+  uint32_t all;     // units of all sequences
+  bool flat;        // short sequences: a unit is 16 tokens of any
   int H, page, dk, dv;
+  int hp;           // heads of a CTA
 };
 
-// The 16-token block that holds position `at` of sequence b for head h, or null: at < 0 (padding)
-// or, with the status word set, a position or page outside its table.
-__device__ __forceinline__ uint8_t* find_block(uint8_t* pool, const int32_t* table, const Dims& p,
-                                               int64_t b, int h, int32_t at, bool report) {
-  if (at < 0) return nullptr;
-  const int64_t slot = at / p.page;
-  int32_t page = -1;
-  if (slot < p.max_pages) page = table[b * p.max_pages + slot];
-  if (page < 0 || page >= p.n_pages) {
-    if (report) atomicExch(&g_moa_kv4_status, kErrIndex);
-    return nullptr;
+// A thread's row: which unit of the CTA, which row of the unit, where it lies in the cache.
+template <int LPR>
+struct Row {
+  static constexpr int kUnits = kThreads / (kBlock * LPR);   // units of a CTA
+  int lane, i, unit;        // lane of the row, row of the unit, unit of the CTA
+  bool live;                // the row exists
+  bool whole;               // the unit is one whole block
+  int64_t b, n;
+  int tok;
+  int32_t at;
+  uint8_t* block;           // of head 0; null: padding or (with the status word set) no such place
+  __device__ __forceinline__ Row(uint8_t* pool, const int32_t* table, const int32_t* pos, const Dims& p) {
+    __shared__ const uint8_t* s_block[kUnits][kBlock];
+    lane = threadIdx.x % LPR;
+    i = threadIdx.x / LPR % kBlock;
+    unit = threadIdx.x / (LPR * kBlock);
+    const uint32_t u = blockIdx.x * kUnits + unit;
+    if (p.flat) {
+      const uint64_t token = uint64_t(u) * kBlock + i;
+      live = token < uint64_t(p.B) * p.N;
+      b = live ? uint32_t(token) / uint32_t(p.N) : 0;
+      n = live ? int64_t(token) - b * p.N : 0;
+    } else {
+      b = u / p.units;
+      live = u < p.all;
+      const int32_t first = live ? pos[b * p.N] : 0;
+      n = int64_t(u - uint32_t(b) * p.units) * kBlock - (first & (kBlock - 1)) + i;
+      live = live && n >= 0 && n < p.N;
+    }
+    at = live ? pos[b * p.N + n] : -1;
+    tok = at & (kBlock - 1);
+    block = nullptr;
+    if (at >= 0) {
+      const uint32_t slot = uint32_t(at) / uint32_t(p.page);
+      int32_t page = -1;
+      if (slot < p.max_pages) page = table[b * p.max_pages + slot];
+      if (page >= 0 && page < p.n_pages)
+        block = pool + (int64_t(page) * p.H * (p.page / kBlock) + (uint32_t(at) - slot * p.page) / kBlock) * block_bytes(p.dk, p.dv);
+      else if (lane == 0)
+        atomicExch(&g_moa_kv4_status, kErrIndex);
+    }
+    // whole: each of the 16 rows in its own place of the same block
+    if (lane == 0) s_block[unit][i] = tok == i ? block : nullptr;
+    __syncthreads();
+    whole = s_block[unit][0] != nullptr;
+#pragma unroll
+    for (int k = 1; k < kBlock; ++k) whole = whole && s_block[unit][k] == s_block[unit][0];
   }
-  const int64_t blocks = p.page / kBlock;
-  const int64_t i = (int64_t(page) * p.H + h) * blocks + (at - int32_t(slot) * p.page) / kBlock;
-  return pool + i * block_bytes(p.dk, p.dv);
-}
+};
+
+constexpr int kMostBytes = block_bytes(128, 128);
 
 template <typename T, int LPR>
 __global__ void __launch_bounds__(kThreads)
 kv4_write_kernel(View k, View v, uint8_t* pool, const int32_t* table, const int32_t* pos, Dims p) {
+  constexpr int kUnits = Row<LPR>::kUnits, kTeam = LPR * kBlock;   // threads of a unit
+  __shared__ __align__(16) uint8_t s_bytes[2][kUnits][kMostBytes];
   wait_for_previous();
-  const int lane = threadIdx.x % LPR;
-  const int64_t row = int64_t(blockIdx.x) * (kThreads / LPR) + threadIdx.x / LPR;
-  const bool live = row < p.rows;
-  const int64_t n = live ? row % p.N : 0, bh = live ? row / p.N : 0;
-  const int h = int(bh % p.H);
-  const int64_t b = bh / p.H;
-  const int32_t at = live ? pos[b * p.N + n] : -1;
-  uint8_t* block = find_block(pool, table, p, b, h, at, lane == 0);
-  const int tok = at & (kBlock - 1);
-  const int f0 = lane * 8, g = lane >> 2, t = lane & 3;
+  const Row<LPR> r(pool, table, pos, p);
+  const int f0 = r.lane * 8, g = r.lane >> 2, t = r.lane & 3;
+  const int bytes = block_bytes(p.dk, p.dv), gk = p.dk / kGroup, gv = p.dv / kGroup;
+  const int64_t head_bytes = int64_t(p.page / kBlock) * bytes;
+  const bool mine_k = r.block != nullptr && f0 < p.dk, mine_v = r.block != nullptr && f0 < p.dv;
+  const int h0 = int(blockIdx.y) * p.hp, h1 = min(h0 + p.hp, p.H);
+  const T* from_k = static_cast<const T*>(k.p) + r.b * k.sb + r.n * k.sn + f0;
+  const T* from_v = static_cast<const T*>(v.p) + r.b * v.sb + r.n * v.sn + f0;
+  // where this lane's words lie in a block
+  const int at_k = key_word(r.tok, t, g, gk), at_ks = key_scales(p.dk, p.dv) + (r.tok * gk + g) * 2;
+  const int at_v = value_word(p.dk, r.tok, 2 * t, g, gv) + (r.tok & 1) * 2;
+  const int at_v1 = value_word(p.dk, r.tok, 2 * t + 1, g, gv) + (r.tok & 1) * 2;
+  const int at_vs = value_scales(p.dk, p.dv) + (r.tok * gv + g) * 2;
+  Raw<T> xk, xv;
+  xk.load(mine_k ? from_k + h0 * k.sh : nullptr);
+  xv.load(mine_v ? from_v + h0 * v.sh : nullptr);
+  for (int h = h0; h < h1; ++h) {
+    const Raw<T> ck = xk, cv = xv;
+    if (h + 1 < h1) {
+      xk.load(mine_k ? from_k + (h + 1) * k.sh : nullptr);
+      xv.load(mine_v ? from_v + (h + 1) * v.sh : nullptr);
+    }
+    uint8_t* block = r.block + h * head_bytes;
+    uint8_t* to = r.whole ? s_bytes[h & 1][r.unit] : block;
+    uint32_t c[8];
+    uint32_t s = quantise8<T>(ck, c);
+    if (mine_k) {
+      *reinterpret_cast<uint32_t*>(to + at_k) = __byte_perm(pack4(c[0], c[2], c[4], c[6]), pack4(c[1], c[3], c[5], c[7]), 0x5410);
+      if (t == 0) *reinterpret_cast<uint16_t*>(to + at_ks) = uint16_t(s);
+    }
+    s = quantise8<T>(cv, c);
+    if (mine_v) {
+      *reinterpret_cast<uint16_t*>(to + at_v) = uint16_t(pack4(c[0], c[1], c[2], c[3]));
+      *reinterpret_cast<uint16_t*>(to + at_v1) = uint16_t(pack4(c[4], c[5], c[6], c[7]));
+      if (t == 0) *reinterpret_cast<uint16_t*>(to + at_vs) = uint16_t(s);
+    }
+    __syncthreads();   // the block is together (the other buffer's copies were read before this)
+    if (r.whole)
+      for (int i = (threadIdx.x % kTeam) * 16; i < bytes; i += kTeam * 16)
+        *reinterpret_cast<uint4*>(block + i) = *reinterpret_cast<const uint4*>(s_bytes[h & 1][r.unit] + i);
+  }
+}
+
+// Code pairs (nibbles 4 j and 4 j + 16 of w, less 8) times the scale, rounded to bf16 once: the codes
+// are exact in bf16, and the product of two bf16 values is rounded from the exact one.
+__device__ __forceinline__ uint32_t scaled_pair(uint32_t w, int j, __nv_bfloat162 s) {
+  uint32_t x = (w >> (4 * j) & 0x000f000fu) | 0x43004300u;   // 128 + n
+  const __nv_bfloat162 bias = __halves2bfloat162(__ushort_as_bfloat16(0x4308), __ushort_as_bfloat16(0x4308));
+  const __nv_bfloat162 y = __hmul2(__hsub2(*reinterpret_cast<__nv_bfloat162*>(&x), bias), s);
+  return *reinterpret_cast<const uint32_t*>(&y);
+}
+// Eight features of w's nibbles in the keys' order (even features in the low half) to p.
+__device__ __forceinline__ void store_scaled(__nv_bfloat16* p, uint32_t w, uint32_t s) {
+  const __nv_bfloat162 s2 = __halves2bfloat162(__ushort_as_bfloat16(uint16_t(s)), __ushort_as_bfloat16(uint16_t(s)));
+  *reinterpret_cast<uint4*>(p) =
+      make_uint4(scaled_pair(w, 0, s2), scaled_pair(w, 1, s2), scaled_pair(w, 2, s2), scaled_pair(w, 3, s2));
+}
+__device__ __forceinline__ void store_scaled(float* p, uint32_t w, uint32_t s) {
+  const float scale = __uint_as_float(s << 16);
   float x[8];
-  uint32_t c[8];
-  {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = 0.f;
-    const bool mine = block != nullptr && f0 < p.dk;
-    if (mine) load8(static_cast<const T*>(k.p) + b * k.sb + h * k.sh + n * k.sn + f0, x);
-    const uint32_t s = quantise8(x, c);
-    if (mine) {
-      const int groups = p.dk / kGroup;
-      *reinterpret_cast<uint32_t*>(block + key_word(tok, t, g, groups)) =
-          c[0] | c[2] << 4 | c[4] << 8 | c[6] << 12 | c[1] << 16 | c[3] << 20 | c[5] << 24 | c[7] << 28;
-      if (t == 0)
-        *reinterpret_cast<uint16_t*>(block + key_scales(p.dk, p.dv) + (tok * groups + g) * 2) = uint16_t(s);
-    }
-  }
-  {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = 0.f;
-    const bool mine = block != nullptr && f0 < p.dv;
-    if (mine) load8(static_cast<const T*>(v.p) + b * v.sb + h * v.sh + n * v.sn + f0, x);
-    const uint32_t s = quantise8(x, c);
-    if (mine) {
-      const int groups = p.dv / kGroup;
-      uint8_t* w = block + value_word(p.dk, tok, 2 * t, g, groups) + (tok & 1) * 2;
-      *reinterpret_cast<uint16_t*>(w) = uint16_t(c[0] | c[1] << 4 | c[2] << 8 | c[3] << 12);
-      w = block + value_word(p.dk, tok, 2 * t + 1, g, groups) + (tok & 1) * 2;
-      *reinterpret_cast<uint16_t*>(w) = uint16_t(c[4] | c[5] << 4 | c[6] << 8 | c[7] << 12);
-      if (t == 0)
-        *reinterpret_cast<uint16_t*>(block + value_scales(p.dk, p.dv) + (tok * groups + g) * 2) = uint16_t(s);
-    }
-  }
+  for (int e = 0; e < 8; ++e) x[e] = float(int((w >> (16 * (e & 1) + 4 * (e >> 1))) & 15u) - 8) * scale;
+  store8(p, x);
+}
+// The same order from the values' two 16-bit words (features 0-3 and 4-7): evens low, odds high.
+__device__ __forceinline__ uint32_t reorder(uint32_t a, uint32_t b) {
+  const uint32_t even = (a & 0x000fu) | (a >> 4 & 0x00f0u) | (b & 0x000fu) << 8 | (b >> 4 & 0x00f0u) << 8;
+  const uint32_t odd = (a >> 4 & 0x000fu) | (a >> 8 & 0x00f0u) | (b >> 4 & 0x000fu) << 8 | (b >> 8 & 0x00f0u) << 8;
+  return even | odd << 16;
+}
+__device__ __forceinline__ void store_all(__nv_bfloat16* p, float x) {
+  const float y[8] = {x, x, x, x, x, x, x, x};
+  store8(p, y);
+}
+__device__ __forceinline__ void store_all(float* p, float x) {
+  const float y[8] = {x, x, x, x, x, x, x, x};
+  store8(p, y);
 }
 
 template <typename T, int LPR>
 __global__ void __launch_bounds__(kThreads)
 kv4_read_kernel(View k, View v, uint8_t* pool, const int32_t* table, const int32_t* pos, Dims p) {
+  constexpr int kUnits = Row<LPR>::kUnits, kTeam = LPR * kBlock;
+  __shared__ __align__(16) uint8_t s_bytes[2][kUnits][kMostBytes];
   wait_for_previous();
-  const int lane = threadIdx.x % LPR;
-  const int64_t row = int64_t(blockIdx.x) * (kThreads / LPR) + threadIdx.x / LPR;
-  if (row >= p.rows) return;
-  const int64_t n = row % p.N, bh = row / p.N;
-  const int h = int(bh % p.H);
-  const int64_t b = bh / p.H;
-  const int32_t at = pos[b * p.N + n];
-  const uint8_t* block = find_block(pool, table, p, b, h, at, lane == 0);
-  const int tok = at & (kBlock - 1);
-  const int f0 = lane * 8, g = lane >> 2, t = lane & 3;
-  const float fill = at < 0 ? 0.f : __int_as_float(0x7fc00000);  // padding, or no such place
-  float x[8];
-  if (f0 < p.dk) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = fill;
-    if (block != nullptr) {
-      const int groups = p.dk / kGroup;
-      const uint32_t w = *reinterpret_cast<const uint32_t*>(block + key_word(tok, t, g, groups));
-      const uint32_t s = *reinterpret_cast<const uint16_t*>(block + key_scales(p.dk, p.dv) + (tok * groups + g) * 2);
-      const float scale = __uint_as_float(s << 16);
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        x[e] = float(int((w >> (16 * (e & 1) + 4 * (e >> 1))) & 15u) - 8) * scale;
+  const Row<LPR> r(pool, table, pos, p);
+  const int f0 = r.lane * 8, g = r.lane >> 2, t = r.lane & 3;
+  const int bytes = block_bytes(p.dk, p.dv), gk = p.dk / kGroup, gv = p.dv / kGroup;
+  const int64_t head_bytes = int64_t(p.page / kBlock) * bytes;
+  const int h0 = int(blockIdx.y) * p.hp, h1 = min(h0 + p.hp, p.H);
+  T* to_k = static_cast<T*>(k.p) + r.b * k.sb + r.n * k.sn + f0;
+  T* to_v = static_cast<T*>(v.p) + r.b * v.sb + r.n * v.sn + f0;
+  const bool mine_k = r.live && f0 < p.dk, mine_v = r.live && f0 < p.dv;
+  const int at_k = key_word(r.tok, t, g, gk), at_ks = key_scales(p.dk, p.dv) + (r.tok * gk + g) * 2;
+  const int at_v = value_word(p.dk, r.tok, 2 * t, g, gv) + (r.tok & 1) * 2;
+  const int at_v1 = value_word(p.dk, r.tok, 2 * t + 1, g, gv) + (r.tok & 1) * 2;
+  const int at_vs = value_scales(p.dk, p.dv) + (r.tok * gv + g) * 2;
+  // a whole block: 16 bytes a thread, the next head's on their way while one is taken apart (a team
+  // of 128 threads or more covers a block of its width in two pieces at most)
+  const int i0 = (threadIdx.x % kTeam) * 16, i1 = i0 + kTeam * 16;
+  uint4 a = make_uint4(0, 0, 0, 0), b = a;
+  auto fetch = [&](int h) {
+    const uint8_t* block = r.block + h * head_bytes;
+    if (i0 < bytes) a = *reinterpret_cast<const uint4*>(block + i0);
+    if (i1 < bytes) b = *reinterpret_cast<const uint4*>(block + i1);
+  };
+  if (r.whole) fetch(h0);
+  for (int h = h0; h < h1; ++h) {
+    const uint8_t* from = r.block + h * head_bytes;
+    if (r.whole) {
+      uint8_t* at = s_bytes[h & 1][r.unit];
+      if (i0 < bytes) *reinterpret_cast<uint4*>(at + i0) = a;
+      if (i1 < bytes) *reinterpret_cast<uint4*>(at + i1) = b;
+      if (h + 1 < h1) fetch(h + 1);
+      from = at;
     }
-    store8(static_cast<T*>(k.p) + b * k.sb + h * k.sh + n * k.sn + f0, x);
-  }
-  if (f0 < p.dv) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = fill;
-    if (block != nullptr) {
-      const int groups = p.dv / kGroup;
-      const uint32_t s = *reinterpret_cast<const uint16_t*>(block + value_scales(p.dk, p.dv) + (tok * groups + g) * 2);
-      const float scale = __uint_as_float(s << 16);
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const uint32_t w = *reinterpret_cast<const uint16_t*>(
-            block + value_word(p.dk, tok, 2 * t + c, g, groups) + (tok & 1) * 2);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[4 * c + j] = float(int((w >> (4 * j)) & 15u) - 8) * scale;
-      }
+    __syncthreads();
+    if (r.block == nullptr) {   // padding: zeros; no such place: NaN
+      const float fill = r.at < 0 ? 0.f : __int_as_float(0x7fc00000);
+      if (mine_k) store_all(to_k + h * k.sh, fill);
+      if (mine_v) store_all(to_v + h * v.sh, fill);
+      continue;
     }
-    store8(static_cast<T*>(v.p) + b * v.sb + h * v.sh + n * v.sn + f0, x);
+    if (mine_k)
+      store_scaled(to_k + h * k.sh, *reinterpret_cast<const uint32_t*>(from + at_k), *reinterpret_cast<const uint16_t*>(from + at_ks));
+    if (mine_v)
+      store_scaled(to_v + h * v.sh, reorder(*reinterpret_cast<const uint16_t*>(from + at_v), *reinterpret_cast<const uint16_t*>(from + at_v1)),
+                   *reinterpret_cast<const uint16_t*>(from + at_vs));
   }
 }
 
 template <typename T, int LPR>
-cudaError_t run(const Kv4MoveArgs& a, const Dims& p, bool write, int64_t grid) {
+cudaError_t run(const Kv4MoveArgs& a, const Dims& p, bool write, dim3 grid) {
   uint8_t* pool = static_cast<uint8_t*>(a.c.pool);
-  return launch_overlapped(write ? kv4_write_kernel<T, LPR> : kv4_read_kernel<T, LPR>, dim3(unsigned(grid)),
+  return launch_overlapped(write ? kv4_write_kernel<T, LPR> : kv4_read_kernel<T, LPR>, grid,
                            dim3(kThreads), 0, a.stream, a.k, a.v, pool, a.c.table, a.pos, p);
 }
 
 int launch(const Kv4MoveArgs& a, bool write, char* msg, size_t msglen) {
-  Dims p{a.B, a.N, a.c.n_pages, a.c.max_pages, a.B * a.c.H * a.N, a.c.H, a.c.page, a.c.dk, a.c.dv};
+  int sms = 0;
+  cudaError_t e = device_sm_count(&sms);
+  if (e != cudaSuccess) {
+    snprintf(msg, msglen, "cache: SM count: %s", cudaGetErrorString(e));
+    return 5;
+  }
+  // Sequences shorter than two blocks hardly fill any: their tokens are taken 16 at a time whosever
+  // they are.  Positions that begin inside a block may need one unit more.
+  const bool flat = a.N < 2 * kBlock;
+  const int64_t units = flat ? 0 : (a.N + 2 * kBlock - 2) / kBlock;
+  const int64_t all = flat ? (a.B * a.N + kBlock - 1) / kBlock : a.B * units;
   const int lpr = a.c.dk <= 64 && a.c.dv <= 64 ? 8 : 16;
-  const int64_t grid = (p.rows + kThreads / lpr - 1) / (kThreads / lpr);
-  if (grid > 0x7fffffffLL) {
+  const int64_t per = kThreads / (lpr * kBlock), x = (all + per - 1) / per;
+  if (all > 0x7fffffffLL || (flat && a.B * a.N > 0x7fffffffLL)) {
     snprintf(msg, msglen, "cache: too many rows for one launch");
     return 3;
   }
-  cudaError_t e;
+  // heads of a CTA: all of them, unless that leaves SMs with less than eight CTAs
+  int hp = a.c.H;
+  while (hp > 1 && x * ((a.c.H + hp - 1) / hp) < int64_t(sms) * 8) hp = (hp + 1) / 2;
+  while ((a.c.H + hp - 1) / hp > 65535) hp *= 2;
+  const Dims p{a.B, a.N, a.c.n_pages, a.c.max_pages, uint32_t(units), uint32_t(all), flat, a.c.H, a.c.page, a.c.dk, a.c.dv, hp};
+  const dim3 grid(unsigned(x), unsigned((a.c.H + hp - 1) / hp));
   if (a.f32)
     e = lpr == 8 ? run<float, 8>(a, p, write, grid) : run<float, 16>(a, p, write, grid);
   else
