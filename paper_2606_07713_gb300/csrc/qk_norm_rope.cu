@@ -12,8 +12,10 @@
 // dx written), with about ten operations for each.
 //
 // Layout of the work: a group of 8, 16 or 32 lanes owns one token and walks over a range of its
-// heads, eight features a lane (one 16-byte load of bf16, two of fp32).  The token's cosines and
-// sines are loaded once and serve all heads of the range.
+// heads, eight features a lane (one 16-byte load of bf16, two of fp32), in batches whose rows are all
+// on their way before the first is used.  The token's cosines and sines are loaded once and serve all
+// heads of the range; with halves, the other member of a lane's pairs comes by a shuffle of the row as
+// it lies in memory.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -45,6 +47,43 @@ __device__ __forceinline__ void load8(const float* p, float* x) {
   const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
   x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
 }
+// A lane's features as they lie in memory, so that several rows can be on their way at once.
+template <typename T>
+struct Raw {
+  uint4 w[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < int(sizeof(T) / 2); ++i) w[i] = reinterpret_cast<const uint4*>(p)[i];
+  }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < int(sizeof(T) / 2); ++i) w[i] = make_uint4(0, 0, 0, 0);
+  }
+  // Those of lane `from` of the group.
+  template <int LPR>
+  __device__ __forceinline__ Raw of(int from) const {
+    Raw r;
+#pragma unroll
+    for (int i = 0; i < int(sizeof(T) / 2); ++i)
+      r.w[i] = make_uint4(__shfl_sync(0xffffffffu, w[i].x, from, LPR), __shfl_sync(0xffffffffu, w[i].y, from, LPR),
+                          __shfl_sync(0xffffffffu, w[i].z, from, LPR), __shfl_sync(0xffffffffu, w[i].w, from, LPR));
+    return r;
+  }
+  __device__ __forceinline__ void widen(float* x) const {
+    if constexpr (sizeof(T) == 2) {
+      const uint32_t v[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(v[i] << 16);
+        x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+      }
+    } else {
+      const uint32_t v[8] = {w[0].x, w[0].y, w[0].z, w[0].w, w[sizeof(T) / 2 - 1].x, w[sizeof(T) / 2 - 1].y, w[sizeof(T) / 2 - 1].z, w[sizeof(T) / 2 - 1].w};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(v[i]);
+    }
+  }
+};
 __device__ __forceinline__ void store8(__nv_bfloat16* p, const float* x) {
   uint32_t w[4];
 #pragma unroll
@@ -73,22 +112,14 @@ struct Turn {
   float c[kV], s[kV];
 };
 
-// Turned features: y = x * c + partner * s, where s carries the sign of the member.
-template <int LPR, bool PAIRS>
-__device__ __forceinline__ void turn(float* x, const Turn& t, int partner) {
+// The other members of this lane's pairs.
+template <typename T, int LPR, bool PAIRS>
+__device__ __forceinline__ void others(const Raw<T>& raw, const float* x, int partner, float* o) {
   if constexpr (PAIRS) {
 #pragma unroll
-    for (int i = 0; i < kV; i += 2) {
-      const float a = x[i], b = x[i + 1];
-      x[i] = a * t.c[i] + b * t.s[i];
-      x[i + 1] = b * t.c[i + 1] + a * t.s[i + 1];
-    }
+    for (int i = 0; i < kV; ++i) o[i] = x[i ^ 1];
   } else {
-#pragma unroll
-    for (int i = 0; i < kV; ++i) {
-      const float o = __shfl_sync(0xffffffffu, x[i], partner, LPR);
-      x[i] = x[i] * t.c[i] + o * t.s[i];
-    }
+    raw.template of<LPR>(partner).widen(o);
   }
 }
 
@@ -100,6 +131,10 @@ struct Dims {
   int nq;            // ranges of query heads (the ranges of key heads follow)
   float eps;
 };
+
+__device__ __forceinline__ int64_t sequence_of(int64_t token, const Dims& p) {
+  return p.tokens <= 0x7fffffff ? uint32_t(token) / uint32_t(p.N) : token / p.N;
+}
 
 // The rotation of the token's position for this lane.  `dir` +1 forward, -1 backward.
 template <bool PAIRS>
@@ -133,10 +168,11 @@ __device__ __forceinline__ void load_turn(Turn& t, const float* cosines, const f
 }
 
 template <typename T, int LPR, bool PAIRS>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 4)
 norm_rope_kernel(View q, View k, View oq, View ok, const T* wq, const T* wk, const float* cosines,
                  const float* sines, const int32_t* pos, Dims p) {
   constexpr int kGroups = kThreads / LPR;
+  constexpr int kBatch = 2;
   wait_for_previous();
   const int lane = threadIdx.x % LPR;
   const int64_t token = int64_t(blockIdx.x) * kGroups + threadIdx.x / LPR;
@@ -148,50 +184,78 @@ norm_rope_kernel(View q, View k, View oq, View ok, const T* wq, const T* wk, con
   const int f0 = lane * kV;
   const bool live = token < p.tokens;
   const bool mine = live && f0 < p.d;
-  const int64_t b = live ? token / p.N : 0, n = live ? token % p.N : 0;
+  const int64_t b = live ? sequence_of(token, p) : 0, n = live ? token - b * p.N : 0;
+  const T* src = static_cast<const T*>(in.p) + b * in.sb + n * in.sn + f0;
+  T* dst = static_cast<T*>(out.p) + b * out.sb + n * out.sn + f0;
+  Raw<T> raw[kBatch];
+  auto fetch = [&](int hb) {
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      if (mine && hb + u < h1) raw[u].load(src + (hb + u) * in.sh);
+      else raw[u].zero();
+    }
+  };
+  fetch(h0);
   const int32_t at = live ? pos[token] : -1;
   const bool bad = live && at >= p.n_pos;
   if (bad && lane == 0) atomicExch(&g_moa_norm_status, kErrIndex);
-  Turn t;
-  load_turn<PAIRS>(t, cosines, sines, at >= 0 && !bad ? at : 0, p, f0, 1.f);
-  float w[kV];
-#pragma unroll
-  for (int i = 0; i < kV; ++i) w[i] = 0.f;
-  if (f0 < p.d) load8((is_q ? wq : wk) + f0, w);
   const int half_lanes = p.d_rot / 2 / kV;
   const int partner = f0 >= p.d_rot ? lane : (f0 < p.d_rot / 2 ? lane + half_lanes : lane - half_lanes);
-  const T* src = static_cast<const T*>(in.p) + b * in.sb + n * in.sn + f0;
-  T* dst = static_cast<T*>(out.p) + b * out.sb + n * out.sn + f0;
-  const float inv_d = 1.f / float(p.d);
-  for (int h = h0; h < h1; ++h) {
-    float x[kV];
+  // y = (x c w + o s w_o) r: the weights of both members go into the angles
+  Turn t;
+  load_turn<PAIRS>(t, cosines, sines, at >= 0 && !bad ? at : 0, p, f0, 1.f);
+  if (f0 < p.d) {
+    float w[kV];
+    const T* wp = is_q ? wq : wk;
+    load8(wp + f0, w);
 #pragma unroll
-    for (int i = 0; i < kV; ++i) x[i] = 0.f;
-    if (mine) load8(src + h * in.sh, x);
-    float ss = 0.f;
-#pragma unroll
-    for (int i = 0; i < kV; ++i) ss += x[i] * x[i];
-    const float r = 1.f / sqrtf(group_sum<LPR>(ss) * inv_d + p.eps);
-#pragma unroll
-    for (int i = 0; i < kV; ++i) x[i] = x[i] * r * w[i];
-    turn<LPR, PAIRS>(x, t, partner);
-    if (at < 0 || bad) {
-      const float fill = bad ? __int_as_float(0x7fc00000) : 0.f;
-#pragma unroll
-      for (int i = 0; i < kV; ++i) x[i] = fill;
+    for (int i = 0; i < kV; ++i) {
+      t.c[i] *= w[i];
+      if (PAIRS) t.s[i] *= w[i ^ 1];
     }
-    if (mine) store8(dst + h * out.sh, x);
+    if (!PAIRS) {
+      load8(wp + partner * kV, w);
+#pragma unroll
+      for (int i = 0; i < kV; ++i) t.s[i] *= w[i];
+    }
+  }
+  const float inv_d = 1.f / float(p.d);
+  for (int hb = h0; hb < h1; hb += kBatch) {
+    Raw<T> now[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) now[u] = raw[u];
+    if (hb + kBatch < h1) fetch(hb + kBatch);
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int h = hb + u;
+      if (h >= h1) break;
+      float x[kV], o[kV];
+      now[u].widen(x);
+      others<T, LPR, PAIRS>(now[u], x, partner, o);
+      float ss = 0.f;
+#pragma unroll
+      for (int i = 0; i < kV; ++i) ss += x[i] * x[i];
+      const float r = rsqrtf(group_sum<LPR>(ss) * inv_d + p.eps);
+#pragma unroll
+      for (int i = 0; i < kV; ++i) x[i] = (x[i] * t.c[i] + o[i] * t.s[i]) * r;
+      if (at < 0 || bad) {
+#pragma unroll
+        for (int i = 0; i < kV; ++i) x[i] = bad ? __int_as_float(0x7fc00000) : 0.f;
+      }
+      if (mine) store8(dst + h * out.sh, x);
+    }
   }
 }
 
 // The gradients: one launch for dx and, for each CTA, the sum of its rows' t x r; a second one
 // adds the CTAs' sums in a fixed order.
 template <typename T, int LPR, bool PAIRS>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 3 : 2)
 norm_rope_bwd_kernel(View q, View k, View gq, View gk, View oq, View ok, const T* wq, const T* wk,
                      const float* cosines, const float* sines, const int32_t* pos, float* partial,
                      Dims p) {
   constexpr int kGroups = kThreads / LPR;
+  constexpr int kBatch = sizeof(T) == 2 ? 2 : 1;
   __shared__ float sums[kGroups][LPR * kV];
   wait_for_previous();
   const int lane = threadIdx.x % LPR, group = threadIdx.x / LPR;
@@ -201,56 +265,88 @@ norm_rope_bwd_kernel(View q, View k, View gq, View gk, View oq, View ok, const T
   const int H = is_q ? p.Hq : p.Hk;
   const int h0 = range * p.hp, h1 = h0 + p.hp < H ? h0 + p.hp : H;
   const int f0 = lane * kV;
-  float w[kV], acc[kV];
+  float acc[kV];
+  Raw<T> wraw;
+  wraw.zero();
 #pragma unroll
-  for (int i = 0; i < kV; ++i) w[i] = acc[i] = 0.f;
-  if (f0 < p.d) load8((is_q ? wq : wk) + f0, w);
+  for (int i = 0; i < kV; ++i) acc[i] = 0.f;
+  if (f0 < p.d) wraw.load((is_q ? wq : wk) + f0);
   const int half_lanes = p.d_rot / 2 / kV;
   const int partner = f0 >= p.d_rot ? lane : (f0 < p.d_rot / 2 ? lane + half_lanes : lane - half_lanes);
   const float inv_d = 1.f / float(p.d);
+  // a token's position is read while the token before it is worked on
+  auto position = [&](int64_t token) { return token < p.tokens ? pos[token] : -1; };
+  int32_t next_at = position(int64_t(blockIdx.x) * kGroups + group);
   // every lane of a warp takes part in each turn of the loop (shuffles), whether its token exists
   for (int64_t base = int64_t(blockIdx.x) * kGroups; base < p.tokens; base += int64_t(gridDim.x) * kGroups) {
     const int64_t token = base + group;
     const bool live = token < p.tokens;
     const bool mine = live && f0 < p.d;
-    const int64_t b = live ? token / p.N : 0, n = live ? token % p.N : 0;
-    const int32_t at = live ? pos[token] : -1;
-    const bool bad = live && at >= p.n_pos;
-    if (bad && lane == 0) atomicExch(&g_moa_norm_status, kErrIndex);
-    const bool counts = mine && at >= 0 && !bad;
-    Turn t;
-    load_turn<PAIRS>(t, cosines, sines, at >= 0 && !bad ? at : 0, p, f0, -1.f);
+    const int64_t b = live ? sequence_of(token, p) : 0, n = live ? token - b * p.N : 0;
     const T* src = static_cast<const T*>(in.p) + b * in.sb + n * in.sn + f0;
     const T* gsrc = static_cast<const T*>(gin.p) + b * gin.sb + n * gin.sn + f0;
     T* dst = static_cast<T*>(out.p) + b * out.sb + n * out.sn + f0;
-    for (int h = h0; h < h1; ++h) {
-      float x[kV], g[kV];
+    Raw<T> xraw[kBatch], graw[kBatch];
+    auto fetch = [&](int hb) {
 #pragma unroll
-      for (int i = 0; i < kV; ++i) x[i] = g[i] = 0.f;
-      if (mine) {
-        load8(src + h * in.sh, x);
-        load8(gsrc + h * gin.sh, g);
+      for (int u = 0; u < kBatch; ++u) {
+        if (mine && hb + u < h1) {
+          xraw[u].load(src + (hb + u) * in.sh);
+          graw[u].load(gsrc + (hb + u) * gin.sh);
+        } else {
+          xraw[u].zero();
+          graw[u].zero();
+        }
       }
-      float ss = 0.f;
+    };
+    fetch(h0);
+    const int32_t at = next_at;
+    const bool bad = at >= p.n_pos;
+    if (bad && lane == 0) atomicExch(&g_moa_norm_status, kErrIndex);
+    const bool counts = at >= 0 && !bad;
+    Turn t;
+    load_turn<PAIRS>(t, cosines, sines, counts ? at : 0, p, f0, -1.f);
+    next_at = position(token + int64_t(gridDim.x) * kGroups);
+    for (int hb = h0; hb < h1; hb += kBatch) {
 #pragma unroll
-      for (int i = 0; i < kV; ++i) ss += x[i] * x[i];
-      const float r = 1.f / sqrtf(group_sum<LPR>(ss) * inv_d + p.eps);
-      turn<LPR, PAIRS>(g, t, partner);
-      float dot = 0.f;
+      for (int u = 0; u < kBatch; ++u) {
+        const int h = hb + u;
+        if (h >= h1) break;
+        float x[kV], g[kV], o[kV], w[kV];
+        xraw[u].widen(x);
+        graw[u].widen(g);
+        others<T, LPR, PAIRS>(graw[u], g, partner, o);
+        // the row's registers are free: the same place of the next batch
+        if (h + kBatch < h1 && mine) {
+          xraw[u].load(src + (h + kBatch) * in.sh);
+          graw[u].load(gsrc + (h + kBatch) * gin.sh);
+        }
+        float ss = 0.f;
 #pragma unroll
-      for (int i = 0; i < kV; ++i) {
-        x[i] *= r;
-        if (counts) acc[i] += g[i] * x[i];
-        g[i] *= w[i];
-        dot += g[i] * x[i];
+        for (int i = 0; i < kV; ++i) ss += x[i] * x[i];
+        const float r = rsqrtf(group_sum<LPR>(ss) * inv_d + p.eps);
+        wraw.widen(w);
+        float dot = 0.f;
+#pragma unroll
+        for (int i = 0; i < kV; ++i) {
+          const float turned = g[i] * t.c[i] + o[i] * t.s[i];
+          x[i] *= r;
+          o[i] = turned * x[i];
+          g[i] = w[i] * turned;
+          dot += g[i] * x[i];
+        }
+        const float mean = group_sum<LPR>(dot) * inv_d;
+#pragma unroll
+        for (int i = 0; i < kV; ++i) g[i] = r * (g[i] - x[i] * mean);
+        if (counts) {
+#pragma unroll
+          for (int i = 0; i < kV; ++i) acc[i] += o[i];
+        } else {
+#pragma unroll
+          for (int i = 0; i < kV; ++i) g[i] = bad ? __int_as_float(0x7fc00000) : 0.f;
+        }
+        if (mine) store8(dst + h * out.sh, g);
       }
-      const float mean = group_sum<LPR>(dot) * inv_d;
-#pragma unroll
-      for (int i = 0; i < kV; ++i) {
-        x[i] = r * (g[i] - x[i] * mean);
-        if (at < 0 || bad) x[i] = bad ? __int_as_float(0x7fc00000) : 0.f;
-      }
-      if (mine) store8(dst + h * out.sh, x);
     }
   }
 #pragma unroll
@@ -292,34 +388,36 @@ norm_rope_bwd_sum_kernel(const float* partial, float* dwq, float* dwk, int64_t r
 
 int lanes_per_row(int64_t d) { return d <= 64 ? 8 : d <= 128 ? 16 : 32; }
 
-// Heads of one range: as many as leave every SM about 2048 threads, eight at most (the token's
-// angles, 64 bytes a lane, are then a quarter of the loads of a bf16 row's lane).
-int heads_per_range(int64_t tokens, int64_t Hq, int64_t Hk, int lpr, int sms) {
-  const int64_t groups = int64_t(sms) * 2048 / lpr;
-  int64_t hp = tokens * (Hq + Hk) / groups;
-  const int64_t most = Hq > Hk ? Hq : Hk;
-  hp = hp < 1 ? 1 : hp > 8 ? 8 : hp;
-  return int(hp < most ? hp : most);
-}
-
 struct Grid {
   int64_t x;
   int y, hp, nq;
 };
+// Ranges of heads.  A range costs its heads and about one and a half more (the token's place, angles
+// and weights), a launch as many ranges as there are rounds of resident CTAs (four on an SM): the
+// number of heads with the smallest product is taken, sixteen at most.  On 4 x (16 + 16) heads x 2048
+// x 64, 1024 CTAs of 8 heads make two rounds and 512 of 16 make one: 15.7 and 14.3 us.
+// The backward's CTAs each leave one row of sums, so a few rounds of them walk over the tokens.
 Grid plan(int64_t tokens, int64_t Hq, int64_t Hk, int64_t d, int sms, bool bwd) {
-  const int lpr = lanes_per_row(d);
-  Grid g;
-  g.hp = heads_per_range(tokens, Hq, Hk, lpr, sms);
-  g.nq = int((Hq + g.hp - 1) / g.hp);
-  g.y = g.nq + int((Hk + g.hp - 1) / g.hp);
-  const int64_t per = kThreads / lpr;
-  g.x = (tokens + per - 1) / per;
-  if (bwd) {  // each CTA leaves one row of sums: a few waves of CTAs walk over the tokens
-    int64_t most = int64_t(sms) * 16 / g.y;
-    most = most < 1 ? 1 : most;
-    if (g.x > most) g.x = most;
+  const int64_t per = kThreads / lanes_per_row(d), x = (tokens + per - 1) / per;
+  const int64_t most = Hq > Hk ? Hq : Hk;
+  Grid best{};
+  double least = 0;
+  for (int64_t hp = 1; hp <= 16 && hp <= most; ++hp) {
+    Grid g;
+    g.hp = int(hp);
+    g.nq = int((Hq + hp - 1) / hp);
+    g.y = g.nq + int((Hk + hp - 1) / hp);
+    g.x = x;
+    const int64_t rounds = (x * g.y + sms * 4 - 1) / (sms * 4);
+    const double cost = double(rounds) * (double(hp) + 1.5);
+    if (best.hp == 0 || cost <= least) best = g, least = cost;
   }
-  return g;
+  if (bwd) {
+    int64_t limit = int64_t(sms) * 3 / best.y;
+    limit = limit < 1 ? 1 : limit;
+    if (best.x > limit) best.x = limit;
+  }
+  return best;
 }
 
 template <typename T, int LPR, bool PAIRS>
