@@ -132,7 +132,11 @@ __device__ __forceinline__ void split_pair(float x, float y, uint32_t* t) {
 
 constexpr int kUnit = 64;              // tokens of a unit of work
 constexpr int kUnitBlocks = kUnit / kBlock;
-constexpr int64_t kTcRows = 32;        // more bf16 query rows of a key head than this go to kv4_attn_tc.cu
+// An item costs about as much as this many units besides its tokens (places, queries, the join of
+// the warps): it counts for that many more, which come first and hold no tokens.  Without them a
+// share of short items takes several times as long as one of long items (48 sequences of 0 to 16384
+// tokens: 94 us with 0, 85 with 3, 81 with 5 to 8, 85 with 12).
+constexpr int kItemUnits = 6;
 constexpr float kSlack = 8.f;          // the running maximum may lag by this (log2): weights up to 2^8
 
 struct Params {
@@ -219,7 +223,8 @@ __device__ __forceinline__ int limit_of(int len, int r, const Params& p) {
 __device__ __forceinline__ int sequence_of(int pair, const Params& p) {
   return p.n_tiles == 1 ? pair : int(unsigned(pair) / unsigned(p.n_tiles));
 }
-// Units of an item of a pair (sequence, query tile): at least one, so that every item is written.
+// Units of tokens of an item of a pair (sequence, query tile): at least one, so that every item is
+// written.
 template <int NT>
 __device__ __forceinline__ int units_of(const int32_t* lens, int pair, const Params& p, bool report) {
   const int rows = int(p.N) * p.G, b = sequence_of(pair, p);
@@ -267,7 +272,7 @@ kv4_attn_kernel(const T* __restrict__ Q, const uint8_t* __restrict__ pool,
 
   // this CTA's share of all units, and the pair in which it begins
   int64_t sum = 0;
-  for (int i = threadIdx.x; i < p.n_pairs; i += kThreads) sum += units_of<NT>(lens, i, p, true);
+  for (int i = threadIdx.x; i < p.n_pairs; i += kThreads) sum += units_of<NT>(lens, i, p, true) + kItemUnits;
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
   if (lane == 0) scan[warp] = sum;
@@ -284,7 +289,7 @@ kv4_attn_kernel(const T* __restrict__ Q, const uint8_t* __restrict__ pool,
   int64_t done = 0;
   for (int base = 0; p.n_pairs > 1 && at < stop; base += kThreads) {
     const int i = base + threadIdx.x;
-    const int64_t mine = i < p.n_pairs ? int64_t(units_of<NT>(lens, i, p, false)) * p.Hk : 0;
+    const int64_t mine = i < p.n_pairs ? int64_t(units_of<NT>(lens, i, p, false) + kItemUnits) * p.Hk : 0;
     int64_t incl = mine;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -322,14 +327,22 @@ kv4_attn_kernel(const T* __restrict__ Q, const uint8_t* __restrict__ pool,
   uint32_t count = 0;     // tiles this warp has taken so far: its place in the ring and the phases
   bool ok = true;
   while (at < stop) {
-    // the item and this CTA's units of it
-    const int units = units_of<NT>(lens, pair, p, false);
+    // the item and this CTA's units of it: u0 to u1 of its units of tokens
+    const int units = units_of<NT>(lens, pair, p, false), counted = units + kItemUnits;
     const uint32_t local = uint32_t(at - before);
-    const int h = int(local / uint32_t(units));
-    const int u0 = int(local - uint32_t(h * units));
-    const int u1 = int(units - u0 < stop - at ? units : u0 + (stop - at));
-    const int64_t b = sequence_of(pair, p);
-    const int r0 = (pair - int(b) * p.n_tiles) * (8 * NT);
+    const int h = int(local / uint32_t(counted));
+    const int64_t item = before + int64_t(h) * counted;      // its first unit
+    const int64_t upto = item + counted < stop ? item + counted : stop;
+    const int u0 = max(0, int(at - item) - kItemUnits), u1 = max(0, int(upto - item) - kItemUnits);
+    at = upto;
+    const int this_pair = pair;
+    if (at == before + int64_t(counted) * p.Hk) {
+      before = at;
+      ++pair;
+    }
+    if (u0 == u1) continue;   // nothing of its tokens: the next CTA begins it
+    const int64_t b = sequence_of(this_pair, p);
+    const int r0 = (this_pair - int(b) * p.n_tiles) * (8 * NT);
     const int len = length_of(lens, b, p, false);
     const int last_row = r0 + 8 * NT < rows ? r0 + 8 * NT - 1 : rows - 1;
     const int all_limit = limit_of(len, r0, p);          // every row sees these
@@ -645,16 +658,10 @@ kv4_attn_kernel(const T* __restrict__ Q, const uint8_t* __restrict__ pool,
     }
     if (u0 == 0 && (by_item || !whole) && threadIdx.x == 0) {
       // the CTA that has the item's last unit
-      const int64_t last = before + int64_t(h + 1) * units - 1;
       uint32_t c = blockIdx.x;
-      while (shares.start(c + 1) <= last) ++c;
-      cuts[by_item ? uint32_t(pair) * p.Hk + h : blockIdx.x] =
-          Cut{pair, h, int(blockIdx.x), whole ? 0 : int(c - blockIdx.x) + 1};
-    }
-    at += u1 - u0;
-    if (at == before + int64_t(units) * p.Hk) {
-      before = at;
-      ++pair;
+      while (shares.start(c + 1) < item + counted) ++c;
+      cuts[by_item ? uint32_t(this_pair) * p.Hk + h : blockIdx.x] =
+          Cut{this_pair, h, int(blockIdx.x), whole ? 0 : int(c - blockIdx.x) + 1};
     }
     // the joined values have been read: copies may write the memory again
     __syncthreads();
@@ -788,10 +795,21 @@ cudaError_t run_d(const Kv4AttnArgs& a, const Kv4Plan& plan, const Params& p) {
 
 }  // namespace
 
+// Whether many query rows are faster through kv4_attn_tc.cu.  This file's kernel widens codes once for
+// every 32 rows: 8 us + 0.08 ns for each cached token of a head and 32 rows.  The other one widens
+// once for all, in a launch of its own: 22 us + 0.13 ns for each, + 0.076 ns for each 256 rows.
+// Measured, 8 key heads (this file's, the other's, us): 64 rows x 8192 tokens 22, 37; 128 x 8192 34,
+// 38; 128 x 65536 165, 130; 256 x 8192 51, 42; 512 x 600 22, 28; 2048 x 600 42, 34.
+bool widening_pays(int64_t heads, int64_t rows, int64_t max_len) {
+  const double tokens = double(heads) * double(max_len);
+  const double n32 = double((rows + 31) / 32), n256 = double((rows + 255) / 256);
+  return tokens * (0.08 * n32 - 0.13 - 0.076 * n256) > 14000.0;
+}
+
 Kv4Plan kv4_attn_plan(int64_t B, int64_t Hk, int64_t G, int64_t N, int64_t max_len, bool f32, int sms) {
   Kv4Plan p;
   const int64_t rows = G * N;
-  p.tc = !f32 && rows > kTcRows;
+  p.tc = !f32 && widening_pays(B * Hk, rows, max_len);
   p.rows_tile = rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
   p.n_tiles = (rows + p.rows_tile - 1) / p.rows_tile;
   // resident CTAs, but none with less than two units if every length is max_len
@@ -817,7 +835,7 @@ int launch_kv4_attn(const Kv4AttnArgs& a, const Kv4Plan& plan, char* msg, size_t
   p.Hk = a.c.H, p.G = int(a.Hq / a.c.H);
   p.blocks_per_page = a.c.page / kv4::kBlock;
   p.n_tiles = int(plan.n_tiles), p.n_pairs = int(a.B * plan.n_tiles);
-  if ((a.max_len / kUnit + 1) * a.c.H > 0x7fffffffLL) {
+  if ((a.max_len / kUnit + 1 + kItemUnits) * a.c.H > 0x7fffffffLL) {
     snprintf(msg, msglen, "cache attention: max_len times the key heads is too large");
     return 3;
   }

@@ -61,6 +61,9 @@ using namespace tc;
 constexpr int kBM = 128;              // query rows of a row tile (= TMEM lanes)
 constexpr int kRows = 2 * kBM;        // query rows of a work item
 constexpr int kBN = 128;              // tokens of a tile
+// A work item costs about as much as this many tiles besides its own (queries, the pipeline's filling,
+// its output): it counts for that many more, which come first and hold no tokens.
+constexpr int kItemUnits = 4;
 constexpr int kThreads = 384;
 constexpr int kMmaWarp0 = 8, kLoadWarp = 9, kMmaWarp1 = 10, kWalkWarp = 11;
 constexpr float kRescaleLog2 = 8.f;   // the running maximum may lag by this: weights up to 2^8
@@ -369,7 +372,7 @@ kv4_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   // this CTA's share of all units, and the item in which it begins
   const int n_items = p.n_bh * p.n_tiles;
   int64_t sum = 0;
-  for (int i = threadIdx.x; i < n_items; i += kThreads) sum += units_of(lens, i, p, true);
+  for (int i = threadIdx.x; i < n_items; i += kThreads) sum += units_of(lens, i, p, true) + kItemUnits;
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
   if (lane == 0) scan[warp] = sum;
@@ -383,7 +386,7 @@ kv4_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   int64_t done = 0;
   for (int base = 0; first_unit < stop; base += kThreads) {
     const int i = base + threadIdx.x;
-    const int64_t mine = i < n_items ? units_of(lens, i, p, false) : 0;
+    const int64_t mine = i < n_items ? units_of(lens, i, p, false) + kItemUnits : 0;
     int64_t incl = mine;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -558,25 +561,26 @@ kv4_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         before = found[1];
       }
       for (uint32_t seg = 0;; ++seg) {
+        int units = 0, u0 = 0, u1 = 0, which = -1;
+        while (at < stop && u0 == u1) {   // (nothing of an item's tiles: the next CTA begins it)
+          units = units_of(lens, item, p, false);
+          const int64_t end = before + units + kItemUnits, upto = end < stop ? end : stop;
+          u0 = max(0, int(at - before) - kItemUnits), u1 = max(0, int(upto - before) - kItemUnits);
+          if (u0 < u1) which = item;
+          if (u0 == 0 && u1 > 0 && u1 < units) {   // begun here, ended by a later CTA
+            uint32_t c = blockIdx.x;
+            while (shares.start(c + 1) < end) ++c;
+            cuts[blockIdx.x] = Cut{item, int(c - blockIdx.x) + 1};
+          }
+          at = upto;
+          before = end;
+          ++item;
+        }
         if (seg >= 2 && !wait_bounded(item_empty(seg & 1), ((seg >> 1) - 1) & 1u, wc)) break;
         volatile Item& x = items[seg & 1];
-        if (at >= stop) {
-          x.item = -1;
-          mbar_arrive(item_full(seg & 1));
-          break;
-        }
-        const int units = units_of(lens, item, p, false), u0 = int(at - before);
-        const int u1 = int(units - u0 < stop - at ? units : u0 + (stop - at));
-        x.item = item, x.u0 = u0, x.u1 = u1, x.units = units;
+        x.item = which, x.u0 = u0, x.u1 = u1, x.units = units;
         mbar_arrive(item_full(seg & 1));
-        at += u1 - u0;
-        if (u0 == 0 && u1 < units) {   // begun here, ended by a later CTA
-          uint32_t c = blockIdx.x;
-          while (shares.start(c + 1) < before + units) ++c;
-          cuts[blockIdx.x] = Cut{item, int(c - blockIdx.x) + 1};
-        }
-        before += units;
-        ++item;
+        if (which < 0) break;
       }
     }
   } else {
@@ -893,7 +897,7 @@ int launch(const Kv4AttnArgs& a, int sms, char* msg, size_t msglen) {
     CUtensorMap mk, mv;
     if (!encode_bf16_map(&mk, wk, p.n_bh, w.tiles_pad * kBN, DK, msg, msglen)) return 5;
     if (!encode_bf16_map(&mv, wv, p.n_bh, w.tiles_pad * kBN, DV, msg, msglen)) return 5;
-    const int64_t most = int64_t(p.n_bh) * p.n_tiles * w.tiles_pad;
+    const int64_t most = int64_t(p.n_bh) * p.n_tiles * w.tiles_pad;   // tiles of tokens, if all are as long as max_len
     const unsigned ctas = unsigned(most < sms ? most : sms);
     e = launch_overlapped(kv4_widen_kernel<DK, DV>, dim3(unsigned(w.tiles_pad), unsigned(p.n_bh)), dim3(256), 0, a.stream,
                           static_cast<const uint8_t*>(a.c.pool), a.c.table, a.lens, wk, wv, factor, p);

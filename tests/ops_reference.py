@@ -143,3 +143,23 @@ def attention(q, k, v, length, scale, causal):
             o[h, i], av[h, i] = p @ vv, p @ np.abs(vv)
             size[h, i] = abs(scale) * (np.abs(kk) @ np.abs(q[h, i])).max()
     return o, lse, av, size
+
+
+def attention_dense(q, k, v, length, scale, causal):
+    """attention() for many rows at once (one sequence, the same results)."""
+    Hq, N, _ = q.shape
+    G = Hq // k.shape[0]
+    seen = np.arange(length)[None] < (length - N + 1 + np.arange(N)[:, None] if causal else np.full((N, 1), length))
+    out = []
+    for h in range(Hq):
+        kk, vv = k[h // G, :length], v[h // G, :length]
+        s = np.where(seen, scale * (q[h] @ kk.T), -np.inf)
+        m = s.max(axis=1, initial=-np.inf, keepdims=True)
+        p = np.where(seen, np.exp(s - np.where(np.isfinite(m), m, 0.0)), 0.0)
+        total = p.sum(axis=1, keepdims=True)
+        with np.errstate(divide="ignore"):
+            lse = (m + np.log(total))[:, 0]
+        p /= np.where(total == 0, 1.0, total)
+        size = np.where(seen, abs(scale) * (np.abs(q[h]) @ np.abs(kk).T), 0.0).max(axis=1, initial=0.0)
+        out.append((p @ vv, lse, p @ np.abs(vv), size))
+    return [np.stack(x) for x in zip(*out)]
