@@ -10,7 +10,7 @@
 // pass over the tokens with the running maximum and sum; partial results of token ranges are
 // joined by o = sum_s e^(m_s - M) o_s / sum_s e^(m_s - M) l_s.
 //
-// Rounding: bf16 queries enter exactly; the weights p sv are rounded to bf16 once (relative
+// Rounding: bf16 queries (below 2^120) enter exactly; the weights p sv are rounded to bf16 once (relative
 // 2^-8, as in the other bf16 forward).  fp32 queries and weights enter as three bf16 terms each
 // (24 bits), so the fp32 form is fp32-accurate on the same instructions.  Scores, maxima, sums
 // and outputs accumulate in fp32.
@@ -26,7 +26,8 @@
 // items of its share.  An item inside one share is written at once; the pieces of a cut item go to
 // the workspace and a second kernel joins them.  Within a CTA four warps take turns at tiles of
 // kSub blocks, each with its own ring of bulk copies, running maximum, sum and output, joined
-// through shared memory at the end of the item.
+// through shared memory at the end of the item.  Tiles are worked on two blocks at a time, two chains of
+// dependent instructions beside each other.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -92,11 +93,28 @@ __device__ __forceinline__ void widen(uint32_t w, uint32_t* r) {
     r[j] = *reinterpret_cast<const uint32_t*>(&y);
   }
 }
+// The same without the multiply-add: n 2^-133 and n 2^-129, for keys against bf16 queries, which are
+// brought up by a power of two and hold the 16 and the 8 (see the queries).
+__device__ __forceinline__ void widen_raw(uint32_t w, uint32_t* r) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) r[j] = (j < 2 ? w : w >> 8) & (j % 2 ? 0x00f000f0u : 0x000f000fu);
+}
+// 2^e, -126 <= e <= 127, and the exponent of a number (0 for zero and what is not finite).
+__device__ __forceinline__ float power_of(int e) { return __uint_as_float(uint32_t(127 + e) << 23); }
+__device__ __forceinline__ int exponent_of(float x) {
+  return x == 0.f || !(x < INFINITY) ? 0 : int(__float_as_uint(x) >> 23) - 127;
+}
+// A query row is multiplied by 2^row_shift: its largest magnitude is then in [2^100, 2^101), so that
+// n 2^-133 times it is an ordinary number; rows from 2^93 on by 2^7, which keeps 2^(133 - shift), the
+// scores' unit, one too.
+__device__ __forceinline__ int row_shift(float top) { return max(100 - exponent_of(top), 7); }
 __device__ __forceinline__ float bf16_bits(uint32_t b) { return __uint_as_float(b << 16); }
 
 template <int G>
 __device__ __forceinline__ void load_words(uint32_t* w, const uint8_t* p) {
-  if constexpr (G == 4) {
+  if constexpr (G == 1) {
+    w[0] = *reinterpret_cast<const uint32_t*>(p);
+  } else if constexpr (G == 4) {
     const uint4 v = *reinterpret_cast<const uint4*>(p);
     w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
   } else {
@@ -162,6 +180,8 @@ struct Cut {
 template <int DK, int DV, int NT, int TERMS>
 struct Cfg {
   static constexpr int kSub = NT == 4 ? 1 : 2;                  // 16-token blocks of a tile
+  static constexpr int kPair = NT == 1 ? 2 : 1;                 // blocks taken at once (independent chains)
+  static_assert(kSub % kPair == 0, "whole pairs in a tile");
   static constexpr int kBytes = block_bytes(DK, DV);
   static constexpr int kStages = (NT * TERMS == 1 ? 13824 : 18432) / (kSub * kBytes);
   static constexpr int kBatch = 32 / kSub;                      // tiles whose places are looked up at once
@@ -173,11 +193,14 @@ struct Cfg {
   // queries in the order of the matrix operands: [nt][term][group][lane] 16 bytes
   static constexpr int kQ = kQRegs ? 0 : NT * TERMS * (DK / 32) * 32 * 16;
   static constexpr int kOffQ = kData;
-  static constexpr int kOffBar = kOffQ + kQ;
+  static constexpr bool kQSmem = !kQRegs && TERMS == 1;
+  static constexpr int kOffBias = kOffQ + kQ;                   // [nt][lane] 8 bytes (bf16 queries)
+  static constexpr int kOffTop = kOffBias + (kQSmem ? NT * 32 * 8 : 0);   // [nt][8] rows' largest
+  static constexpr int kOffBar = kOffTop + (kQSmem ? NT * 8 * 4 : 0);
   static constexpr int kOffMisc = kOffBar + kWarps * kStages * 8;
   static constexpr int kSmem = kOffMisc + 64;
-  // resident CTAs: registers (128 or 255 a thread) and 228 KB of shared memory
-  static constexpr int kCtas = NT * TERMS == 1 ? 4 : 2;
+  // resident CTAs: registers (168 or 255 a thread) and 228 KB of shared memory
+  static constexpr int kCtas = NT * TERMS == 1 ? 3 : 2;
   static_assert(kBytes % 16 == 0, "bulk copies are whole 16-byte units");
   static_assert(8 + 8 * kWarps <= 64, "the warps' sums fit behind the abort flag");
   static_assert(kCtas * (kSmem + 1024) <= 233472, "shared memory of the resident CTAs");
@@ -322,7 +345,6 @@ kv4_attn_kernel(const T* __restrict__ Q, const uint8_t* __restrict__ pool,
 
   const bool by_item = int64_t(p.n_pairs) * p.Hk <= gridDim.x;
   if (threadIdx.x == 0 && !by_item) cuts[blockIdx.x].pieces = 0;
-  const float c2 = fabsf(p.scale) * kLog2e * kCodeUnit, slack = c2 > 0.f ? kSlack / c2 : INFINITY;
   const int rows = int(p.N) * p.G;
   uint32_t count = 0;     // tiles this warp has taken so far: its place in the ring and the phases
   bool ok = true;
@@ -392,13 +414,92 @@ kv4_attn_kernel(const T* __restrict__ Q, const uint8_t* __restrict__ pool,
       static_assert(C::kStages <= C::kBatch, "the first tiles are of one batch");
     }
 
-    // queries: registers or shared memory, in operand order; a negative scale turns their signs
+    // Queries: registers or shared memory, in operand order; a negative scale turns their signs.
+    // bf16: a row times a power of two, its largest magnitude then in [2^100, 2^101), and -8 2^-133
+    // sum q of each group as bf16 terms beside it (see widen_raw).  fp32: three bf16 terms.
     uint4 qreg[C::kQRegs ? GK : 1];
-    {
+    uint2 qbias = make_uint2(0, 0);
+    float c2[NT][2], slack[NT][2];   // log2 units of a score, and kSlack in scores
+    if constexpr (TERMS == 1) {
+      for (int nt = C::kQRegs ? 0 : warp; nt < NT; nt += C::kQRegs ? 1 : kWarps) {
+        const int r = r0 + nt * 8 + g, i_n = int(unsigned(r) / unsigned(p.G));
+        const T* src = Q + b * p.q_sb + (int64_t(h) * p.G + r - i_n * p.G) * p.q_sh + i_n * p.q_sn + 8 * t;
+        float x[GK][8];
+        float top = 0.f;
+#pragma unroll
+        for (int gi = 0; gi < GK; ++gi) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[gi][e] = 0.f;
+          if (r < rows) load8(src + 32 * gi, x[gi]);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[gi][e]));
+        }
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        // in two factors: it may be above the largest number
+        const int up = row_shift(top);
+        const float up0 = power_of(up / 2) * (p.scale < 0.f ? -1.f : 1.f), up1 = power_of(up - up / 2);
+        float part[GK];
+#pragma unroll
+        for (int gi = 0; gi < GK; ++gi) {
+          float q = 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            x[gi][e] = x[gi][e] * up0 * up1;
+            q += x[gi][e] * power_of(-100);
+          }
+          q += __shfl_xor_sync(0xffffffffu, q, 1);
+          q += __shfl_xor_sync(0xffffffffu, q, 2);
+          part[gi] = q * -power_of(100 + 3 - 133);
+          // features 0 1 and 4 5 meet nibbles as they are, 2 3 and 6 7 nibbles times 16
+          const uint4 w = make_uint4(pack_bf16x2(x[gi][0], x[gi][1]), pack_bf16x2(x[gi][2] * 0.0625f, x[gi][3] * 0.0625f),
+                                     pack_bf16x2(x[gi][4], x[gi][5]), pack_bf16x2(x[gi][6] * 0.0625f, x[gi][7] * 0.0625f));
+          if constexpr (C::kQRegs) qreg[gi] = w;
+          else *reinterpret_cast<uint4*>(smem + C::kOffQ + ((nt * GK + gi) * 32 + lane) * 16) = w;
+        }
+        // index k = GK term + group of the bias product: a lane's pairs are k = 2t, 2t + 1 and 2t + 8, 2t + 9
+        uint32_t terms[3][GK / 2];
+#pragma unroll
+        for (int i = 0; i < GK / 2; ++i) {
+          uint32_t s3[3];
+          split_pair<3>(part[2 * i], part[2 * i + 1], s3);
+          terms[0][i] = s3[0], terms[1][i] = s3[1], terms[2][i] = s3[2];
+        }
+        uint2 bias = make_uint2(0, 0);
+        if constexpr (GK == 4) {
+          const int i = t & 1;
+          bias.x = t < 2 ? (i ? terms[0][GK / 2 - 1] : terms[0][0]) : (i ? terms[1][GK / 2 - 1] : terms[1][0]);
+          bias.y = t < 2 ? (i ? terms[2][GK / 2 - 1] : terms[2][0]) : 0u;
+        } else {
+          bias.x = t == 0 ? terms[0][0] : t == 1 ? terms[1][0] : t == 2 ? terms[2][0] : 0u;
+        }
+        if constexpr (C::kQRegs) {
+          qbias = bias;
+#pragma unroll
+          for (int c = 0; c < 2; ++c) c2[0][c] = __shfl_sync(0xffffffffu, top, 8 * t + 4 * c);
+        } else {
+          *reinterpret_cast<uint2*>(smem + C::kOffBias + (nt * 32 + lane) * 8) = bias;
+          if (t == 0) reinterpret_cast<float*>(smem + C::kOffTop)[nt * 8 + g] = top;
+        }
+      }
+      if constexpr (!C::kQRegs) {
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) c2[n][c] = reinterpret_cast<const float*>(smem + C::kOffTop)[n * 8 + 2 * t + c];
+      }
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const float top = c2[n][c];   // not finite: neither are the row's scores
+          c2[n][c] = top < INFINITY ? fabsf(p.scale) * kLog2e * power_of(133 - row_shift(top)) : __int_as_float(0x7fc00000);
+        }
+    } else {
       const uint32_t sign = p.scale < 0.f ? 0x80008000u : 0u;
-      for (int i = C::kQRegs ? warp * GK * 32 + lane : threadIdx.x; i < (C::kQRegs ? (warp + 1) * GK : NT * GK) * 32;
-           i += C::kQRegs ? 32 : kThreads) {
-        const int gi = (i >> 5) % GK, nt = C::kQRegs ? 0 : (i >> 5) / GK;
+      for (int i = threadIdx.x; i < NT * GK * 32; i += kThreads) {
+        const int gi = (i >> 5) % GK, nt = (i >> 5) / GK;
         const int r = r0 + nt * 8 + g, i_n = int(unsigned(r) / unsigned(p.G));
         float x[8];
 #pragma unroll
@@ -412,19 +513,19 @@ kv4_attn_kernel(const T* __restrict__ Q, const uint8_t* __restrict__ pool,
 #pragma unroll
           for (int k = 0; k < TERMS; ++k) w[e][k] ^= sign;
         }
-        if constexpr (C::kQRegs) {
 #pragma unroll
-          for (int j = 0; j < GK; ++j)
-            if (j == gi) qreg[j] = make_uint4(w[0][0], w[1][0], w[2][0], w[3][0]);
-        } else {
-#pragma unroll
-          for (int k = 0; k < TERMS; ++k)
-            *reinterpret_cast<uint4*>(smem + C::kOffQ + (((nt * TERMS + k) * GK + gi) * 32 + lane) * 16) =
-                make_uint4(w[0][k], w[1][k], w[2][k], w[3][k]);
-        }
+        for (int k = 0; k < TERMS; ++k)
+          *reinterpret_cast<uint4*>(smem + C::kOffQ + (((nt * TERMS + k) * GK + gi) * 32 + lane) * 16) =
+              make_uint4(w[0][k], w[1][k], w[2][k], w[3][k]);
       }
-      if constexpr (!C::kQRegs) __syncthreads();
+      __syncthreads();
+#pragma unroll
+      for (int n = 0; n < NT; ++n) c2[n][0] = c2[n][1] = fabsf(p.scale) * kLog2e * kCodeUnit;
     }
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) slack[n][c] = c2[n][c] > 0.f ? kSlack / c2[n][c] : INFINITY;
 
     float o[NT][DV / 16][4];
     // maximum, sum, where the maximum has to move, and what weights subtract: -m c2
@@ -443,24 +544,48 @@ kv4_attn_kernel(const T* __restrict__ Q, const uint8_t* __restrict__ pool,
       for (int i = 0; i < DV / 16; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.f;
     }
 
-    // One block of 16 tokens.  PLAIN: it is there and every row sees every token of it.
-    auto block = [&](auto plain_tag, const uint8_t* blk, int tok0, bool there) {
+    // kPair blocks of 16 tokens.  PLAIN: they are there and every row sees every token of them.
+    // `there`: one bit a block.
+    auto blocks = [&](auto plain_tag, const uint8_t* blk, int tok0, uint32_t there) {
       constexpr bool PLAIN = decltype(plain_tag)::value;
-      // scores: sc[nt]: (token g, rows 2t, 2t+1), (token g+8, ...)
-      float sc[NT][4];
-      {
+      // scores: sc[block][nt]: (token g, rows 2t, 2t+1), (token g+8, ...)
+      float sc[C::kPair][NT][4];
+#pragma unroll
+      for (int u = 0; u < C::kPair; ++u) {
+        const uint8_t* at_blk = blk + u * C::kBytes;
         uint32_t kw[2][GK];
-        float ks[2][GK];
+        uint32_t sw[2][GK / 2];      // scales, two groups a word
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          load_words<GK>(kw[r], blk + ((g + 8 * r) * 4 + t) * GK * 4);
-          load_scales<GK>(ks[r], blk + key_scales(DK, DV) + (g + 8 * r) * GK * 2);
+          load_words<GK>(kw[r], at_blk + ((g + 8 * r) * 4 + t) * GK * 4);
+          load_words<GK / 2>(sw[r], at_blk + key_scales(DK, DV) + (g + 8 * r) * GK * 2);
+        }
+        if constexpr (TERMS == 1) {
+          // what code + 8 is too much: sum_g ks (-8 sum q), one product over groups and terms
+          const uint32_t s0 = GK == 4 && (t & 1) ? sw[0][GK / 2 - 1] : sw[0][0];
+          const uint32_t s1 = GK == 4 && (t & 1) ? sw[1][GK / 2 - 1] : sw[1][0];
+          const uint32_t a[4] = {s0, s1, s0, s1};
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            uint2 qb = qbias;
+            if constexpr (!C::kQRegs) qb = *reinterpret_cast<const uint2*>(smem + C::kOffBias + (n * 32 + lane) * 8);
+            mma_16816_first(sc[u][n], a, qb.x, qb.y);
+          }
         }
 #pragma unroll
         for (int gi = 0; gi < GK; ++gi) {
+          float ks[2];
+#pragma unroll
+          for (int r = 0; r < 2; ++r)
+            ks[r] = gi & 1 ? __uint_as_float(sw[r][gi / 2] & 0xffff0000u) : bf16_bits(sw[r][gi / 2]);
           uint32_t lo[4], hi[4];
-          widen(kw[0][gi], lo);
-          widen(kw[1][gi], hi);
+          if constexpr (TERMS == 1) {
+            widen_raw(kw[0][gi], lo);
+            widen_raw(kw[1][gi], hi);
+          } else {
+            widen(kw[0][gi], lo);
+            widen(kw[1][gi], hi);
+          }
           const uint32_t a0[4] = {lo[0], hi[0], lo[1], hi[1]}, a1[4] = {lo[2], hi[2], lo[3], hi[3]};
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
@@ -476,37 +601,43 @@ kv4_attn_kernel(const T* __restrict__ Q, const uint8_t* __restrict__ pool,
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              sc[n][e] = gi == 0 ? ks[e >> 1][gi] * acc[e] : fmaf(ks[e >> 1][gi], acc[e], sc[n][e]);
+              sc[u][n][e] = TERMS > 1 && gi == 0 ? ks[e >> 1] * acc[e] : fmaf(ks[e >> 1], acc[e], sc[u][n][e]);
           }
         }
-      }
-      if constexpr (!PLAIN) {
+        if constexpr (!PLAIN) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+          for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (!there || tok0 + g + (e >> 1) * 8 >= lim[n][e & 1]) sc[n][e] = -INFINITY;
+            for (int e = 0; e < 4; ++e)
+              if (!(there >> u & 1u) || tok0 + u * kBlock + g + (e >> 1) * 8 >= lim[n][e & 1]) sc[u][n][e] = -INFINITY;
+        }
       }
       // The maximum moves only when a score passes it by more than kSlack (in log2): until then
       // the weights stay below 2^kSlack and nothing is rescaled.
+      float top[NT][2];
       bool moves = false;
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int c = 0; c < 2; ++c) moves |= fmaxf(sc[n][c], sc[n][2 + c]) > above[n][c];
+        for (int c = 0; c < 2; ++c) {
+          top[n][c] = fmaxf(sc[0][n][c], sc[0][n][2 + c]);
+#pragma unroll
+          for (int u = 1; u < C::kPair; ++u) top[n][c] = max3f(top[n][c], sc[u][n][c], sc[u][n][2 + c]);
+          moves |= top[n][c] > above[n][c];
+        }
       if (__any_sync(0xffffffffu, moves)) {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            float x = fmaxf(sc[n][c], sc[n][2 + c]);
+            float x = top[n][c];
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
             const float mn = fmaxf(m[n][c], x);
-            const float alpha = m[n][c] == -INFINITY ? 0.f : ex2_approx((m[n][c] - mn) * c2);
+            const float alpha = m[n][c] == -INFINITY ? 0.f : ex2_approx((m[n][c] - mn) * c2[n][c]);
             m[n][c] = mn;
-            above[n][c] = mn == -INFINITY ? -INFINITY : mn + slack;
-            mb[n][c] = mn == -INFINITY ? 0.f : -mn * c2;
+            above[n][c] = mn == -INFINITY ? -INFINITY : mn + slack[n][c];
+            mb[n][c] = mn == -INFINITY ? 0.f : -mn * c2[n][c];
             l[n][c] *= alpha;
 #pragma unroll
             for (int i = 0; i < DV / 16; ++i) {
@@ -516,45 +647,51 @@ kv4_attn_kernel(const T* __restrict__ Q, const uint8_t* __restrict__ pool,
           }
       }
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+      for (int u = 0; u < C::kPair; ++u)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float w = ex2_approx(fmaf(sc[n][e], c2, mb[n][e & 1]));
-          if (!PLAIN && sc[n][e] == -INFINITY) w = 0.f;
-          sc[n][e] = w;
-          l[n][e & 1] += w;
-        }
-      // o += (p sv) codes
-      uint32_t vw[2][GV];
-      float vs[2][GV];
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        load_words<GV>(vw[r], blk + value_codes(DK) + ((r * 8 + g) * 4 + t) * GV * 4);
-        load_scales<GV>(vs[r], blk + value_scales(DK, DV) + (g + 8 * r) * GV * 2);
-      }
-#pragma unroll
-      for (int gi = 0; gi < GV; ++gi) {
-        uint32_t lo[4], hi[4];
-        widen(vw[0][gi], lo);
-        widen(vw[1][gi], hi);
-        const uint32_t a0[4] = {lo[0], lo[1], hi[0], hi[1]}, a1[4] = {lo[2], lo[3], hi[2], hi[3]};
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          float w[4];
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            w[e] = sc[n][e] * vs[e >> 1][gi];
-            // a hidden token's scale may be anything: its weight is zero whatever that is
-            if (!PLAIN && sc[n][e] == 0.f) w[e] = 0.f;
+            float w = ex2_approx(fmaf(sc[u][n][e], c2[n][e & 1], mb[n][e & 1]));
+            if (!PLAIN && sc[u][n][e] == -INFINITY) w = 0.f;
+            sc[u][n][e] = w;
+            l[n][e & 1] += w;
           }
-          uint32_t p0[TERMS], p1[TERMS];
-          split_pair<TERMS>(w[0], w[1], p0);
-          split_pair<TERMS>(w[2], w[3], p1);
+      // o += (p sv) codes
 #pragma unroll
-          for (int k = 0; k < TERMS; ++k) {
-            const uint32_t b0 = transpose8(p0[k]), b1 = transpose8(p1[k]);
-            mma_16816(o[n][2 * gi], a0, b0, b1);
-            mma_16816(o[n][2 * gi + 1], a1, b0, b1);
+      for (int u = 0; u < C::kPair; ++u) {
+        const uint8_t* at_blk = blk + u * C::kBytes;
+        uint32_t vw[2][GV];
+        float vs[2][GV];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          load_words<GV>(vw[r], at_blk + value_codes(DK) + ((r * 8 + g) * 4 + t) * GV * 4);
+          load_scales<GV>(vs[r], at_blk + value_scales(DK, DV) + (g + 8 * r) * GV * 2);
+        }
+#pragma unroll
+        for (int gi = 0; gi < GV; ++gi) {
+          uint32_t lo[4], hi[4];
+          widen(vw[0][gi], lo);
+          widen(vw[1][gi], hi);
+          const uint32_t a0[4] = {lo[0], lo[1], hi[0], hi[1]}, a1[4] = {lo[2], lo[3], hi[2], hi[3]};
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            float w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              w[e] = sc[u][n][e] * vs[e >> 1][gi];
+              // a hidden token's scale may be anything: its weight is zero whatever that is
+              if (!PLAIN && sc[u][n][e] == 0.f) w[e] = 0.f;
+            }
+            uint32_t p0[TERMS], p1[TERMS];
+            split_pair<TERMS>(w[0], w[1], p0);
+            split_pair<TERMS>(w[2], w[3], p1);
+#pragma unroll
+            for (int k = 0; k < TERMS; ++k) {
+              const uint32_t b0 = transpose8(p0[k]), b1 = transpose8(p1[k]);
+              mma_16816(o[n][2 * gi], a0, b0, b1);
+              mma_16816(o[n][2 * gi + 1], a1, b0, b1);
+            }
           }
         }
       }
@@ -570,14 +707,15 @@ kv4_attn_kernel(const T* __restrict__ Q, const uint8_t* __restrict__ pool,
       const uint8_t* st = ring + s * C::kSub * C::kBytes;
       const int tok0 = (first + (warp + it * kWarps) * C::kSub) * kBlock;
       const uint32_t got = here >> (it % C::kBatch * C::kSub) & kTileBits;
+      constexpr uint32_t kPairBits = (1u << C::kPair) - 1;
 #pragma unroll 1
-      for (int sub = 0; sub < C::kSub; ++sub) {
+      for (int sub = 0; sub < C::kSub; sub += C::kPair) {
         const int tok = tok0 + sub * kBlock;
-        const bool there = got >> sub & 1u;
-        if (there && tok + kBlock <= all_limit)
-          block(std::true_type{}, st + sub * C::kBytes, tok, true);
+        const uint32_t there = got >> sub & kPairBits;
+        if (there == kPairBits && tok + C::kPair * kBlock <= all_limit)
+          blocks(std::true_type{}, st + sub * C::kBytes, tok, there);
         else
-          block(std::false_type{}, st + sub * C::kBytes, tok, there);
+          blocks(std::false_type{}, st + sub * C::kBytes, tok, there);
       }
       if (it % C::kBatch == C::kBatch - 1) here = here_next;
       // the stage is free again: start its next tile
@@ -616,7 +754,7 @@ kv4_attn_kernel(const T* __restrict__ Q, const uint8_t* __restrict__ pool,
       for (int c = 0; c < 2; ++c) {
         const int row = warp * 8 * NT + n * 8 + 2 * t + c;
         if (g == 0) {
-          jm[row] = m[n][c] == -INFINITY ? -INFINITY : m[n][c] * c2;
+          jm[row] = m[n][c] == -INFINITY ? -INFINITY : m[n][c] * c2[n][c];
           jl[row] = l[n][c];
         }
 #pragma unroll
@@ -813,7 +951,7 @@ Kv4Plan kv4_attn_plan(int64_t B, int64_t Hk, int64_t G, int64_t N, int64_t max_l
   p.rows_tile = rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
   p.n_tiles = (rows + p.rows_tile - 1) / p.rows_tile;
   // resident CTAs, but none with less than two units if every length is max_len
-  const int64_t resident = int64_t(sms) * (p.rows_tile == 8 && !f32 ? 4 : 2);
+  const int64_t resident = int64_t(sms) * (p.rows_tile == 8 && !f32 ? 3 : 2);
   const int64_t units = (max_len + kUnit - 1) / kUnit;
   const int64_t items = B * Hk * p.n_tiles;
   const int64_t most = items * ((units + 1) / 2);

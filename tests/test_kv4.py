@@ -462,3 +462,22 @@ def test_reference_packs_and_unpacks():
     q = R.quantise(k) + R.quantise(v)
     for a, b in zip(R.unpack(R.pack(*q), 128, 64), q):
         assert np.array_equal(a, b)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("N", [1, 5])
+def test_attention_of_very_large_and_small_queries(N, dtype):
+    """Rows of queries from 2^-100 to 2^100 against keys of the inverse size: scores of ordinary size."""
+    Hq, Hk, dk, dv, page, n = 8, 4, 64, 64, 16, 200
+    r = np.random.default_rng(17)
+    table, n_pages = table_of(r, [n], page)
+    for power in (-100, -60, 0, 60, 96):
+        k = cast(r.normal(size=(1, Hk, n, dk)) * 2.0 ** -power, dtype)
+        v = cast(r.normal(size=(1, Hk, n, dv)), dtype)
+        q = cast(r.normal(size=(1, Hq, N, dk)) * 2.0 ** power, dtype)
+        pool = pkg.kv4_pool(n_pages, Hk, page, dk, dv)
+        pkg.kv4_write(dev(k, dtype), dev(v, dtype), pool, dev(table), dev(np.arange(n, dtype=np.int32)[None]))
+        ref = [x[None] for x in R.attention(q[0], R.values(*R.quantise(k))[0], R.values(*R.quantise(v))[0], n, dk ** -0.5, True)]
+        o, lse = pkg.kv4_attn_lse(dev(q, dtype), pool, dev(table), dev(np.array([n], dtype=np.int32)))
+        check(o, lse, ref, dk, dtype, power)
