@@ -57,10 +57,10 @@ struct Raw {
   // The largest magnitude's bits, as a float's: a NaN's are above every number's.
   __device__ __forceinline__ uint32_t top() const {
     if constexpr (sizeof(T) == 2) {
-      uint32_t m = 0;   // of each half; as integers, since they are magnitudes
+      uint32_t m = 0;   // of each half; a NaN in either operand gives the NaN 0x7fff
       const uint32_t v[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) m = __vmaxu2(m, v[i] & 0x7fff7fffu);
+      for (int i = 0; i < 4; ++i) asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(v[i] & 0x7fff7fffu));
       return max(m << 16, m & 0xffff0000u);
     } else {
       uint32_t m = 0;
@@ -85,6 +85,28 @@ __device__ __forceinline__ void store8(float* p, const float* x) {
   *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
 }
 
+// Two floats in a register pair, and arithmetic on both at once (each rounded as by itself).
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
 // Codes + 8 of this lane's eight features, and the group's scale (bits of a bf16).
 // The quotient of bf16 inputs: x (1/s), then one residual step (Markstein's correction), which is
 // exact where x / s is a half-integer; where it is not, it is at least 2^-12 away from one (8-bit
@@ -96,24 +118,31 @@ __device__ __forceinline__ uint32_t quantise8(const Raw<T>& raw, uint32_t* code)
   uint32_t m = raw.top();
 #pragma unroll
   for (int o = 1; o < 4; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-  uint32_t bits = 0x7fc0u;
-  float s = 0.f;
-  if (m < 0x7f800000u) {
-    const __nv_bfloat16 h = __float2bfloat16_rn(__fdiv_rn(__uint_as_float(m), 7.f));
-    bits = __bfloat16_as_ushort(h);
-    s = __bfloat162float(h);
+  const bool finite = m < 0x7f800000u;
+  float s;
+  uint32_t bits;
+  {
+    // bf16: m / 7 is never within 2^-12 of a boundary between bf16 values (7 times one of those has
+    // 9 bits and a factor of 7, m has 8 bits), so the rounded reciprocal gives the same
+    const float top = __uint_as_float(m);
+    const __nv_bfloat16 h = __float2bfloat16_rn(sizeof(T) == 2 ? top * (1.f / 7.f) : __fdiv_rn(top, 7.f));
+    bits = finite ? __bfloat16_as_ushort(h) : 0x7fc0u;
+    s = finite ? __bfloat162float(h) : 0.f;
   }
   float x[8];
   raw.widen(x);
   // rint and the bias of 8 at once: 1.5 * 2^23 + 8 makes an integer of the sum, ties to even
   constexpr float kRound = 12582920.f;
   if (sizeof(T) == 2 && s > 1.2e-38f && s < 8.0e37f) {   // 1/s is a normal number
-    const float inv = __frcp_rn(s);
+    float inv;   // within 2^-22: enough for the residual step
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
+    const uint64_t inv2 = pair(inv, inv), neg2 = pair(-s, -s), round2 = pair(kRound, kRound);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 8; i += 2) {
       // |x / s| <= 7 (1 + 2^-8): the code needs no bound
-      const float q = x[i] * inv;
-      code[i] = __float_as_uint(fmaf(fmaf(-q, s, x[i]), inv, q) + kRound);
+      const uint64_t x2 = pair(x[i], x[i + 1]), q2 = mul2(x2, inv2);
+      const uint64_t c2 = add2(fma2(fma2(q2, neg2, x2), inv2, q2), round2);
+      code[i] = uint32_t(c2), code[i + 1] = uint32_t(c2 >> 32);
     }
   } else {
 #pragma unroll
@@ -190,6 +219,7 @@ struct Row {
 };
 
 constexpr int kMostBytes = block_bytes(128, 128);
+static_assert(8 * kBlock * 16 >= block_bytes(64, 64) && 16 * kBlock * 16 >= kMostBytes, "a thread for each 16 bytes of a block");
 
 template <typename T, int LPR>
 __global__ void __launch_bounds__(kThreads)
@@ -211,15 +241,20 @@ kv4_write_kernel(View k, View v, uint8_t* pool, const int32_t* table, const int3
   const int at_v1 = value_word(p.dk, r.tok, 2 * t + 1, g, gv) + (r.tok & 1) * 2;
   const int at_vs = value_scales(p.dk, p.dv) + (r.tok * gv + g) * 2;
   Raw<T> xk, xv;
-  xk.load(mine_k ? from_k + h0 * k.sh : nullptr);
-  xv.load(mine_v ? from_v + h0 * v.sh : nullptr);
-  for (int h = h0; h < h1; ++h) {
+  from_k += h0 * k.sh, from_v += h0 * v.sh;
+  xk.load(mine_k ? from_k : nullptr);
+  xv.load(mine_v ? from_v : nullptr);
+  // a team has at least as many threads as a block has 16-byte pieces
+  const int piece = (threadIdx.x % kTeam) * 16;
+  const bool copies = r.whole && piece < bytes;
+  uint8_t* block = r.block + h0 * head_bytes;
+  for (int h = h0; h < h1; ++h, block += head_bytes) {
     const Raw<T> ck = xk, cv = xv;
     if (h + 1 < h1) {
-      xk.load(mine_k ? from_k + (h + 1) * k.sh : nullptr);
-      xv.load(mine_v ? from_v + (h + 1) * v.sh : nullptr);
+      from_k += k.sh, from_v += v.sh;
+      xk.load(mine_k ? from_k : nullptr);
+      xv.load(mine_v ? from_v : nullptr);
     }
-    uint8_t* block = r.block + h * head_bytes;
     uint8_t* to = r.whole ? s_bytes[h & 1][r.unit] : block;
     uint32_t c[8];
     uint32_t s = quantise8<T>(ck, c);
@@ -234,9 +269,7 @@ kv4_write_kernel(View k, View v, uint8_t* pool, const int32_t* table, const int3
       if (t == 0) *reinterpret_cast<uint16_t*>(to + at_vs) = uint16_t(s);
     }
     __syncthreads();   // the block is together (the other buffer's copies were read before this)
-    if (r.whole)
-      for (int i = (threadIdx.x % kTeam) * 16; i < bytes; i += kTeam * 16)
-        *reinterpret_cast<uint4*>(block + i) = *reinterpret_cast<const uint4*>(s_bytes[h & 1][r.unit] + i);
+    if (copies) *reinterpret_cast<uint4*>(block + piece) = *reinterpret_cast<const uint4*>(s_bytes[h & 1][r.unit] + piece);
   }
 }
 
@@ -280,7 +313,7 @@ template <typename T, int LPR>
 __global__ void __launch_bounds__(kThreads)
 kv4_read_kernel(View k, View v, uint8_t* pool, const int32_t* table, const int32_t* pos, Dims p) {
   constexpr int kUnits = Row<LPR>::kUnits, kTeam = LPR * kBlock;
-  __shared__ __align__(16) uint8_t s_bytes[2][kUnits][kMostBytes];
+  __shared__ __align__(16) uint8_t s_bytes[2][2][kUnits][kMostBytes];
   wait_for_previous();
   const Row<LPR> r(pool, table, pos, p);
   const int f0 = r.lane * 8, g = r.lane >> 2, t = r.lane & 3;
@@ -294,37 +327,43 @@ kv4_read_kernel(View k, View v, uint8_t* pool, const int32_t* table, const int32
   const int at_v = value_word(p.dk, r.tok, 2 * t, g, gv) + (r.tok & 1) * 2;
   const int at_v1 = value_word(p.dk, r.tok, 2 * t + 1, g, gv) + (r.tok & 1) * 2;
   const int at_vs = value_scales(p.dk, p.dv) + (r.tok * gv + g) * 2;
-  // a whole block: 16 bytes a thread, the next head's on their way while one is taken apart (a team
-  // of 128 threads or more covers a block of its width in two pieces at most)
-  const int i0 = (threadIdx.x % kTeam) * 16, i1 = i0 + kTeam * 16;
-  uint4 a = make_uint4(0, 0, 0, 0), b = a;
-  auto fetch = [&](int h) {
-    const uint8_t* block = r.block + h * head_bytes;
-    if (i0 < bytes) a = *reinterpret_cast<const uint4*>(block + i0);
-    if (i1 < bytes) b = *reinterpret_cast<const uint4*>(block + i1);
+  // whole blocks, two heads at a time: 16 bytes a thread of each, the next ones on their way while
+  // these are taken apart (a team has at least as many threads as a block has such pieces)
+  const int piece = (threadIdx.x % kTeam) * 16;
+  const bool copies = r.whole && piece < bytes;
+  const uint8_t* block = r.block + h0 * head_bytes;
+  to_k += h0 * k.sh, to_v += h0 * v.sh;
+  uint4 a[2];
+  auto fetch = [&](const uint8_t* from, int h) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      if (copies && h + u < h1) a[u] = *reinterpret_cast<const uint4*>(from + u * head_bytes + piece);
   };
-  if (r.whole) fetch(h0);
-  for (int h = h0; h < h1; ++h) {
-    const uint8_t* from = r.block + h * head_bytes;
-    if (r.whole) {
-      uint8_t* at = s_bytes[h & 1][r.unit];
-      if (i0 < bytes) *reinterpret_cast<uint4*>(at + i0) = a;
-      if (i1 < bytes) *reinterpret_cast<uint4*>(at + i1) = b;
-      if (h + 1 < h1) fetch(h + 1);
-      from = at;
+  fetch(block, h0);
+  for (int h = h0; h < h1; h += 2) {
+    uint8_t* mid = s_bytes[(h - h0) >> 1 & 1][0][r.unit];
+    if (copies) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) *reinterpret_cast<uint4*>(mid + u * kUnits * kMostBytes + piece) = a[u];
+      fetch(block + 2 * head_bytes, h + 2);
     }
     __syncthreads();
-    if (r.block == nullptr) {   // padding: zeros; no such place: NaN
-      const float fill = r.at < 0 ? 0.f : __int_as_float(0x7fc00000);
-      if (mine_k) store_all(to_k + h * k.sh, fill);
-      if (mine_v) store_all(to_v + h * v.sh, fill);
-      continue;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      if (h + u >= h1) break;
+      if (r.block == nullptr) {   // padding: zeros; no such place: NaN
+        const float fill = r.at < 0 ? 0.f : __int_as_float(0x7fc00000);
+        if (mine_k) store_all(to_k, fill);
+        if (mine_v) store_all(to_v, fill);
+      } else {
+        const uint8_t* from = r.whole ? mid + u * kUnits * kMostBytes : block;
+        if (mine_k) store_scaled(to_k, *reinterpret_cast<const uint32_t*>(from + at_k), *reinterpret_cast<const uint16_t*>(from + at_ks));
+        if (mine_v)
+          store_scaled(to_v, reorder(*reinterpret_cast<const uint16_t*>(from + at_v), *reinterpret_cast<const uint16_t*>(from + at_v1)),
+                       *reinterpret_cast<const uint16_t*>(from + at_vs));
+      }
+      block += head_bytes, to_k += k.sh, to_v += v.sh;
     }
-    if (mine_k)
-      store_scaled(to_k + h * k.sh, *reinterpret_cast<const uint32_t*>(from + at_k), *reinterpret_cast<const uint16_t*>(from + at_ks));
-    if (mine_v)
-      store_scaled(to_v + h * v.sh, reorder(*reinterpret_cast<const uint16_t*>(from + at_v), *reinterpret_cast<const uint16_t*>(from + at_v1)),
-                   *reinterpret_cast<const uint16_t*>(from + at_vs));
   }
 }
 
