@@ -34,6 +34,31 @@ constexpr int kThreads = 256;
 constexpr int kV = 8;  // features of a lane
 constexpr unsigned kErrIndex = 7u;  // MOA_ERR_DEVICE_INDEX
 
+// Two floats in a register pair, and arithmetic on both at once (each rounded as by itself): half the
+// instructions of a row, which are what the memory would otherwise wait for.
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float low(uint64_t a) { return __uint_as_float(uint32_t(a)); }
+__device__ __forceinline__ float high(uint64_t a) { return __uint_as_float(uint32_t(a >> 32)); }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
 __device__ __forceinline__ void load8(const __nv_bfloat16* p, float* x) {
   const uint4 v = *reinterpret_cast<const uint4*>(p);
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -69,35 +94,33 @@ struct Raw {
                           __shfl_sync(0xffffffffu, w[i].z, from, LPR), __shfl_sync(0xffffffffu, w[i].w, from, LPR));
     return r;
   }
-  __device__ __forceinline__ void widen(float* x) const {
+  __device__ __forceinline__ void widen(uint64_t* x) const {   // kV / 2 pairs
     if constexpr (sizeof(T) == 2) {
       const uint32_t v[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        x[2 * i] = __uint_as_float(v[i] << 16);
-        x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
-      }
+      for (int i = 0; i < 4; ++i) x[i] = pair(__uint_as_float(v[i] << 16), __uint_as_float(v[i] & 0xffff0000u));
     } else {
-      const uint32_t v[8] = {w[0].x, w[0].y, w[0].z, w[0].w, w[sizeof(T) / 2 - 1].x, w[sizeof(T) / 2 - 1].y, w[sizeof(T) / 2 - 1].z, w[sizeof(T) / 2 - 1].w};
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(v[i]);
+      for (int i = 0; i < int(sizeof(T) / 2); ++i) {
+        x[2 * i] = pair(__uint_as_float(w[i].x), __uint_as_float(w[i].y));
+        x[2 * i + 1] = pair(__uint_as_float(w[i].z), __uint_as_float(w[i].w));
+      }
     }
   }
 };
-__device__ __forceinline__ void store8(__nv_bfloat16* p, const float* x) {
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const uint64_t* x) {
   uint32_t w[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    __nv_bfloat162 v = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+    __nv_bfloat162 v = __floats2bfloat162_rn(low(x[i]), high(x[i]));
     w[i] = *reinterpret_cast<uint32_t*>(&v);
   }
   *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ void store8(float* p, const float* x) {
-  *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
-  *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+__device__ __forceinline__ void store8(float* p, const uint64_t* x) {
+  *reinterpret_cast<float4*>(p) = make_float4(low(x[0]), high(x[0]), low(x[1]), high(x[1]));
+  *reinterpret_cast<float4*>(p + 4) = make_float4(low(x[2]), high(x[2]), low(x[3]), high(x[3]));
 }
-
 template <int LPR>
 __device__ __forceinline__ float group_sum(float v) {
 #pragma unroll
@@ -114,13 +137,20 @@ struct Turn {
 
 // The other members of this lane's pairs.
 template <typename T, int LPR, bool PAIRS>
-__device__ __forceinline__ void others(const Raw<T>& raw, const float* x, int partner, float* o) {
+__device__ __forceinline__ void others(const Raw<T>& raw, const uint64_t* x, int partner, uint64_t* o) {
   if constexpr (PAIRS) {
 #pragma unroll
-    for (int i = 0; i < kV; ++i) o[i] = x[i ^ 1];
+    for (int i = 0; i < kV / 2; ++i) o[i] = pair(high(x[i]), low(x[i]));
   } else {
     raw.template of<LPR>(partner).widen(o);
   }
+}
+// The sum of a lane's eight squares, or products.
+__device__ __forceinline__ float dot8(const uint64_t* a, const uint64_t* b) {
+  uint64_t s = mul2(a[0], b[0]);
+#pragma unroll
+  for (int i = 1; i < kV / 2; ++i) s = fma2(a[i], b[i], s);
+  return low(s) + high(s);
 }
 
 struct Dims {
@@ -219,6 +249,9 @@ norm_rope_kernel(View q, View k, View oq, View ok, const T* wq, const T* wk, con
       for (int i = 0; i < kV; ++i) t.s[i] *= w[i];
     }
   }
+  uint64_t c2[kV / 2], s2[kV / 2];
+#pragma unroll
+  for (int i = 0; i < kV / 2; ++i) c2[i] = pair(t.c[2 * i], t.c[2 * i + 1]), s2[i] = pair(t.s[2 * i], t.s[2 * i + 1]);
   const float inv_d = 1.f / float(p.d);
   for (int hb = h0; hb < h1; hb += kBatch) {
     Raw<T> now[kBatch];
@@ -229,18 +262,17 @@ norm_rope_kernel(View q, View k, View oq, View ok, const T* wq, const T* wk, con
     for (int u = 0; u < kBatch; ++u) {
       const int h = hb + u;
       if (h >= h1) break;
-      float x[kV], o[kV];
+      uint64_t x[kV / 2], o[kV / 2];
       now[u].widen(x);
       others<T, LPR, PAIRS>(now[u], x, partner, o);
-      float ss = 0.f;
+      const float r = rsqrtf(group_sum<LPR>(dot8(x, x)) * inv_d + p.eps);
+      const uint64_t r2 = pair(r, r);
 #pragma unroll
-      for (int i = 0; i < kV; ++i) ss += x[i] * x[i];
-      const float r = rsqrtf(group_sum<LPR>(ss) * inv_d + p.eps);
-#pragma unroll
-      for (int i = 0; i < kV; ++i) x[i] = (x[i] * t.c[i] + o[i] * t.s[i]) * r;
+      for (int i = 0; i < kV / 2; ++i) x[i] = mul2(fma2(x[i], c2[i], mul2(o[i], s2[i])), r2);
       if (at < 0 || bad) {
+        const float fill = bad ? __int_as_float(0x7fc00000) : 0.f;
 #pragma unroll
-        for (int i = 0; i < kV; ++i) x[i] = bad ? __int_as_float(0x7fc00000) : 0.f;
+        for (int i = 0; i < kV / 2; ++i) x[i] = pair(fill, fill);
       }
       if (mine) store8(dst + h * out.sh, x);
     }
@@ -265,11 +297,11 @@ norm_rope_bwd_kernel(View q, View k, View gq, View gk, View oq, View ok, const T
   const int H = is_q ? p.Hq : p.Hk;
   const int h0 = range * p.hp, h1 = h0 + p.hp < H ? h0 + p.hp : H;
   const int f0 = lane * kV;
-  float acc[kV];
+  uint64_t acc[kV / 2];
   Raw<T> wraw;
   wraw.zero();
 #pragma unroll
-  for (int i = 0; i < kV; ++i) acc[i] = 0.f;
+  for (int i = 0; i < kV / 2; ++i) acc[i] = 0;
   if (f0 < p.d) wraw.load((is_q ? wq : wk) + f0);
   const int half_lanes = p.d_rot / 2 / kV;
   const int partner = f0 >= p.d_rot ? lane : (f0 < p.d_rot / 2 ? lane + half_lanes : lane - half_lanes);
@@ -306,13 +338,16 @@ norm_rope_bwd_kernel(View q, View k, View gq, View gk, View oq, View ok, const T
     const bool counts = at >= 0 && !bad;
     Turn t;
     load_turn<PAIRS>(t, cosines, sines, counts ? at : 0, p, f0, -1.f);
+    uint64_t c2[kV / 2], s2[kV / 2];
+#pragma unroll
+    for (int i = 0; i < kV / 2; ++i) c2[i] = pair(t.c[2 * i], t.c[2 * i + 1]), s2[i] = pair(t.s[2 * i], t.s[2 * i + 1]);
     next_at = position(token + int64_t(gridDim.x) * kGroups);
     for (int hb = h0; hb < h1; hb += kBatch) {
 #pragma unroll
       for (int u = 0; u < kBatch; ++u) {
         const int h = hb + u;
         if (h >= h1) break;
-        float x[kV], g[kV], o[kV], w[kV];
+        uint64_t x[kV / 2], g[kV / 2], o[kV / 2], w[kV / 2];
         xraw[u].widen(x);
         graw[u].widen(g);
         others<T, LPR, PAIRS>(graw[u], g, partner, o);
@@ -321,36 +356,34 @@ norm_rope_bwd_kernel(View q, View k, View gq, View gk, View oq, View ok, const T
           xraw[u].load(src + (h + kBatch) * in.sh);
           graw[u].load(gsrc + (h + kBatch) * gin.sh);
         }
-        float ss = 0.f;
-#pragma unroll
-        for (int i = 0; i < kV; ++i) ss += x[i] * x[i];
-        const float r = rsqrtf(group_sum<LPR>(ss) * inv_d + p.eps);
+        const float r = rsqrtf(group_sum<LPR>(dot8(x, x)) * inv_d + p.eps);
+        const uint64_t r2 = pair(r, r);
         wraw.widen(w);
-        float dot = 0.f;
 #pragma unroll
-        for (int i = 0; i < kV; ++i) {
-          const float turned = g[i] * t.c[i] + o[i] * t.s[i];
-          x[i] *= r;
-          o[i] = turned * x[i];
-          g[i] = w[i] * turned;
-          dot += g[i] * x[i];
+        for (int i = 0; i < kV / 2; ++i) {
+          const uint64_t turned = fma2(g[i], c2[i], mul2(o[i], s2[i]));
+          x[i] = mul2(x[i], r2);
+          o[i] = mul2(turned, x[i]);
+          g[i] = mul2(w[i], turned);
         }
-        const float mean = group_sum<LPR>(dot) * inv_d;
+        const float mean = group_sum<LPR>(dot8(g, x)) * inv_d;
+        const uint64_t m2 = pair(-mean, -mean);
 #pragma unroll
-        for (int i = 0; i < kV; ++i) g[i] = r * (g[i] - x[i] * mean);
+        for (int i = 0; i < kV / 2; ++i) g[i] = mul2(r2, fma2(x[i], m2, g[i]));
         if (counts) {
 #pragma unroll
-          for (int i = 0; i < kV; ++i) acc[i] += o[i];
+          for (int i = 0; i < kV / 2; ++i) acc[i] = add2(acc[i], o[i]);
         } else {
+          const float fill = bad ? __int_as_float(0x7fc00000) : 0.f;
 #pragma unroll
-          for (int i = 0; i < kV; ++i) g[i] = bad ? __int_as_float(0x7fc00000) : 0.f;
+          for (int i = 0; i < kV / 2; ++i) g[i] = pair(fill, fill);
         }
         if (mine) store8(dst + h * out.sh, g);
       }
     }
   }
 #pragma unroll
-  for (int i = 0; i < kV; ++i) sums[group][f0 + i] = acc[i];
+  for (int i = 0; i < kV / 2; ++i) sums[group][f0 + 2 * i] = low(acc[i]), sums[group][f0 + 2 * i + 1] = high(acc[i]);
   __syncthreads();
   const int64_t row = int64_t(blockIdx.y) * gridDim.x + blockIdx.x;
   for (int f = threadIdx.x; f < p.d; f += kThreads) {
