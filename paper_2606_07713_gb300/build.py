@@ -107,7 +107,7 @@ def _link_binding(obj: str) -> None:
     tmp = BINDING + f".tmp{os.getpid()}"
     _run_cxx([_cxx(), "-shared", obj, "-o", tmp, "-L", BUILD, "-l:libmoa_attn.so", "-Wl,-rpath,$ORIGIN",
               "-L", os.path.join(os.path.dirname(torch.__file__), "lib"),
-              "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"], "linking the PyTorch binding")
+              "-ltorch_python", "-ltorch", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda"], "linking the PyTorch binding")
     os.replace(tmp, BINDING)
 
 

@@ -7,7 +7,8 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
-#include <ATen/ops/empty.h>
+#include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -120,33 +121,62 @@ bool truth(PyObject* o) {
   return r != 0;
 }
 
-// The raw stream: None is torch's current stream of the device, else an object with .cuda_stream.
-void* raw_stream(PyObject* o, at::Device device) {
-  if (o == Py_None) return c10::cuda::getCurrentCUDAStream(device.index()).stream();
-  PyObject* s = PyObject_GetAttrString(o, "cuda_stream");
-  if (s == nullptr) throw Raise{nullptr, ""};
-  void* p = PyLong_AsVoidPtr(s);
-  Py_DECREF(s);
-  if (p == nullptr && PyErr_Occurred()) throw Raise{nullptr, ""};
-  return p;
+// The call's device and stream: None is torch's current stream of the device, else an object with
+// .cuda_stream.  Memory allocated inside belongs to that stream, so that it is not handed out again
+// before the call's work on it is done.
+struct Place {
+  c10::cuda::CUDAGuard device;
+  c10::cuda::OptionalCUDAStreamGuard guard;
+  c10::cuda::CUDAStream stream;
+  Place(PyObject* o, at::Device dev) : device(dev), stream(c10::cuda::getCurrentCUDAStream(dev.index())) {
+    if (o == Py_None) return;
+    PyObject* s = PyObject_GetAttrString(o, "cuda_stream");
+    if (s == nullptr) throw Raise{nullptr, ""};
+    void* p = PyLong_AsVoidPtr(s);
+    Py_DECREF(s);
+    if (p == nullptr && PyErr_Occurred()) throw Raise{nullptr, ""};
+    if (p == static_cast<void*>(stream.stream())) return;
+    stream = p == nullptr ? c10::cuda::getDefaultCUDAStream(dev.index())
+                          : c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(p), dev.index());
+    guard.reset_stream(stream);
+  }
+  void* raw() const { return stream.stream(); }
+};
+
+at::Tensor make(at::IntArrayRef size, at::ScalarType type, at::Device dev) {
+  return at::Tensor(at::detail::empty_cuda(size, type, dev, std::nullopt));
 }
 
-at::Tensor scratch(const char* what, PyObject* given, size_t need, at::Device device) {
-  if (given != Py_None) {
-    const at::Tensor& t = tensor(what, "workspace", given);
-    if (t.device() != device || !t.is_contiguous())
-      fail(PyExc_ValueError, "%s: workspace must be a contiguous tensor on %s", what, device.str().c_str());
-    return t;
+// The workspace: what the caller gives, or memory of the call's stream for the time of the call.
+struct Scratch {
+  void* p = nullptr;
+  size_t bytes = 0;
+  bool mine = false;
+  Scratch(const char* what, PyObject* given, size_t need, const Place& place) {
+    if (given != Py_None) {
+      const at::Tensor& t = tensor(what, "workspace", given);
+      if (t.device() != place.stream.device() || !t.is_contiguous())
+        fail(PyExc_ValueError, "%s: workspace must be a contiguous tensor on %s", what, place.stream.device().str().c_str());
+      p = t.data_ptr(), bytes = t.nbytes();
+      return;
+    }
+    bytes = need < 16 ? 16 : need;
+    p = c10::cuda::CUDACachingAllocator::raw_alloc_with_stream(bytes, place.stream);
+    mine = true;
   }
-  return at::empty({int64_t(need < 16 ? 16 : need)}, at::TensorOptions().dtype(at::kByte).device(device));
-}
+  ~Scratch() {
+    if (mine) c10::cuda::CUDACachingAllocator::raw_delete(p);
+  }
+  Scratch(const Scratch&) = delete;
+  Scratch& operator=(const Scratch&) = delete;
+};
 
 // Two tensors of `out` (a pair), or new contiguous ones of these shapes like `like`.
-void outputs(const char* what, PyObject* out, const at::TensorOptions& like, const int64_t* a, const int64_t* b,
+void outputs(const char* what, PyObject* out, at::ScalarType type, at::Device dev, const int64_t* a, const int64_t* b,
              at::Tensor* t) {
   if (out == Py_None) {
-    t[0] = at::empty(at::IntArrayRef(a, 4), like);
-    t[1] = at::empty(at::IntArrayRef(b, 4), like);
+    t[0] = make(at::IntArrayRef(a, 4), type, dev);
+    t[1] = make(at::IntArrayRef(b, 4), type, dev);
     return;
   }
   PyObject* s = PySequence_Fast(out, "out must be a pair of tensors");
@@ -210,15 +240,15 @@ const int32_t* i32(const at::Tensor& t) { return static_cast<const int32_t*>(t.d
 PyObject* qk_norm_rope(PyObject* const* a) {
   const char* what = "qk_norm_rope";
   Norm n = norm_args(what, a);
-  const c10::cuda::CUDAGuard guard(n.q->device());
+  const Place place(a[10], n.q->device());
   at::Tensor o[2];
-  outputs(what, a[9], n.q->options(), n.qs, n.ks, o);
+  outputs(what, a[9], n.q->scalar_type(), n.q->device(), n.qs, n.ks, o);
   heads(what, "out[0]", o[0], n.q, n.qs, n.strides + 6);
   heads(what, "out[1]", o[1], n.q, n.ks, n.strides + 9);
   check(moa_qk_norm_rope(n.q->data_ptr(), n.k->data_ptr(), n.wq->data_ptr(), n.wk->data_ptr(), f32(*n.cos),
                          f32(*n.sin), i32(*n.pos), o[0].data_ptr(), o[1].data_ptr(), n.B, n.Hq, n.Hk, n.N, n.d, n.rot,
                          n.n_pos, n.strides, float(number(what, "eps", a[7])), truth(a[8]), code(what, *n.q),
-                         raw_stream(a[10], n.q->device())));
+                         place.raw()));
   return pair(o[0], o[1]);
 }
 
@@ -229,21 +259,19 @@ PyObject* qk_norm_rope_bwd(PyObject* const* a) {
   const at::Tensor &gq = tensor(what, "dqo", a[7]), &gk = tensor(what, "dko", a[8]);
   heads(what, "dqo", gq, n.q, n.qs, n.strides + 6);
   heads(what, "dko", gk, n.q, n.ks, n.strides + 9);
-  const c10::cuda::CUDAGuard guard(n.q->device());
+  const Place place(a[13], n.q->device());
   at::Tensor o[2];
-  outputs(what, a[11], n.q->options(), n.qs, n.ks, o);
+  outputs(what, a[11], n.q->scalar_type(), n.q->device(), n.qs, n.ks, o);
   heads(what, "out[0]", o[0], n.q, n.qs, n.strides + 12);
   heads(what, "out[1]", o[1], n.q, n.ks, n.strides + 15);
   const int dtype = code(what, *n.q);
-  const at::TensorOptions f = n.q->options().dtype(at::kFloat);
-  at::Tensor dwq = at::empty({n.d}, f), dwk = at::empty({n.d}, f);
-  const at::Tensor ws = scratch(what, a[12], moa_qk_norm_rope_bwd_workspace_bytes(n.B, n.Hq, n.Hk, n.N, n.d),
-                                n.q->device());
+  at::Tensor dwq = make({n.d}, at::kFloat, n.q->device()), dwk = make({n.d}, at::kFloat, n.q->device());
+  const Scratch ws(what, a[12], moa_qk_norm_rope_bwd_workspace_bytes(n.B, n.Hq, n.Hk, n.N, n.d), place);
   check(moa_qk_norm_rope_bwd(n.q->data_ptr(), n.k->data_ptr(), n.wq->data_ptr(), n.wk->data_ptr(), f32(*n.cos),
                              f32(*n.sin), i32(*n.pos), gq.data_ptr(), gk.data_ptr(), o[0].data_ptr(), o[1].data_ptr(),
                              static_cast<float*>(dwq.data_ptr()), static_cast<float*>(dwk.data_ptr()), n.B, n.Hq, n.Hk,
                              n.N, n.d, n.rot, n.n_pos, n.strides, float(number(what, "eps", a[9])), truth(a[10]), dtype,
-                             ws.data_ptr(), ws.nbytes(), raw_stream(a[13], n.q->device())));
+                             ws.p, ws.bytes, place.raw()));
   PyObject* r = PyTuple_New(4);
   if (r == nullptr) return nullptr;
   const at::Tensor* t[4] = {&o[0], &o[1], &dwq, &dwk};
@@ -286,9 +314,9 @@ PyObject* kv4_write(PyObject* const* a) {
     fail(PyExc_ValueError, "%s: k %s and v %s do not fit the pool (%lld heads, d_v = %lld)", what,
          text(k.sizes()).c_str(), text(v.sizes()).c_str(), (long long)c.H, (long long)c.dv);
   flat(what, "pos", pos, at::kInt, {B, N}, k.device());
-  const c10::cuda::CUDAGuard guard(k.device());
+  const Place place(a[5], k.device());
   check(moa_kv4_write(k.data_ptr(), v.data_ptr(), c.pool->data_ptr(), i32(*c.pages), i32(pos), B, H, N, dk, c.dv,
-                      c.n_pages, c.page, c.max_pages, strides, code(what, k), raw_stream(a[5], k.device())));
+                      c.n_pages, c.page, c.max_pages, strides, code(what, k), place.raw()));
   Py_RETURN_NONE;
 }
 
@@ -302,16 +330,16 @@ PyObject* kv4_read(PyObject* const* a) {
   const Cache c = cache_args(what, a[0], a[1], B, dk, dev);
   flat(what, "pos", pos, at::kInt, {B, N}, dev);
   const int64_t ks[4] = {B, c.H, N, dk}, vs[4] = {B, c.H, N, c.dv};
-  const c10::cuda::CUDAGuard guard(dev);
+  const Place place(a[6], dev);
   at::Tensor o[2];
   const at::ScalarType type = integer(what, "dtype", a[4]) == MOA_FP32 ? at::kFloat : at::kBFloat16;
-  outputs(what, a[5], pos.options().dtype(type), ks, vs, o);
+  outputs(what, a[5], type, dev, ks, vs, o);
   if (o[0].device() != dev) fail(PyExc_ValueError, "%s: out is on another device", what);
   int64_t strides[6];
   heads(what, "k", o[0], nullptr, ks, strides);
   heads(what, "v", o[1], &o[0], vs, strides + 3);
   check(moa_kv4_read(o[0].data_ptr(), o[1].data_ptr(), c.pool->data_ptr(), i32(*c.pages), i32(pos), B, c.H, N, dk,
-                     c.dv, c.n_pages, c.page, c.max_pages, strides, code(what, o[0]), raw_stream(a[6], dev)));
+                     c.dv, c.n_pages, c.page, c.max_pages, strides, code(what, o[0]), place.raw()));
   return pair(o[0], o[1]);
 }
 
@@ -330,22 +358,21 @@ PyObject* kv4_attn(PyObject* const* a) {
   const int64_t max_len = a[4] == Py_None ? c.max_pages * c.page : integer(what, "max_len", a[4]);
   const float scale = a[5] == Py_None ? float(1.0 / std::sqrt(double(dk))) : float(number(what, "scale", a[5]));
   const int dtype = code(what, q);
-  const c10::cuda::CUDAGuard guard(dev);
+  const Place place(a[10], dev);
   const int64_t os[4] = {B, Hq, N, c.dv};
-  at::Tensor o = a[7] == Py_None ? at::empty(at::IntArrayRef(os, 4), q.options()) : tensor(what, "out", a[7]);
+  at::Tensor o = a[7] == Py_None ? make(at::IntArrayRef(os, 4), q.scalar_type(), dev) : tensor(what, "out", a[7]);
   heads(what, "out", o, &q, os, strides + 3);
   at::Tensor lse;
   if (a[8] == Py_True) {
-    lse = at::empty({B, Hq, N}, q.options().dtype(at::kFloat));
+    lse = make({B, Hq, N}, at::kFloat, dev);
   } else if (with_lse) {
     lse = tensor(what, "lse", a[8]);
     flat(what, "lse", lse, at::kFloat, {B, Hq, N}, dev);
   }
-  const at::Tensor ws = scratch(what, a[9], moa_kv4_attn_workspace_bytes(B, Hq, c.H, N, dk, c.dv, max_len, dtype), dev);
+  const Scratch ws(what, a[9], moa_kv4_attn_workspace_bytes(B, Hq, c.H, N, dk, c.dv, max_len, dtype), place);
   check(moa_kv4_attn(q.data_ptr(), c.pool->data_ptr(), i32(*c.pages), i32(lens), o.data_ptr(),
                      with_lse ? static_cast<float*>(lse.data_ptr()) : nullptr, B, Hq, c.H, N, dk, c.dv, c.n_pages,
-                     c.page, c.max_pages, max_len, strides, scale, truth(a[6]), dtype, ws.data_ptr(), ws.nbytes(),
-                     raw_stream(a[10], dev)));
+                     c.page, c.max_pages, max_len, strides, scale, truth(a[6]), dtype, ws.p, ws.bytes, place.raw()));
   return with_lse ? pair(o, lse) : THPVariable_Wrap(o);
 }
 
