@@ -187,6 +187,23 @@ kv4_widen_kernel(const uint8_t* __restrict__ pool, const int32_t* __restrict__ t
       atomicExch(&g_moa_kv4_tc_status, kErrIndex);
   }
   const int n_tok = src == nullptr ? 0 : min(kBlock, len - blk * kBlock);
+  // the lane's words, on their way while the scales are looked at.  Keys: a word is eight neighbouring
+  // features of a token.  Values: two words are eight neighbouring features of two tokens.
+  constexpr int kChunks = DK / 8, kChunksV = DV / 8, kItsK = kBlock * kChunks / 32, kItsV = kBlock / 2 * kChunksV / 32;
+  uint32_t kw[kItsK], vw[kItsV][2];
+#pragma unroll
+  for (int it = 0; it < kItsK; ++it) {
+    const int i = it * 32 + lane, token = i / kChunks, f8 = i % kChunks;
+    kw[it] = token < n_tok ? *reinterpret_cast<const uint32_t*>(src + key_word(token, f8 & 3, f8 >> 2, GK)) : 0x88888888u;
+  }
+#pragma unroll
+  for (int it = 0; it < kItsV; ++it) {
+    const int i = it * 32 + lane, token = 2 * (i / kChunksV), f8 = i % kChunksV;
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      vw[it][k] = token < n_tok ? *reinterpret_cast<const uint32_t*>(src + value_word(DK, token, (f8 & 3) * 2 + k, f8 >> 2, GV))
+                                : 0x88888888u;
+  }
   // the largest key scale, and the tokens with a value scale that is not finite
   float top = 0.f;
   uint32_t bad = 0;
@@ -223,48 +240,46 @@ kv4_widen_kernel(const uint8_t* __restrict__ pool, const int32_t* __restrict__ t
   if (threadIdx.x == 0) factor[int64_t(bh) * p.tiles_pad + tile] = make_float2(up, __uint_as_float(gone));
 
   const int64_t row0 = (int64_t(bh) * p.tiles_pad + tile) * kBN + warp * kBlock;
-  // keys: a word is eight neighbouring features of a token
-  constexpr int kChunks = DK / 8;
 #pragma unroll
-  for (int it = 0; it < kBlock * kChunks / 32; ++it) {
-    const int i = it * 32 + lane, token = i / kChunks, f8 = i % kChunks, g = f8 >> 2, t = f8 & 3;
-    uint32_t w = 0x88888888u;
+  for (int it = 0; it < kItsK; ++it) {
+    const int i = it * 32 + lane, token = i / kChunks, f8 = i % kChunks, g = f8 >> 2;
     float s = 0.f;
     if (token < n_tok) {
-      w = *reinterpret_cast<const uint32_t*>(src + key_word(token, t, g, GK));
       s = bf16_value(src + key_scales(DK, DV) + (token * GK + g) * 2) * down;
       if (bad >> token & 1u) s = __int_as_float(0x7fc00000);
     }
+    // codes as 1024 + n, less 1032; an fp16 scale is exact down to 2^-25 of the tile's largest
+    const __half2 s2 = __float2half2_rn(s), bias = __float2half2_rn(1032.f);
     uint32_t o[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      o[j] = pack_f16x2(float(int(w >> (4 * j) & 15u) - 8) * s, float(int(w >> (4 * j + 16) & 15u) - 8) * s);
+      const uint32_t x = (kw[it] >> (4 * j) & 0x000f000fu) | 0x64006400u;
+      const __half2 y = __hmul2(__hsub2(*reinterpret_cast<const __half2*>(&x), bias), s2);
+      o[j] = *reinterpret_cast<const uint32_t*>(&y);
     }
     *reinterpret_cast<uint4*>(wk + (row0 + token) * DK + f8 * 8) = make_uint4(o[0], o[1], o[2], o[3]);
   }
-  // values: two words are eight neighbouring features of two tokens
-  constexpr int kChunksV = DV / 8;
 #pragma unroll
-  for (int it = 0; it < kBlock / 2 * kChunksV / 32; ++it) {
-    const int i = it * 32 + lane, pr = i / kChunksV, f8 = i % kChunksV, g = f8 >> 2, c = (f8 & 3) * 2, token = 2 * pr;
-    uint32_t w[2] = {0x88888888u, 0x88888888u};
-    float s[2] = {0.f, 0.f};
-    if (token < n_tok) {
+  for (int it = 0; it < kItsV; ++it) {
+    const int i = it * 32 + lane, f8 = i % kChunksV, g = f8 >> 2, token = 2 * (i / kChunksV);
+    uint32_t s = 0;   // the two tokens' scales
 #pragma unroll
-      for (int k = 0; k < 2; ++k) w[k] = *reinterpret_cast<const uint32_t*>(src + value_word(DK, token, c + k, g, GV));
+    for (int k = 0; k < 2; ++k)
+      if (token + k < n_tok && !(bad >> (token + k) & 1u))
+        s |= uint32_t(*reinterpret_cast<const uint16_t*>(src + value_scales(DK, DV) + ((token + k) * GV + g) * 2)) << (16 * k);
+    const __nv_bfloat162 s2 = *reinterpret_cast<const __nv_bfloat162*>(&s), bias = __float2bfloat162_rn(136.f);
+    uint32_t y[8];   // a feature of both tokens: codes as 128 + n, less 136; the product is rounded once
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
-        if (token + k < n_tok && !(bad >> (token + k) & 1u))
-          s[k] = bf16_value(src + value_scales(DK, DV) + ((token + k) * GV + g) * 2);
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t x = (vw[it][j >> 2] >> (4 * (j & 3)) & 0x000f000fu) | 0x43004300u;
+      const __nv_bfloat162 z = __hmul2(__hsub2(*reinterpret_cast<const __nv_bfloat162*>(&x), bias), s2);
+      y[j] = *reinterpret_cast<const uint32_t*>(&z);
     }
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       uint32_t o[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t u = w[j >> 1] >> (16 * k + 8 * (j & 1));
-        o[j] = pack_bf16x2(float(int(u & 15u) - 8) * s[k], float(int(u >> 4 & 15u) - 8) * s[k]);
-      }
+      for (int j = 0; j < 4; ++j) o[j] = __byte_perm(y[2 * j], y[2 * j + 1], k ? 0x7632 : 0x5410);
       *reinterpret_cast<uint4*>(wv + (row0 + token + k) * DV + f8 * 8) = make_uint4(o[0], o[1], o[2], o[3]);
     }
   }
