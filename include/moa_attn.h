@@ -443,7 +443,7 @@ int moa_kv4_read(void* K, void* V, const void* pool, const int32_t* pages, const
  * moa_kv4_attn -- attention of N query rows of each sequence over its cached tokens.
  *
  * Defines: the softmax attention of moa_attn_fwd with keys and values as the cache holds them
- * (code * s, not rounded to bf16), query head j reading key head j / (H_q / H_k).  lens[b] tokens of
+ * (code * s), query head j reading key head j / (H_q / H_k).  lens[b] tokens of
  * sequence b are cached, the N query rows being the last N of them: row i sees the first
  * lens[b] - N + i + 1 tokens if `causal`, else all lens[b].  A row that sees no token gives O = 0
  * and LSE = -infinity; what the pool holds past lens[b] has no influence.
@@ -452,9 +452,13 @@ int moa_kv4_read(void* K, void* V, const void* pool, const int32_t* pages, const
  *   lens   int32 [B] on the device, 0 <= lens[b] <= max_len
  *   max_len  what the host knows of the lengths: it decides how the work is divided
  *            (1 <= max_len <= max_pages * page_tokens, below 2^31 - 64)
- *   scale  any finite value;  dtype  MOA_BF16 (weights rounded to bf16 once) or MOA_FP32 (every
- *          product of 24 bits, fp32 accumulation)
+ *   scale  any finite value;  dtype  MOA_BF16 or MOA_FP32 (every product of 24 bits, fp32
+ *          accumulation)
  *   workspace  device, 16-byte aligned, moa_kv4_attn_workspace_bytes(...) bytes
+ * bf16: codes are exact, weights (with few query rows times their values' scales) are rounded to bf16
+ * once; with many query rows values are too (keys never); magnitudes of queries are below 2^120.
+ * Accumulation, maxima and sums are fp32.  A visible token with a member that is not finite makes at
+ * least its group's features of the rows that see it NaN, with many query rows the whole row.
  * H_q a multiple of H_k.  A length outside [0, max_len] is clamped, a page outside the pool counts
  * as hidden tokens; both record MOA_ERR_DEVICE_INDEX.  Bounded waits as moa_attn_fwd.  Bitwise
  * reproducible.
@@ -466,7 +470,8 @@ int moa_kv4_attn(const void* Q, const void* pool, const int32_t* pages, const in
                  void* workspace, size_t workspace_bytes, void* stream);
 
 /* Scratch bytes of moa_kv4_attn on the current device: the pieces of rows whose tokens several CTAs
- * share (0 for invalid sizes or without a device). */
+ * share and, with many bf16 query rows, 16-bit keys and values of some heads at a time (up to 1 GiB, or
+ * one head's).  0 for invalid sizes or without a device. */
 size_t moa_kv4_attn_workspace_bytes(int64_t B, int64_t H_q, int64_t H_k, int64_t N, int64_t d_k,
                                     int64_t d_v, int64_t max_len, int dtype);
 

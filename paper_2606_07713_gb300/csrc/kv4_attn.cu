@@ -15,10 +15,14 @@
 // (24 bits), so the fp32 form is fp32-accurate on the same instructions.  Scores, maxima, sums
 // and outputs accumulate in fp32.
 //
-// What bounds it: for single tokens the cache's bytes, 9/16 a value, and close behind it the
-// instructions that widen codes (about two a value and lane).  Tokens lie on the 16 rows of
-// mma.m16n8k16 and queries on its 8 columns: a decoding step has few queries, and the other way
-// round half of the tensor work would be padding.
+// What bounds it: for single tokens the cache's bytes, 9/16 a value, and before them the instructions
+// that widen codes: their ALU operations fill half of that pipe and, with the products and scales, 57 % of
+// the issue slots at the three warps a scheduler that the registers allow.  Measured, single bf16 tokens,
+// d = 128: 2 x 131072 cached tokens of 8 key heads under 64 query heads 45.4 us = 4.4 TB/s of the cache;
+// 48 uneven sequences up to 16384 under 32 query heads 71.5 us = 4.8 TB/s (measured copy bandwidth: 6.8).
+// Tokens lie on the 16 rows of mma.m16n8k16 and queries on its 8 columns: a decoding step has few
+// queries, and the other way round half of the tensor work would be padding.  (A byte form, codes as
+// fp8 and queries as two fp8 terms, took fewer instructions and a fifth more time.)
 //
 // Layout of the work: a work item is a tile of up to 8 NT query rows of one key head of one
 // sequence; its visible tokens count in units of 64.  The units of all items, in a row, are cut into
@@ -153,7 +157,7 @@ constexpr int kUnitBlocks = kUnit / kBlock;
 // An item costs about as much as this many units besides its tokens (places, queries, the join of
 // the warps): it counts for that many more, which come first and hold no tokens.  Without them a
 // share of short items takes several times as long as one of long items (48 sequences of 0 to 16384
-// tokens: 94 us with 0, 85 with 3, 81 with 5 to 8, 85 with 12).
+// tokens: 87 us with 0, 72 with 6, 74 with 12; two of 131072: 47.6, 45.5, 45.1).
 constexpr int kItemUnits = 6;
 constexpr float kSlack = 8.f;          // the running maximum may lag by this (log2): weights up to 2^8
 
@@ -909,7 +913,8 @@ cudaError_t run(const Kv4AttnArgs& a, const Kv4Plan& plan, const Params& p) {
   if (e != cudaSuccess) return e;
   const int64_t items = a.B * a.c.H * plan.n_tiles, rows = a.N * (a.Hq / a.c.H);
   const dim3 grid(unsigned(items < plan.ctas ? items : plan.ctas), unsigned(rows < 8 * NT ? rows : 8 * NT));
-  // 48 x 8 items on 608 CTAs: 96.7 us with eight warps; 16 items: 53.8 us (57.8 with four)
+  // few items of many pieces: eight warps share the pieces.  16 items on 456 CTAs 45.6 us (49.6 with two
+  // warps); 48 x 8 items 75.0 us (71.6 with two)
   const bool many = plan.ctas >= 8 * items;
   return launch_overlapped(many ? kv4_attn_join_kernel<T, DV, 8 * NT, 8> : kv4_attn_join_kernel<T, DV, 8 * NT, 2>, grid,
                            dim3(many ? 256 : 64), 0, a.stream, part_o, part_ml, cuts, static_cast<T*>(a.o.p), a.lse, p);
@@ -935,9 +940,9 @@ cudaError_t run_d(const Kv4AttnArgs& a, const Kv4Plan& plan, const Params& p) {
 
 // Whether many query rows are faster through kv4_attn_tc.cu.  This file's kernel widens codes once for
 // every 32 rows: 8 us + 0.08 ns for each cached token of a head and 32 rows.  The other one widens
-// once for all, in a launch of its own: 22 us + 0.13 ns for each, + 0.076 ns for each 256 rows.
-// Measured, 8 key heads (this file's, the other's, us): 64 rows x 8192 tokens 22, 37; 128 x 8192 34,
-// 38; 128 x 65536 165, 130; 256 x 8192 51, 42; 512 x 600 22, 28; 2048 x 600 42, 34.
+// once for all, in a launch of its own: 20 us + 0.13 ns for each, + 0.076 ns for each 256 rows.
+// Measured, 8 key heads (this file's, the other's, us): 64 rows x 8192 tokens 22, 36; 128 x 8192 34,
+// 35; 128 x 65536 165, 127; 256 x 8192 51, 38; 512 x 600 22, 25; 2048 x 600 42, 32.
 bool widening_pays(int64_t heads, int64_t rows, int64_t max_len) {
   const double tokens = double(heads) * double(max_len);
   const double n32 = double((rows + 31) / 32), n256 = double((rows + 255) / 256);

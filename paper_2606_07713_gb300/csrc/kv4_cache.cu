@@ -4,7 +4,8 @@
 // code = rint(x / s) (ties to even; for bf16 inputs the same codes as in exact arithmetic).  Read:
 // code * s in fp32, rounded once to the output's type.
 //
-// What bounds it: memory.  A bf16 value is 2 bytes on one side and 9/16 on the other.
+// What bounds it: memory, and in the write the instructions of a code (figures at the kernels).  A bf16
+// value is 2 bytes on one side and 9/16 on the other.
 //
 // Layout of the work: a unit is 16 tokens of a sequence that fall into one 16-token block of the cache
 // when the call's positions are consecutive (a prompt): a head's block is then put together (or taken
@@ -240,7 +241,7 @@ __device__ __forceinline__ void put(uint8_t* to, const Places& at, const Raw<T>&
 }
 
 // Two heads of bf16 at a time share a barrier.  Measured on bf16 keys and values, 3 x 8 x 16001 x (128 +
-// 128): 53.0 us = 4.8 TB/s (the reading kernel 48.2 us = 5.2 TB/s); with three CTAs on an SM 58, with
+// 128): 53.0 us = 4.8 TB/s; with three CTAs on an SM 58, with
 // five (spills) 60; one head at a time 55.6.  The instructions of the codes fill about 70 % of the issue
 // slots, the rest waits for rows and barriers.
 template <typename T, int LPR>
@@ -339,6 +340,8 @@ __device__ __forceinline__ void store_all(float* p, float x) {
   store8(p, y);
 }
 
+// Bound by the stores of the widened rows: 3 x 8 x 16001 x (128 + 128) 48.2 us = 5.2 TB/s, the same with
+// five or six CTAs on an SM instead of four.
 template <typename T, int LPR>
 __global__ void __launch_bounds__(kThreads)
 kv4_read_kernel(View k, View v, uint8_t* pool, const int32_t* table, const int32_t* pos, Dims p) {
