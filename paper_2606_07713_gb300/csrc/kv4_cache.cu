@@ -58,11 +58,11 @@ struct Raw {
   // The largest magnitude's bits, as a float's: a NaN's are above every number's.
   __device__ __forceinline__ uint32_t top() const {
     if constexpr (sizeof(T) == 2) {
-      uint32_t m = 0;   // of each half; a NaN in either operand gives the NaN 0x7fff
-      const uint32_t v[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
+      uint32_t m = w[0].x;   // of each half's magnitudes (the sign is no use); a NaN in either operand gives a NaN
+      const uint32_t v[3] = {w[0].y, w[0].z, w[0].w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(v[i] & 0x7fff7fffu));
-      return max(m << 16, m & 0xffff0000u);
+      for (int i = 0; i < 3; ++i) asm("max.NaN.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(v[i]));
+      return max(m << 16 & 0x7fff0000u, m & 0x7fff0000u);
     } else {
       uint32_t m = 0;
 #pragma unroll
@@ -241,8 +241,8 @@ __device__ __forceinline__ void put(uint8_t* to, const Places& at, const Raw<T>&
 }
 
 // Two heads of bf16 at a time share a barrier.  Measured on bf16 keys and values, 3 x 8 x 16001 x (128 +
-// 128): 53.0 us = 4.8 TB/s; with three CTAs on an SM 58, with
-// five (spills) 60; one head at a time 55.6.  The instructions of the codes fill about 70 % of the issue
+// 128): 52.3 us = 4.8 TB/s; with three CTAs on an SM 58, with
+// five (spills) 60; one head at a time 55.1.  The instructions of the codes fill about 70 % of the issue
 // slots, the rest waits for rows and barriers.
 template <typename T, int LPR>
 __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3)
