@@ -25,7 +25,7 @@
 //
 // What bounds it: the second and first products' tensor time and, beside it, a softmax warp's chain of
 // score load, maximum, 128 exponentials and stores.  Measured, 2048 causal queries of 32 heads against
-// 16384 tokens of 8 key heads, d = 128: 355 us in all = 1.45 PFLOP/s (measured matrix-product rate: 1.89),
+// 16384 tokens of 8 key heads, d = 128: 354 us in all = 1.45 PFLOP/s (measured matrix-product rate: 1.89),
 // of them about 325 us the attention, tensor pipe 67 % active, issue 42 %; the widening 15 to 21 us, the
 // join the rest.
 //
@@ -95,7 +95,9 @@ struct Cfg {
   static constexpr int kOffMisc = kOffBar + kNumBars * 8;
   static constexpr int kOffItems = (kOffMisc + 8 + 15) / 16 * 16;    // two items, then scan[12] and found[2]
   static constexpr int kSmemBytes = kOffItems + 2 * 16 + 14 * 8 + 1024;
-  static constexpr int kEarlyChunks = DV == 64 ? 2 : 3;
+  // exponentials, in chunks of 32 tokens, before the wait for the buffer of P: 2, 3, 4 of 4 at d_v = 128 363, 356,
+  // 354 us (the chunk above); at 64 one to three are the same
+  static constexpr int kEarlyChunks = DV == 64 ? 2 : 4;
   static constexpr uint32_t kTmemCols = 512;
   static constexpr uint32_t kTmemS0 = 0, kTmemS1 = kSharedS ? 0 : 128;
   static constexpr uint32_t kTmemP0 = kSharedS ? 128 : 256, kTmemP1 = kSharedS ? 192 : 320;
