@@ -6,7 +6,8 @@ libmoa_attn.so, and argument checks and marshalling in moa_torch.so beside it (a
 several of these calls, so they are kept to a few microseconds).  Tensors are [B, H, N, d] CUDA
 tensors with unit stride along d and any other strides (a transposed view of a token-major
 [B, N, H, d] tensor needs no copy).  Calls run asynchronously on `stream` (default: torch's current
-stream of the device).  What lives on the device (positions, lengths, page numbers) is checked
+stream of the device); outputs and workspaces that they make are memory of that stream, as if it were
+the current one.  What lives on the device (positions, lengths, page numbers) is checked
 there: check(get_device_status()) raises if one was outside its table.
 """
 from __future__ import annotations
