@@ -12,7 +12,7 @@
 // once and written once (backward: x and g read, dx written), with about ten operations for each, which
 // fill 60 to 65 % of the issue slots.  Measured, bf16: forward 4 x (16 + 16) x 2048 x 64 13.4 us = 5.0
 // TB/s; backward 2 x (32 + 8) x 8192 x 128 95.5 us = 5.3 TB/s; fp32 forward 3 x (10 + 2) x 1021 x 96,
-// 5.1 us, backward 2 x (6 + 3) x 517 x 128, 7.0 us: a launch's own time.
+// 5.1 us, backward 2 x (6 + 3) x 517 x 128, 6.9 us: a launch's own time.
 //
 // Layout of the work: a group of 8, 16 or 32 lanes owns one token and walks over a range of its
 // heads, eight features a lane (one 16-byte load of bf16, two of fp32), in batches whose rows are all
@@ -300,7 +300,6 @@ norm_rope_bwd_kernel(View q, View k, View gq, View gk, View oq, View ok, const T
   const int range = is_q ? int(blockIdx.y) : int(blockIdx.y) - p.nq;
   const View in = is_q ? q : k, gin = is_q ? gq : gk, out = is_q ? oq : ok;
   const int H = is_q ? p.Hq : p.Hk;
-  const int h0 = range * p.hp, h1 = h0 + p.hp < H ? h0 + p.hp : H;
   const int f0 = lane * kV;
   uint64_t acc[kV / 2];
   Raw<T> wraw;
@@ -311,12 +310,28 @@ norm_rope_bwd_kernel(View q, View k, View gq, View gk, View oq, View ok, const T
   const int half_lanes = p.d_rot / 2 / kV;
   const int partner = f0 >= p.d_rot ? lane : (f0 < p.d_rot / 2 ? lane + half_lanes : lane - half_lanes);
   const float inv_d = 1.f / float(p.d);
+  // Rounds of gridDim.x groups of tokens.  In the last one `left` groups may be fewer than CTAs: then
+  // several CTAs share a group's heads.
+  const int64_t all = (p.tokens + kGroups - 1) / kGroups;
+  auto token_of = [&](int64_t round) {
+    const int64_t left = all - round;
+    return (round + (left > 0 && left < gridDim.x ? blockIdx.x % uint32_t(left) : blockIdx.x)) * kGroups + group;
+  };
   // a token's position is read while the token before it is worked on
   auto position = [&](int64_t token) { return token < p.tokens ? pos[token] : -1; };
-  int32_t next_at = position(int64_t(blockIdx.x) * kGroups + group);
+  int32_t next_at = position(token_of(0));
   // every lane of a warp takes part in each turn of the loop (shuffles), whether its token exists
-  for (int64_t base = int64_t(blockIdx.x) * kGroups; base < p.tokens; base += int64_t(gridDim.x) * kGroups) {
-    const int64_t token = base + group;
+  for (int64_t round = 0; round < all; round += gridDim.x) {
+    int h0 = range * p.hp, h1 = h0 + p.hp < H ? h0 + p.hp : H;
+    const int64_t left = all - round;
+    if (left < gridDim.x) {
+      const uint32_t n = gridDim.x / uint32_t(left), mine = blockIdx.x / uint32_t(left);
+      const int each = (h1 - h0 + int(n) - 1) / int(n);
+      if (mine >= n || h0 + int(mine) * each >= h1) break;
+      h0 += int(mine) * each;
+      h1 = h0 + each < h1 ? h0 + each : h1;
+    }
+    const int64_t token = token_of(round);
     const bool live = token < p.tokens;
     const bool mine = live && f0 < p.d;
     const int64_t b = live ? sequence_of(token, p) : 0, n = live ? token - b * p.N : 0;
@@ -346,7 +361,7 @@ norm_rope_bwd_kernel(View q, View k, View gq, View gk, View oq, View ok, const T
     uint64_t c2[kV / 2], s2[kV / 2];
 #pragma unroll
     for (int i = 0; i < kV / 2; ++i) c2[i] = pair(t.c[2 * i], t.c[2 * i + 1]), s2[i] = pair(t.s[2 * i], t.s[2 * i + 1]);
-    next_at = position(token + int64_t(gridDim.x) * kGroups);
+    next_at = position(token_of(round + gridDim.x));
     for (int hb = h0; hb < h1; hb += kBatch) {
 #pragma unroll
       for (int u = 0; u < kBatch; ++u) {
@@ -432,14 +447,15 @@ struct Grid {
   int y, hp, nq;
 };
 // Ranges of heads.  A range costs its heads and about one and a half more (the token's place, angles
-// and weights), a launch as many ranges as there are rounds of resident CTAs (four on an SM): the
-// number of heads with the smallest product is taken, sixteen at most.  On 4 x (16 + 16) heads x 2048
-// x 64, 1024 CTAs of 8 heads make two rounds and 512 of 16 make one: 13.9 and 13.5 us.
+// and weights), a launch as many ranges as a CTA's place takes one after another: the number of heads with
+// the smallest sum is taken, sixteen at most.  On 4 x (16 + 16) heads x 2048 x 64, 1024 CTAs of 8 heads make
+// two rounds of the four that fit on an SM and 512 of 16 make one: 13.9 and 13.5 us.
 // The backward's CTAs each leave one row of sums, so as many as are resident at once (`ctas` on an SM;
-// 0 in the forward) walk over the tokens.  Three CTAs an SM of fp32, where two fit, cost a second round:
-// 8.4 instead of 7.0 us on 2 x (6 + 3) heads x 517 x 128.
+// 0 in the forward) walk over the tokens, and where the last round has fewer groups of tokens than
+// CTAs, several share a group's heads (the same sizes: 25.0 us, without that 30.6).  Three CTAs an SM of
+// fp32, where two fit, cost a second round: 8.4 instead of 6.9 us on 2 x (6 + 3) heads x 517 x 128.
 Grid plan(int64_t tokens, int64_t Hq, int64_t Hk, int64_t d, int sms, int ctas) {
-  const int64_t per = kThreads / lanes_per_row(d), x = (tokens + per - 1) / per;
+  const int64_t per = kThreads / lanes_per_row(d), groups = (tokens + per - 1) / per;
   const int64_t most = Hq > Hk ? Hq : Hk;
   Grid best{};
   double least = 0;
@@ -448,15 +464,18 @@ Grid plan(int64_t tokens, int64_t Hq, int64_t Hk, int64_t d, int sms, int ctas) 
     g.hp = int(hp);
     g.nq = int((Hq + hp - 1) / hp);
     g.y = g.nq + int((Hk + hp - 1) / hp);
-    g.x = x;
-    const int64_t rounds = (x * g.y + sms * 4 - 1) / (sms * 4);
-    const double cost = double(rounds) * (double(hp) + 1.5);
+    g.x = groups;
+    double cost;
+    if (ctas > 0) {
+      const int64_t limit = int64_t(sms) * ctas / g.y;
+      if (g.x > limit) g.x = limit < 1 ? 1 : limit;
+      const int64_t left = groups % g.x;
+      cost = double(groups / g.x) * (double(hp) + 1.5);
+      if (left > 0) cost += double((hp + g.x / left - 1) / (g.x / left)) + 1.5;
+    } else {
+      cost = double((g.x * g.y + sms * 4 - 1) / (sms * 4)) * (double(hp) + 1.5);
+    }
     if (best.hp == 0 || cost <= least) best = g, least = cost;
-  }
-  if (ctas > 0) {
-    int64_t limit = int64_t(sms) * ctas / best.y;
-    limit = limit < 1 ? 1 : limit;
-    if (best.x > limit) best.x = limit;
   }
   return best;
 }
@@ -518,8 +537,12 @@ int launch(const NormRopeArgs& a, bool bwd, char* msg, size_t msglen) {
 }  // namespace
 
 int64_t norm_rope_partial_rows(int64_t B, int64_t Hq, int64_t Hk, int64_t N, int64_t d, int sms) {
-  const Grid g = plan(B * N, Hq, Hk, d, sms, bwd_ctas(false));  // the larger of the two types'
-  return g.x * g.y;
+  int64_t rows = 0;   // the larger of the two types'
+  for (const bool f32 : {false, true}) {
+    const Grid g = plan(B * N, Hq, Hk, d, sms, bwd_ctas(f32));
+    rows = g.x * g.y > rows ? g.x * g.y : rows;
+  }
+  return rows;
 }
 
 int launch_norm_rope(const NormRopeArgs& a, char* msg, size_t msglen) {

@@ -104,6 +104,24 @@ def test_forward_and_gradients(shape, dtype):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("dims", [(1, 4, 4, 7501, 64, 64), (2, 5, 3, 2570, 64, 32), (1, 7, 2, 5003, 128, 128)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_gradients_of_more_tokens_than_one_round(dims, dtype):
+    """More groups of tokens than CTAs: whole rounds, and a last one whose few groups' heads are shared
+    by several CTAs (evenly, unevenly, or by more than there are heads).  The bounds are those above:
+    a lane's chain of additions is its rounds' heads, far below 200."""
+    x = make(*dims, dtype, seed=sum(dims))
+    x["pos"][:, ::97] = -1
+    t = on_device(x, dtype)
+    dq, dk, dwq, dwk = pkg.qk_norm_rope_bwd(t["q"], t["k"], t["wq"], t["wk"], t["cos"], t["sin"], t["pos"],
+                                            t["gq"], t["gk"], EPS, False)
+    assert pkg.get_device_status() == _lib.MOA_OK
+    for dy, dw, n in ((dq, dwq, "q"), (dk, dwk, "k")):
+        check_bwd(dy, dw, x[n], x["w" + n], x["cos"], x["sin"], x["pos"], x["g" + n], False, dtype, n)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_slices_of_one_buffer_in_place_and_transposed(dtype):
     """Token-major projections [B, N, (Hq + Hk + Hv) d]: q and k as strided views, written in place;
     the values between the tokens' heads stay untouched.  Outputs may be token-major too, and
