@@ -8,13 +8,15 @@
 //
 //   widen    one CTA for 128 tokens of a head.  Keys become fp16: code * scale has at most 3 + 8
 //            significant bits, so with the tile's power of two 2^E taken out (E from its largest
-//            scale) the products are exact; 2^E goes into the tile's softmax factor.  Values become
-//            bf16, rounded once.  Tokens past the end, and pages that are not there, become zeros
+//            scale) the products are exact while the scales are within 2^28 of each other; 2^E goes
+//            into the tile's softmax factor.  A tile with scales further apart is marked, and its
+//            scores are computed from the codes in fp32 instead (exact_scores: about 0.1 ms a tile, for
+//            keys that a trained model does not have).  Values become bf16, rounded once.  Tokens past the end, and pages that are not there, become zeros
 //            (the rows' limits, and a mark beside the factor, hide them).
 //            A token whose value is not finite gets zeros and a NaN key: the rows that see it
 //            read NaN, the others nothing (0 * NaN would reach them through the second product).
-//   attend   query rows, as fp16 with each row's power of two taken out (bf16 queries fit exactly),
-//            against 128-token tiles: S = Q K^T (fp16), running maximum and sum per row, O += P V
+//   attend   query rows, as fp16 with each row's power of two taken out (members within 2^-31 of the
+//            row's largest fit exactly, smaller ones are rounded to 2^-40 of it), against 128-token tiles: S = Q K^T (fp16), running maximum and sum per row, O += P V
 //            (bf16) in TMEM.  Maximum, exponentials, sum in fp32.  P and V in fp16 (11 bits, V then
 //            exact) would halve the rounding of ordinary rows, but weights below 2^-31 of the largest
 //            would be lost, and they are all there is of a feature that the larger ones leave at zero.
@@ -170,6 +172,24 @@ __device__ __forceinline__ float bf16_value(const uint8_t* p) {
   return __uint_as_float(uint32_t(*reinterpret_cast<const uint16_t*>(p)) << 16);
 }
 
+// 2^e, -126 <= e <= 127, and the exponent that brings a largest scale (its bits) into [2^to, 2^(to + 1)).
+__device__ __forceinline__ float power_of(int e) { return __uint_as_float(uint32_t(127 + e) << 23); }
+__device__ __forceinline__ int tile_exponent(uint32_t top, int to) {
+  return top == 0 ? 0 : max(int(top >> 23) - 127 - to, -126);
+}
+// Of tiles with scales far apart: room for queries below 2^15, codes and 128 products above, and for
+// scales down to 2^-186 of the largest below.
+constexpr int kMixedTop = 60;
+// The power of two that a row's largest magnitude (its bf16 bits) is brought into [2^14, 2^15) by; a row
+// with a member that is not finite stays as it is.
+__device__ __forceinline__ int row_exponent(uint32_t top) {
+  return top == 0 || top >= 0x7f80u ? 0 : max(int(top >> 7) - 127 - 14, -126);
+}
+
+// What a tile's factor carries beside its power of two: a bit for each 16-token block whose page is not
+// there, and whether the tile's scores have to be computed in fp32.
+constexpr uint32_t kGoneBlocks = 0xffu, kMixedKeys = 0x100u;
+
 // Bound by its stores into L2 and the latency of a warp's one block: 2304 bytes in, 8 KB out.  Words
 // asked for before the scales are looked at, and products in pairs: 5 us less than one after the other
 // (128 tiles of 8 heads, of 355 us).
@@ -179,8 +199,7 @@ kv4_widen_kernel(const uint8_t* __restrict__ pool, const int32_t* __restrict__ t
                  const int32_t* __restrict__ lens, __half* __restrict__ wk, __nv_bfloat16* __restrict__ wv,
                  float2* __restrict__ factor, Params p) {
   constexpr int GK = DK / 32, GV = DV / 32;
-  __shared__ float s_max[8];
-  __shared__ uint32_t s_gone[8];
+  __shared__ uint32_t s_max[8], s_min[8], s_gone[8];
   wait_for_previous();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int tile = int(blockIdx.x), bh = int(blockIdx.y);
@@ -216,40 +235,45 @@ kv4_widen_kernel(const uint8_t* __restrict__ pool, const int32_t* __restrict__ t
       vw[it][k] = token < n_tok ? *reinterpret_cast<const uint32_t*>(src + value_word(DK, token, (f8 & 3) * 2 + k, f8 >> 2, GV))
                                 : 0x88888888u;
   }
-  // the largest key scale, and the tokens with a value scale that is not finite
-  float top = 0.f;
+  // the largest and the smallest key scale that is a number and not zero (their bits are in the same
+  // order), and the tokens with a value scale that is not finite
+  uint32_t top_bits = 0, low_bits = 0x7f800000u;
   uint32_t bad = 0;
   if (src != nullptr) {
     for (int i = lane; i < kBlock * GK; i += 32) {
       const float s = bf16_value(src + key_scales(DK, DV) + 2 * i);
-      if (i / GK < n_tok && s < INFINITY) top = fmaxf(top, s);
+      if (i / GK < n_tok && s > 0.f && s < INFINITY)
+        top_bits = max(top_bits, __float_as_uint(s)), low_bits = min(low_bits, __float_as_uint(s));
     }
     for (int i = lane; i < kBlock * GV; i += 32) {
       const float s = bf16_value(src + value_scales(DK, DV) + 2 * i);
       if (!(s < INFINITY)) bad |= 1u << (i / GV);
     }
   }
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) {
-    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-    bad |= __shfl_xor_sync(0xffffffffu, bad, d);
-  }
+  top_bits = __reduce_max_sync(0xffffffffu, top_bits);
+  low_bits = __reduce_min_sync(0xffffffffu, low_bits);
+  bad = __reduce_or_sync(0xffffffffu, bad);
   if (lane == 0) {
-    s_max[warp] = top;
+    s_max[warp] = top_bits;
+    s_min[warp] = low_bits;
     s_gone[warp] = src == nullptr && blk * kBlock < len ? 1u << warp : 0u;
   }
   __syncthreads();
   uint32_t gone = 0;   // the tile's blocks whose page is not there
 #pragma unroll
   for (int w = 0; w < 8; ++w) {
-    top = fmaxf(top, s_max[w]);
+    top_bits = max(top_bits, s_max[w]);
+    low_bits = min(low_bits, s_min[w]);
     gone |= s_gone[w];
   }
-  // 2^E with the largest scale times 2^-E in [2^11, 2^12)
-  int e = int(__float_as_uint(top) >> 23) - 127 - 11;
-  e = top == 0.f ? 0 : e < -126 ? -126 : e;
-  const float up = __uint_as_float(uint32_t(127 + e) << 23), down = __uint_as_float(uint32_t(127 - e) << 23);
-  if (threadIdx.x == 0) factor[int64_t(bh) * p.tiles_pad + tile] = make_float2(up, __uint_as_float(gone));
+  // 2^E with the largest scale times 2^-E in [2^11, 2^12); eight bits of a scale then end above 2^-24, the
+  // spacing of the smallest fp16, if it is 2^-17 or more
+  const int e = tile_exponent(top_bits, 11);
+  const float down = power_of(-e);
+  const bool mixed = low_bits < 0x7f800000u && __uint_as_float(low_bits) * down < 0x1p-17f;
+  if (threadIdx.x == 0)
+    factor[int64_t(bh) * p.tiles_pad + tile] = make_float2(
+        power_of(mixed ? tile_exponent(top_bits, kMixedTop) : e), __uint_as_float(mixed ? gone | kMixedKeys : gone));
 
   const int64_t row0 = (int64_t(bh) * p.tiles_pad + tile) * kBN + warp * kBlock;
 #pragma unroll
@@ -260,7 +284,7 @@ kv4_widen_kernel(const uint8_t* __restrict__ pool, const int32_t* __restrict__ t
       s = bf16_value(src + key_scales(DK, DV) + (token * GK + g) * 2) * down;
       if (bad >> token & 1u) s = __int_as_float(0x7fc00000);
     }
-    // codes as 1024 + n, less 1032; an fp16 scale is exact down to 2^-25 of the tile's largest
+    // codes as 1024 + n, less 1032
     const __half2 s2 = __float2half2_rn(s), bias = __float2half2_rn(1032.f);
     uint32_t o[4];
 #pragma unroll
@@ -336,6 +360,171 @@ __host__ __device__ constexpr uint32_t make_idesc_f16(int M, int N) {
   return (1u << 4) | (uint32_t(N >> 3) << 17) | (uint32_t(M >> 4) << 24);
 }
 
+// A thread's query row and where its head's codes lie.
+struct Codes {
+  const __nv_bfloat16* q;   // null: no row
+  const uint8_t* pool;      // the head's place in page 0
+  const int32_t* pages;     // of the sequence
+  int64_t page_bytes, n_pages;
+  int blocks_per_page, len;
+  float sign;               // of the scale
+};
+
+// The scores of a thread's row against a tile whose key scales lie too far apart for fp16, into its TMEM
+// lane (warp-collective), in fp32 from the cache's codes: the row with its power of two taken out, as in
+// the product, the scales times `down`.  Tokens that are not there get zeros; the caller hides them.
+template <int DK, int DV>
+__device__ void exact_scores(uint32_t tS, const Codes& a, int tile, float down) {
+  constexpr int GK = DK / 32;
+  uint32_t top = 0;
+  for (int i = 0; a.q != nullptr && i < DK; ++i)
+    top = max(top, uint32_t(reinterpret_cast<const uint16_t*>(a.q)[i]) & 0x7fffu);
+  const float row_down = power_of(-row_exponent(top)) * a.sign;
+#pragma unroll 1
+  for (int k = 0; k < kBN / kBlock; ++k) {
+    const int blk = tile * (kBN / kBlock) + k, slot = int(unsigned(blk) / unsigned(a.blocks_per_page));
+    const int pg = blk * kBlock < a.len ? a.pages[slot] : -1;
+    float s[kBlock];
+#pragma unroll
+    for (int u = 0; u < kBlock; ++u) s[u] = 0.f;
+    if (a.q != nullptr && pg >= 0 && pg < a.n_pages) {
+      const uint8_t* src = a.pool + pg * a.page_bytes + (blk - slot * a.blocks_per_page) * block_bytes(DK, DV);
+#pragma unroll 1
+      for (int g = 0; g < GK; ++g) {
+        float part[kBlock];
+#pragma unroll
+        for (int u = 0; u < kBlock; ++u) part[u] = 0.f;
+#pragma unroll 1
+        for (int t = 0; t < 4; ++t) {
+          float x[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = __bfloat162float(a.q[32 * g + 8 * t + e]) * row_down;
+#pragma unroll
+          for (int u = 0; u < kBlock; ++u) {
+            const uint32_t w = *reinterpret_cast<const uint32_t*>(src + key_word(u, t, g, GK));
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              part[u] += x[e] * float(int(w >> (16 * (e & 1) + 4 * (e >> 1)) & 15u) - 8);
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < kBlock; ++u) s[u] += part[u] * (bf16_value(src + key_scales(DK, DV) + (u * GK + g) * 2) * down);
+      }
+    }
+    uint32_t r[kBlock];
+#pragma unroll
+    for (int u = 0; u < kBlock; ++u) r[u] = __float_as_uint(s[u]);
+    __syncwarp();
+    tmem_st_32x32b_x16(tS + kBlock * k, r);
+  }
+  tmem_wait_st();
+}
+
+// What a softmax thread of row tile j works with in an item: its lane of the TMEM buffers, barriers, the
+// tiles' factors from the sequence's first on, the tokens that its row sees, its tiles, its row's factor.
+struct Tiles {
+  uint32_t tS, tO, tP;
+  uint32_t s_full, s_free, p_ready, p_free;
+  const float2* fac;
+  int lim, u0, u1;
+  float c_row;
+};
+
+// The softmax of an item's tiles: maximum m and sum l of the thread's row.  `t`: the tiles of the CTA
+// before them.  ODD: some carry marks; false if a wait ran out.
+template <int DK, int DV, bool ODD>
+__device__ __forceinline__ bool item_tiles(const Tiles& x, const Codes* codes, uint32_t t, float& m, float& l,
+                                           const WaitCtl& wc) {
+  using C = Cfg<DK, DV>;
+  float2 f_next = x.fac[x.u0];
+  for (int n = x.u0; n < x.u1; ++n, ++t) {
+    const float c = fmaxf(x.c_row * f_next.x, FLT_MIN);   // not zero: c * -infinity hides a token
+    const uint32_t marks = ODD ? __float_as_uint(f_next.y) : 0;
+    [[maybe_unused]] const float up = f_next.x;
+    if (n + 1 < x.u1) f_next = x.fac[n + 1];
+    if (!wait_bounded(x.s_full, t & 1u, wc)) return false;
+    tc_fence_after_sync();
+    if constexpr (ODD) {
+      if (marks & kMixedKeys) exact_scores<DK, DV>(x.tS, *codes, n, 1.f / up);
+    }
+    uint32_t sr[128];
+    tmem_load_row128(x.tS, sr);
+    tc_fence_before_sync();
+    mbar_arrive(x.s_free);
+    float* s = reinterpret_cast<float*>(sr);
+    const int valid = x.lim - n * kBN;   // of this row
+    const bool full = __all_sync(0xffffffffu, valid >= kBN) && marks == 0;
+    if (!full) {   // hidden tokens: -infinity, and the rest is the same code
+#pragma unroll
+      for (int i = 0; i < kBN; ++i) s[i] = i < valid && !(marks & kGoneBlocks & 1u << i / kBlock) ? s[i] : -INFINITY;
+    }
+    const float m_tile = c * row_max128(s);
+    bool rescale = false;   // warp-uniform
+    float alpha = 1.f;
+    if (n == x.u0) {
+      m = m_tile;
+    } else if (__any_sync(0xffffffffu, m_tile > m + kRescaleLog2)) {
+      const float m_new = fmaxf(m, m_tile);
+      alpha = m == -INFINITY ? 0.f : ex2_approx(m - m_new);
+      l *= alpha;
+      m = m_new;
+      rescale = true;
+    }
+    const float base = m == -INFINITY ? 0.f : m;
+    const uint64_t cc = pack_f32x2(c, c);
+    const uint64_t mm = pack_f32x2(-base, -base);
+    float l0 = 0.f, l1 = 0.f, l2 = 0.f, l3 = 0.f;
+    auto exp_chunk = [&](int ch, uint32_t* pk) {
+#pragma unroll
+      for (int i = 0; i < 32; i += 4) {
+        const int k = 32 * ch + i;
+        float x0, x1, x2, x3;
+        ffma2(x0, x1, s[k], s[k + 1], cc, mm);
+        ffma2(x2, x3, s[k + 2], s[k + 3], cc, mm);
+        const float p0 = ex2_approx(x0), p1 = ex2_approx(x1), p2 = ex2_approx(x2), p3 = ex2_approx(x3);
+        fadd2(l0, l1, p0, p1);
+        fadd2(l2, l3, p2, p3);
+        pk[i >> 1] = pack_bf16x2(p0, p1);
+        pk[(i >> 1) + 1] = pack_bf16x2(p2, p3);
+      }
+    };
+    auto store_chunk = [&](int ch, const uint32_t* pk) { tmem_st_32x32b_x16(x.tP + 16 * ch, pk); };
+    constexpr int kEarly = C::kEarlyChunks;
+    uint32_t pe[16 * kEarly];
+#pragma unroll
+    for (int ch = 0; ch < kEarly; ++ch) exp_chunk(ch, pe + 16 * ch);
+    // P_j's buffer is free, and O_j may be rescaled, once the previous tile's product is done
+    if (t > 0 && !wait_bounded(x.p_free, (t - 1) & 1u, wc)) return false;
+    tc_fence_after_sync();
+#pragma unroll
+    for (int ch = 0; ch < kEarly; ++ch) store_chunk(ch, pe + 16 * ch);
+#pragma unroll
+    for (int ch = kEarly; ch < 4; ++ch) {
+      uint32_t pk[16];
+      exp_chunk(ch, pk);
+      store_chunk(ch, pk);
+    }
+    l += (l0 + l1) + (l2 + l3);
+    if (rescale) tmem_scale_row<DV>(x.tO, alpha);
+    tmem_wait_st();
+    tc_fence_before_sync();
+    mbar_arrive(x.p_ready);
+  }
+  return true;
+}
+// Items with marks, which are rare, in a function of their own: in the one loop for all items, the call of
+// exact_scores cost that 3 to 5 %.
+struct Row {
+  float m, l;
+  bool ok;
+};
+template <int DK, int DV>
+__device__ __noinline__ Row odd_item_tiles(const Tiles& x, const Codes& codes, uint32_t t, const WaitCtl& wc) {
+  Row r{-INFINITY, 0.f, true};
+  r.ok = item_tiles<DK, DV, true>(x, &codes, t, r.m, r.l, wc);
+  return r;
+}
+
 // One item of a CTA's share: its tiles [u0, u1) of `units` are this CTA's.  item < 0: no more.
 struct Item {
   int item, u0, u1, units;
@@ -344,7 +533,8 @@ struct Item {
 template <int DK, int DV>
 __global__ void __launch_bounds__(kThreads, 1)
 kv4_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
-                   const __nv_bfloat16* __restrict__ Q, const float2* __restrict__ factor,
+                   const __nv_bfloat16* __restrict__ Q, const uint8_t* __restrict__ pool,
+                   const int32_t* __restrict__ table, const float2* __restrict__ factor,
                    const int32_t* __restrict__ lens, __nv_bfloat16* __restrict__ O, float* __restrict__ lse,
                    float* __restrict__ part_o, float2* __restrict__ part_ml, Cut* __restrict__ cuts, Params p) {
   using C = Cfg<DK, DV>;
@@ -623,7 +813,7 @@ kv4_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     for (uint32_t seg = 0;; ++seg) {
       const Item x0 = get_item(seg, ok);
       if (x0.item < 0) break;
-      int u0 = x0.u0, u1 = x0.u1;
+      const int u0 = x0.u0, u1 = x0.u1;
       // where the thread's row lies: row r of key head bh is query ri of its query head rh
       struct Place {
         int r, b, h, rh, ri;
@@ -659,12 +849,9 @@ kv4_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
             top = max(top, (q[k] >> 16) & 0x7fffu);
           }
         }
-        // the largest magnitude in [2^14, 2^15); a row with a member that is not finite as it is
-        int e = int(top >> 7) - 127 - 14;
-        if (top == 0 || top >= 0x7f80u) e = 0;
-        if (e < -126) e = -126;
-        const float down = __uint_as_float(uint32_t(127 - e) << 23) * (p.negate ? -1.f : 1.f);
-        c_row *= __uint_as_float(uint32_t(127 + e) << 23);
+        const int e = row_exponent(top);
+        const float down = power_of(-e) * (p.negate ? -1.f : 1.f);
+        c_row *= power_of(e);
 #pragma unroll
         for (int i = 0; i < DK / 8; ++i) {
           const uint32_t q[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
@@ -678,83 +865,25 @@ kv4_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         fence_proxy_async_smem();
         mbar_arrive(q_full);
       }
+      bool odd = false;   // a tile of the item is marked (looked for while the first product runs)
+      for (int n = u0 + lane; n < u1; n += 32) odd |= __float_as_uint(fac[n].y) != 0;
+      odd = __any_sync(0xffffffffu, odd);
       float m = -INFINITY, l = 0.f;
-      float2 f_next = fac[u0];
-      for (int n = u0; n < u1; ++n, ++t) {
-        const float c = fmaxf(c_row * f_next.x, FLT_MIN);   // not zero: c * -infinity hides a token
-        const uint32_t gone = __float_as_uint(f_next.y);   // blocks whose page is not there
-        if (n + 1 < u1) f_next = fac[n + 1];
-        if (!wait_bounded(s_full(j), t & 1u, wc)) {
-          ok = false;
-          break;
-        }
-        tc_fence_after_sync();
-        uint32_t sr[128];
-        tmem_load_row128(tS, sr);
-        tc_fence_before_sync();
-        mbar_arrive(s_free(j));
-        float* s = reinterpret_cast<float*>(sr);
-        const int valid = lim - n * kBN;   // of this row
-        const bool full = __all_sync(0xffffffffu, valid >= kBN) && gone == 0;
-        if (!full) {   // hidden tokens: -infinity, and the rest is the same code
-#pragma unroll
-          for (int i = 0; i < kBN; ++i) s[i] = i < valid && !(gone >> (i / kBlock) & 1u) ? s[i] : -INFINITY;
-        }
-        const float m_tile = c * row_max128(s);
-        bool rescale = false;   // warp-uniform
-        float alpha = 1.f;
-        if (n == u0) {
-          m = m_tile;
-        } else if (__any_sync(0xffffffffu, m_tile > m + kRescaleLog2)) {
-          const float m_new = fmaxf(m, m_tile);
-          alpha = m == -INFINITY ? 0.f : ex2_approx(m - m_new);
-          l *= alpha;
-          m = m_new;
-          rescale = true;
-        }
-        const float base = m == -INFINITY ? 0.f : m;
-        const uint64_t cc = pack_f32x2(c, c);
-        const uint64_t mm = pack_f32x2(-base, -base);
-        float l0 = 0.f, l1 = 0.f, l2 = 0.f, l3 = 0.f;
-        auto exp_chunk = [&](int ch, uint32_t* pk) {
-#pragma unroll
-          for (int i = 0; i < 32; i += 4) {
-            const int k = 32 * ch + i;
-            float x0, x1, x2, x3;
-            ffma2(x0, x1, s[k], s[k + 1], cc, mm);
-            ffma2(x2, x3, s[k + 2], s[k + 3], cc, mm);
-            const float p0 = ex2_approx(x0), p1 = ex2_approx(x1), p2 = ex2_approx(x2), p3 = ex2_approx(x3);
-            fadd2(l0, l1, p0, p1);
-            fadd2(l2, l3, p2, p3);
-            pk[i >> 1] = pack_bf16x2(p0, p1);
-            pk[(i >> 1) + 1] = pack_bf16x2(p2, p3);
-          }
-        };
-        auto store_chunk = [&](int ch, const uint32_t* pk) { tmem_st_32x32b_x16(tP + 16 * ch, pk); };
-        constexpr int kEarly = C::kEarlyChunks;
-        uint32_t pe[16 * kEarly];
-#pragma unroll
-        for (int ch = 0; ch < kEarly; ++ch) exp_chunk(ch, pe + 16 * ch);
-        // P_j's buffer is free, and O_j may be rescaled, once the previous tile's product is done
-        if (t > 0 && !wait_bounded(p_free(j), (t - 1) & 1u, wc)) {
-          ok = false;
-          break;
-        }
-        tc_fence_after_sync();
-#pragma unroll
-        for (int ch = 0; ch < kEarly; ++ch) store_chunk(ch, pe + 16 * ch);
-#pragma unroll
-        for (int ch = kEarly; ch < 4; ++ch) {
-          uint32_t pk[16];
-          exp_chunk(ch, pk);
-          store_chunk(ch, pk);
-        }
-        l += (l0 + l1) + (l2 + l3);
-        if (rescale) tmem_scale_row<DV>(tO, alpha);
-        tmem_wait_st();
-        tc_fence_before_sync();
-        mbar_arrive(p_ready(j));
+      const Tiles x{tS, tO, tP, s_full(j), s_free(j), p_ready(j), p_free(j), fac, lim, u0, u1, c_row};
+      if (odd) {
+        const Place w = place(items[seg & 1].item);
+        const __nv_bfloat16* q = Q + int64_t(w.b) * p.q_sb + (int64_t(w.h) * p.G + w.rh) * p.q_sh + int64_t(w.ri) * p.q_sn;
+        const int64_t head_bytes = int64_t(p.blocks_per_page) * block_bytes(DK, DV);
+        const Codes codes{w.live ? q : nullptr, pool + w.h * head_bytes, table + w.b * p.max_pages, p.Hk * head_bytes,
+                          p.n_pages, p.blocks_per_page, length_of(lens, w.b, p, false), p.negate ? -1.f : 1.f};
+        const Tiles x_there = x;   // copies, so that what is in registers needs no address
+        const WaitCtl wc_there = wc;
+        const Row r = odd_item_tiles<DK, DV>(x_there, codes, t, wc_there);
+        m = r.m, l = r.l, ok = r.ok;
+      } else {
+        ok = item_tiles<DK, DV, false>(x, nullptr, t, m, l, wc);
       }
+      t += u1 - u0;
       if (!ok || !wait_bounded(o_done(j), seg & 1u, wc)) break;
       tc_fence_after_sync();
       // the item is written, or this CTA's piece of it
@@ -931,7 +1060,8 @@ int launch(const Kv4AttnArgs& a, int sms, char* msg, size_t msglen) {
                           static_cast<const uint8_t*>(a.c.pool), a.c.table, a.lens, wk, wv, factor, p);
     if (e == cudaSuccess)
       e = launch_overlapped(kern, dim3(ctas), dim3(kThreads), C::kSmemBytes, a.stream, mk, mv,
-                            static_cast<const __nv_bfloat16*>(a.q.p), factor, a.lens, static_cast<__nv_bfloat16*>(a.o.p),
+                            static_cast<const __nv_bfloat16*>(a.q.p), static_cast<const uint8_t*>(a.c.pool), a.c.table,
+                            factor, a.lens, static_cast<__nv_bfloat16*>(a.o.p),
                             a.lse, part_o, part_ml, cuts, p);
     if (e == cudaSuccess)
       e = launch_overlapped(kv4_attn_tc_join_kernel<DV>, dim3(ctas, kRows / 8), dim3(256), 0, a.stream, part_o, part_ml,

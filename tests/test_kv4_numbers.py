@@ -1,0 +1,89 @@
+"""Attention over the 4-bit cache where its inputs are far apart in size, or are no numbers: single
+queries and drafts as well as chunks that are attended to on the tensor cores, with the same answers.
+
+The bounds are those of test_kv4.py; what a row does not see leaves no trace in it.
+"""
+import numpy as np
+import pytest
+
+import ops_reference as R
+import paper_2606_07713_gb300 as pkg
+from paper_2606_07713_gb300 import _lib
+from test_kv4 import cast, check, dev, host, table_of
+from test_kv4_chunks import reference, widened
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+HQ, HK, PAGE = 4, 1, 64
+ROWS = [1, 40, 512]      # 4, 160 and 2048 query rows of the key head: the last as a chunk
+
+
+def filled(k, v):
+    """A pool holding keys and values [1, H, T, d] in shuffled pages, and its table."""
+    table, n_pages = table_of(np.random.default_rng(1), [k.shape[2]], PAGE)
+    pool = torch.full((n_pages, HK, PAGE // 16, 9 * (k.shape[3] + v.shape[3])), 255, dtype=torch.uint8, device="cuda:0")
+    pos = np.arange(k.shape[2], dtype=np.int32)[None]
+    pkg.kv4_write(dev(k, "bf16"), dev(v, "bf16"), pool, dev(table), dev(pos))
+    return pool, dev(table)
+
+
+def attend(q, k, v, causal=True):
+    o, lse = pkg.kv4_attn_lse(dev(q, "bf16"), *filled(k, v), dev(np.array([k.shape[2]], dtype=np.int32)),
+                              max_len=k.shape[2], causal=causal)
+    assert pkg.get_device_status() == _lib.MOA_OK
+    return o, lse
+
+
+def inputs(N, T, dk, dv, seed):
+    if N == 512:
+        assert widened(1, HQ, HK, N, dk, dv, T)
+    r = np.random.default_rng(seed)
+    q = r.normal(size=(1, HQ, N, dk))
+    return q, r.normal(size=(1, HK, T, dk)), r.normal(size=(1, HK, T, dv))
+
+
+def stored(k, v):
+    return R.values(*R.quantise(k)), R.values(*R.quantise(v))
+
+
+@pytest.mark.parametrize("power", [20, 28, 30, 36, 60, 100])
+@pytest.mark.parametrize("N", ROWS)
+def test_keys_of_mixed_sizes(N, power):
+    """Every third token's keys, and 32 features of every other token's, are 2^power times larger than the
+    rest, where the queries are zero: the scores are those of the small ones."""
+    T, d = 4100, 128
+    q, k, v = inputs(N, T, d, d, seed=power)
+    q[..., 32:64] = 0.0
+    third = np.arange(T) % 3 == 0
+    k[:, :, ~third & (np.arange(T) % 2 == 1), 32:64] *= 2.0 ** power
+    k[:, :, third, :32] = k[:, :, third, 64:] = 0.0
+    k[:, :, third, 32:64] *= 2.0 ** (power - 3)
+    q, k, v = cast(q, "bf16"), cast(k, "bf16"), cast(v, "bf16")
+    o, lse = attend(q, k, v)
+    check(o, lse, reference(q, *stored(k, v), [T], d ** -0.5, True), d, "bf16", power)
+
+
+@pytest.mark.parametrize("power", [20, 40, 100])
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_huge_key_is_no_concern_of_rows_before_it(d, power):
+    N, T, at = 512, 4096, 3800
+    q, k, v = inputs(N, T, d, d, seed=power + d)
+    k[:, :, at] *= 2.0 ** power
+    q, k, v = cast(q, "bf16"), cast(k, "bf16"), cast(v, "bf16")
+    before = at - (T - N)                     # rows that do not see it
+    o, lse = attend(q, k, v)
+    ref = reference(q, *stored(k, v), [T], d ** -0.5, True)
+    check(o[:, :, :before], lse[:, :, :before], [x[:, :, :before] for x in ref], d, "bf16", power)
+
+
+def test_single_precision_reads_of_mixed_sizes():
+    """The cache itself loses nothing of them: what the cases above expect is what it holds."""
+    T, d = 64, 128
+    _, k, v = inputs(1, T, d, d, seed=8)
+    k[:, :, ::2, 32:64] *= 2.0 ** 100
+    k, v = cast(k, "bf16"), cast(v, "bf16")
+    pool, table = filled(k, v)
+    got = pkg.kv4_read(pool, table, dev(np.arange(T, dtype=np.int32)[None]), d, dtype=torch.float32)
+    for x, y in zip(got, stored(k, v)):
+        assert np.array_equal(host(x), y)
