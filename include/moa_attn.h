@@ -458,8 +458,8 @@ int moa_kv4_read(void* K, void* V, const void* pool, const int32_t* pages, const
  * bf16: codes are exact, weights (with few query rows times their values' scales) are rounded to bf16
  * once; with many query rows values are too (keys never), and members of a query row below 2^-31 of its
  * largest to 2^-40 of that; magnitudes of queries are below 2^120.
- * Accumulation, maxima and sums are fp32.  A visible token with a member that is not finite makes at
- * least its group's features of the rows that see it NaN, with many query rows the whole row.
+ * Accumulation, maxima and sums are fp32.  A key that is not finite makes the rows that see it NaN, a
+ * value that is not finite the 32 features of its group in those rows, however small its weight.
  * H_q a multiple of H_k.  A length outside [0, max_len] is clamped, a page outside the pool counts
  * as hidden tokens; both record MOA_ERR_DEVICE_INDEX.  Bounded waits as moa_attn_fwd.  Bitwise
  * reproducible.

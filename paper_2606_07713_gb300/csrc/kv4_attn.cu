@@ -657,7 +657,7 @@ kv4_attn_kernel(const T* __restrict__ Q, const uint8_t* __restrict__ pool,
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             float w = ex2_approx(fmaf(sc[u][n][e], c2[n][e & 1], mb[n][e & 1]));
-            if (!PLAIN && sc[u][n][e] == -INFINITY) w = 0.f;
+            if (!PLAIN && sc[u][n][e] == -INFINITY) w = -0.f;   // hidden; a small visible weight ends as +0
             sc[u][n][e] = w;
             l[n][e & 1] += w;
           }
@@ -685,7 +685,7 @@ kv4_attn_kernel(const T* __restrict__ Q, const uint8_t* __restrict__ pool,
             for (int e = 0; e < 4; ++e) {
               w[e] = sc[u][n][e] * vs[e >> 1][gi];
               // a hidden token's scale may be anything: its weight is zero whatever that is
-              if (!PLAIN && sc[u][n][e] == 0.f) w[e] = 0.f;
+              if (!PLAIN && __float_as_uint(sc[u][n][e]) == 0x80000000u) w[e] = 0.f;
             }
             uint32_t p0[TERMS], p1[TERMS];
             split_pair<TERMS>(w[0], w[1], p0);

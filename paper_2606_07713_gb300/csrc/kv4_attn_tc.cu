@@ -13,8 +13,9 @@
 //            scores are computed from the codes in fp32 instead (exact_scores: about 0.1 ms a tile, for
 //            keys that a trained model does not have).  Values become bf16, rounded once.  Tokens past the end, and pages that are not there, become zeros
 //            (the rows' limits, and a mark beside the factor, hide them).
-//            A token whose value is not finite gets zeros and a NaN key: the rows that see it
-//            read NaN, the others nothing (0 * NaN would reach them through the second product).
+//            A value group that is not finite gets zeros, and a bit in its block's mask: the rows
+//            that see it are made NaN in that group at the end (0 * NaN would reach all rows through the
+//            second product).
 //   attend   query rows, as fp16 with each row's power of two taken out (members within 2^-31 of the
 //            row's largest fit exactly, smaller ones are rounded to 2^-40 of it), against 128-token tiles: S = Q K^T (fp16), running maximum and sum per row, O += P V
 //            (bf16) in TMEM.  Maximum, exponentials, sum in fp32.  P and V in fp16 (11 bits, V then
@@ -187,8 +188,9 @@ __device__ __forceinline__ int row_exponent(uint32_t top) {
 }
 
 // What a tile's factor carries beside its power of two: a bit for each 16-token block whose page is not
-// there, and whether the tile's scores have to be computed in fp32.
-constexpr uint32_t kGoneBlocks = 0xffu, kMixedKeys = 0x100u;
+// there, whether the tile's scores have to be computed in fp32, and whether a value is not finite (the
+// blocks' masks are only written then).
+constexpr uint32_t kGoneBlocks = 0xffu, kMixedKeys = 0x100u, kBadValues = 0x200u;
 
 // Bound by its stores into L2 and the latency of a warp's one block: 2304 bytes in, 8 KB out.  Words
 // asked for before the scales are looked at, and products in pairs: 5 us less than one after the other
@@ -197,9 +199,9 @@ template <int DK, int DV>
 __global__ void __launch_bounds__(256)
 kv4_widen_kernel(const uint8_t* __restrict__ pool, const int32_t* __restrict__ table,
                  const int32_t* __restrict__ lens, __half* __restrict__ wk, __nv_bfloat16* __restrict__ wv,
-                 float2* __restrict__ factor, Params p) {
+                 float2* __restrict__ factor, uint64_t* __restrict__ bad_values, Params p) {
   constexpr int GK = DK / 32, GV = DV / 32;
-  __shared__ uint32_t s_max[8], s_min[8], s_gone[8];
+  __shared__ uint32_t s_max[8], s_min[8], s_marks[8];
   wait_for_previous();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int tile = int(blockIdx.x), bh = int(blockIdx.y);
@@ -236,54 +238,53 @@ kv4_widen_kernel(const uint8_t* __restrict__ pool, const int32_t* __restrict__ t
                                 : 0x88888888u;
   }
   // the largest and the smallest key scale that is a number and not zero (their bits are in the same
-  // order), and the tokens with a value scale that is not finite
+  // order), and the value groups that are not finite: bit GV token + group
   uint32_t top_bits = 0, low_bits = 0x7f800000u;
-  uint32_t bad = 0;
+  uint64_t bad = 0;
   if (src != nullptr) {
     for (int i = lane; i < kBlock * GK; i += 32) {
       const float s = bf16_value(src + key_scales(DK, DV) + 2 * i);
       if (i / GK < n_tok && s > 0.f && s < INFINITY)
         top_bits = max(top_bits, __float_as_uint(s)), low_bits = min(low_bits, __float_as_uint(s));
     }
-    for (int i = lane; i < kBlock * GV; i += 32) {
-      const float s = bf16_value(src + value_scales(DK, DV) + 2 * i);
-      if (!(s < INFINITY)) bad |= 1u << (i / GV);
+#pragma unroll
+    for (int i = 0; i < kBlock * GV; i += 32) {
+      const float s = bf16_value(src + value_scales(DK, DV) + 2 * (i + lane));
+      bad |= uint64_t(__ballot_sync(0xffffffffu, (i + lane) / GV < n_tok && !(s < INFINITY))) << i;
     }
   }
   top_bits = __reduce_max_sync(0xffffffffu, top_bits);
   low_bits = __reduce_min_sync(0xffffffffu, low_bits);
-  bad = __reduce_or_sync(0xffffffffu, bad);
   if (lane == 0) {
     s_max[warp] = top_bits;
     s_min[warp] = low_bits;
-    s_gone[warp] = src == nullptr && blk * kBlock < len ? 1u << warp : 0u;
+    s_marks[warp] = (src == nullptr && blk * kBlock < len ? 1u << warp : 0u) | (bad != 0 ? kBadValues : 0u);
   }
   __syncthreads();
-  uint32_t gone = 0;   // the tile's blocks whose page is not there
+  uint32_t marks = 0;
 #pragma unroll
   for (int w = 0; w < 8; ++w) {
     top_bits = max(top_bits, s_max[w]);
     low_bits = min(low_bits, s_min[w]);
-    gone |= s_gone[w];
+    marks |= s_marks[w];
   }
   // 2^E with the largest scale times 2^-E in [2^11, 2^12); eight bits of a scale then end above 2^-24, the
   // spacing of the smallest fp16, if it is 2^-17 or more
   const int e = tile_exponent(top_bits, 11);
   const float down = power_of(-e);
   const bool mixed = low_bits < 0x7f800000u && __uint_as_float(low_bits) * down < 0x1p-17f;
+  if (mixed) marks |= kMixedKeys;
+  const int64_t at = int64_t(bh) * p.tiles_pad + tile;
   if (threadIdx.x == 0)
-    factor[int64_t(bh) * p.tiles_pad + tile] = make_float2(
-        power_of(mixed ? tile_exponent(top_bits, kMixedTop) : e), __uint_as_float(mixed ? gone | kMixedKeys : gone));
+    factor[at] = make_float2(power_of(mixed ? tile_exponent(top_bits, kMixedTop) : e), __uint_as_float(marks));
+  if ((marks & kBadValues) && lane == 0) bad_values[at * 8 + warp] = bad;
 
-  const int64_t row0 = (int64_t(bh) * p.tiles_pad + tile) * kBN + warp * kBlock;
+  const int64_t row0 = at * kBN + warp * kBlock;
 #pragma unroll
   for (int it = 0; it < kItsK; ++it) {
     const int i = it * 32 + lane, token = i / kChunks, f8 = i % kChunks, g = f8 >> 2;
     float s = 0.f;
-    if (token < n_tok) {
-      s = bf16_value(src + key_scales(DK, DV) + (token * GK + g) * 2) * down;
-      if (bad >> token & 1u) s = __int_as_float(0x7fc00000);
-    }
+    if (token < n_tok) s = bf16_value(src + key_scales(DK, DV) + (token * GK + g) * 2) * down;
     // codes as 1024 + n, less 1032
     const __half2 s2 = __float2half2_rn(s), bias = __float2half2_rn(1032.f);
     uint32_t o[4];
@@ -301,7 +302,7 @@ kv4_widen_kernel(const uint8_t* __restrict__ pool, const int32_t* __restrict__ t
     uint32_t s = 0;   // the two tokens' scales
 #pragma unroll
     for (int k = 0; k < 2; ++k)
-      if (token + k < n_tok && !(bad >> (token + k) & 1u))
+      if (token + k < n_tok && !(bad >> (GV * (token + k) + g) & 1u))
         s |= uint32_t(*reinterpret_cast<const uint16_t*>(src + value_scales(DK, DV) + ((token + k) * GV + g) * 2)) << (16 * k);
     const __nv_bfloat162 s2 = *reinterpret_cast<const __nv_bfloat162*>(&s), bias = __float2bfloat162_rn(136.f);
     uint32_t y[8];   // a feature of both tokens: codes as 128 + n, less 136; the product is rounded once
@@ -368,7 +369,21 @@ struct Codes {
   int64_t page_bytes, n_pages;
   int blocks_per_page, len;
   float sign;               // of the scale
+  const uint64_t* bad;      // the masks of value groups that are not finite, of the sequence's blocks
 };
+
+// The value groups that are not finite in the first `valid` tokens of a tile, from its blocks' masks.
+template <int GV>
+__device__ uint32_t bad_groups(const uint64_t* bad, int valid) {
+  uint64_t all = 0;
+  for (int k = 0; k < kBN / kBlock; ++k) {
+    const int bits = GV * min(max(valid - k * kBlock, 0), kBlock);
+    all |= bits == 64 ? bad[k] : bad[k] & ((uint64_t(1) << bits) - 1);
+  }
+#pragma unroll
+  for (int d = 32; d >= GV; d >>= 1) all |= all >> d;
+  return uint32_t(all) & ((1u << GV) - 1);
+}
 
 // The scores of a thread's row against a tile whose key scales lie too far apart for fp16, into its TMEM
 // lane (warp-collective), in fp32 from the cache's codes: the row with its power of two taken out, as in
@@ -431,10 +446,11 @@ struct Tiles {
 };
 
 // The softmax of an item's tiles: maximum m and sum l of the thread's row.  `t`: the tiles of the CTA
-// before them.  ODD: some carry marks; false if a wait ran out.
+// before them.  ODD: some carry marks; `bad`: the value groups that make the row NaN.  False if a wait
+// ran out.
 template <int DK, int DV, bool ODD>
 __device__ __forceinline__ bool item_tiles(const Tiles& x, const Codes* codes, uint32_t t, float& m, float& l,
-                                           const WaitCtl& wc) {
+                                           [[maybe_unused]] uint32_t& bad, const WaitCtl& wc) {
   using C = Cfg<DK, DV>;
   float2 f_next = x.fac[x.u0];
   for (int n = x.u0; n < x.u1; ++n, ++t) {
@@ -446,6 +462,7 @@ __device__ __forceinline__ bool item_tiles(const Tiles& x, const Codes* codes, u
     tc_fence_after_sync();
     if constexpr (ODD) {
       if (marks & kMixedKeys) exact_scores<DK, DV>(x.tS, *codes, n, 1.f / up);
+      if (marks & kBadValues) bad |= bad_groups<DV / 32>(codes->bad + n * int64_t(kBN / kBlock), x.lim - n * kBN);
     }
     uint32_t sr[128];
     tmem_load_row128(x.tS, sr);
@@ -516,12 +533,13 @@ __device__ __forceinline__ bool item_tiles(const Tiles& x, const Codes* codes, u
 // exact_scores cost that 3 to 5 %.
 struct Row {
   float m, l;
+  uint32_t bad;
   bool ok;
 };
 template <int DK, int DV>
 __device__ __noinline__ Row odd_item_tiles(const Tiles& x, const Codes& codes, uint32_t t, const WaitCtl& wc) {
-  Row r{-INFINITY, 0.f, true};
-  r.ok = item_tiles<DK, DV, true>(x, &codes, t, r.m, r.l, wc);
+  Row r{-INFINITY, 0.f, 0u, true};
+  r.ok = item_tiles<DK, DV, true>(x, &codes, t, r.m, r.l, r.bad, wc);
   return r;
 }
 
@@ -535,6 +553,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 kv4_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                    const __nv_bfloat16* __restrict__ Q, const uint8_t* __restrict__ pool,
                    const int32_t* __restrict__ table, const float2* __restrict__ factor,
+                   const uint64_t* __restrict__ bad_values,
                    const int32_t* __restrict__ lens, __nv_bfloat16* __restrict__ O, float* __restrict__ lse,
                    float* __restrict__ part_o, float2* __restrict__ part_ml, Cut* __restrict__ cuts, Params p) {
   using C = Cfg<DK, DV>;
@@ -869,19 +888,21 @@ kv4_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
       for (int n = u0 + lane; n < u1; n += 32) odd |= __float_as_uint(fac[n].y) != 0;
       odd = __any_sync(0xffffffffu, odd);
       float m = -INFINITY, l = 0.f;
+      uint32_t bad = 0;    // value groups that make the row NaN
       const Tiles x{tS, tO, tP, s_full(j), s_free(j), p_ready(j), p_free(j), fac, lim, u0, u1, c_row};
       if (odd) {
         const Place w = place(items[seg & 1].item);
         const __nv_bfloat16* q = Q + int64_t(w.b) * p.q_sb + (int64_t(w.h) * p.G + w.rh) * p.q_sh + int64_t(w.ri) * p.q_sn;
         const int64_t head_bytes = int64_t(p.blocks_per_page) * block_bytes(DK, DV);
         const Codes codes{w.live ? q : nullptr, pool + w.h * head_bytes, table + w.b * p.max_pages, p.Hk * head_bytes,
-                          p.n_pages, p.blocks_per_page, length_of(lens, w.b, p, false), p.negate ? -1.f : 1.f};
+                          p.n_pages, p.blocks_per_page, length_of(lens, w.b, p, false), p.negate ? -1.f : 1.f,
+                          bad_values + (fac - factor) * (kBN / kBlock)};
         const Tiles x_there = x;   // copies, so that what is in registers needs no address
         const WaitCtl wc_there = wc;
         const Row r = odd_item_tiles<DK, DV>(x_there, codes, t, wc_there);
-        m = r.m, l = r.l, ok = r.ok;
+        m = r.m, l = r.l, bad = r.bad, ok = r.ok;
       } else {
-        ok = item_tiles<DK, DV, false>(x, nullptr, t, m, l, wc);
+        ok = item_tiles<DK, DV, false>(x, nullptr, t, m, l, bad, wc);
       }
       t += u1 - u0;
       if (!ok || !wait_bounded(o_done(j), seg & 1u, wc)) break;
@@ -898,6 +919,10 @@ kv4_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
           tmem_ld_32x32b_x16(tO + c, o);
           tmem_wait_ld();
           reg_anchor_x16(o);
+          if (bad >> (c / 32) & 1u) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[i] = 0x7fc00000u;
+          }
           float4* dst = reinterpret_cast<float4*>(part_o + at * DV + c);
 #pragma unroll
           for (int i = 0; i < 4; ++i)
@@ -916,6 +941,10 @@ kv4_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
           tmem_ld_32x32b_x16(tO + c, o);
           tmem_wait_ld();
           reg_anchor_x16(o);
+          if (bad >> (c / 32) & 1u) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[i] = 0x7fc00000u;
+          }
           if (w.live) {
             uint32_t y[8];
 #pragma unroll
@@ -989,10 +1018,10 @@ constexpr int64_t kWidenedMost = int64_t(1) << 30;   // bytes of widened heads a
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
-// The workspace: widened keys and values of `heads` heads, the tiles' factors, pieces, cuts.
+// The workspace: widened keys and values of `heads` heads, the tiles' factors and masks, pieces, cuts.
 struct Work {
   int64_t tiles_pad, heads;
-  int64_t k, v, factor, part_o, part_ml, cuts, bytes;   // offsets, and the sum
+  int64_t k, v, factor, bad, part_o, part_ml, cuts, bytes;   // offsets, and the sum
   Work(int64_t bh, int64_t max_len, int64_t dk, int64_t dv, int sms) {
     tiles_pad = (max_len + kBN - 1) / kBN;
     const int64_t head = tiles_pad * kBN * (dk + dv) * 2;
@@ -1002,7 +1031,8 @@ struct Work {
     k = 0;
     v = k + heads * tiles_pad * kBN * dk * 2;
     factor = v + heads * tiles_pad * kBN * dv * 2;
-    part_o = factor + round_up(heads * tiles_pad * 8, 256);
+    bad = factor + round_up(heads * tiles_pad * 8, 256);
+    part_o = bad + heads * tiles_pad * (kBN / kBlock) * 8;
     part_ml = part_o + int64_t(sms) * 2 * kRows * dv * 4;
     cuts = part_ml + int64_t(sms) * 2 * kRows * 8;
     bytes = cuts + round_up(int64_t(sms) * sizeof(Cut), 256);
@@ -1034,6 +1064,7 @@ int launch(const Kv4AttnArgs& a, int sms, char* msg, size_t msglen) {
   __half* wk = reinterpret_cast<__half*>(ws + w.k);
   __nv_bfloat16* wv = reinterpret_cast<__nv_bfloat16*>(ws + w.v);
   float2* factor = reinterpret_cast<float2*>(ws + w.factor);
+  uint64_t* bad = reinterpret_cast<uint64_t*>(ws + w.bad);
   float* part_o = reinterpret_cast<float*>(ws + w.part_o);
   float2* part_ml = reinterpret_cast<float2*>(ws + w.part_ml);
   Cut* cuts = reinterpret_cast<Cut*>(ws + w.cuts);
@@ -1057,11 +1088,11 @@ int launch(const Kv4AttnArgs& a, int sms, char* msg, size_t msglen) {
     const int64_t most = int64_t(p.n_bh) * p.n_tiles * w.tiles_pad;   // tiles of tokens, if all are as long as max_len
     const unsigned ctas = unsigned(most < sms ? most : sms);
     e = launch_overlapped(kv4_widen_kernel<DK, DV>, dim3(unsigned(w.tiles_pad), unsigned(p.n_bh)), dim3(256), 0, a.stream,
-                          static_cast<const uint8_t*>(a.c.pool), a.c.table, a.lens, wk, wv, factor, p);
+                          static_cast<const uint8_t*>(a.c.pool), a.c.table, a.lens, wk, wv, factor, bad, p);
     if (e == cudaSuccess)
       e = launch_overlapped(kern, dim3(ctas), dim3(kThreads), C::kSmemBytes, a.stream, mk, mv,
                             static_cast<const __nv_bfloat16*>(a.q.p), static_cast<const uint8_t*>(a.c.pool), a.c.table,
-                            factor, a.lens, static_cast<__nv_bfloat16*>(a.o.p),
+                            factor, bad, a.lens, static_cast<__nv_bfloat16*>(a.o.p),
                             a.lse, part_o, part_ml, cuts, p);
     if (e == cudaSuccess)
       e = launch_overlapped(kv4_attn_tc_join_kernel<DV>, dim3(ctas, kRows / 8), dim3(256), 0, a.stream, part_o, part_ml,

@@ -87,3 +87,24 @@ def test_single_precision_reads_of_mixed_sizes():
     got = pkg.kv4_read(pool, table, dev(np.arange(T, dtype=np.int32)[None]), d, dtype=torch.float32)
     for x, y in zip(got, stored(k, v)):
         assert np.array_equal(host(x), y)
+@pytest.mark.parametrize("dv", [64, 128])
+@pytest.mark.parametrize("N", ROWS)
+def test_a_value_that_is_no_number_reaches_its_group_only(N, dv):
+    """The rows that see it are NaN in the 32 features of its group, however small its weight; the other
+    features, the other rows and every log-sum-exp keep their bits."""
+    T, d = 4000, 64
+    q, k, v = inputs(N, T, d, dv, seed=dv)
+    token = T - 1 - N // 2
+    q[..., 0] = 1.0
+    k[:, :, token] = 0.0
+    k[:, :, token, 0] = -4096.0               # its weight is e^-512: nothing in 32 bits
+    q, k, v = cast(q, "bf16"), cast(k, "bf16"), cast(v, "bf16")
+    good, good_lse = attend(q, k, v)
+    v[:, :, token, 33] = np.inf
+    o, lse = attend(q, k, v)
+    first = N - 1 - N // 2                    # the first row that sees it
+    assert bool(torch.isnan(o[:, :, first:, 32:64]).all())
+    o[:, :, first:, 32:64] = good[:, :, first:, 32:64]
+    assert torch.equal(o, good) and torch.equal(lse, good_lse)
+
+
