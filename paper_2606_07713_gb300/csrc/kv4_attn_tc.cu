@@ -181,8 +181,7 @@ __device__ __forceinline__ int tile_exponent(uint32_t top, int to) {
 // Of tiles with scales far apart: room for queries below 2^15, codes and 128 products above, and for
 // scales down to 2^-186 of the largest below.
 constexpr int kMixedTop = 60;
-// The power of two that a row's largest magnitude (its bf16 bits) is brought into [2^14, 2^15) by; a row
-// with a member that is not finite stays as it is.
+// The power of two that a row's largest magnitude (its bf16 bits) is brought into [2^14, 2^15) by.
 __device__ __forceinline__ int row_exponent(uint32_t top) {
   return top == 0 || top >= 0x7f80u ? 0 : max(int(top >> 7) - 127 - 14, -126);
 }
@@ -394,7 +393,7 @@ __device__ void exact_scores(uint32_t tS, const Codes& a, int tile, float down) 
   uint32_t top = 0;
   for (int i = 0; a.q != nullptr && i < DK; ++i)
     top = max(top, uint32_t(reinterpret_cast<const uint16_t*>(a.q)[i]) & 0x7fffu);
-  const float row_down = power_of(-row_exponent(top)) * a.sign;
+  const float row_down = top >= 0x7f80u ? __int_as_float(0x7fc00000) : power_of(-row_exponent(top)) * a.sign;
 #pragma unroll 1
   for (int k = 0; k < kBN / kBlock; ++k) {
     const int blk = tile * (kBN / kBlock) + k, slot = int(unsigned(blk) / unsigned(a.blocks_per_page));
@@ -868,6 +867,8 @@ kv4_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
             top = max(top, (q[k] >> 16) & 0x7fffu);
           }
         }
+        // a row with a member that is not finite gets a NaN: scores of -infinity would hide its tokens
+        if (top >= 0x7f80u) x[0].x = 0x7fc07fc0u;
         const int e = row_exponent(top);
         const float down = power_of(-e) * (p.negate ? -1.f : 1.f);
         c_row *= power_of(e);

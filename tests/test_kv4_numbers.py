@@ -108,3 +108,19 @@ def test_a_value_that_is_no_number_reaches_its_group_only(N, dv):
     assert torch.equal(o, good) and torch.equal(lse, good_lse)
 
 
+@pytest.mark.parametrize("N", ROWS)
+def test_an_infinite_query_gives_nan(N):
+    """Scores of minus infinity for every visible token have no softmax: NaN, not an empty row."""
+    T, d = 4000, 64
+    q, k, v = inputs(N, T, d, d, seed=3)
+    k[..., 5] = -1.0 - np.abs(k[..., 5])
+    q, k, v = cast(q, "bf16"), cast(k, "bf16"), cast(v, "bf16")
+    good, good_lse = attend(q, k, v)
+    q[0, 2, N - 1] = 0.0
+    q[0, 2, N - 1, 5] = np.inf
+    o, lse = attend(q, k, v)
+    assert bool(torch.isnan(o[0, 2, N - 1]).all()) and bool(torch.isnan(lse[0, 2, N - 1]))
+    o[0, 2, N - 1], lse[0, 2, N - 1] = good[0, 2, N - 1], good_lse[0, 2, N - 1]
+    assert torch.equal(o, good) and torch.equal(lse, good_lse)
+
+
