@@ -240,6 +240,7 @@ kv4_widen_kernel(const uint8_t* __restrict__ pool, const int32_t* __restrict__ t
   // order), and the value groups that are not finite: bit GV token + group
   uint32_t top_bits = 0, low_bits = 0x7f800000u;
   uint64_t bad = 0;
+  bool huge = false;   // a value may round to infinity: seven times the largest scale there is, 1.140625 * 2^125
   if (src != nullptr) {
     for (int i = lane; i < kBlock * GK; i += 32) {
       const float s = bf16_value(src + key_scales(DK, DV) + 2 * i);
@@ -250,8 +251,10 @@ kv4_widen_kernel(const uint8_t* __restrict__ pool, const int32_t* __restrict__ t
     for (int i = 0; i < kBlock * GV; i += 32) {
       const float s = bf16_value(src + value_scales(DK, DV) + 2 * (i + lane));
       bad |= uint64_t(__ballot_sync(0xffffffffu, (i + lane) / GV < n_tok && !(s < INFINITY))) << i;
+      huge |= s >= 0x1.24p125f;
     }
   }
+  huge = __any_sync(0xffffffffu, huge);
   top_bits = __reduce_max_sync(0xffffffffu, top_bits);
   low_bits = __reduce_min_sync(0xffffffffu, low_bits);
   if (lane == 0) {
@@ -308,7 +311,11 @@ kv4_widen_kernel(const uint8_t* __restrict__ pool, const int32_t* __restrict__ t
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const uint32_t x = (vw[it][j >> 2] >> (4 * (j & 3)) & 0x000f000fu) | 0x43004300u;
-      const __nv_bfloat162 z = __hmul2(__hsub2(*reinterpret_cast<const __nv_bfloat162*>(&x), bias), s2);
+      __nv_bfloat162 z = __hmul2(__hsub2(*reinterpret_cast<const __nv_bfloat162*>(&x), bias), s2);
+      if (huge) {   // the largest number instead, half a unit away: infinity times a hidden token's zero is NaN
+        const __nv_bfloat162 most = __halves2bfloat162(__ushort_as_bfloat16(0x7f7f), __ushort_as_bfloat16(0x7f7f));
+        z = __hmax2(__hmin2(z, most), __hneg2(most));
+      }
       y[j] = *reinterpret_cast<const uint32_t*>(&z);
     }
 #pragma unroll

@@ -124,3 +124,16 @@ def test_an_infinite_query_gives_nan(N):
     assert torch.equal(o, good) and torch.equal(lse, good_lse)
 
 
+@pytest.mark.parametrize("N", [40, 512])
+def test_the_largest_values_are_no_concern_of_rows_before_them(N):
+    T, d = 4000, 64
+    q, k, v = inputs(N, T, d, d, seed=4)
+    q, k, v = cast(q, "bf16"), cast(k, "bf16"), cast(v, "bf16")
+    good, _ = attend(q, k, v)
+    token = T - 1 - N // 2
+    v[:, :, token] = 3.3895313892515355e38    # the largest bf16
+    o, _ = attend(q, k, v)
+    first = N - 1 - N // 2
+    assert torch.equal(o[:, :, :first], good[:, :, :first])
+
+
