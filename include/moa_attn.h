@@ -369,7 +369,9 @@ int moa_attn_fwd_splitkv_noalloc(const void* Q, const void* K, const void* V, vo
  *   strides    12 values: Q, K, Qo, Ko
  *   eps        > 0 and finite;   dtype  MOA_BF16 or MOA_FP32
  * d a multiple of 8 up to 256; d_rot a multiple of 16, 16 <= d_rot <= d.  Qo may be Q and Ko may
- * be K with the same strides (in place); no other overlap.  Q and K may be slices of one buffer.
+ * be K with the same strides (in place); no other overlap.  Q and K, and Qo and Ko, may be slices of one
+ * buffer, its dimensions in any order: equal strides along B and N, heads one tensor's after the other's
+ * or in turn.
  * Computed in fp32, rounded once.  Position >= n_pos: the row is NaN, MOA_ERR_DEVICE_INDEX.
  */
 int moa_qk_norm_rope(const void* Q, const void* K, const void* W_q, const void* W_k,

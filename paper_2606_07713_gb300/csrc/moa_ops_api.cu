@@ -5,6 +5,7 @@
 #include <cmath>
 #include <cstdint>
 #include <exception>
+#include <utility>
 
 #include "../../include/moa_attn.h"
 #include "internal.h"
@@ -91,20 +92,46 @@ bool same_view(const View& a, const View& b) {
   return a.p == b.p && a.sb == b.sb && a.sh == b.sh && a.sn == b.sn;
 }
 
-// Whether two tensors of the same B and N whose spans meet are disjoint slices of one buffer's token
-// rows: equal strides along B and N, and their heads beside each other within one token's stride.
-bool token_slices(const View& a, const Shape& sa, const View& b, const Shape& sb, int64_t elt) {
+// Whether two tensors of the same B, N and d whose spans meet are slices of one buffer that share no
+// element: equal strides along B and N, and heads that lie apart.  The buffer's dimensions may be in any
+// order: with k of B and N (those of the smaller strides) inside a head, a head is a piece of `inner`
+// elements; the two tensors' pieces must lie apart, one tensor's after the other's or in turn, and all of
+// them within the strides of the dimensions outside.
+bool disjoint_slices(const View& a, const Shape& sa, const View& b, const Shape& sb, int64_t elt) {
   if ((sa.B > 1 && a.sb != b.sb) || (sa.N > 1 && a.sn != b.sn)) return false;
   if (a.sh < 0 || b.sh < 0 || a.sn < 0 || a.sb < 0) return false;
-  const uintptr_t pa = reinterpret_cast<uintptr_t>(a.p), pb = reinterpret_cast<uintptr_t>(b.p);
-  const int64_t ea = ((sa.H - 1) * a.sh + sa.d) * elt, eb = ((sb.H - 1) * b.sh + sb.d) * elt;
-  const uintptr_t end_a = pa + uintptr_t(ea), end_b = pb + uintptr_t(eb);
-  if (!(end_a <= pb || end_b <= pa)) return false;  // one token's heads overlap
-  const int64_t whole = int64_t((end_a > end_b ? end_a : end_b) - (pa < pb ? pa : pb));
-  // a token's heads end before the next token's begin, and a sequence's tokens before the next's
-  if (sa.N > 1 && whole > a.sn * elt) return false;
-  if (sa.B > 1 && whole + (sa.N > 1 ? (sa.N - 1) * a.sn * elt : 0) > a.sb * elt) return false;
-  return true;
+  const intptr_t bytes = reinterpret_cast<intptr_t>(b.p) - reinterpret_cast<intptr_t>(a.p);
+  if (bytes % elt != 0) return false;
+  const int64_t off = bytes / elt;   // of b's first element from a's
+  int64_t size[2] = {sa.N, sa.B}, stride[2] = {sa.N > 1 ? a.sn : 0, sa.B > 1 ? a.sb : 0};
+  if (stride[0] > stride[1]) {
+    std::swap(stride[0], stride[1]);
+    std::swap(size[0], size[1]);
+  }
+  int64_t inner = sa.d;
+  for (int k = 0; k <= 2; ++k) {
+    if (k > 0) {
+      if (size[k - 1] > 1 && stride[k - 1] < inner) return false;   // rows on one another
+      inner += (size[k - 1] - 1) * stride[k - 1];
+    }
+    if ((sa.H > 1 && a.sh < inner) || (sb.H > 1 && b.sh < inner)) continue;
+    const int64_t end_a = (sa.H - 1) * a.sh + inner, end_b = off + (sb.H - 1) * b.sh + inner;
+    bool apart = end_a <= off || end_b <= 0;
+    if (!apart && sa.H > 1 && sb.H > 1 && a.sh == b.sh) {
+      const int64_t turn = (off % a.sh + a.sh) % a.sh;   // where b's pieces lie between a's
+      apart = turn >= inner && turn + inner <= a.sh;
+    }
+    if (!apart) continue;
+    int64_t whole = (end_a > end_b ? end_a : end_b) - (off < 0 ? off : 0);
+    bool nested = true;
+    for (int i = k; i < 2; ++i) {
+      if (size[i] == 1) continue;
+      nested = nested && stride[i] >= whole;
+      whole += (size[i] - 1) * stride[i];
+    }
+    if (nested) return true;
+  }
+  return false;
 }
 
 int check_dtype(int dtype) {
@@ -189,7 +216,7 @@ int norm_call(NormRopeArgs& a, int64_t d, int64_t d_rot, int dtype, bool bwd, si
     for (int j = 0; j < n_t; ++j) {
       if (j == i || (t[j].output && j < i) || !overlap(span[i], span[j])) continue;
       if (j == t[i].alias && same_view(*t[i].v, *t[j].v)) continue;
-      if (token_slices(*t[i].v, shape[i], *t[j].v, shape[j], elt)) continue;
+      if (disjoint_slices(*t[i].v, shape[i], *t[j].v, shape[j], elt)) continue;
       return api_fail(MOA_ERR_INVALID_ARG, "%s overlaps %s", t[i].name, t[j].name);
     }
     for (int j = 0; j < n_flat; ++j)
@@ -281,7 +308,7 @@ int move_call(const void* K, const void* V, const void* pool, const int32_t* pag
   if (overlap(pool_s, ks) || overlap(pool_s, vs) || overlap(pool_s, pages_s) || overlap(pool_s, pos_s))
     return api_fail(MOA_ERR_INVALID_ARG, "the pool overlaps a tensor");
   if (!write) {
-    if (overlap(ks, vs) && !token_slices(a.k, sk, a.v, sv, elt))
+    if (overlap(ks, vs) && !disjoint_slices(a.k, sk, a.v, sv, elt))
       return api_fail(MOA_ERR_INVALID_ARG, "K overlaps V");
     for (const Span& s : {ks, vs})
       if (overlap(s, pages_s) || overlap(s, pos_s))
