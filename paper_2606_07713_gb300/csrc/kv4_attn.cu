@@ -274,8 +274,8 @@ struct Shares {
 
 template <typename T, int DK, int DV, int NT, int TERMS>
 __global__ void __launch_bounds__(kThreads, Cfg<DK, DV, NT, TERMS>::kCtas)
-kv4_attn_kernel(const T* __restrict__ Q, const uint8_t* __restrict__ pool,
-                const int32_t* __restrict__ table, const int32_t* __restrict__ lens,
+kv4_attn_kernel(const T* Q, const uint8_t* pool,
+                const int32_t* table, const int32_t* lens,
                 T* __restrict__ O, float* __restrict__ lse, float* __restrict__ part_o,
                 float* __restrict__ part_ml, Cut* __restrict__ cuts, Params p) {
   using C = Cfg<DK, DV, NT, TERMS>;
@@ -816,8 +816,8 @@ kv4_attn_kernel(const T* __restrict__ Q, const uint8_t* __restrict__ pool,
 // items of many pieces, two where most have a few (then the CTAs are many and short).
 template <typename T, int DV, int ROWS, int kJoinWarps>
 __global__ void __launch_bounds__(32 * kJoinWarps)
-kv4_attn_join_kernel(const float* __restrict__ part_o, const float* __restrict__ part_ml,
-                     const Cut* __restrict__ cuts, T* __restrict__ O, float* __restrict__ lse, Params p) {
+kv4_attn_join_kernel(const float* part_o, const float* part_ml,
+                     const Cut* cuts, T* __restrict__ O, float* __restrict__ lse, Params p) {
   constexpr int kAhead = kJoinWarps == 8 ? 8 : 2;
   __shared__ float so[kJoinWarps][DV], sl[kJoinWarps];
   wait_for_previous();
