@@ -191,8 +191,11 @@ struct Row {
     } else {
       b = u / p.units;
       live = u < p.all;
-      const int32_t first = live ? pos[b * p.N] : 0;
-      n = int64_t(u - uint32_t(b) * p.units) * kBlock - (first & (kBlock - 1)) + i;
+      // where in its block the first row would lie, going by the last row if that has a position (padding
+      // comes first where the rows are a chunk's queries), else by the first
+      const int32_t first = live ? pos[b * p.N] : 0, last = live ? pos[b * p.N + p.N - 1] : 0;
+      const uint32_t from = last >= 0 ? uint32_t(last) - uint32_t(p.N - 1) : uint32_t(first);
+      n = int64_t(u - uint32_t(b) * p.units) * kBlock - int(from & (kBlock - 1)) + i;
       live = live && n >= 0 && n < p.N;
     }
     at = live ? pos[b * p.N + n] : -1;
