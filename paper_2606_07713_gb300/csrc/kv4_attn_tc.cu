@@ -10,9 +10,10 @@
 //            significant bits, so with the tile's power of two 2^E taken out (E from its largest
 //            scale) the products are exact while the scales are within 2^28 of each other; 2^E goes
 //            into the tile's softmax factor.  A tile with scales further apart is marked, and its
-//            scores are computed from the codes in fp32 instead (exact_scores: about 0.1 ms a tile, for
-//            keys that a trained model does not have).  Values become bf16, rounded once.  Tokens past the end, and pages that are not there, become zeros
-//            (the rows' limits, and a mark beside the factor, hide them).
+//            scores are computed from the codes in fp32 instead (exact_scores: 0.3 ms a tile, for keys that
+//            a trained model does not have).  Values become bf16, rounded once.  Tokens past the end, and
+//            pages that are not there, become zeros (the rows' limits, and a mark beside the factor, hide
+//            them).
 //            A value group that is not finite gets zeros, and a bit in its block's mask: the rows
 //            that see it are made NaN in that group at the end (0 * NaN would reach all rows through the
 //            second product).
@@ -818,7 +819,9 @@ kv4_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
           before = end;
           ++item;
         }
-        if (seg >= 2 && !wait_bounded(item_empty(seg & 1), ((seg >> 1) - 1) & 1u, wc)) break;
+        // the wait lasts as long as the item before this one takes: up to 0.3 ms a tile (exact_scores)
+        const WaitCtl wi{abort_flag, p.wait_limit_ns + uint64_t(p.tiles_pad) * 1000000u, 0u, &g_moa_kv4_tc_status};
+        if (seg >= 2 && !wait_bounded(item_empty(seg & 1), ((seg >> 1) - 1) & 1u, wi)) break;
         volatile Item& x = items[seg & 1];
         x.item = which, x.u0 = u0, x.u1 = u1, x.units = units;
         mbar_arrive(item_full(seg & 1));
@@ -969,8 +972,9 @@ kv4_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     }
   }
 
-  // Teardown: the tensor core is quiet before TMEM is freed, on the abort path too.
-  if (warp == kMmaWarp0) wait_quiesce(drain, 0, p.wait_limit_ns, &g_moa_kv4_tc_status);
+  // Teardown: the tensor core is quiet before TMEM is freed, on the abort path too.  Only the lane of the role
+  // waits: the others come here at the start, and their time would run out in a kernel longer than the limit.
+  if (warp == kMmaWarp0 && lane == 0) wait_quiesce(drain, 0, p.wait_limit_ns, &g_moa_kv4_tc_status);
   tc_fence_before_sync();
   __syncthreads();
   if (warp == kMmaWarp0) {

@@ -3,6 +3,10 @@ queries and drafts as well as chunks that are attended to on the tensor cores, w
 
 The bounds are those of test_kv4.py; what a row does not see leaves no trace in it.
 """
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 
@@ -137,3 +141,53 @@ def test_the_largest_values_are_no_concern_of_rows_before_them(N):
     assert torch.equal(o[:, :, :first], good[:, :, :first])
 
 
+
+
+def test_slow_items_do_not_run_out_of_time():
+    """Chunks all of whose tiles take the slow path keep within the kernel's time limits, which are per wait:
+    here 5 ms each, read once a process, while an item takes about 40 ms."""
+    code = (
+        "import torch, paper_2606_07713_gb300 as p\n"
+        "L, H, d, N, page = 16384, 8, 128, 2048, 64\n"
+        "pool = p.kv4_pool(L // page, H, page, d, d)\n"
+        "pages = torch.arange(L // page, dtype=torch.int32, device='cuda')[None]\n"
+        "k = torch.randn(1, H, L, d, device='cuda')\n"
+        "k[:, :, ::100, 32:64] *= 2.0 ** 30\n"
+        "v = torch.randn(1, H, L, d, device='cuda').bfloat16()\n"
+        "p.kv4_write(k.bfloat16(), v, pool, pages, torch.arange(L, dtype=torch.int32, device='cuda')[None])\n"
+        "q = torch.randn(1, 4 * H, N, d, device='cuda').bfloat16()\n"
+        "p.kv4_attn(q, pool, pages, torch.tensor([L], dtype=torch.int32, device='cuda'))\n"
+        "print('status', p.get_device_status())\n")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300,
+                       env=dict(os.environ, MOA_WAIT_LIMIT_NS="5000000", PYTHONPATH=root))
+    assert r.returncode == 0 and "status 0" in r.stdout, r.stdout + r.stderr
+
+
+@pytest.mark.parametrize("N", [1, 4, 40])
+def test_single_precision_queries(N):
+    """The fp32 form: a value that is no number and hardly weighs, and an infinite query."""
+    T, d = 1003, 64
+    q, k, v = inputs(N, T, d, d, seed=21)
+    token = T - 1 - N // 2
+    q[..., 0], k[:, :, token], k[:, :, token, 0] = 1.0, 0.0, -4096.0
+    q, k, v = (cast(x, "fp32") for x in (q, k, v))
+
+    def run(q, v):
+        o, lse = pkg.kv4_attn_lse(dev(q, "fp32"), *filled(k, v), dev(np.array([T], dtype=np.int32)), max_len=T)
+        assert pkg.get_device_status() == _lib.MOA_OK
+        return o, lse
+
+    good, good_lse = run(q, v)
+    w, x = v.copy(), q.copy()
+    w[:, :, token, 33] = np.nan
+    o, lse = run(q, w)
+    first = N - 1 - N // 2
+    assert bool(torch.isnan(o[:, :, first:, 32:64]).all())
+    o[:, :, first:, 32:64] = good[:, :, first:, 32:64]
+    assert torch.equal(o, good) and torch.equal(lse, good_lse)
+    x[0, 1, 0, 7] = -np.inf
+    o, lse = run(x, v)
+    assert bool(torch.isnan(o[0, 1, 0]).all()) and bool(torch.isnan(lse[0, 1, 0]))
+    o[0, 1, 0], lse[0, 1, 0] = good[0, 1, 0], good_lse[0, 1, 0]
+    assert torch.equal(o, good) and torch.equal(lse, good_lse)
