@@ -372,7 +372,8 @@ int moa_attn_fwd_splitkv_noalloc(const void* Q, const void* K, const void* V, vo
  * be K with the same strides (in place); no other overlap.  Q and K, and Qo and Ko, may be slices of one
  * buffer, its dimensions in any order: equal strides along B and N, heads one tensor's after the other's
  * or in turn.
- * Computed in fp32, rounded once.  Position >= n_pos: the row is NaN, MOA_ERR_DEVICE_INDEX.
+ * Computed in fp32, rounded once; a row's sum of squares has to be below 2^128 (members below about
+ * 2^60).  Position >= n_pos: the row is NaN, MOA_ERR_DEVICE_INDEX.
  */
 int moa_qk_norm_rope(const void* Q, const void* K, const void* W_q, const void* W_k,
                      const float* cos, const float* sin, const int32_t* pos, void* Qo, void* Ko,

@@ -15,11 +15,13 @@
 // (24 bits), so the fp32 form is fp32-accurate on the same instructions.  Scores, maxima, sums
 // and outputs accumulate in fp32.
 //
-// What bounds it: for single tokens the cache's bytes, 9/16 a value, and before them the instructions
-// that widen codes: their ALU operations fill half of that pipe and, with the products and scales, 57 % of
-// the issue slots at the three warps a scheduler that the registers allow.  Measured, single bf16 tokens,
-// d = 128: 2 x 131072 cached tokens of 8 key heads under 64 query heads 45.4 us = 4.4 TB/s of the cache;
-// 48 uneven sequences up to 16384 under 32 query heads 71.5 us = 4.8 TB/s (measured copy bandwidth: 6.8).
+// What bounds it: for single tokens chains of dependent instructions at the three warps a scheduler that
+// the registers allow (fixed latency is the largest stall).  No unit is full: memory 56 to 60 %, the ALU
+// pipe, which widens codes, half, issue 57 %.  The floor is the cache's bytes, 9/16 a value.  Measured,
+// single bf16 tokens, d = 128: 131072 + 42256 cached tokens of 8 key heads under 64 query heads 45.4 us =
+// 4.4 TB/s of the cache; 48 uneven sequences up to 16384 under 32 query heads 71.5 us = 4.8 TB/s (measured
+// copy bandwidth: 6.8).  From 17 to some 1000 query rows of a key head it is far from a floor: see
+// widening_pays below.
 // Tokens lie on the 16 rows of mma.m16n8k16 and queries on its 8 columns: a decoding step has few
 // queries, and the other way round half of the tensor work would be padding.  (A byte form, codes as
 // fp8 and queries as two fp8 terms, took fewer instructions and a fifth more time.)
@@ -157,7 +159,7 @@ constexpr int kUnitBlocks = kUnit / kBlock;
 // An item costs about as much as this many units besides its tokens (places, queries, the join of
 // the warps): it counts for that many more, which come first and hold no tokens.  Without them a
 // share of short items takes several times as long as one of long items (48 sequences of 0 to 16384
-// tokens: 87 us with 0, 72 with 6, 74 with 12; two of 131072: 47.6, 45.5, 45.1).
+// tokens: 87 us with 0, 72 with 6, 74 with 12; 131072 + 42256: 47.6, 45.5, 45.1).
 constexpr int kItemUnits = 6;
 constexpr float kSlack = 8.f;          // the running maximum may lag by this (log2): weights up to 2^8
 
@@ -203,7 +205,8 @@ struct Cfg {
   static constexpr int kOffBar = kOffTop + (kQSmem ? NT * 8 * 4 : 0);
   static constexpr int kOffMisc = kOffBar + kWarps * kStages * 8;
   static constexpr int kSmem = kOffMisc + 64;
-  // resident CTAs: registers (168 or 255 a thread) and 228 KB of shared memory
+  // resident CTAs: registers (168 or 255 a thread; 32-row tiles spill all the same, at d = 128 132 bytes
+  // with bf16 queries and 104 with fp32 ones) and 228 KB of shared memory
   static constexpr int kCtas = NT * TERMS == 1 ? 3 : 2;
   static_assert(kBytes % 16 == 0, "bulk copies are whole 16-byte units");
   static_assert(8 + 8 * kWarps <= 64, "the warps' sums fit behind the abort flag");
@@ -942,7 +945,10 @@ cudaError_t run_d(const Kv4AttnArgs& a, const Kv4Plan& plan, const Params& p) {
 // every 32 rows: 8 us + 0.08 ns for each cached token of a head and 32 rows.  The other one widens
 // once for all, in a launch of its own: 20 us + 0.13 ns for each, + 0.076 ns for each 256 rows.
 // Measured, 8 key heads (this file's, the other's, us): 64 rows x 8192 tokens 22, 36; 128 x 8192 34,
-// 35; 128 x 65536 165, 127; 256 x 8192 51, 38; 512 x 600 22, 25; 2048 x 600 42, 32.
+// 35; 128 x 65536 165, 127; 256 x 8192 51, 38; 512 x 600 22, 25; 2048 x 600 42, 32 (all causal, d = 128:
+// the heads' sizes and the mask do not enter the rule).  Either way this range is 7 to 15 times above its
+// floors, in the same order 1.4, 2.3, 18, 4.5 and 0.7 us: codes are widened too often here, and there it
+// takes three launches, 16-bit copies of all keys and values, and items of 256 rows.
 bool widening_pays(int64_t heads, int64_t rows, int64_t max_len) {
   const double tokens = double(heads) * double(max_len);
   const double n32 = double((rows + 31) / 32), n256 = double((rows + 255) / 256);

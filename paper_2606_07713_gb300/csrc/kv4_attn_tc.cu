@@ -29,9 +29,10 @@
 //
 // What bounds it: the second and first products' tensor time and, beside it, a softmax warp's chain of
 // score load, maximum, 128 exponentials and stores.  Measured, 2048 causal queries of 32 heads against
-// 16384 tokens of 8 key heads, d = 128: 354 us in all = 1.45 PFLOP/s (measured matrix-product rate: 1.89),
-// of them about 325 us the attention, tensor pipe 67 % active, issue 42 %; the widening 15 to 21 us, the
-// join the rest.
+// 16384 tokens of 8 key heads, d = 128: 346 us in all in replayed graphs = 1.49 PFLOP/s (measured
+// matrix-product rate: 1.89), of them about 315 us the attention, tensor pipe 70 % active, issue 44 %; the
+// widening 15 to 20 us, the join the rest.  The attention's time moves by 3 % with the compiler's schedule
+// of its softmax loop, whatever else changes: 346 to 362 us in all have been seen of the same loop.
 //
 // Work items (key head, block of 256 rows) count in units of 128-token tiles; the units of all items
 // are cut into equal shares, one for each SM (one CTA fills an SM): with 256 items on 152 SMs whole
@@ -82,7 +83,8 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 template <int DK, int DV>
 struct Cfg {
-  // 256 kRegsSoftmax + 128 kRegsCtrl is what the launch allocates (the host checks it)
+  // 256 kRegsSoftmax + 128 kRegsCtrl is what the launch allocates (the host checks it).  At 168 registers
+  // the compiler spills 8 to 20 bytes, which it reloads in many places
   static constexpr int kRegsLaunch = 168, kRegsSoftmax = 208, kRegsCtrl = 88;
   static_assert(256 * kRegsSoftmax + 128 * kRegsCtrl <= kThreads * kRegsLaunch, "register split");
   static constexpr int kPanelBytes = 128 * 128;   // 64 columns of 128 rows, 128-byte swizzle
@@ -100,7 +102,7 @@ struct Cfg {
   static constexpr int kOffItems = (kOffMisc + 8 + 15) / 16 * 16;    // two items, then scan[12] and found[2]
   static constexpr int kSmemBytes = kOffItems + 2 * 16 + 14 * 8 + 1024;
   // exponentials, in chunks of 32 tokens, before the wait for the buffer of P: 2, 3, 4 of 4 at d_v = 128 363, 356,
-  // 354 us (the chunk above); at 64 one to three are the same
+  // 354 us (the chunk above); at 64 one to four 283, 279, 278, 278 us
   static constexpr int kEarlyChunks = DV == 64 ? 2 : 4;
   static constexpr uint32_t kTmemCols = 512;
   static constexpr uint32_t kTmemS0 = 0, kTmemS1 = kSharedS ? 0 : 128;

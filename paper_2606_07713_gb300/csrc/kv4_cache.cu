@@ -244,8 +244,8 @@ __device__ __forceinline__ void put(uint8_t* to, const Places& at, const Raw<T>&
 }
 
 // Two heads of bf16 at a time share a barrier.  Measured on bf16 keys and values, 3 x 8 x 16001 x (128 +
-// 128): 52.3 us = 4.8 TB/s; with three CTAs on an SM 58, with
-// five (spills) 60; one head at a time 55.1.  The instructions of the codes fill about 70 % of the issue
+// 128): 52.3 us = 4.8 TB/s with four CTAs on an SM (64 registers, 20
+// bytes spilled); with three 58, with five 60; one head at a time 55.1.  The instructions of the codes fill about 70 % of the issue
 // slots, the rest waits for rows and barriers.
 template <typename T, int LPR>
 __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3)

@@ -7,8 +7,11 @@ several of these calls, so they are kept to a few microseconds).  Tensors are [B
 tensors with unit stride along d and any other strides (a transposed view of a token-major
 [B, N, H, d] tensor needs no copy).  Calls run asynchronously on `stream` (default: torch's current
 stream of the device); outputs and workspaces that they make are memory of that stream, as if it were
-the current one.  What lives on the device (positions, lengths, page numbers) is checked
-there: check(get_device_status()) raises if one was outside its table.
+the current one; inputs have to live until their call has run there.  Nothing is recorded for
+automatic differentiation: results of tensors that require gradients carry none, as with the rest of
+the package, and writing into `out` does not count as a change of it.  What lives on the device
+(positions, lengths, page numbers) is checked there: check(get_device_status()) raises if one was
+outside its table.
 """
 from __future__ import annotations
 
