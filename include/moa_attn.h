@@ -479,6 +479,120 @@ int moa_kv4_attn(const void* Q, const void* pool, const int32_t* pages, const in
 size_t moa_kv4_attn_workspace_bytes(int64_t B, int64_t H_q, int64_t H_k, int64_t N, int64_t d_k,
                                     int64_t d_v, int64_t max_len, int dtype);
 
+/* ------------------------------------------------------------------------------------------
+ * Attention with a sliding window, its gradients, and a 16- or 32-bit paged cache.
+ *
+ * Which tokens a query sees, in all of them: of a sequence's L tokens the N queries are the last N,
+ * query i standing at position p = L - N + i.  It sees token j if j <= p (causal), and
+ * j > p - window or j < sinks.  window = 0: no window (sinks then mean nothing); a window of 1 is
+ * the token itself.  A query that sees nothing (p < 0) gives O = 0 and LSE = -infinity.  Query head h
+ * reads key head h / (H_q / H_k); H_q is a multiple of H_k.  d_k, d_v in {64, 128}.  The common rules
+ * above hold.
+ * ------------------------------------------------------------------------------------------ */
+
+/*
+ * moa_window_attn -- O = softmax(scale Q K^T) V over the tokens that each query sees, L = N_k.
+ *   Q [B, H_q, N_q, d_k], K [B, H_k, N_k, d_k], V [B, H_k, N_k, d_v] inputs, O [B, H_q, N_q, d_v] output;
+ *   strides 12 values: Q, K, V, O
+ *   LSE       float32 [B, H_q, N_q] contiguous, or null: ln of the sum of exp of the row's scaled scores
+ *   scale     any finite value;  dtype MOA_BF16 or MOA_FP32
+ *   workspace device, 16-byte aligned, moa_window_attn_workspace_bytes(...) bytes
+ * A batch padded at the end needs no lengths: later tokens are hidden from earlier ones.  What a token
+ * that a query does not see holds, not numbers included, has no influence on that query.
+ * B H_q N_q and B H_k N_k below 2^31.  fp32 accumulation, maxima and sums; bf16: weights are rounded to
+ * bf16 once.  Bounded waits as moa_attn_fwd.  Bitwise reproducible.
+ */
+int moa_window_attn(const void* Q, const void* K, const void* V, void* O, float* LSE, int64_t B,
+                    int64_t H_q, int64_t H_k, int64_t N_q, int64_t N_k, int64_t d_k, int64_t d_v,
+                    int64_t window, int64_t sinks, const int64_t* strides, float scale, int dtype,
+                    void* workspace, size_t workspace_bytes, void* stream);
+
+/* Scratch bytes of moa_window_attn on the current device (0 for invalid sizes or without a device, and
+ * where none is needed). */
+size_t moa_window_attn_workspace_bytes(int64_t B, int64_t H_q, int64_t H_k, int64_t N_q, int64_t N_k,
+                                       int64_t d_k, int64_t d_v, int64_t window, int64_t sinks,
+                                       int dtype);
+
+/*
+ * moa_window_attn_bwd -- the gradients of moa_window_attn for the gradient dO of its output, from its O
+ * and LSE.
+ *   dQ, dK, dV  outputs, of the shapes and the element type of Q, K, V (a key head's gradients are the
+ *               sums over its query heads)
+ *   strides     24 values: Q, K, V, O, dO, dQ, dK, dV
+ *   LSE         float32 [B, H_q, N_q] contiguous, as moa_window_attn wrote it
+ *   workspace   device, 16-byte aligned, moa_window_attn_bwd_workspace_bytes(...) bytes
+ * Tokens that no query sees get zeros, and so do queries that see nothing.  Inputs are finite: one that
+ * is not can make the gradients of its neighbours (128 rows, 128 tokens) NaN that it does not reach by the
+ * formula.  Accumulation in fp32; bf16: weights and dS are rounded to bf16 once.  dQ, dK and dV may be
+ * slices of one buffer.  Bitwise reproducible.
+ */
+int moa_window_attn_bwd(const void* Q, const void* K, const void* V, const void* O, const void* dO,
+                        const float* LSE, void* dQ, void* dK, void* dV, int64_t B, int64_t H_q,
+                        int64_t H_k, int64_t N_q, int64_t N_k, int64_t d_k, int64_t d_v,
+                        int64_t window, int64_t sinks, const int64_t* strides, float scale, int dtype,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* Scratch bytes of moa_window_attn_bwd (0 for invalid sizes). */
+size_t moa_window_attn_bwd_workspace_bytes(int64_t B, int64_t H_q, int64_t H_k, int64_t N_q,
+                                           int64_t N_k, int64_t d_k, int64_t d_v, int64_t window,
+                                           int64_t sinks, int dtype);
+
+/*
+ * The 16- or 32-bit cache.  A pool is [n_pages, H, page_tokens, d_k + d_v] of bf16 or fp32, contiguous and
+ * 16-byte aligned: a token's key, then its value.  page_tokens is a multiple of 16.  Sequence b's token at
+ * position p lies in page pages[b, p / page_tokens], at place p % page_tokens.  Its contents need no
+ * initial value.
+ *
+ * moa_kv_pool_bytes -- size of a pool (0 for unsupported sizes).
+ */
+size_t moa_kv_pool_bytes(int64_t n_pages, int64_t H, int64_t page_tokens, int64_t d_k, int64_t d_v,
+                         int dtype);
+
+/*
+ * moa_kv_append -- writes rows of keys and values into the pool, keys rotated by their positions' angles
+ * on the way, and rotates the queries beside them.
+ *   K [B, H_k, N, d_k], V [B, H_k, N, d_v]  inputs, the pool's element type
+ *   Q, Qo     [B, H_q, N, d_k] input and output, or both null.  Qo may be Q with the same strides (in place)
+ *   cos, sin  float32 [n_pos, d_rot / 2], contiguous, 16-byte aligned, or both null (nothing is rotated; Q
+ *             must be null then).  Pairs and formula of moa_qk_norm_rope; d_rot a multiple of 16 up to d_k
+ *   pages     int32 [B, max_pages];  pos  int32 [B, N], the tokens' positions; negative: nothing is
+ *             written, the row of Qo is zeros
+ *   strides   12 values: Q, K, V, Qo (Q's and Qo's unused if they are null)
+ * Rotation in fp32, rounded once.  No two rows of a call may name the same place.  A position outside the
+ * page table or the angles' tables, or a page outside the pool: that row is not written,
+ * MOA_ERR_DEVICE_INDEX (Qo: NaN where the position has no angles).
+ */
+int moa_kv_append(const void* Q, const void* K, const void* V, const float* cos, const float* sin,
+                  void* pool, const int32_t* pages, const int32_t* pos, void* Qo, int64_t B,
+                  int64_t H_q, int64_t H_k, int64_t N, int64_t d_k, int64_t d_v, int64_t d_rot,
+                  int64_t n_pos, int64_t n_pages, int64_t page_tokens, int64_t max_pages,
+                  const int64_t* strides, int interleaved, int dtype, void* stream);
+
+/*
+ * moa_kv_attn -- attention of N query rows of each sequence over its tokens in such a cache.
+ *   Q  [B, H_q, N, d_k] input, O  [B, H_q, N, d_v] output;  strides  6 values: Q, O
+ *   lens     int32 [B] on the device: L of each sequence, 0 <= lens[b] <= max_len
+ *   max_len  what the host knows of the lengths: it decides how the work is divided
+ *            (1 <= max_len <= max_pages * page_tokens, below 2^31 - 64)
+ *   causal   0: queries see later tokens too (those before their window are hidden all the same)
+ *   LSE, scale, dtype (the pool's), workspace  as moa_window_attn
+ * What the pool holds past lens[b], and at tokens that a query does not see, has no influence on it.
+ * Pages all of whose tokens lie before every query's window (and are no sinks) are not looked at: their
+ * entries of the table may hold anything.  Tokens of a page outside the pool read as zeros, a length
+ * outside [0, max_len] is clamped; both record MOA_ERR_DEVICE_INDEX.
+ */
+int moa_kv_attn(const void* Q, const void* pool, const int32_t* pages, const int32_t* lens, void* O,
+                float* LSE, int64_t B, int64_t H_q, int64_t H_k, int64_t N, int64_t d_k, int64_t d_v,
+                int64_t n_pages, int64_t page_tokens, int64_t max_pages, int64_t max_len,
+                int64_t window, int64_t sinks, const int64_t* strides, float scale, int causal,
+                int dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Scratch bytes of moa_kv_attn on the current device (0 for invalid sizes or without a device, and where
+ * none is needed). */
+size_t moa_kv_attn_workspace_bytes(int64_t B, int64_t H_q, int64_t H_k, int64_t N, int64_t d_k,
+                                   int64_t d_v, int64_t max_len, int64_t window, int64_t sinks,
+                                   int dtype);
+
 /*
  * moa_last_error -- human-readable reason for the last non-OK status returned
  * on the calling thread ("" if none).  The string is owned by the library and

@@ -22,9 +22,13 @@ from ._lib import (MOA_BF16, MOA_FP32, MoaError, check, lib, moa_attn_dnf_bytes,
                    moa_attn_bwd_fused_workspace_bytes, moa_kv4_attn,
                    moa_kv4_attn_workspace_bytes, moa_kv4_pool_bytes, moa_kv4_read,
                    moa_kv4_write, moa_qk_norm_rope, moa_qk_norm_rope_bwd,
-                   moa_qk_norm_rope_bwd_workspace_bytes)
-from .ops import (kv4_attn, kv4_attn_lse, kv4_pool, kv4_read, kv4_write, qk_norm_rope,  # noqa: F401
-                  qk_norm_rope_bwd, rope_table)
+                   moa_qk_norm_rope_bwd_workspace_bytes, moa_kv_append, moa_kv_attn,
+                   moa_kv_attn_workspace_bytes, moa_kv_pool_bytes, moa_window_attn,
+                   moa_window_attn_bwd, moa_window_attn_bwd_workspace_bytes,
+                   moa_window_attn_workspace_bytes)
+from .ops import (kv4_attn, kv4_attn_lse, kv4_pool, kv4_read, kv4_write, kv_append, kv_attn,  # noqa: F401
+                  kv_attn_lse, kv_pool, qk_norm_rope, qk_norm_rope_bwd, rope_table, window_attn,
+                  window_attn_bwd, window_attn_lse)
 
 __all__ = ["attn_fwd", "attn_fwd_staged", "get_device_status", "attn_flops", "dnf_bytes",
            "MOA_FP32", "MOA_BF16", "MoaError", "moa_attn_fwd", "moa_attn_fwd_staged",
@@ -37,7 +41,11 @@ __all__ = ["attn_fwd", "attn_fwd_staged", "get_device_status", "attn_flops", "dn
            "qk_norm_rope_bwd", "rope_table", "kv4_pool", "kv4_write", "kv4_read", "kv4_attn",
            "kv4_attn_lse", "moa_qk_norm_rope", "moa_qk_norm_rope_bwd",
            "moa_qk_norm_rope_bwd_workspace_bytes", "moa_kv4_pool_bytes", "moa_kv4_write",
-           "moa_kv4_read", "moa_kv4_attn", "moa_kv4_attn_workspace_bytes"]
+           "moa_kv4_read", "moa_kv4_attn", "moa_kv4_attn_workspace_bytes", "window_attn",
+           "window_attn_lse", "window_attn_bwd", "kv_pool", "kv_append", "kv_attn", "kv_attn_lse",
+           "moa_window_attn", "moa_window_attn_workspace_bytes", "moa_window_attn_bwd",
+           "moa_window_attn_bwd_workspace_bytes", "moa_kv_pool_bytes", "moa_kv_append", "moa_kv_attn",
+           "moa_kv_attn_workspace_bytes"]
 
 
 def _dtype_code(t) -> int:

@@ -80,6 +80,17 @@ SIGNATURES = {
     "moa_kv4_attn": (ctypes.c_int, [_VP] * 6 + [_I64] * 10 +
                      [_VP, ctypes.c_float, ctypes.c_int, ctypes.c_int, _VP, ctypes.c_size_t, _VP]),
     "moa_kv4_attn_workspace_bytes": (ctypes.c_size_t, [_I64] * 7 + [ctypes.c_int]),
+    "moa_window_attn": (ctypes.c_int, [_VP] * 5 + [_I64] * 9 +
+                        [_VP, ctypes.c_float, ctypes.c_int, _VP, ctypes.c_size_t, _VP]),
+    "moa_window_attn_workspace_bytes": (ctypes.c_size_t, [_I64] * 9 + [ctypes.c_int]),
+    "moa_window_attn_bwd": (ctypes.c_int, [_VP] * 9 + [_I64] * 9 +
+                            [_VP, ctypes.c_float, ctypes.c_int, _VP, ctypes.c_size_t, _VP]),
+    "moa_window_attn_bwd_workspace_bytes": (ctypes.c_size_t, [_I64] * 9 + [ctypes.c_int]),
+    "moa_kv_pool_bytes": (ctypes.c_size_t, [_I64] * 5 + [ctypes.c_int]),
+    "moa_kv_append": (ctypes.c_int, [_VP] * 9 + [_I64] * 11 + [_VP, ctypes.c_int, ctypes.c_int, _VP]),
+    "moa_kv_attn": (ctypes.c_int, [_VP] * 6 + [_I64] * 12 +
+                    [_VP, ctypes.c_float, ctypes.c_int, ctypes.c_int, _VP, ctypes.c_size_t, _VP]),
+    "moa_kv_attn_workspace_bytes": (ctypes.c_size_t, [_I64] * 9 + [ctypes.c_int]),
     "moa_last_error": (ctypes.c_char_p, []),
     "moa_get_device_status": (ctypes.c_int, [_VP]),
     "moa_selftest_wait_timeout": (ctypes.c_int, [ctypes.c_uint64, _VP]),
@@ -238,6 +249,51 @@ def moa_kv4_attn(Q, pool, pages, lens, O, LSE, B, H_q, H_k, N, d_k, d_v, n_pages
 
 def moa_kv4_attn_workspace_bytes(B, H_q, H_k, N, d_k, d_v, max_len, dtype) -> int:
     return lib().moa_kv4_attn_workspace_bytes(B, H_q, H_k, N, d_k, d_v, max_len, dtype)
+
+
+def moa_window_attn(Q, K, V, O, LSE, B, H_q, H_k, N_q, N_k, d_k, d_v, window, sinks, strides, scale,
+                    dtype, workspace, workspace_bytes, stream) -> int:
+    return lib().moa_window_attn(Q, K, V, O, LSE, B, H_q, H_k, N_q, N_k, d_k, d_v, window, sinks,
+                                 _strides(strides), scale, dtype, workspace, workspace_bytes, stream)
+
+
+def moa_window_attn_workspace_bytes(B, H_q, H_k, N_q, N_k, d_k, d_v, window, sinks, dtype) -> int:
+    return lib().moa_window_attn_workspace_bytes(B, H_q, H_k, N_q, N_k, d_k, d_v, window, sinks, dtype)
+
+
+def moa_window_attn_bwd(Q, K, V, O, dO, LSE, dQ, dK, dV, B, H_q, H_k, N_q, N_k, d_k, d_v, window,
+                        sinks, strides, scale, dtype, workspace, workspace_bytes, stream) -> int:
+    return lib().moa_window_attn_bwd(Q, K, V, O, dO, LSE, dQ, dK, dV, B, H_q, H_k, N_q, N_k, d_k, d_v,
+                                     window, sinks, _strides(strides), scale, dtype, workspace,
+                                     workspace_bytes, stream)
+
+
+def moa_window_attn_bwd_workspace_bytes(B, H_q, H_k, N_q, N_k, d_k, d_v, window, sinks, dtype) -> int:
+    return lib().moa_window_attn_bwd_workspace_bytes(B, H_q, H_k, N_q, N_k, d_k, d_v, window, sinks,
+                                                     dtype)
+
+
+def moa_kv_pool_bytes(n_pages, H, page_tokens, d_k, d_v, dtype) -> int:
+    return lib().moa_kv_pool_bytes(n_pages, H, page_tokens, d_k, d_v, dtype)
+
+
+def moa_kv_append(Q, K, V, cos, sin, pool, pages, pos, Qo, B, H_q, H_k, N, d_k, d_v, d_rot, n_pos,
+                  n_pages, page_tokens, max_pages, strides, interleaved, dtype, stream) -> int:
+    return lib().moa_kv_append(Q, K, V, cos, sin, pool, pages, pos, Qo, B, H_q, H_k, N, d_k, d_v, d_rot,
+                               n_pos, n_pages, page_tokens, max_pages, _strides(strides), interleaved,
+                               dtype, stream)
+
+
+def moa_kv_attn(Q, pool, pages, lens, O, LSE, B, H_q, H_k, N, d_k, d_v, n_pages, page_tokens, max_pages,
+                max_len, window, sinks, strides, scale, causal, dtype, workspace, workspace_bytes,
+                stream) -> int:
+    return lib().moa_kv_attn(Q, pool, pages, lens, O, LSE, B, H_q, H_k, N, d_k, d_v, n_pages,
+                             page_tokens, max_pages, max_len, window, sinks, _strides(strides), scale,
+                             causal, dtype, workspace, workspace_bytes, stream)
+
+
+def moa_kv_attn_workspace_bytes(B, H_q, H_k, N, d_k, d_v, max_len, window, sinks, dtype) -> int:
+    return lib().moa_kv_attn_workspace_bytes(B, H_q, H_k, N, d_k, d_v, max_len, window, sinks, dtype)
 
 
 # MOA_NOALLOC_SCRATCH_BYTES and MOA_SPLITS_AUTO of include/moa_attn.h

@@ -10,6 +10,7 @@
 #include "../../include/moa_attn.h"
 #include "internal.h"
 #include "ops_internal.h"
+#include "window.cuh"
 
 namespace moa {
 namespace {
@@ -393,6 +394,302 @@ int attn_call(const void* Q, const void* pool, const int32_t* pages, const int32
   return api_debug_check(stream);
 }
 
+// ---------------------------------------------------------------------------------------------
+// Attention with a window, its gradients, and the 16- and 32-bit cache
+// ---------------------------------------------------------------------------------------------
+// Two tensors that may share a buffer without sharing an element.
+bool apart(const View& a, const Shape& sa, const View& b, const Shape& sb, int64_t elt) {
+  return sa.d == sb.d && sa.N == sb.N && sa.B == sb.B && disjoint_slices(a, sa, b, sb, elt);
+}
+
+struct Tensor {
+  const char* name;
+  const View* v;
+  Shape shape;
+  bool output;
+  int alias;   // index of the input that this output may be, or -1
+};
+struct Buffer {
+  const char* name;
+  const void* p;
+  int64_t bytes;
+  int align;
+  bool output;
+};
+
+// Every tensor and buffer by itself, then no output on anything else.
+template <int NT, int NB>
+int check_operands(const Tensor (&t)[NT], const Buffer (&f)[NB], int64_t elt) {
+  Span span[NT];
+  for (int i = 0; i < NB; ++i) {
+    if (f[i].p == nullptr) return api_fail(MOA_ERR_INVALID_ARG, "null pointer %s", f[i].name);
+    if (reinterpret_cast<uintptr_t>(f[i].p) % f[i].align != 0)
+      return api_fail(MOA_ERR_MISALIGNED, "%s is not %d-byte aligned", f[i].name, f[i].align);
+  }
+  for (int i = 0; i < NT; ++i) {
+    const int rc = check_view(t[i].name, *t[i].v, t[i].shape, elt, t[i].output, &span[i]);
+    if (rc != MOA_OK) return rc;
+  }
+  for (int i = 0; i < NT; ++i) {
+    if (!t[i].output) continue;
+    for (int j = 0; j < NT; ++j) {
+      if (j == i || (t[j].output && j < i) || !overlap(span[i], span[j])) continue;
+      if (j == t[i].alias && same_view(*t[i].v, *t[j].v)) continue;
+      if (apart(*t[i].v, t[i].shape, *t[j].v, t[j].shape, elt)) continue;
+      return api_fail(MOA_ERR_INVALID_ARG, "%s overlaps %s", t[i].name, t[j].name);
+    }
+    for (int j = 0; j < NB; ++j)
+      if (overlap(span[i], flat(f[j].p, f[j].bytes)))
+        return api_fail(MOA_ERR_INVALID_ARG, "%s overlaps %s", t[i].name, f[j].name);
+  }
+  for (int i = 0; i < NB; ++i) {
+    if (!f[i].output) continue;
+    const Span s = flat(f[i].p, f[i].bytes);
+    for (int j = 0; j < NT; ++j)
+      if (!t[j].output && overlap(s, span[j])) return api_fail(MOA_ERR_INVALID_ARG, "%s overlaps %s", f[i].name, t[j].name);
+    for (int j = 0; j < NB; ++j)
+      if (j != i && overlap(s, flat(f[j].p, f[j].bytes)))
+        return api_fail(MOA_ERR_INVALID_ARG, "%s overlaps %s", f[i].name, f[j].name);
+  }
+  return MOA_OK;
+}
+
+// Sizes and settings that windowed attention, its gradients and cache attention share.
+int check_window(int64_t B, int64_t Hq, int64_t Hk, int64_t N, int64_t dk, int64_t dv, int64_t window, int64_t sinks,
+                 float scale) {
+  if (B < 1 || Hq < 1 || Hk < 1 || N < 1) return api_fail(MOA_ERR_INVALID_ARG, "sizes must be >= 1");
+  if (Hq % Hk != 0)
+    return api_fail(MOA_ERR_UNSUPPORTED_SHAPE, "H_q must be a multiple of H_k; got %lld, %lld", (long long)Hq, (long long)Hk);
+  if ((dk != 64 && dk != 128) || (dv != 64 && dv != 128))
+    return api_fail(MOA_ERR_UNSUPPORTED_SHAPE, "d_k, d_v must be 64 or 128; got %lld, %lld", (long long)dk, (long long)dv);
+  int64_t rows;
+  if (!mul(B, Hq, &rows) || !mul(rows, N, &rows) || rows > kMax31)
+    return api_fail(MOA_ERR_UNSUPPORTED_SHAPE, "B * H_q * N must be below 2^31");
+  if (window < 0 || sinks < 0) return api_fail(MOA_ERR_INVALID_ARG, "window and sinks must not be negative");
+  if (!std::isfinite(scale)) return api_fail(MOA_ERR_INVALID_ARG, "scale must be finite");
+  return MOA_OK;
+}
+
+// A window as the kernels take it: one that reaches past every token is none, and then nothing but the
+// sequence's beginning is a sink.
+void set_window(WindowArgs& a, int64_t window, int64_t sinks) {
+  a.window = window == 0 || window >= a.max_len ? win::kNoWindow : int(window);
+  a.sinks = int(a.window == win::kNoWindow ? 0 : sinks < a.max_len ? sinks : a.max_len);
+}
+
+size_t window_workspace(const WindowArgs& a, int sms) {
+  return window_cc_workspace(a, window_cc_plan(a, sms));
+}
+int launch_window(const WindowArgs& a, int sms, char* msg, size_t msglen) {
+  return launch_window_cc(a, window_cc_plan(a, sms), msg, msglen);
+}
+
+// The workspace of a call: as large as it has to be, aligned, and on nothing else.
+int run_window(WindowArgs& a, const Span* in, int n_in, const Span& out, void* workspace, size_t workspace_bytes) {
+  int64_t rows = a.B * a.Hq * a.N;
+  if (reinterpret_cast<uintptr_t>(a.lse) % 4 != 0) return api_fail(MOA_ERR_MISALIGNED, "LSE is not 4-byte aligned");
+  const Span lse_s = flat(a.lse, a.lse ? rows * 4 : 0);
+  for (int i = 0; i < n_in; ++i)
+    if (overlap(out, in[i]) || (a.lse != nullptr && overlap(lse_s, in[i])))
+      return api_fail(MOA_ERR_INVALID_ARG, "an output overlaps an input");
+  if (a.lse != nullptr && overlap(out, lse_s)) return api_fail(MOA_ERR_INVALID_ARG, "O overlaps LSE");
+  int sms = 0;
+  const cudaError_t e = device_sm_count(&sms);
+  if (e != cudaSuccess) return api_fail(MOA_ERR_CUDA, "SM count of the current device: %s", cudaGetErrorString(e));
+  const size_t need = window_workspace(a, sms);
+  if (need > 0) {
+    if (workspace == nullptr || workspace_bytes < need)
+      return api_fail(MOA_ERR_INVALID_ARG, "workspace too small: need %zu bytes, got %zu", need,
+                      workspace == nullptr ? size_t(0) : workspace_bytes);
+    if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return api_fail(MOA_ERR_MISALIGNED, "workspace is not 16-byte aligned");
+    const Span ws = flat(workspace, int64_t(need));
+    for (int i = 0; i < n_in; ++i)
+      if (overlap(ws, in[i])) return api_fail(MOA_ERR_INVALID_ARG, "the workspace overlaps an input");
+    if (overlap(ws, out) || (a.lse != nullptr && overlap(ws, lse_s)))
+      return api_fail(MOA_ERR_INVALID_ARG, "the workspace overlaps an output");
+  }
+  a.ws = workspace;
+  char msg[256] = {0};
+  const int rc = launch_window(a, sms, msg, sizeof(msg));
+  if (rc != MOA_OK) return api_fail(rc, "%s", msg);
+  api_clear();
+  return api_debug_check(a.stream);
+}
+
+int check_keys(int64_t B, int64_t Hk, int64_t Nk) {
+  if (Nk < 1) return api_fail(MOA_ERR_INVALID_ARG, "sizes must be >= 1");
+  int64_t rows;
+  if (Nk > kMax31 - 64 || !mul(B, Hk, &rows) || !mul(rows, Nk, &rows) || rows > kMax31)
+    return api_fail(MOA_ERR_UNSUPPORTED_SHAPE, "B * H_k * N_k must be below 2^31");
+  return MOA_OK;
+}
+
+int window_call(const void* Q, const void* K, const void* V, void* O, float* LSE, int64_t B, int64_t H_q, int64_t H_k,
+                int64_t N_q, int64_t N_k, int64_t d_k, int64_t d_v, int64_t window, int64_t sinks, const int64_t* strides,
+                float scale, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = check_dtype(dtype);
+  if (rc == MOA_OK) rc = check_window(B, H_q, H_k, N_q, d_k, d_v, window, sinks, scale);
+  if (rc == MOA_OK) rc = check_keys(B, H_k, N_k);
+  if (rc != MOA_OK) return rc;
+  if (!strides) return api_fail(MOA_ERR_INVALID_ARG, "null strides pointer");
+  const int64_t elt = dtype == MOA_FP32 ? 4 : 2;
+  WindowArgs a{};
+  const View k = view(K, strides + 3), v = view(V, strides + 6);
+  a.q = view(Q, strides), a.o = view(O, strides + 9);
+  Span in[3], out;
+  rc = check_view("Q", a.q, Shape{B, H_q, N_q, d_k}, elt, false, &in[0]);
+  if (rc == MOA_OK) rc = check_view("K", k, Shape{B, H_k, N_k, d_k}, elt, false, &in[1]);
+  if (rc == MOA_OK) rc = check_view("V", v, Shape{B, H_k, N_k, d_v}, elt, false, &in[2]);
+  if (rc == MOA_OK) rc = check_view("O", a.o, Shape{B, H_q, N_q, d_v}, elt, true, &out);
+  if (rc != MOA_OK) return rc;
+  a.kv = KvSource{K, V, k.sb, k.sh, k.sn, v.sb, v.sh, v.sn, nullptr, B, 0, 0};
+  a.lse = LSE, a.lens = nullptr;
+  a.B = B, a.Hq = H_q, a.Hk = H_k, a.N = N_q, a.max_len = N_k;
+  a.dk = int(d_k), a.dv = int(d_v);
+  set_window(a, window, sinks);
+  a.scale = scale, a.causal = true, a.f32 = dtype == MOA_FP32;
+  a.stream = static_cast<cudaStream_t>(stream);
+  return run_window(a, in, 3, out, workspace, workspace_bytes);
+}
+
+bool kv_pool_size(int64_t n_pages, int64_t H, int64_t page, int64_t dk, int64_t dv, int64_t elt, int64_t* bytes) {
+  if (n_pages < 1 || H < 1 || page < 16 || page % 16 != 0) return false;
+  if ((dk != 64 && dk != 128) || (dv != 64 && dv != 128)) return false;
+  int64_t x;
+  return mul(n_pages, H, &x) && mul(x, page, &x) && mul(x, (dk + dv) * elt, bytes);
+}
+
+// The pool, its table, and their sizes.
+int check_pool(const void* pool, const int32_t* pages, int64_t B, int64_t H, int64_t d_k, int64_t d_v, int64_t n_pages,
+               int64_t page_tokens, int64_t max_pages, int64_t elt, Span* pool_span, Span* pages_span) {
+  if (!pool || !pages) return api_fail(MOA_ERR_INVALID_ARG, "null pool or pages pointer");
+  if (n_pages < 1 || max_pages < 1 || page_tokens < 1) return api_fail(MOA_ERR_INVALID_ARG, "sizes must be >= 1");
+  if (page_tokens % 16 != 0 || page_tokens > (1 << 20))
+    return api_fail(MOA_ERR_UNSUPPORTED_SHAPE, "page_tokens must be a multiple of 16 up to 2^20; got %lld",
+                    (long long)page_tokens);
+  int64_t bytes, table;
+  if (H > kMax31 || n_pages > kMax31 - 1 || !kv_pool_size(n_pages, H, page_tokens, d_k, d_v, elt, &bytes) ||
+      !mul(B, max_pages, &table) || max_pages > kMax31)
+    return api_fail(MOA_ERR_UNSUPPORTED_SHAPE, "the pool or its table is too large");
+  if (reinterpret_cast<uintptr_t>(pool) % 16 != 0) return api_fail(MOA_ERR_MISALIGNED, "pool is not 16-byte aligned");
+  if (reinterpret_cast<uintptr_t>(pages) % 4 != 0) return api_fail(MOA_ERR_MISALIGNED, "pages is not 4-byte aligned");
+  *pool_span = flat(pool, bytes);
+  *pages_span = flat(pages, table * 4);
+  return MOA_OK;
+}
+
+int cache_call(const void* Q, const void* pool, const int32_t* pages, const int32_t* lens, void* O, float* LSE, int64_t B,
+               int64_t H_q, int64_t H_k, int64_t N, int64_t d_k, int64_t d_v, int64_t n_pages, int64_t page_tokens,
+               int64_t max_pages, int64_t max_len, int64_t window, int64_t sinks, const int64_t* strides, float scale,
+               int causal, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = check_dtype(dtype);
+  if (rc == MOA_OK) rc = check_window(B, H_q, H_k, N, d_k, d_v, window, sinks, scale);
+  if (rc != MOA_OK) return rc;
+  const int64_t elt = dtype == MOA_FP32 ? 4 : 2;
+  Span in[4], out;
+  rc = check_pool(pool, pages, B, H_k, d_k, d_v, n_pages, page_tokens, max_pages, elt, &in[1], &in[2]);
+  if (rc != MOA_OK) return rc;
+  if (!lens || !strides) return api_fail(MOA_ERR_INVALID_ARG, "null lens or strides pointer");
+  if (reinterpret_cast<uintptr_t>(lens) % 4 != 0) return api_fail(MOA_ERR_MISALIGNED, "lens is not 4-byte aligned");
+  if (max_len < 1) return api_fail(MOA_ERR_INVALID_ARG, "sizes must be >= 1");
+  if (max_len > max_pages * page_tokens || max_len > kMax31 - 64)
+    return api_fail(MOA_ERR_INVALID_ARG, "max_len %lld is more than the page table or the kernels take", (long long)max_len);
+  WindowArgs a{};
+  a.q = view(Q, strides), a.o = view(O, strides + 3);
+  rc = check_view("Q", a.q, Shape{B, H_q, N, d_k}, elt, false, &in[0]);
+  if (rc == MOA_OK) rc = check_view("O", a.o, Shape{B, H_q, N, d_v}, elt, true, &out);
+  if (rc != MOA_OK) return rc;
+  in[3] = flat(lens, B * 4);
+  const int64_t row = d_k + d_v;
+  a.kv = KvSource{pool, static_cast<const char*>(pool) + d_k * elt, H_k * page_tokens * row, page_tokens * row, row,
+                  H_k * page_tokens * row, page_tokens * row, row, pages, n_pages, max_pages, int(page_tokens)};
+  a.lse = LSE, a.lens = lens;
+  a.B = B, a.Hq = H_q, a.Hk = H_k, a.N = N, a.max_len = max_len;
+  a.dk = int(d_k), a.dv = int(d_v);
+  set_window(a, window, sinks);
+  a.scale = scale, a.causal = causal != 0, a.f32 = dtype == MOA_FP32;
+  a.stream = static_cast<cudaStream_t>(stream);
+  return run_window(a, in, 4, out, workspace, workspace_bytes);
+}
+
+size_t window_bwd_workspace(const WindowBwdArgs& a) { return window_bwd_cc_workspace(a); }
+
+void set_bwd_window(WindowBwdArgs& a, int64_t window, int64_t sinks) {
+  a.window = window == 0 || window >= a.Nk ? win::kNoWindow : int(window);
+  a.sinks = int(a.window == win::kNoWindow ? 0 : sinks < a.Nk ? sinks : a.Nk);
+}
+
+int window_bwd_call(WindowBwdArgs& a, int64_t window, int64_t sinks, int dtype, size_t workspace_bytes) {
+  const int64_t elt = dtype == MOA_FP32 ? 4 : 2;
+  set_bwd_window(a, window, sinks);
+  const size_t need = window_bwd_workspace(a);
+  const Shape q{a.B, a.Hq, a.Nq, a.dk}, k{a.B, a.Hk, a.Nk, a.dk}, v{a.B, a.Hk, a.Nk, a.dv}, o{a.B, a.Hq, a.Nq, a.dv};
+  const Tensor t[] = {{"Q", &a.q, q, false, -1},  {"K", &a.k, k, false, -1},   {"V", &a.v, v, false, -1},
+                      {"O", &a.o, o, false, -1},  {"dO", &a.go, o, false, -1}, {"dQ", &a.dq, q, true, -1},
+                      {"dK", &a.dk_, k, true, -1}, {"dV", &a.dv_, v, true, -1}};
+  const Buffer f[] = {{"LSE", a.lse, a.B * a.Hq * a.Nq * 4, 4, false}, {"workspace", a.ws, int64_t(need), 16, true}};
+  int rc = check_operands(t, f, elt);
+  if (rc != MOA_OK) return rc;
+  if (workspace_bytes < need)
+    return api_fail(MOA_ERR_INVALID_ARG, "workspace too small: need %zu bytes, got %zu", need, workspace_bytes);
+  char msg[256] = {0};
+  rc = launch_window_bwd_cc(a, msg, sizeof(msg));
+  if (rc != MOA_OK) return api_fail(rc, "%s", msg);
+  api_clear();
+  return api_debug_check(a.stream);
+}
+
+int append_call(KvAppendArgs& a, int64_t d_k, int64_t d_v, int64_t d_rot, int64_t page_tokens, int dtype) {
+  const int64_t elt = dtype == MOA_FP32 ? 4 : 2;
+  const bool with_q = a.q.p != nullptr, turns = a.cosines != nullptr;
+  if (a.B < 1 || a.Hk < 1 || a.N < 1 || (with_q && a.Hq < 1)) return api_fail(MOA_ERR_INVALID_ARG, "sizes must be >= 1");
+  if ((d_k != 64 && d_k != 128) || (d_v != 64 && d_v != 128))
+    return api_fail(MOA_ERR_UNSUPPORTED_SHAPE, "d_k, d_v must be 64 or 128; got %lld, %lld", (long long)d_k, (long long)d_v);
+  if (!with_q) a.Hq = 0;
+  if (a.Hq > 65535 || a.Hk > 65535) return api_fail(MOA_ERR_UNSUPPORTED_SHAPE, "at most 65535 heads");
+  int64_t tokens, all;
+  if (!mul(a.B, a.N, &tokens) || !mul(tokens, (a.Hq + 2 * a.Hk) * 128, &all) || tokens > kMax31)
+    return api_fail(MOA_ERR_UNSUPPORTED_SHAPE, "too many tokens");
+  if (turns != (a.sines != nullptr)) return api_fail(MOA_ERR_INVALID_ARG, "cos and sin go together");
+  if (with_q && !turns) return api_fail(MOA_ERR_INVALID_ARG, "queries are only passed to be rotated: cos and sin are null");
+  if (turns) {
+    if (a.n_pos < 1) return api_fail(MOA_ERR_INVALID_ARG, "sizes must be >= 1");
+    if (a.n_pos > kMax31) return api_fail(MOA_ERR_UNSUPPORTED_SHAPE, "n_pos must be below 2^31");
+    if (d_rot < 16 || d_rot > d_k || d_rot % 16 != 0)
+      return api_fail(MOA_ERR_UNSUPPORTED_SHAPE, "d_rot must be a multiple of 16 up to d_k; got %lld", (long long)d_rot);
+  }
+  Span pool_s, pages_s;
+  int rc = check_pool(a.pool, a.table, a.B, a.Hk, d_k, d_v, a.n_pages, page_tokens, a.max_pages, elt, &pool_s, &pages_s);
+  if (rc != MOA_OK) return rc;
+  a.page = int(page_tokens), a.dk = int(d_k), a.dv = int(d_v), a.d_rot = turns ? int(d_rot) : 0;
+  a.f32 = dtype == MOA_FP32;
+  const Shape q{a.B, a.Hq, a.N, d_k}, k{a.B, a.Hk, a.N, d_k}, v{a.B, a.Hk, a.N, d_v};
+  const Buffer pool{"the pool", a.pool, int64_t(pool_s.hi - pool_s.lo), 16, true};
+  const Buffer pages{"pages", a.table, int64_t(pages_s.hi - pages_s.lo), 4, false}, pos{"pos", a.pos, tokens * 4, 4, false};
+  const Tensor tk{"K", &a.k, k, false, -1}, tv{"V", &a.v, v, false, -1};
+  if (turns) {
+    const Buffer f[] = {pool, pages, pos, {"cos", a.cosines, a.n_pos * d_rot * 2, 16, false},
+                        {"sin", a.sines, a.n_pos * d_rot * 2, 16, false}};
+    if (with_q) {
+      const Tensor t[] = {{"Q", &a.q, q, false, -1}, {"Qo", &a.oq, q, true, 0}, tk, tv};
+      rc = check_operands(t, f, elt);
+    } else {
+      const Tensor t[] = {tk, tv};
+      rc = check_operands(t, f, elt);
+    }
+  } else {
+    const Buffer f[] = {pool, pages, pos};
+    const Tensor t[] = {tk, tv};
+    rc = check_operands(t, f, elt);
+  }
+  if (rc != MOA_OK) return rc;
+  char msg[256] = {0};
+  rc = launch_kv_append(a, msg, sizeof(msg));
+  if (rc != MOA_OK) return api_fail(rc, "%s", msg);
+  api_clear();
+  return api_debug_check(a.stream);
+}
+
 }  // namespace
 }  // namespace moa
 
@@ -494,6 +791,110 @@ size_t moa_kv4_attn_workspace_bytes(int64_t B, int64_t H_q, int64_t H_k, int64_t
   if (moa::device_sm_count(&sms) != cudaSuccess) return 0;
   return moa::kv4_attn_workspace(B, H_k, max_len, d_k, d_v,
                                  moa::kv4_attn_plan(B, H_k, H_q / H_k, N, max_len, dtype == MOA_FP32, sms), sms);
+}
+
+int moa_window_attn(const void* Q, const void* K, const void* V, void* O, float* LSE, int64_t B, int64_t H_q, int64_t H_k,
+                    int64_t N_q, int64_t N_k, int64_t d_k, int64_t d_v, int64_t window, int64_t sinks,
+                    const int64_t* strides, float scale, int dtype, void* workspace, size_t workspace_bytes,
+                    void* stream) {
+  return moa::guarded([&] {
+    return moa::window_call(Q, K, V, O, LSE, B, H_q, H_k, N_q, N_k, d_k, d_v, window, sinks, strides, scale, dtype,
+                            workspace, workspace_bytes, stream);
+  });
+}
+
+size_t moa_window_attn_workspace_bytes(int64_t B, int64_t H_q, int64_t H_k, int64_t N_q, int64_t N_k, int64_t d_k,
+                                       int64_t d_v, int64_t window, int64_t sinks, int dtype) {
+  return moa_kv_attn_workspace_bytes(B, H_q, H_k, N_q, d_k, d_v, N_k, window, sinks, dtype);
+}
+
+int moa_window_attn_bwd(const void* Q, const void* K, const void* V, const void* O, const void* dO, const float* LSE,
+                        void* dQ, void* dK, void* dV, int64_t B, int64_t H_q, int64_t H_k, int64_t N_q, int64_t N_k,
+                        int64_t d_k, int64_t d_v, int64_t window, int64_t sinks, const int64_t* strides, float scale,
+                        int dtype, void* workspace, size_t workspace_bytes, void* stream) {
+  return moa::guarded([&] {
+    int rc = moa::check_dtype(dtype);
+    if (rc == MOA_OK) rc = moa::check_window(B, H_q, H_k, N_q, d_k, d_v, window, sinks, scale);
+    if (rc == MOA_OK) rc = moa::check_keys(B, H_k, N_k);
+    if (rc != MOA_OK) return rc;
+    if (!strides) return moa::api_fail(MOA_ERR_INVALID_ARG, "null strides pointer");
+    moa::WindowBwdArgs a{};
+    const moa::View x[] = {moa::view(Q, strides), moa::view(K, strides + 3), moa::view(V, strides + 6),
+                           moa::view(O, strides + 9), moa::view(dO, strides + 12), moa::view(dQ, strides + 15),
+                           moa::view(dK, strides + 18), moa::view(dV, strides + 21)};
+    a.q = x[0], a.k = x[1], a.v = x[2], a.o = x[3], a.go = x[4], a.dq = x[5], a.dk_ = x[6], a.dv_ = x[7];
+    a.lse = LSE;
+    a.B = B, a.Hq = H_q, a.Hk = H_k, a.Nq = N_q, a.Nk = N_k, a.dk = int(d_k), a.dv = int(d_v);
+    a.scale = scale, a.f32 = dtype == MOA_FP32;
+    a.ws = workspace;
+    a.stream = static_cast<cudaStream_t>(stream);
+    return moa::window_bwd_call(a, window, sinks, dtype, workspace_bytes);
+  });
+}
+
+size_t moa_window_attn_bwd_workspace_bytes(int64_t B, int64_t H_q, int64_t H_k, int64_t N_q, int64_t N_k, int64_t d_k,
+                                           int64_t d_v, int64_t window, int64_t sinks, int dtype) {
+  if ((dtype != MOA_BF16 && dtype != MOA_FP32) || B < 1 || H_q < 1 || H_k < 1 || N_q < 1 || N_k < 1) return 0;
+  if (H_q % H_k != 0 || (d_k != 64 && d_k != 128) || (d_v != 64 && d_v != 128) || window < 0 || sinks < 0) return 0;
+  int64_t rows;
+  if (!moa::mul(B, H_q, &rows) || !moa::mul(rows, N_q, &rows) || rows > moa::kMax31) return 0;
+  if (!moa::mul(B, H_k, &rows) || !moa::mul(rows, N_k, &rows) || rows > moa::kMax31 || N_k > moa::kMax31 - 64) return 0;
+  moa::WindowBwdArgs a{};
+  a.B = B, a.Hq = H_q, a.Hk = H_k, a.Nq = N_q, a.Nk = N_k, a.dk = int(d_k), a.dv = int(d_v);
+  a.f32 = dtype == MOA_FP32;
+  moa::set_bwd_window(a, window, sinks);
+  return moa::window_bwd_workspace(a);
+}
+
+size_t moa_kv_pool_bytes(int64_t n_pages, int64_t H, int64_t page_tokens, int64_t d_k, int64_t d_v, int dtype) {
+  int64_t bytes;
+  if (dtype != MOA_BF16 && dtype != MOA_FP32) return 0;
+  return moa::kv_pool_size(n_pages, H, page_tokens, d_k, d_v, dtype == MOA_FP32 ? 4 : 2, &bytes) ? size_t(bytes) : 0;
+}
+
+int moa_kv_append(const void* Q, const void* K, const void* V, const float* cos, const float* sin, void* pool,
+                  const int32_t* pages, const int32_t* pos, void* Qo, int64_t B, int64_t H_q, int64_t H_k, int64_t N,
+                  int64_t d_k, int64_t d_v, int64_t d_rot, int64_t n_pos, int64_t n_pages, int64_t page_tokens,
+                  int64_t max_pages, const int64_t* strides, int interleaved, int dtype, void* stream) {
+  return moa::guarded([&] {
+    const int rc = moa::check_dtype(dtype);
+    if (rc != MOA_OK) return rc;
+    if (!strides) return moa::api_fail(MOA_ERR_INVALID_ARG, "null strides pointer");
+    if ((Q == nullptr) != (Qo == nullptr)) return moa::api_fail(MOA_ERR_INVALID_ARG, "Q and Qo go together");
+    moa::KvAppendArgs a{};
+    a.q = moa::view(Q, strides), a.k = moa::view(K, strides + 3), a.v = moa::view(V, strides + 6);
+    a.oq = moa::view(Qo, strides + 9);
+    a.pool = pool, a.table = pages, a.pos = pos, a.cosines = cos, a.sines = sin;
+    a.B = B, a.Hq = H_q, a.Hk = H_k, a.N = N, a.n_pages = n_pages, a.max_pages = max_pages, a.n_pos = n_pos;
+    a.pairs = interleaved != 0;
+    a.stream = static_cast<cudaStream_t>(stream);
+    return moa::append_call(a, d_k, d_v, d_rot, page_tokens, dtype);
+  });
+}
+
+int moa_kv_attn(const void* Q, const void* pool, const int32_t* pages, const int32_t* lens, void* O, float* LSE, int64_t B,
+                int64_t H_q, int64_t H_k, int64_t N, int64_t d_k, int64_t d_v, int64_t n_pages, int64_t page_tokens,
+                int64_t max_pages, int64_t max_len, int64_t window, int64_t sinks, const int64_t* strides, float scale,
+                int causal, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
+  return moa::guarded([&] {
+    return moa::cache_call(Q, pool, pages, lens, O, LSE, B, H_q, H_k, N, d_k, d_v, n_pages, page_tokens, max_pages, max_len,
+                           window, sinks, strides, scale, causal, dtype, workspace, workspace_bytes, stream);
+  });
+}
+
+size_t moa_kv_attn_workspace_bytes(int64_t B, int64_t H_q, int64_t H_k, int64_t N, int64_t d_k, int64_t d_v,
+                                   int64_t max_len, int64_t window, int64_t sinks, int dtype) {
+  if ((dtype != MOA_BF16 && dtype != MOA_FP32) || B < 1 || H_q < 1 || H_k < 1 || N < 1 || max_len < 1) return 0;
+  if (H_q % H_k != 0 || (d_k != 64 && d_k != 128) || (d_v != 64 && d_v != 128) || max_len > moa::kMax31 - 64) return 0;
+  int64_t rows;
+  if (window < 0 || sinks < 0 || !moa::mul(B, H_q, &rows) || !moa::mul(rows, N, &rows) || rows > moa::kMax31) return 0;
+  int sms = 0;
+  if (moa::device_sm_count(&sms) != cudaSuccess) return 0;
+  moa::WindowArgs a{};
+  a.B = B, a.Hq = H_q, a.Hk = H_k, a.N = N, a.max_len = max_len, a.dk = int(d_k), a.dv = int(d_v);
+  a.f32 = dtype == MOA_FP32;
+  moa::set_window(a, window, sinks);
+  return moa::window_workspace(a, sms);
 }
 
 }  // extern "C"

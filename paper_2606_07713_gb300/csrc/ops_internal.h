@@ -107,7 +107,78 @@ size_t kv4_attn_tc_workspace(int64_t bh, int64_t max_len, int64_t dk, int64_t dv
 int launch_kv4_attn_tc(const Kv4AttnArgs& a, char* msg, size_t msglen);
 int launch_kv4_attn(const Kv4AttnArgs& a, const Kv4Plan& p, char* msg, size_t msglen);
 
-// Status words of the four translation units (0, MOA_ERR_DEVICE_TIMEOUT or
+// Where keys and values of attention with a window lie: token t of sequence b and key head h at
+// k + b * k_sb + h * k_sh + t * k_sn (and v alike), or, with a page table, page table[b, t / page] in
+// the place of b and t % page in that of t.  Strides in elements.
+struct KvSource {
+  const void* k;
+  const void* v;
+  int64_t k_sb, k_sh, k_sn, v_sb, v_sh, v_sn;
+  const int32_t* table;   // null: no pages
+  int64_t n_pages, max_pages;
+  int page;
+};
+// Attention of the last N of each sequence's tokens with a window and sinks (window.cuh).
+struct WindowArgs {
+  View q, o;
+  KvSource kv;
+  float* lse;            // [B, Hq, N] or null
+  const int32_t* lens;   // [B], or null: every sequence has max_len tokens
+  int64_t B, Hq, Hk, N, max_len;
+  int dk, dv;
+  int window, sinks;     // window: win::kNoWindow for none
+  float scale;
+  bool causal, f32;
+  void* ws;
+  cudaStream_t stream;
+};
+// CUDA cores: fp32, and bf16 tensors that no tensor map describes (window_fwd_cc.cu).
+struct WindowCcPlan {
+  int rows;              // query rows of a tile
+  int64_t items;         // tiles of all key heads
+  int64_t splits;        // shares of a tile's tokens, joined at the end
+};
+WindowCcPlan window_cc_plan(const WindowArgs& a, int sms);
+size_t window_cc_workspace(const WindowArgs& a, const WindowCcPlan& p);
+int launch_window_cc(const WindowArgs& a, const WindowCcPlan& p, char* msg, size_t msglen);
+
+// Gradients of attention with a window (dense keys and values).
+struct WindowBwdArgs {
+  View q, k, v, o, go;   // inputs
+  const float* lse;      // [B, Hq, Nq]
+  View dq, dk_, dv_;     // outputs
+  int64_t B, Hq, Hk, Nq, Nk;
+  int dk, dv;
+  int window, sinks;
+  float scale;
+  bool f32;
+  void* ws;
+  cudaStream_t stream;
+};
+size_t window_bwd_cc_workspace(const WindowBwdArgs& a);
+int launch_window_bwd_cc(const WindowBwdArgs& a, char* msg, size_t msglen);
+
+// New keys and values into a 16- or 32-bit paged cache [n_pages, H, page, dk + dv], keys (and
+// queries, into oq) rotated on the way.
+struct KvAppendArgs {
+  View q, oq;            // q.p null: no queries
+  View k, v;
+  void* pool;
+  const int32_t* table;  // [B, max_pages]
+  const int32_t* pos;    // [B, N]
+  const float* cosines;  // [n_pos, d_rot / 2], null: no rotation
+  const float* sines;
+  int64_t B, Hq, Hk, N, n_pages, max_pages, n_pos;
+  int page, dk, dv, d_rot;
+  bool pairs, f32;
+  cudaStream_t stream;
+};
+int launch_kv_append(const KvAppendArgs& a, char* msg, size_t msglen);
+
+cudaError_t window_cc_read_and_clear_status(unsigned* value);
+cudaError_t kv_append_read_and_clear_status(unsigned* value);
+
+// Status words of the translation units above (0, MOA_ERR_DEVICE_TIMEOUT or
 // MOA_ERR_DEVICE_INDEX); read and cleared after a synchronisation.
 cudaError_t norm_read_and_clear_status(unsigned* value);
 cudaError_t kv4_read_and_clear_status(unsigned* value);

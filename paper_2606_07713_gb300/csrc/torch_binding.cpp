@@ -376,6 +376,208 @@ PyObject* kv4_attn(PyObject* const* a) {
   return with_lse ? pair(o, lse) : THPVariable_Wrap(o);
 }
 
+// A window: None is none (0 of the C interface); anything else at least one token.
+int64_t window_of(const char* what, PyObject* o) {
+  if (o == Py_None) return 0;
+  const int64_t w = integer(what, "window", o);
+  if (w < 1) fail(PyExc_ValueError, "%s: window must be at least 1, or None", what);
+  return w;
+}
+
+// The output and the log-sum-exp of an attention call: given, or made.
+void row_outputs(const char* what, PyObject* out, PyObject* lse, const at::Tensor& q, int64_t dv, at::Tensor* o, at::Tensor* l,
+                 int64_t* strides) {
+  const int64_t os[4] = {q.size(0), q.size(1), q.size(2), dv};
+  *o = out == Py_None ? make(at::IntArrayRef(os, 4), q.scalar_type(), q.device()) : tensor(what, "out", out);
+  heads(what, "out", *o, &q, os, strides);
+  if (lse == Py_True) {
+    *l = make(at::IntArrayRef(os, 3), at::kFloat, q.device());
+  } else if (lse != Py_None) {
+    *l = tensor(what, "lse", lse);
+    flat(what, "lse", *l, at::kFloat, at::IntArrayRef(os, 3), q.device());
+  }
+}
+
+struct Dense {
+  const at::Tensor *q, *k, *v;
+  int64_t B, Hq, Hk, Nq, Nk, dk, dv, window, sinks;
+  float scale;
+  int64_t strides[24];
+};
+
+// q, k, v; a[0] window, a[1] sinks, a[2] scale
+Dense dense_args(const char* what, PyObject* const* qkv, PyObject* const* a) {
+  Dense n{};
+  n.q = &tensor(what, "q", qkv[0]), n.k = &tensor(what, "k", qkv[1]), n.v = &tensor(what, "v", qkv[2]);
+  heads(what, "q", *n.q, nullptr, nullptr, n.strides);
+  heads(what, "k", *n.k, n.q, nullptr, n.strides + 3);
+  heads(what, "v", *n.v, n.q, nullptr, n.strides + 6);
+  n.B = n.q->size(0), n.Hq = n.q->size(1), n.Nq = n.q->size(2), n.dk = n.q->size(3);
+  n.Hk = n.k->size(1), n.Nk = n.k->size(2), n.dv = n.v->size(3);
+  if (n.k->size(0) != n.B || n.k->size(3) != n.dk || n.v->size(0) != n.B || n.v->size(1) != n.Hk || n.v->size(2) != n.Nk)
+    fail(PyExc_ValueError, "%s: q, k and v do not fit: %s %s %s", what, text(n.q->sizes()).c_str(),
+         text(n.k->sizes()).c_str(), text(n.v->sizes()).c_str());
+  n.window = window_of(what, a[0]);
+  n.sinks = integer(what, "sinks", a[1]);
+  n.scale = a[2] == Py_None ? float(1.0 / std::sqrt(double(n.dk))) : float(number(what, "scale", a[2]));
+  return n;
+}
+
+// (q, k, v, window, sinks, scale, out, lse, workspace, stream); lse: None, or a tensor, or True to make
+// one.  Returns o or (o, lse).
+PyObject* window_attn(PyObject* const* a) {
+  const bool with_lse = a[7] != Py_None;
+  const char* what = with_lse ? "window_attn_lse" : "window_attn";
+  Dense n = dense_args(what, a, a + 3);
+  const int dtype = code(what, *n.q);
+  const Place place(a[9], n.q->device());
+  at::Tensor o, lse;
+  row_outputs(what, a[6], a[7], *n.q, n.dv, &o, &lse, n.strides + 9);
+  const Scratch ws(what, a[8], moa_window_attn_workspace_bytes(n.B, n.Hq, n.Hk, n.Nq, n.Nk, n.dk, n.dv, n.window,
+                                                               n.sinks < 0 ? 0 : n.sinks, dtype), place);
+  check(moa_window_attn(n.q->data_ptr(), n.k->data_ptr(), n.v->data_ptr(), o.data_ptr(),
+                        with_lse ? static_cast<float*>(lse.data_ptr()) : nullptr, n.B, n.Hq, n.Hk, n.Nq, n.Nk, n.dk, n.dv,
+                        n.window, n.sinks, n.strides, n.scale, dtype, ws.p, ws.bytes, place.raw()));
+  return with_lse ? pair(o, lse) : THPVariable_Wrap(o);
+}
+
+// (q, k, v, o, lse, do, window, sinks, scale, out, workspace, stream)
+PyObject* window_attn_bwd(PyObject* const* a) {
+  const char* what = "window_attn_bwd";
+  Dense n = dense_args(what, a, a + 6);
+  const at::Tensor &o = tensor(what, "o", a[3]), &lse = tensor(what, "lse", a[4]), &go = tensor(what, "do", a[5]);
+  const int64_t os[4] = {n.B, n.Hq, n.Nq, n.dv};
+  heads(what, "o", o, n.q, os, n.strides + 9);
+  heads(what, "do", go, n.q, os, n.strides + 12);
+  flat(what, "lse", lse, at::kFloat, {n.B, n.Hq, n.Nq}, n.q->device());
+  const int dtype = code(what, *n.q);
+  const Place place(a[11], n.q->device());
+  at::Tensor t[3];
+  const at::Tensor* like[3] = {n.q, n.k, n.v};
+  const char* names[3] = {"out[0]", "out[1]", "out[2]"};
+  if (a[9] == Py_None) {
+    for (int i = 0; i < 3; ++i) t[i] = make(like[i]->sizes(), n.q->scalar_type(), n.q->device());
+  } else {
+    PyObject* s = PySequence_Fast(a[9], "out must be three tensors");
+    if (s == nullptr) throw Raise{nullptr, ""};
+    bool good = PySequence_Fast_GET_SIZE(s) == 3;
+    for (int i = 0; good && i < 3; ++i) {
+      PyObject* x = PySequence_Fast_GET_ITEM(s, i);
+      good = THPVariable_Check(x);
+      if (good) t[i] = THPVariable_Unpack(x);
+    }
+    Py_DECREF(s);
+    if (!good) fail(PyExc_ValueError, "%s: out must be three tensors", what);
+  }
+  for (int i = 0; i < 3; ++i) heads(what, names[i], t[i], n.q, like[i]->sizes().data(), n.strides + 15 + 3 * i);
+  const Scratch ws(what, a[10], moa_window_attn_bwd_workspace_bytes(n.B, n.Hq, n.Hk, n.Nq, n.Nk, n.dk, n.dv, n.window,
+                                                                    n.sinks < 0 ? 0 : n.sinks, dtype), place);
+  check(moa_window_attn_bwd(n.q->data_ptr(), n.k->data_ptr(), n.v->data_ptr(), o.data_ptr(), go.data_ptr(), f32(lse),
+                            t[0].data_ptr(), t[1].data_ptr(), t[2].data_ptr(), n.B, n.Hq, n.Hk, n.Nq, n.Nk, n.dk, n.dv,
+                            n.window, n.sinks, n.strides, n.scale, dtype, ws.p, ws.bytes, place.raw()));
+  PyObject* r = PyTuple_New(3);
+  if (r == nullptr) return nullptr;
+  for (int i = 0; i < 3; ++i) PyTuple_SET_ITEM(r, i, THPVariable_Wrap(t[i]));
+  return r;
+}
+
+// The pool of the 16- or 32-bit cache, of `like`'s type, and its table.
+struct Pool {
+  const at::Tensor *pool, *pages;
+  int64_t n_pages, H, page, max_pages, dv;
+};
+Pool pool_args(const char* what, PyObject* pool, PyObject* pages, const at::Tensor& like, int64_t B, int64_t dk) {
+  Pool c{};
+  c.pool = &tensor(what, "pool", pool), c.pages = &tensor(what, "pages", pages);
+  if (c.pool->dim() != 4 || !c.pool->is_contiguous())
+    fail(PyExc_ValueError, "%s: pool must be a contiguous tensor as kv_pool makes it", what);
+  if (c.pool->scalar_type() != like.scalar_type())
+    fail(PyExc_TypeError, "%s: pool must be %s, got %s", what, c10::toString(like.scalar_type()),
+         c10::toString(c.pool->scalar_type()));
+  if (c.pool->device() != like.device())
+    fail(PyExc_ValueError, "%s: pool is on %s, not on %s", what, c.pool->device().str().c_str(), like.device().str().c_str());
+  if (c.pages->dim() != 2) fail(PyExc_ValueError, "%s: pages must be [B, max_pages]", what);
+  flat(what, "pages", *c.pages, at::kInt, {B, c.pages->size(1)}, like.device());
+  c.n_pages = c.pool->size(0), c.H = c.pool->size(1), c.page = c.pool->size(2), c.max_pages = c.pages->size(1);
+  c.dv = c.pool->size(3) - dk;
+  if ((dk != 64 && dk != 128) || (c.dv != 64 && c.dv != 128))
+    fail(PyExc_ValueError, "%s: the pool's rows do not fit d_k = %lld", what, (long long)dk);
+  return c;
+}
+
+// (k, v, pool, pages, pos, cos, sin, q, interleaved, out, stream)
+PyObject* kv_append(PyObject* const* a) {
+  const char* what = "kv_append";
+  const at::Tensor &k = tensor(what, "k", a[0]), &v = tensor(what, "v", a[1]), &pos = tensor(what, "pos", a[4]);
+  int64_t strides[12] = {};
+  heads(what, "k", k, nullptr, nullptr, strides + 3);
+  const int64_t B = k.size(0), H = k.size(1), N = k.size(2), dk = k.size(3);
+  heads(what, "v", v, &k, nullptr, strides + 6);
+  const Pool c = pool_args(what, a[2], a[3], k, B, dk);
+  const int64_t vs[4] = {B, H, N, c.dv};
+  if (c.H != H || v.sizes() != at::IntArrayRef(vs, 4))
+    fail(PyExc_ValueError, "%s: k %s and v %s do not fit the pool (%lld heads, d_v = %lld)", what,
+         text(k.sizes()).c_str(), text(v.sizes()).c_str(), (long long)c.H, (long long)c.dv);
+  flat(what, "pos", pos, at::kInt, {B, N}, k.device());
+  const int dtype = code(what, k);
+  const float *cos = nullptr, *sin = nullptr;
+  int64_t rot = 0, n_pos = 0;
+  if (a[5] != Py_None || a[6] != Py_None) {
+    const at::Tensor &tc = tensor(what, "cos", a[5]), &ts = tensor(what, "sin", a[6]);
+    if (tc.dim() != 2) fail(PyExc_ValueError, "%s: cos must be [n_pos, d_rot / 2]", what);
+    flat(what, "cos", tc, at::kFloat, tc.sizes(), k.device());
+    flat(what, "sin", ts, at::kFloat, tc.sizes(), k.device());
+    cos = f32(tc), sin = f32(ts);
+    rot = 2 * tc.size(1), n_pos = tc.size(0);
+  }
+  const Place place(a[10], k.device());
+  at::Tensor o;
+  const at::Tensor* q = nullptr;
+  int64_t Hq = 0;
+  if (a[7] != Py_None) {
+    q = &tensor(what, "q", a[7]);
+    if (cos == nullptr) fail(PyExc_ValueError, "%s: q is only taken with cos and sin", what);
+    if (q->dim() == 4) Hq = q->size(1);
+    const int64_t qs[4] = {B, Hq, N, dk};
+    heads(what, "q", *q, &k, qs, strides);
+    o = a[9] == Py_None ? make(at::IntArrayRef(qs, 4), k.scalar_type(), k.device()) : tensor(what, "out", a[9]);
+    heads(what, "out", o, &k, qs, strides + 9);
+  } else if (a[9] != Py_None) {
+    fail(PyExc_ValueError, "%s: out is the rotated q, and there is no q", what);
+  }
+  check(moa_kv_append(q ? q->data_ptr() : nullptr, k.data_ptr(), v.data_ptr(), cos, sin, c.pool->data_ptr(), i32(*c.pages),
+                      i32(pos), q ? o.data_ptr() : nullptr, B, Hq, H, N, dk, c.dv, rot, n_pos, c.n_pages, c.page,
+                      c.max_pages, strides, truth(a[8]), dtype, place.raw()));
+  if (q != nullptr) return THPVariable_Wrap(o);
+  Py_RETURN_NONE;
+}
+
+// (q, pool, pages, lens, max_len, window, sinks, scale, causal, out, lse, workspace, stream); lse: None, or
+// a tensor, or True to make one.  Returns o or (o, lse).
+PyObject* kv_attn(PyObject* const* a) {
+  const bool with_lse = a[10] != Py_None;
+  const char* what = with_lse ? "kv_attn_lse" : "kv_attn";
+  const at::Tensor &q = tensor(what, "q", a[0]), &lens = tensor(what, "lens", a[3]);
+  int64_t strides[6];
+  heads(what, "q", q, nullptr, nullptr, strides);
+  const int64_t B = q.size(0), Hq = q.size(1), N = q.size(2), dk = q.size(3);
+  const Pool c = pool_args(what, a[1], a[2], q, B, dk);
+  flat(what, "lens", lens, at::kInt, {B}, q.device());
+  const int64_t max_len = a[4] == Py_None ? c.max_pages * c.page : integer(what, "max_len", a[4]);
+  const int64_t window = window_of(what, a[5]), sinks = integer(what, "sinks", a[6]);
+  const float scale = a[7] == Py_None ? float(1.0 / std::sqrt(double(dk))) : float(number(what, "scale", a[7]));
+  const int dtype = code(what, q);
+  const Place place(a[12], q.device());
+  at::Tensor o, lse;
+  row_outputs(what, a[9], a[10], q, c.dv, &o, &lse, strides + 3);
+  const Scratch ws(what, a[11], moa_kv_attn_workspace_bytes(B, Hq, c.H, N, dk, c.dv, max_len, window, sinks < 0 ? 0 : sinks, dtype),
+                   place);
+  check(moa_kv_attn(q.data_ptr(), c.pool->data_ptr(), i32(*c.pages), i32(lens), o.data_ptr(),
+                    with_lse ? static_cast<float*>(lse.data_ptr()) : nullptr, B, Hq, c.H, N, dk, c.dv, c.n_pages, c.page,
+                    c.max_pages, max_len, window, sinks, strides, scale, truth(a[8]), dtype, ws.p, ws.bytes, place.raw()));
+  return with_lse ? pair(o, lse) : THPVariable_Wrap(o);
+}
+
 // Runs an entry point on its positional arguments; no C++ exception leaves it.
 template <PyObject* (*F)(PyObject* const*), int ARGS>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -412,6 +614,10 @@ PyMethodDef g_methods[] = {method<qk_norm_rope, 11>("qk_norm_rope"),
                            method<kv4_write, 6>("kv4_write"),
                            method<kv4_read, 7>("kv4_read"),
                            method<kv4_attn, 11>("kv4_attn"),
+                           method<window_attn, 10>("window_attn"),
+                           method<window_attn_bwd, 12>("window_attn_bwd"),
+                           method<kv_append, 11>("kv_append"),
+                           method<kv_attn, 13>("kv_attn"),
                            {"set_error", set_error, METH_O, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "moa_torch", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,493 @@
+// Gradients of causal attention with a sliding window and first tokens that stay visible, on CUDA cores
+// (sm_103a): for fp32, and for bf16 tensors whose strides no tensor map can describe.
+//
+// Mathematics, with P_ij = exp(scale <q_i, k_j> - LSE_i) for the tokens j that row i sees (window.cuh), 0 for
+// the others, and D_i = <dO_i, O_i>:
+//     dV_j = sum_i P_ij dO_i,   dS_ij = P_ij (<dO_i, v_j> - D_i),
+//     dQ_i = scale sum_j dS_ij k_j,   dK_j = scale sum_i dS_ij q_i,
+// the sums over i also over the query heads that share the key head.  The weights are rebuilt from the
+// scores; nothing of N_q x N_k size is stored.
+//
+//   delta   D of every row and the row's -LSE log2 e (-infinity for rows that see nothing: their weights
+//           are then zero), a warp a row;
+//   dkdv    a CTA for 64 tokens of a key head and a piece of the rows that see them, 32 rows at a time.  A
+//           token's rows are those of its window; a sink's are all later ones, so tokens among the sinks
+//           (or all of them, without a window) have their rows cut into pieces of at most a window's length;
+//   join    adds the pieces, in order;
+//   dq      a CTA for 64 rows, 32 tokens at a time.
+// Rows of a key head are counted position by position (row r: position r / G, head r % G of the group).
+// No atomics: results do not depend on the order in which CTAs run.
+//
+// What bounds it: fused multiply-adds.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <cstdio>
+
+#include "internal.h"
+#include "ops_internal.h"
+#include "window.cuh"
+
+namespace moa {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kKeysKv = 64, kRowsKv = 32;   // dkdv: tokens of a CTA, rows of a step
+constexpr int kRowsQ = 64, kKeysQ = 32;     // dq: rows of a CTA, tokens of a step
+constexpr int kThreads = 256;
+
+struct Params {
+  View q, k, v, o, go, dq, dk, dv;
+  const float* lse;
+  float* nl;      // [B * Hk][N * G] -LSE log2 e, rows of a key head in their order
+  float* delta;   // alike
+  float* part;    // [piece item][64][DK + DV], null: no pieces
+  int64_t Hk;
+  int N, G, Nk;
+  win::Mask mask;
+  float c_log2, scale;
+  int n_kt;       // tiles of tokens
+  int cut;        // the first `cut` of them are cut into `pieces` pieces of `piece_rows` rows
+  int pieces;
+  int64_t piece_rows;
+};
+
+template <typename T>
+__device__ __forceinline__ float4 load4(const T* p);
+template <>
+__device__ __forceinline__ float4 load4(const float* p) {
+  return *reinterpret_cast<const float4*>(p);
+}
+template <>
+__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
+  const uint2 x = *reinterpret_cast<const uint2*>(p);
+  return make_float4(__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xffff0000u), __uint_as_float(x.y << 16),
+                     __uint_as_float(x.y & 0xffff0000u));
+}
+__device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
+__device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v) {
+  __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+  *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<uint32_t*>(&a), *reinterpret_cast<uint32_t*>(&b));
+}
+__device__ __forceinline__ float dot4(float4 a, float4 b, float s) {
+  s = fmaf(a.x, b.x, s);
+  s = fmaf(a.y, b.y, s);
+  s = fmaf(a.z, b.z, s);
+  return fmaf(a.w, b.w, s);
+}
+__device__ __forceinline__ void axpy4(float w, float4 v, float* acc) {
+  acc[0] = fmaf(w, v.x, acc[0]);
+  acc[1] = fmaf(w, v.y, acc[1]);
+  acc[2] = fmaf(w, v.z, acc[2]);
+  acc[3] = fmaf(w, v.w, acc[3]);
+}
+
+template <typename T>
+__device__ __forceinline__ const T* row_of(const View& x, int64_t b, int64_t h, int64_t n) {
+  return static_cast<const T*>(x.p) + b * x.sb + h * x.sh + n * x.sn;
+}
+
+template <typename T, int DV>
+__global__ void __launch_bounds__(kThreads)
+window_delta_kernel(Params p, int64_t rows) {
+  wait_for_previous();
+  const int lane = threadIdx.x & 31;
+  const int64_t r = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5);
+  if (r >= rows) return;
+  const int64_t per = int64_t(p.N) * p.G, bh = r / per, b = bh / p.Hk, h = bh - b * p.Hk;
+  const int64_t at = r - bh * per, i = at / p.G, g = at - i * p.G, hq = h * p.G + g;
+  float s = 0.f;
+  if (lane * 4 < DV) s = dot4(load4(row_of<T>(p.o, b, hq, i) + lane * 4), load4(row_of<T>(p.go, b, hq, i) + lane * 4), 0.f);
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+  if (lane == 0) {
+    const float l = p.lse[(b * p.Hk * p.G + hq) * p.N + i];
+    p.delta[r] = s;
+    p.nl[r] = l == -INFINITY ? -INFINITY : -l * kLog2e;
+  }
+}
+
+// Rows of X (and Y) of a key head from row r0 on into shared memory, in fp32; rows past `rows` are zero.
+template <typename T, int DX, int DY, int ROWS>
+__device__ __forceinline__ void load_rows(const View& x, const View& y, float* sx, float* sy, int64_t b, int64_t h, int G,
+                                          int64_t r0, int64_t rows) {
+  for (int e = threadIdx.x; e < ROWS * ((DX + DY) / 4); e += kThreads) {
+    const int r = e / ((DX + DY) / 4), c = e % ((DX + DY) / 4) * 4;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (r0 + r < rows) {
+      const int64_t i = (r0 + r) / G, hq = h * G + (r0 + r - i * G);
+      v = c < DX ? load4(row_of<T>(x, b, hq, i) + c) : load4(row_of<T>(y, b, hq, i) + (c - DX));
+    }
+    *reinterpret_cast<float4*>(c < DX ? sx + r * (DX + 4) + c : sy + r * (DY + 4) + (c - DX)) = v;
+  }
+}
+
+template <int DK, int DV>
+struct KvSmem {
+  static constexpr int kLdW = kKeysKv + 4;
+  static constexpr int kFloats = (kKeysKv + kRowsKv) * (DK + 4 + DV + 4) + 2 * kRowsKv * kLdW;
+};
+
+template <typename T, int DK, int DV>
+__global__ void __launch_bounds__(kThreads)
+window_dkdv_cc_kernel(Params p) {
+  constexpr int kLdW = KvSmem<DK, DV>::kLdW;
+  extern __shared__ float smem[];
+  float* sK = smem;
+  float* sV = sK + kKeysKv * (DK + 4);
+  float* sQ = sV + kKeysKv * (DV + 4);
+  float* sG = sQ + kRowsKv * (DK + 4);
+  float* sP = sG + kRowsKv * (DV + 4);   // [rows][tokens]
+  float* sS = sP + kRowsKv * kLdW;
+  wait_for_previous();
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  // items of a key head: the pieces of its first `cut` tiles, then the other tiles
+  const int per = p.cut * p.pieces + p.n_kt - p.cut;
+  const int64_t bh = int64_t(blockIdx.x) / per, b = bh / p.Hk, h = bh - b * p.Hk;
+  const int item = int(int64_t(blockIdx.x) - bh * per);
+  const bool whole = item >= p.cut * p.pieces;
+  const int kt = whole ? item - p.cut * p.pieces + p.cut : item / p.pieces, piece = whole ? 0 : item - kt * p.pieces;
+  const int k0 = kt * kKeysKv, off = p.Nk - p.N;   // row i's position: i + off
+  const int keys = p.Nk - k0 < kKeysKv ? p.Nk - k0 : kKeysKv;
+  const int64_t rows = int64_t(p.N) * p.G;
+  // rows that see a token of the tile: from position k0 to the last one's window, or to the end
+  const int64_t i0 = k0 > off ? int64_t(k0) - off : 0;
+  int64_t i1 = p.N;
+  if (k0 >= p.mask.sinks && p.mask.window != win::kNoWindow) {
+    const int64_t n = int64_t(k0) + keys - 1 + p.mask.window - off;
+    i1 = n < 0 ? 0 : n < i1 ? n : i1;
+  }
+  int64_t ra = i0 * p.G, rz = i1 * p.G;
+  if (!whole) {
+    ra += piece * p.piece_rows;
+    if (ra + p.piece_rows < rz) rz = ra + p.piece_rows;
+  }
+
+  for (int e = threadIdx.x; e < kKeysKv * ((DK + DV) / 4); e += kThreads) {
+    const int j = e / ((DK + DV) / 4), c = e % ((DK + DV) / 4) * 4;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (j < keys) x = c < DK ? load4(row_of<T>(p.k, b, h, k0 + j) + c) : load4(row_of<T>(p.v, b, h, k0 + j) + (c - DK));
+    *reinterpret_cast<float4*>(c < DK ? sK + j * (DK + 4) + c : sV + j * (DV + 4) + (c - DK)) = x;
+  }
+  float dv[4][DV / 16], dk[4][DK / 16];   // tokens 4 ty + a, features 64 c + 4 tx + e
+#pragma unroll
+  for (int a = 0; a < 4; ++a) {
+#pragma unroll
+    for (int c = 0; c < DV / 16; ++c) dv[a][c] = 0.f;
+#pragma unroll
+    for (int c = 0; c < DK / 16; ++c) dk[a][c] = 0.f;
+  }
+  for (int64_t r0 = ra; r0 < rz; r0 += kRowsKv) {
+    __syncthreads();
+    load_rows<T, DK, DV, kRowsKv>(p.q, p.go, sQ, sG, b, h, p.G, r0, rz);
+    __syncthreads();
+    // rows tx, tx + 16 against tokens 4 ty + a
+    float s[4][2], e[4][2];
+#pragma unroll
+    for (int a = 0; a < 4; ++a) s[a][0] = s[a][1] = e[a][0] = e[a][1] = 0.f;
+#pragma unroll 4
+    for (int c = 0; c < DK; c += 4) {
+      const float4 q0 = *reinterpret_cast<const float4*>(sQ + tx * (DK + 4) + c);
+      const float4 q1 = *reinterpret_cast<const float4*>(sQ + (tx + 16) * (DK + 4) + c);
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const float4 kk = *reinterpret_cast<const float4*>(sK + (4 * ty + a) * (DK + 4) + c);
+        s[a][0] = dot4(q0, kk, s[a][0]);
+        s[a][1] = dot4(q1, kk, s[a][1]);
+      }
+    }
+#pragma unroll 4
+    for (int c = 0; c < DV; c += 4) {
+      const float4 g0 = *reinterpret_cast<const float4*>(sG + tx * (DV + 4) + c);
+      const float4 g1 = *reinterpret_cast<const float4*>(sG + (tx + 16) * (DV + 4) + c);
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const float4 vv = *reinterpret_cast<const float4*>(sV + (4 * ty + a) * (DV + 4) + c);
+        e[a][0] = dot4(g0, vv, e[a][0]);
+        e[a][1] = dot4(g1, vv, e[a][1]);
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int64_t r = r0 + tx + 16 * x;
+      const bool live = r < rz;
+      const int pos = int((live ? r : rz - 1) / p.G) + off;
+      const float nl = live ? p.nl[bh * rows + r] : -INFINITY, d = live ? p.delta[bh * rows + r] : 0.f;
+      float4 wp, ws;
+      float* fp = reinterpret_cast<float*>(&wp);
+      float* fs = reinterpret_cast<float*>(&ws);
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const int j = k0 + 4 * ty + a;
+        const bool seen = live && j <= pos && (pos - j < p.mask.window || j < p.mask.sinks) && j < p.Nk;
+        fp[a] = seen ? exp2f(fmaf(s[a][x], p.c_log2, nl)) : 0.f;
+        fs[a] = seen ? fp[a] * (e[a][x] - d) : 0.f;
+      }
+      *reinterpret_cast<float4*>(sP + (tx + 16 * x) * kLdW + 4 * ty) = wp;
+      *reinterpret_cast<float4*>(sS + (tx + 16 * x) * kLdW + 4 * ty) = ws;
+    }
+    __syncwarp();   // tokens 4 ty .. of all rows: written and read by the same half warp
+#pragma unroll 2
+    for (int r = 0; r < kRowsKv; ++r) {
+      const float4 wp = *reinterpret_cast<const float4*>(sP + r * kLdW + 4 * ty);
+      const float4 ws = *reinterpret_cast<const float4*>(sS + r * kLdW + 4 * ty);
+#pragma unroll
+      for (int c = 0; c < DV / 64; ++c) {
+        const float4 g = *reinterpret_cast<const float4*>(sG + r * (DV + 4) + 64 * c + 4 * tx);
+        axpy4(wp.x, g, dv[0] + 4 * c);
+        axpy4(wp.y, g, dv[1] + 4 * c);
+        axpy4(wp.z, g, dv[2] + 4 * c);
+        axpy4(wp.w, g, dv[3] + 4 * c);
+      }
+#pragma unroll
+      for (int c = 0; c < DK / 64; ++c) {
+        const float4 q = *reinterpret_cast<const float4*>(sQ + r * (DK + 4) + 64 * c + 4 * tx);
+        axpy4(ws.x, q, dk[0] + 4 * c);
+        axpy4(ws.y, q, dk[1] + 4 * c);
+        axpy4(ws.z, q, dk[2] + 4 * c);
+        axpy4(ws.w, q, dk[3] + 4 * c);
+      }
+    }
+  }
+#pragma unroll
+  for (int a = 0; a < 4; ++a) {
+    const int j = 4 * ty + a;
+    if (j >= keys) continue;
+    if (!whole) {
+      float* dst = p.part + (((bh * p.cut + kt) * p.pieces + piece) * kKeysKv + j) * (DK + DV);
+#pragma unroll
+      for (int c = 0; c < DK / 64; ++c)
+        store4(dst + 64 * c + 4 * tx, make_float4(dk[a][4 * c], dk[a][4 * c + 1], dk[a][4 * c + 2], dk[a][4 * c + 3]));
+#pragma unroll
+      for (int c = 0; c < DV / 64; ++c)
+        store4(dst + DK + 64 * c + 4 * tx, make_float4(dv[a][4 * c], dv[a][4 * c + 1], dv[a][4 * c + 2], dv[a][4 * c + 3]));
+      continue;
+    }
+    T* ok = const_cast<T*>(row_of<T>(p.dk, b, h, k0 + j));
+    T* ov = const_cast<T*>(row_of<T>(p.dv, b, h, k0 + j));
+#pragma unroll
+    for (int c = 0; c < DK / 64; ++c)
+      store4(ok + 64 * c + 4 * tx, make_float4(dk[a][4 * c] * p.scale, dk[a][4 * c + 1] * p.scale, dk[a][4 * c + 2] * p.scale,
+                                               dk[a][4 * c + 3] * p.scale));
+#pragma unroll
+    for (int c = 0; c < DV / 64; ++c)
+      store4(ov + 64 * c + 4 * tx, make_float4(dv[a][4 * c], dv[a][4 * c + 1], dv[a][4 * c + 2], dv[a][4 * c + 3]));
+  }
+}
+
+// Adds the pieces of cut tiles: four features of a token a thread.
+template <typename T, int DK, int DV>
+__global__ void __launch_bounds__(kThreads)
+window_dkdv_join_kernel(Params p, int64_t n) {
+  wait_for_previous();
+  constexpr int kQuads = (DK + DV) / 4;
+  const int64_t x = int64_t(blockIdx.x) * kThreads + threadIdx.x;
+  if (x >= n) return;
+  const int64_t row = x / kQuads, c = (x - row * kQuads) * 4;        // row: (key head, tile, token)
+  const int64_t tile = row / kKeysKv, j = row - tile * kKeysKv;
+  const int64_t bh = tile / p.cut, kt = tile - bh * p.cut, b = bh / p.Hk, h = bh - b * p.Hk;
+  if (kt * kKeysKv + j >= p.Nk) return;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i = 0; i < p.pieces; ++i) {
+    const float4 v = load4(p.part + ((tile * p.pieces + i) * kKeysKv + j) * (DK + DV) + c);
+    s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+  }
+  if (c < DK)
+    store4(const_cast<T*>(row_of<T>(p.dk, b, h, kt * kKeysKv + j)) + c,
+           make_float4(s.x * p.scale, s.y * p.scale, s.z * p.scale, s.w * p.scale));
+  else
+    store4(const_cast<T*>(row_of<T>(p.dv, b, h, kt * kKeysKv + j)) + (c - DK), s);
+}
+
+template <int DK, int DV>
+struct QSmem {
+  static constexpr int kLdW = kRowsQ + 4;
+  static constexpr int kFloats = (kRowsQ + kKeysQ) * (DK + 4 + DV + 4) + kKeysQ * kLdW;
+};
+
+template <typename T, int DK, int DV>
+__global__ void __launch_bounds__(kThreads)
+window_dq_cc_kernel(Params p, int n_rt) {
+  constexpr int kLdW = QSmem<DK, DV>::kLdW;
+  extern __shared__ float smem[];
+  float* sQ = smem;
+  float* sG = sQ + kRowsQ * (DK + 4);
+  float* sK = sG + kRowsQ * (DV + 4);
+  float* sV = sK + kKeysQ * (DK + 4);
+  float* sS = sV + kKeysQ * (DV + 4);   // [tokens][rows]
+  wait_for_previous();
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const int64_t bh = int64_t(blockIdx.x) / n_rt, b = bh / p.Hk, h = bh - b * p.Hk;
+  const int64_t rows = int64_t(p.N) * p.G, r0 = (int64_t(blockIdx.x) - bh * n_rt) * kRowsQ;
+  const int live = int(rows - r0 < kRowsQ ? rows - r0 : kRowsQ);
+  const int off = p.Nk - p.N;
+  const int i0 = int(r0 / p.G), i1 = int((r0 + live - 1) / p.G);
+  const win::Tiles list = win::tiles_of(p.mask, p.Nk, p.N, i0, i1, kKeysQ);
+  load_rows<T, DK, DV, kRowsQ>(p.q, p.go, sQ, sG, b, h, p.G, r0, rows);
+  float nl[4], d[4], dq[4][DK / 16];
+  int pos[4];
+#pragma unroll
+  for (int a = 0; a < 4; ++a) {
+    const int64_t r = r0 + 4 * ty + a;
+    const bool in = r < rows;
+    nl[a] = in ? p.nl[bh * rows + r] : -INFINITY;
+    d[a] = in ? p.delta[bh * rows + r] : 0.f;
+    pos[a] = in ? int(r / p.G) + off : -1;   // sees nothing
+#pragma unroll
+    for (int c = 0; c < DK / 16; ++c) dq[a][c] = 0.f;
+  }
+  for (int t = 0; t < list.n; ++t) {
+    const int n0 = list.at(t) * kKeysQ;
+    __syncthreads();
+    for (int e = threadIdx.x; e < kKeysQ * ((DK + DV) / 4); e += kThreads) {
+      const int j = e / ((DK + DV) / 4), c = e % ((DK + DV) / 4) * 4;
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (n0 + j < p.Nk) x = c < DK ? load4(row_of<T>(p.k, b, h, n0 + j) + c) : load4(row_of<T>(p.v, b, h, n0 + j) + (c - DK));
+      *reinterpret_cast<float4*>(c < DK ? sK + j * (DK + 4) + c : sV + j * (DV + 4) + (c - DK)) = x;
+    }
+    __syncthreads();
+    // tokens tx, tx + 16 against rows 4 ty + a
+    float s[4][2], e[4][2];
+#pragma unroll
+    for (int a = 0; a < 4; ++a) s[a][0] = s[a][1] = e[a][0] = e[a][1] = 0.f;
+#pragma unroll 4
+    for (int c = 0; c < DK; c += 4) {
+      const float4 k0 = *reinterpret_cast<const float4*>(sK + tx * (DK + 4) + c);
+      const float4 k1 = *reinterpret_cast<const float4*>(sK + (tx + 16) * (DK + 4) + c);
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const float4 q = *reinterpret_cast<const float4*>(sQ + (4 * ty + a) * (DK + 4) + c);
+        s[a][0] = dot4(q, k0, s[a][0]);
+        s[a][1] = dot4(q, k1, s[a][1]);
+      }
+    }
+#pragma unroll 4
+    for (int c = 0; c < DV; c += 4) {
+      const float4 v0 = *reinterpret_cast<const float4*>(sV + tx * (DV + 4) + c);
+      const float4 v1 = *reinterpret_cast<const float4*>(sV + (tx + 16) * (DV + 4) + c);
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const float4 g = *reinterpret_cast<const float4*>(sG + (4 * ty + a) * (DV + 4) + c);
+        e[a][0] = dot4(g, v0, e[a][0]);
+        e[a][1] = dot4(g, v1, e[a][1]);
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int j = n0 + tx + 16 * x;
+      float4 ws;
+      float* fs = reinterpret_cast<float*>(&ws);
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const bool seen = j <= pos[a] && (pos[a] - j < p.mask.window || j < p.mask.sinks);
+        fs[a] = seen ? exp2f(fmaf(s[a][x], p.c_log2, nl[a])) * (e[a][x] - d[a]) : 0.f;
+      }
+      *reinterpret_cast<float4*>(sS + (tx + 16 * x) * kLdW + 4 * ty) = ws;
+    }
+    __syncwarp();
+#pragma unroll 4
+    for (int j = 0; j < kKeysQ; ++j) {
+      const float4 ws = *reinterpret_cast<const float4*>(sS + j * kLdW + 4 * ty);
+#pragma unroll
+      for (int c = 0; c < DK / 64; ++c) {
+        const float4 k = *reinterpret_cast<const float4*>(sK + j * (DK + 4) + 64 * c + 4 * tx);
+        axpy4(ws.x, k, dq[0] + 4 * c);
+        axpy4(ws.y, k, dq[1] + 4 * c);
+        axpy4(ws.z, k, dq[2] + 4 * c);
+        axpy4(ws.w, k, dq[3] + 4 * c);
+      }
+    }
+  }
+#pragma unroll
+  for (int a = 0; a < 4; ++a) {
+    const int64_t r = r0 + 4 * ty + a;
+    if (r >= rows) continue;
+    const int64_t i = r / p.G, hq = h * p.G + (r - i * p.G);
+    T* dst = const_cast<T*>(row_of<T>(p.dq, b, hq, i));
+#pragma unroll
+    for (int c = 0; c < DK / 64; ++c)
+      store4(dst + 64 * c + 4 * tx, make_float4(dq[a][4 * c] * p.scale, dq[a][4 * c + 1] * p.scale, dq[a][4 * c + 2] * p.scale,
+                                                dq[a][4 * c + 3] * p.scale));
+  }
+}
+
+// How the rows of tokens among the sinks (or of all tokens, without a window) are cut: pieces of a window's
+// length, or of an eighth of all rows without one, in whole steps.
+struct Cut {
+  int64_t n_kt, cut, pieces, piece_rows;
+};
+Cut cut_of(const WindowBwdArgs& a) {
+  const int64_t G = a.Hq / a.Hk, rows = a.Nq * G;
+  Cut c;
+  c.n_kt = (a.Nk + kKeysKv - 1) / kKeysKv;
+  const bool windowed = a.window != win::kNoWindow;
+  int64_t want = windowed ? (int64_t(a.window) + kKeysKv) * G : (rows + 7) / 8;
+  if (want < 512) want = 512;
+  if (want > rows) want = rows;
+  c.piece_rows = (want + kRowsKv - 1) / kRowsKv * kRowsKv;
+  c.pieces = (rows + c.piece_rows - 1) / c.piece_rows;
+  c.cut = windowed ? (int64_t(a.sinks) + kKeysKv - 1) / kKeysKv : c.n_kt;
+  if (c.cut > c.n_kt) c.cut = c.n_kt;
+  if (c.pieces == 1) c.cut = 0;
+  return c;
+}
+
+// The workspace: -LSE log2 e and D of every row, then the pieces.
+int64_t rows_bytes(const WindowBwdArgs& a) { return (a.B * a.Hq * a.Nq * 4 + 255) / 256 * 256; }
+
+template <typename T, int DK, int DV>
+int launch(const WindowBwdArgs& a, char* msg, size_t msglen) {
+  const Cut cut = cut_of(a);
+  const int64_t bh = a.B * a.Hk, G = a.Hq / a.Hk, rows = a.B * a.Hq * a.Nq;
+  uint8_t* ws = static_cast<uint8_t*>(a.ws);
+  Params p{};
+  p.q = a.q, p.k = a.k, p.v = a.v, p.o = a.o, p.go = a.go, p.dq = a.dq, p.dk = a.dk_, p.dv = a.dv_;
+  p.lse = a.lse;
+  p.nl = reinterpret_cast<float*>(ws);
+  p.delta = reinterpret_cast<float*>(ws + rows_bytes(a));
+  p.part = reinterpret_cast<float*>(ws + 2 * rows_bytes(a));
+  p.Hk = a.Hk, p.N = int(a.Nq), p.G = int(G), p.Nk = int(a.Nk);
+  p.mask = win::Mask{a.window, a.sinks, true};
+  p.c_log2 = a.scale * kLog2e, p.scale = a.scale;
+  p.n_kt = int(cut.n_kt), p.cut = int(cut.cut), p.pieces = int(cut.pieces), p.piece_rows = cut.piece_rows;
+  const int kv_smem = KvSmem<DK, DV>::kFloats * 4, q_smem = QSmem<DK, DV>::kFloats * 4;
+  auto kv = window_dkdv_cc_kernel<T, DK, DV>;
+  auto dq = window_dq_cc_kernel<T, DK, DV>;
+  cudaError_t e = ensure_smem_limit(reinterpret_cast<const void*>(kv), kv_smem);
+  if (e == cudaSuccess) e = ensure_smem_limit(reinterpret_cast<const void*>(dq), q_smem);
+  if (e == cudaSuccess)
+    e = launch_overlapped(window_delta_kernel<T, DV>, dim3(unsigned((rows + 7) / 8)), dim3(kThreads), 0, a.stream, p, rows);
+  const int64_t items = bh * (cut.cut * cut.pieces + cut.n_kt - cut.cut);
+  if (e == cudaSuccess) e = launch_overlapped(kv, dim3(unsigned(items)), dim3(kThreads), size_t(kv_smem), a.stream, p);
+  const int64_t joined = bh * cut.cut * kKeysKv * ((DK + DV) / 4);
+  if (e == cudaSuccess && joined > 0)
+    e = launch_overlapped(window_dkdv_join_kernel<T, DK, DV>, dim3(unsigned((joined + kThreads - 1) / kThreads)), dim3(kThreads),
+                          0, a.stream, p, joined);
+  const int64_t n_rt = (a.Nq * G + kRowsQ - 1) / kRowsQ;
+  if (e == cudaSuccess)
+    e = launch_overlapped(dq, dim3(unsigned(bh * n_rt)), dim3(kThreads), size_t(q_smem), a.stream, p, int(n_rt));
+  if (e != cudaSuccess) {
+    snprintf(msg, msglen, "gradients of attention with a window: %s", cudaGetErrorString(e));
+    return 5;
+  }
+  return 0;
+}
+
+template <typename T>
+int launch_sizes(const WindowBwdArgs& a, char* msg, size_t msglen) {
+  if (a.dk == 64) return a.dv == 64 ? launch<T, 64, 64>(a, msg, msglen) : launch<T, 64, 128>(a, msg, msglen);
+  return a.dv == 64 ? launch<T, 128, 64>(a, msg, msglen) : launch<T, 128, 128>(a, msg, msglen);
+}
+
+}  // namespace
+
+size_t window_bwd_cc_workspace(const WindowBwdArgs& a) {
+  const Cut c = cut_of(a);
+  return size_t(2 * rows_bytes(a) + a.B * a.Hk * c.cut * c.pieces * kKeysKv * (a.dk + a.dv) * 4);
+}
+
+int launch_window_bwd_cc(const WindowBwdArgs& a, char* msg, size_t msglen) {
+  return a.f32 ? launch_sizes<float>(a, msg, msglen) : launch_sizes<__nv_bfloat16>(a, msg, msglen);
+}
+
+}  // namespace moa

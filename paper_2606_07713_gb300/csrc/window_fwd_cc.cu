@@ -1,0 +1,378 @@
+// Causal attention with a sliding window and first tokens that stay visible, on CUDA cores (sm_103a):
+// for fp32, and for bf16 tensors whose strides no tensor map can describe.  Keys and values lie in
+// dense tensors or in the pages of a cache.
+//
+// Mathematics: o_i = sum_j p_ij v_j / l_i over the tokens j that row i sees (window.cuh), with
+// p_ij = 2^(c s_ij - m_i), s_ij = <q_i, k_j>, c = scale log2 e, m_i the running maximum of c s_ij and
+// l_i = sum_j p_ij: one pass over the tokens, the sums rescaled when a tile raises the maximum.
+//
+// A key head's query rows are counted position by position: row r is query r / G of head r % G of the
+// group, so that a tile of rows covers few positions and a window few tiles of tokens.  A CTA takes one
+// tile of rows (64, or 16 where there are few) and a share of the 64-token tiles that it visits; shares
+// are joined by a second kernel.  Thread (ty, tx) holds RM rows: the scores of four tokens of each,
+// then DV / 16 features of their outputs.
+//
+// What bounds it: fused multiply-adds, one for each shared-memory word of a row's and a token's
+// features pair at RM = 4.
+//
+// Hidden tokens get the weight -1, which the second product skips: what their values hold (not numbers,
+// perhaps) then reaches no row that does not see them.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <cstdio>
+
+#include "internal.h"
+#include "ops_internal.h"
+#include "window.cuh"
+
+namespace moa {
+
+__device__ unsigned int g_moa_window_cc_status = 0;
+
+namespace {
+
+constexpr int kKeys = 64;            // tokens of a tile
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct Params {
+  View q, o;
+  KvSource kv;
+  float* lse;
+  const int32_t* lens;
+  int64_t Hk;
+  int N, G, max_len, n_tiles;   // n_tiles: row tiles of a key head
+  win::Mask mask;
+  float c_log2;
+  int splits;
+  float* part_o;                // [item * splits + split][rows][DV], null: no shares
+  float2* part_ml;
+};
+
+template <typename T>
+__device__ __forceinline__ float4 load4(const T* p);
+template <>
+__device__ __forceinline__ float4 load4(const float* p) {
+  return *reinterpret_cast<const float4*>(p);
+}
+template <>
+__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
+  const uint2 x = *reinterpret_cast<const uint2*>(p);
+  return make_float4(__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xffff0000u), __uint_as_float(x.y << 16),
+                     __uint_as_float(x.y & 0xffff0000u));
+}
+__device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
+__device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v) {
+  __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+  *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<uint32_t*>(&a), *reinterpret_cast<uint32_t*>(&b));
+}
+
+__device__ __forceinline__ int length_of(const Params& p, int64_t b) {
+  if (p.lens == nullptr) return p.max_len;
+  const int len = p.lens[b];
+  if (len >= 0 && len <= p.max_len) return len;
+  atomicExch(&g_moa_window_cc_status, win::kErrIndex);
+  return len < 0 ? 0 : p.max_len;
+}
+
+template <int DK, int DV, int RM, int NT>
+struct Cfg {
+  static constexpr int kRows = NT / 16 * RM;
+  // rows of 16-byte groups, one group longer: neighbouring rows then start in different banks
+  static constexpr int kLdQ = DK + 4, kLdK = DK + 4, kLdP = kRows + 4;
+  static constexpr int kFloats = kRows * kLdQ + kKeys * kLdK + kKeys * DV + kKeys * kLdP;
+  static constexpr int kSmem = kFloats * 4;
+};
+
+template <typename T, int DK, int DV, int RM, int NT>
+__global__ void __launch_bounds__(NT)
+window_cc_kernel(Params p) {
+  using C = Cfg<DK, DV, RM, NT>;
+  extern __shared__ float smem[];
+  float* sQ = smem;                        // [rows][DK]
+  float* sK = sQ + C::kRows * C::kLdQ;     // [tokens][DK]
+  float* sV = sK + kKeys * C::kLdK;        // [tokens][DV]
+  float* sP = sV + kKeys * DV;             // [tokens][rows]
+  wait_for_previous();
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const int64_t item = blockIdx.x, bh = item / p.n_tiles;
+  const int tile = int(item - bh * p.n_tiles);
+  const int64_t b = bh / p.Hk, h = bh - b * p.Hk;
+  const int64_t rows_all = int64_t(p.N) * p.G, r0 = int64_t(tile) * C::kRows;
+  const int rows = int(rows_all - r0 < C::kRows ? rows_all - r0 : C::kRows);
+  const int len = length_of(p, b);
+  const int i0 = int(r0 / p.G), i1 = int((r0 + rows - 1) / p.G);
+  const win::Tiles list = win::tiles_of(p.mask, len, p.N, i0, i1, kKeys);
+  const int first = int(int64_t(list.n) * blockIdx.y / p.splits), last = int(int64_t(list.n) * (blockIdx.y + 1) / p.splits);
+
+  const T* Q = static_cast<const T*>(p.q.p) + b * p.q.sb + h * p.G * p.q.sh;
+  for (int x = threadIdx.x; x < C::kRows * (DK / 4); x += NT) {
+    const int r = x / (DK / 4), c = x % (DK / 4) * 4;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (r < rows) {
+      const int64_t i = (r0 + r) / p.G, g = r0 + r - i * p.G;
+      v = load4(Q + g * p.q.sh + i * p.q.sn + c);
+    }
+    *reinterpret_cast<float4*>(sQ + r * C::kLdQ + c) = v;
+  }
+  int end[RM], low[RM];
+#pragma unroll
+  for (int a = 0; a < RM; ++a) {
+    const int r = ty * RM + a;
+    const int i = int((r0 + (r < rows ? r : rows - 1)) / p.G);
+    end[a] = r < rows ? win::row_end(p.mask, len, p.N, i) : 0;
+    low[a] = win::row_low(p.mask, len, p.N, i);
+  }
+  float m[RM], l[RM], acc[RM][DV / 16];
+#pragma unroll
+  for (int a = 0; a < RM; ++a) {
+    m[a] = -INFINITY, l[a] = 0.f;
+#pragma unroll
+    for (int c = 0; c < DV / 16; ++c) acc[a][c] = 0.f;
+  }
+  const int32_t* table = p.kv.table + b * p.kv.max_pages;
+  // the first token that any row sees by its window: between the sinks and it nothing is read
+  const int low0 = win::row_low(p.mask, len, p.N, i0), end1 = win::row_end(p.mask, len, p.N, i1);
+  for (int t = first; t < last; ++t) {
+    const int n0 = list.at(t) * kKeys;
+    __syncthreads();
+    constexpr int kQuads = (DK + DV) / 4;
+    for (int x = threadIdx.x; x < kKeys * kQuads; x += NT) {
+      const int j = x / kQuads, c = x % kQuads * 4, n = n0 + j;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (n < end1 && (n >= low0 || n < p.mask.sinks)) {
+        int64_t at = b, place = n;
+        bool there = true;
+        if (p.kv.table != nullptr) {
+          const int slot = n / p.kv.page;
+          at = table[slot];
+          place = n - slot * p.kv.page;
+          there = at >= 0 && at < p.kv.n_pages;
+          if (!there) atomicExch(&g_moa_window_cc_status, win::kErrIndex);
+        }
+        if (there)
+          v = c < DK ? load4(static_cast<const T*>(p.kv.k) + at * p.kv.k_sb + h * p.kv.k_sh + place * p.kv.k_sn + c)
+                     : load4(static_cast<const T*>(p.kv.v) + at * p.kv.v_sb + h * p.kv.v_sh + place * p.kv.v_sn + (c - DK));
+      }
+      float* dst = c < DK ? sK + j * C::kLdK + c : sV + j * DV + (c - DK);
+      *reinterpret_cast<float4*>(dst) = v;
+    }
+    __syncthreads();
+    // scores of tokens tx, tx + 16, ... : a quarter warp's rows of sK then lie in all banks
+    float s[RM][4];
+#pragma unroll
+    for (int a = 0; a < RM; ++a)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) s[a][k] = 0.f;
+#pragma unroll 4
+    for (int c = 0; c < DK; c += 4) {
+      float4 q[RM], kk[4];
+#pragma unroll
+      for (int a = 0; a < RM; ++a) q[a] = *reinterpret_cast<const float4*>(sQ + (ty * RM + a) * C::kLdQ + c);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) kk[k] = *reinterpret_cast<const float4*>(sK + (tx + 16 * k) * C::kLdK + c);
+#pragma unroll
+      for (int a = 0; a < RM; ++a)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          s[a][k] = fmaf(q[a].x, kk[k].x, s[a][k]);
+          s[a][k] = fmaf(q[a].y, kk[k].y, s[a][k]);
+          s[a][k] = fmaf(q[a].z, kk[k].z, s[a][k]);
+          s[a][k] = fmaf(q[a].w, kk[k].w, s[a][k]);
+        }
+    }
+    float w[RM][4];
+#pragma unroll
+    for (int a = 0; a < RM; ++a) {
+      bool seen[4];
+      float top = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int n = n0 + tx + 16 * k;
+        seen[k] = n < end[a] && (n >= low[a] || n < p.mask.sinks);
+        w[a][k] = s[a][k] * p.c_log2;
+        if (seen[k]) top = fmaxf(top, w[a][k]);
+      }
+#pragma unroll
+      for (int d = 8; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+      const float m_new = fmaxf(m[a], top), base = m_new == -INFINITY ? 0.f : m_new;
+      const float alpha = exp2f(m[a] - base);   // 0 before the first token
+      float sum = 0.f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        w[a][k] = seen[k] ? exp2f(w[a][k] - base) : -1.f;
+        if (seen[k]) sum += w[a][k];
+      }
+#pragma unroll
+      for (int d = 8; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+      l[a] = l[a] * alpha + sum;
+      m[a] = m_new;
+#pragma unroll
+      for (int c = 0; c < DV / 16; ++c) acc[a][c] *= alpha;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int a = 0; a < RM; ++a) sP[(tx + 16 * k) * C::kLdP + ty * RM + a] = w[a][k];
+    __syncwarp();   // a row's weights are written and read by one warp
+#pragma unroll 4
+    for (int j = 0; j < kKeys; ++j) {
+      float pw[RM];
+#pragma unroll
+      for (int a = 0; a < RM; ++a) pw[a] = sP[j * C::kLdP + ty * RM + a];
+#pragma unroll
+      for (int c = 0; c < DV / 64; ++c) {
+        const float4 v = *reinterpret_cast<const float4*>(sV + j * DV + c * 64 + tx * 4);
+#pragma unroll
+        for (int a = 0; a < RM; ++a) {
+          if (pw[a] >= 0.f || pw[a] != pw[a]) {
+            acc[a][4 * c] = fmaf(pw[a], v.x, acc[a][4 * c]);
+            acc[a][4 * c + 1] = fmaf(pw[a], v.y, acc[a][4 * c + 1]);
+            acc[a][4 * c + 2] = fmaf(pw[a], v.z, acc[a][4 * c + 2]);
+            acc[a][4 * c + 3] = fmaf(pw[a], v.w, acc[a][4 * c + 3]);
+          }
+        }
+      }
+    }
+  }
+
+#pragma unroll
+  for (int a = 0; a < RM; ++a) {
+    const int r = ty * RM + a;
+    if (r >= rows) continue;
+    if (p.part_o != nullptr) {
+      const int64_t at = (item * p.splits + blockIdx.y) * C::kRows + r;
+#pragma unroll
+      for (int c = 0; c < DV / 64; ++c)
+        store4(p.part_o + at * DV + c * 64 + tx * 4,
+               make_float4(acc[a][4 * c], acc[a][4 * c + 1], acc[a][4 * c + 2], acc[a][4 * c + 3]));
+      if (tx == 0) p.part_ml[at] = make_float2(m[a], l[a]);
+      continue;
+    }
+    const int64_t i = (r0 + r) / p.G, g = r0 + r - i * p.G;
+    const float inv = m[a] == -INFINITY && l[a] == 0.f ? 0.f : 1.f / l[a];
+    T* o = static_cast<T*>(p.o.p) + b * p.o.sb + (h * p.G + g) * p.o.sh + i * p.o.sn;
+#pragma unroll
+    for (int c = 0; c < DV / 64; ++c)
+      store4(o + c * 64 + tx * 4, make_float4(acc[a][4 * c] * inv, acc[a][4 * c + 1] * inv, acc[a][4 * c + 2] * inv,
+                                              acc[a][4 * c + 3] * inv));
+    if (p.lse != nullptr && tx == 0)
+      p.lse[((b * p.Hk + h) * p.G + g) * p.N + i] = l[a] == 0.f ? -INFINITY : (m[a] + log2f(l[a])) * kLn2;
+  }
+}
+
+// Joins the shares of a row: one warp a row, eight rows a CTA.
+template <typename T, int DV>
+__global__ void __launch_bounds__(256)
+window_cc_join_kernel(Params p, int tile_rows) {
+  wait_for_previous();
+  const int lane = threadIdx.x & 31;
+  const int64_t item = blockIdx.x, bh = item / p.n_tiles;
+  const int r = int(blockIdx.y) * 8 + (threadIdx.x >> 5);
+  const int64_t row = (item - bh * p.n_tiles) * tile_rows + r;
+  if (row >= int64_t(p.N) * p.G) return;
+  auto place = [&](int k) { return (item * p.splits + k) * tile_rows + r; };
+  float M = -INFINITY;
+  for (int k = lane; k < p.splits; k += 32) M = fmaxf(M, p.part_ml[place(k)].x);
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+  const float base = M == -INFINITY ? 0.f : M;
+  float L = 0.f;
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int k = 0; k < p.splits; ++k) {
+    const float2 ml = p.part_ml[place(k)];
+    const float f = exp2f(ml.x - base);   // 0 of a share that saw nothing
+    L += f * ml.y;
+    if (lane * 4 < DV) {
+      const float4 v = load4(p.part_o + place(k) * DV + lane * 4);
+      x.x += f * v.x, x.y += f * v.y, x.z += f * v.z, x.w += f * v.w;
+    }
+  }
+  const float inv = L == 0.f ? 0.f : 1.f / L;
+  const int64_t b = bh / p.Hk, h = bh - b * p.Hk, i = row / p.G, g = row - i * p.G;
+  if (lane * 4 < DV)
+    store4(static_cast<T*>(p.o.p) + b * p.o.sb + (h * p.G + g) * p.o.sh + i * p.o.sn + lane * 4,
+           make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv));
+  if (p.lse != nullptr && lane == 0)
+    p.lse[((b * p.Hk + h) * p.G + g) * p.N + i] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
+}
+
+template <typename T, int DK, int DV, int RM, int NT>
+int launch(const WindowArgs& a, const WindowCcPlan& plan, char* msg, size_t msglen) {
+  using C = Cfg<DK, DV, RM, NT>;
+  auto kern = window_cc_kernel<T, DK, DV, RM, NT>;
+  cudaError_t e = ensure_smem_limit(reinterpret_cast<const void*>(kern), C::kSmem);
+  Params p{};
+  p.q = a.q, p.o = a.o, p.kv = a.kv, p.lse = a.lse, p.lens = a.lens;
+  p.Hk = a.Hk, p.N = int(a.N), p.G = int(a.Hq / a.Hk), p.max_len = int(a.max_len);
+  p.n_tiles = int(plan.items / (a.B * a.Hk));
+  p.mask = win::Mask{a.window, a.sinks, a.causal};
+  p.c_log2 = a.scale * kLog2e;
+  p.splits = int(plan.splits);
+  if (plan.splits > 1) {
+    p.part_o = static_cast<float*>(a.ws);
+    p.part_ml = reinterpret_cast<float2*>(p.part_o + plan.items * plan.splits * C::kRows * DV);
+  }
+  if (e == cudaSuccess)
+    e = launch_overlapped(kern, dim3(unsigned(plan.items), unsigned(plan.splits)), dim3(NT), C::kSmem, a.stream, p);
+  if (e == cudaSuccess && plan.splits > 1)
+    e = launch_overlapped(window_cc_join_kernel<T, DV>, dim3(unsigned(plan.items), C::kRows / 8), dim3(256), 0, a.stream, p,
+                          int(C::kRows));
+  if (e != cudaSuccess) {
+    snprintf(msg, msglen, "attention with a window: %s", cudaGetErrorString(e));
+    return 5;
+  }
+  return 0;
+}
+
+template <typename T, int DK, int DV>
+int launch_rows(const WindowArgs& a, const WindowCcPlan& plan, char* msg, size_t msglen) {
+  return plan.rows == 16 ? launch<T, DK, DV, 2, 128>(a, plan, msg, msglen) : launch<T, DK, DV, 4, 256>(a, plan, msg, msglen);
+}
+template <typename T>
+int launch_sizes(const WindowArgs& a, const WindowCcPlan& plan, char* msg, size_t msglen) {
+  if (a.dk == 64)
+    return a.dv == 64 ? launch_rows<T, 64, 64>(a, plan, msg, msglen) : launch_rows<T, 64, 128>(a, plan, msg, msglen);
+  return a.dv == 64 ? launch_rows<T, 128, 64>(a, plan, msg, msglen) : launch_rows<T, 128, 128>(a, plan, msg, msglen);
+}
+
+}  // namespace
+
+// Tiles of 16 rows where 64 would be mostly empty, or too few for the machine; shares of a tile's
+// tokens until there are two CTAs for each SM, none of less than one tile of tokens.
+WindowCcPlan window_cc_plan(const WindowArgs& a, int sms) {
+  const int64_t G = a.Hq / a.Hk, rows = a.N * G, bh = a.B * a.Hk;
+  WindowCcPlan p;
+  const int64_t big = bh * ((rows + 63) / 64);
+  p.rows = rows <= 32 || big < sms ? 16 : 64;
+  const int64_t tiles = (rows + p.rows - 1) / p.rows;
+  p.items = bh * tiles;
+  // most tiles of tokens that a row tile visits
+  int64_t most = (a.max_len + kKeys - 1) / kKeys;
+  if (a.window != win::kNoWindow) {
+    const int64_t span = int64_t(a.window) + p.rows / G + 2;
+    const int64_t seen = (span + kKeys - 1) / kKeys + 1 + (int64_t(a.sinks) + kKeys - 1) / kKeys;
+    if (seen < most) most = seen;
+  }
+  p.splits = p.items >= 2 * sms ? 1 : (2 * sms + p.items - 1) / p.items;
+  if (p.splits > most) p.splits = most;
+  if (p.splits < 1) p.splits = 1;
+  return p;
+}
+
+size_t window_cc_workspace(const WindowArgs& a, const WindowCcPlan& p) {
+  return p.splits > 1 ? size_t(p.items * p.splits * p.rows) * size_t(a.dv * 4 + 8) : 0;
+}
+
+int launch_window_cc(const WindowArgs& a, const WindowCcPlan& plan, char* msg, size_t msglen) {
+  return a.f32 ? launch_sizes<float>(a, plan, msg, msglen) : launch_sizes<__nv_bfloat16>(a, plan, msg, msglen);
+}
+
+cudaError_t window_cc_read_and_clear_status(unsigned* value) {
+  cudaError_t e = cudaMemcpyFromSymbol(value, g_moa_window_cc_status, sizeof(unsigned));
+  if (e != cudaSuccess || *value == 0) return e;
+  const unsigned zero = 0;
+  return cudaMemcpyToSymbol(g_moa_window_cc_status, &zero, sizeof(unsigned));
+}
+
+}  // namespace moa

@@ -1,5 +1,6 @@
 """Operators around attention: per-head norms of queries and keys with the rotation of positions,
-their gradients, and a paged 4-bit cache with the attention that reads it.
+their gradients, a paged 4-bit cache with the attention that reads it, attention with a sliding window
+and its gradients, and a paged 16- or 32-bit cache with the attention that reads it.
 
 The same thin binding as the rest of the package: every step of the computation runs in
 libmoa_attn.so, and argument checks and marshalling in moa_torch.so beside it (a decoding step makes
@@ -128,3 +129,73 @@ def kv4_attn_lse(q, pool, pages, lens, max_len: int | None = None, scale: float 
     exponentials of scaled scores (-inf for a query that sees nothing)."""
     return _b.kv4_attn(q, pool, pages, lens, max_len, scale, causal, out, True if lse is None else lse, workspace,
                        stream)
+
+
+def window_attn(q, k, v, window: int | None = None, sinks: int = 0, scale: float | None = None, out=None,
+                workspace=None, stream=None):
+    """Causal attention of q [B, H_q, N_q, d_k] over k [B, H_k, N_k, d_k] and v [B, H_k, N_k, d_v]:
+    [B, H_q, N_q, d_v].
+
+    The queries stand at the last N_q of the N_k positions.  A query at position p sees the tokens
+    j <= p with j > p - window or j < sinks (window None: all j <= p); one that sees nothing gives
+    zeros.  Query head h reads key head h // (H_q / H_k).  scale defaults to 1 / sqrt(d_k)."""
+    return _b.window_attn(q, k, v, window, sinks, scale, out, None, workspace, stream)
+
+
+def window_attn_lse(q, k, v, window: int | None = None, sinks: int = 0, scale: float | None = None, out=None,
+                    lse=None, workspace=None, stream=None):
+    """(o, lse): window_attn's output and the float32 [B, H_q, N_q] natural logarithm of each row's sum
+    of exponentials of scaled scores (-inf for a query that sees nothing)."""
+    return _b.window_attn(q, k, v, window, sinks, scale, out, True if lse is None else lse, workspace, stream)
+
+
+def window_attn_bwd(q, k, v, o, lse, do, window: int | None = None, sinks: int = 0, scale: float | None = None,
+                    out=None, workspace=None, stream=None):
+    """(dq, dk, dv): the gradients of window_attn for the gradient do of its output, from the o and lse
+    of window_attn_lse.  out: three tensors of the shapes of q, k and v."""
+    return _b.window_attn_bwd(q, k, v, o, lse, do, window, sinks, scale, out, workspace, stream)
+
+
+def kv_pool(n_pages: int, H: int, page_tokens: int, d_k: int, d_v: int, dtype=None, device="cuda"):
+    """An empty pool of the 16- or 32-bit cache: [n_pages, H, page_tokens, d_k + d_v] of dtype
+    (torch.bfloat16 by default), a token's key and then its value."""
+    import torch
+    dtype = torch.bfloat16 if dtype is None else dtype
+    if page_tokens % 16 or page_tokens < 16 or d_k not in (64, 128) or d_v not in (64, 128):
+        raise ValueError("kv_pool: page_tokens must be a multiple of 16, d_k and d_v 64 or 128")
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"kv_pool: unsupported dtype {dtype}; use torch.bfloat16 or torch.float32")
+    return torch.zeros((n_pages, H, page_tokens, d_k + d_v), dtype=dtype, device=device)
+
+
+def kv_append(k, v, pool, pages, pos, cos=None, sin=None, q=None, interleaved: bool = False, out=None, stream=None):
+    """Writes keys [B, H_k, N, d_k] and values [B, H_k, N, d_v] into the pool (kv_pool): token n of
+    sequence b goes to position pos[b, n], that is to page pages[b, pos // page_tokens], place
+    pos % page_tokens.  pages: int32 [B, max_pages]; pos: int32 [B, N], negative: not written.
+
+    With cos and sin (rope_table) the keys' first d_rot features are rotated by their positions' angles
+    on the way (pairs as in qk_norm_rope), and so is q [B, H_q, N, d_k] if given: it is returned rotated
+    (out: a tensor for it, q itself for in place), with zeros where the position is negative."""
+    return _b.kv_append(k, v, pool, pages, pos, cos, sin, q, interleaved, out, stream)
+
+
+def kv_attn(q, pool, pages, lens, max_len: int | None = None, window: int | None = None, sinks: int = 0,
+            scale: float | None = None, causal: bool = True, out=None, workspace=None, stream=None):
+    """Attention of q [B, H_q, N, d_k] over each sequence's tokens in the pool (kv_pool, kv_append):
+    [B, H_q, N, d_v].
+
+    lens: int32 [B] on the device, the tokens that each sequence has in the cache, the N queries being
+    its last N: a query at position p sees the tokens j <= p (without causal: all) with j > p - window
+    or j < sinks (window None: all of them).  A query that sees nothing gives zeros.  Query head h reads
+    key head h // (H_q / H_k).  Pages that lie before every query's window are not looked at.
+    max_len: an upper bound of lens known to the host (default: what the page table holds); the work is
+    divided by it, so a close bound is faster."""
+    return _b.kv_attn(q, pool, pages, lens, max_len, window, sinks, scale, causal, out, None, workspace, stream)
+
+
+def kv_attn_lse(q, pool, pages, lens, max_len: int | None = None, window: int | None = None, sinks: int = 0,
+                scale: float | None = None, causal: bool = True, out=None, lse=None, workspace=None, stream=None):
+    """(o, lse): kv_attn's output and the float32 [B, H_q, N] natural logarithm of each row's sum of
+    exponentials of scaled scores (-inf for a query that sees nothing)."""
+    return _b.kv_attn(q, pool, pages, lens, max_len, window, sinks, scale, causal, out, True if lse is None else lse,
+                      workspace, stream)
