@@ -477,10 +477,13 @@ void set_window(WindowArgs& a, int64_t window, int64_t sinks) {
   a.sinks = int(a.window == win::kNoWindow ? 0 : sinks < a.max_len ? sinks : a.max_len);
 }
 
+// What either kernel needs: a workspace's size does not go by strides.
 size_t window_workspace(const WindowArgs& a, int sms) {
-  return window_cc_workspace(a, window_cc_plan(a, sms));
+  const size_t cc = window_cc_workspace(a, window_cc_plan(a, sms)), tc = a.f32 ? 0 : window_tc_workspace(a, sms);
+  return cc > tc ? cc : tc;
 }
 int launch_window(const WindowArgs& a, int sms, char* msg, size_t msglen) {
+  if (window_tc_takes(a)) return launch_window_tc(a, sms, msg, msglen);
   return launch_window_cc(a, window_cc_plan(a, sms), msg, msglen);
 }
 

@@ -142,6 +142,12 @@ WindowCcPlan window_cc_plan(const WindowArgs& a, int sms);
 size_t window_cc_workspace(const WindowArgs& a, const WindowCcPlan& p);
 int launch_window_cc(const WindowArgs& a, const WindowCcPlan& p, char* msg, size_t msglen);
 
+// Tensor cores: bf16 (window_fwd_tc.cu).  Whether it takes a call: tensor maps describe its tensors (no strides that
+// are zero or negative), and the scale is not negative.
+bool window_tc_takes(const WindowArgs& a);
+size_t window_tc_workspace(const WindowArgs& a, int sms);
+int launch_window_tc(const WindowArgs& a, int sms, char* msg, size_t msglen);
+
 // Gradients of attention with a window (dense keys and values).
 struct WindowBwdArgs {
   View q, k, v, o, go;   // inputs
@@ -175,6 +181,7 @@ struct KvAppendArgs {
 };
 int launch_kv_append(const KvAppendArgs& a, char* msg, size_t msglen);
 
+cudaError_t window_tc_read_and_clear_status(unsigned* value);
 cudaError_t window_cc_read_and_clear_status(unsigned* value);
 cudaError_t kv_append_read_and_clear_status(unsigned* value);
 

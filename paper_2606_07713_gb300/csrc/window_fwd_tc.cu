@@ -1,0 +1,1011 @@
+// Causal attention with a sliding window and first tokens that stay visible, bf16, on the fifth-generation
+// tensor cores (tcgen05 + TMEM + TMA), sm_103a.  Keys and values lie in dense tensors or in the pages of a
+// cache; any number of query rows, from a decoding step's to a training batch's.
+//
+// Mathematics: o_i = sum_j p_ij v_j / l_i over the tokens j that row i sees (window.cuh), p_ij = 2^(c s_ij - m_i),
+// c = scale log2 e, running maximum m_i and sum l_i: one pass over the tokens.  S = Q K^T and O += P V are
+// 128 x 128 tiles in TMEM; maximum, exponentials and sums are fp32, P is rounded to bf16 (the operand type).
+//
+// Rows of a key head are counted position by position: row r of a 128-row tile is position r / GC and query
+// head r % GC of the group (GC = min(G, 128) heads), so that a tile covers few positions: a window then needs few
+// tiles of tokens, and a decoding step's heads share one tile.  TMA puts them in that order itself (a
+// five-dimensional map: feature, head of the group, position, key head, sequence); heads and positions past the
+// end are zeros.  Keys and values come by TMA as well, a page (or the part of it that divides 128) a copy, straight from
+// the pool.  A page that no row of the work item sees is asked for past the pool's end, which fills zeros: its
+// entry in the table may be anything.
+//
+// Work items (key head, chunk of heads, 128 QT rows) count in 128-token tiles; all items' tiles are cut into equal
+// shares, one for each SM (one CTA fills an SM), and a CTA walks over its share.  Cut items are joined by a
+// second kernel.  QT = 2 where there are more rows than a tile holds: keys and values in shared memory then serve
+// twice the rows.
+//
+// Hidden tokens: a tile that some row sees only in part is masked by words of bits, -infinity in place of the
+// score.  Past a sequence's end the cache may hold anything: the values' rows there are zeroed in
+// shared memory before the product.  Any other hidden value that is not finite (0 * NaN) makes the output NaN;
+// rows whose output is not finite are computed again at the end, token by token, from what they do see
+// (exact_row).  That costs nothing where all values are finite.
+//
+// CTA organisation (QT = 2): warps 0-3 and 4-7 softmax and epilogue of row tiles 0 and 1 (thread = row), then the
+// products of tile 0 (and TMEM allocation), TMA, the products of tile 1, the share's items for the other roles.
+// QT = 1: warps 0-3, then four such warps of which one idles.  K and V tiles stream through a ring in the
+// order of use, K0 K1 V0 K2 V1 ...  Waits are bounded: on expiry MOA_ERR_DEVICE_TIMEOUT is recorded and every
+// role leaves its loop.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <atomic>
+#include <cfloat>
+#include <cstdio>
+
+#include "internal.h"
+#include "ops_internal.h"
+#include "ptx.cuh"
+#include "tc_common.cuh"
+#include "window.cuh"
+
+namespace moa {
+
+__device__ unsigned int g_moa_window_tc_status = 0;
+
+namespace {
+
+using namespace ptx;
+using namespace tc;
+
+constexpr int kBM = 128;              // rows of a row tile (= TMEM lanes)
+constexpr int kBN = 128;              // tokens of a tile
+constexpr int kItemUnits = 4;         // what an item costs besides its tiles, in tiles
+constexpr float kRescaleLog2 = 8.f;   // the running maximum may lag by this: weights up to 2^8
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+template <int DK, int DV, int QT>
+struct Cfg {
+  static constexpr int kSoftmax = 128 * QT, kThreads = kSoftmax + 128;
+  static constexpr int kRows = kBM * QT;
+  static constexpr int kMmaWarp0 = 4 * QT, kLoadWarp = kMmaWarp0 + 1, kMmaWarp1 = kMmaWarp0 + 2, kWalkWarp = kMmaWarp0 + 3;
+  // QT = 2: 256 kRegsSoftmax + 128 kRegsCtrl is what the launch allocates (the host checks it)
+  static constexpr int kRegsLaunch = 168, kRegsSoftmax = 208, kRegsCtrl = 88;
+  static_assert(256 * kRegsSoftmax + 128 * kRegsCtrl <= 384 * kRegsLaunch, "register split");
+  static constexpr int kPanelBytes = 128 * 128;   // 64 columns of 128 rows, 128-byte swizzle
+  static constexpr int kQTileBytes = kBM * DK * 2;
+  static constexpr int kKTileBytes = kBN * DK * 2, kVTileBytes = kBN * DV * 2;
+  static constexpr int kStageBytes = kKTileBytes > kVTileBytes ? kKTileBytes : kVTileBytes;
+  static constexpr bool kSharedS = DV == 128 && QT == 2;   // one S for both row tiles
+  static constexpr int kOffKV = QT * kQTileBytes;
+  static constexpr int kStages = (229376 - kOffKV) / kStageBytes < 8 ? (229376 - kOffKV) / kStageBytes : 8;
+  static constexpr int kOffBar = kOffKV + kStages * kStageBytes;
+  // barriers: full[NS], empty[NS], q_full, q_empty, drain, s_full[2], p_ready[2], o_done[2], s_free[2], p_free[2],
+  // item_full[2], item_empty[2]
+  static constexpr int kNumBars = 2 * kStages + 17;
+  static constexpr int kOffMisc = kOffBar + kNumBars * 8;
+  static constexpr int kOffItems = (kOffMisc + 12 + 15) / 16 * 16;   // two items, then scan[12] and found[2]
+  static constexpr int kSmemBytes = kOffItems + 2 * 32 + 14 * 8 + 1024;
+  static constexpr int kEarlyChunks = DV == 64 ? 2 : 4;   // of 32 tokens, exponentials before the wait for P's buffer
+  static constexpr uint32_t kTmemCols = 512;
+  static constexpr uint32_t kTmemS0 = 0, kTmemS1 = kSharedS ? 0 : 128;
+  static constexpr uint32_t kTmemP0 = kSharedS ? 128 : 256, kTmemP1 = kSharedS ? 192 : 320;
+  static constexpr uint32_t kTmemO0 = kSharedS ? 256 : 384, kTmemO1 = kTmemO0 + (QT == 2 ? DV : 0);
+  static_assert(kTmemO1 + DV <= kTmemCols, "TMEM budget");
+  static_assert(kSmemBytes <= 232448, "shared memory budget");
+};
+
+struct Params {
+  int64_t q_sb, q_sh, q_sn, o_sb, o_sh, o_sn;
+  KvSource kv;
+  const int32_t* lens;   // null: every sequence has max_len tokens
+  int N, max_len, Hk, G;
+  int GC, chunks, PT;    // heads of a tile, chunks of heads, positions of a tile
+  int n_tiles;           // work items of a key head
+  int n_items;
+  int box;               // tokens of a TMA copy
+  win::Mask mask;
+  float c_log2;          // scale log2 e, >= 0
+  uint64_t wait_limit_ns;
+};
+
+__device__ __forceinline__ int length_of(const Params& p, int b, bool report) {
+  if (p.lens == nullptr) return p.max_len;
+  const int len = p.lens[b];
+  if (len >= 0 && len <= p.max_len) return len;
+  if (report) atomicExch(&g_moa_window_tc_status, win::kErrIndex);
+  return len < 0 ? 0 : p.max_len;
+}
+
+// A work item: its key head, chunk of heads and positions.
+struct Where {
+  int b, h, chunk, i0, i1;   // the last position is i1
+};
+template <int QT>
+__device__ __forceinline__ Where where_of(const Params& p, int item) {
+  Where w;
+  const int bh = int(unsigned(item) / unsigned(p.n_tiles)), rest = item - bh * p.n_tiles;
+  const int tile = int(unsigned(rest) / unsigned(p.chunks));
+  w.chunk = rest - tile * p.chunks;
+  w.b = int(unsigned(bh) / unsigned(p.Hk)), w.h = bh - w.b * p.Hk;
+  w.i0 = tile * QT * p.PT;
+  const int64_t last = int64_t(w.i0) + QT * p.PT - 1;
+  w.i1 = last < p.N ? int(last) : p.N - 1;
+  return w;
+}
+// Tiles of tokens that it counts for: at least one, so that every item is written.
+template <int QT>
+__device__ __forceinline__ int units_of(const Params& p, int item, bool report) {
+  const Where w = where_of<QT>(p, item);
+  const int n = win::tiles_of(p.mask, length_of(p, w.b, report), p.N, w.i0, w.i1, kBN).n;
+  return n < 1 ? 1 : n;
+}
+
+// Equal shares of `total` units: share c begins at start(c).
+struct Shares {
+  int64_t each;
+  uint32_t rest, n;
+  __device__ __forceinline__ Shares(int64_t total, uint32_t ctas) {
+    n = total < ctas ? uint32_t(total) : ctas;
+    each = total / n;
+    rest = uint32_t(total - each * n);
+  }
+  __device__ __forceinline__ int64_t start(uint32_t c) const { return each * c + rest * c / n; }
+};
+
+// An item cut by CTA c's share, begun by it and not ended: its pieces lie with CTAs c, c + 1, ...
+struct Cut {
+  int item;
+  int pieces;   // 0: none
+};
+
+// One item of a CTA's share: its tiles [u0, u1) of `units` are this CTA's; tile t is token tile
+// list.at(t).  item < 0: no more.
+struct Item {
+  int item, u0, u1, units;
+  int first, from, len;
+};
+
+__device__ __forceinline__ float row_max128(const float* s) {
+  float a0 = s[0], a1 = s[1], a2 = s[2], a3 = s[3];
+#pragma unroll
+  for (int i = 4; i < 124; i += 8) {
+    a0 = max3f(a0, s[i], s[i + 1]);
+    a1 = max3f(a1, s[i + 2], s[i + 3]);
+    a2 = max3f(a2, s[i + 4], s[i + 5]);
+    a3 = max3f(a3, s[i + 6], s[i + 7]);
+  }
+  a0 = max3f(a0, s[124], s[125]);
+  a1 = max3f(a1, s[126], s[127]);
+  return max3f(a0, a1, fmaxf(a2, a3));
+}
+
+// Multiplies DV fp32 TMEM columns of this thread's lane by alpha (warp-collective).
+template <int DV>
+__device__ __forceinline__ void tmem_scale_row(uint32_t taddr, float alpha) {
+#pragma unroll
+  for (int c = 0; c < DV; c += 32) {
+    uint32_t o[32];
+    tmem_ld_32x32b_x32(taddr + c, o);
+    tmem_wait_ld();
+    reg_anchor_x32(o);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+    tmem_st_32x32b_x32(taddr + c, o);
+  }
+  tmem_wait_st();
+}
+
+// Bits 32 w .. 32 w + 31 of the number with the lowest x bits set.
+__device__ __forceinline__ uint32_t below(int x, int w) {
+  const int n = x - 32 * w;
+  return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u;
+}
+
+__device__ __forceinline__ bool not_finite(float x) { return !(fabsf(x) < INFINITY); }
+
+// One row again, token by token over what it sees: a warp, 4 features a lane.
+template <int DK, int DV>
+__device__ __noinline__ void exact_row(const __nv_bfloat16* q, __nv_bfloat16* o, const Params& p, int b, int h, int i) {
+  const int lane = threadIdx.x & 31;
+  constexpr int NK = DK / 32, NV = DV / 32;
+  float x[NK], acc[NV];
+#pragma unroll
+  for (int e = 0; e < NK; ++e) x[e] = __bfloat162float(q[lane * NK + e]);
+#pragma unroll
+  for (int e = 0; e < NV; ++e) acc[e] = 0.f;
+  const int len = length_of(p, b, false);
+  const int end = win::row_end(p.mask, len, p.N, i), low = win::row_low(p.mask, len, p.N, i);
+  float m = -INFINITY, l = 0.f;
+  for (int t = 0; t < end; ++t) {
+    if (t >= p.mask.sinks && t < low) {
+      t = low;
+      if (t >= end) break;
+    }
+    int64_t at = b, place = t;
+    bool there = true;
+    if (p.kv.table != nullptr) {
+      const int slot = t / p.kv.page;
+      at = p.kv.table[b * p.kv.max_pages + slot];
+      place = t - slot * p.kv.page;
+      there = at >= 0 && at < p.kv.n_pages;
+    }
+    const __nv_bfloat16* k = static_cast<const __nv_bfloat16*>(p.kv.k) + at * p.kv.k_sb + h * p.kv.k_sh + place * p.kv.k_sn;
+    const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(p.kv.v) + at * p.kv.v_sb + h * p.kv.v_sh + place * p.kv.v_sn;
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < NK; ++e) s = fmaf(x[e], there ? __bfloat162float(k[lane * NK + e]) : 0.f, s);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+    s *= p.c_log2;
+    const float m_new = fmaxf(m, s), base = m_new == -INFINITY ? 0.f : m_new;
+    const float alpha = exp2f(m - base), w = exp2f(s - base);
+    l = l * alpha + w;
+    m = m_new;
+#pragma unroll
+    for (int e = 0; e < NV; ++e) acc[e] = acc[e] * alpha + w * (there ? __bfloat162float(v[lane * NV + e]) : 0.f);
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int e = 0; e < NV; ++e) o[lane * NV + e] = __float2bfloat16(acc[e] * inv);
+}
+
+// ------------------------------------------------------------------------------------------------
+// Attention
+// ------------------------------------------------------------------------------------------------
+template <int DK, int DV, int QT>
+__global__ void __launch_bounds__(Cfg<DK, DV, QT>::kThreads, 1)
+window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                 const __grid_constant__ CUtensorMap tmV, __nv_bfloat16* O, float* lse, float* part_o, float2* part_ml,
+                 Cut* cuts, uint8_t* odd, const Params p) {
+  using C = Cfg<DK, DV, QT>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  const uint32_t sQ = smem_u32(smem), sKV = smem_u32(smem + C::kOffKV), bar0 = smem_u32(smem + C::kOffBar);
+  auto full_bar = [&](int s) { return bar0 + 8u * s; };
+  auto empty_bar = [&](int s) { return bar0 + 8u * (C::kStages + s); };
+  const uint32_t q_full = bar0 + 8u * (2 * C::kStages), q_empty = q_full + 8, drain = q_full + 16;
+  auto s_full = [&](int j) { return q_full + 8u * (3 + j); };
+  auto p_ready = [&](int j) { return q_full + 8u * (5 + j); };
+  auto o_done = [&](int j) { return q_full + 8u * (7 + j); };
+  auto s_free = [&](int j) { return q_full + 8u * (9 + j); };
+  auto p_free = [&](int j) { return q_full + 8u * (11 + j); };
+  auto item_full = [&](int i) { return q_full + 8u * (13 + i); };
+  auto item_empty = [&](int i) { return q_full + 8u * (15 + i); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::kOffMisc);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::kOffMisc + 4);
+  volatile Item* items = reinterpret_cast<volatile Item*>(smem + C::kOffItems);
+  int64_t* scan = reinterpret_cast<int64_t*>(smem + C::kOffItems + 64);   // warp sums
+  int64_t* found = scan + 12;                                             // item, its first unit
+  constexpr int kWarps = C::kThreads / 32;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const WaitCtl wc{abort_flag, p.wait_limit_ns, 0u, &g_moa_window_tc_status};
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < C::kStages; ++s) {
+      mbar_init(full_bar(s), 1);
+      mbar_init(empty_bar(s), QT);   // one commit from each issuer
+    }
+    mbar_init(q_full, 1);
+    mbar_init(q_empty, QT);
+    mbar_init(drain, QT);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(item_full(i), 1);
+      mbar_init(item_empty(i), 5 * QT + 1);   // the softmax warps, the issuers, the loads
+    }
+    for (int j = 0; j < QT; ++j) {
+      mbar_init(s_full(j), 1);
+      mbar_init(p_ready(j), 128);
+      mbar_init(o_done(j), 1);
+      mbar_init(s_free(j), 128);
+      mbar_init(p_free(j), 1);
+    }
+    *abort_flag = 0;
+    fence_barrier_init();
+  }
+  if (warp == C::kMmaWarp0) {
+    tmem_alloc(smem_u32(tmem_slot), C::kTmemCols);
+    tmem_relinquish();
+  }
+  if (p.GC * p.PT < kBM) {   // rows of a tile that no copy fills
+    for (int x = threadIdx.x; x < QT * C::kQTileBytes / 16; x += C::kThreads)
+      reinterpret_cast<uint4*>(smem)[x] = make_uint4(0, 0, 0, 0);
+    fence_proxy_async_smem();
+  }
+  wait_for_previous();
+  // this CTA's share of all units, and the item in which it begins
+  int64_t sum = 0;
+  for (int i = threadIdx.x; i < p.n_items; i += C::kThreads) sum += units_of<QT>(p, i, true) + kItemUnits;
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+  if (lane == 0) scan[warp] = sum;
+  __syncthreads();
+  int64_t total = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) total += scan[w];
+  const Shares shares(total, gridDim.x);
+  const int64_t first_unit = blockIdx.x < shares.n ? shares.start(blockIdx.x) : total;
+  const int64_t stop = blockIdx.x < shares.n ? shares.start(blockIdx.x + 1) : total;
+  int64_t done = 0;
+  for (int base = 0; first_unit < stop; base += C::kThreads) {
+    const int i = base + threadIdx.x;
+    const int64_t mine = i < p.n_items ? units_of<QT>(p, i, false) + kItemUnits : 0;
+    int64_t incl = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int64_t o = __shfl_up_sync(0xffffffffu, incl, d);
+      if (lane >= d) incl += o;
+    }
+    __syncthreads();
+    if (lane == 31) scan[warp] = incl;
+    __syncthreads();
+    int64_t all = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      if (w < warp) incl += scan[w];
+      all += scan[w];
+    }
+    incl += done;
+    done += all;
+    if (first_unit >= incl - mine && first_unit < incl) {
+      found[0] = i;
+      found[1] = incl - mine;
+    }
+    if (first_unit < done) break;
+  }
+  if (threadIdx.x == 0) cuts[blockIdx.x].pieces = 0;
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = *tmem_slot;
+  // A whole warp's wait: on expiry all its lanes leave together.
+  auto wait_warp = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_bounded(bar, parity, wc)) != 0; };
+  // Item number i of the share, as every role sees it: valid until the role's release.
+  auto get_item = [&](uint32_t i, bool& ok) {
+    ok = ok && wait_warp(item_full(i & 1), i >> 1 & 1u);
+    const volatile Item& x = items[i & 1];
+    return ok ? Item{x.item, x.u0, x.u1, x.units, x.first, x.from, x.len} : Item{-1, 0, 0, 0, 0, 0, 0};
+  };
+
+  if (warp >= C::kMmaWarp0) {
+    if constexpr (QT == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRegsCtrl));
+    if (warp == C::kLoadWarp) {
+      // ------------------------------------------------------------ TMA producer: a copy a lane
+      if (lane == 0) {
+        tma_prefetch_desc(&tmQ);
+        tma_prefetch_desc(&tmK);
+        tma_prefetch_desc(&tmV);
+      }
+      const int boxes = kBN / p.box;
+      int slot = 0;
+      uint32_t phase = 0, issued = 0, issued_phase = 0, q_issued = 0;
+      bool ok = true;
+      for (uint32_t seg = 0; ok; ++seg) {
+        const Item x = get_item(seg, ok);
+        if (x.item < 0) break;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(item_empty(seg & 1));
+        const Where w = where_of<QT>(p, x.item);
+        const win::Tiles list{x.first, x.from, x.units};
+        const int end = win::row_end(p.mask, x.len, p.N, w.i1), low = win::row_low(p.mask, x.len, p.N, w.i0);
+        const int n_kt = x.u1 - x.u0;
+        // the lane's copy of tile u0 + n: its first token, and the page (of a dense tensor the sequence)
+        struct Source {
+          int token, page;
+        };
+        auto source = [&](int n) {
+          Source s{0, w.b};
+          if (n >= n_kt || lane >= boxes) return s;
+          const int t0 = list.at(x.u0 + n) * kBN + lane * p.box;
+          if (p.kv.table == nullptr) {
+            s.token = t0;
+            return s;
+          }
+          s.page = int(p.kv.n_pages);   // past the pool: zeros
+          if (t0 < end && (t0 + p.box > low || t0 < p.mask.sinks)) {
+            const int at = int(unsigned(t0) / unsigned(p.kv.page));
+            const int pg = p.kv.table[w.b * p.kv.max_pages + at];
+            s.token = t0 - at * p.kv.page;
+            if (pg >= 0 && pg < p.kv.n_pages)
+              s.page = pg;
+            else
+              atomicExch(&g_moa_window_tc_status, win::kErrIndex);
+          }
+          return s;
+        };
+        Source cur = source(0), next = cur, after = source(1);
+        for (int t = 0; t < 2 * n_kt; ++t) {
+          // K0 K1 V0 K2 V1 ... (tile n + 1's scores come before tile n's P V)
+          const int u = t - 1, nn = u >> 1;
+          const bool is_k = t == 0 || ((u & 1) == 0 && nn + 1 < n_kt);
+          const int n = t == 0 ? 0 : is_k ? nn + 1 : nn;
+          if (is_k && n > 0) {
+            next = after;
+            after = source(n + 1);
+          }
+          if (!wait_warp(empty_bar(slot), phase ^ 1u)) {
+            ok = false;
+            break;
+          }
+          issued |= 1u << slot;
+          issued_phase = (issued_phase & ~(1u << slot)) | (phase << slot);
+          const uint32_t dst = sKV + slot * C::kStageBytes + lane * p.box * 128;
+          if (lane == 0) mbar_arrive_expect_tx(full_bar(slot), is_k ? C::kKTileBytes : C::kVTileBytes);
+          __syncwarp();
+          if (lane < boxes) {
+            if (is_k) {
+              const Source& s = n == 0 ? cur : next;
+#pragma unroll
+              for (int q = 0; q < DK / 64; ++q)
+                tma_load_4d(dst + q * C::kPanelBytes, &tmK, full_bar(slot), q * 64, s.token, w.h, s.page);
+            } else {
+#pragma unroll
+              for (int q = 0; q < DV / 64; ++q)
+                tma_load_4d(dst + q * C::kPanelBytes, &tmV, full_bar(slot), q * 64, cur.token, w.h, cur.page);
+            }
+          }
+          if (!is_k) cur = next;
+          if (t == 0) {   // the queries, once the item before has no use for its own
+            if (seg > 0 && !wait_warp(q_empty, (seg - 1) & 1u)) {
+              ok = false;
+            } else if (lane == 0) {
+              mbar_arrive_expect_tx(q_full, QT * DK * 2 * p.GC * p.PT);
+#pragma unroll
+              for (int j = 0; j < QT; ++j)
+#pragma unroll
+                for (int q = 0; q < DK / 64; ++q)
+                  tma_load_5d(sQ + j * C::kQTileBytes + q * C::kPanelBytes, &tmQ, q_full, q * 64, w.chunk * p.GC,
+                              w.i0 + j * p.PT, w.h, w.b);
+            }
+            if (!ok) break;
+            ++q_issued;
+          }
+          if (++slot == C::kStages) {
+            slot = 0;
+            phase ^= 1u;
+          }
+        }
+      }
+      __syncwarp();
+      if (lane == 0 && (!ok || *abort_flag)) {   // let every copy land before the CTA can exit
+        if (q_issued > 0) wait_quiesce(q_full, (q_issued - 1) & 1u, p.wait_limit_ns, &g_moa_window_tc_status);
+        for (int sl = 0; sl < C::kStages; ++sl)
+          if (issued & (1u << sl))
+            wait_quiesce(full_bar(sl), (issued_phase >> sl) & 1u, p.wait_limit_ns, &g_moa_window_tc_status);
+      }
+    } else if (warp == C::kMmaWarp0 || (QT == 2 && warp == C::kMmaWarp1)) {
+      // ------------------------------------------------------------ MMA issuers, one for each row tile
+      const int j = warp == C::kMmaWarp0 ? 0 : 1;
+      constexpr uint32_t kIdescQK = make_idesc(kBM, kBN, false);
+      constexpr uint32_t kIdescPV = make_idesc(kBM, DV, true);
+      const uint32_t tS = tmem + (j ? C::kTmemS1 : C::kTmemS0);
+      const uint32_t tP = tmem + (j ? C::kTmemP1 : C::kTmemP0);
+      const uint32_t tO = tmem + (j ? C::kTmemO1 : C::kTmemO0);
+      const uint32_t sQj = sQ + j * C::kQTileBytes;
+      int slot = 0;
+      uint32_t phase = 0;
+      uint32_t t = 0;   // tiles so far: the phases of the barriers between the roles
+      auto next = [&]() {
+        if (++slot == C::kStages) {
+          slot = 0;
+          phase ^= 1u;
+        }
+      };
+      auto issue_qk = [&](uint32_t kb) {
+#pragma unroll
+        for (int kk = 0; kk < DK / 16; ++kk) {
+          const uint32_t off = (kk >> 2) * C::kPanelBytes + (kk & 3) * 32;
+          mma_f16_ss(tS, make_sdesc_sw128(sQj + off, 16, 1024), make_sdesc_sw128(kb + off, 16, 1024), kIdescQK,
+                     kk > 0 ? 1u : 0u);
+        }
+      };
+      auto issue_pv = [&](uint32_t vb, uint32_t acc_first) {
+#pragma unroll
+        for (int kk = 0; kk < kBN / 16; ++kk)
+          mma_f16_ts(tO, tP + kk * 8, make_sdesc_sw128(vb + kk * 2048, C::kPanelBytes, 1024), kIdescPV,
+                     kk > 0 ? 1u : acc_first);
+      };
+      // The S buffer may take tile u's scores once its last reader holds what it has: this row
+      // tile's softmax (tile u - 1), or with one buffer for both, the other one's (tile u - 1 for
+      // row tile 0, tile u for row tile 1).
+      auto s_buffer = [&](uint32_t u) {
+        if (C::kSharedS) return j ? wait_warp(s_free(0), u & 1u) : u == 0 || wait_warp(s_free(1), (u - 1) & 1u);
+        return u == 0 || wait_warp(s_free(j), (u - 1) & 1u);
+      };
+      bool ok = true;
+      for (uint32_t seg = 0; ok; ++seg) {
+        const Item x = get_item(seg, ok);
+        if (x.item < 0) break;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(item_empty(seg & 1));
+        const int n_kt = x.u1 - x.u0;
+        const win::Tiles list{x.first, x.from, x.units};
+        ok = wait_warp(q_full, seg & 1u) && wait_warp(full_bar(slot), phase) && s_buffer(t);
+        if (ok) {
+          tc_fence_after_sync();
+          const int ks = slot;
+          next();
+          if (lane == 0) {
+            issue_qk(sKV + ks * C::kStageBytes);
+            mma_commit(s_full(j));
+            mma_commit(empty_bar(ks));
+            if (n_kt == 1) mma_commit(q_empty);
+          }
+        }
+        for (int n = 0; ok && n < n_kt; ++n, ++t) {
+          if (n + 1 < n_kt) {
+            const int ks = slot;
+            ok = wait_warp(full_bar(slot), phase) && s_buffer(t + 1);
+            next();
+            if (!ok) break;
+            tc_fence_after_sync();
+            if (lane == 0) {
+              issue_qk(sKV + ks * C::kStageBytes);
+              mma_commit(s_full(j));
+              mma_commit(empty_bar(ks));
+              if (n + 2 == n_kt) mma_commit(q_empty);
+            }
+          }
+          const int vs = slot;
+          ok = wait_warp(full_bar(slot), phase);
+          if (p.kv.table != nullptr) {
+            // rows past the sequence's end hold whatever the page held
+            const int gone = x.len - list.at(x.u0 + n) * kBN;   // the first one
+            if (ok && gone < kBN) {
+              const int z = gone < 0 ? 0 : gone;
+#pragma unroll
+              for (int q = 0; q < DV / 64; ++q)
+                for (int e = lane; e < (kBN - z) * 8; e += 32)
+                  reinterpret_cast<uint4*>(smem + C::kOffKV + vs * C::kStageBytes + q * C::kPanelBytes + z * 128)[e] =
+                      make_uint4(0, 0, 0, 0);
+              fence_proxy_async_smem();
+            }
+          }
+          ok = ok && wait_warp(p_ready(j), t & 1u);
+          next();
+          if (!ok) break;
+          tc_fence_after_sync();
+          if (lane == 0) {
+            issue_pv(sKV + vs * C::kStageBytes, n > 0 ? 1u : 0u);
+            mma_commit(p_free(j));
+            mma_commit(empty_bar(vs));
+          }
+        }
+        // arrives when the item's products are complete
+        if (lane == 0) mma_commit(o_done(j));
+        __syncwarp();
+      }
+      if (lane == 0) mma_commit(drain);
+    } else if (warp == C::kWalkWarp && lane == 0) {
+      // ------------------------------------------------------------ the items of the share
+      int64_t at = first_unit, before = 0;
+      int item = 0;
+      if (at < stop) {
+        item = int(found[0]);
+        before = found[1];
+      }
+      for (uint32_t seg = 0;; ++seg) {
+        int units = 0, u0 = 0, u1 = 0, which = -1, len = 0;
+        win::Tiles list{};
+        while (at < stop && u0 == u1) {   // (nothing of an item's tiles: the next CTA begins it)
+          const Where w = where_of<QT>(p, item);
+          len = length_of(p, w.b, false);
+          list = win::tiles_of(p.mask, len, p.N, w.i0, w.i1, kBN);
+          units = list.n < 1 ? 1 : list.n;
+          const int64_t end = before + units + kItemUnits, upto = end < stop ? end : stop;
+          u0 = max(0, int(at - before) - kItemUnits), u1 = max(0, int(upto - before) - kItemUnits);
+          if (u0 < u1) which = item;
+          if (u0 == 0 && u1 > 0 && u1 < units) {   // begun here, ended by a later CTA
+            uint32_t c = blockIdx.x;
+            while (shares.start(c + 1) < end) ++c;
+            cuts[blockIdx.x] = Cut{item, int(c - blockIdx.x) + 1};
+          }
+          at = upto;
+          before = end;
+          ++item;
+        }
+        if (seg >= 2 && !wait_bounded(item_empty(seg & 1), ((seg >> 1) - 1) & 1u, wc)) break;
+        volatile Item& x = items[seg & 1];
+        x.item = which, x.u0 = u0, x.u1 = u1, x.units = units;
+        x.first = list.first, x.from = list.from, x.len = len;
+        mbar_arrive(item_full(seg & 1));
+        if (which < 0) break;
+      }
+    }
+  } else {
+    if constexpr (QT == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kRegsSoftmax));
+    // -------------------------------------------------------------- softmax warpgroups
+    const int j = warp >> 2;
+    const int lane_base = (warp & 3) * 32, row = lane_base + lane;
+    const uint32_t tS = tmem + (uint32_t(lane_base) << 16) + (j ? C::kTmemS1 : C::kTmemS0);
+    const uint32_t tO = tmem + (uint32_t(lane_base) << 16) + (j ? C::kTmemO1 : C::kTmemO0);
+    const uint32_t tP = tmem + (uint32_t(lane_base) << 16) + (j ? C::kTmemP1 : C::kTmemP0);
+    const float c = fmaxf(p.c_log2, FLT_MIN);   // not zero: c * -infinity hides a token
+    const int row_pos = int(unsigned(row) / unsigned(p.GC)), row_head = row - row_pos * p.GC;
+    bool ok = true;
+    uint32_t t = 0;
+    for (uint32_t seg = 0;; ++seg) {
+      const Item x = get_item(seg, ok);
+      if (x.item < 0) break;
+      const Where w = where_of<QT>(p, x.item);
+      const win::Tiles list{x.first, x.from, x.units};
+      const int g = w.chunk * p.GC + row_head, i = w.i0 + j * p.PT + row_pos;
+      const bool live = row_pos < p.PT && g < p.G && i < p.N;
+      const bool live_warp = __any_sync(0xffffffffu, live);
+      int lim = 0x7fffffff, low = 0;
+      if (live) {
+        lim = win::row_end(p.mask, x.len, p.N, i);
+        low = win::row_low(p.mask, x.len, p.N, i);
+      }
+      float m = -INFINITY, l = 0.f;
+      for (int n = x.u0; n < x.u1; ++n, ++t) {
+        if (!wait_warp(s_full(j), t & 1u)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after_sync();
+        if (!live_warp) {   // rows that are not there: in step with the others, and no more
+          tc_fence_before_sync();
+          mbar_arrive(s_free(j));
+          if (t > 0 && !wait_warp(p_free(j), (t - 1) & 1u)) {
+            ok = false;
+            break;
+          }
+          mbar_arrive(p_ready(j));
+          continue;
+        }
+        uint32_t sr[128];
+        tmem_load_row128(tS, sr);
+        tc_fence_before_sync();
+        mbar_arrive(s_free(j));
+        float* s = reinterpret_cast<float*>(sr);
+        const int n0 = list.at(n) * kBN;
+        if (!__all_sync(0xffffffffu, lim - n0 >= kBN && (n0 >= low || n0 + kBN <= p.mask.sinks))) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t bits = below(lim - n0, k) & (~below(low - n0, k) | below(p.mask.sinks - n0, k));
+#pragma unroll
+            for (int e = 0; e < 32; ++e) s[32 * k + e] = bits >> e & 1u ? s[32 * k + e] : -INFINITY;
+          }
+        }
+        const float m_tile = c * row_max128(s);
+        bool rescale = false;   // warp-uniform
+        float alpha = 1.f;
+        if (n == x.u0) {
+          m = m_tile;
+        } else if (__any_sync(0xffffffffu, m_tile > m + kRescaleLog2)) {
+          const float m_new = fmaxf(m, m_tile);
+          alpha = m == -INFINITY ? 0.f : ex2_approx(m - m_new);
+          l *= alpha;
+          m = m_new;
+          rescale = true;
+        }
+        const float base = m == -INFINITY ? 0.f : m;
+        const uint64_t cc = pack_f32x2(c, c);
+        const uint64_t mm = pack_f32x2(-base, -base);
+        float l0 = 0.f, l1 = 0.f, l2 = 0.f, l3 = 0.f;
+        auto exp_chunk = [&](int ch, uint32_t* pk) {
+#pragma unroll
+          for (int e = 0; e < 32; e += 4) {
+            const int k = 32 * ch + e;
+            float x0, x1, x2, x3;
+            ffma2(x0, x1, s[k], s[k + 1], cc, mm);
+            ffma2(x2, x3, s[k + 2], s[k + 3], cc, mm);
+            const float p0 = ex2_approx(x0), p1 = ex2_approx(x1), p2 = ex2_approx(x2), p3 = ex2_approx(x3);
+            fadd2(l0, l1, p0, p1);
+            fadd2(l2, l3, p2, p3);
+            pk[e >> 1] = pack_bf16x2(p0, p1);
+            pk[(e >> 1) + 1] = pack_bf16x2(p2, p3);
+          }
+        };
+        auto store_chunk = [&](int ch, const uint32_t* pk) { tmem_st_32x32b_x16(tP + 16 * ch, pk); };
+        constexpr int kEarly = C::kEarlyChunks;
+        uint32_t pe[16 * kEarly];
+#pragma unroll
+        for (int ch = 0; ch < kEarly; ++ch) exp_chunk(ch, pe + 16 * ch);
+        // P_j's buffer is free, and O_j may be rescaled, once the previous tile's product is done
+        if (t > 0 && !wait_warp(p_free(j), (t - 1) & 1u)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after_sync();
+#pragma unroll
+        for (int ch = 0; ch < kEarly; ++ch) store_chunk(ch, pe + 16 * ch);
+#pragma unroll
+        for (int ch = kEarly; ch < 4; ++ch) {
+          uint32_t pk[16];
+          exp_chunk(ch, pk);
+          store_chunk(ch, pk);
+        }
+        l += (l0 + l1) + (l2 + l3);
+        if (rescale) tmem_scale_row<DV>(tO, alpha);
+        tmem_wait_st();
+        tc_fence_before_sync();
+        mbar_arrive(p_ready(j));
+      }
+      if (!ok || !wait_warp(o_done(j), seg & 1u)) break;
+      tc_fence_after_sync();
+      // the item is written, or this CTA's piece of it
+      const bool first_piece = x.u0 == 0, whole = first_piece && x.u1 == x.units;
+      if (live_warp) {
+        const int hq = w.h * p.G + g;
+        bool bad = false;
+        if (!whole) {
+          const int64_t at = (int64_t(blockIdx.x) * 2 + first_piece) * C::kRows + j * kBM + row;
+#pragma unroll
+          for (int d = 0; d < DV; d += 16) {
+            uint32_t o[16];
+            tmem_ld_32x32b_x16(tO + d, o);
+            tmem_wait_ld();
+            reg_anchor_x16(o);
+            if (live) {
+              float4* dst = reinterpret_cast<float4*>(part_o + at * DV + d);
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                dst[e] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]),
+                                     __uint_as_float(o[4 * e + 3]));
+            }
+          }
+          if (live) part_ml[at] = make_float2(m, l);
+        } else {
+          const float inv = l == 0.f ? 0.f : 1.f / l;
+          __nv_bfloat16* orow = O + int64_t(w.b) * p.o_sb + int64_t(hq) * p.o_sh + int64_t(i) * p.o_sn;
+          if (lse != nullptr && live)
+            lse[(int64_t(w.b) * p.Hk * p.G + hq) * p.N + i] = l == 0.f ? -INFINITY : (m + lg2_approx(l)) * kLn2;
+#pragma unroll
+          for (int d = 0; d < DV; d += 16) {
+            uint32_t o[16];
+            tmem_ld_32x32b_x16(tO + d, o);
+            tmem_wait_ld();
+            reg_anchor_x16(o);
+            float y[16], top = 0.f;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              y[e] = __uint_as_float(o[e]) * inv;
+              top += y[e] * 0.f;   // not zero if one is not finite
+            }
+            if (live) {
+              bad |= top != 0.f;
+              uint32_t z[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) z[e] = pack_bf16x2(y[2 * e], y[2 * e + 1]);
+              reinterpret_cast<uint4*>(orow + d)[0] = make_uint4(z[0], z[1], z[2], z[3]);
+              reinterpret_cast<uint4*>(orow + d)[1] = make_uint4(z[4], z[5], z[6], z[7]);
+            }
+          }
+        }
+        bad = __any_sync(0xffffffffu, bad);
+        if (lane == 0 && first_piece) odd[int64_t(x.item) * 8 + warp] = bad;   // (a cut item's rows are looked at when joined)
+      }
+      tc_fence_before_sync();   // O is read: the next item's first product (after p_ready) may write it
+      __syncwarp();
+      if (lane == 0) mbar_arrive(item_empty(seg & 1));
+    }
+  }
+
+  // Teardown: the tensor core is quiet before TMEM is freed, on the abort path too.  Only the lane of the role
+  // waits: the others come here at the start, and their time would run out in a kernel longer than the limit.
+  if (warp == C::kMmaWarp0 && lane == 0) wait_quiesce(drain, 0, p.wait_limit_ns, &g_moa_window_tc_status);
+  tc_fence_before_sync();
+  __syncthreads();
+  if (warp == C::kMmaWarp0) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, C::kTmemCols);
+  }
+}
+
+// Joins the pieces of cut items, one warp a row, and computes rows again whose output is not finite: of the
+// joined ones, and of whole items that are marked.  CTA (x, y): eight rows of CTA x's cut, and of the marked
+// ones among items x, x + gridDim.x, ...
+template <int DK, int DV, int QT>
+__global__ void __launch_bounds__(256)
+window_tc_join_kernel(const __nv_bfloat16* Q, __nv_bfloat16* O, float* lse, const float* part_o, const float2* part_ml,
+                      const Cut* cuts, const uint8_t* odd, const Params p) {
+  constexpr int kRows = kBM * QT;
+  wait_for_previous();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = int(blockIdx.y) * 8 + warp;
+  const int tile = row / kBM, in_tile = row - tile * kBM;
+  const int row_pos = int(unsigned(in_tile) / unsigned(p.GC)), row_head = in_tile - row_pos * p.GC;
+  struct Row {
+    int b, h, hq, i;
+    bool live;
+  };
+  auto row_of = [&](int item) {
+    const Where w = where_of<QT>(p, item);
+    const int g = w.chunk * p.GC + row_head, i = w.i0 + tile * p.PT + row_pos;
+    return Row{w.b, w.h, w.h * p.G + g, i, row_pos < p.PT && g < p.G && i < p.N};
+  };
+  auto out = [&](const Row& r) { return O + int64_t(r.b) * p.o_sb + int64_t(r.hq) * p.o_sh + int64_t(r.i) * p.o_sn; };
+  auto again = [&](const Row& r) {
+    exact_row<DK, DV>(Q + int64_t(r.b) * p.q_sb + int64_t(r.hq) * p.q_sh + int64_t(r.i) * p.q_sn, out(r), p, r.b, r.h, r.i);
+  };
+  const Cut cut = cuts[blockIdx.x];
+  if (cut.pieces != 0) {
+    const Row r = row_of(cut.item);
+    if (r.live) {
+      auto place = [&](int k) -> int64_t { return ((int64_t(blockIdx.x) + k) * 2 + (k == 0)) * kRows + row; };
+      float M = -INFINITY;
+      for (int k = lane; k < cut.pieces; k += 32) M = fmaxf(M, part_ml[place(k)].x);
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+      const float base = M == -INFINITY ? 0.f : M;
+      float L = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+      for (int k = 0; k < cut.pieces; ++k) {
+        const float2 ml = part_ml[place(k)];
+        const float f = ex2_approx(ml.x - base);
+        L += f * ml.y;
+        if (lane * 4 < DV) {
+          const float4 v = *reinterpret_cast<const float4*>(part_o + place(k) * DV + lane * 4);
+          x[0] += f * v.x, x[1] += f * v.y, x[2] += f * v.z, x[3] += f * v.w;
+        }
+      }
+      const float inv = L == 0.f ? 0.f : 1.f / L;
+      bool bad = false;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[e] *= inv;
+        bad |= not_finite(x[e]);
+      }
+      if (lane * 4 < DV)
+        *reinterpret_cast<uint2*>(out(r) + lane * 4) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+      if (lse != nullptr && lane == 0)
+        lse[(int64_t(r.b) * p.Hk * p.G + r.hq) * p.N + r.i] = L == 0.f ? -INFINITY : (M + lg2_approx(L)) * kLn2;
+      __syncwarp();
+      if (__any_sync(0xffffffffu, bad)) again(r);
+    }
+  }
+  // whole items: one mark for each 32 rows
+  for (int64_t base = blockIdx.x; base < p.n_items; base += 32 * int64_t(gridDim.x)) {
+    const int64_t mine = base + lane * int64_t(gridDim.x);
+    uint32_t marked = __ballot_sync(0xffffffffu, mine < p.n_items && odd[mine * 8 + row / 32] == 1);
+    while (marked != 0) {
+      const int k = __ffs(marked) - 1;
+      marked &= marked - 1;
+      const int item = int(base + k * int64_t(gridDim.x));
+      const Row r = row_of(item);
+      if (!r.live) continue;
+      bool bad = false;
+      for (int e = lane; e < DV; e += 32) bad |= not_finite(__bfloat162float(out(r)[e]));
+      if (__any_sync(0xffffffffu, bad)) again(r);
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------
+// Host side
+// ------------------------------------------------------------------------------------------------
+int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+// How the rows of a key head are divided.
+struct Plan {
+  int64_t GC, chunks, PT, QT, n_tiles, n_items;
+  explicit Plan(const WindowArgs& a) {
+    const int64_t G = a.Hq / a.Hk;
+    GC = G < kBM ? G : kBM;
+    chunks = (G + GC - 1) / GC;
+    PT = kBM / GC;
+    QT = a.N > PT ? 2 : 1;
+    n_tiles = chunks * ((a.N + QT * PT - 1) / (QT * PT));
+    n_items = a.B * a.Hk * n_tiles;
+  }
+};
+
+// The workspace: pieces, cuts, marks of whole items.
+struct Work {
+  int64_t part_o, part_ml, cuts, odd, bytes;
+  Work(const WindowArgs& a, const Plan& plan, int sms) {
+    const int64_t rows = int64_t(sms) * 2 * kBM * plan.QT;
+    part_o = 0;
+    part_ml = part_o + rows * a.dv * 4;
+    cuts = part_ml + rows * 8;
+    odd = cuts + round_up(int64_t(sms) * sizeof(Cut), 256);
+    bytes = odd + round_up(plan.n_items * 8, 256);
+  }
+};
+
+// A tensor's stride as a tensor map has it: positive, whole 16 bytes, below 2^40 bytes.
+bool describable(int64_t stride, int64_t size) { return size == 1 || (stride > 0 && stride < (int64_t(1) << 39)); }
+uint64_t map_stride(int64_t stride, int64_t size) { return size == 1 ? 16 : uint64_t(stride) * 2; }
+
+template <int DK, int DV, int QT>
+int launch(const WindowArgs& a, const Plan& plan, int sms, char* msg, size_t msglen) {
+  using C = Cfg<DK, DV, QT>;
+  auto kern = window_tc_kernel<DK, DV, QT>;
+  cudaError_t e = ensure_smem_limit(reinterpret_cast<const void*>(kern), C::kSmemBytes);
+  if constexpr (QT == 2) {
+    static std::atomic<int> regs{-1};
+    if (e == cudaSuccess && regs.load(std::memory_order_relaxed) < 0) {
+      cudaFuncAttributes fa;
+      e = cudaFuncGetAttributes(&fa, reinterpret_cast<const void*>(kern));
+      if (e == cudaSuccess) regs.store(fa.numRegs, std::memory_order_relaxed);
+    }
+    if (e == cudaSuccess && regs.load(std::memory_order_relaxed) * C::kThreads < 256 * C::kRegsSoftmax + 128 * C::kRegsCtrl) {
+      snprintf(msg, msglen, "attention with a window: %d registers per thread, short of the register split", regs.load());
+      return 5;
+    }
+  }
+  if (e != cudaSuccess) {
+    snprintf(msg, msglen, "attention with a window: function attributes: %s", cudaGetErrorString(e));
+    return 5;
+  }
+  const Work w(a, plan, sms);
+  uint8_t* ws = static_cast<uint8_t*>(a.ws);
+  float* part_o = reinterpret_cast<float*>(ws + w.part_o);
+  float2* part_ml = reinterpret_cast<float2*>(ws + w.part_ml);
+  Cut* cuts = reinterpret_cast<Cut*>(ws + w.cuts);
+  uint8_t* odd = ws + w.odd;
+  const int64_t G = a.Hq / a.Hk;
+  Params p{};
+  p.q_sb = a.q.sb, p.q_sh = a.q.sh, p.q_sn = a.q.sn;
+  p.o_sb = a.o.sb, p.o_sh = a.o.sh, p.o_sn = a.o.sn;
+  p.kv = a.kv, p.lens = a.lens;
+  p.N = int(a.N), p.max_len = int(a.max_len), p.Hk = int(a.Hk), p.G = int(G);
+  p.GC = int(plan.GC), p.chunks = int(plan.chunks), p.PT = int(plan.PT);
+  p.n_tiles = int(plan.n_tiles), p.n_items = int(plan.n_items);
+  p.mask = win::Mask{a.window, a.sinks, a.causal};
+  p.c_log2 = a.scale * kLog2e;
+  p.wait_limit_ns = wait_limit_ns();
+  const bool paged = a.kv.table != nullptr;
+  p.box = kBN;
+  if (paged)
+    while (a.kv.page % p.box != 0) p.box /= 2;
+  CUtensorMap mq, mk, mv;
+  const uint64_t q_dims[5] = {DK, uint64_t(G), uint64_t(a.N), uint64_t(a.Hk), uint64_t(a.B)};
+  const uint64_t q_str[4] = {map_stride(a.q.sh, G), map_stride(a.q.sn, a.N), map_stride(G * a.q.sh, a.Hk),
+                             map_stride(a.q.sb, a.B)};
+  const uint32_t q_box[5] = {64, uint32_t(plan.GC), uint32_t(plan.PT), 1, 1};
+  const uint64_t rows = uint64_t(paged ? a.kv.page : a.max_len), outer = uint64_t(paged ? a.kv.n_pages : a.B);
+  const uint64_t k_dims[4] = {DK, rows, uint64_t(a.Hk), outer}, v_dims[4] = {DV, rows, uint64_t(a.Hk), outer};
+  const uint64_t k_str[3] = {map_stride(a.kv.k_sn, int64_t(rows)), map_stride(a.kv.k_sh, a.Hk), map_stride(a.kv.k_sb, int64_t(outer))};
+  const uint64_t v_str[3] = {map_stride(a.kv.v_sn, int64_t(rows)), map_stride(a.kv.v_sh, a.Hk), map_stride(a.kv.v_sb, int64_t(outer))};
+  const uint32_t kv_box[4] = {64, uint32_t(p.box), 1, 1};
+  if (!encode_bf16_map_nd(&mq, a.q.p, 5, q_dims, q_str, q_box, msg, msglen) ||
+      !encode_bf16_map_nd(&mk, a.kv.k, 4, k_dims, k_str, kv_box, msg, msglen) ||
+      !encode_bf16_map_nd(&mv, a.kv.v, 4, v_dims, v_str, kv_box, msg, msglen))
+    return 5;
+  // tiles of tokens, if every sequence is as long as max_len and no window hides any
+  const int64_t most_tiles = (a.max_len + kBN - 1) / kBN, most = plan.n_items * most_tiles;
+  const unsigned ctas = unsigned(most < sms ? most : sms);
+  // rows of an item that may be there
+  const int64_t positions = a.N < plan.PT ? a.N : plan.PT, live = QT == 2 ? C::kRows : positions * plan.GC;
+  e = launch_overlapped(kern, dim3(ctas), dim3(C::kThreads), C::kSmemBytes, a.stream, mq, mk, mv,
+                        static_cast<__nv_bfloat16*>(a.o.p), a.lse, part_o, part_ml, cuts, odd, p);
+  if (e == cudaSuccess)
+    e = launch_overlapped(window_tc_join_kernel<DK, DV, QT>, dim3(ctas, unsigned((live + 7) / 8)), dim3(256), 0, a.stream,
+                          static_cast<const __nv_bfloat16*>(a.q.p), static_cast<__nv_bfloat16*>(a.o.p), a.lse, part_o, part_ml,
+                          cuts, odd, p);
+  if (e != cudaSuccess) {
+    snprintf(msg, msglen, "attention with a window: %s", cudaGetErrorString(e));
+    return 5;
+  }
+  return 0;
+}
+
+template <int DK, int DV>
+int launch_rows(const WindowArgs& a, int sms, char* msg, size_t msglen) {
+  const Plan plan(a);
+  return plan.QT == 2 ? launch<DK, DV, 2>(a, plan, sms, msg, msglen) : launch<DK, DV, 1>(a, plan, sms, msg, msglen);
+}
+
+}  // namespace
+
+bool window_tc_takes(const WindowArgs& a) {
+  const int64_t G = a.Hq / a.Hk, rows = a.kv.table != nullptr ? a.kv.page : a.max_len;
+  const int64_t outer = a.kv.table != nullptr ? a.kv.n_pages : a.B;
+  return !a.f32 && a.scale >= 0.f && describable(a.q.sh, G) && describable(G * a.q.sh, a.Hk) && describable(a.q.sn, a.N) &&
+         describable(a.q.sb, a.B) && describable(a.kv.k_sn, rows) && describable(a.kv.k_sh, a.Hk) &&
+         describable(a.kv.k_sb, outer) && describable(a.kv.v_sn, rows) && describable(a.kv.v_sh, a.Hk) &&
+         describable(a.kv.v_sb, outer);
+}
+
+size_t window_tc_workspace(const WindowArgs& a, int sms) { return size_t(Work(a, Plan(a), sms).bytes); }
+
+int launch_window_tc(const WindowArgs& a, int sms, char* msg, size_t msglen) {
+  if (a.dk == 64) return a.dv == 64 ? launch_rows<64, 64>(a, sms, msg, msglen) : launch_rows<64, 128>(a, sms, msg, msglen);
+  return a.dv == 64 ? launch_rows<128, 64>(a, sms, msg, msglen) : launch_rows<128, 128>(a, sms, msg, msglen);
+}
+
+cudaError_t window_tc_read_and_clear_status(unsigned* value) {
+  cudaError_t e = cudaMemcpyFromSymbol(value, g_moa_window_tc_status, sizeof(unsigned));
+  if (e != cudaSuccess || *value == 0) return e;
+  const unsigned zero = 0;
+  return cudaMemcpyToSymbol(g_moa_window_tc_status, &zero, sizeof(unsigned));
+}
+
+}  // namespace moa
