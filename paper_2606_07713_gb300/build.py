@@ -24,7 +24,7 @@ LIB = os.path.join(BUILD, "libmoa_attn.so")
 SOURCES = ["moa_attn_api.cu", "attn_fwd_f32_cc.cu", "attn_fwd_bf16_tc.cu", "attn_bwd_bf16_tc.cu",
            "attn_bwd_f32_cc.cu", "qkv_proj_bf16_tc.cu", "moa_ops_api.cu", "qk_norm_rope.cu",
            "kv4_cache.cu", "kv4_attn.cu", "kv4_attn_tc.cu", "kv_append.cu", "window_fwd_cc.cu", "window_fwd_tc.cu",
-           "window_bwd_cc.cu"]
+           "window_bwd_cc.cu", "window_bwd_tc.cu"]
 BINDING = os.path.join(BUILD, "moa_torch.so")
 BINDING_SOURCE = "torch_binding.cpp"
 BINDING_TORCH = BINDING + ".torch"   # which PyTorch it was built against

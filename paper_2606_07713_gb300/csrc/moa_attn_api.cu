@@ -165,7 +165,7 @@ int read_status(const char* where) {
   cudaError_t (*const readers[])(unsigned*) = {
       bf16_read_and_clear_status, bwd_read_and_clear_status,  proj_read_and_clear_status,
       norm_read_and_clear_status, kv4_read_and_clear_status, kv4_attn_read_and_clear_status,
-      kv4_tc_read_and_clear_status, window_tc_read_and_clear_status, window_cc_read_and_clear_status, kv_append_read_and_clear_status};
+      kv4_tc_read_and_clear_status, window_tc_read_and_clear_status, window_bwd_read_and_clear_status, window_cc_read_and_clear_status, kv_append_read_and_clear_status};
   unsigned timeout = 0, index = 0;
   for (auto read : readers) {
     unsigned v = 0;

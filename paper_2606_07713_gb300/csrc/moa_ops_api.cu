@@ -615,7 +615,10 @@ int cache_call(const void* Q, const void* pool, const int32_t* pages, const int3
   return run_window(a, in, 4, out, workspace, workspace_bytes);
 }
 
-size_t window_bwd_workspace(const WindowBwdArgs& a) { return window_bwd_cc_workspace(a); }
+size_t window_bwd_workspace(const WindowBwdArgs& a) {
+  const size_t cc = window_bwd_cc_workspace(a), tc = a.f32 ? 0 : window_bwd_tc_workspace(a);
+  return cc > tc ? cc : tc;
+}
 
 void set_bwd_window(WindowBwdArgs& a, int64_t window, int64_t sinks) {
   a.window = window == 0 || window >= a.Nk ? win::kNoWindow : int(window);
@@ -636,7 +639,7 @@ int window_bwd_call(WindowBwdArgs& a, int64_t window, int64_t sinks, int dtype, 
   if (workspace_bytes < need)
     return api_fail(MOA_ERR_INVALID_ARG, "workspace too small: need %zu bytes, got %zu", need, workspace_bytes);
   char msg[256] = {0};
-  rc = launch_window_bwd_cc(a, msg, sizeof(msg));
+  rc = window_bwd_tc_takes(a) ? launch_window_bwd_tc(a, msg, sizeof(msg)) : launch_window_bwd_cc(a, msg, sizeof(msg));
   if (rc != MOA_OK) return api_fail(rc, "%s", msg);
   api_clear();
   return api_debug_check(a.stream);

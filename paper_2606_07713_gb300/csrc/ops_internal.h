@@ -163,6 +163,10 @@ struct WindowBwdArgs {
 };
 size_t window_bwd_cc_workspace(const WindowBwdArgs& a);
 int launch_window_bwd_cc(const WindowBwdArgs& a, char* msg, size_t msglen);
+// Tensor cores: bf16 tensors that tensor maps describe (window_bwd_tc.cu).
+bool window_bwd_tc_takes(const WindowBwdArgs& a);
+size_t window_bwd_tc_workspace(const WindowBwdArgs& a);
+int launch_window_bwd_tc(const WindowBwdArgs& a, char* msg, size_t msglen);
 
 // New keys and values into a 16- or 32-bit paged cache [n_pages, H, page, dk + dv], keys (and
 // queries, into oq) rotated on the way.
@@ -182,6 +186,7 @@ struct KvAppendArgs {
 int launch_kv_append(const KvAppendArgs& a, char* msg, size_t msglen);
 
 cudaError_t window_tc_read_and_clear_status(unsigned* value);
+cudaError_t window_bwd_read_and_clear_status(unsigned* value);
 cudaError_t window_cc_read_and_clear_status(unsigned* value);
 cudaError_t kv_append_read_and_clear_status(unsigned* value);
 

@@ -35,6 +35,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kKeysKv = 64, kRowsKv = 32;   // dkdv: tokens of a CTA, rows of a step
 constexpr int kRowsQ = 64, kKeysQ = 32;     // dq: rows of a CTA, tokens of a step
 constexpr int kThreads = 256;
+constexpr int64_t kMostPieces = 1216;       // of cut token tiles: eight for each SM
 
 struct Params {
   View q, k, v, o, go, dq, dk, dv;
@@ -425,9 +426,12 @@ Cut cut_of(const WindowBwdArgs& a) {
   if (want < 512) want = 512;
   if (want > rows) want = rows;
   c.piece_rows = (want + kRowsKv - 1) / kRowsKv * kRowsKv;
-  c.pieces = (rows + c.piece_rows - 1) / c.piece_rows;
   c.cut = windowed ? (int64_t(a.sinks) + kKeysKv - 1) / kKeysKv : c.n_kt;
   if (c.cut > c.n_kt) c.cut = c.n_kt;
+  // not more pieces than keep the machine busy: each is 64 rows of fp32 in the workspace (80 MB in all)
+  const int64_t bh = a.B * a.Hk, most = c.cut > 0 && bh * c.cut < kMostPieces ? kMostPieces / (bh * c.cut) : 1;
+  if ((rows + c.piece_rows - 1) / c.piece_rows > most) c.piece_rows = ((rows + most - 1) / most + kRowsKv - 1) / kRowsKv * kRowsKv;
+  c.pieces = (rows + c.piece_rows - 1) / c.piece_rows;
   if (c.pieces == 1) c.cut = 0;
   return c;
 }

@@ -1,0 +1,995 @@
+// Gradients of causal attention with a sliding window and first tokens that stay visible, bf16, on the
+// fifth-generation tensor cores (tcgen05 + TMEM + TMA), sm_103a.
+//
+// Mathematics, with P_ij = 2^(c s_ij - LSE_i log2 e) for the tokens j that row i sees (window.cuh), 0 for the
+// others, c = scale log2 e, and D_i = <dO_i, O_i>:
+//     dV_j = sum_i P_ij dO_i,   dS_ij = P_ij (<dO_i, v_j> - D_i),
+//     dQ_i = scale sum_j dS_ij k_j,   dK_j = scale sum_i dS_ij q_i,
+// the sums over i also over the query heads that share the key head.  P and dS are rounded to bf16 (operands of the
+// products), all sums are fp32 in TMEM.
+//
+//   delta  D and -LSE log2 e of every row, in tiles of 128 rows;
+//   dkdv   a CTA for 128 tokens of a key head and a piece of the row tiles that see them:
+//            S^T = K Q^T, dP^T = V dO^T, P^T and dS^T back into TMEM as bf16, dV += P^T dO, dK += dS^T Q;
+//   join   adds the pieces of cut token tiles, in order;
+//   dq     a CTA for 128 rows, over the token tiles that they see:
+//            S = Q K^T, dP = dO V^T, dS = P (dP - D), dQ += dS K.
+// dQ apart from dK and dV: seven tile products in place of five, but every sum stays within one CTA (no
+// atomics, the same bits every time).
+//
+// Rows of a key head are counted as in the forward kernel: row r of a 128-row tile is position r / GC, query
+// head r % GC of the group (TMA brings them in that order), so that a window's tiles hold few rows that are hidden, and
+// for a token the rows that see it are one range of a tile's columns, for a row the tokens two ranges.
+//
+// Pieces.  A token's rows are those of a window; a sink's are all later ones, which one CTA would walk over while the
+// others are done: token tiles with more row tiles than `piece` are cut.  `piece` is a window's row tiles, or less
+// where there are too few CTAs for the machine.
+//
+// CTA organisation of both tile kernels (one CTA an SM): 4P compute warps (warp w: TMEM lanes 32 (w % 4) .., columns
+// 128 / P (w / 4) .. of the score tiles; its bf16 values go back into the first half of its own columns), one warp
+// for TMEM and the products, one for the copies.  Waits are bounded; on expiry MOA_ERR_DEVICE_TIMEOUT is recorded and
+// every role leaves its loop.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <cstdio>
+
+#include "internal.h"
+#include "ops_internal.h"
+#include "ptx.cuh"
+#include "tc_common.cuh"
+#include "window.cuh"
+
+namespace moa {
+
+__device__ unsigned int g_moa_window_bwd_status = 0;
+
+namespace {
+
+using namespace ptx;
+using namespace tc;
+
+constexpr int kBlk = 128;
+constexpr int kTmemCols = 512;
+constexpr int kPanelBytes = 128 * 128;   // 64 bf16 columns of 128 rows, 128-byte swizzle
+constexpr int kVecBytes = kBlk * 4;
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct Params {
+  View q, k, v, o, go, dq, dk, dv;
+  const float* lse;
+  float* nl;      // [row tile][128] -LSE log2 e; -infinity for rows that are not there or see nothing
+  float* delta;   // alike: D
+  float* part;    // [cut tile][piece][128][DK + DV]
+  int B, Hk, G, N, Nk;
+  int GC, chunks, PT;   // heads of a row tile, chunks of heads, positions of a row tile
+  int n_pt;             // row tiles along the positions
+  int n_kt;             // token tiles
+  int cut, pieces, piece;   // the first `cut` token tiles come in up to `pieces` pieces of `piece` row tiles
+  int group;            // key heads whose token tiles are handed out in turn, longest first
+  win::Mask mask;
+  float c_log2, scale;
+  uint64_t wait_limit_ns;
+};
+
+// P column parts of the score tiles, 4P compute warps, then the warps of the products and of the copies.  P = 4
+// where the tile products are short (d_k + d_v = 128) and the exponentials dominate.
+template <int P>
+struct Warps {
+  static constexpr int kParts = P;
+  static constexpr int kCols = kBlk / P;
+  static constexpr int kComputeWarps = 4 * P;
+  static constexpr int kComputeThreads = 32 * kComputeWarps;
+  static constexpr int kThreads = kComputeThreads + 64;
+  static constexpr int kMmaWarp = kComputeWarps;
+  static constexpr int kLoadWarp = kComputeWarps + 1;
+};
+__host__ __device__ constexpr int parts_of(int dk, int dv) { return dk + dv <= 128 ? 4 : 2; }
+__host__ __device__ constexpr int ring_stages(int dk, int dv) { return dk + dv <= 128 ? 4 : (dk + dv <= 192 ? 3 : 2); }
+
+// TMEM column of step kk (16 rows of the reduction axis) of a bf16 operand that the column parts wrote.
+template <int COLS>
+__device__ __forceinline__ uint32_t part_col(int kk) {
+  return uint32_t((kk * 16 / COLS) * COLS + (kk * 16 % COLS) / 2);
+}
+template <int COLS>
+__device__ __forceinline__ void tmem_load_part(uint32_t taddr, uint32_t* r) {
+#pragma unroll
+  for (int c = 0; c < COLS; c += 32) tmem_ld_32x32b_x32(taddr + c, r + c);
+  tmem_wait_ld();
+#pragma unroll
+  for (int c = 0; c < COLS; c += 32) reg_anchor_x32(r + c);
+}
+template <int COLS>
+__device__ __forceinline__ void tmem_store_part(uint32_t taddr, const uint32_t* pk) {
+  if constexpr (COLS == 64)
+    tmem_st_32x32b_x32(taddr, pk);
+  else
+    tmem_st_32x32b_x16(taddr, pk);
+}
+__device__ __forceinline__ float4 lds_f32x4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+// Bits 32 w .. 32 w + 31 of the number with the lowest x bits set.
+__device__ __forceinline__ uint32_t below(int x, int w) {
+  const int n = x - 32 * w;
+  return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u;
+}
+
+// NCOLS fp32 TMEM columns of this thread's lane, times mul: as bf16 to dst, or as they are to part.
+template <int NCOLS>
+__device__ __forceinline__ void store_row(uint32_t taddr, float mul, __nv_bfloat16* dst, float* part, bool valid) {
+#pragma unroll
+  for (int c = 0; c < NCOLS; c += 32) {
+    uint32_t o[32];
+    tmem_ld_32x32b_x32(taddr + c, o);
+    tmem_wait_ld();
+    reg_anchor_x32(o);
+    if (!valid) continue;
+    if (part != nullptr) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        reinterpret_cast<float4*>(part + c)[i] = make_float4(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1]),
+                                                             __uint_as_float(o[4 * i + 2]), __uint_as_float(o[4 * i + 3]));
+    } else {
+      uint32_t w[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) w[i] = pack_bf16x2(__uint_as_float(o[2 * i]) * mul, __uint_as_float(o[2 * i + 1]) * mul);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        reinterpret_cast<uint4*>(dst + c)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    }
+  }
+}
+
+__device__ __forceinline__ __nv_bfloat16* row_of(const View& x, int b, int h, int n) {
+  return static_cast<__nv_bfloat16*>(x.p) + b * x.sb + h * x.sh + n * x.sn;
+}
+
+// Row tile t: its key head, chunk of heads and first position.
+struct RowTile {
+  int b, h, chunk, i0;
+};
+__device__ __forceinline__ RowTile row_tile(const Params& p, int64_t t) {
+  RowTile r;
+  const int64_t per = int64_t(p.chunks) * p.n_pt, bh = t / per;
+  const int rest = int(t - bh * per);
+  r.chunk = rest / p.n_pt;
+  r.i0 = (rest - r.chunk * p.n_pt) * p.PT;
+  r.b = int(bh / p.Hk), r.h = int(bh - int64_t(r.b) * p.Hk);
+  return r;
+}
+
+// ------------------------------------------------------------------------------------------------
+// D and -LSE log2 e: DV / 8 lanes a row
+// ------------------------------------------------------------------------------------------------
+template <int DV>
+__global__ void __launch_bounds__(256)
+window_delta_tc_kernel(const Params p, int64_t rows) {
+  constexpr int L = DV / 8;
+  wait_for_previous();
+  const int64_t r = (int64_t(blockIdx.x) * 256 + threadIdx.x) / L;
+  const int gl = threadIdx.x % L;
+  if (r >= rows) return;   // (rows are a multiple of 128: whole warps)
+  const int in_tile = int(r % kBlk), pos = in_tile / p.GC, head = in_tile - pos * p.GC;
+  const RowTile t = row_tile(p, r / kBlk);
+  const int g = t.chunk * p.GC + head, i = t.i0 + pos, hq = t.h * p.G + g;
+  const bool real = pos < p.PT && g < p.G && i < p.N;
+  float acc = 0.f;
+  if (real) {
+    const uint4 ov = *reinterpret_cast<const uint4*>(row_of(p.o, t.b, hq, i) + gl * 8);
+    const uint4 gv = *reinterpret_cast<const uint4*>(row_of(p.go, t.b, hq, i) + gl * 8);
+    const __nv_bfloat162* o2 = reinterpret_cast<const __nv_bfloat162*>(&ov);
+    const __nv_bfloat162* g2 = reinterpret_cast<const __nv_bfloat162*>(&gv);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float2 of = __bfloat1622float2(o2[e]), gf = __bfloat1622float2(g2[e]);
+      acc = fmaf(of.x, gf.x, acc);
+      acc = fmaf(of.y, gf.y, acc);
+    }
+  }
+#pragma unroll
+  for (int d = L / 2; d > 0; d >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, d);
+  if (gl == 0) {
+    float nl = -INFINITY;
+    if (real) {
+      const float l = p.lse[(int64_t(t.b) * p.Hk * p.G + hq) * p.N + i];
+      if (l != -INFINITY) nl = -l * kLog2e;
+    }
+    p.nl[r] = nl;
+    p.delta[r] = real ? acc : 0.f;
+  }
+}
+
+// ------------------------------------------------------------------------------------------------
+// dK and dV
+// ------------------------------------------------------------------------------------------------
+// The row tiles along the positions that see a token of tile kt: [first, first + n).
+struct Range {
+  int first, n;
+};
+__host__ __device__ __forceinline__ Range rows_of_tokens(const win::Mask& m, int kt, int N, int Nk, int PT) {
+  const int off = Nk - N, k0 = kt * kBlk, k1 = k0 + kBlk < Nk ? k0 + kBlk : Nk;
+  const int64_t i0 = k0 > off ? int64_t(k0) - off : 0;
+  int64_t i1 = N;
+  if (k0 >= m.sinks && m.window != win::kNoWindow) {
+    const int64_t n = int64_t(k1) - 1 + m.window - off;
+    i1 = n < 0 ? 0 : n < i1 ? n : i1;
+  }
+  Range r;
+  r.first = int(i0 / PT);
+  r.n = i1 > i0 ? int((i1 + PT - 1) / PT) - r.first : 0;
+  return r;
+}
+
+template <int DK, int DV>
+struct KvCfg : Warps<parts_of(DK, DV)> {
+  static constexpr int kKBytes = kBlk * DK * 2, kVBytes = kBlk * DV * 2;
+  static constexpr int kQBytes = kBlk * DK * 2, kGBytes = kBlk * DV * 2;
+  // stage: Q tile, dO tile, -L and D of its 128 rows
+  static constexpr int kStageBytes = kQBytes + kGBytes + 2 * kVecBytes;
+  static constexpr int kStages = ring_stages(DK, DV);
+  static constexpr int kOffK = 0, kOffV = kKBytes, kOffStage = kKBytes + kVBytes;
+  // barriers: full[NS], empty[NS], kv_full, s_full, dp_full, p_ready, ds_ready, acc_done
+  static constexpr int kNumBars = 2 * kStages + 6;
+  static constexpr int kOffBar = kOffStage + kStages * kStageBytes;
+  static constexpr int kOffMisc = kOffBar + kNumBars * 8;
+  static constexpr int kSmemBytes = kOffMisc + 16 + 1024;
+  static constexpr uint32_t kTmemS = 0, kTmemDP = 128, kTmemDV = 256, kTmemDK = 256 + DV;
+  static_assert(kStageBytes % 1024 == 0, "stage alignment");
+  static_assert(kTmemDK + DK <= kTmemCols, "TMEM budget");
+  static_assert(kSmemBytes <= 232448, "shared memory budget");
+};
+
+// A CTA's work: token tile kt of a key head, row tiles [t0, t0 + n) of the list (chunk after chunk).
+struct KvItem {
+  int b, h, kt, piece;
+  bool whole;   // not cut: the result is written, not a piece of it
+};
+__host__ __device__ __forceinline__ KvItem kv_item(const Params& p, int64_t x) {
+  // groups of key heads; within one, token tile after token tile (the first have the most rows), head after head
+  const int per = p.cut * p.pieces + p.n_kt - p.cut;   // items of a key head
+  const int64_t heads = int64_t(p.B) * p.Hk, first = x / (int64_t(per) * p.group) * p.group;
+  const int64_t g = heads - first < p.group ? heads - first : p.group;
+  const int64_t rest = x - first * per, item = rest / g, bh = first + (rest - item * g);
+  KvItem k;
+  k.b = int(bh / p.Hk), k.h = int(bh - int64_t(k.b) * p.Hk);
+  const int64_t n_cut = int64_t(p.cut) * p.pieces;
+  k.whole = item >= n_cut;
+  k.kt = k.whole ? int(item - n_cut) + p.cut : int(item / p.pieces);
+  k.piece = k.whole ? 0 : int(item - int64_t(k.kt) * p.pieces);
+  return k;
+}
+
+template <int DK, int DV>
+__global__ void __launch_bounds__(KvCfg<DK, DV>::kThreads, 1)
+window_dkdv_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                      const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmG, const Params p) {
+  using C = KvCfg<DK, DV>;
+  constexpr int kCols = C::kCols;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  const uint32_t sK = smem_u32(smem + C::kOffK), sV = smem_u32(smem + C::kOffV), sStage = smem_u32(smem + C::kOffStage);
+  const uint32_t bar0 = smem_u32(smem + C::kOffBar);
+  auto full_bar = [&](int s) { return bar0 + 8u * s; };
+  auto empty_bar = [&](int s) { return bar0 + 8u * (C::kStages + s); };
+  const uint32_t kv_full = bar0 + 8u * (2 * C::kStages);
+  const uint32_t s_full = kv_full + 8, dp_full = kv_full + 16, p_ready = kv_full + 24;
+  const uint32_t ds_ready = kv_full + 32, acc_done = kv_full + 40;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::kOffMisc);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::kOffMisc + 4);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const WaitCtl wc{abort_flag, p.wait_limit_ns, 0u, &g_moa_window_bwd_status};
+
+  const KvItem it = kv_item(p, blockIdx.x);
+  const int k0 = it.kt * kBlk;
+  const Range range = rows_of_tokens(p.mask, it.kt, p.N, p.Nk, p.PT);
+  const int all = range.n * p.chunks;
+  const int t0 = it.whole ? 0 : it.piece * p.piece;
+  const int n_t = it.whole ? all : all - t0 < p.piece ? all - t0 : p.piece;
+  if (n_t <= 0 && !it.whole) return;   // the join adds what pieces there are
+  const int64_t bh = int64_t(it.b) * p.Hk + it.h;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < C::kStages; ++s) {
+      mbar_init(full_bar(s), 1);
+      mbar_init(empty_bar(s), 1);
+    }
+    mbar_init(kv_full, 1);
+    mbar_init(s_full, 1);
+    mbar_init(dp_full, 1);
+    mbar_init(p_ready, C::kComputeThreads);
+    mbar_init(ds_ready, C::kComputeThreads);
+    mbar_init(acc_done, 1);
+    *abort_flag = 0;
+    fence_barrier_init();
+  }
+  if (warp == C::kMmaWarp) {
+    tmem_alloc(smem_u32(tmem_slot), kTmemCols);
+    tmem_relinquish();
+  }
+  if (p.GC * p.PT < kBlk) {   // rows of a tile that no copy fills
+    for (int x = threadIdx.x; x < C::kStages * C::kStageBytes / 16; x += C::kThreads)
+      reinterpret_cast<uint4*>(smem + C::kOffStage)[x] = make_uint4(0, 0, 0, 0);
+    fence_proxy_async_smem();
+  }
+  wait_for_previous();
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = *tmem_slot;
+
+  if (warp == C::kLoadWarp) {
+    // ---------------------------------------------------------------- TMA producer
+    if (lane == 0 && n_t > 0) {
+      tma_prefetch_desc(&tmQ);
+      tma_prefetch_desc(&tmK);
+      tma_prefetch_desc(&tmV);
+      tma_prefetch_desc(&tmG);
+      mbar_arrive_expect_tx(kv_full, C::kKBytes + C::kVBytes);
+#pragma unroll
+      for (int q = 0; q < DK / 64; ++q) tma_load_4d(sK + q * kPanelBytes, &tmK, kv_full, q * 64, k0, it.h, it.b);
+#pragma unroll
+      for (int q = 0; q < DV / 64; ++q) tma_load_4d(sV + q * kPanelBytes, &tmV, kv_full, q * 64, k0, it.h, it.b);
+      int slot = 0;
+      uint32_t phase = 0, issued = 0, issued_phase = 0;
+      bool aborted = false;
+      int chunk = t0 / range.n, pt = range.first + (t0 - chunk * range.n);
+      const uint32_t bytes = (DK + DV) * 2 * p.GC * p.PT + 2 * kVecBytes;
+      for (int i = 0; i < n_t; ++i) {
+        if (!wait_bounded(empty_bar(slot), phase ^ 1u, wc)) {
+          aborted = true;
+          break;
+        }
+        issued |= 1u << slot;
+        issued_phase = (issued_phase & ~(1u << slot)) | (phase << slot);
+        const uint32_t st = sStage + slot * C::kStageBytes;
+        mbar_arrive_expect_tx(full_bar(slot), bytes);
+#pragma unroll
+        for (int q = 0; q < DK / 64; ++q)
+          tma_load_5d(st + q * kPanelBytes, &tmQ, full_bar(slot), q * 64, chunk * p.GC, pt * p.PT, it.h, it.b);
+#pragma unroll
+        for (int q = 0; q < DV / 64; ++q)
+          tma_load_5d(st + C::kQBytes + q * kPanelBytes, &tmG, full_bar(slot), q * 64, chunk * p.GC, pt * p.PT, it.h, it.b);
+        const int64_t vrow = ((bh * p.chunks + chunk) * p.n_pt + pt) * kBlk;
+        bulk_load(st + C::kQBytes + C::kGBytes, p.nl + vrow, kVecBytes, full_bar(slot));
+        bulk_load(st + C::kQBytes + C::kGBytes + kVecBytes, p.delta + vrow, kVecBytes, full_bar(slot));
+        if (++pt == range.first + range.n) {
+          pt = range.first;
+          ++chunk;
+        }
+        if (++slot == C::kStages) {
+          slot = 0;
+          phase ^= 1u;
+        }
+      }
+      if (aborted || *abort_flag) {
+        wait_quiesce(kv_full, 0, p.wait_limit_ns, &g_moa_window_bwd_status);
+        for (int sl = 0; sl < C::kStages; ++sl)
+          if (issued & (1u << sl)) wait_quiesce(full_bar(sl), (issued_phase >> sl) & 1u, p.wait_limit_ns, &g_moa_window_bwd_status);
+      }
+    }
+  } else if (warp == C::kMmaWarp) {
+    // ---------------------------------------------------------------- MMA issuer
+    if (lane == 0) {
+      constexpr uint32_t kIdescS = make_idesc(kBlk, kBlk, false);
+      constexpr uint32_t kIdescDV = make_idesc(kBlk, DV, true);
+      constexpr uint32_t kIdescDK = make_idesc(kBlk, DK, true);
+      const uint32_t tS = tmem + C::kTmemS, tDP = tmem + C::kTmemDP;
+      const uint32_t tDV = tmem + C::kTmemDV, tDK = tmem + C::kTmemDK;
+      int slot = 0;
+      uint32_t phase = 0;
+      // S^T = K Q^T: M = 128 tokens, N = 128 rows, both operands K-major
+      auto issue_s = [&](uint32_t sQ) {
+#pragma unroll
+        for (int kk = 0; kk < DK / 16; ++kk) {
+          const uint32_t off = (kk >> 2) * kPanelBytes + (kk & 3) * 32;
+          mma_f16_ss(tS, make_sdesc_sw128(sK + off, 16, 1024), make_sdesc_sw128(sQ + off, 16, 1024), kIdescS, kk > 0 ? 1u : 0u);
+        }
+        mma_commit(s_full);
+      };
+      // dP^T = V dO^T
+      auto issue_dp = [&](uint32_t sG) {
+#pragma unroll
+        for (int kk = 0; kk < DV / 16; ++kk) {
+          const uint32_t off = (kk >> 2) * kPanelBytes + (kk & 3) * 32;
+          mma_f16_ss(tDP, make_sdesc_sw128(sV + off, 16, 1024), make_sdesc_sw128(sG + off, 16, 1024), kIdescS, kk > 0 ? 1u : 0u);
+        }
+        mma_commit(dp_full);
+      };
+      auto stage = [&](int st) { return sStage + st * C::kStageBytes; };
+      // S(0) dP(0) | dV(0) S(1) dK(0) dP(1) | dV(1) S(2) dK(1) dP(2) | ...: the scores of tile i + 1 are ready when
+      // the compute warps finish dS of tile i.  S(i + 1) overwrites the columns of P^T(i) only after dV(i), and
+      // dP(i + 1) those of dS^T(i) only after dK(i), both issued earlier (products of one CTA complete in order).
+      bool ok = n_t > 0 && wait_bounded(kv_full, 0, wc) && wait_bounded(full_bar(0), 0, wc);
+      if (ok) {
+        tc_fence_after_sync();
+        issue_s(stage(0));
+        issue_dp(stage(0) + C::kQBytes);
+      }
+      for (int i = 0; ok && i < n_t; ++i) {
+        const int st = slot;
+        if (++slot == C::kStages) {
+          slot = 0;
+          phase ^= 1u;
+        }
+        const uint32_t sQ = stage(st), sG = sQ + C::kQBytes;
+        const uint32_t par = uint32_t(i) & 1u;
+        // dV += P^T dO: A from TMEM, B = dO tile MN-major
+        ok = wait_bounded(p_ready, par, wc);
+        if (!ok) break;
+        tc_fence_after_sync();
+#pragma unroll
+        for (int kk = 0; kk < kBlk / 16; ++kk)
+          mma_f16_ts(tDV, tS + part_col<kCols>(kk), make_sdesc_sw128(sG + kk * 2048, kPanelBytes, 1024), kIdescDV,
+                     (kk > 0 || i > 0) ? 1u : 0u);
+        const bool more = i + 1 < n_t;
+        if (more) {
+          ok = wait_bounded(full_bar(slot), phase, wc);
+          if (!ok) break;
+          tc_fence_after_sync();
+          issue_s(stage(slot));
+        }
+        // dK += dS^T Q (the scale comes at the end)
+        ok = wait_bounded(ds_ready, par, wc);
+        if (!ok) break;
+        tc_fence_after_sync();
+#pragma unroll
+        for (int kk = 0; kk < kBlk / 16; ++kk)
+          mma_f16_ts(tDK, tDP + part_col<kCols>(kk), make_sdesc_sw128(sQ + kk * 2048, kPanelBytes, 1024), kIdescDK,
+                     (kk > 0 || i > 0) ? 1u : 0u);
+        mma_commit(empty_bar(st));
+        if (more) issue_dp(stage(slot) + C::kQBytes);
+      }
+      // arrives once everything issued is complete, on the abort path too
+      mma_commit(acc_done);
+    }
+  } else {
+    // ---------------------------------------------------------------- compute warps
+    const int part = warp >> 2;
+    const int lane_base = (warp & 3) * 32, row = lane_base + lane;
+    const uint32_t lanes = uint32_t(lane_base) << 16;
+    const uint32_t tS = tmem + lanes + C::kTmemS + part * kCols;
+    const uint32_t tDP = tmem + lanes + C::kTmemDP + part * kCols;
+    const uint64_t cc = pack_f32x2(p.c_log2, p.c_log2);
+    const int key = k0 + row;
+    const bool bounded = p.mask.window != win::kNoWindow && key >= p.mask.sinks;   // seen by a window's rows only
+    int slot = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    int pt = n_t > 0 ? range.first + t0 % range.n : 0;
+    auto wait_warp = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_bounded(bar, parity, wc)) != 0; };
+    for (int i = 0; i < n_t; ++i) {
+      const int st = slot;
+      const uint32_t par = uint32_t(i) & 1u;
+      // -L and D came with the tiles: the wait for the stage makes them visible to this thread
+      ok = wait_warp(full_bar(st), phase) && wait_warp(s_full, par);
+      if (++slot == C::kStages) {
+        slot = 0;
+        phase ^= 1u;
+      }
+      if (!ok) break;
+      tc_fence_after_sync();
+      const uint32_t nl4 = sStage + st * C::kStageBytes + C::kQBytes + C::kGBytes + part * kCols * 4;
+      const uint32_t d4 = nl4 + kBlk * 4;
+      // the rows that see the token: columns [from, upto) of this part
+      const int p0 = pt * p.PT + (p.Nk - p.N);
+      if (++pt == range.first + range.n) pt = range.first;
+      const int ahead = key - p0;   // positions of the tile before the token's own
+      int from = ahead <= 0 ? 0 : ahead >= p.PT ? kBlk : ahead * p.GC, upto = kBlk;
+      if (bounded) {
+        const int64_t left = int64_t(ahead) + p.mask.window;
+        upto = left <= 0 ? 0 : left >= p.PT ? kBlk : int(left) * p.GC;
+      }
+      from -= part * kCols, upto -= part * kCols;
+      const bool full = __all_sync(0xffffffffu, from <= 0 && upto >= kCols);
+      uint32_t r[kCols];
+      tmem_load_part<kCols>(tS, r);
+      float w[kCols];
+#pragma unroll
+      for (int q = 0; q < kCols; q += 4) {
+        const float4 l = lds_f32x4(nl4 + q * 4);
+        ffma2(w[q], w[q + 1], __uint_as_float(r[q]), __uint_as_float(r[q + 1]), cc, pack_f32x2(l.x, l.y));
+        ffma2(w[q + 2], w[q + 3], __uint_as_float(r[q + 2]), __uint_as_float(r[q + 3]), cc, pack_f32x2(l.z, l.w));
+      }
+      if (!full) {
+#pragma unroll
+        for (int k = 0; k < kCols / 32; ++k) {
+          const uint32_t bits = below(upto, k) & ~below(from, k);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) w[32 * k + e] = bits >> e & 1u ? w[32 * k + e] : -INFINITY;
+        }
+      }
+      uint32_t pk[kCols / 2];
+#pragma unroll
+      for (int q = 0; q < kCols; q += 2) {
+        w[q] = ex2_approx(w[q]);
+        w[q + 1] = ex2_approx(w[q + 1]);
+        pk[q >> 1] = pack_bf16x2(w[q], w[q + 1]);
+      }
+      tmem_store_part<kCols>(tS, pk);
+      tmem_wait_st();
+      tc_fence_before_sync();
+      mbar_arrive(p_ready);
+      ok = wait_warp(dp_full, par);
+      if (!ok) break;
+      tc_fence_after_sync();
+      tmem_load_part<kCols>(tDP, r);
+#pragma unroll
+      for (int q = 0; q < kCols; q += 4) {
+        const float4 d = lds_f32x4(d4 + q * 4);
+        const float s0 = w[q] * (__uint_as_float(r[q]) - d.x);
+        const float s1 = w[q + 1] * (__uint_as_float(r[q + 1]) - d.y);
+        const float s2 = w[q + 2] * (__uint_as_float(r[q + 2]) - d.z);
+        const float s3 = w[q + 3] * (__uint_as_float(r[q + 3]) - d.w);
+        pk[q >> 1] = pack_bf16x2(s0, s1);
+        pk[(q >> 1) + 1] = pack_bf16x2(s2, s3);
+      }
+      tmem_store_part<kCols>(tDP, pk);
+      tmem_wait_st();
+      tc_fence_before_sync();
+      mbar_arrive(ds_ready);
+    }
+    // The first half of the parts write dV, the others scale dK, each a slice of the columns.
+    const bool valid = key < p.Nk;
+    constexpr int kHalf = C::kParts / 2, wv = DV / kHalf, wk = DK / kHalf;
+    if (n_t <= 0) {   // tokens that no row sees
+      if (valid) {
+        uint4* dst = reinterpret_cast<uint4*>(part < kHalf ? row_of(p.dv, it.b, it.h, key) + part * wv
+                                                           : row_of(p.dk, it.b, it.h, key) + (part - kHalf) * wk);
+        for (int e = 0; e < (part < kHalf ? wv : wk) / 8; ++e) dst[e] = make_uint4(0, 0, 0, 0);
+      }
+    } else if (ok && wait_warp(acc_done, 0)) {
+      tc_fence_after_sync();
+      float* piece = it.whole ? nullptr : p.part + (((bh * p.cut + it.kt) * p.pieces + it.piece) * kBlk + row) * (DK + DV);
+      if (part < kHalf)
+        store_row<wv>(tmem + lanes + C::kTmemDV + part * wv, 1.f, row_of(p.dv, it.b, it.h, valid ? key : 0) + part * wv,
+                      piece ? piece + DK + part * wv : nullptr, valid);
+      else
+        store_row<wk>(tmem + lanes + C::kTmemDK + (part - kHalf) * wk, p.scale,
+                      row_of(p.dk, it.b, it.h, valid ? key : 0) + (part - kHalf) * wk,
+                      piece ? piece + (part - kHalf) * wk : nullptr, valid);
+    }
+  }
+
+  if (warp == C::kMmaWarp && lane == 0) wait_quiesce(acc_done, 0, p.wait_limit_ns, &g_moa_window_bwd_status);
+  tc_fence_before_sync();
+  __syncthreads();
+  if (warp == C::kMmaWarp) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+// Adds the pieces of cut token tiles: four features of a token a thread.
+template <int DK, int DV>
+__global__ void __launch_bounds__(256)
+window_dkdv_tc_join_kernel(const Params p, int64_t n) {
+  wait_for_previous();
+  constexpr int kQuads = (DK + DV) / 4;
+  const int64_t x = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  if (x >= n) return;
+  const int64_t row = x / kQuads;   // (key head, tile, token)
+  const int c = int(x - row * kQuads) * 4;
+  const int64_t tile = row / kBlk, bh = tile / p.cut;
+  const int j = int(row - tile * kBlk), kt = int(tile - bh * p.cut);
+  const int b = int(bh / p.Hk), h = int(bh - int64_t(b) * p.Hk), key = kt * kBlk + j;
+  if (key >= p.Nk) return;
+  const int all = rows_of_tokens(p.mask, kt, p.N, p.Nk, p.PT).n * p.chunks;
+  const int pieces = (all + p.piece - 1) / p.piece;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int i = 0; i < pieces; ++i) {
+    const float4 v = *reinterpret_cast<const float4*>(p.part + ((tile * p.pieces + i) * kBlk + j) * (DK + DV) + c);
+    s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+  }
+  const float mul = c < DK ? p.scale : 1.f;
+  __nv_bfloat16* dst = c < DK ? row_of(p.dk, b, h, key) + c : row_of(p.dv, b, h, key) + (c - DK);
+  *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(s.x * mul, s.y * mul), pack_bf16x2(s.z * mul, s.w * mul));
+}
+
+// ------------------------------------------------------------------------------------------------
+// dQ
+// ------------------------------------------------------------------------------------------------
+template <int DK, int DV>
+struct QCfg : Warps<parts_of(DK, DV)> {
+  static constexpr int kQBytes = kBlk * DK * 2, kGBytes = kBlk * DV * 2;
+  static constexpr int kKBytes = kBlk * DK * 2, kVBytes = kBlk * DV * 2;
+  static constexpr int kStageBytes = kKBytes + kVBytes;
+  static constexpr int kStages = ring_stages(DK, DV);
+  static constexpr int kOffQ = 0, kOffG = kQBytes, kOffStage = kQBytes + kGBytes;
+  // barriers: full[NS], empty[NS], q_full, s_full, dp_full, ds_ready, acc_done, s_free
+  static constexpr int kNumBars = 2 * kStages + 6;
+  static constexpr int kOffBar = kOffStage + kStages * kStageBytes;
+  static constexpr int kOffMisc = kOffBar + kNumBars * 8;
+  static constexpr int kSmemBytes = kOffMisc + 16 + 1024;
+  static constexpr uint32_t kTmemS = 0, kTmemDP = 128, kTmemDQ = 256;
+  static_assert(kTmemDQ + DK <= kTmemCols, "TMEM budget");
+  static_assert(kSmemBytes <= 232448, "shared memory budget");
+};
+
+template <int DK, int DV>
+__global__ void __launch_bounds__(QCfg<DK, DV>::kThreads, 1)
+window_dq_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                    const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmG, const Params p) {
+  using C = QCfg<DK, DV>;
+  constexpr int kCols = C::kCols;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  const uint32_t sQ = smem_u32(smem + C::kOffQ), sG = smem_u32(smem + C::kOffG), sStage = smem_u32(smem + C::kOffStage);
+  const uint32_t bar0 = smem_u32(smem + C::kOffBar);
+  auto full_bar = [&](int s) { return bar0 + 8u * s; };
+  auto empty_bar = [&](int s) { return bar0 + 8u * (C::kStages + s); };
+  const uint32_t q_full = bar0 + 8u * (2 * C::kStages);
+  const uint32_t s_full = q_full + 8, dp_full = q_full + 16, ds_ready = q_full + 24;
+  const uint32_t acc_done = q_full + 32, s_free = q_full + 40;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::kOffMisc);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::kOffMisc + 4);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const WaitCtl wc{abort_flag, p.wait_limit_ns, 0u, &g_moa_window_bwd_status};
+
+  // the last positions, which see the most without a window, come first
+  const int64_t per = int64_t(p.chunks) * p.n_pt, group = blockIdx.x / per;
+  const int64_t tile_id = group * per + (per - 1 - (blockIdx.x - group * per));
+  const RowTile t = row_tile(p, tile_id);
+  const int i1 = t.i0 + p.PT - 1 < p.N ? t.i0 + p.PT - 1 : p.N - 1;
+  const win::Tiles list = win::tiles_of(p.mask, p.Nk, p.N, t.i0, i1, kBlk);
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < C::kStages; ++s) {
+      mbar_init(full_bar(s), 1);
+      mbar_init(empty_bar(s), 1);
+    }
+    mbar_init(q_full, 1);
+    mbar_init(s_full, 1);
+    mbar_init(dp_full, 1);
+    mbar_init(ds_ready, C::kComputeThreads);
+    mbar_init(acc_done, 1);
+    mbar_init(s_free, C::kComputeThreads);
+    *abort_flag = 0;
+    fence_barrier_init();
+  }
+  if (warp == C::kMmaWarp) {
+    tmem_alloc(smem_u32(tmem_slot), kTmemCols);
+    tmem_relinquish();
+  }
+  if (p.GC * p.PT < kBlk) {   // rows that no copy fills
+    for (int x = threadIdx.x; x < (C::kQBytes + C::kGBytes) / 16; x += C::kThreads)
+      reinterpret_cast<uint4*>(smem)[x] = make_uint4(0, 0, 0, 0);
+    fence_proxy_async_smem();
+  }
+  wait_for_previous();
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = *tmem_slot;
+
+  if (warp == C::kLoadWarp) {
+    // ---------------------------------------------------------------- TMA producer
+    if (lane == 0 && list.n > 0) {
+      tma_prefetch_desc(&tmQ);
+      tma_prefetch_desc(&tmK);
+      tma_prefetch_desc(&tmV);
+      tma_prefetch_desc(&tmG);
+      mbar_arrive_expect_tx(q_full, (DK + DV) * 2 * p.GC * p.PT);
+#pragma unroll
+      for (int q = 0; q < DK / 64; ++q) tma_load_5d(sQ + q * kPanelBytes, &tmQ, q_full, q * 64, t.chunk * p.GC, t.i0, t.h, t.b);
+#pragma unroll
+      for (int q = 0; q < DV / 64; ++q) tma_load_5d(sG + q * kPanelBytes, &tmG, q_full, q * 64, t.chunk * p.GC, t.i0, t.h, t.b);
+      int slot = 0;
+      uint32_t phase = 0, issued = 0, issued_phase = 0;
+      bool aborted = false;
+      for (int j = 0; j < list.n; ++j) {
+        if (!wait_bounded(empty_bar(slot), phase ^ 1u, wc)) {
+          aborted = true;
+          break;
+        }
+        issued |= 1u << slot;
+        issued_phase = (issued_phase & ~(1u << slot)) | (phase << slot);
+        const uint32_t st = sStage + slot * C::kStageBytes;
+        mbar_arrive_expect_tx(full_bar(slot), C::kStageBytes);
+        const int n0 = list.at(j) * kBlk;
+#pragma unroll
+        for (int q = 0; q < DK / 64; ++q) tma_load_4d(st + q * kPanelBytes, &tmK, full_bar(slot), q * 64, n0, t.h, t.b);
+#pragma unroll
+        for (int q = 0; q < DV / 64; ++q)
+          tma_load_4d(st + C::kKBytes + q * kPanelBytes, &tmV, full_bar(slot), q * 64, n0, t.h, t.b);
+        if (++slot == C::kStages) {
+          slot = 0;
+          phase ^= 1u;
+        }
+      }
+      if (aborted || *abort_flag) {
+        wait_quiesce(q_full, 0, p.wait_limit_ns, &g_moa_window_bwd_status);
+        for (int sl = 0; sl < C::kStages; ++sl)
+          if (issued & (1u << sl)) wait_quiesce(full_bar(sl), (issued_phase >> sl) & 1u, p.wait_limit_ns, &g_moa_window_bwd_status);
+      }
+    }
+  } else if (warp == C::kMmaWarp) {
+    // ---------------------------------------------------------------- MMA issuer
+    if (lane == 0) {
+      constexpr uint32_t kIdescS = make_idesc(kBlk, kBlk, false);
+      constexpr uint32_t kIdescDQ = make_idesc(kBlk, DK, true);
+      const uint32_t tS = tmem + C::kTmemS, tDP = tmem + C::kTmemDP, tDQ = tmem + C::kTmemDQ;
+      int slot = 0;
+      uint32_t phase = 0;
+      auto stage = [&](int st) { return sStage + st * C::kStageBytes; };
+      auto issue_s = [&](uint32_t sK) {   // S = Q K^T
+#pragma unroll
+        for (int kk = 0; kk < DK / 16; ++kk) {
+          const uint32_t off = (kk >> 2) * kPanelBytes + (kk & 3) * 32;
+          mma_f16_ss(tS, make_sdesc_sw128(sQ + off, 16, 1024), make_sdesc_sw128(sK + off, 16, 1024), kIdescS, kk > 0 ? 1u : 0u);
+        }
+        mma_commit(s_full);
+      };
+      auto issue_dp = [&](uint32_t sV) {   // dP = dO V^T
+#pragma unroll
+        for (int kk = 0; kk < DV / 16; ++kk) {
+          const uint32_t off = (kk >> 2) * kPanelBytes + (kk & 3) * 32;
+          mma_f16_ss(tDP, make_sdesc_sw128(sG + off, 16, 1024), make_sdesc_sw128(sV + off, 16, 1024), kIdescS, kk > 0 ? 1u : 0u);
+        }
+        mma_commit(dp_full);
+      };
+      // S(0) dP(0) | S(1) dQ(0) dP(1) | S(2) dQ(1) dP(2) | ...: S(j + 1) goes as soon as the compute warps hold S(j)
+      // in registers (s_free); dP(j + 1) overwrites the columns of dS(j) only after dQ(j), issued earlier.
+      bool ok = list.n > 0 && wait_bounded(q_full, 0, wc) && wait_bounded(full_bar(0), 0, wc);
+      if (ok) {
+        tc_fence_after_sync();
+        issue_s(stage(0));
+        issue_dp(stage(0) + C::kKBytes);
+      }
+      for (int j = 0; ok && j < list.n; ++j) {
+        const int st = slot;
+        if (++slot == C::kStages) {
+          slot = 0;
+          phase ^= 1u;
+        }
+        const uint32_t par = uint32_t(j) & 1u;
+        const bool more = j + 1 < list.n;
+        if (more) {
+          ok = wait_bounded(full_bar(slot), phase, wc) && wait_bounded(s_free, par, wc);
+          if (!ok) break;
+          tc_fence_after_sync();
+          issue_s(stage(slot));
+        }
+        // dQ += dS K (the scale comes at the end): A from TMEM, B = K tile MN-major
+        ok = wait_bounded(ds_ready, par, wc);
+        if (!ok) break;
+        tc_fence_after_sync();
+        const uint32_t sK = stage(st);
+#pragma unroll
+        for (int kk = 0; kk < kBlk / 16; ++kk)
+          mma_f16_ts(tDQ, tDP + part_col<kCols>(kk), make_sdesc_sw128(sK + kk * 2048, kPanelBytes, 1024), kIdescDQ,
+                     (kk > 0 || j > 0) ? 1u : 0u);
+        mma_commit(empty_bar(st));
+        if (more) issue_dp(stage(slot) + C::kKBytes);
+      }
+      mma_commit(acc_done);
+    }
+  } else {
+    // ---------------------------------------------------------------- compute warps
+    const int part = warp >> 2;
+    const int lane_base = (warp & 3) * 32, row = lane_base + lane;
+    const uint32_t lanes = uint32_t(lane_base) << 16;
+    const uint32_t tS = tmem + lanes + C::kTmemS + part * kCols;
+    const uint32_t tDP = tmem + lanes + C::kTmemDP + part * kCols;
+    const float nl = p.nl[tile_id * kBlk + row], dd = p.delta[tile_id * kBlk + row];
+    const uint64_t cc = pack_f32x2(p.c_log2, p.c_log2), nn = pack_f32x2(nl, nl);
+    const int pos = row / p.GC, g = t.chunk * p.GC + row - pos * p.GC, i = t.i0 + pos;
+    const bool live = pos < p.PT && g < p.G && i < p.N;
+    // rows that are not there weigh nothing anyway (their nl)
+    const int lim = live ? win::row_end(p.mask, p.Nk, p.N, i) : 0x7fffffff, low = live ? win::row_low(p.mask, p.Nk, p.N, i) : 0;
+    bool ok = true;
+    auto wait_warp = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_bounded(bar, parity, wc)) != 0; };
+    for (int j = 0; j < list.n; ++j) {
+      const uint32_t par = uint32_t(j) & 1u;
+      ok = wait_warp(s_full, par);
+      if (!ok) break;
+      tc_fence_after_sync();
+      uint32_t r[kCols];
+      tmem_load_part<kCols>(tS, r);
+      tc_fence_before_sync();
+      mbar_arrive(s_free);
+      const int n0 = list.at(j) * kBlk + part * kCols;
+      float w[kCols];
+#pragma unroll
+      for (int k = 0; k < kCols; k += 2) ffma2(w[k], w[k + 1], __uint_as_float(r[k]), __uint_as_float(r[k + 1]), cc, nn);
+      if (!__all_sync(0xffffffffu, lim - n0 >= kCols && (n0 >= low || n0 + kCols <= p.mask.sinks))) {
+#pragma unroll
+        for (int k = 0; k < kCols / 32; ++k) {
+          const uint32_t bits = below(lim - n0, k) & (~below(low - n0, k) | below(p.mask.sinks - n0, k));
+#pragma unroll
+          for (int e = 0; e < 32; ++e) w[32 * k + e] = bits >> e & 1u ? w[32 * k + e] : -INFINITY;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kCols; ++k) w[k] = ex2_approx(w[k]);
+      ok = wait_warp(dp_full, par);
+      if (!ok) break;
+      tc_fence_after_sync();
+      tmem_load_part<kCols>(tDP, r);
+      uint32_t pk[kCols / 2];
+#pragma unroll
+      for (int k = 0; k < kCols; k += 2)
+        pk[k >> 1] = pack_bf16x2(w[k] * (__uint_as_float(r[k]) - dd), w[k + 1] * (__uint_as_float(r[k + 1]) - dd));
+      tmem_store_part<kCols>(tDP, pk);
+      tmem_wait_st();
+      tc_fence_before_sync();
+      mbar_arrive(ds_ready);
+    }
+    // part q writes columns [wq q, wq q + wq)
+    constexpr int wq = DK / C::kParts < 32 ? 32 : DK / C::kParts;
+    if (part * wq < DK) {
+      __nv_bfloat16* dst = row_of(p.dq, t.b, t.h * p.G + (live ? g : 0), live ? i : 0) + part * wq;
+      if (list.n == 0) {
+        if (live)
+          for (int e = 0; e < wq / 8; ++e) reinterpret_cast<uint4*>(dst)[e] = make_uint4(0, 0, 0, 0);
+      } else if (ok && wait_warp(acc_done, 0)) {
+        tc_fence_after_sync();
+        store_row<wq>(tmem + lanes + C::kTmemDQ + part * wq, p.scale, dst, nullptr, live);
+      }
+    }
+  }
+
+  if (warp == C::kMmaWarp && lane == 0) wait_quiesce(acc_done, 0, p.wait_limit_ns, &g_moa_window_bwd_status);
+  tc_fence_before_sync();
+  __syncthreads();
+  if (warp == C::kMmaWarp) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------
+// Host side
+// ------------------------------------------------------------------------------------------------
+constexpr int kSms = 152;   // the pieces aim at two CTAs for each SM; results do not go by the device's count
+
+struct Plan {
+  int64_t GC, chunks, PT, n_pt, n_kt, row_tiles;
+  int64_t cut, pieces, piece, items;
+  explicit Plan(const WindowBwdArgs& a) {
+    const int64_t G = a.Hq / a.Hk, bh = a.B * a.Hk;
+    GC = G < kBlk ? G : kBlk;
+    chunks = (G + GC - 1) / GC;
+    PT = kBlk / GC;
+    n_pt = (a.Nq + PT - 1) / PT;
+    n_kt = (a.Nk + kBlk - 1) / kBlk;
+    row_tiles = bh * chunks * n_pt;
+    const win::Mask m{a.window, a.sinks, true};
+    // row tiles of a token tile: the most of any, and of one without sinks
+    const int64_t top = rows_of_tokens(m, 0, int(a.Nq), int(a.Nk), int(PT)).n * chunks;
+    const int64_t sink_tiles = a.window == win::kNoWindow ? 0 : (int64_t(a.sinks) + kBlk - 1) / kBlk;
+    int64_t usual = top;
+    if (a.window != win::kNoWindow) {
+      usual = (int64_t(a.window) + kBlk + 2 * PT - 1) / PT * chunks;
+      if (usual > top) usual = top;
+    }
+    piece = usual;
+    cut = sink_tiles;
+    if (n_kt * bh < 2 * kSms) {   // too few token tiles for the machine: all are cut
+      int64_t total = 0;
+      for (int64_t t = 0; t < n_kt; ++t) total += rows_of_tokens(m, int(t), int(a.Nq), int(a.Nk), int(PT)).n * chunks;
+      const int64_t want = (total * bh + 2 * kSms - 1) / (2 * kSms);
+      if (want < usual) {
+        piece = want;
+        cut = n_kt;
+      }
+    }
+    if (piece < 4) piece = 4;
+    if (cut > n_kt) cut = n_kt;
+    // not more pieces than keep the machine busy: each is 128 rows of fp32 in the workspace (160 MB in all)
+    const int64_t most = cut > 0 && bh * cut < 8 * kSms ? 8 * kSms / (bh * cut) : 1;
+    if ((chunks * n_pt + piece - 1) / piece > most) piece = (chunks * n_pt + most - 1) / most;
+    pieces = (chunks * n_pt + piece - 1) / piece;
+    if (pieces <= 1) cut = 0, pieces = 1;
+    items = bh * (cut * pieces + n_kt - cut);
+  }
+};
+
+// The workspace: -LSE log2 e and D of every row of every tile, then the pieces.
+struct Work {
+  int64_t nl, delta, part, bytes;
+  Work(const WindowBwdArgs& a, const Plan& p) {
+    nl = 0;
+    delta = p.row_tiles * kBlk * 4;
+    part = 2 * delta;
+    bytes = part + a.B * a.Hk * p.cut * p.pieces * kBlk * (a.dk + a.dv) * 4;
+  }
+};
+
+bool describable(int64_t stride, int64_t size) { return size == 1 || (stride > 0 && stride < (int64_t(1) << 39)); }
+uint64_t map_stride(int64_t stride, int64_t size) { return size == 1 ? 16 : uint64_t(stride) * 2; }
+
+template <int DK, int DV>
+int launch(const WindowBwdArgs& a, char* msg, size_t msglen) {
+  using CK = KvCfg<DK, DV>;
+  using CQ = QCfg<DK, DV>;
+  auto kv = window_dkdv_tc_kernel<DK, DV>;
+  auto dq = window_dq_tc_kernel<DK, DV>;
+  cudaError_t e = ensure_smem_limit(reinterpret_cast<const void*>(kv), CK::kSmemBytes);
+  if (e == cudaSuccess) e = ensure_smem_limit(reinterpret_cast<const void*>(dq), CQ::kSmemBytes);
+  const Plan plan(a);
+  const Work w(a, plan);
+  uint8_t* ws = static_cast<uint8_t*>(a.ws);
+  const int64_t G = a.Hq / a.Hk, bh = a.B * a.Hk;
+  Params p{};
+  p.q = a.q, p.k = a.k, p.v = a.v, p.o = a.o, p.go = a.go, p.dq = a.dq, p.dk = a.dk_, p.dv = a.dv_;
+  p.lse = a.lse;
+  p.nl = reinterpret_cast<float*>(ws + w.nl);
+  p.delta = reinterpret_cast<float*>(ws + w.delta);
+  p.part = reinterpret_cast<float*>(ws + w.part);
+  p.B = int(a.B), p.Hk = int(a.Hk), p.G = int(G), p.N = int(a.Nq), p.Nk = int(a.Nk);
+  p.GC = int(plan.GC), p.chunks = int(plan.chunks), p.PT = int(plan.PT);
+  p.n_pt = int(plan.n_pt), p.n_kt = int(plan.n_kt);
+  p.cut = int(plan.cut), p.pieces = int(plan.pieces), p.piece = int(plan.piece);
+  // as many key heads side by side as leave their queries and output gradients in L2
+  const int64_t head = a.Nq * G * (DK + DV) * 2;
+  p.group = int((int64_t(48) << 20) / head < 1 ? 1 : (int64_t(48) << 20) / head > bh ? bh : (int64_t(48) << 20) / head);
+  p.mask = win::Mask{a.window, a.sinks, true};
+  p.c_log2 = a.scale * kLog2e, p.scale = a.scale;
+  p.wait_limit_ns = wait_limit_ns();
+  CUtensorMap mq, mk, mv, mg;
+  const uint64_t q_dims[5] = {DK, uint64_t(G), uint64_t(a.Nq), uint64_t(a.Hk), uint64_t(a.B)};
+  const uint64_t g_dims[5] = {DV, uint64_t(G), uint64_t(a.Nq), uint64_t(a.Hk), uint64_t(a.B)};
+  const uint64_t q_str[4] = {map_stride(a.q.sh, G), map_stride(a.q.sn, a.Nq), map_stride(G * a.q.sh, a.Hk), map_stride(a.q.sb, a.B)};
+  const uint64_t g_str[4] = {map_stride(a.go.sh, G), map_stride(a.go.sn, a.Nq), map_stride(G * a.go.sh, a.Hk),
+                             map_stride(a.go.sb, a.B)};
+  const uint32_t row_box[5] = {64, uint32_t(plan.GC), uint32_t(plan.PT), 1, 1};
+  const uint64_t k_dims[4] = {DK, uint64_t(a.Nk), uint64_t(a.Hk), uint64_t(a.B)};
+  const uint64_t v_dims[4] = {DV, uint64_t(a.Nk), uint64_t(a.Hk), uint64_t(a.B)};
+  const uint64_t k_str[3] = {map_stride(a.k.sn, a.Nk), map_stride(a.k.sh, a.Hk), map_stride(a.k.sb, a.B)};
+  const uint64_t v_str[3] = {map_stride(a.v.sn, a.Nk), map_stride(a.v.sh, a.Hk), map_stride(a.v.sb, a.B)};
+  const uint32_t kv_box[4] = {64, kBlk, 1, 1};
+  if (!encode_bf16_map_nd(&mq, a.q.p, 5, q_dims, q_str, row_box, msg, msglen) ||
+      !encode_bf16_map_nd(&mg, a.go.p, 5, g_dims, g_str, row_box, msg, msglen) ||
+      !encode_bf16_map_nd(&mk, a.k.p, 4, k_dims, k_str, kv_box, msg, msglen) ||
+      !encode_bf16_map_nd(&mv, a.v.p, 4, v_dims, v_str, kv_box, msg, msglen))
+    return 5;
+  const int64_t rows = plan.row_tiles * kBlk, threads = rows * (DV / 8);
+  if (e == cudaSuccess)
+    e = launch_overlapped(window_delta_tc_kernel<DV>, dim3(unsigned((threads + 255) / 256)), dim3(256), 0, a.stream, p, rows);
+  if (e == cudaSuccess)
+    e = launch_overlapped(kv, dim3(unsigned(plan.items)), dim3(CK::kThreads), CK::kSmemBytes, a.stream, mq, mk, mv, mg, p);
+  const int64_t joined = bh * plan.cut * kBlk * ((DK + DV) / 4);
+  if (e == cudaSuccess && joined > 0)
+    e = launch_overlapped(window_dkdv_tc_join_kernel<DK, DV>, dim3(unsigned((joined + 255) / 256)), dim3(256), 0, a.stream, p,
+                          joined);
+  if (e == cudaSuccess)
+    e = launch_overlapped(dq, dim3(unsigned(plan.row_tiles)), dim3(CQ::kThreads), CQ::kSmemBytes, a.stream, mq, mk, mv, mg, p);
+  if (e != cudaSuccess) {
+    snprintf(msg, msglen, "gradients of attention with a window: %s", cudaGetErrorString(e));
+    return 5;
+  }
+  return 0;
+}
+
+}  // namespace
+
+bool window_bwd_tc_takes(const WindowBwdArgs& a) {
+  const int64_t G = a.Hq / a.Hk;
+  auto rows = [&](const View& x) {
+    return describable(x.sh, G) && describable(G * x.sh, a.Hk) && describable(x.sn, a.Nq) && describable(x.sb, a.B);
+  };
+  auto keys = [&](const View& x) { return describable(x.sn, a.Nk) && describable(x.sh, a.Hk) && describable(x.sb, a.B); };
+  return !a.f32 && rows(a.q) && rows(a.go) && keys(a.k) && keys(a.v);
+}
+
+size_t window_bwd_tc_workspace(const WindowBwdArgs& a) { return size_t(Work(a, Plan(a)).bytes); }
+
+int launch_window_bwd_tc(const WindowBwdArgs& a, char* msg, size_t msglen) {
+  if (a.dk == 64) return a.dv == 64 ? launch<64, 64>(a, msg, msglen) : launch<64, 128>(a, msg, msglen);
+  return a.dv == 64 ? launch<128, 64>(a, msg, msglen) : launch<128, 128>(a, msg, msglen);
+}
+
+cudaError_t window_bwd_read_and_clear_status(unsigned* value) {
+  cudaError_t e = cudaMemcpyFromSymbol(value, g_moa_window_bwd_status, sizeof(unsigned));
+  if (e != cudaSuccess || *value == 0) return e;
+  const unsigned zero = 0;
+  return cudaMemcpyToSymbol(g_moa_window_bwd_status, &zero, sizeof(unsigned));
+}
+
+}  // namespace moa
