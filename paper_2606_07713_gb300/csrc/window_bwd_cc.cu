@@ -10,11 +10,12 @@
 //
 //   delta   D of every row and the row's -LSE log2 e (-infinity for rows that see nothing: their weights
 //           are then zero), a warp a row;
-//   dkdv    a CTA for 64 tokens of a key head and a piece of the rows that see them, 32 rows at a time.  A
-//           token's rows are those of its window; a sink's are all later ones, so tokens among the sinks
-//           (or all of them, without a window) have their rows cut into pieces of at most a window's length;
-//   join    adds the pieces, in order;
-//   dq      a CTA for 64 rows, 32 tokens at a time.
+//   tiles   one launch, two kinds of CTAs.  dK and dV: 64 tokens of a key head and a piece of the rows that see
+//           them, 32 rows at a time.  A token's rows are those of its window; a sink's are all later ones: token
+//           tiles with more rows than a piece are cut, a piece being a window's rows, or less where there are too
+//           few CTAs for the machine.  dQ: 64 rows, 32 tokens at a time.  The next step's rows (tokens) are on their
+//           way while a step is computed;
+//   join    adds the pieces, in order.
 // Rows of a key head are counted position by position (row r: position r / G, head r % G of the group).
 // No atomics: results do not depend on the order in which CTAs run.
 //
@@ -43,14 +44,14 @@ struct Params {
   float* nl;      // [B * Hk][N * G] -LSE log2 e, rows of a key head in their order
   float* delta;   // alike
   float* part;    // [piece item][64][DK + DV], null: no pieces
-  int64_t Hk;
-  int N, G, Nk;
+  int Hk, N, G, Nk;
   win::Mask mask;
   float c_log2, scale;
   int n_kt;       // tiles of tokens
   int cut;        // the first `cut` of them are cut into `pieces` pieces of `piece_rows` rows
   int pieces;
   int64_t piece_rows;
+  int n_rt;       // tiles of rows
 };
 
 template <typename T>
@@ -108,68 +109,100 @@ window_delta_kernel(Params p, int64_t rows) {
   }
 }
 
-// Rows of X (and Y) of a key head from row r0 on into shared memory, in fp32; rows past `rows` are zero.
+// Four features from global into shared memory: asynchronously (fp32), or widened (bf16).  Absent ones are zeros.
+__device__ __forceinline__ void fill4(float* dst, const float* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(uint32_t(__cvta_generic_to_shared(dst))), "l"(src),
+               "r"(there ? 16 : 0)
+               : "memory");
+}
+__device__ __forceinline__ void fill4(float* dst, const __nv_bfloat16* src, bool there) {
+  *reinterpret_cast<float4*>(dst) = there ? load4(src) : make_float4(0.f, 0.f, 0.f, 0.f);
+}
+__device__ __forceinline__ void fill_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void fill_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// Rows r0 .. of X and Y of a key head into shared memory; rows past `rows` are zero.
 template <typename T, int DX, int DY, int ROWS>
-__device__ __forceinline__ void load_rows(const View& x, const View& y, float* sx, float* sy, int64_t b, int64_t h, int G,
-                                          int64_t r0, int64_t rows) {
-  for (int e = threadIdx.x; e < ROWS * ((DX + DY) / 4); e += kThreads) {
-    const int r = e / ((DX + DY) / 4), c = e % ((DX + DY) / 4) * 4;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (r0 + r < rows) {
-      const int64_t i = (r0 + r) / G, hq = h * G + (r0 + r - i * G);
-      v = c < DX ? load4(row_of<T>(x, b, hq, i) + c) : load4(row_of<T>(y, b, hq, i) + (c - DX));
-    }
-    *reinterpret_cast<float4*>(c < DX ? sx + r * (DX + 4) + c : sy + r * (DY + 4) + (c - DX)) = v;
+__device__ __forceinline__ void fill_rows(const View& x, const View& y, float* sx, float* sy, int b, int h, int G, int r0,
+                                          int rows) {
+  for (int r = threadIdx.x >> 4; r < ROWS; r += kThreads / 16) {
+    const bool there = r0 + r < rows;
+    const int at = there ? r0 + r : r0, i = int(unsigned(at) / unsigned(G));
+    const int64_t hq = int64_t(h) * G + (at - i * G);
+    const T *px = row_of<T>(x, b, hq, i), *py = row_of<T>(y, b, hq, i);
+#pragma unroll
+    for (int c = 4 * (threadIdx.x & 15); c < DX; c += 64) fill4(sx + r * (DX + 4) + c, px + c, there);
+#pragma unroll
+    for (int c = 4 * (threadIdx.x & 15); c < DY; c += 64) fill4(sy + r * (DY + 4) + c, py + c, there);
+  }
+}
+// Tokens n0 .. alike.
+template <typename T, int DK, int DV, int TOKENS>
+__device__ __forceinline__ void fill_tokens(const View& k, const View& v, float* sk, float* sv, int b, int h, int n0, int Nk) {
+  for (int j = threadIdx.x >> 4; j < TOKENS; j += kThreads / 16) {
+    const bool there = n0 + j < Nk;
+    const T *pk = row_of<T>(k, b, h, there ? n0 + j : n0), *pv = row_of<T>(v, b, h, there ? n0 + j : n0);
+#pragma unroll
+    for (int c = 4 * (threadIdx.x & 15); c < DK; c += 64) fill4(sk + j * (DK + 4) + c, pk + c, there);
+#pragma unroll
+    for (int c = 4 * (threadIdx.x & 15); c < DV; c += 64) fill4(sv + j * (DV + 4) + c, pv + c, there);
   }
 }
 
-template <int DK, int DV>
-struct KvSmem {
-  static constexpr int kLdW = kKeysKv + 4;
-  static constexpr int kFloats = (kKeysKv + kRowsKv) * (DK + 4 + DV + 4) + 2 * kRowsKv * kLdW;
-};
-
-template <typename T, int DK, int DV>
-__global__ void __launch_bounds__(kThreads)
-window_dkdv_cc_kernel(Params p) {
-  constexpr int kLdW = KvSmem<DK, DV>::kLdW;
-  extern __shared__ float smem[];
-  float* sK = smem;
-  float* sV = sK + kKeysKv * (DK + 4);
-  float* sQ = sV + kKeysKv * (DV + 4);
-  float* sG = sQ + kRowsKv * (DK + 4);
-  float* sP = sG + kRowsKv * (DV + 4);   // [rows][tokens]
-  float* sS = sP + kRowsKv * kLdW;
-  wait_for_previous();
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  // items of a key head: the pieces of its first `cut` tiles, then the other tiles
-  const int per = p.cut * p.pieces + p.n_kt - p.cut;
-  const int64_t bh = int64_t(blockIdx.x) / per, b = bh / p.Hk, h = bh - b * p.Hk;
-  const int item = int(int64_t(blockIdx.x) - bh * per);
-  const bool whole = item >= p.cut * p.pieces;
-  const int kt = whole ? item - p.cut * p.pieces + p.cut : item / p.pieces, piece = whole ? 0 : item - kt * p.pieces;
-  const int k0 = kt * kKeysKv, off = p.Nk - p.N;   // row i's position: i + off
-  const int keys = p.Nk - k0 < kKeysKv ? p.Nk - k0 : kKeysKv;
-  const int64_t rows = int64_t(p.N) * p.G;
-  // rows that see a token of the tile: from position k0 to the last one's window, or to the end
+// The rows [ra, rz) that see a token of tile kt, or a piece of them (piece < 0: all); false: there is no such piece.
+__device__ __forceinline__ bool rows_of_piece(const Params& p, int kt, int piece, int* ra, int* rz) {
+  const int k0 = kt * kKeysKv, keys = p.Nk - k0 < kKeysKv ? p.Nk - k0 : kKeysKv, off = p.Nk - p.N;
+  // from position k0 to the last token's window, or to the end
   const int64_t i0 = k0 > off ? int64_t(k0) - off : 0;
   int64_t i1 = p.N;
   if (k0 >= p.mask.sinks && p.mask.window != win::kNoWindow) {
     const int64_t n = int64_t(k0) + keys - 1 + p.mask.window - off;
     i1 = n < 0 ? 0 : n < i1 ? n : i1;
   }
-  int64_t ra = i0 * p.G, rz = i1 * p.G;
-  if (!whole) {
-    ra += piece * p.piece_rows;
-    if (ra + p.piece_rows < rz) rz = ra + p.piece_rows;
+  int64_t a = i0 * p.G, z = i1 * p.G;
+  if (piece >= 0) {
+    a += piece * p.piece_rows;
+    if (a >= z) return false;
+    if (a + p.piece_rows < z) z = a + p.piece_rows;
   }
+  *ra = int(a), *rz = int(z);
+  return true;
+}
 
-  for (int e = threadIdx.x; e < kKeysKv * ((DK + DV) / 4); e += kThreads) {
-    const int j = e / ((DK + DV) / 4), c = e % ((DK + DV) / 4) * 4;
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (j < keys) x = c < DK ? load4(row_of<T>(p.k, b, h, k0 + j) + c) : load4(row_of<T>(p.v, b, h, k0 + j) + (c - DK));
-    *reinterpret_cast<float4*>(c < DK ? sK + j * (DK + 4) + c : sV + j * (DV + 4) + (c - DK)) = x;
-  }
+template <int DK, int DV>
+struct KvSmem {
+  static constexpr int kLdW = kKeysKv + 4;
+  static constexpr int kRows = kRowsKv * (DK + 4 + DV + 4);   // a step's queries and output gradients
+  static constexpr int kFloats = kKeysKv * (DK + 4 + DV + 4) + 2 * kRows + 2 * kRowsKv * kLdW;
+};
+
+template <typename T, int DK, int DV>
+__device__ __forceinline__ void dkdv_tile(const Params& p, unsigned index, float* smem) {
+  using S = KvSmem<DK, DV>;
+  constexpr int kLdW = S::kLdW;
+  float* sK = smem;
+  float* sV = sK + kKeysKv * (DK + 4);
+  float* sRows = sV + kKeysKv * (DV + 4);
+  float* sP = sRows + 2 * S::kRows;   // [rows][tokens]
+  float* sS = sP + kRowsKv * kLdW;
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  // items of a key head: the pieces of its first `cut` tiles, then the other tiles
+  const unsigned per = unsigned(p.cut * p.pieces + p.n_kt - p.cut);
+  const int bh = int(index / per), b = bh / p.Hk, h = bh - b * p.Hk;
+  const int item = int(index - unsigned(bh) * per);
+  const bool whole = item >= p.cut * p.pieces;
+  const int kt = whole ? item - p.cut * p.pieces + p.cut : item / p.pieces, piece = whole ? 0 : item - kt * p.pieces;
+  const int k0 = kt * kKeysKv, off = p.Nk - p.N;   // row i's position: i + off
+  const int keys = p.Nk - k0 < kKeysKv ? p.Nk - k0 : kKeysKv;
+  const int64_t rows = int64_t(p.N) * p.G;
+  int ra, rz;
+  if (!rows_of_piece(p, kt, whole ? -1 : piece, &ra, &rz)) return;   // the join adds what pieces there are
+  fill_tokens<T, DK, DV, kKeysKv>(p.k, p.v, sK, sV, b, h, k0, p.Nk);
+  if (ra < rz) fill_rows<T, DK, DV, kRowsKv>(p.q, p.go, sRows, sRows + kRowsKv * (DK + 4), b, h, p.G, ra, rz);
+  fill_commit();
   float dv[4][DV / 16], dk[4][DK / 16];   // tokens 4 ty + a, features 64 c + 4 tx + e
 #pragma unroll
   for (int a = 0; a < 4; ++a) {
@@ -178,9 +211,13 @@ window_dkdv_cc_kernel(Params p) {
 #pragma unroll
     for (int c = 0; c < DK / 16; ++c) dk[a][c] = 0.f;
   }
-  for (int64_t r0 = ra; r0 < rz; r0 += kRowsKv) {
-    __syncthreads();
-    load_rows<T, DK, DV, kRowsKv>(p.q, p.go, sQ, sG, b, h, p.G, r0, rz);
+  for (int r0 = ra, step = 0; r0 < rz; r0 += kRowsKv, ++step) {
+    const float* sQ = sRows + (step & 1) * S::kRows;
+    const float* sG = sQ + kRowsKv * (DK + 4);
+    float* next = sRows + (~step & 1) * S::kRows;
+    if (r0 + kRowsKv < rz) fill_rows<T, DK, DV, kRowsKv>(p.q, p.go, next, next + kRowsKv * (DK + 4), b, h, p.G, r0 + kRowsKv, rz);
+    fill_commit();
+    fill_wait<1>();
     __syncthreads();
     // rows tx, tx + 16 against tokens 4 ty + a
     float s[4][2], e[4][2];
@@ -210,9 +247,9 @@ window_dkdv_cc_kernel(Params p) {
     }
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      const int64_t r = r0 + tx + 16 * x;
+      const int r = r0 + tx + 16 * x;
       const bool live = r < rz;
-      const int pos = int((live ? r : rz - 1) / p.G) + off;
+      const int pos = int(unsigned(live ? r : rz - 1) / unsigned(p.G)) + off;
       const float nl = live ? p.nl[bh * rows + r] : -INFINITY, d = live ? p.delta[bh * rows + r] : 0.f;
       float4 wp, ws;
       float* fp = reinterpret_cast<float*>(&wp);
@@ -249,13 +286,15 @@ window_dkdv_cc_kernel(Params p) {
         axpy4(ws.w, q, dk[3] + 4 * c);
       }
     }
+    __syncthreads();   // this step's rows make room for those after the next
   }
+  fill_wait<0>();
 #pragma unroll
   for (int a = 0; a < 4; ++a) {
     const int j = 4 * ty + a;
     if (j >= keys) continue;
     if (!whole) {
-      float* dst = p.part + (((bh * p.cut + kt) * p.pieces + piece) * kKeysKv + j) * (DK + DV);
+      float* dst = p.part + (((int64_t(bh) * p.cut + kt) * p.pieces + piece) * kKeysKv + j) * (DK + DV);
 #pragma unroll
       for (int c = 0; c < DK / 64; ++c)
         store4(dst + 64 * c + 4 * tx, make_float4(dk[a][4 * c], dk[a][4 * c + 1], dk[a][4 * c + 2], dk[a][4 * c + 3]));
@@ -289,7 +328,8 @@ window_dkdv_join_kernel(Params p, int64_t n) {
   const int64_t bh = tile / p.cut, kt = tile - bh * p.cut, b = bh / p.Hk, h = bh - b * p.Hk;
   if (kt * kKeysKv + j >= p.Nk) return;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int i = 0; i < p.pieces; ++i) {
+  int ra, rz;
+  for (int i = 0; i < p.pieces && rows_of_piece(p, int(kt), i, &ra, &rz); ++i) {
     const float4 v = load4(p.part + ((tile * p.pieces + i) * kKeysKv + j) * (DK + DV) + c);
     s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
   }
@@ -303,33 +343,35 @@ window_dkdv_join_kernel(Params p, int64_t n) {
 template <int DK, int DV>
 struct QSmem {
   static constexpr int kLdW = kRowsQ + 4;
-  static constexpr int kFloats = (kRowsQ + kKeysQ) * (DK + 4 + DV + 4) + kKeysQ * kLdW;
+  static constexpr int kTokens = kKeysQ * (DK + 4 + DV + 4);   // a step's keys and values
+  static constexpr int kFloats = kRowsQ * (DK + 4 + DV + 4) + 2 * kTokens + kKeysQ * kLdW;
 };
 
 template <typename T, int DK, int DV>
-__global__ void __launch_bounds__(kThreads)
-window_dq_cc_kernel(Params p, int n_rt) {
-  constexpr int kLdW = QSmem<DK, DV>::kLdW;
-  extern __shared__ float smem[];
+__device__ __forceinline__ void dq_tile(const Params& p, unsigned index, float* smem) {
+  using S = QSmem<DK, DV>;
+  constexpr int kLdW = S::kLdW;
   float* sQ = smem;
   float* sG = sQ + kRowsQ * (DK + 4);
-  float* sK = sG + kRowsQ * (DV + 4);
-  float* sV = sK + kKeysQ * (DK + 4);
-  float* sS = sV + kKeysQ * (DV + 4);   // [tokens][rows]
-  wait_for_previous();
+  float* sTokens = sG + kRowsQ * (DV + 4);
+  float* sS = sTokens + 2 * S::kTokens;   // [tokens][rows]
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int64_t bh = int64_t(blockIdx.x) / n_rt, b = bh / p.Hk, h = bh - b * p.Hk;
-  const int64_t rows = int64_t(p.N) * p.G, r0 = (int64_t(blockIdx.x) - bh * n_rt) * kRowsQ;
+  const int bh = int(index / unsigned(p.n_rt)), b = bh / p.Hk, h = bh - b * p.Hk;
+  // the last rows, which see the most without a window, come first
+  const int r0 = (p.n_rt - 1 - int(index - unsigned(bh) * unsigned(p.n_rt))) * kRowsQ;
+  const int64_t rows = int64_t(p.N) * p.G;
   const int live = int(rows - r0 < kRowsQ ? rows - r0 : kRowsQ);
   const int off = p.Nk - p.N;
-  const int i0 = int(r0 / p.G), i1 = int((r0 + live - 1) / p.G);
+  const int i0 = r0 / p.G, i1 = (r0 + live - 1) / p.G;
   const win::Tiles list = win::tiles_of(p.mask, p.Nk, p.N, i0, i1, kKeysQ);
-  load_rows<T, DK, DV, kRowsQ>(p.q, p.go, sQ, sG, b, h, p.G, r0, rows);
+  fill_rows<T, DK, DV, kRowsQ>(p.q, p.go, sQ, sG, b, h, p.G, r0, int(rows));
+  if (list.n > 0) fill_tokens<T, DK, DV, kKeysQ>(p.k, p.v, sTokens, sTokens + kKeysQ * (DK + 4), b, h, list.at(0) * kKeysQ, p.Nk);
+  fill_commit();
   float nl[4], d[4], dq[4][DK / 16];
   int pos[4];
 #pragma unroll
   for (int a = 0; a < 4; ++a) {
-    const int64_t r = r0 + 4 * ty + a;
+    const int r = r0 + 4 * ty + a;
     const bool in = r < rows;
     nl[a] = in ? p.nl[bh * rows + r] : -INFINITY;
     d[a] = in ? p.delta[bh * rows + r] : 0.f;
@@ -339,13 +381,13 @@ window_dq_cc_kernel(Params p, int n_rt) {
   }
   for (int t = 0; t < list.n; ++t) {
     const int n0 = list.at(t) * kKeysQ;
-    __syncthreads();
-    for (int e = threadIdx.x; e < kKeysQ * ((DK + DV) / 4); e += kThreads) {
-      const int j = e / ((DK + DV) / 4), c = e % ((DK + DV) / 4) * 4;
-      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (n0 + j < p.Nk) x = c < DK ? load4(row_of<T>(p.k, b, h, n0 + j) + c) : load4(row_of<T>(p.v, b, h, n0 + j) + (c - DK));
-      *reinterpret_cast<float4*>(c < DK ? sK + j * (DK + 4) + c : sV + j * (DV + 4) + (c - DK)) = x;
-    }
+    const float* sK = sTokens + (t & 1) * S::kTokens;
+    const float* sV = sK + kKeysQ * (DK + 4);
+    float* next = sTokens + (~t & 1) * S::kTokens;
+    if (t + 1 < list.n)
+      fill_tokens<T, DK, DV, kKeysQ>(p.k, p.v, next, next + kKeysQ * (DK + 4), b, h, list.at(t + 1) * kKeysQ, p.Nk);
+    fill_commit();
+    fill_wait<1>();
     __syncthreads();
     // tokens tx, tx + 16 against rows 4 ty + a
     float s[4][2], e[4][2];
@@ -398,12 +440,15 @@ window_dq_cc_kernel(Params p, int n_rt) {
         axpy4(ws.w, k, dq[3] + 4 * c);
       }
     }
+    __syncthreads();   // this step's tokens make room for those after the next
   }
+  fill_wait<0>();
 #pragma unroll
   for (int a = 0; a < 4; ++a) {
-    const int64_t r = r0 + 4 * ty + a;
+    const int r = r0 + 4 * ty + a;
     if (r >= rows) continue;
-    const int64_t i = r / p.G, hq = h * p.G + (r - i * p.G);
+    const int i = r / p.G;
+    const int64_t hq = int64_t(h) * p.G + (r - i * p.G);
     T* dst = const_cast<T*>(row_of<T>(p.dq, b, hq, i));
 #pragma unroll
     for (int c = 0; c < DK / 64; ++c)
@@ -412,24 +457,46 @@ window_dq_cc_kernel(Params p, int n_rt) {
   }
 }
 
-// How the rows of tokens among the sinks (or of all tokens, without a window) are cut: pieces of a window's
-// length, or of an eighth of all rows without one, in whole steps.
+// CTAs below n_kv: dK and dV; the others: dQ.
+template <typename T, int DK, int DV>
+__global__ void __launch_bounds__(kThreads)
+window_bwd_cc_kernel(const Params p, unsigned n_kv) {
+  extern __shared__ float smem[];
+  wait_for_previous();
+  if (blockIdx.x < n_kv)
+    dkdv_tile<T, DK, DV>(p, blockIdx.x, smem);
+  else
+    dq_tile<T, DK, DV>(p, blockIdx.x - n_kv, smem);
+}
+
+// How token tiles are cut: pieces of a window's rows (of all rows without one), or of so few that there are two CTAs
+// for each SM; the first `cut` tiles then come in up to `pieces` pieces.
 struct Cut {
   int64_t n_kt, cut, pieces, piece_rows;
 };
 Cut cut_of(const WindowBwdArgs& a) {
-  const int64_t G = a.Hq / a.Hk, rows = a.Nq * G;
+  const int64_t G = a.Hq / a.Hk, bh = a.B * a.Hk, rows = a.Nq * G;
   Cut c;
   c.n_kt = (a.Nk + kKeysKv - 1) / kKeysKv;
   const bool windowed = a.window != win::kNoWindow;
-  int64_t want = windowed ? (int64_t(a.window) + kKeysKv) * G : (rows + 7) / 8;
-  if (want < 512) want = 512;
-  if (want > rows) want = rows;
+  int64_t usual = windowed ? (int64_t(a.window) + kKeysKv) * G : rows;
+  if (usual > rows) usual = rows;
+  int64_t want = usual;
+  c.cut = windowed ? (int64_t(a.sinks) + kKeysKv - 1) / kKeysKv : 0;
+  if (c.n_kt * bh < kMostPieces / 4) {
+    // about the rows of all tiles: half of them without a window
+    const int64_t all = bh * c.n_kt * (windowed ? usual : (usual + 1) / 2);
+    const int64_t fine = all / (kMostPieces / 4);
+    if (fine < usual) {
+      want = fine;
+      c.cut = c.n_kt;
+    }
+  }
+  if (want < 2 * kRowsKv) want = 2 * kRowsKv;
   c.piece_rows = (want + kRowsKv - 1) / kRowsKv * kRowsKv;
-  c.cut = windowed ? (int64_t(a.sinks) + kKeysKv - 1) / kKeysKv : c.n_kt;
   if (c.cut > c.n_kt) c.cut = c.n_kt;
   // not more pieces than keep the machine busy: each is 64 rows of fp32 in the workspace (80 MB in all)
-  const int64_t bh = a.B * a.Hk, most = c.cut > 0 && bh * c.cut < kMostPieces ? kMostPieces / (bh * c.cut) : 1;
+  const int64_t most = c.cut > 0 && bh * c.cut < kMostPieces ? kMostPieces / (bh * c.cut) : 1;
   if ((rows + c.piece_rows - 1) / c.piece_rows > most) c.piece_rows = ((rows + most - 1) / most + kRowsKv - 1) / kRowsKv * kRowsKv;
   c.pieces = (rows + c.piece_rows - 1) / c.piece_rows;
   if (c.pieces == 1) c.cut = 0;
@@ -450,26 +517,24 @@ int launch(const WindowBwdArgs& a, char* msg, size_t msglen) {
   p.nl = reinterpret_cast<float*>(ws);
   p.delta = reinterpret_cast<float*>(ws + rows_bytes(a));
   p.part = reinterpret_cast<float*>(ws + 2 * rows_bytes(a));
-  p.Hk = a.Hk, p.N = int(a.Nq), p.G = int(G), p.Nk = int(a.Nk);
+  p.Hk = int(a.Hk), p.N = int(a.Nq), p.G = int(G), p.Nk = int(a.Nk);
   p.mask = win::Mask{a.window, a.sinks, true};
   p.c_log2 = a.scale * kLog2e, p.scale = a.scale;
   p.n_kt = int(cut.n_kt), p.cut = int(cut.cut), p.pieces = int(cut.pieces), p.piece_rows = cut.piece_rows;
-  const int kv_smem = KvSmem<DK, DV>::kFloats * 4, q_smem = QSmem<DK, DV>::kFloats * 4;
-  auto kv = window_dkdv_cc_kernel<T, DK, DV>;
-  auto dq = window_dq_cc_kernel<T, DK, DV>;
-  cudaError_t e = ensure_smem_limit(reinterpret_cast<const void*>(kv), kv_smem);
-  if (e == cudaSuccess) e = ensure_smem_limit(reinterpret_cast<const void*>(dq), q_smem);
+  p.n_rt = int((a.Nq * G + kRowsQ - 1) / kRowsQ);
+  constexpr int kSmem = (KvSmem<DK, DV>::kFloats > QSmem<DK, DV>::kFloats ? KvSmem<DK, DV>::kFloats : QSmem<DK, DV>::kFloats) * 4;
+  static_assert(kSmem <= 232448, "shared memory budget");
+  auto kern = window_bwd_cc_kernel<T, DK, DV>;
+  cudaError_t e = ensure_smem_limit(reinterpret_cast<const void*>(kern), kSmem);
   if (e == cudaSuccess)
     e = launch_overlapped(window_delta_kernel<T, DV>, dim3(unsigned((rows + 7) / 8)), dim3(kThreads), 0, a.stream, p, rows);
   const int64_t items = bh * (cut.cut * cut.pieces + cut.n_kt - cut.cut);
-  if (e == cudaSuccess) e = launch_overlapped(kv, dim3(unsigned(items)), dim3(kThreads), size_t(kv_smem), a.stream, p);
+  if (e == cudaSuccess)
+    e = launch_overlapped(kern, dim3(unsigned(items + bh * p.n_rt)), dim3(kThreads), size_t(kSmem), a.stream, p, unsigned(items));
   const int64_t joined = bh * cut.cut * kKeysKv * ((DK + DV) / 4);
   if (e == cudaSuccess && joined > 0)
     e = launch_overlapped(window_dkdv_join_kernel<T, DK, DV>, dim3(unsigned((joined + kThreads - 1) / kThreads)), dim3(kThreads),
                           0, a.stream, p, joined);
-  const int64_t n_rt = (a.Nq * G + kRowsQ - 1) / kRowsQ;
-  if (e == cudaSuccess)
-    e = launch_overlapped(dq, dim3(unsigned(bh * n_rt)), dim3(kThreads), size_t(q_smem), a.stream, p, int(n_rt));
   if (e != cudaSuccess) {
     snprintf(msg, msglen, "gradients of attention with a window: %s", cudaGetErrorString(e));
     return 5;

@@ -40,8 +40,7 @@ struct Params {
   KvSource kv;
   float* lse;
   const int32_t* lens;
-  int64_t Hk;
-  int N, G, max_len, n_tiles;   // n_tiles: row tiles of a key head
+  int Hk, N, G, max_len, n_tiles;   // n_tiles: row tiles of a key head
   win::Mask mask;
   float c_log2;
   int splits;
@@ -84,42 +83,104 @@ struct Cfg {
   static constexpr int kSmem = kFloats * 4;
 };
 
+// Four features from global into shared memory: asynchronously (fp32), or widened (bf16).  Absent ones are zeros.
+__device__ __forceinline__ void fill4(float* dst, const float* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(uint32_t(__cvta_generic_to_shared(dst))), "l"(src),
+               "r"(there ? 16 : 0)
+               : "memory");
+}
+__device__ __forceinline__ void fill4(float* dst, const __nv_bfloat16* src, bool there) {
+  *reinterpret_cast<float4*>(dst) = there ? load4(src) : make_float4(0.f, 0.f, 0.f, 0.f);
+}
+__device__ __forceinline__ void fill_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void fill_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
 template <typename T, int DK, int DV, int RM, int NT>
 __global__ void __launch_bounds__(NT)
-window_cc_kernel(Params p) {
+window_cc_kernel(const Params p) {
   using C = Cfg<DK, DV, RM, NT>;
   extern __shared__ float smem[];
   float* sQ = smem;                        // [rows][DK]
   float* sK = sQ + C::kRows * C::kLdQ;     // [tokens][DK]
   float* sV = sK + kKeys * C::kLdK;        // [tokens][DV]
   float* sP = sV + kKeys * DV;             // [tokens][rows]
+  __shared__ const T* s_at[2][2][kKeys];   // a tile's keys and values; null: nothing there, zeros
   wait_for_previous();
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int64_t item = blockIdx.x, bh = item / p.n_tiles;
-  const int tile = int(item - bh * p.n_tiles);
-  const int64_t b = bh / p.Hk, h = bh - b * p.Hk;
-  const int64_t rows_all = int64_t(p.N) * p.G, r0 = int64_t(tile) * C::kRows;
-  const int rows = int(rows_all - r0 < C::kRows ? rows_all - r0 : C::kRows);
+  const unsigned item = blockIdx.x, bh = item / unsigned(p.n_tiles);
+  const int tile = int(item - bh * unsigned(p.n_tiles));
+  const int b = int(bh / unsigned(p.Hk)), h = int(bh - unsigned(b) * unsigned(p.Hk));
+  const int rows_all = p.N * p.G, r0 = tile * C::kRows;
+  const int rows = rows_all - r0 < C::kRows ? rows_all - r0 : C::kRows;
   const int len = length_of(p, b);
-  const int i0 = int(r0 / p.G), i1 = int((r0 + rows - 1) / p.G);
+  const int i0 = r0 / p.G, i1 = (r0 + rows - 1) / p.G;
   const win::Tiles list = win::tiles_of(p.mask, len, p.N, i0, i1, kKeys);
   const int first = int(int64_t(list.n) * blockIdx.y / p.splits), last = int(int64_t(list.n) * (blockIdx.y + 1) / p.splits);
+  // the first token that any row sees by its window: between the sinks and it nothing is read
+  const int low0 = win::row_low(p.mask, len, p.N, i0), end1 = win::row_end(p.mask, len, p.N, i1);
 
-  const T* Q = static_cast<const T*>(p.q.p) + b * p.q.sb + h * p.G * p.q.sh;
-  for (int x = threadIdx.x; x < C::kRows * (DK / 4); x += NT) {
-    const int r = x / (DK / 4), c = x % (DK / 4) * 4;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (r < rows) {
-      const int64_t i = (r0 + r) / p.G, g = r0 + r - i * p.G;
-      v = load4(Q + g * p.q.sh + i * p.q.sn + c);
+  auto find = [&](int t) {   // where tile t's tokens lie
+    if (t >= last || threadIdx.x >= kKeys) return;
+    const int n = list.at(t) * kKeys + int(threadIdx.x);
+    const T *k = nullptr, *v = nullptr;
+    if (n < end1 && (n >= low0 || n < p.mask.sinks)) {
+      int64_t at = b, place = n;
+      bool there = true;
+      if (p.kv.table != nullptr) {
+        const int slot = int(unsigned(n) / unsigned(p.kv.page));
+        at = p.kv.table[b * p.kv.max_pages + slot];
+        place = n - slot * p.kv.page;
+        there = at >= 0 && at < p.kv.n_pages;
+        if (!there) atomicExch(&g_moa_window_cc_status, win::kErrIndex);
+      }
+      if (there) {
+        k = static_cast<const T*>(p.kv.k) + at * p.kv.k_sb + h * p.kv.k_sh + place * p.kv.k_sn;
+        v = static_cast<const T*>(p.kv.v) + at * p.kv.v_sb + h * p.kv.v_sh + place * p.kv.v_sn;
+      }
     }
-    *reinterpret_cast<float4*>(sQ + r * C::kLdQ + c) = v;
+    s_at[t & 1][0][threadIdx.x] = k;
+    s_at[t & 1][1][threadIdx.x] = v;
+  };
+  const T* any = static_cast<const T*>(p.q.p);   // an address for copies of nothing
+  auto fill_keys = [&](int t) {
+    if (t < last)
+#pragma unroll 4
+      for (int x = threadIdx.x; x < kKeys * (DK / 4); x += NT) {
+        const int j = x / (DK / 4), c = x % (DK / 4) * 4;
+        const T* src = s_at[t & 1][0][j];
+        fill4(sK + j * C::kLdK + c, src == nullptr ? any : src + c, src != nullptr);
+      }
+    fill_commit();
+  };
+  auto fill_values = [&](int t) {
+    if (t < last)
+#pragma unroll 4
+      for (int x = threadIdx.x; x < kKeys * (DV / 4); x += NT) {
+        const int j = x / (DV / 4), c = x % (DV / 4) * 4;
+        const T* src = s_at[t & 1][1][j];
+        fill4(sV + j * DV + c, src == nullptr ? any : src + c, src != nullptr);
+      }
+    fill_commit();
+  };
+
+  find(first);
+  const T* Q = static_cast<const T*>(p.q.p) + b * p.q.sb + int64_t(h) * p.G * p.q.sh;
+  for (int x = threadIdx.x; x < C::kRows * (DK / 4); x += NT) {
+    const int r = x / (DK / 4), c = x % (DK / 4) * 4, i = (r0 + r) / p.G, g = r0 + r - i * p.G;
+    fill4(sQ + r * C::kLdQ + c, r < rows ? Q + g * p.q.sh + i * p.q.sn + c : any, r < rows);
   }
+  __syncthreads();
+  fill_keys(first);
+  fill_values(first);
+  find(first + 1);
   int end[RM], low[RM];
 #pragma unroll
   for (int a = 0; a < RM; ++a) {
     const int r = ty * RM + a;
-    const int i = int((r0 + (r < rows ? r : rows - 1)) / p.G);
+    const int i = (r0 + (r < rows ? r : rows - 1)) / p.G;
     end[a] = r < rows ? win::row_end(p.mask, len, p.N, i) : 0;
     low[a] = win::row_low(p.mask, len, p.N, i);
   }
@@ -130,33 +191,10 @@ window_cc_kernel(Params p) {
 #pragma unroll
     for (int c = 0; c < DV / 16; ++c) acc[a][c] = 0.f;
   }
-  const int32_t* table = p.kv.table + b * p.kv.max_pages;
-  // the first token that any row sees by its window: between the sinks and it nothing is read
-  const int low0 = win::row_low(p.mask, len, p.N, i0), end1 = win::row_end(p.mask, len, p.N, i1);
+  // the next tile's keys are on their way during the second product, its values during the next first one
   for (int t = first; t < last; ++t) {
     const int n0 = list.at(t) * kKeys;
-    __syncthreads();
-    constexpr int kQuads = (DK + DV) / 4;
-    for (int x = threadIdx.x; x < kKeys * kQuads; x += NT) {
-      const int j = x / kQuads, c = x % kQuads * 4, n = n0 + j;
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (n < end1 && (n >= low0 || n < p.mask.sinks)) {
-        int64_t at = b, place = n;
-        bool there = true;
-        if (p.kv.table != nullptr) {
-          const int slot = n / p.kv.page;
-          at = table[slot];
-          place = n - slot * p.kv.page;
-          there = at >= 0 && at < p.kv.n_pages;
-          if (!there) atomicExch(&g_moa_window_cc_status, win::kErrIndex);
-        }
-        if (there)
-          v = c < DK ? load4(static_cast<const T*>(p.kv.k) + at * p.kv.k_sb + h * p.kv.k_sh + place * p.kv.k_sn + c)
-                     : load4(static_cast<const T*>(p.kv.v) + at * p.kv.v_sb + h * p.kv.v_sh + place * p.kv.v_sn + (c - DK));
-      }
-      float* dst = c < DK ? sK + j * C::kLdK + c : sV + j * DV + (c - DK);
-      *reinterpret_cast<float4*>(dst) = v;
-    }
+    fill_wait<1>();
     __syncthreads();
     // scores of tokens tx, tx + 16, ... : a quarter warp's rows of sK then lie in all banks
     float s[RM][4];
@@ -214,7 +252,10 @@ window_cc_kernel(Params p) {
     for (int k = 0; k < 4; ++k)
 #pragma unroll
       for (int a = 0; a < RM; ++a) sP[(tx + 16 * k) * C::kLdP + ty * RM + a] = w[a][k];
-    __syncwarp();   // a row's weights are written and read by one warp
+    __syncthreads();
+    fill_keys(t + 1);
+    fill_wait<1>();
+    __syncthreads();
 #pragma unroll 4
     for (int j = 0; j < kKeys; ++j) {
       float pw[RM];
@@ -234,14 +275,18 @@ window_cc_kernel(Params p) {
         }
       }
     }
+    __syncthreads();
+    fill_values(t + 1);
+    find(t + 2);
   }
+  fill_wait<0>();
 
 #pragma unroll
   for (int a = 0; a < RM; ++a) {
     const int r = ty * RM + a;
     if (r >= rows) continue;
     if (p.part_o != nullptr) {
-      const int64_t at = (item * p.splits + blockIdx.y) * C::kRows + r;
+      const int64_t at = (int64_t(item) * p.splits + blockIdx.y) * C::kRows + r;
 #pragma unroll
       for (int c = 0; c < DV / 64; ++c)
         store4(p.part_o + at * DV + c * 64 + tx * 4,
@@ -249,15 +294,15 @@ window_cc_kernel(Params p) {
       if (tx == 0) p.part_ml[at] = make_float2(m[a], l[a]);
       continue;
     }
-    const int64_t i = (r0 + r) / p.G, g = r0 + r - i * p.G;
+    const int i = (r0 + r) / p.G, g = r0 + r - i * p.G;
     const float inv = m[a] == -INFINITY && l[a] == 0.f ? 0.f : 1.f / l[a];
-    T* o = static_cast<T*>(p.o.p) + b * p.o.sb + (h * p.G + g) * p.o.sh + i * p.o.sn;
+    T* o = static_cast<T*>(p.o.p) + b * p.o.sb + (int64_t(h) * p.G + g) * p.o.sh + i * p.o.sn;
 #pragma unroll
     for (int c = 0; c < DV / 64; ++c)
       store4(o + c * 64 + tx * 4, make_float4(acc[a][4 * c] * inv, acc[a][4 * c + 1] * inv, acc[a][4 * c + 2] * inv,
                                               acc[a][4 * c + 3] * inv));
     if (p.lse != nullptr && tx == 0)
-      p.lse[((b * p.Hk + h) * p.G + g) * p.N + i] = l[a] == 0.f ? -INFINITY : (m[a] + log2f(l[a])) * kLn2;
+      p.lse[((int64_t(b) * p.Hk + h) * p.G + g) * p.N + i] = l[a] == 0.f ? -INFINITY : (m[a] + log2f(l[a])) * kLn2;
   }
 }
 
@@ -267,7 +312,7 @@ __global__ void __launch_bounds__(256)
 window_cc_join_kernel(Params p, int tile_rows) {
   wait_for_previous();
   const int lane = threadIdx.x & 31;
-  const int64_t item = blockIdx.x, bh = item / p.n_tiles;
+  const int64_t item = blockIdx.x, bh = unsigned(blockIdx.x) / unsigned(p.n_tiles);
   const int r = int(blockIdx.y) * 8 + (threadIdx.x >> 5);
   const int64_t row = (item - bh * p.n_tiles) * tile_rows + r;
   if (row >= int64_t(p.N) * p.G) return;
@@ -289,7 +334,7 @@ window_cc_join_kernel(Params p, int tile_rows) {
     }
   }
   const float inv = L == 0.f ? 0.f : 1.f / L;
-  const int64_t b = bh / p.Hk, h = bh - b * p.Hk, i = row / p.G, g = row - i * p.G;
+  const int64_t b = unsigned(bh) / unsigned(p.Hk), h = bh - b * p.Hk, i = unsigned(row) / unsigned(p.G), g = row - i * p.G;
   if (lane * 4 < DV)
     store4(static_cast<T*>(p.o.p) + b * p.o.sb + (h * p.G + g) * p.o.sh + i * p.o.sn + lane * 4,
            make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv));
@@ -304,7 +349,7 @@ int launch(const WindowArgs& a, const WindowCcPlan& plan, char* msg, size_t msgl
   cudaError_t e = ensure_smem_limit(reinterpret_cast<const void*>(kern), C::kSmem);
   Params p{};
   p.q = a.q, p.o = a.o, p.kv = a.kv, p.lse = a.lse, p.lens = a.lens;
-  p.Hk = a.Hk, p.N = int(a.N), p.G = int(a.Hq / a.Hk), p.max_len = int(a.max_len);
+  p.Hk = int(a.Hk), p.N = int(a.N), p.G = int(a.Hq / a.Hk), p.max_len = int(a.max_len);
   p.n_tiles = int(plan.items / (a.B * a.Hk));
   p.mask = win::Mask{a.window, a.sinks, a.causal};
   p.c_log2 = a.scale * kLog2e;
