@@ -9,11 +9,11 @@
 // products), all sums are fp32 in TMEM.
 //
 //   delta  D and -LSE log2 e of every row, in tiles of 128 rows;
-//   dkdv   a CTA for 128 tokens of a key head and a piece of the row tiles that see them:
+//   tiles  one launch, two kinds of CTAs.  dK and dV: 128 tokens of a key head and a piece of the row tiles that see them,
 //            S^T = K Q^T, dP^T = V dO^T, P^T and dS^T back into TMEM as bf16, dV += P^T dO, dK += dS^T Q;
-//   join   adds the pieces of cut token tiles, in order;
-//   dq     a CTA for 128 rows, over the token tiles that they see:
-//            S = Q K^T, dP = dO V^T, dS = P (dP - D), dQ += dS K.
+//          dQ: 128 rows, over the token tiles that they see,
+//            S = Q K^T, dP = dO V^T, dS = P (dP - D), dQ += dS K;
+//   join   adds the pieces of cut token tiles, in order.
 // dQ apart from dK and dV: seven tile products in place of five, but every sum stays within one CTA (no
 // atomics, the same bits every time).
 //
@@ -25,7 +25,7 @@
 // others are done: token tiles with more row tiles than `piece` are cut.  `piece` is a window's row tiles, or less
 // where there are too few CTAs for the machine.
 //
-// CTA organisation of both tile kernels (one CTA an SM): 4P compute warps (warp w: TMEM lanes 32 (w % 4) .., columns
+// CTA organisation of both kinds (one CTA an SM): 4P compute warps (warp w: TMEM lanes 32 (w % 4) .., columns
 // 128 / P (w / 4) .. of the score tiles; its bf16 values go back into the first half of its own columns), one warp
 // for TMEM and the products, one for the copies.  Waits are bounded; on expiry MOA_ERR_DEVICE_TIMEOUT is recorded and
 // every role leaves its loop.
@@ -166,41 +166,48 @@ __device__ __forceinline__ RowTile row_tile(const Params& p, int64_t t) {
 // ------------------------------------------------------------------------------------------------
 // D and -LSE log2 e: DV / 8 lanes a row
 // ------------------------------------------------------------------------------------------------
+// A CTA for one row tile; its rows' loads are all on their way together.  Bound by memory: O and dO once.
 template <int DV>
 __global__ void __launch_bounds__(256)
-window_delta_tc_kernel(const Params p, int64_t rows) {
-  constexpr int L = DV / 8;
+window_delta_tc_kernel(const Params p) {
+  constexpr int L = DV / 8, kStep = 256 / L, kIts = kBlk / kStep;
   wait_for_previous();
-  const int64_t r = (int64_t(blockIdx.x) * 256 + threadIdx.x) / L;
-  const int gl = threadIdx.x % L;
-  if (r >= rows) return;   // (rows are a multiple of 128: whole warps)
-  const int in_tile = int(r % kBlk), pos = in_tile / p.GC, head = in_tile - pos * p.GC;
-  const RowTile t = row_tile(p, r / kBlk);
-  const int g = t.chunk * p.GC + head, i = t.i0 + pos, hq = t.h * p.G + g;
-  const bool real = pos < p.PT && g < p.G && i < p.N;
-  float acc = 0.f;
-  if (real) {
-    const uint4 ov = *reinterpret_cast<const uint4*>(row_of(p.o, t.b, hq, i) + gl * 8);
-    const uint4 gv = *reinterpret_cast<const uint4*>(row_of(p.go, t.b, hq, i) + gl * 8);
-    const __nv_bfloat162* o2 = reinterpret_cast<const __nv_bfloat162*>(&ov);
-    const __nv_bfloat162* g2 = reinterpret_cast<const __nv_bfloat162*>(&gv);
+  const RowTile t = row_tile(p, blockIdx.x);
+  const int gl = threadIdx.x % L, first = threadIdx.x / L;
+  uint4 ov[kIts], gv[kIts];
+  float lse[kIts];
+  bool real[kIts];
+#pragma unroll
+  for (int k = 0; k < kIts; ++k) {
+    const int r = first + k * kStep, pos = int(unsigned(r) / unsigned(p.GC));
+    const int g = t.chunk * p.GC + (r - pos * p.GC), i = t.i0 + pos, hq = t.h * p.G + g;
+    real[k] = pos < p.PT && g < p.G && i < p.N;
+    ov[k] = gv[k] = make_uint4(0, 0, 0, 0);
+    lse[k] = -INFINITY;
+    if (real[k]) {
+      ov[k] = *reinterpret_cast<const uint4*>(row_of(p.o, t.b, hq, i) + gl * 8);
+      gv[k] = *reinterpret_cast<const uint4*>(row_of(p.go, t.b, hq, i) + gl * 8);
+      if (gl == 0) lse[k] = p.lse[(int64_t(t.b) * p.Hk * p.G + hq) * p.N + i];
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < kIts; ++k) {
+    const __nv_bfloat162* o2 = reinterpret_cast<const __nv_bfloat162*>(&ov[k]);
+    const __nv_bfloat162* g2 = reinterpret_cast<const __nv_bfloat162*>(&gv[k]);
+    float acc = 0.f;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const float2 of = __bfloat1622float2(o2[e]), gf = __bfloat1622float2(g2[e]);
       acc = fmaf(of.x, gf.x, acc);
       acc = fmaf(of.y, gf.y, acc);
     }
-  }
 #pragma unroll
-  for (int d = L / 2; d > 0; d >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, d);
-  if (gl == 0) {
-    float nl = -INFINITY;
-    if (real) {
-      const float l = p.lse[(int64_t(t.b) * p.Hk * p.G + hq) * p.N + i];
-      if (l != -INFINITY) nl = -l * kLog2e;
+    for (int d = L / 2; d > 0; d >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, d);
+    if (gl == 0) {
+      const int64_t r = int64_t(blockIdx.x) * kBlk + first + k * kStep;
+      p.nl[r] = lse[k] == -INFINITY ? -INFINITY : -lse[k] * kLog2e;
+      p.delta[r] = acc;
     }
-    p.nl[r] = nl;
-    p.delta[r] = real ? acc : 0.f;
   }
 }
 
@@ -265,9 +272,8 @@ __host__ __device__ __forceinline__ KvItem kv_item(const Params& p, int64_t x) {
 }
 
 template <int DK, int DV>
-__global__ void __launch_bounds__(KvCfg<DK, DV>::kThreads, 1)
-window_dkdv_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
-                      const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmG, const Params p) {
+__device__ __forceinline__ void dkdv_tile(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV,
+                                          const CUtensorMap& tmG, const Params& p, unsigned index) {
   using C = KvCfg<DK, DV>;
   constexpr int kCols = C::kCols;
   extern __shared__ uint8_t smem_raw[];
@@ -284,7 +290,7 @@ window_dkdv_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const WaitCtl wc{abort_flag, p.wait_limit_ns, 0u, &g_moa_window_bwd_status};
 
-  const KvItem it = kv_item(p, blockIdx.x);
+  const KvItem it = kv_item(p, index);
   const int k0 = it.kt * kBlk;
   const Range range = rows_of_tokens(p.mask, it.kt, p.N, p.Nk, p.PT);
   const int all = range.n * p.chunks;
@@ -612,9 +618,8 @@ struct QCfg : Warps<parts_of(DK, DV)> {
 };
 
 template <int DK, int DV>
-__global__ void __launch_bounds__(QCfg<DK, DV>::kThreads, 1)
-window_dq_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
-                    const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmG, const Params p) {
+__device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV,
+                                        const CUtensorMap& tmG, const Params& p, unsigned index) {
   using C = QCfg<DK, DV>;
   constexpr int kCols = C::kCols;
   extern __shared__ uint8_t smem_raw[];
@@ -632,8 +637,8 @@ window_dq_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   const WaitCtl wc{abort_flag, p.wait_limit_ns, 0u, &g_moa_window_bwd_status};
 
   // the last positions, which see the most without a window, come first
-  const int64_t per = int64_t(p.chunks) * p.n_pt, group = blockIdx.x / per;
-  const int64_t tile_id = group * per + (per - 1 - (blockIdx.x - group * per));
+  const int64_t per = int64_t(p.chunks) * p.n_pt, group = index / per;
+  const int64_t tile_id = group * per + (per - 1 - (index - group * per));
   const RowTile t = row_tile(p, tile_id);
   const int i1 = t.i0 + p.PT - 1 < p.N ? t.i0 + p.PT - 1 : p.N - 1;
   const win::Tiles list = win::tiles_of(p.mask, p.Nk, p.N, t.i0, i1, kBlk);
@@ -843,6 +848,18 @@ window_dq_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   }
 }
 
+// CTAs below n_kv: dK and dV; the others: dQ, which are shorter and fill the SMs that run out of the former.
+template <int DK, int DV>
+__global__ void __launch_bounds__(KvCfg<DK, DV>::kThreads, 1)
+window_bwd_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                     const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmG, const Params p,
+                     unsigned n_kv) {
+  if (blockIdx.x < n_kv)
+    dkdv_tile<DK, DV>(tmQ, tmK, tmV, tmG, p, blockIdx.x);
+  else
+    dq_tile<DK, DV>(tmQ, tmK, tmV, tmG, p, blockIdx.x - n_kv);
+}
+
 // ------------------------------------------------------------------------------------------------
 // Host side
 // ------------------------------------------------------------------------------------------------
@@ -908,10 +925,10 @@ template <int DK, int DV>
 int launch(const WindowBwdArgs& a, char* msg, size_t msglen) {
   using CK = KvCfg<DK, DV>;
   using CQ = QCfg<DK, DV>;
-  auto kv = window_dkdv_tc_kernel<DK, DV>;
-  auto dq = window_dq_tc_kernel<DK, DV>;
-  cudaError_t e = ensure_smem_limit(reinterpret_cast<const void*>(kv), CK::kSmemBytes);
-  if (e == cudaSuccess) e = ensure_smem_limit(reinterpret_cast<const void*>(dq), CQ::kSmemBytes);
+  auto kern = window_bwd_tc_kernel<DK, DV>;
+  static_assert(int(CK::kThreads) == int(CQ::kThreads), "one launch");
+  constexpr int kSmem = CK::kSmemBytes > CQ::kSmemBytes ? CK::kSmemBytes : CQ::kSmemBytes;
+  cudaError_t e = ensure_smem_limit(reinterpret_cast<const void*>(kern), kSmem);
   const Plan plan(a);
   const Work w(a, plan);
   uint8_t* ws = static_cast<uint8_t*>(a.ws);
@@ -949,17 +966,15 @@ int launch(const WindowBwdArgs& a, char* msg, size_t msglen) {
       !encode_bf16_map_nd(&mk, a.k.p, 4, k_dims, k_str, kv_box, msg, msglen) ||
       !encode_bf16_map_nd(&mv, a.v.p, 4, v_dims, v_str, kv_box, msg, msglen))
     return 5;
-  const int64_t rows = plan.row_tiles * kBlk, threads = rows * (DV / 8);
   if (e == cudaSuccess)
-    e = launch_overlapped(window_delta_tc_kernel<DV>, dim3(unsigned((threads + 255) / 256)), dim3(256), 0, a.stream, p, rows);
+    e = launch_overlapped(window_delta_tc_kernel<DV>, dim3(unsigned(plan.row_tiles)), dim3(256), 0, a.stream, p);
   if (e == cudaSuccess)
-    e = launch_overlapped(kv, dim3(unsigned(plan.items)), dim3(CK::kThreads), CK::kSmemBytes, a.stream, mq, mk, mv, mg, p);
+    e = launch_overlapped(kern, dim3(unsigned(plan.items + plan.row_tiles)), dim3(CK::kThreads), kSmem, a.stream, mq, mk, mv, mg, p,
+                          unsigned(plan.items));
   const int64_t joined = bh * plan.cut * kBlk * ((DK + DV) / 4);
   if (e == cudaSuccess && joined > 0)
     e = launch_overlapped(window_dkdv_tc_join_kernel<DK, DV>, dim3(unsigned((joined + 255) / 256)), dim3(256), 0, a.stream, p,
                           joined);
-  if (e == cudaSuccess)
-    e = launch_overlapped(dq, dim3(unsigned(plan.row_tiles)), dim3(CQ::kThreads), CQ::kSmemBytes, a.stream, mq, mk, mv, mg, p);
   if (e != cudaSuccess) {
     snprintf(msg, msglen, "gradients of attention with a window: %s", cudaGetErrorString(e));
     return 5;

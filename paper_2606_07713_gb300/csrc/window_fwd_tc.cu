@@ -20,7 +20,7 @@
 // twice the rows.
 //
 // Hidden tokens: a tile that some row sees only in part is masked by words of bits, -infinity in place of the
-// score.  Past a sequence's end the cache may hold anything: the values' rows there are zeroed in
+// score.  Past a sequence's end the cache may hold anything: the softmax threads zero the values' rows there in
 // shared memory before the product.  Any other hidden value that is not finite (0 * NaN) makes the output NaN;
 // rows whose output is not finite are computed again at the end, token by token, from what they do see
 // (exact_row).  That costs nothing where all values are finite.
@@ -79,8 +79,8 @@ struct Cfg {
   // item_full[2], item_empty[2]
   static constexpr int kNumBars = 2 * kStages + 17;
   static constexpr int kOffMisc = kOffBar + kNumBars * 8;
-  static constexpr int kOffItems = (kOffMisc + 12 + 15) / 16 * 16;   // two items, then scan[12] and found[2]
-  static constexpr int kSmemBytes = kOffItems + 2 * 32 + 14 * 8 + 1024;
+  static constexpr int kOffItems = (kOffMisc + 12 + 15) / 16 * 16;   // two items, then scan[12] and the share's beginning
+  static constexpr int kSmemBytes = kOffItems + 2 * 32 + 15 * 8 + 1024;
   static constexpr int kEarlyChunks = DV == 64 ? 2 : 4;   // of 32 tokens, exponentials before the wait for P's buffer
   static constexpr uint32_t kTmemCols = 512;
   static constexpr uint32_t kTmemS0 = 0, kTmemS1 = kSharedS ? 0 : 128;
@@ -245,14 +245,61 @@ __device__ __noinline__ void exact_row(const __nv_bfloat16* q, __nv_bfloat16* o,
   for (int e = 0; e < NV; ++e) o[lane * NV + e] = __float2bfloat16(acc[e] * inv);
 }
 
+// Zeros in a row of a values' tile that has arrived, or false.  (A function of its own: an item's last tile only.)
+template <int DV>
+__device__ __noinline__ bool zero_row(uint8_t* tile, int row, bool mine, uint32_t full, uint32_t parity, const WaitCtl& wc) {
+  const bool ok = wait_bounded(full, parity, wc);
+  if (mine) {
+#pragma unroll
+    for (int q = 0; q < DV / 64; ++q)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) reinterpret_cast<uint4*>(tile + q * 128 * 128 + row * 128)[e] = make_uint4(0, 0, 0, 0);
+  }
+  fence_proxy_async_smem();
+  return ok;
+}
+
+// What a CTA needs to find its share again, in shared memory: the item in which it begins, that item's first unit, all units.
+struct Begin {
+  int64_t item, unit, total;
+};
+
+// Rows of a CTA's whole items whose output is not finite, again: a softmax warp a row.  (A function of its own: what it holds
+// would cost the softmax loop registers.)
+template <int DK, int DV, int QT>
+__device__ __noinline__ void whole_rows_again(const __nv_bfloat16* Q, __nv_bfloat16* O, const Params& p, const Begin* begin) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const Shares shares(begin->total, gridDim.x);
+  const int64_t first_unit = shares.start(blockIdx.x), stop = shares.start(blockIdx.x + 1);
+  int64_t before = begin->unit;
+  for (int item = int(begin->item); before < stop; ++item) {
+    const int64_t end = before + units_of<QT>(p, item, false) + kItemUnits;
+    // its tiles, which come after its first units, are all in this share
+    if (before + kItemUnits >= first_unit && end <= stop) {
+      const Where w = where_of<QT>(p, item);
+      for (int r = warp; r < kBM * QT; r += 4 * QT) {
+        const int tile = r / kBM, in_tile = r - tile * kBM, row_pos = in_tile / p.GC;
+        const int g = w.chunk * p.GC + in_tile - row_pos * p.GC, hq = w.h * p.G + g, i = w.i0 + tile * p.PT + row_pos;
+        if (row_pos >= p.PT || g >= p.G || i >= p.N) continue;
+        __nv_bfloat16* o = O + int64_t(w.b) * p.o_sb + int64_t(hq) * p.o_sh + int64_t(i) * p.o_sn;
+        bool bad = false;
+        for (int e = lane; e < DV; e += 32) bad |= not_finite(__bfloat162float(o[e]));
+        if (__any_sync(0xffffffffu, bad))
+          exact_row<DK, DV>(Q + int64_t(w.b) * p.q_sb + int64_t(hq) * p.q_sh + int64_t(i) * p.q_sn, o, p, w.b, w.h, i);
+      }
+    }
+    before = end;
+  }
+}
+
 // ------------------------------------------------------------------------------------------------
 // Attention
 // ------------------------------------------------------------------------------------------------
 template <int DK, int DV, int QT>
 __global__ void __launch_bounds__(Cfg<DK, DV, QT>::kThreads, 1)
 window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
-                 const __grid_constant__ CUtensorMap tmV, __nv_bfloat16* O, float* lse, float* part_o, float2* part_ml,
-                 Cut* cuts, uint8_t* odd, const Params p) {
+                 const __grid_constant__ CUtensorMap tmV, const __nv_bfloat16* Q, __nv_bfloat16* O, float* lse, float* part_o,
+                 float2* part_ml, Cut* cuts, const Params p) {
   using C = Cfg<DK, DV, QT>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -269,9 +316,10 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
   auto item_empty = [&](int i) { return q_full + 8u * (15 + i); };
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::kOffMisc);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::kOffMisc + 4);
+  volatile int* any_odd = reinterpret_cast<volatile int*>(smem + C::kOffMisc + 8);   // an item's row is to be computed again
   volatile Item* items = reinterpret_cast<volatile Item*>(smem + C::kOffItems);
   int64_t* scan = reinterpret_cast<int64_t*>(smem + C::kOffItems + 64);   // warp sums
-  int64_t* found = scan + 12;                                             // item, its first unit
+  Begin* found = reinterpret_cast<Begin*>(scan + 12);
   constexpr int kWarps = C::kThreads / 32;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const WaitCtl wc{abort_flag, p.wait_limit_ns, 0u, &g_moa_window_tc_status};
@@ -296,6 +344,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       mbar_init(p_free(j), 1);
     }
     *abort_flag = 0;
+    *any_odd = 0;
     fence_barrier_init();
   }
   if (warp == C::kMmaWarp0) {
@@ -308,23 +357,9 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     fence_proxy_async_smem();
   }
   wait_for_previous();
-  // this CTA's share of all units, and the item in which it begins
-  int64_t sum = 0;
-  for (int i = threadIdx.x; i < p.n_items; i += C::kThreads) sum += units_of<QT>(p, i, true) + kItemUnits;
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-  if (lane == 0) scan[warp] = sum;
-  __syncthreads();
-  int64_t total = 0;
-#pragma unroll
-  for (int w = 0; w < kWarps; ++w) total += scan[w];
-  const Shares shares(total, gridDim.x);
-  const int64_t first_unit = blockIdx.x < shares.n ? shares.start(blockIdx.x) : total;
-  const int64_t stop = blockIdx.x < shares.n ? shares.start(blockIdx.x + 1) : total;
-  int64_t done = 0;
-  for (int base = 0; first_unit < stop; base += C::kThreads) {
-    const int i = base + threadIdx.x;
-    const int64_t mine = i < p.n_items ? units_of<QT>(p, i, false) + kItemUnits : 0;
+  // this CTA's share of all units, and the item in which it begins: the sum of all units, then their running sum
+  // (the same pass where there is an item for each thread at most)
+  auto block_scan = [&](int64_t mine, int64_t* all) {
     int64_t incl = mine;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -334,19 +369,32 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     __syncthreads();
     if (lane == 31) scan[warp] = incl;
     __syncthreads();
-    int64_t all = 0;
+    *all = 0;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
       if (w < warp) incl += scan[w];
-      all += scan[w];
+      *all += scan[w];
     }
-    incl += done;
-    done += all;
-    if (first_unit >= incl - mine && first_unit < incl) {
-      found[0] = i;
-      found[1] = incl - mine;
+    return incl;
+  };
+  const bool one_pass = p.n_items <= C::kThreads;
+  int64_t mine = 0;
+  for (int i = threadIdx.x; i < p.n_items; i += C::kThreads) mine += units_of<QT>(p, i, true) + kItemUnits;
+  int64_t total, incl = block_scan(mine, &total);
+  const Shares shares(total, gridDim.x);
+  const int64_t first_unit = blockIdx.x < shares.n ? shares.start(blockIdx.x) : total;
+  const int64_t stop = blockIdx.x < shares.n ? shares.start(blockIdx.x + 1) : total;
+  int64_t done = 0;
+  for (int base = 0; first_unit < stop; base += C::kThreads) {
+    const int i = base + threadIdx.x;
+    if (!one_pass) {
+      int64_t all;
+      mine = i < p.n_items ? units_of<QT>(p, i, false) + kItemUnits : 0;
+      incl = block_scan(mine, &all) + done;
+      done += all;
     }
-    if (first_unit < done) break;
+    if (first_unit >= incl - mine && first_unit < incl) *found = Begin{i, incl - mine, total};
+    if (one_pass || first_unit < done) break;
   }
   if (threadIdx.x == 0) cuts[blockIdx.x].pieces = 0;
   tc_fence_before_sync();
@@ -470,114 +518,94 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       }
     } else if (warp == C::kMmaWarp0 || (QT == 2 && warp == C::kMmaWarp1)) {
       // ------------------------------------------------------------ MMA issuers, one for each row tile
-      const int j = warp == C::kMmaWarp0 ? 0 : 1;
-      constexpr uint32_t kIdescQK = make_idesc(kBM, kBN, false);
-      constexpr uint32_t kIdescPV = make_idesc(kBM, DV, true);
-      const uint32_t tS = tmem + (j ? C::kTmemS1 : C::kTmemS0);
-      const uint32_t tP = tmem + (j ? C::kTmemP1 : C::kTmemP0);
-      const uint32_t tO = tmem + (j ? C::kTmemO1 : C::kTmemO0);
-      const uint32_t sQj = sQ + j * C::kQTileBytes;
-      int slot = 0;
-      uint32_t phase = 0;
-      uint32_t t = 0;   // tiles so far: the phases of the barriers between the roles
-      auto next = [&]() {
-        if (++slot == C::kStages) {
-          slot = 0;
-          phase ^= 1u;
-        }
-      };
-      auto issue_qk = [&](uint32_t kb) {
+      if (lane == 0) {
+        const int j = warp == C::kMmaWarp0 ? 0 : 1;
+        constexpr uint32_t kIdescQK = make_idesc(kBM, kBN, false);
+        constexpr uint32_t kIdescPV = make_idesc(kBM, DV, true);
+        const uint32_t tS = tmem + (j ? C::kTmemS1 : C::kTmemS0);
+        const uint32_t tP = tmem + (j ? C::kTmemP1 : C::kTmemP0);
+        const uint32_t tO = tmem + (j ? C::kTmemO1 : C::kTmemO0);
+        const uint32_t sQj = sQ + j * C::kQTileBytes;
+        int slot = 0;
+        uint32_t phase = 0;
+        uint32_t t = 0;   // tiles so far: the phases of the barriers between the roles
+        auto next = [&]() {
+          if (++slot == C::kStages) {
+            slot = 0;
+            phase ^= 1u;
+          }
+        };
+        auto issue_qk = [&](uint32_t kb) {
 #pragma unroll
-        for (int kk = 0; kk < DK / 16; ++kk) {
-          const uint32_t off = (kk >> 2) * C::kPanelBytes + (kk & 3) * 32;
-          mma_f16_ss(tS, make_sdesc_sw128(sQj + off, 16, 1024), make_sdesc_sw128(kb + off, 16, 1024), kIdescQK,
-                     kk > 0 ? 1u : 0u);
-        }
-      };
-      auto issue_pv = [&](uint32_t vb, uint32_t acc_first) {
+          for (int kk = 0; kk < DK / 16; ++kk) {
+            const uint32_t off = (kk >> 2) * C::kPanelBytes + (kk & 3) * 32;
+            mma_f16_ss(tS, make_sdesc_sw128(sQj + off, 16, 1024), make_sdesc_sw128(kb + off, 16, 1024), kIdescQK,
+                       kk > 0 ? 1u : 0u);
+          }
+        };
+        auto issue_pv = [&](uint32_t vb, uint32_t acc_first) {
 #pragma unroll
-        for (int kk = 0; kk < kBN / 16; ++kk)
-          mma_f16_ts(tO, tP + kk * 8, make_sdesc_sw128(vb + kk * 2048, C::kPanelBytes, 1024), kIdescPV,
-                     kk > 0 ? 1u : acc_first);
-      };
-      // The S buffer may take tile u's scores once its last reader holds what it has: this row
-      // tile's softmax (tile u - 1), or with one buffer for both, the other one's (tile u - 1 for
-      // row tile 0, tile u for row tile 1).
-      auto s_buffer = [&](uint32_t u) {
-        if (C::kSharedS) return j ? wait_warp(s_free(0), u & 1u) : u == 0 || wait_warp(s_free(1), (u - 1) & 1u);
-        return u == 0 || wait_warp(s_free(j), (u - 1) & 1u);
-      };
-      bool ok = true;
-      for (uint32_t seg = 0; ok; ++seg) {
-        const Item x = get_item(seg, ok);
-        if (x.item < 0) break;
-        __syncwarp();
-        if (lane == 0) mbar_arrive(item_empty(seg & 1));
-        const int n_kt = x.u1 - x.u0;
-        const win::Tiles list{x.first, x.from, x.units};
-        ok = wait_warp(q_full, seg & 1u) && wait_warp(full_bar(slot), phase) && s_buffer(t);
-        if (ok) {
-          tc_fence_after_sync();
-          const int ks = slot;
-          next();
-          if (lane == 0) {
+          for (int kk = 0; kk < kBN / 16; ++kk)
+            mma_f16_ts(tO, tP + kk * 8, make_sdesc_sw128(vb + kk * 2048, C::kPanelBytes, 1024), kIdescPV,
+                       kk > 0 ? 1u : acc_first);
+        };
+        // The S buffer may take tile u's scores once its last reader holds what it has: this row
+        // tile's softmax (tile u - 1), or with one buffer for both, the other one's (tile u - 1 for
+        // row tile 0, tile u for row tile 1).
+        auto s_buffer = [&](uint32_t u) {
+          if (C::kSharedS) return j ? wait_bounded(s_free(0), u & 1u, wc) : u == 0 || wait_bounded(s_free(1), (u - 1) & 1u, wc);
+          return u == 0 || wait_bounded(s_free(j), (u - 1) & 1u, wc);
+        };
+        bool ok = true;
+        for (uint32_t seg = 0; ok; ++seg) {
+          ok = wait_bounded(item_full(seg & 1), seg >> 1 & 1u, wc);
+          const volatile Item& xi = items[seg & 1];
+          const int item = xi.item, n_kt = xi.u1 - xi.u0;
+          if (!ok || item < 0) break;
+          mbar_arrive(item_empty(seg & 1));
+          ok = wait_bounded(q_full, seg & 1u, wc) && wait_bounded(full_bar(slot), phase, wc) && s_buffer(t);
+          if (ok) {
+            tc_fence_after_sync();
+            const int ks = slot;
+            next();
             issue_qk(sKV + ks * C::kStageBytes);
             mma_commit(s_full(j));
             mma_commit(empty_bar(ks));
             if (n_kt == 1) mma_commit(q_empty);
           }
-        }
-        for (int n = 0; ok && n < n_kt; ++n, ++t) {
-          if (n + 1 < n_kt) {
-            const int ks = slot;
-            ok = wait_warp(full_bar(slot), phase) && s_buffer(t + 1);
-            next();
-            if (!ok) break;
-            tc_fence_after_sync();
-            if (lane == 0) {
+          for (int n = 0; ok && n < n_kt; ++n, ++t) {
+            if (n + 1 < n_kt) {
+              const int ks = slot;
+              ok = wait_bounded(full_bar(slot), phase, wc) && s_buffer(t + 1);
+              next();
+              if (!ok) break;
+              tc_fence_after_sync();
               issue_qk(sKV + ks * C::kStageBytes);
               mma_commit(s_full(j));
               mma_commit(empty_bar(ks));
               if (n + 2 == n_kt) mma_commit(q_empty);
             }
-          }
-          const int vs = slot;
-          ok = wait_warp(full_bar(slot), phase);
-          if (p.kv.table != nullptr) {
-            // rows past the sequence's end hold whatever the page held
-            const int gone = x.len - list.at(x.u0 + n) * kBN;   // the first one
-            if (ok && gone < kBN) {
-              const int z = gone < 0 ? 0 : gone;
-#pragma unroll
-              for (int q = 0; q < DV / 64; ++q)
-                for (int e = lane; e < (kBN - z) * 8; e += 32)
-                  reinterpret_cast<uint4*>(smem + C::kOffKV + vs * C::kStageBytes + q * C::kPanelBytes + z * 128)[e] =
-                      make_uint4(0, 0, 0, 0);
-              fence_proxy_async_smem();
-            }
-          }
-          ok = ok && wait_warp(p_ready(j), t & 1u);
-          next();
-          if (!ok) break;
-          tc_fence_after_sync();
-          if (lane == 0) {
+            const int vs = slot;
+            ok = wait_bounded(full_bar(slot), phase, wc) && wait_bounded(p_ready(j), t & 1u, wc);
+            next();
+            if (!ok) break;
+            tc_fence_after_sync();
             issue_pv(sKV + vs * C::kStageBytes, n > 0 ? 1u : 0u);
             mma_commit(p_free(j));
             mma_commit(empty_bar(vs));
           }
+          // arrives when the item's products are complete
+          mma_commit(o_done(j));
         }
-        // arrives when the item's products are complete
-        if (lane == 0) mma_commit(o_done(j));
-        __syncwarp();
+        mma_commit(drain);
       }
-      if (lane == 0) mma_commit(drain);
     } else if (warp == C::kWalkWarp && lane == 0) {
       // ------------------------------------------------------------ the items of the share
       int64_t at = first_unit, before = 0;
       int item = 0;
       if (at < stop) {
-        item = int(found[0]);
-        before = found[1];
+        item = int(found->item);
+        before = found->unit;
       }
       for (uint32_t seg = 0;; ++seg) {
         int units = 0, u0 = 0, u1 = 0, which = -1, len = 0;
@@ -618,35 +646,51 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     const float c = fmaxf(p.c_log2, FLT_MIN);   // not zero: c * -infinity hides a token
     const int row_pos = int(unsigned(row) / unsigned(p.GC)), row_head = row - row_pos * p.GC;
     bool ok = true;
-    uint32_t t = 0;
+    uint32_t t = 0, ring = 0;   // tiles and stages of the ring before this item
     for (uint32_t seg = 0;; ++seg) {
       const Item x = get_item(seg, ok);
       if (x.item < 0) break;
-      const Where w = where_of<QT>(p, x.item);
-      const win::Tiles list{x.first, x.from, x.units};
-      const int g = w.chunk * p.GC + row_head, i = w.i0 + j * p.PT + row_pos;
-      const bool live = row_pos < p.PT && g < p.G && i < p.N;
-      const bool live_warp = __any_sync(0xffffffffu, live);
+      const win::Tiles list{x.first, x.from, 0};
+      // where the thread's row lies
+      struct Place {
+        int b, hq, i;
+        bool live;
+      };
+      auto place = [&](int item) {
+        const Where w = where_of<QT>(p, item);
+        const int g = w.chunk * p.GC + row_head, i = w.i0 + j * p.PT + row_pos;
+        return Place{w.b, w.h * p.G + g, i, row_pos < p.PT && g < p.G && i < p.N};
+      };
       int lim = 0x7fffffff, low = 0;
-      if (live) {
-        lim = win::row_end(p.mask, x.len, p.N, i);
-        low = win::row_low(p.mask, x.len, p.N, i);
-      }
-      float m = -INFINITY, l = 0.f;
-      for (int n = x.u0; n < x.u1; ++n, ++t) {
-        if (!wait_warp(s_full(j), t & 1u)) {
-          ok = false;
-          break;
+      bool live_warp;
+      {
+        const Place w = place(x.item);
+        live_warp = __any_sync(0xffffffffu, w.live);
+        if (w.live) {
+          lim = win::row_end(p.mask, x.len, p.N, w.i);
+          low = win::row_low(p.mask, x.len, p.N, w.i);
         }
+      }
+      // past the sequence's end a page holds whatever it held: the first such token, of a cache
+      const int gone = p.kv.table != nullptr ? x.len : 0x7fffffff;
+      float m = -INFINITY, l = 0.f;
+      for (int n = x.u0; ok && n < x.u1; ++n, ++t) {
+        const int n0 = list.at(n) * kBN;
+        // Waits that run out leave the loop together, at its end: until then what they would have brought is used
+        // as it is.
+        ok = wait_bounded(s_full(j), t & 1u, wc);
         tc_fence_after_sync();
+        if (gone - n0 < kBN) {   // the item's last tile: zeros in the place of the thread's row of values
+          const int k = n - x.u0, at = int(ring) + (n + 1 < x.u1 ? 2 * k + 2 : 2 * k + 1);
+          ok = zero_row<DV>(smem + C::kOffKV + at % C::kStages * C::kStageBytes, row, n0 + row >= gone, full_bar(at % C::kStages),
+                            at / C::kStages & 1, wc) && ok;
+        }
         if (!live_warp) {   // rows that are not there: in step with the others, and no more
           tc_fence_before_sync();
           mbar_arrive(s_free(j));
-          if (t > 0 && !wait_warp(p_free(j), (t - 1) & 1u)) {
-            ok = false;
-            break;
-          }
+          if (t > 0) ok = wait_bounded(p_free(j), (t - 1) & 1u, wc) && ok;
           mbar_arrive(p_ready(j));
+          ok = __all_sync(0xffffffffu, ok);
           continue;
         }
         uint32_t sr[128];
@@ -654,7 +698,6 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         tc_fence_before_sync();
         mbar_arrive(s_free(j));
         float* s = reinterpret_cast<float*>(sr);
-        const int n0 = list.at(n) * kBN;
         if (!__all_sync(0xffffffffu, lim - n0 >= kBN && (n0 >= low || n0 + kBN <= p.mask.sinks))) {
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
@@ -699,10 +742,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
 #pragma unroll
         for (int ch = 0; ch < kEarly; ++ch) exp_chunk(ch, pe + 16 * ch);
         // P_j's buffer is free, and O_j may be rescaled, once the previous tile's product is done
-        if (t > 0 && !wait_warp(p_free(j), (t - 1) & 1u)) {
-          ok = false;
-          break;
-        }
+        if (t > 0) ok = wait_bounded(p_free(j), (t - 1) & 1u, wc) && ok;
         tc_fence_after_sync();
 #pragma unroll
         for (int ch = 0; ch < kEarly; ++ch) store_chunk(ch, pe + 16 * ch);
@@ -717,13 +757,16 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         tmem_wait_st();
         tc_fence_before_sync();
         mbar_arrive(p_ready(j));
+        ok = __all_sync(0xffffffffu, ok);
       }
       if (!ok || !wait_warp(o_done(j), seg & 1u)) break;
       tc_fence_after_sync();
       // the item is written, or this CTA's piece of it
-      const bool first_piece = x.u0 == 0, whole = first_piece && x.u1 == x.units;
+      const volatile Item& xi = items[seg & 1];
+      ring += 2u * uint32_t(xi.u1 - xi.u0);
+      const bool first_piece = xi.u0 == 0, whole = first_piece && xi.u1 == xi.units;
       if (live_warp) {
-        const int hq = w.h * p.G + g;
+        const Place w = place(xi.item);
         bool bad = false;
         if (!whole) {
           const int64_t at = (int64_t(blockIdx.x) * 2 + first_piece) * C::kRows + j * kBM + row;
@@ -733,7 +776,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             tmem_ld_32x32b_x16(tO + d, o);
             tmem_wait_ld();
             reg_anchor_x16(o);
-            if (live) {
+            if (w.live) {
               float4* dst = reinterpret_cast<float4*>(part_o + at * DV + d);
 #pragma unroll
               for (int e = 0; e < 4; ++e)
@@ -741,36 +784,35 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                                      __uint_as_float(o[4 * e + 3]));
             }
           }
-          if (live) part_ml[at] = make_float2(m, l);
+          if (w.live) part_ml[at] = make_float2(m, l);
         } else {
           const float inv = l == 0.f ? 0.f : 1.f / l;
-          __nv_bfloat16* orow = O + int64_t(w.b) * p.o_sb + int64_t(hq) * p.o_sh + int64_t(i) * p.o_sn;
-          if (lse != nullptr && live)
-            lse[(int64_t(w.b) * p.Hk * p.G + hq) * p.N + i] = l == 0.f ? -INFINITY : (m + lg2_approx(l)) * kLn2;
+          __nv_bfloat16* orow = O + int64_t(w.b) * p.o_sb + int64_t(w.hq) * p.o_sh + int64_t(w.i) * p.o_sn;
+          if (lse != nullptr && w.live)
+            lse[(int64_t(w.b) * p.Hk * p.G + w.hq) * p.N + w.i] = l == 0.f ? -INFINITY : (m + lg2_approx(l)) * kLn2;
+          float top = 0.f;
 #pragma unroll
           for (int d = 0; d < DV; d += 16) {
             uint32_t o[16];
             tmem_ld_32x32b_x16(tO + d, o);
             tmem_wait_ld();
             reg_anchor_x16(o);
-            float y[16], top = 0.f;
+            uint32_t z[8];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              y[e] = __uint_as_float(o[e]) * inv;
-              top += y[e] * 0.f;   // not zero if one is not finite
+            for (int e = 0; e < 8; ++e) {
+              const float y0 = __uint_as_float(o[2 * e]) * inv, y1 = __uint_as_float(o[2 * e + 1]) * inv;
+              top = fmaf(y0, 0.f, top);   // not zero if one is not finite
+              top = fmaf(y1, 0.f, top);
+              z[e] = pack_bf16x2(y0, y1);
             }
-            if (live) {
-              bad |= top != 0.f;
-              uint32_t z[8];
-#pragma unroll
-              for (int e = 0; e < 8; ++e) z[e] = pack_bf16x2(y[2 * e], y[2 * e + 1]);
+            if (w.live) {
               reinterpret_cast<uint4*>(orow + d)[0] = make_uint4(z[0], z[1], z[2], z[3]);
               reinterpret_cast<uint4*>(orow + d)[1] = make_uint4(z[4], z[5], z[6], z[7]);
             }
           }
+          bad = __any_sync(0xffffffffu, w.live && top != 0.f);
         }
-        bad = __any_sync(0xffffffffu, bad);
-        if (lane == 0 && first_piece) odd[int64_t(x.item) * 8 + warp] = bad;   // (a cut item's rows are looked at when joined)
+        if (bad && lane == 0) *any_odd = 1;   // (a cut item's rows are looked at when joined)
       }
       tc_fence_before_sync();   // O is read: the next item's first product (after p_ready) may write it
       __syncwarp();
@@ -787,83 +829,88 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     tc_fence_after_sync();
     tmem_dealloc(tmem, C::kTmemCols);
   }
+  if (*any_odd != 0 && warp < C::kMmaWarp0) whole_rows_again<DK, DV, QT>(Q, O, p, found);
 }
 
-// Joins the pieces of cut items, one warp a row, and computes rows again whose output is not finite: of the
-// joined ones, and of whole items that are marked.  CTA (x, y): eight rows of CTA x's cut, and of the marked
-// ones among items x, x + gridDim.x, ...
+// Joins the pieces of cut items: CTA (x, y) 32 / WS rows of CTA x's cut, four for every WS warps, eight lanes a row (a row a
+// warp spent most of its instructions on places: the call of 4 x 16 heads x 2048 x 64 took 78 us in place of 67); each of the WS warps takes
+// every WS-th piece, where items have many.  Rows whose output is not finite are computed again.
+constexpr int kJoinRows = 4;
 template <int DK, int DV, int QT>
 __global__ void __launch_bounds__(256)
 window_tc_join_kernel(const __nv_bfloat16* Q, __nv_bfloat16* O, float* lse, const float* part_o, const float2* part_ml,
-                      const Cut* cuts, const uint8_t* odd, const Params p) {
-  constexpr int kRows = kBM * QT;
+                      const Cut* cuts, const Params p, int WS) {
+  constexpr int kRows = kBM * QT, kQuads = DV / 32;
+  __shared__ float4 s_x[8][32][kQuads];
+  __shared__ float s_l[8][kJoinRows];
   wait_for_previous();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = int(blockIdx.y) * 8 + warp;
+  const Cut cut = cuts[blockIdx.x];
+  if (cut.pieces == 0) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, turn = warp % WS, sub = lane & 7;
+  const int row = (int(blockIdx.y) * (8 / WS) + warp / WS) * kJoinRows + (lane >> 3);
+  const Where w = where_of<QT>(p, cut.item);
   const int tile = row / kBM, in_tile = row - tile * kBM;
   const int row_pos = int(unsigned(in_tile) / unsigned(p.GC)), row_head = in_tile - row_pos * p.GC;
-  struct Row {
-    int b, h, hq, i;
-    bool live;
-  };
-  auto row_of = [&](int item) {
-    const Where w = where_of<QT>(p, item);
-    const int g = w.chunk * p.GC + row_head, i = w.i0 + tile * p.PT + row_pos;
-    return Row{w.b, w.h, w.h * p.G + g, i, row_pos < p.PT && g < p.G && i < p.N};
-  };
-  auto out = [&](const Row& r) { return O + int64_t(r.b) * p.o_sb + int64_t(r.hq) * p.o_sh + int64_t(r.i) * p.o_sn; };
-  auto again = [&](const Row& r) {
-    exact_row<DK, DV>(Q + int64_t(r.b) * p.q_sb + int64_t(r.hq) * p.q_sh + int64_t(r.i) * p.q_sn, out(r), p, r.b, r.h, r.i);
-  };
-  const Cut cut = cuts[blockIdx.x];
-  if (cut.pieces != 0) {
-    const Row r = row_of(cut.item);
-    if (r.live) {
-      auto place = [&](int k) -> int64_t { return ((int64_t(blockIdx.x) + k) * 2 + (k == 0)) * kRows + row; };
-      float M = -INFINITY;
-      for (int k = lane; k < cut.pieces; k += 32) M = fmaxf(M, part_ml[place(k)].x);
+  const int g = w.chunk * p.GC + row_head, hq = w.h * p.G + g, i = w.i0 + tile * p.PT + row_pos;
+  const bool live = row < kRows && row_pos < p.PT && g < p.G && i < p.N;
+  if (WS == 1 && !__any_sync(0xffffffffu, live)) return;
+  auto place = [&](int k) -> int64_t { return ((int64_t(blockIdx.x) + k) * 2 + (k == 0)) * kRows + row; };
+  float M = -INFINITY, L = 0.f;
+  float4 x[kQuads];
 #pragma unroll
-      for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
-      const float base = M == -INFINITY ? 0.f : M;
-      float L = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-      for (int k = 0; k < cut.pieces; ++k) {
-        const float2 ml = part_ml[place(k)];
-        const float f = ex2_approx(ml.x - base);
-        L += f * ml.y;
-        if (lane * 4 < DV) {
-          const float4 v = *reinterpret_cast<const float4*>(part_o + place(k) * DV + lane * 4);
-          x[0] += f * v.x, x[1] += f * v.y, x[2] += f * v.z, x[3] += f * v.w;
-        }
-      }
-      const float inv = L == 0.f ? 0.f : 1.f / L;
-      bool bad = false;
+  for (int q = 0; q < kQuads; ++q) x[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (live)
+    for (int k = sub; k < cut.pieces; k += 8) M = fmaxf(M, part_ml[place(k)].x);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        x[e] *= inv;
-        bad |= not_finite(x[e]);
+  for (int d = 4; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+  const float base = M == -INFINITY ? 0.f : M;
+  if (live) {
+#pragma unroll 2
+    for (int k = turn; k < cut.pieces; k += WS) {
+      const int64_t at = place(k);
+      const float2 ml = part_ml[at];
+      const float f = ex2_approx(ml.x - base);
+      L += f * ml.y;
+#pragma unroll
+      for (int q = 0; q < kQuads; ++q) {
+        const float4 v = *reinterpret_cast<const float4*>(part_o + at * DV + (sub + 8 * q) * 4);
+        x[q].x += f * v.x, x[q].y += f * v.y, x[q].z += f * v.z, x[q].w += f * v.w;
       }
-      if (lane * 4 < DV)
-        *reinterpret_cast<uint2*>(out(r) + lane * 4) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
-      if (lse != nullptr && lane == 0)
-        lse[(int64_t(r.b) * p.Hk * p.G + r.hq) * p.N + r.i] = L == 0.f ? -INFINITY : (M + lg2_approx(L)) * kLn2;
-      __syncwarp();
-      if (__any_sync(0xffffffffu, bad)) again(r);
     }
   }
-  // whole items: one mark for each 32 rows
-  for (int64_t base = blockIdx.x; base < p.n_items; base += 32 * int64_t(gridDim.x)) {
-    const int64_t mine = base + lane * int64_t(gridDim.x);
-    uint32_t marked = __ballot_sync(0xffffffffu, mine < p.n_items && odd[mine * 8 + row / 32] == 1);
-    while (marked != 0) {
-      const int k = __ffs(marked) - 1;
-      marked &= marked - 1;
-      const int item = int(base + k * int64_t(gridDim.x));
-      const Row r = row_of(item);
-      if (!r.live) continue;
-      bool bad = false;
-      for (int e = lane; e < DV; e += 32) bad |= not_finite(__bfloat162float(out(r)[e]));
-      if (__any_sync(0xffffffffu, bad)) again(r);
+  if (WS > 1) {   // the other warps' sums, in their order
+#pragma unroll
+    for (int q = 0; q < kQuads; ++q) s_x[warp][lane][q] = x[q];
+    if (sub == 0) s_l[warp][lane >> 3] = L;
+    __syncthreads();
+    if (turn != 0) return;
+    for (int k = 1; k < WS; ++k) {
+      L += s_l[warp + k][lane >> 3];
+#pragma unroll
+      for (int q = 0; q < kQuads; ++q) {
+        const float4 v = s_x[warp + k][lane][q];
+        x[q].x += v.x, x[q].y += v.y, x[q].z += v.z, x[q].w += v.w;
+      }
     }
+  }
+  const float inv = L == 0.f ? 0.f : 1.f / L;
+  __nv_bfloat16* o = O + int64_t(w.b) * p.o_sb + int64_t(hq) * p.o_sh + int64_t(i) * p.o_sn;
+  bool bad = false;
+#pragma unroll
+  for (int q = 0; q < kQuads; ++q) {
+    x[q].x *= inv, x[q].y *= inv, x[q].z *= inv, x[q].w *= inv;
+    bad |= not_finite(x[q].x) || not_finite(x[q].y) || not_finite(x[q].z) || not_finite(x[q].w);
+    if (live)
+      *reinterpret_cast<uint2*>(o + (sub + 8 * q) * 4) = make_uint2(pack_bf16x2(x[q].x, x[q].y), pack_bf16x2(x[q].z, x[q].w));
+  }
+  if (lse != nullptr && live && sub == 0)
+    lse[(int64_t(w.b) * p.Hk * p.G + hq) * p.N + i] = L == 0.f ? -INFINITY : (M + lg2_approx(L)) * kLn2;
+  uint32_t again = __ballot_sync(0xffffffffu, bad && live);
+  for (; again != 0; again &= ~(0xffu << (__ffs(again) - 1 & ~7))) {
+    const int from = __ffs(again) - 1;
+    const int h_ = __shfl_sync(0xffffffffu, hq, from), i_ = __shfl_sync(0xffffffffu, i, from);
+    exact_row<DK, DV>(Q + int64_t(w.b) * p.q_sb + int64_t(h_) * p.q_sh + int64_t(i_) * p.q_sn,
+                      O + int64_t(w.b) * p.o_sb + int64_t(h_) * p.o_sh + int64_t(i_) * p.o_sn, p, w.b, w.h, i_);
   }
 }
 
@@ -886,16 +933,15 @@ struct Plan {
   }
 };
 
-// The workspace: pieces, cuts, marks of whole items.
+// The workspace: pieces, cuts.
 struct Work {
-  int64_t part_o, part_ml, cuts, odd, bytes;
+  int64_t part_o, part_ml, cuts, bytes;
   Work(const WindowArgs& a, const Plan& plan, int sms) {
     const int64_t rows = int64_t(sms) * 2 * kBM * plan.QT;
     part_o = 0;
     part_ml = part_o + rows * a.dv * 4;
     cuts = part_ml + rows * 8;
-    odd = cuts + round_up(int64_t(sms) * sizeof(Cut), 256);
-    bytes = odd + round_up(plan.n_items * 8, 256);
+    bytes = cuts + round_up(int64_t(sms) * sizeof(Cut), 256);
   }
 };
 
@@ -929,7 +975,6 @@ int launch(const WindowArgs& a, const Plan& plan, int sms, char* msg, size_t msg
   float* part_o = reinterpret_cast<float*>(ws + w.part_o);
   float2* part_ml = reinterpret_cast<float2*>(ws + w.part_ml);
   Cut* cuts = reinterpret_cast<Cut*>(ws + w.cuts);
-  uint8_t* odd = ws + w.odd;
   const int64_t G = a.Hq / a.Hk;
   Params p{};
   p.q_sb = a.q.sb, p.q_sh = a.q.sh, p.q_sn = a.q.sn;
@@ -965,11 +1010,16 @@ int launch(const WindowArgs& a, const Plan& plan, int sms, char* msg, size_t msg
   // rows of an item that may be there
   const int64_t positions = a.N < plan.PT ? a.N : plan.PT, live = QT == 2 ? C::kRows : positions * plan.GC;
   e = launch_overlapped(kern, dim3(ctas), dim3(C::kThreads), C::kSmemBytes, a.stream, mq, mk, mv,
-                        static_cast<__nv_bfloat16*>(a.o.p), a.lse, part_o, part_ml, cuts, odd, p);
+                        static_cast<const __nv_bfloat16*>(a.q.p), static_cast<__nv_bfloat16*>(a.o.p), a.lse, part_o, part_ml,
+                        cuts, p);
+  // warps for a row's pieces: about a quarter of the pieces that an item may have
+  const int64_t pieces = ctas / plan.n_items + 1;
+  const int split = pieces <= 4 ? 1 : pieces <= 8 ? 2 : pieces <= 16 ? 4 : 8;
+  const int64_t per = 32 / split;
   if (e == cudaSuccess)
-    e = launch_overlapped(window_tc_join_kernel<DK, DV, QT>, dim3(ctas, unsigned((live + 7) / 8)), dim3(256), 0, a.stream,
+    e = launch_overlapped(window_tc_join_kernel<DK, DV, QT>, dim3(ctas, unsigned((live + per - 1) / per)), dim3(256), 0, a.stream,
                           static_cast<const __nv_bfloat16*>(a.q.p), static_cast<__nv_bfloat16*>(a.o.p), a.lse, part_o, part_ml,
-                          cuts, odd, p);
+                          cuts, p, split);
   if (e != cudaSuccess) {
     snprintf(msg, msglen, "attention with a window: %s", cudaGetErrorString(e));
     return 5;
