@@ -17,17 +17,21 @@
 // dQ apart from dK and dV: seven tile products in place of five, but every sum stays within one CTA (no
 // atomics, the same bits every time).
 //
-// Rows of a key head are counted as in the forward kernel: row r of a 128-row tile is position r / GC, query
-// head r % GC of the group (TMA brings them in that order), so that a window's tiles hold few rows that are hidden, and
-// for a token the rows that see it are one range of a tile's columns, for a row the tokens two ranges.
+// Rows of a key head are counted position by position as in the forward kernel, here in halves of 64: row r of a half is
+// position r / GC, query head r % GC of the group (TMA brings them in that order), so that a window's tiles hold few rows
+// that are hidden; for a token the rows that see it are one range of a half's columns, for a row the tokens two ranges.
+//
+// Score tiles are 128 x 128 (M x N).  With d_k = d_v = 64 the products are short, and a tile's chain of product,
+// exponentials, product, dS, product is what takes the time (@ of the tensor pipe): there N is 64, a CTA takes half of an SM's
+// tensor and shared memory, and the chains of two CTAs an SM overlap.
 //
 // Pieces.  A token's rows are those of a window; a sink's are all later ones, which one CTA would walk over while the
 // others are done: token tiles with more row tiles than `piece` are cut.  `piece` is a window's row tiles, or less
 // where there are too few CTAs for the machine.
 //
-// CTA organisation of both kinds (one CTA an SM): 4P compute warps (warp w: TMEM lanes 32 (w % 4) .., columns
-// 128 / P (w / 4) .. of the score tiles; its bf16 values go back into the first half of its own columns), one warp
-// for TMEM and the products, one for the copies.  Waits are bounded; on expiry MOA_ERR_DEVICE_TIMEOUT is recorded and
+// CTA organisation of both kinds: 8 compute warps (warp w: TMEM lanes 32 (w % 4) .., columns N / 2 (w / 4) .. of the score
+// tiles; its bf16 values go back into the first half of its own columns), one warp for TMEM and the products, one for the
+// copies.  Waits are bounded; on expiry MOA_ERR_DEVICE_TIMEOUT is recorded and
 // every role leaves its loop.
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -50,42 +54,32 @@ namespace {
 using namespace ptx;
 using namespace tc;
 
-constexpr int kBlk = 128;
-constexpr int kTmemCols = 512;
+constexpr int kBlk = 128;                // tokens of dK's and dV's tiles, rows of dQ's
+constexpr int kHalf = 64;                // rows of half a row tile
 constexpr int kPanelBytes = 128 * 128;   // 64 bf16 columns of 128 rows, 128-byte swizzle
-constexpr int kVecBytes = kBlk * 4;
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct Params {
   View q, k, v, o, go, dq, dk, dv;
   const float* lse;
-  float* nl;      // [row tile][128] -LSE log2 e; -infinity for rows that are not there or see nothing
+  float* nl;      // [half][64] -LSE log2 e; -infinity for rows that are not there or see nothing
   float* delta;   // alike: D
   float* part;    // [cut tile][piece][128][DK + DV]
   int B, Hk, G, N, Nk;
-  int GC, chunks, PT;   // heads of a row tile, chunks of heads, positions of a row tile
-  int n_pt;             // row tiles along the positions
+  int GC, chunks, PT;   // heads of a half, chunks of heads, positions of a half
+  int n_ht;             // halves along the positions, an even number
   int n_kt;             // token tiles
-  int cut, pieces, piece;   // the first `cut` token tiles come in up to `pieces` pieces of `piece` row tiles
+  int cut, pieces, piece;   // the first `cut` token tiles come in up to `pieces` pieces of `piece` row tiles (of N rows)
   int group;            // key heads whose token tiles are handed out in turn, longest first
   win::Mask mask;
   float c_log2, scale;
   uint64_t wait_limit_ns;
 };
 
-// P column parts of the score tiles, 4P compute warps, then the warps of the products and of the copies.  P = 4
-// where the tile products are short (d_k + d_v = 128) and the exponentials dominate.
-template <int P>
-struct Warps {
-  static constexpr int kParts = P;
-  static constexpr int kCols = kBlk / P;
-  static constexpr int kComputeWarps = 4 * P;
-  static constexpr int kComputeThreads = 32 * kComputeWarps;
-  static constexpr int kThreads = kComputeThreads + 64;
-  static constexpr int kMmaWarp = kComputeWarps;
-  static constexpr int kLoadWarp = kComputeWarps + 1;
-};
-__host__ __device__ constexpr int parts_of(int dk, int dv) { return dk + dv <= 128 ? 4 : 2; }
+constexpr int kParts = 2, kComputeThreads = 256, kThreads = 320, kMmaWarp = 8, kLoadWarp = 9;
+// Columns of the score tiles, CTAs of an SM, the ring's stages.
+__host__ __device__ constexpr int width_of(int dk, int dv) { return dk + dv <= 128 ? 64 : 128; }
+__host__ __device__ constexpr int ctas_of(int dk, int dv) { return dk + dv <= 128 ? 2 : 1; }
 __host__ __device__ constexpr int ring_stages(int dk, int dv) { return dk + dv <= 128 ? 4 : (dk + dv <= 192 ? 3 : 2); }
 
 // TMEM column of step kk (16 rows of the reduction axis) of a bf16 operand that the column parts wrote.
@@ -149,24 +143,37 @@ __device__ __forceinline__ __nv_bfloat16* row_of(const View& x, int b, int h, in
   return static_cast<__nv_bfloat16*>(x.p) + b * x.sb + h * x.sh + n * x.sn;
 }
 
-// Row tile t: its key head, chunk of heads and first position.
+// Pair of halves t: its key head, chunk of heads and first position.
 struct RowTile {
   int b, h, chunk, i0;
 };
 __device__ __forceinline__ RowTile row_tile(const Params& p, int64_t t) {
   RowTile r;
-  const int64_t per = int64_t(p.chunks) * p.n_pt, bh = t / per;
+  const int64_t per = int64_t(p.chunks) * (p.n_ht / 2), bh = t / per;
   const int rest = int(t - bh * per);
-  r.chunk = rest / p.n_pt;
-  r.i0 = (rest - r.chunk * p.n_pt) * p.PT;
+  r.chunk = rest / (p.n_ht / 2);
+  r.i0 = (rest - r.chunk * (p.n_ht / 2)) * 2 * p.PT;
   r.b = int(bh / p.Hk), r.h = int(bh - int64_t(r.b) * p.Hk);
   return r;
+}
+// Row r of a pair of halves: its head of the group and position, and whether it is there.
+struct RowAt {
+  int g, i;
+  bool real;
+};
+__device__ __forceinline__ RowAt row_at(const Params& p, const RowTile& t, int r) {
+  const int in_half = r % kHalf, pos = int(unsigned(in_half) / unsigned(p.GC));
+  RowAt a;
+  a.g = t.chunk * p.GC + (in_half - pos * p.GC);
+  a.i = t.i0 + r / kHalf * p.PT + pos;
+  a.real = pos < p.PT && a.g < p.G && a.i < p.N;
+  return a;
 }
 
 // ------------------------------------------------------------------------------------------------
 // D and -LSE log2 e: DV / 8 lanes a row
 // ------------------------------------------------------------------------------------------------
-// A CTA for one row tile; its rows' loads are all on their way together.  Bound by memory: O and dO once.
+// A CTA for two halves; its rows' loads are all on their way together.  Bound by memory: O and dO once.
 template <int DV>
 __global__ void __launch_bounds__(256)
 window_delta_tc_kernel(const Params p) {
@@ -179,9 +186,9 @@ window_delta_tc_kernel(const Params p) {
   bool real[kIts];
 #pragma unroll
   for (int k = 0; k < kIts; ++k) {
-    const int r = first + k * kStep, pos = int(unsigned(r) / unsigned(p.GC));
-    const int g = t.chunk * p.GC + (r - pos * p.GC), i = t.i0 + pos, hq = t.h * p.G + g;
-    real[k] = pos < p.PT && g < p.G && i < p.N;
+    const RowAt at = row_at(p, t, first + k * kStep);
+    const int hq = t.h * p.G + at.g, i = at.i;
+    real[k] = at.real;
     ov[k] = gv[k] = make_uint4(0, 0, 0, 0);
     lse[k] = -INFINITY;
     if (real[k]) {
@@ -214,11 +221,11 @@ window_delta_tc_kernel(const Params p) {
 // ------------------------------------------------------------------------------------------------
 // dK and dV
 // ------------------------------------------------------------------------------------------------
-// The row tiles along the positions that see a token of tile kt: [first, first + n).
+// The row tiles (of `positions` positions) that see a token of tile kt: [first, first + n) along the positions.
 struct Range {
   int first, n;
 };
-__host__ __device__ __forceinline__ Range rows_of_tokens(const win::Mask& m, int kt, int N, int Nk, int PT) {
+__host__ __device__ __forceinline__ Range rows_of_tokens(const win::Mask& m, int kt, int N, int Nk, int positions) {
   const int off = Nk - N, k0 = kt * kBlk, k1 = k0 + kBlk < Nk ? k0 + kBlk : Nk;
   const int64_t i0 = k0 > off ? int64_t(k0) - off : 0;
   int64_t i1 = N;
@@ -227,17 +234,19 @@ __host__ __device__ __forceinline__ Range rows_of_tokens(const win::Mask& m, int
     i1 = n < 0 ? 0 : n < i1 ? n : i1;
   }
   Range r;
-  r.first = int(i0 / PT);
-  r.n = i1 > i0 ? int((i1 + PT - 1) / PT) - r.first : 0;
+  r.first = int(i0 / positions);
+  r.n = i1 > i0 ? int((i1 + positions - 1) / positions) - r.first : 0;
   return r;
 }
 
 template <int DK, int DV>
-struct KvCfg : Warps<parts_of(DK, DV)> {
+struct KvCfg {
+  static constexpr int kN = width_of(DK, DV), kCols = kN / kParts, kHalves = kN / kHalf;
   static constexpr int kKBytes = kBlk * DK * 2, kVBytes = kBlk * DV * 2;
-  static constexpr int kQBytes = kBlk * DK * 2, kGBytes = kBlk * DV * 2;
-  // stage: Q tile, dO tile, -L and D of its 128 rows
-  static constexpr int kStageBytes = kQBytes + kGBytes + 2 * kVecBytes;
+  static constexpr int kRowPanel = kN * 128;   // 64 columns of a row tile
+  static constexpr int kQBytes = kN * DK * 2, kGBytes = kN * DV * 2, kVecBytes = kN * 4;
+  // stage: Q tile, dO tile, -L and D of its rows
+  static constexpr int kStageBytes = (kQBytes + kGBytes + 2 * kVecBytes + 1023) / 1024 * 1024;
   static constexpr int kStages = ring_stages(DK, DV);
   static constexpr int kOffK = 0, kOffV = kKBytes, kOffStage = kKBytes + kVBytes;
   // barriers: full[NS], empty[NS], kv_full, s_full, dp_full, p_ready, ds_ready, acc_done
@@ -245,10 +254,10 @@ struct KvCfg : Warps<parts_of(DK, DV)> {
   static constexpr int kOffBar = kOffStage + kStages * kStageBytes;
   static constexpr int kOffMisc = kOffBar + kNumBars * 8;
   static constexpr int kSmemBytes = kOffMisc + 16 + 1024;
-  static constexpr uint32_t kTmemS = 0, kTmemDP = 128, kTmemDV = 256, kTmemDK = 256 + DV;
-  static_assert(kStageBytes % 1024 == 0, "stage alignment");
+  static constexpr uint32_t kTmemS = 0, kTmemDP = kN, kTmemDV = 2 * kN, kTmemDK = 2 * kN + DV;
+  static constexpr uint32_t kTmemCols = 512 / ctas_of(DK, DV);
   static_assert(kTmemDK + DK <= kTmemCols, "TMEM budget");
-  static_assert(kSmemBytes <= 232448, "shared memory budget");
+  static_assert((kSmemBytes + 1024) * ctas_of(DK, DV) <= 233472, "shared memory budget");
 };
 
 // A CTA's work: token tile kt of a key head, row tiles [t0, t0 + n) of the list (chunk after chunk).
@@ -292,7 +301,7 @@ __device__ __forceinline__ void dkdv_tile(const CUtensorMap& tmQ, const CUtensor
 
   const KvItem it = kv_item(p, index);
   const int k0 = it.kt * kBlk;
-  const Range range = rows_of_tokens(p.mask, it.kt, p.N, p.Nk, p.PT);
+  const Range range = rows_of_tokens(p.mask, it.kt, p.N, p.Nk, C::kHalves * p.PT);
   const int all = range.n * p.chunks;
   const int t0 = it.whole ? 0 : it.piece * p.piece;
   const int n_t = it.whole ? all : all - t0 < p.piece ? all - t0 : p.piece;
@@ -307,18 +316,18 @@ __device__ __forceinline__ void dkdv_tile(const CUtensorMap& tmQ, const CUtensor
     mbar_init(kv_full, 1);
     mbar_init(s_full, 1);
     mbar_init(dp_full, 1);
-    mbar_init(p_ready, C::kComputeThreads);
-    mbar_init(ds_ready, C::kComputeThreads);
+    mbar_init(p_ready, kComputeThreads);
+    mbar_init(ds_ready, kComputeThreads);
     mbar_init(acc_done, 1);
     *abort_flag = 0;
     fence_barrier_init();
   }
-  if (warp == C::kMmaWarp) {
-    tmem_alloc(smem_u32(tmem_slot), kTmemCols);
+  if (warp == kMmaWarp) {
+    tmem_alloc(smem_u32(tmem_slot), C::kTmemCols);
     tmem_relinquish();
   }
-  if (p.GC * p.PT < kBlk) {   // rows of a tile that no copy fills
-    for (int x = threadIdx.x; x < C::kStages * C::kStageBytes / 16; x += C::kThreads)
+  if (p.GC * p.PT < kHalf) {   // rows of a half that no copy fills
+    for (int x = threadIdx.x; x < C::kStages * C::kStageBytes / 16; x += kThreads)
       reinterpret_cast<uint4*>(smem + C::kOffStage)[x] = make_uint4(0, 0, 0, 0);
     fence_proxy_async_smem();
   }
@@ -328,7 +337,7 @@ __device__ __forceinline__ void dkdv_tile(const CUtensorMap& tmQ, const CUtensor
   tc_fence_after_sync();
   const uint32_t tmem = *tmem_slot;
 
-  if (warp == C::kLoadWarp) {
+  if (warp == kLoadWarp) {
     // ---------------------------------------------------------------- TMA producer
     if (lane == 0 && n_t > 0) {
       tma_prefetch_desc(&tmQ);
@@ -337,14 +346,19 @@ __device__ __forceinline__ void dkdv_tile(const CUtensorMap& tmQ, const CUtensor
       tma_prefetch_desc(&tmG);
       mbar_arrive_expect_tx(kv_full, C::kKBytes + C::kVBytes);
 #pragma unroll
-      for (int q = 0; q < DK / 64; ++q) tma_load_4d(sK + q * kPanelBytes, &tmK, kv_full, q * 64, k0, it.h, it.b);
+      for (int f = 0; f < kBlk / C::kN; ++f) {
 #pragma unroll
-      for (int q = 0; q < DV / 64; ++q) tma_load_4d(sV + q * kPanelBytes, &tmV, kv_full, q * 64, k0, it.h, it.b);
+        for (int q = 0; q < DK / 64; ++q)
+          tma_load_4d(sK + q * kPanelBytes + f * C::kRowPanel, &tmK, kv_full, q * 64, k0 + f * C::kN, it.h, it.b);
+#pragma unroll
+        for (int q = 0; q < DV / 64; ++q)
+          tma_load_4d(sV + q * kPanelBytes + f * C::kRowPanel, &tmV, kv_full, q * 64, k0 + f * C::kN, it.h, it.b);
+      }
       int slot = 0;
       uint32_t phase = 0, issued = 0, issued_phase = 0;
       bool aborted = false;
       int chunk = t0 / range.n, pt = range.first + (t0 - chunk * range.n);
-      const uint32_t bytes = (DK + DV) * 2 * p.GC * p.PT + 2 * kVecBytes;
+      const uint32_t bytes = C::kHalves * (DK + DV) * 2 * p.GC * p.PT + 2 * C::kVecBytes;
       for (int i = 0; i < n_t; ++i) {
         if (!wait_bounded(empty_bar(slot), phase ^ 1u, wc)) {
           aborted = true;
@@ -355,14 +369,19 @@ __device__ __forceinline__ void dkdv_tile(const CUtensorMap& tmQ, const CUtensor
         const uint32_t st = sStage + slot * C::kStageBytes;
         mbar_arrive_expect_tx(full_bar(slot), bytes);
 #pragma unroll
-        for (int q = 0; q < DK / 64; ++q)
-          tma_load_5d(st + q * kPanelBytes, &tmQ, full_bar(slot), q * 64, chunk * p.GC, pt * p.PT, it.h, it.b);
+        for (int f = 0; f < C::kHalves; ++f) {
+          const int i0 = (pt * C::kHalves + f) * p.PT;
 #pragma unroll
-        for (int q = 0; q < DV / 64; ++q)
-          tma_load_5d(st + C::kQBytes + q * kPanelBytes, &tmG, full_bar(slot), q * 64, chunk * p.GC, pt * p.PT, it.h, it.b);
-        const int64_t vrow = ((bh * p.chunks + chunk) * p.n_pt + pt) * kBlk;
-        bulk_load(st + C::kQBytes + C::kGBytes, p.nl + vrow, kVecBytes, full_bar(slot));
-        bulk_load(st + C::kQBytes + C::kGBytes + kVecBytes, p.delta + vrow, kVecBytes, full_bar(slot));
+          for (int q = 0; q < DK / 64; ++q)
+            tma_load_5d(st + q * C::kRowPanel + f * kHalf * 128, &tmQ, full_bar(slot), q * 64, chunk * p.GC, i0, it.h, it.b);
+#pragma unroll
+          for (int q = 0; q < DV / 64; ++q)
+            tma_load_5d(st + C::kQBytes + q * C::kRowPanel + f * kHalf * 128, &tmG, full_bar(slot), q * 64, chunk * p.GC, i0,
+                        it.h, it.b);
+        }
+        const int64_t vrow = ((bh * p.chunks + chunk) * p.n_ht + pt * C::kHalves) * kHalf;
+        bulk_load(st + C::kQBytes + C::kGBytes, p.nl + vrow, C::kVecBytes, full_bar(slot));
+        bulk_load(st + C::kQBytes + C::kGBytes + C::kVecBytes, p.delta + vrow, C::kVecBytes, full_bar(slot));
         if (++pt == range.first + range.n) {
           pt = range.first;
           ++chunk;
@@ -378,22 +397,22 @@ __device__ __forceinline__ void dkdv_tile(const CUtensorMap& tmQ, const CUtensor
           if (issued & (1u << sl)) wait_quiesce(full_bar(sl), (issued_phase >> sl) & 1u, p.wait_limit_ns, &g_moa_window_bwd_status);
       }
     }
-  } else if (warp == C::kMmaWarp) {
+  } else if (warp == kMmaWarp) {
     // ---------------------------------------------------------------- MMA issuer
     if (lane == 0) {
-      constexpr uint32_t kIdescS = make_idesc(kBlk, kBlk, false);
+      constexpr uint32_t kIdescS = make_idesc(kBlk, C::kN, false);
       constexpr uint32_t kIdescDV = make_idesc(kBlk, DV, true);
       constexpr uint32_t kIdescDK = make_idesc(kBlk, DK, true);
       const uint32_t tS = tmem + C::kTmemS, tDP = tmem + C::kTmemDP;
       const uint32_t tDV = tmem + C::kTmemDV, tDK = tmem + C::kTmemDK;
       int slot = 0;
       uint32_t phase = 0;
-      // S^T = K Q^T: M = 128 tokens, N = 128 rows, both operands K-major
+      // S^T = K Q^T: M = 128 tokens, N rows, both operands K-major
       auto issue_s = [&](uint32_t sQ) {
 #pragma unroll
         for (int kk = 0; kk < DK / 16; ++kk) {
-          const uint32_t off = (kk >> 2) * kPanelBytes + (kk & 3) * 32;
-          mma_f16_ss(tS, make_sdesc_sw128(sK + off, 16, 1024), make_sdesc_sw128(sQ + off, 16, 1024), kIdescS, kk > 0 ? 1u : 0u);
+          const uint32_t k = (kk >> 2) * kPanelBytes + (kk & 3) * 32, r = (kk >> 2) * C::kRowPanel + (kk & 3) * 32;
+          mma_f16_ss(tS, make_sdesc_sw128(sK + k, 16, 1024), make_sdesc_sw128(sQ + r, 16, 1024), kIdescS, kk > 0 ? 1u : 0u);
         }
         mma_commit(s_full);
       };
@@ -401,8 +420,8 @@ __device__ __forceinline__ void dkdv_tile(const CUtensorMap& tmQ, const CUtensor
       auto issue_dp = [&](uint32_t sG) {
 #pragma unroll
         for (int kk = 0; kk < DV / 16; ++kk) {
-          const uint32_t off = (kk >> 2) * kPanelBytes + (kk & 3) * 32;
-          mma_f16_ss(tDP, make_sdesc_sw128(sV + off, 16, 1024), make_sdesc_sw128(sG + off, 16, 1024), kIdescS, kk > 0 ? 1u : 0u);
+          const uint32_t k = (kk >> 2) * kPanelBytes + (kk & 3) * 32, r = (kk >> 2) * C::kRowPanel + (kk & 3) * 32;
+          mma_f16_ss(tDP, make_sdesc_sw128(sV + k, 16, 1024), make_sdesc_sw128(sG + r, 16, 1024), kIdescS, kk > 0 ? 1u : 0u);
         }
         mma_commit(dp_full);
       };
@@ -429,8 +448,8 @@ __device__ __forceinline__ void dkdv_tile(const CUtensorMap& tmQ, const CUtensor
         if (!ok) break;
         tc_fence_after_sync();
 #pragma unroll
-        for (int kk = 0; kk < kBlk / 16; ++kk)
-          mma_f16_ts(tDV, tS + part_col<kCols>(kk), make_sdesc_sw128(sG + kk * 2048, kPanelBytes, 1024), kIdescDV,
+        for (int kk = 0; kk < C::kN / 16; ++kk)
+          mma_f16_ts(tDV, tS + part_col<kCols>(kk), make_sdesc_sw128(sG + kk * 2048, C::kRowPanel, 1024), kIdescDV,
                      (kk > 0 || i > 0) ? 1u : 0u);
         const bool more = i + 1 < n_t;
         if (more) {
@@ -444,8 +463,8 @@ __device__ __forceinline__ void dkdv_tile(const CUtensorMap& tmQ, const CUtensor
         if (!ok) break;
         tc_fence_after_sync();
 #pragma unroll
-        for (int kk = 0; kk < kBlk / 16; ++kk)
-          mma_f16_ts(tDK, tDP + part_col<kCols>(kk), make_sdesc_sw128(sQ + kk * 2048, kPanelBytes, 1024), kIdescDK,
+        for (int kk = 0; kk < C::kN / 16; ++kk)
+          mma_f16_ts(tDK, tDP + part_col<kCols>(kk), make_sdesc_sw128(sQ + kk * 2048, C::kRowPanel, 1024), kIdescDK,
                      (kk > 0 || i > 0) ? 1u : 0u);
         mma_commit(empty_bar(st));
         if (more) issue_dp(stage(slot) + C::kQBytes);
@@ -480,17 +499,17 @@ __device__ __forceinline__ void dkdv_tile(const CUtensorMap& tmQ, const CUtensor
       if (!ok) break;
       tc_fence_after_sync();
       const uint32_t nl4 = sStage + st * C::kStageBytes + C::kQBytes + C::kGBytes + part * kCols * 4;
-      const uint32_t d4 = nl4 + kBlk * 4;
-      // the rows that see the token: columns [from, upto) of this part
-      const int p0 = pt * p.PT + (p.Nk - p.N);
+      const uint32_t d4 = nl4 + C::kVecBytes;
+      // the rows that see the token: columns [from, upto) of this part, which lies in one half
+      const int p0 = pt * C::kHalves * p.PT + part * kCols / kHalf * p.PT + (p.Nk - p.N);
       if (++pt == range.first + range.n) pt = range.first;
-      const int ahead = key - p0;   // positions of the tile before the token's own
-      int from = ahead <= 0 ? 0 : ahead >= p.PT ? kBlk : ahead * p.GC, upto = kBlk;
+      const int ahead = key - p0;   // positions of the half before the token's own
+      int from = ahead <= 0 ? 0 : ahead >= p.PT ? kHalf : ahead * p.GC, upto = kHalf;
       if (bounded) {
         const int64_t left = int64_t(ahead) + p.mask.window;
-        upto = left <= 0 ? 0 : left >= p.PT ? kBlk : int(left) * p.GC;
+        upto = left <= 0 ? 0 : left >= p.PT ? kHalf : int(left) * p.GC;
       }
-      from -= part * kCols, upto -= part * kCols;
+      from -= part * kCols % kHalf, upto -= part * kCols % kHalf;
       const bool full = __all_sync(0xffffffffu, from <= 0 && upto >= kCols);
       uint32_t r[kCols];
       tmem_load_part<kCols>(tS, r);
@@ -539,34 +558,29 @@ __device__ __forceinline__ void dkdv_tile(const CUtensorMap& tmQ, const CUtensor
       tc_fence_before_sync();
       mbar_arrive(ds_ready);
     }
-    // The first half of the parts write dV, the others scale dK, each a slice of the columns.
+    // The first part writes dV, the second scale dK.
     const bool valid = key < p.Nk;
-    constexpr int kHalf = C::kParts / 2, wv = DV / kHalf, wk = DK / kHalf;
     if (n_t <= 0) {   // tokens that no row sees
       if (valid) {
-        uint4* dst = reinterpret_cast<uint4*>(part < kHalf ? row_of(p.dv, it.b, it.h, key) + part * wv
-                                                           : row_of(p.dk, it.b, it.h, key) + (part - kHalf) * wk);
-        for (int e = 0; e < (part < kHalf ? wv : wk) / 8; ++e) dst[e] = make_uint4(0, 0, 0, 0);
+        uint4* dst = reinterpret_cast<uint4*>(row_of(part == 0 ? p.dv : p.dk, it.b, it.h, key));
+        for (int e = 0; e < (part == 0 ? DV : DK) / 8; ++e) dst[e] = make_uint4(0, 0, 0, 0);
       }
     } else if (ok && wait_warp(acc_done, 0)) {
       tc_fence_after_sync();
       float* piece = it.whole ? nullptr : p.part + (((bh * p.cut + it.kt) * p.pieces + it.piece) * kBlk + row) * (DK + DV);
-      if (part < kHalf)
-        store_row<wv>(tmem + lanes + C::kTmemDV + part * wv, 1.f, row_of(p.dv, it.b, it.h, valid ? key : 0) + part * wv,
-                      piece ? piece + DK + part * wv : nullptr, valid);
+      if (part == 0)
+        store_row<DV>(tmem + lanes + C::kTmemDV, 1.f, row_of(p.dv, it.b, it.h, valid ? key : 0), piece ? piece + DK : nullptr, valid);
       else
-        store_row<wk>(tmem + lanes + C::kTmemDK + (part - kHalf) * wk, p.scale,
-                      row_of(p.dk, it.b, it.h, valid ? key : 0) + (part - kHalf) * wk,
-                      piece ? piece + (part - kHalf) * wk : nullptr, valid);
+        store_row<DK>(tmem + lanes + C::kTmemDK, p.scale, row_of(p.dk, it.b, it.h, valid ? key : 0), piece, valid);
     }
   }
 
-  if (warp == C::kMmaWarp && lane == 0) wait_quiesce(acc_done, 0, p.wait_limit_ns, &g_moa_window_bwd_status);
+  if (warp == kMmaWarp && lane == 0) wait_quiesce(acc_done, 0, p.wait_limit_ns, &g_moa_window_bwd_status);
   tc_fence_before_sync();
   __syncthreads();
-  if (warp == C::kMmaWarp) {
+  if (warp == kMmaWarp) {
     tc_fence_after_sync();
-    tmem_dealloc(tmem, kTmemCols);
+    tmem_dealloc(tmem, C::kTmemCols);
   }
 }
 
@@ -584,7 +598,7 @@ window_dkdv_tc_join_kernel(const Params p, int64_t n) {
   const int j = int(row - tile * kBlk), kt = int(tile - bh * p.cut);
   const int b = int(bh / p.Hk), h = int(bh - int64_t(b) * p.Hk), key = kt * kBlk + j;
   if (key >= p.Nk) return;
-  const int all = rows_of_tokens(p.mask, kt, p.N, p.Nk, p.PT).n * p.chunks;
+  const int all = rows_of_tokens(p.mask, kt, p.N, p.Nk, width_of(DK, DV) / kHalf * p.PT).n * p.chunks;
   const int pieces = (all + p.piece - 1) / p.piece;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
@@ -601,9 +615,11 @@ window_dkdv_tc_join_kernel(const Params p, int64_t n) {
 // dQ
 // ------------------------------------------------------------------------------------------------
 template <int DK, int DV>
-struct QCfg : Warps<parts_of(DK, DV)> {
+struct QCfg {
+  static constexpr int kN = width_of(DK, DV), kCols = kN / kParts;
   static constexpr int kQBytes = kBlk * DK * 2, kGBytes = kBlk * DV * 2;
-  static constexpr int kKBytes = kBlk * DK * 2, kVBytes = kBlk * DV * 2;
+  static constexpr int kTokenPanel = kN * 128;
+  static constexpr int kKBytes = kN * DK * 2, kVBytes = kN * DV * 2;
   static constexpr int kStageBytes = kKBytes + kVBytes;
   static constexpr int kStages = ring_stages(DK, DV);
   static constexpr int kOffQ = 0, kOffG = kQBytes, kOffStage = kQBytes + kGBytes;
@@ -612,9 +628,10 @@ struct QCfg : Warps<parts_of(DK, DV)> {
   static constexpr int kOffBar = kOffStage + kStages * kStageBytes;
   static constexpr int kOffMisc = kOffBar + kNumBars * 8;
   static constexpr int kSmemBytes = kOffMisc + 16 + 1024;
-  static constexpr uint32_t kTmemS = 0, kTmemDP = 128, kTmemDQ = 256;
+  static constexpr uint32_t kTmemS = 0, kTmemDP = kN, kTmemDQ = 2 * kN;
+  static constexpr uint32_t kTmemCols = 512 / ctas_of(DK, DV);
   static_assert(kTmemDQ + DK <= kTmemCols, "TMEM budget");
-  static_assert(kSmemBytes <= 232448, "shared memory budget");
+  static_assert((kSmemBytes + 1024) * ctas_of(DK, DV) <= 233472, "shared memory budget");
 };
 
 template <int DK, int DV>
@@ -637,11 +654,12 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
   const WaitCtl wc{abort_flag, p.wait_limit_ns, 0u, &g_moa_window_bwd_status};
 
   // the last positions, which see the most without a window, come first
-  const int64_t per = int64_t(p.chunks) * p.n_pt, group = index / per;
+  const int64_t per = int64_t(p.chunks) * (p.n_ht / 2), group = index / per;
   const int64_t tile_id = group * per + (per - 1 - (index - group * per));
   const RowTile t = row_tile(p, tile_id);
-  const int i1 = t.i0 + p.PT - 1 < p.N ? t.i0 + p.PT - 1 : p.N - 1;
-  const win::Tiles list = win::tiles_of(p.mask, p.Nk, p.N, t.i0, i1, kBlk);
+  // (a pair's positions may all lie past the end)
+  const int i1 = t.i0 + 2 * p.PT - 1 < p.N ? t.i0 + 2 * p.PT - 1 : p.N - 1;
+  const win::Tiles list = win::tiles_of(p.mask, p.Nk, p.N, t.i0, i1, C::kN);
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::kStages; ++s) {
@@ -651,18 +669,18 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
     mbar_init(q_full, 1);
     mbar_init(s_full, 1);
     mbar_init(dp_full, 1);
-    mbar_init(ds_ready, C::kComputeThreads);
+    mbar_init(ds_ready, kComputeThreads);
     mbar_init(acc_done, 1);
-    mbar_init(s_free, C::kComputeThreads);
+    mbar_init(s_free, kComputeThreads);
     *abort_flag = 0;
     fence_barrier_init();
   }
-  if (warp == C::kMmaWarp) {
-    tmem_alloc(smem_u32(tmem_slot), kTmemCols);
+  if (warp == kMmaWarp) {
+    tmem_alloc(smem_u32(tmem_slot), C::kTmemCols);
     tmem_relinquish();
   }
-  if (p.GC * p.PT < kBlk) {   // rows that no copy fills
-    for (int x = threadIdx.x; x < (C::kQBytes + C::kGBytes) / 16; x += C::kThreads)
+  if (p.GC * p.PT < kHalf) {   // rows that no copy fills
+    for (int x = threadIdx.x; x < (C::kQBytes + C::kGBytes) / 16; x += kThreads)
       reinterpret_cast<uint4*>(smem)[x] = make_uint4(0, 0, 0, 0);
     fence_proxy_async_smem();
   }
@@ -672,18 +690,23 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
   tc_fence_after_sync();
   const uint32_t tmem = *tmem_slot;
 
-  if (warp == C::kLoadWarp) {
+  if (warp == kLoadWarp) {
     // ---------------------------------------------------------------- TMA producer
     if (lane == 0 && list.n > 0) {
       tma_prefetch_desc(&tmQ);
       tma_prefetch_desc(&tmK);
       tma_prefetch_desc(&tmV);
       tma_prefetch_desc(&tmG);
-      mbar_arrive_expect_tx(q_full, (DK + DV) * 2 * p.GC * p.PT);
+      mbar_arrive_expect_tx(q_full, 2 * (DK + DV) * 2 * p.GC * p.PT);
 #pragma unroll
-      for (int q = 0; q < DK / 64; ++q) tma_load_5d(sQ + q * kPanelBytes, &tmQ, q_full, q * 64, t.chunk * p.GC, t.i0, t.h, t.b);
+      for (int f = 0; f < 2; ++f) {
 #pragma unroll
-      for (int q = 0; q < DV / 64; ++q) tma_load_5d(sG + q * kPanelBytes, &tmG, q_full, q * 64, t.chunk * p.GC, t.i0, t.h, t.b);
+        for (int q = 0; q < DK / 64; ++q)
+          tma_load_5d(sQ + q * kPanelBytes + f * kHalf * 128, &tmQ, q_full, q * 64, t.chunk * p.GC, t.i0 + f * p.PT, t.h, t.b);
+#pragma unroll
+        for (int q = 0; q < DV / 64; ++q)
+          tma_load_5d(sG + q * kPanelBytes + f * kHalf * 128, &tmG, q_full, q * 64, t.chunk * p.GC, t.i0 + f * p.PT, t.h, t.b);
+      }
       int slot = 0;
       uint32_t phase = 0, issued = 0, issued_phase = 0;
       bool aborted = false;
@@ -696,12 +719,12 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
         issued_phase = (issued_phase & ~(1u << slot)) | (phase << slot);
         const uint32_t st = sStage + slot * C::kStageBytes;
         mbar_arrive_expect_tx(full_bar(slot), C::kStageBytes);
-        const int n0 = list.at(j) * kBlk;
+        const int n0 = list.at(j) * C::kN;
 #pragma unroll
-        for (int q = 0; q < DK / 64; ++q) tma_load_4d(st + q * kPanelBytes, &tmK, full_bar(slot), q * 64, n0, t.h, t.b);
+        for (int q = 0; q < DK / 64; ++q) tma_load_4d(st + q * C::kTokenPanel, &tmK, full_bar(slot), q * 64, n0, t.h, t.b);
 #pragma unroll
         for (int q = 0; q < DV / 64; ++q)
-          tma_load_4d(st + C::kKBytes + q * kPanelBytes, &tmV, full_bar(slot), q * 64, n0, t.h, t.b);
+          tma_load_4d(st + C::kKBytes + q * C::kTokenPanel, &tmV, full_bar(slot), q * 64, n0, t.h, t.b);
         if (++slot == C::kStages) {
           slot = 0;
           phase ^= 1u;
@@ -713,10 +736,10 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
           if (issued & (1u << sl)) wait_quiesce(full_bar(sl), (issued_phase >> sl) & 1u, p.wait_limit_ns, &g_moa_window_bwd_status);
       }
     }
-  } else if (warp == C::kMmaWarp) {
+  } else if (warp == kMmaWarp) {
     // ---------------------------------------------------------------- MMA issuer
     if (lane == 0) {
-      constexpr uint32_t kIdescS = make_idesc(kBlk, kBlk, false);
+      constexpr uint32_t kIdescS = make_idesc(kBlk, C::kN, false);
       constexpr uint32_t kIdescDQ = make_idesc(kBlk, DK, true);
       const uint32_t tS = tmem + C::kTmemS, tDP = tmem + C::kTmemDP, tDQ = tmem + C::kTmemDQ;
       int slot = 0;
@@ -725,16 +748,16 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
       auto issue_s = [&](uint32_t sK) {   // S = Q K^T
 #pragma unroll
         for (int kk = 0; kk < DK / 16; ++kk) {
-          const uint32_t off = (kk >> 2) * kPanelBytes + (kk & 3) * 32;
-          mma_f16_ss(tS, make_sdesc_sw128(sQ + off, 16, 1024), make_sdesc_sw128(sK + off, 16, 1024), kIdescS, kk > 0 ? 1u : 0u);
+          const uint32_t r = (kk >> 2) * kPanelBytes + (kk & 3) * 32, k = (kk >> 2) * C::kTokenPanel + (kk & 3) * 32;
+          mma_f16_ss(tS, make_sdesc_sw128(sQ + r, 16, 1024), make_sdesc_sw128(sK + k, 16, 1024), kIdescS, kk > 0 ? 1u : 0u);
         }
         mma_commit(s_full);
       };
       auto issue_dp = [&](uint32_t sV) {   // dP = dO V^T
 #pragma unroll
         for (int kk = 0; kk < DV / 16; ++kk) {
-          const uint32_t off = (kk >> 2) * kPanelBytes + (kk & 3) * 32;
-          mma_f16_ss(tDP, make_sdesc_sw128(sG + off, 16, 1024), make_sdesc_sw128(sV + off, 16, 1024), kIdescS, kk > 0 ? 1u : 0u);
+          const uint32_t r = (kk >> 2) * kPanelBytes + (kk & 3) * 32, k = (kk >> 2) * C::kTokenPanel + (kk & 3) * 32;
+          mma_f16_ss(tDP, make_sdesc_sw128(sG + r, 16, 1024), make_sdesc_sw128(sV + k, 16, 1024), kIdescS, kk > 0 ? 1u : 0u);
         }
         mma_commit(dp_full);
       };
@@ -766,8 +789,8 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
         tc_fence_after_sync();
         const uint32_t sK = stage(st);
 #pragma unroll
-        for (int kk = 0; kk < kBlk / 16; ++kk)
-          mma_f16_ts(tDQ, tDP + part_col<kCols>(kk), make_sdesc_sw128(sK + kk * 2048, kPanelBytes, 1024), kIdescDQ,
+        for (int kk = 0; kk < C::kN / 16; ++kk)
+          mma_f16_ts(tDQ, tDP + part_col<kCols>(kk), make_sdesc_sw128(sK + kk * 2048, C::kTokenPanel, 1024), kIdescDQ,
                      (kk > 0 || j > 0) ? 1u : 0u);
         mma_commit(empty_bar(st));
         if (more) issue_dp(stage(slot) + C::kKBytes);
@@ -783,8 +806,9 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
     const uint32_t tDP = tmem + lanes + C::kTmemDP + part * kCols;
     const float nl = p.nl[tile_id * kBlk + row], dd = p.delta[tile_id * kBlk + row];
     const uint64_t cc = pack_f32x2(p.c_log2, p.c_log2), nn = pack_f32x2(nl, nl);
-    const int pos = row / p.GC, g = t.chunk * p.GC + row - pos * p.GC, i = t.i0 + pos;
-    const bool live = pos < p.PT && g < p.G && i < p.N;
+    const RowAt at = row_at(p, t, row);
+    const int g = at.g, i = at.i;
+    const bool live = at.real;
     // rows that are not there weigh nothing anyway (their nl)
     const int lim = live ? win::row_end(p.mask, p.Nk, p.N, i) : 0x7fffffff, low = live ? win::row_low(p.mask, p.Nk, p.N, i) : 0;
     bool ok = true;
@@ -798,7 +822,7 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
       tmem_load_part<kCols>(tS, r);
       tc_fence_before_sync();
       mbar_arrive(s_free);
-      const int n0 = list.at(j) * kBlk + part * kCols;
+      const int n0 = list.at(j) * C::kN + part * kCols;
       float w[kCols];
 #pragma unroll
       for (int k = 0; k < kCols; k += 2) ffma2(w[k], w[k + 1], __uint_as_float(r[k]), __uint_as_float(r[k + 1]), cc, nn);
@@ -826,8 +850,8 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
       mbar_arrive(ds_ready);
     }
     // part q writes columns [wq q, wq q + wq)
-    constexpr int wq = DK / C::kParts < 32 ? 32 : DK / C::kParts;
-    if (part * wq < DK) {
+    constexpr int wq = DK / kParts;
+    {
       __nv_bfloat16* dst = row_of(p.dq, t.b, t.h * p.G + (live ? g : 0), live ? i : 0) + part * wq;
       if (list.n == 0) {
         if (live)
@@ -839,18 +863,18 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
     }
   }
 
-  if (warp == C::kMmaWarp && lane == 0) wait_quiesce(acc_done, 0, p.wait_limit_ns, &g_moa_window_bwd_status);
+  if (warp == kMmaWarp && lane == 0) wait_quiesce(acc_done, 0, p.wait_limit_ns, &g_moa_window_bwd_status);
   tc_fence_before_sync();
   __syncthreads();
-  if (warp == C::kMmaWarp) {
+  if (warp == kMmaWarp) {
     tc_fence_after_sync();
-    tmem_dealloc(tmem, kTmemCols);
+    tmem_dealloc(tmem, C::kTmemCols);
   }
 }
 
 // CTAs below n_kv: dK and dV; the others: dQ, which are shorter and fill the SMs that run out of the former.
 template <int DK, int DV>
-__global__ void __launch_bounds__(KvCfg<DK, DV>::kThreads, 1)
+__global__ void __launch_bounds__(kThreads, ctas_of(DK, DV))
 window_bwd_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                      const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmG, const Params p,
                      unsigned n_kv) {
@@ -866,30 +890,32 @@ window_bwd_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
 constexpr int kSms = 152;   // the pieces aim at two CTAs for each SM; results do not go by the device's count
 
 struct Plan {
-  int64_t GC, chunks, PT, n_pt, n_kt, row_tiles;
+  int64_t GC, chunks, PT, n_ht, n_kt, pairs;   // pairs of halves
   int64_t cut, pieces, piece, items;
   explicit Plan(const WindowBwdArgs& a) {
     const int64_t G = a.Hq / a.Hk, bh = a.B * a.Hk;
-    GC = G < kBlk ? G : kBlk;
-    chunks = (G + GC - 1) / GC;
-    PT = kBlk / GC;
-    n_pt = (a.Nq + PT - 1) / PT;
+    chunks = (G + kHalf - 1) / kHalf;
+    GC = (G + chunks - 1) / chunks;
+    PT = kHalf / GC;
+    n_ht = (a.Nq + 2 * PT - 1) / (2 * PT) * 2;
     n_kt = (a.Nk + kBlk - 1) / kBlk;
-    row_tiles = bh * chunks * n_pt;
+    pairs = bh * chunks * (n_ht / 2);
     const win::Mask m{a.window, a.sinks, true};
+    // positions of the row tiles that dK's and dV's CTAs step by, and those tiles along the positions
+    const int64_t step = width_of(a.dk, a.dv) / kHalf * PT, n_pt = (a.Nq + step - 1) / step;
     // row tiles of a token tile: the most of any, and of one without sinks
-    const int64_t top = rows_of_tokens(m, 0, int(a.Nq), int(a.Nk), int(PT)).n * chunks;
+    const int64_t top = rows_of_tokens(m, 0, int(a.Nq), int(a.Nk), int(step)).n * chunks;
     const int64_t sink_tiles = a.window == win::kNoWindow ? 0 : (int64_t(a.sinks) + kBlk - 1) / kBlk;
     int64_t usual = top;
     if (a.window != win::kNoWindow) {
-      usual = (int64_t(a.window) + kBlk + 2 * PT - 1) / PT * chunks;
+      usual = (int64_t(a.window) + kBlk + 2 * step - 1) / step * chunks;
       if (usual > top) usual = top;
     }
     piece = usual;
     cut = sink_tiles;
     if (n_kt * bh < 2 * kSms) {   // too few token tiles for the machine: all are cut
       int64_t total = 0;
-      for (int64_t t = 0; t < n_kt; ++t) total += rows_of_tokens(m, int(t), int(a.Nq), int(a.Nk), int(PT)).n * chunks;
+      for (int64_t t = 0; t < n_kt; ++t) total += rows_of_tokens(m, int(t), int(a.Nq), int(a.Nk), int(step)).n * chunks;
       const int64_t want = (total * bh + 2 * kSms - 1) / (2 * kSms);
       if (want < usual) {
         piece = want;
@@ -907,12 +933,12 @@ struct Plan {
   }
 };
 
-// The workspace: -LSE log2 e and D of every row of every tile, then the pieces.
+// The workspace: -LSE log2 e and D of every row of every half, then the pieces.
 struct Work {
   int64_t nl, delta, part, bytes;
   Work(const WindowBwdArgs& a, const Plan& p) {
     nl = 0;
-    delta = p.row_tiles * kBlk * 4;
+    delta = p.pairs * kBlk * 4;
     part = 2 * delta;
     bytes = part + a.B * a.Hk * p.cut * p.pieces * kBlk * (a.dk + a.dv) * 4;
   }
@@ -926,7 +952,6 @@ int launch(const WindowBwdArgs& a, char* msg, size_t msglen) {
   using CK = KvCfg<DK, DV>;
   using CQ = QCfg<DK, DV>;
   auto kern = window_bwd_tc_kernel<DK, DV>;
-  static_assert(int(CK::kThreads) == int(CQ::kThreads), "one launch");
   constexpr int kSmem = CK::kSmemBytes > CQ::kSmemBytes ? CK::kSmemBytes : CQ::kSmemBytes;
   cudaError_t e = ensure_smem_limit(reinterpret_cast<const void*>(kern), kSmem);
   const Plan plan(a);
@@ -941,7 +966,7 @@ int launch(const WindowBwdArgs& a, char* msg, size_t msglen) {
   p.part = reinterpret_cast<float*>(ws + w.part);
   p.B = int(a.B), p.Hk = int(a.Hk), p.G = int(G), p.N = int(a.Nq), p.Nk = int(a.Nk);
   p.GC = int(plan.GC), p.chunks = int(plan.chunks), p.PT = int(plan.PT);
-  p.n_pt = int(plan.n_pt), p.n_kt = int(plan.n_kt);
+  p.n_ht = int(plan.n_ht), p.n_kt = int(plan.n_kt);
   p.cut = int(plan.cut), p.pieces = int(plan.pieces), p.piece = int(plan.piece);
   // as many key heads side by side as leave their queries and output gradients in L2
   const int64_t head = a.Nq * G * (DK + DV) * 2;
@@ -960,16 +985,16 @@ int launch(const WindowBwdArgs& a, char* msg, size_t msglen) {
   const uint64_t v_dims[4] = {DV, uint64_t(a.Nk), uint64_t(a.Hk), uint64_t(a.B)};
   const uint64_t k_str[3] = {map_stride(a.k.sn, a.Nk), map_stride(a.k.sh, a.Hk), map_stride(a.k.sb, a.B)};
   const uint64_t v_str[3] = {map_stride(a.v.sn, a.Nk), map_stride(a.v.sh, a.Hk), map_stride(a.v.sb, a.B)};
-  const uint32_t kv_box[4] = {64, kBlk, 1, 1};
+  const uint32_t kv_box[4] = {64, width_of(DK, DV), 1, 1};
   if (!encode_bf16_map_nd(&mq, a.q.p, 5, q_dims, q_str, row_box, msg, msglen) ||
       !encode_bf16_map_nd(&mg, a.go.p, 5, g_dims, g_str, row_box, msg, msglen) ||
       !encode_bf16_map_nd(&mk, a.k.p, 4, k_dims, k_str, kv_box, msg, msglen) ||
       !encode_bf16_map_nd(&mv, a.v.p, 4, v_dims, v_str, kv_box, msg, msglen))
     return 5;
   if (e == cudaSuccess)
-    e = launch_overlapped(window_delta_tc_kernel<DV>, dim3(unsigned(plan.row_tiles)), dim3(256), 0, a.stream, p);
+    e = launch_overlapped(window_delta_tc_kernel<DV>, dim3(unsigned(plan.pairs)), dim3(256), 0, a.stream, p);
   if (e == cudaSuccess)
-    e = launch_overlapped(kern, dim3(unsigned(plan.items + plan.row_tiles)), dim3(CK::kThreads), kSmem, a.stream, mq, mk, mv, mg, p,
+    e = launch_overlapped(kern, dim3(unsigned(plan.items + plan.pairs)), dim3(kThreads), kSmem, a.stream, mq, mk, mv, mg, p,
                           unsigned(plan.items));
   const int64_t joined = bh * plan.cut * kBlk * ((DK + DV) / 4);
   if (e == cudaSuccess && joined > 0)
