@@ -50,5 +50,21 @@ __host__ __device__ __forceinline__ Tiles tiles_of(const Mask& m, int len, int N
   return t;
 }
 
+// The same tokens as one sequence without the gap between them: token at(x) of the sequence is the x-th that
+// rows i0 .. i1 visit, of n.
+struct Run {
+  int first, from, n;
+  __host__ __device__ __forceinline__ int at(int x) const { return x < first ? x : x - first + from; }
+};
+__host__ __device__ __forceinline__ Run run_of(const Mask& m, int len, int N, int i0, int i1) {
+  const int end = row_end(m, len, N, i1), low = row_low(m, len, N, i0);
+  Run r;
+  r.first = m.sinks < low ? m.sinks : low;
+  r.from = low;
+  if (r.first > end) r.first = end;
+  r.n = r.first + (end > low ? end - low : 0);
+  return r;
+}
+
 }  // namespace win
 }  // namespace moa

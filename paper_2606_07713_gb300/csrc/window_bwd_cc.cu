@@ -139,12 +139,14 @@ __device__ __forceinline__ void fill_rows(const View& x, const View& y, float* s
     for (int c = 4 * (threadIdx.x & 15); c < DY; c += 64) fill4(sy + r * (DY + 4) + c, py + c, there);
   }
 }
-// Tokens n0 .. alike.
+// Tokens run.at(x0) .. alike.
 template <typename T, int DK, int DV, int TOKENS>
-__device__ __forceinline__ void fill_tokens(const View& k, const View& v, float* sk, float* sv, int b, int h, int n0, int Nk) {
+__device__ __forceinline__ void fill_tokens(const View& k, const View& v, float* sk, float* sv, int b, int h, int x0,
+                                            const win::Run& run) {
   for (int j = threadIdx.x >> 4; j < TOKENS; j += kThreads / 16) {
-    const bool there = n0 + j < Nk;
-    const T *pk = row_of<T>(k, b, h, there ? n0 + j : n0), *pv = row_of<T>(v, b, h, there ? n0 + j : n0);
+    const bool there = x0 + j < run.n;
+    const int n = run.at(there ? x0 + j : x0);
+    const T *pk = row_of<T>(k, b, h, n), *pv = row_of<T>(v, b, h, n);
 #pragma unroll
     for (int c = 4 * (threadIdx.x & 15); c < DK; c += 64) fill4(sk + j * (DK + 4) + c, pk + c, there);
 #pragma unroll
@@ -200,7 +202,7 @@ __device__ __forceinline__ void dkdv_tile(const Params& p, unsigned index, float
   const int64_t rows = int64_t(p.N) * p.G;
   int ra, rz;
   if (!rows_of_piece(p, kt, whole ? -1 : piece, &ra, &rz)) return;   // the join adds what pieces there are
-  fill_tokens<T, DK, DV, kKeysKv>(p.k, p.v, sK, sV, b, h, k0, p.Nk);
+  fill_tokens<T, DK, DV, kKeysKv>(p.k, p.v, sK, sV, b, h, k0, win::Run{p.Nk, p.Nk, p.Nk});
   if (ra < rz) fill_rows<T, DK, DV, kRowsKv>(p.q, p.go, sRows, sRows + kRowsKv * (DK + 4), b, h, p.G, ra, rz);
   fill_commit();
   float dv[4][DV / 16], dk[4][DK / 16];   // tokens 4 ty + a, features 64 c + 4 tx + e
@@ -363,9 +365,11 @@ __device__ __forceinline__ void dq_tile(const Params& p, unsigned index, float* 
   const int live = int(rows - r0 < kRowsQ ? rows - r0 : kRowsQ);
   const int off = p.Nk - p.N;
   const int i0 = r0 / p.G, i1 = (r0 + live - 1) / p.G;
-  const win::Tiles list = win::tiles_of(p.mask, p.Nk, p.N, i0, i1, kKeysQ);
+  // the tokens that they visit, 32 at a time, the sinks and the window's next to each other
+  const win::Run run = win::run_of(p.mask, p.Nk, p.N, i0, i1);
+  const int steps = (run.n + kKeysQ - 1) / kKeysQ;
   fill_rows<T, DK, DV, kRowsQ>(p.q, p.go, sQ, sG, b, h, p.G, r0, int(rows));
-  if (list.n > 0) fill_tokens<T, DK, DV, kKeysQ>(p.k, p.v, sTokens, sTokens + kKeysQ * (DK + 4), b, h, list.at(0) * kKeysQ, p.Nk);
+  if (steps > 0) fill_tokens<T, DK, DV, kKeysQ>(p.k, p.v, sTokens, sTokens + kKeysQ * (DK + 4), b, h, 0, run);
   fill_commit();
   float nl[4], d[4], dq[4][DK / 16];
   int pos[4];
@@ -379,13 +383,12 @@ __device__ __forceinline__ void dq_tile(const Params& p, unsigned index, float* 
 #pragma unroll
     for (int c = 0; c < DK / 16; ++c) dq[a][c] = 0.f;
   }
-  for (int t = 0; t < list.n; ++t) {
-    const int n0 = list.at(t) * kKeysQ;
+  for (int t = 0; t < steps; ++t) {
     const float* sK = sTokens + (t & 1) * S::kTokens;
     const float* sV = sK + kKeysQ * (DK + 4);
     float* next = sTokens + (~t & 1) * S::kTokens;
-    if (t + 1 < list.n)
-      fill_tokens<T, DK, DV, kKeysQ>(p.k, p.v, next, next + kKeysQ * (DK + 4), b, h, list.at(t + 1) * kKeysQ, p.Nk);
+    if (t + 1 < steps)
+      fill_tokens<T, DK, DV, kKeysQ>(p.k, p.v, next, next + kKeysQ * (DK + 4), b, h, (t + 1) * kKeysQ, run);
     fill_commit();
     fill_wait<1>();
     __syncthreads();
@@ -417,7 +420,7 @@ __device__ __forceinline__ void dq_tile(const Params& p, unsigned index, float* 
     }
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      const int j = n0 + tx + 16 * x;
+      const int at = t * kKeysQ + tx + 16 * x, j = at < run.n ? run.at(at) : 0x7fffffff;
       float4 ws;
       float* fs = reinterpret_cast<float*>(&ws);
 #pragma unroll

@@ -117,16 +117,17 @@ window_cc_kernel(const Params p) {
   const int rows = rows_all - r0 < C::kRows ? rows_all - r0 : C::kRows;
   const int len = length_of(p, b);
   const int i0 = r0 / p.G, i1 = (r0 + rows - 1) / p.G;
-  const win::Tiles list = win::tiles_of(p.mask, len, p.N, i0, i1, kKeys);
-  const int first = int(int64_t(list.n) * blockIdx.y / p.splits), last = int(int64_t(list.n) * (blockIdx.y + 1) / p.splits);
-  // the first token that any row sees by its window: between the sinks and it nothing is read
-  const int low0 = win::row_low(p.mask, len, p.N, i0), end1 = win::row_end(p.mask, len, p.N, i1);
+  // the tokens that its rows visit, 64 at a time, the sinks and the window's next to each other
+  const win::Run run = win::run_of(p.mask, len, p.N, i0, i1);
+  const int tiles = (run.n + kKeys - 1) / kKeys;
+  const int first = int(int64_t(tiles) * blockIdx.y / p.splits), last = int(int64_t(tiles) * (blockIdx.y + 1) / p.splits);
 
   auto find = [&](int t) {   // where tile t's tokens lie
     if (t >= last || threadIdx.x >= kKeys) return;
-    const int n = list.at(t) * kKeys + int(threadIdx.x);
+    const int x = t * kKeys + int(threadIdx.x);
     const T *k = nullptr, *v = nullptr;
-    if (n < end1 && (n >= low0 || n < p.mask.sinks)) {
+    if (x < run.n) {
+      const int n = run.at(x);
       int64_t at = b, place = n;
       bool there = true;
       if (p.kv.table != nullptr) {
@@ -193,7 +194,6 @@ window_cc_kernel(const Params p) {
   }
   // the next tile's keys are on their way during the second product, its values during the next first one
   for (int t = first; t < last; ++t) {
-    const int n0 = list.at(t) * kKeys;
     fill_wait<1>();
     __syncthreads();
     // scores of tokens tx, tx + 16, ... : a quarter warp's rows of sK then lie in all banks
@@ -220,14 +220,16 @@ window_cc_kernel(const Params p) {
         }
     }
     float w[RM][4];
+    int token[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) token[k] = t * kKeys + tx + 16 * k < run.n ? run.at(t * kKeys + tx + 16 * k) : 0x7fffffff;
 #pragma unroll
     for (int a = 0; a < RM; ++a) {
       bool seen[4];
       float top = -INFINITY;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const int n = n0 + tx + 16 * k;
-        seen[k] = n < end[a] && (n >= low[a] || n < p.mask.sinks);
+        seen[k] = token[k] < end[a] && (token[k] >= low[a] || token[k] < p.mask.sinks);
         w[a][k] = s[a][k] * p.c_log2;
         if (seen[k]) top = fmaxf(top, w[a][k]);
       }
@@ -324,6 +326,7 @@ window_cc_join_kernel(Params p, int tile_rows) {
   const float base = M == -INFINITY ? 0.f : M;
   float L = 0.f;
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
   for (int k = 0; k < p.splits; ++k) {
     const float2 ml = p.part_ml[place(k)];
     const float f = exp2f(ml.x - base);   // 0 of a share that saw nothing
@@ -395,8 +398,7 @@ WindowCcPlan window_cc_plan(const WindowArgs& a, int sms) {
   // most tiles of tokens that a row tile visits
   int64_t most = (a.max_len + kKeys - 1) / kKeys;
   if (a.window != win::kNoWindow) {
-    const int64_t span = int64_t(a.window) + p.rows / G + 2;
-    const int64_t seen = (span + kKeys - 1) / kKeys + 1 + (int64_t(a.sinks) + kKeys - 1) / kKeys;
+    const int64_t seen = (int64_t(a.window) + p.rows / G + 2 + a.sinks + kKeys - 1) / kKeys;
     if (seen < most) most = seen;
   }
   p.splits = p.items >= 2 * sms ? 1 : (2 * sms + p.items - 1) / p.items;
