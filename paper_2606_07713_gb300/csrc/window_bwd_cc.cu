@@ -174,22 +174,25 @@ __device__ __forceinline__ bool rows_of_piece(const Params& p, int kt, int piece
   return true;
 }
 
+// Buffers of a step's rows or tokens: two where two CTAs still fit on an SM (8 warps alone left it waiting for shared memory
+// half of the time: gradients of 2 x (6 / 3) heads x 517 x (128 / 64), window 100: 77 us, with all that is below 61).
+__host__ __device__ constexpr int buffers(int dk, int dv) { return dk + dv <= 192 ? 2 : 1; }
+
 template <int DK, int DV>
 struct KvSmem {
   static constexpr int kLdW = kKeysKv + 4;
   static constexpr int kRows = kRowsKv * (DK + 4 + DV + 4);   // a step's queries and output gradients
-  static constexpr int kFloats = kKeysKv * (DK + 4 + DV + 4) + 2 * kRows + 2 * kRowsKv * kLdW;
+  static constexpr int kFloats = kKeysKv * (DK + 4 + DV + 4) + buffers(DK, DV) * kRows + kRowsKv * kLdW;
 };
 
 template <typename T, int DK, int DV>
 __device__ __forceinline__ void dkdv_tile(const Params& p, unsigned index, float* smem) {
   using S = KvSmem<DK, DV>;
-  constexpr int kLdW = S::kLdW;
+  constexpr int kLdW = S::kLdW, kBuf = buffers(DK, DV);
   float* sK = smem;
   float* sV = sK + kKeysKv * (DK + 4);
   float* sRows = sV + kKeysKv * (DV + 4);
-  float* sP = sRows + 2 * S::kRows;   // [rows][tokens]
-  float* sS = sP + kRowsKv * kLdW;
+  float* sP = sRows + kBuf * S::kRows;   // [rows][tokens]: the weights, then dS
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   // items of a key head: the pieces of its first `cut` tiles, then the other tiles
   const unsigned per = unsigned(p.cut * p.pieces + p.n_kt - p.cut);
@@ -214,81 +217,95 @@ __device__ __forceinline__ void dkdv_tile(const Params& p, unsigned index, float
     for (int c = 0; c < DK / 16; ++c) dk[a][c] = 0.f;
   }
   for (int r0 = ra, step = 0; r0 < rz; r0 += kRowsKv, ++step) {
-    const float* sQ = sRows + (step & 1) * S::kRows;
+    const float* sQ = sRows + (step % kBuf) * S::kRows;
     const float* sG = sQ + kRowsKv * (DK + 4);
-    float* next = sRows + (~step & 1) * S::kRows;
-    if (r0 + kRowsKv < rz) fill_rows<T, DK, DV, kRowsKv>(p.q, p.go, next, next + kRowsKv * (DK + 4), b, h, p.G, r0 + kRowsKv, rz);
+    float* next = sRows + ((step + 1) % kBuf) * S::kRows;
+    if (kBuf == 2 && r0 + kRowsKv < rz)
+      fill_rows<T, DK, DV, kRowsKv>(p.q, p.go, next, next + kRowsKv * (DK + 4), b, h, p.G, r0 + kRowsKv, rz);
     fill_commit();
-    fill_wait<1>();
+    fill_wait<kBuf - 1>();
     __syncthreads();
-    // rows tx, tx + 16 against tokens 4 ty + a
-    float s[4][2], e[4][2];
+    // A warp whose eight tokens no row of the step sees has nothing to add: beside a window's ends, and of the tokens
+    // behind the sinks in all rows that only see those.
+    const int p0 = int(unsigned(r0) / unsigned(p.G)) + off, r1 = r0 + kRowsKv < rz ? r0 + kRowsKv : rz;
+    const int p1 = int(unsigned(r1 - 1) / unsigned(p.G)) + off, j0 = k0 + 8 * (threadIdx.x >> 5);
+    if (j0 <= p1 && (p0 - (j0 + 7) < p.mask.window || j0 < p.mask.sinks)) {
+      // rows tx, tx + 16 against tokens 4 ty + a
+      float s[4][2], e[4][2];
 #pragma unroll
-    for (int a = 0; a < 4; ++a) s[a][0] = s[a][1] = e[a][0] = e[a][1] = 0.f;
+      for (int a = 0; a < 4; ++a) s[a][0] = s[a][1] = e[a][0] = e[a][1] = 0.f;
 #pragma unroll 4
-    for (int c = 0; c < DK; c += 4) {
-      const float4 q0 = *reinterpret_cast<const float4*>(sQ + tx * (DK + 4) + c);
-      const float4 q1 = *reinterpret_cast<const float4*>(sQ + (tx + 16) * (DK + 4) + c);
+      for (int c = 0; c < DK; c += 4) {
+        const float4 q0 = *reinterpret_cast<const float4*>(sQ + tx * (DK + 4) + c);
+        const float4 q1 = *reinterpret_cast<const float4*>(sQ + (tx + 16) * (DK + 4) + c);
 #pragma unroll
-      for (int a = 0; a < 4; ++a) {
-        const float4 kk = *reinterpret_cast<const float4*>(sK + (4 * ty + a) * (DK + 4) + c);
-        s[a][0] = dot4(q0, kk, s[a][0]);
-        s[a][1] = dot4(q1, kk, s[a][1]);
+        for (int a = 0; a < 4; ++a) {
+          const float4 kk = *reinterpret_cast<const float4*>(sK + (4 * ty + a) * (DK + 4) + c);
+          s[a][0] = dot4(q0, kk, s[a][0]);
+          s[a][1] = dot4(q1, kk, s[a][1]);
+        }
       }
-    }
 #pragma unroll 4
-    for (int c = 0; c < DV; c += 4) {
-      const float4 g0 = *reinterpret_cast<const float4*>(sG + tx * (DV + 4) + c);
-      const float4 g1 = *reinterpret_cast<const float4*>(sG + (tx + 16) * (DV + 4) + c);
+      for (int c = 0; c < DV; c += 4) {
+        const float4 g0 = *reinterpret_cast<const float4*>(sG + tx * (DV + 4) + c);
+        const float4 g1 = *reinterpret_cast<const float4*>(sG + (tx + 16) * (DV + 4) + c);
 #pragma unroll
-      for (int a = 0; a < 4; ++a) {
-        const float4 vv = *reinterpret_cast<const float4*>(sV + (4 * ty + a) * (DV + 4) + c);
-        e[a][0] = dot4(g0, vv, e[a][0]);
-        e[a][1] = dot4(g1, vv, e[a][1]);
+        for (int a = 0; a < 4; ++a) {
+          const float4 vv = *reinterpret_cast<const float4*>(sV + (4 * ty + a) * (DV + 4) + c);
+          e[a][0] = dot4(g0, vv, e[a][0]);
+          e[a][1] = dot4(g1, vv, e[a][1]);
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int r = r0 + tx + 16 * x;
+        const bool live = r < rz;
+        const int pos = int(unsigned(live ? r : rz - 1) / unsigned(p.G)) + off;
+        const float nl = live ? p.nl[bh * rows + r] : -INFINITY, d = live ? p.delta[bh * rows + r] : 0.f;
+        // the weights into s, dS into e
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+          const int j = k0 + 4 * ty + a;
+          const bool seen = live && j <= pos && (pos - j < p.mask.window || j < p.mask.sinks) && j < p.Nk;
+          s[a][x] = seen ? exp2f(fmaf(s[a][x], p.c_log2, nl)) : 0.f;
+          e[a][x] = seen ? s[a][x] * (e[a][x] - d) : 0.f;
+        }
+        *reinterpret_cast<float4*>(sP + (tx + 16 * x) * kLdW + 4 * ty) = make_float4(s[0][x], s[1][x], s[2][x], s[3][x]);
+      }
+      __syncwarp();   // tokens 4 ty .. of all rows: written and read by the same half warp
+#pragma unroll 4
+      for (int r = 0; r < kRowsKv; ++r) {
+        const float4 w = *reinterpret_cast<const float4*>(sP + r * kLdW + 4 * ty);
+#pragma unroll
+        for (int c = 0; c < DV / 64; ++c) {
+          const float4 g = *reinterpret_cast<const float4*>(sG + r * (DV + 4) + 64 * c + 4 * tx);
+          axpy4(w.x, g, dv[0] + 4 * c);
+          axpy4(w.y, g, dv[1] + 4 * c);
+          axpy4(w.z, g, dv[2] + 4 * c);
+          axpy4(w.w, g, dv[3] + 4 * c);
+        }
+      }
+      __syncwarp();
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+        *reinterpret_cast<float4*>(sP + (tx + 16 * x) * kLdW + 4 * ty) = make_float4(e[0][x], e[1][x], e[2][x], e[3][x]);
+      __syncwarp();
+#pragma unroll 4
+      for (int r = 0; r < kRowsKv; ++r) {
+        const float4 w = *reinterpret_cast<const float4*>(sP + r * kLdW + 4 * ty);
+#pragma unroll
+        for (int c = 0; c < DK / 64; ++c) {
+          const float4 q = *reinterpret_cast<const float4*>(sQ + r * (DK + 4) + 64 * c + 4 * tx);
+          axpy4(w.x, q, dk[0] + 4 * c);
+          axpy4(w.y, q, dk[1] + 4 * c);
+          axpy4(w.z, q, dk[2] + 4 * c);
+          axpy4(w.w, q, dk[3] + 4 * c);
+        }
       }
     }
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int r = r0 + tx + 16 * x;
-      const bool live = r < rz;
-      const int pos = int(unsigned(live ? r : rz - 1) / unsigned(p.G)) + off;
-      const float nl = live ? p.nl[bh * rows + r] : -INFINITY, d = live ? p.delta[bh * rows + r] : 0.f;
-      float4 wp, ws;
-      float* fp = reinterpret_cast<float*>(&wp);
-      float* fs = reinterpret_cast<float*>(&ws);
-#pragma unroll
-      for (int a = 0; a < 4; ++a) {
-        const int j = k0 + 4 * ty + a;
-        const bool seen = live && j <= pos && (pos - j < p.mask.window || j < p.mask.sinks) && j < p.Nk;
-        fp[a] = seen ? exp2f(fmaf(s[a][x], p.c_log2, nl)) : 0.f;
-        fs[a] = seen ? fp[a] * (e[a][x] - d) : 0.f;
-      }
-      *reinterpret_cast<float4*>(sP + (tx + 16 * x) * kLdW + 4 * ty) = wp;
-      *reinterpret_cast<float4*>(sS + (tx + 16 * x) * kLdW + 4 * ty) = ws;
-    }
-    __syncwarp();   // tokens 4 ty .. of all rows: written and read by the same half warp
-#pragma unroll 2
-    for (int r = 0; r < kRowsKv; ++r) {
-      const float4 wp = *reinterpret_cast<const float4*>(sP + r * kLdW + 4 * ty);
-      const float4 ws = *reinterpret_cast<const float4*>(sS + r * kLdW + 4 * ty);
-#pragma unroll
-      for (int c = 0; c < DV / 64; ++c) {
-        const float4 g = *reinterpret_cast<const float4*>(sG + r * (DV + 4) + 64 * c + 4 * tx);
-        axpy4(wp.x, g, dv[0] + 4 * c);
-        axpy4(wp.y, g, dv[1] + 4 * c);
-        axpy4(wp.z, g, dv[2] + 4 * c);
-        axpy4(wp.w, g, dv[3] + 4 * c);
-      }
-#pragma unroll
-      for (int c = 0; c < DK / 64; ++c) {
-        const float4 q = *reinterpret_cast<const float4*>(sQ + r * (DK + 4) + 64 * c + 4 * tx);
-        axpy4(ws.x, q, dk[0] + 4 * c);
-        axpy4(ws.y, q, dk[1] + 4 * c);
-        axpy4(ws.z, q, dk[2] + 4 * c);
-        axpy4(ws.w, q, dk[3] + 4 * c);
-      }
-    }
-    __syncthreads();   // this step's rows make room for those after the next
+    __syncthreads();   // this step's rows make room for others
+    if (kBuf == 1 && r0 + kRowsKv < rz)
+      fill_rows<T, DK, DV, kRowsKv>(p.q, p.go, next, next + kRowsKv * (DK + 4), b, h, p.G, r0 + kRowsKv, rz);
   }
   fill_wait<0>();
 #pragma unroll
@@ -346,17 +363,17 @@ template <int DK, int DV>
 struct QSmem {
   static constexpr int kLdW = kRowsQ + 4;
   static constexpr int kTokens = kKeysQ * (DK + 4 + DV + 4);   // a step's keys and values
-  static constexpr int kFloats = kRowsQ * (DK + 4 + DV + 4) + 2 * kTokens + kKeysQ * kLdW;
+  static constexpr int kFloats = kRowsQ * (DK + 4 + DV + 4) + buffers(DK, DV) * kTokens + kKeysQ * kLdW;
 };
 
 template <typename T, int DK, int DV>
 __device__ __forceinline__ void dq_tile(const Params& p, unsigned index, float* smem) {
   using S = QSmem<DK, DV>;
-  constexpr int kLdW = S::kLdW;
+  constexpr int kLdW = S::kLdW, kBuf = buffers(DK, DV);
   float* sQ = smem;
   float* sG = sQ + kRowsQ * (DK + 4);
   float* sTokens = sG + kRowsQ * (DV + 4);
-  float* sS = sTokens + 2 * S::kTokens;   // [tokens][rows]
+  float* sS = sTokens + kBuf * S::kTokens;   // [tokens][rows]
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const int bh = int(index / unsigned(p.n_rt)), b = bh / p.Hk, h = bh - b * p.Hk;
   // the last rows, which see the most without a window, come first
@@ -383,67 +400,77 @@ __device__ __forceinline__ void dq_tile(const Params& p, unsigned index, float* 
 #pragma unroll
     for (int c = 0; c < DK / 16; ++c) dq[a][c] = 0.f;
   }
+  // positions of the warp's rows
+  const int wr = r0 + 8 * (threadIdx.x >> 5), wz = r0 + live < wr + 8 ? r0 + live : wr + 8;
+  const int warp_first = wr / p.G + off, warp_last = wz > wr ? (wz - 1) / p.G + off : -1;
   for (int t = 0; t < steps; ++t) {
-    const float* sK = sTokens + (t & 1) * S::kTokens;
+    const float* sK = sTokens + (t % kBuf) * S::kTokens;
     const float* sV = sK + kKeysQ * (DK + 4);
-    float* next = sTokens + (~t & 1) * S::kTokens;
-    if (t + 1 < steps)
+    float* next = sTokens + ((t + 1) % kBuf) * S::kTokens;
+    if (kBuf == 2 && t + 1 < steps)
       fill_tokens<T, DK, DV, kKeysQ>(p.k, p.v, next, next + kKeysQ * (DK + 4), b, h, (t + 1) * kKeysQ, run);
     fill_commit();
-    fill_wait<1>();
+    fill_wait<kBuf - 1>();
     __syncthreads();
-    // tokens tx, tx + 16 against rows 4 ty + a
-    float s[4][2], e[4][2];
+    // A warp whose eight rows see no token of the step has nothing to add.
+    const int x1 = (t + 1) * kKeysQ < run.n ? (t + 1) * kKeysQ - 1 : run.n - 1;
+    const int first = run.at(t * kKeysQ), last = run.at(x1);   // tokens
+    if (first <= warp_last && (warp_first - last < p.mask.window || first < p.mask.sinks)) {
+      // tokens tx, tx + 16 against rows 4 ty + a
+      float s[4][2], e[4][2];
 #pragma unroll
-    for (int a = 0; a < 4; ++a) s[a][0] = s[a][1] = e[a][0] = e[a][1] = 0.f;
+      for (int a = 0; a < 4; ++a) s[a][0] = s[a][1] = e[a][0] = e[a][1] = 0.f;
 #pragma unroll 4
-    for (int c = 0; c < DK; c += 4) {
-      const float4 k0 = *reinterpret_cast<const float4*>(sK + tx * (DK + 4) + c);
-      const float4 k1 = *reinterpret_cast<const float4*>(sK + (tx + 16) * (DK + 4) + c);
+      for (int c = 0; c < DK; c += 4) {
+        const float4 k0 = *reinterpret_cast<const float4*>(sK + tx * (DK + 4) + c);
+        const float4 k1 = *reinterpret_cast<const float4*>(sK + (tx + 16) * (DK + 4) + c);
 #pragma unroll
-      for (int a = 0; a < 4; ++a) {
-        const float4 q = *reinterpret_cast<const float4*>(sQ + (4 * ty + a) * (DK + 4) + c);
-        s[a][0] = dot4(q, k0, s[a][0]);
-        s[a][1] = dot4(q, k1, s[a][1]);
+        for (int a = 0; a < 4; ++a) {
+          const float4 q = *reinterpret_cast<const float4*>(sQ + (4 * ty + a) * (DK + 4) + c);
+          s[a][0] = dot4(q, k0, s[a][0]);
+          s[a][1] = dot4(q, k1, s[a][1]);
+        }
       }
-    }
 #pragma unroll 4
-    for (int c = 0; c < DV; c += 4) {
-      const float4 v0 = *reinterpret_cast<const float4*>(sV + tx * (DV + 4) + c);
-      const float4 v1 = *reinterpret_cast<const float4*>(sV + (tx + 16) * (DV + 4) + c);
+      for (int c = 0; c < DV; c += 4) {
+        const float4 v0 = *reinterpret_cast<const float4*>(sV + tx * (DV + 4) + c);
+        const float4 v1 = *reinterpret_cast<const float4*>(sV + (tx + 16) * (DV + 4) + c);
 #pragma unroll
-      for (int a = 0; a < 4; ++a) {
-        const float4 g = *reinterpret_cast<const float4*>(sG + (4 * ty + a) * (DV + 4) + c);
-        e[a][0] = dot4(g, v0, e[a][0]);
-        e[a][1] = dot4(g, v1, e[a][1]);
+        for (int a = 0; a < 4; ++a) {
+          const float4 g = *reinterpret_cast<const float4*>(sG + (4 * ty + a) * (DV + 4) + c);
+          e[a][0] = dot4(g, v0, e[a][0]);
+          e[a][1] = dot4(g, v1, e[a][1]);
+        }
       }
-    }
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int at = t * kKeysQ + tx + 16 * x, j = at < run.n ? run.at(at) : 0x7fffffff;
-      float4 ws;
-      float* fs = reinterpret_cast<float*>(&ws);
+      for (int x = 0; x < 2; ++x) {
+        const int at = t * kKeysQ + tx + 16 * x, j = at < run.n ? run.at(at) : 0x7fffffff;
+        float4 ws;
+        float* fs = reinterpret_cast<float*>(&ws);
 #pragma unroll
-      for (int a = 0; a < 4; ++a) {
-        const bool seen = j <= pos[a] && (pos[a] - j < p.mask.window || j < p.mask.sinks);
-        fs[a] = seen ? exp2f(fmaf(s[a][x], p.c_log2, nl[a])) * (e[a][x] - d[a]) : 0.f;
+        for (int a = 0; a < 4; ++a) {
+          const bool seen = j <= pos[a] && (pos[a] - j < p.mask.window || j < p.mask.sinks);
+          fs[a] = seen ? exp2f(fmaf(s[a][x], p.c_log2, nl[a])) * (e[a][x] - d[a]) : 0.f;
+        }
+        *reinterpret_cast<float4*>(sS + (tx + 16 * x) * kLdW + 4 * ty) = ws;
       }
-      *reinterpret_cast<float4*>(sS + (tx + 16 * x) * kLdW + 4 * ty) = ws;
-    }
-    __syncwarp();
+      __syncwarp();
 #pragma unroll 4
-    for (int j = 0; j < kKeysQ; ++j) {
-      const float4 ws = *reinterpret_cast<const float4*>(sS + j * kLdW + 4 * ty);
+      for (int j = 0; j < kKeysQ; ++j) {
+        const float4 ws = *reinterpret_cast<const float4*>(sS + j * kLdW + 4 * ty);
 #pragma unroll
-      for (int c = 0; c < DK / 64; ++c) {
-        const float4 k = *reinterpret_cast<const float4*>(sK + j * (DK + 4) + 64 * c + 4 * tx);
-        axpy4(ws.x, k, dq[0] + 4 * c);
-        axpy4(ws.y, k, dq[1] + 4 * c);
-        axpy4(ws.z, k, dq[2] + 4 * c);
-        axpy4(ws.w, k, dq[3] + 4 * c);
+        for (int c = 0; c < DK / 64; ++c) {
+          const float4 k = *reinterpret_cast<const float4*>(sK + j * (DK + 4) + 64 * c + 4 * tx);
+          axpy4(ws.x, k, dq[0] + 4 * c);
+          axpy4(ws.y, k, dq[1] + 4 * c);
+          axpy4(ws.z, k, dq[2] + 4 * c);
+          axpy4(ws.w, k, dq[3] + 4 * c);
+        }
       }
     }
-    __syncthreads();   // this step's tokens make room for those after the next
+    __syncthreads();   // this step's tokens make room for others
+    if (kBuf == 1 && t + 1 < steps)
+      fill_tokens<T, DK, DV, kKeysQ>(p.k, p.v, next, next + kKeysQ * (DK + 4), b, h, (t + 1) * kKeysQ, run);
   }
   fill_wait<0>();
 #pragma unroll
@@ -460,16 +487,16 @@ __device__ __forceinline__ void dq_tile(const Params& p, unsigned index, float* 
   }
 }
 
-// CTAs below n_kv: dK and dV; the others: dQ.
+// CTAs below n_q: dQ; the others, whose pieces are shorter: dK and dV.
 template <typename T, int DK, int DV>
-__global__ void __launch_bounds__(kThreads)
-window_bwd_cc_kernel(const Params p, unsigned n_kv) {
+__global__ void __launch_bounds__(kThreads, 2)
+window_bwd_cc_kernel(const Params p, unsigned n_q) {
   extern __shared__ float smem[];
   wait_for_previous();
-  if (blockIdx.x < n_kv)
-    dkdv_tile<T, DK, DV>(p, blockIdx.x, smem);
+  if (blockIdx.x < n_q)
+    dq_tile<T, DK, DV>(p, blockIdx.x, smem);
   else
-    dq_tile<T, DK, DV>(p, blockIdx.x - n_kv, smem);
+    dkdv_tile<T, DK, DV>(p, blockIdx.x - n_q, smem);
 }
 
 // How token tiles are cut: pieces of a window's rows (of all rows without one), or of so few that there are two CTAs
@@ -495,7 +522,7 @@ Cut cut_of(const WindowBwdArgs& a) {
       c.cut = c.n_kt;
     }
   }
-  if (want < 2 * kRowsKv) want = 2 * kRowsKv;
+  if (want < 3 * kRowsKv) want = 3 * kRowsKv;   // (2, 3, 4, 6 steps: 64, 61, 63, 75 us of the case above)
   c.piece_rows = (want + kRowsKv - 1) / kRowsKv * kRowsKv;
   if (c.cut > c.n_kt) c.cut = c.n_kt;
   // not more pieces than keep the machine busy: each is 64 rows of fp32 in the workspace (80 MB in all)
@@ -533,7 +560,7 @@ int launch(const WindowBwdArgs& a, char* msg, size_t msglen) {
     e = launch_overlapped(window_delta_kernel<T, DV>, dim3(unsigned((rows + 7) / 8)), dim3(kThreads), 0, a.stream, p, rows);
   const int64_t items = bh * (cut.cut * cut.pieces + cut.n_kt - cut.cut);
   if (e == cudaSuccess)
-    e = launch_overlapped(kern, dim3(unsigned(items + bh * p.n_rt)), dim3(kThreads), size_t(kSmem), a.stream, p, unsigned(items));
+    e = launch_overlapped(kern, dim3(unsigned(items + bh * p.n_rt)), dim3(kThreads), size_t(kSmem), a.stream, p, unsigned(bh * p.n_rt));
   const int64_t joined = bh * cut.cut * kKeysKv * ((DK + DV) / 4);
   if (e == cudaSuccess && joined > 0)
     e = launch_overlapped(window_dkdv_join_kernel<T, DK, DV>, dim3(unsigned((joined + kThreads - 1) / kThreads)), dim3(kThreads),
