@@ -24,7 +24,39 @@ cudaError_t launch_overlapped(void (*kernel)(P...), dim3 grid, dim3 block, size_
   c.numAttrs = 1;
   return cudaLaunchKernelEx(&c, kernel, P(std::forward<A>(args))...);
 }
+// The same with clusters of `cluster` CTAs along the grid's y axis.
+template <typename... P, typename... A>
+cudaError_t launch_clusters(void (*kernel)(P...), dim3 grid, unsigned cluster, dim3 block, size_t smem, cudaStream_t stream,
+                            A&&... args) {
+  cudaLaunchAttribute attr[2]{};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = 1;
+  attr[1].val.clusterDim.y = cluster;
+  attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t c{};
+  c.gridDim = grid;
+  c.blockDim = block;
+  c.dynamicSmemBytes = smem;
+  c.stream = stream;
+  c.attrs = attr;
+  c.numAttrs = 2;
+  return cudaLaunchKernelEx(&c, kernel, P(std::forward<A>(args))...);
+}
 #ifdef __CUDACC__
+// All threads of all CTAs of the cluster; what they wrote before is seen after.
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// Four floats of CTA `rank`'s shared memory, at the place that `p` has in this CTA's.
+__device__ __forceinline__ float4 load_of_cta(const float4* p, unsigned rank) {
+  uint32_t at;
+  float4 v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(uint32_t(__cvta_generic_to_shared(p))), "r"(rank));
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+  return v;
+}
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 #endif
 
@@ -137,6 +169,7 @@ struct WindowCcPlan {
   int rows;              // query rows of a tile
   int64_t items;         // tiles of all key heads
   int64_t splits;        // shares of a tile's tokens, joined at the end
+  bool cluster;          // by the CTAs of a cluster, in the same launch
 };
 WindowCcPlan window_cc_plan(const WindowArgs& a, int sms);
 size_t window_cc_workspace(const WindowArgs& a, const WindowCcPlan& p);

@@ -9,7 +9,7 @@
 // A key head's query rows are counted position by position: row r is query r / G of head r % G of the
 // group, so that a tile of rows covers few positions and a window few tiles of tokens.  A CTA takes one
 // tile of rows (64, or 16 where there are few) and a share of the 64-token tiles that it visits; shares
-// are joined by a second kernel.  Thread (ty, tx) holds RM rows: the scores of four tokens of each,
+// are joined through the shared memory of a cluster, or by a second kernel where there are more than sixteen.  Thread (ty, tx) holds RM rows: the scores of four tokens of each,
 // then DV / 16 features of their outputs.
 //
 // What bounds it: fused multiply-adds, one for each shared-memory word of a row's and a token's
@@ -33,6 +33,7 @@ __device__ unsigned int g_moa_window_cc_status = 0;
 namespace {
 
 constexpr int kKeys = 64;            // tokens of a tile
+constexpr int kMostCluster = 16;     // CTAs of a cluster (more than 8 are asked for by an attribute)
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct Params {
@@ -283,6 +284,46 @@ window_cc_kernel(const Params p) {
   }
   fill_wait<0>();
 
+  if (p.splits > 1 && p.part_o == nullptr) {
+    // The shares are the CTAs of a cluster: each leaves its rows' sums in shared memory (where keys were) and joins every
+    // splits-th row from all of them.
+    float4* sum = reinterpret_cast<float4*>(sK);                                   // [rows][DV / 4]
+    float4* stat = reinterpret_cast<float4*>(sK + C::kRows * DV);                  // [rows] m, l
+    __syncthreads();
+#pragma unroll
+    for (int a = 0; a < RM; ++a) {
+      const int r = ty * RM + a;
+#pragma unroll
+      for (int c = 0; c < DV / 64; ++c)
+        sum[r * (DV / 4) + c * 16 + tx] = make_float4(acc[a][4 * c], acc[a][4 * c + 1], acc[a][4 * c + 2], acc[a][4 * c + 3]);
+      if (tx == 0) stat[r] = make_float4(m[a], l[a], 0.f, 0.f);
+    }
+    cluster_sync();
+    for (int x = threadIdx.x; x < (rows + p.splits - 1) / p.splits * (DV / 4); x += NT) {
+      const int r = x / (DV / 4) * p.splits + int(blockIdx.y), c = x % (DV / 4);
+      if (r >= rows) continue;
+      float M = -INFINITY, L = 0.f;
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+      for (int k = 0; k < p.splits; ++k) M = fmaxf(M, load_of_cta(stat + r, k).x);
+      const float base = M == -INFINITY ? 0.f : M;
+#pragma unroll 4
+      for (int k = 0; k < p.splits; ++k) {
+        const float4 ml = load_of_cta(stat + r, k), v = load_of_cta(sum + r * (DV / 4) + c, k);
+        const float f = exp2f(ml.x - base);
+        L += f * ml.y;
+        o.x += f * v.x, o.y += f * v.y, o.z += f * v.z, o.w += f * v.w;
+      }
+      const float inv = L == 0.f ? 0.f : 1.f / L;
+      const int i = (r0 + r) / p.G, g = r0 + r - i * p.G;
+      store4(static_cast<T*>(p.o.p) + b * p.o.sb + (int64_t(h) * p.G + g) * p.o.sh + i * p.o.sn + c * 4,
+             make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+      if (p.lse != nullptr && c == 0)
+        p.lse[((int64_t(b) * p.Hk + h) * p.G + g) * p.N + i] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
+    }
+    cluster_sync();   // no CTA leaves while others read from it
+    return;
+  }
 #pragma unroll
   for (int a = 0; a < RM; ++a) {
     const int r = ty * RM + a;
@@ -357,13 +398,18 @@ int launch(const WindowArgs& a, const WindowCcPlan& plan, char* msg, size_t msgl
   p.mask = win::Mask{a.window, a.sinks, a.causal};
   p.c_log2 = a.scale * kLog2e;
   p.splits = int(plan.splits);
-  if (plan.splits > 1) {
+  if (plan.splits > 1 && !plan.cluster) {
     p.part_o = static_cast<float*>(a.ws);
     p.part_ml = reinterpret_cast<float2*>(p.part_o + plan.items * plan.splits * C::kRows * DV);
   }
+  static_assert(C::kRows * DV + 4 * C::kRows <= kKeys * C::kLdK + kKeys * DV, "the sums lie where keys and values were");
+  const dim3 grid(unsigned(plan.items), unsigned(plan.splits));
+  if (e == cudaSuccess && plan.cluster && plan.splits > 8)
+    e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kern), cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e == cudaSuccess)
-    e = launch_overlapped(kern, dim3(unsigned(plan.items), unsigned(plan.splits)), dim3(NT), C::kSmem, a.stream, p);
-  if (e == cudaSuccess && plan.splits > 1)
+    e = plan.cluster ? launch_clusters(kern, grid, unsigned(plan.splits), dim3(NT), C::kSmem, a.stream, p)
+                     : launch_overlapped(kern, grid, dim3(NT), C::kSmem, a.stream, p);
+  if (e == cudaSuccess && plan.splits > 1 && !plan.cluster)
     e = launch_overlapped(window_cc_join_kernel<T, DV>, dim3(unsigned(plan.items), C::kRows / 8), dim3(256), 0, a.stream, p,
                           int(C::kRows));
   if (e != cudaSuccess) {
@@ -404,11 +450,14 @@ WindowCcPlan window_cc_plan(const WindowArgs& a, int sms) {
   p.splits = p.items >= 2 * sms ? 1 : (2 * sms + p.items - 1) / p.items;
   if (p.splits > most) p.splits = most;
   if (p.splits < 1) p.splits = 1;
+  // joined by clusters where sixteen CTAs have no more than three tiles each
+  p.cluster = p.splits > 1 && (p.splits <= kMostCluster || most <= 3 * kMostCluster);
+  if (p.cluster && p.splits > kMostCluster) p.splits = kMostCluster;
   return p;
 }
 
 size_t window_cc_workspace(const WindowArgs& a, const WindowCcPlan& p) {
-  return p.splits > 1 ? size_t(p.items * p.splits * p.rows) * size_t(a.dv * 4 + 8) : 0;
+  return p.splits > 1 && !p.cluster ? size_t(p.items * p.splits * p.rows) * size_t(a.dv * 4 + 8) : 0;
 }
 
 int launch_window_cc(const WindowArgs& a, const WindowCcPlan& plan, char* msg, size_t msglen) {
