@@ -45,15 +45,29 @@ cudaError_t launch_clusters(void (*kernel)(P...), dim3 grid, unsigned cluster, d
   return cudaLaunchKernelEx(&c, kernel, P(std::forward<A>(args))...);
 }
 #ifdef __CUDACC__
+// The cluster's barrier in two halves: a CTA's shared memory may be written from others once all have arrived.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 // All threads of all CTAs of the cluster; what they wrote before is seen after.
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// The address in CTA `rank`'s shared memory of what lies at `at` in this CTA's, and stores there.
+__device__ __forceinline__ uint32_t smem_of_cta(uint32_t at, unsigned rank) {
+  uint32_t there;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(rank));
+  return there;
+}
+__device__ __forceinline__ void store4_to_cta(uint32_t there, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(there), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ void store2_to_cta(uint32_t there, float a, float b) {
+  asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(a), "f"(b) : "memory");
+}
 // Four floats of CTA `rank`'s shared memory, at the place that `p` has in this CTA's.
 __device__ __forceinline__ float4 load_of_cta(const float4* p, unsigned rank) {
-  uint32_t at;
+  const uint32_t at = smem_of_cta(uint32_t(__cvta_generic_to_shared(p)), rank);
   float4 v;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(uint32_t(__cvta_generic_to_shared(p))), "r"(rank));
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
   return v;
 }

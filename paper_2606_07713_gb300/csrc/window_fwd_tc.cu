@@ -80,12 +80,14 @@ struct Cfg {
   static constexpr int kNumBars = 2 * kStages + 17;
   static constexpr int kOffMisc = kOffBar + kNumBars * 8;
   static constexpr int kOffItems = (kOffMisc + 12 + 15) / 16 * 16;   // two items, then scan[12] and the share's beginning
-  static constexpr int kSmemBytes = kOffItems + 2 * 32 + 15 * 8 + 1024;
+  static constexpr int kOffSums = (kOffItems + 2 * 32 + 15 * 8 + 15) / 16 * 16;   // m and l of a row, for the cluster (QT = 1)
+  static constexpr int kSmemBytes = kOffSums + (QT == 1 ? kBM * 8 : 0) + 1024;
   static constexpr int kEarlyChunks = DV == 64 ? 2 : 4;   // of 32 tokens, exponentials before the wait for P's buffer
   static constexpr uint32_t kTmemCols = 512;
   static constexpr uint32_t kTmemS0 = 0, kTmemS1 = kSharedS ? 0 : 128;
   static constexpr uint32_t kTmemP0 = kSharedS ? 128 : 256, kTmemP1 = kSharedS ? 192 : 320;
   static constexpr uint32_t kTmemO0 = kSharedS ? 256 : 384, kTmemO1 = kTmemO0 + (QT == 2 ? DV : 0);
+  static_assert(QT == 2 || (2 * kStageBytes >= kBM * DV * 4 && kStages >= 6), "parts of a cluster's rows beside two tiles");
   static_assert(kTmemO1 + DV <= kTmemCols, "TMEM budget");
   static_assert(kSmemBytes <= 232448, "shared memory budget");
 };
@@ -99,6 +101,7 @@ struct Params {
   int n_tiles;           // work items of a key head
   int n_items;
   int box;               // tokens of a TMA copy
+  int cluster;           // CTAs for each work item, joined in the same launch; 0: equal shares of all items
   win::Mask mask;
   float c_log2;          // scale log2 e, >= 0
   uint64_t wait_limit_ns;
@@ -245,11 +248,14 @@ __device__ __noinline__ void exact_row(const __nv_bfloat16* q, __nv_bfloat16* o,
   for (int e = 0; e < NV; ++e) o[lane * NV + e] = __float2bfloat16(acc[e] * inv);
 }
 
-// Zeros in a row of a values' tile that has arrived, or false.  (A function of its own: an item's last tile only.)
+// Zeros in rows `row`, row + step, ... of a values' tile that has arrived, from row `gone` on; false if it has not.  (A
+// function of its own: an item's last tile only.)
 template <int DV>
-__device__ __noinline__ bool zero_row(uint8_t* tile, int row, bool mine, uint32_t full, uint32_t parity, const WaitCtl& wc) {
+__device__ __noinline__ bool zero_rows(uint8_t* tile, int row, int step, int gone, uint32_t full, uint32_t parity,
+                                       const WaitCtl& wc) {
   const bool ok = wait_bounded(full, parity, wc);
-  if (mine) {
+  for (; row < kBN; row += step) {
+    if (row < gone) continue;
 #pragma unroll
     for (int q = 0; q < DV / 64; ++q)
 #pragma unroll
@@ -289,6 +295,75 @@ __device__ __noinline__ void whole_rows_again(const __nv_bfloat16* Q, __nv_bfloa
       }
     }
     before = end;
+  }
+}
+
+// Of the four rows that a warp's groups of eight lanes hold, those with a member that is `bad`, again.
+template <int DK, int DV>
+__device__ __forceinline__ void rows_again(const __nv_bfloat16* Q, __nv_bfloat16* O, const Params& p, const Where& w, bool bad,
+                                           int hq, int i) {
+  uint32_t again = __ballot_sync(0xffffffffu, bad);
+  while (again != 0) {
+    const int from = __ffs(again) - 1;
+    again &= ~(0xffu << (from & ~7));
+    const int h = __shfl_sync(0xffffffffu, hq, from), n = __shfl_sync(0xffffffffu, i, from);
+    exact_row<DK, DV>(Q + int64_t(w.b) * p.q_sb + int64_t(h) * p.q_sh + int64_t(n) * p.q_sn,
+                      O + int64_t(w.b) * p.o_sb + int64_t(h) * p.o_sh + int64_t(n) * p.o_sn, p, w.b, w.h, n);
+  }
+}
+
+// A cluster's item: CTA (r / 4) % size joins row r.  Every CTA leaves its part of the row there, in the last two stages of the
+// ring, which an item of two tiles does not use: [CTA][row of the owner][DV], and m and l.  (Parts fetched by the owner instead
+// took 3 us more: two round trips and a second barrier.)
+struct Owner {
+  int rank, row;
+};
+__device__ __forceinline__ Owner owner_of(int r, int size) { return Owner{(r >> 2) % size, (r >> 2) / size * 4 + (r & 3)}; }
+
+template <int DK, int DV>
+__device__ __noinline__ void cluster_rows(const __nv_bfloat16* Q, __nv_bfloat16* O, float* lse, const Params& p, const float* sum,
+                                          const float2* stat) {
+  // eight lanes a row
+  constexpr int kQuads = DV / 32;
+  const int lane = threadIdx.x & 31, sub = lane & 7, rows = kBM / p.cluster;
+  const Where w = where_of<1>(p, int(blockIdx.x));
+  for (int base = 0; base < rows; base += 16) {
+    const int at = base + int(threadIdx.x >> 3), r = ((at >> 2) * p.cluster + int(blockIdx.y)) * 4 + (at & 3);
+    const int pos = int(unsigned(r) / unsigned(p.GC)), g = w.chunk * p.GC + r - pos * p.GC, i = w.i0 + pos, hq = w.h * p.G + g;
+    const bool live = at < rows && pos < p.PT && i <= w.i1 && g < p.G;
+    if (!__any_sync(0xffffffffu, live)) continue;
+    float M = -INFINITY, L = 0.f;
+    float4 x[kQuads];
+#pragma unroll
+    for (int q = 0; q < kQuads; ++q) x[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (live) {
+      for (int k = 0; k < p.cluster; ++k) M = fmaxf(M, stat[k * rows + at].x);
+#pragma unroll 2
+      for (int k = 0; k < p.cluster; ++k) {
+        const float2 ml = stat[k * rows + at];
+        if (ml.x == -INFINITY) continue;   // its tiles held nothing that the row sees, or it had none
+        const float f = ex2_approx(ml.x - M);
+        L += f * ml.y;
+#pragma unroll
+        for (int q = 0; q < kQuads; ++q) {
+          const float4 v = *reinterpret_cast<const float4*>(sum + (k * rows + at) * DV + (sub + 8 * q) * 4);
+          x[q].x += f * v.x, x[q].y += f * v.y, x[q].z += f * v.z, x[q].w += f * v.w;
+        }
+      }
+    }
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+    __nv_bfloat16* o = O + int64_t(w.b) * p.o_sb + int64_t(hq) * p.o_sh + int64_t(i) * p.o_sn;
+    bool bad = false;
+#pragma unroll
+    for (int q = 0; q < kQuads; ++q) {
+      x[q].x *= inv, x[q].y *= inv, x[q].z *= inv, x[q].w *= inv;
+      bad |= not_finite(x[q].x) || not_finite(x[q].y) || not_finite(x[q].z) || not_finite(x[q].w);
+      if (live)
+        *reinterpret_cast<uint2*>(o + (sub + 8 * q) * 4) = make_uint2(pack_bf16x2(x[q].x, x[q].y), pack_bf16x2(x[q].z, x[q].w));
+    }
+    if (lse != nullptr && live && sub == 0)
+      lse[(int64_t(w.b) * p.Hk * p.G + hq) * p.N + i] = L == 0.f ? -INFINITY : (M + lg2_approx(L)) * kLn2;
+    rows_again<DK, DV>(Q, O, p, w, bad && live, hq, i);
   }
 }
 
@@ -347,6 +422,11 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     *any_odd = 0;
     fence_barrier_init();
   }
+  if (warp == C::kLoadWarp && lane == 0) {
+    tma_prefetch_desc(&tmQ);
+    tma_prefetch_desc(&tmK);
+    tma_prefetch_desc(&tmV);
+  }
   if (warp == C::kMmaWarp0) {
     tmem_alloc(smem_u32(tmem_slot), C::kTmemCols);
     tmem_relinquish();
@@ -357,50 +437,66 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     fence_proxy_async_smem();
   }
   wait_for_previous();
-  // this CTA's share of all units, and the item in which it begins: the sum of all units, then their running sum
-  // (the same pass where there is an item for each thread at most)
-  auto block_scan = [&](int64_t mine, int64_t* all) {
-    int64_t incl = mine;
+  int64_t total = 1, first_unit = 0, stop = 0;
+  if (p.cluster != 0) {
+    if (warp == C::kWalkWarp && lane == 0) {   // one item, of which the cluster's CTAs take equal parts
+      const Where w = where_of<QT>(p, int(blockIdx.x));
+      const int len = length_of(p, w.b, blockIdx.y == 0);
+      const win::Tiles list = win::tiles_of(p.mask, len, p.N, w.i0, w.i1, kBN);
+      const int units = list.n < 1 ? 1 : list.n;
+      volatile Item& x = items[0];
+      x.u0 = units * int(blockIdx.y) / p.cluster, x.u1 = units * (int(blockIdx.y) + 1) / p.cluster;
+      x.item = x.u0 < x.u1 ? int(blockIdx.x) : -1;
+      x.units = units, x.first = list.first, x.from = list.from, x.len = len;
+    }
+  } else {
+    // this CTA's share of all units, and the item in which it begins: the sum of all units, then their running sum
+    // (the same pass where there is an item for each thread at most)
+    auto block_scan = [&](int64_t mine, int64_t* all) {
+      int64_t incl = mine;
 #pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const int64_t o = __shfl_up_sync(0xffffffffu, incl, d);
-      if (lane >= d) incl += o;
-    }
-    __syncthreads();
-    if (lane == 31) scan[warp] = incl;
-    __syncthreads();
-    *all = 0;
+      for (int d = 1; d < 32; d <<= 1) {
+        const int64_t o = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += o;
+      }
+      __syncthreads();
+      if (lane == 31) scan[warp] = incl;
+      __syncthreads();
+      *all = 0;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      if (w < warp) incl += scan[w];
-      *all += scan[w];
+      for (int w = 0; w < kWarps; ++w) {
+        if (w < warp) incl += scan[w];
+        *all += scan[w];
+      }
+      return incl;
+    };
+    const bool one_pass = p.n_items <= C::kThreads;
+    int64_t mine = 0;
+    for (int i = threadIdx.x; i < p.n_items; i += C::kThreads) mine += units_of<QT>(p, i, true) + kItemUnits;
+    int64_t incl = block_scan(mine, &total);
+    const Shares shares(total, gridDim.x);
+    first_unit = blockIdx.x < shares.n ? shares.start(blockIdx.x) : total;
+    stop = blockIdx.x < shares.n ? shares.start(blockIdx.x + 1) : total;
+    int64_t done = 0;
+    for (int base = 0; first_unit < stop; base += C::kThreads) {
+      const int i = base + threadIdx.x;
+      if (!one_pass) {
+        int64_t all;
+        mine = i < p.n_items ? units_of<QT>(p, i, false) + kItemUnits : 0;
+        incl = block_scan(mine, &all) + done;
+        done += all;
+      }
+      if (first_unit >= incl - mine && first_unit < incl) *found = Begin{i, incl - mine, total};
+      if (one_pass || first_unit < done) break;
     }
-    return incl;
-  };
-  const bool one_pass = p.n_items <= C::kThreads;
-  int64_t mine = 0;
-  for (int i = threadIdx.x; i < p.n_items; i += C::kThreads) mine += units_of<QT>(p, i, true) + kItemUnits;
-  int64_t total, incl = block_scan(mine, &total);
-  const Shares shares(total, gridDim.x);
-  const int64_t first_unit = blockIdx.x < shares.n ? shares.start(blockIdx.x) : total;
-  const int64_t stop = blockIdx.x < shares.n ? shares.start(blockIdx.x + 1) : total;
-  int64_t done = 0;
-  for (int base = 0; first_unit < stop; base += C::kThreads) {
-    const int i = base + threadIdx.x;
-    if (!one_pass) {
-      int64_t all;
-      mine = i < p.n_items ? units_of<QT>(p, i, false) + kItemUnits : 0;
-      incl = block_scan(mine, &all) + done;
-      done += all;
-    }
-    if (first_unit >= incl - mine && first_unit < incl) *found = Begin{i, incl - mine, total};
-    if (one_pass || first_unit < done) break;
+    if (threadIdx.x == 0) cuts[blockIdx.x].pieces = 0;
   }
-  if (threadIdx.x == 0) cuts[blockIdx.x].pieces = 0;
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = *tmem_slot;
+  const bool clustered = QT == 1 && p.cluster != 0;
+  if (clustered) cluster_arrive();   // every thread waits for it once: the softmax threads before they write to other CTAs
   // A whole warp's wait: on expiry all its lanes leave together.
   auto wait_warp = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_bounded(bar, parity, wc)) != 0; };
   // Item number i of the share, as every role sees it: valid until the role's release.
@@ -414,11 +510,6 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     if constexpr (QT == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRegsCtrl));
     if (warp == C::kLoadWarp) {
       // ------------------------------------------------------------ TMA producer: a copy a lane
-      if (lane == 0) {
-        tma_prefetch_desc(&tmQ);
-        tma_prefetch_desc(&tmK);
-        tma_prefetch_desc(&tmV);
-      }
       const int boxes = kBN / p.box;
       int slot = 0;
       uint32_t phase = 0, issued = 0, issued_phase = 0, q_issued = 0;
@@ -601,13 +692,18 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       }
     } else if (warp == C::kWalkWarp && lane == 0) {
       // ------------------------------------------------------------ the items of the share
+      const Shares shares(total, gridDim.x);
       int64_t at = first_unit, before = 0;
       int item = 0;
-      if (at < stop) {
+      if (p.cluster != 0) {
+        mbar_arrive(item_full(0));
+        items[1].item = -1;
+        mbar_arrive(item_full(1));
+      } else if (at < stop) {
         item = int(found->item);
         before = found->unit;
       }
-      for (uint32_t seg = 0;; ++seg) {
+      for (uint32_t seg = 0; p.cluster == 0; ++seg) {
         int units = 0, u0 = 0, u1 = 0, which = -1, len = 0;
         win::Tiles list{};
         while (at < stop && u0 == u1) {   // (nothing of an item's tiles: the next CTA begins it)
@@ -647,6 +743,8 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     const int row_pos = int(unsigned(row) / unsigned(p.GC)), row_head = row - row_pos * p.GC;
     bool ok = true;
     uint32_t t = 0, ring = 0;   // tiles and stages of the ring before this item
+    if (clustered) cluster_wait();
+    [[maybe_unused]] float cluster_m = -INFINITY, cluster_l = 0.f;   // the row's, for the CTA that joins it (if this one has no tiles)
     for (uint32_t seg = 0;; ++seg) {
       const Item x = get_item(seg, ok);
       if (x.item < 0) break;
@@ -671,8 +769,17 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
           low = win::row_low(p.mask, x.len, p.N, w.i);
         }
       }
-      // past the sequence's end a page holds whatever it held: the first such token, of a cache
+      // past the sequence's end a page holds whatever it held: the first such token, of a cache.  Its rows of values are
+      // zeroed by the warps that have no rows of queries, or else by all, each its own rows.
       const int gone = p.kv.table != nullptr ? x.len : 0x7fffffff;
+      int zero_row = row, zero_step = kBN;
+      if (QT == 1) {
+        const int warps = (p.N * p.GC + 31) / 32;   // those with rows
+        if (warps < 4) {
+          zero_row = row - 32 * warps;
+          zero_step = live_warp ? 0 : kBN - 32 * warps;
+        }
+      }
       float m = -INFINITY, l = 0.f;
       for (int n = x.u0; ok && n < x.u1; ++n, ++t) {
         const int n0 = list.at(n) * kBN;
@@ -680,10 +787,10 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         // as it is.
         ok = wait_bounded(s_full(j), t & 1u, wc);
         tc_fence_after_sync();
-        if (gone - n0 < kBN) {   // the item's last tile: zeros in the place of the thread's row of values
+        if (gone - n0 < kBN && zero_step > 0) {   // the item's last tile
           const int k = n - x.u0, at = int(ring) + (n + 1 < x.u1 ? 2 * k + 2 : 2 * k + 1);
-          ok = zero_row<DV>(smem + C::kOffKV + at % C::kStages * C::kStageBytes, row, n0 + row >= gone, full_bar(at % C::kStages),
-                            at / C::kStages & 1, wc) && ok;
+          ok = zero_rows<DV>(smem + C::kOffKV + at % C::kStages * C::kStageBytes, zero_row, zero_step, gone - n0,
+                             full_bar(at % C::kStages), at / C::kStages & 1, wc) && ok;
         }
         if (!live_warp) {   // rows that are not there: in step with the others, and no more
           tc_fence_before_sync();
@@ -768,7 +875,23 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       if (live_warp) {
         const Place w = place(xi.item);
         bool bad = false;
-        if (!whole) {
+        if (clustered) {   // the row's sums, to the CTA that joins it
+          const Owner own = owner_of(row, p.cluster);
+          const uint32_t sum = smem_of_cta(sKV + (C::kStages - 2) * C::kStageBytes +
+                                           ((int(blockIdx.y) * (kBM / p.cluster) + own.row) * DV) * 4, own.rank);
+#pragma unroll
+          for (int d = 0; d < DV; d += 16) {
+            uint32_t o[16];
+            tmem_ld_32x32b_x16(tO + d, o);
+            tmem_wait_ld();
+            reg_anchor_x16(o);
+            if (w.live) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) store4_to_cta(sum + (d + 4 * e) * 4, o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+            }
+          }
+          cluster_m = m, cluster_l = l;
+        } else if (!whole) {
           const int64_t at = (int64_t(blockIdx.x) * 2 + first_piece) * C::kRows + j * kBM + row;
 #pragma unroll
           for (int d = 0; d < DV; d += 16) {
@@ -818,6 +941,11 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       __syncwarp();
       if (lane == 0) mbar_arrive(item_empty(seg & 1));
     }
+    if (clustered) {
+      const Owner own = owner_of(row, p.cluster);
+      store2_to_cta(smem_of_cta(smem_u32(smem + C::kOffSums) + (int(blockIdx.y) * (kBM / p.cluster) + own.row) * 8, own.rank),
+                    cluster_m, cluster_l);
+    }
   }
 
   // Teardown: the tensor core is quiet before TMEM is freed, on the abort path too.  Only the lane of the role
@@ -828,6 +956,17 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
   if (warp == C::kMmaWarp0) {
     tc_fence_after_sync();
     tmem_dealloc(tmem, C::kTmemCols);
+  }
+  if constexpr (QT == 1) {
+    if (clustered) {
+      if (warp >= C::kMmaWarp0) cluster_wait();
+      __syncwarp();
+      cluster_sync();
+      if (warp < C::kMmaWarp0)
+        cluster_rows<DK, DV>(Q, O, lse, p, reinterpret_cast<const float*>(smem + C::kOffKV + (C::kStages - 2) * C::kStageBytes),
+                             reinterpret_cast<const float2*>(smem + C::kOffSums));
+      return;
+    }
   }
   if (*any_odd != 0 && warp < C::kMmaWarp0) whole_rows_again<DK, DV, QT>(Q, O, p, found);
 }
@@ -905,19 +1044,15 @@ window_tc_join_kernel(const __nv_bfloat16* Q, __nv_bfloat16* O, float* lse, cons
   }
   if (lse != nullptr && live && sub == 0)
     lse[(int64_t(w.b) * p.Hk * p.G + hq) * p.N + i] = L == 0.f ? -INFINITY : (M + lg2_approx(L)) * kLn2;
-  uint32_t again = __ballot_sync(0xffffffffu, bad && live);
-  for (; again != 0; again &= ~(0xffu << (__ffs(again) - 1 & ~7))) {
-    const int from = __ffs(again) - 1;
-    const int h_ = __shfl_sync(0xffffffffu, hq, from), i_ = __shfl_sync(0xffffffffu, i, from);
-    exact_row<DK, DV>(Q + int64_t(w.b) * p.q_sb + int64_t(h_) * p.q_sh + int64_t(i_) * p.q_sn,
-                      O + int64_t(w.b) * p.o_sb + int64_t(h_) * p.o_sh + int64_t(i_) * p.o_sn, p, w.b, w.h, i_);
-  }
+  rows_again<DK, DV>(Q, O, p, w, bad && live, hq, i);
 }
 
 // ------------------------------------------------------------------------------------------------
 // Host side
 // ------------------------------------------------------------------------------------------------
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+constexpr int64_t kClusters16 = 7, kClusters8 = 14;   // clusters of this many CTAs at a time, one less a kind than there is room for
 
 // How the rows of a key head are divided.
 struct Plan {
@@ -1007,6 +1142,30 @@ int launch(const WindowArgs& a, const Plan& plan, int sms, char* msg, size_t msg
   // tiles of tokens, if every sequence is as long as max_len and no window hides any
   const int64_t most_tiles = (a.max_len + kBN - 1) / kBN, most = plan.n_items * most_tiles;
   const unsigned ctas = unsigned(most < sms ? most : sms);
+  // Few items of few tiles: a cluster for each, joined in the same launch, where that is no more than two tiles a CTA.  A
+  // processing cluster of the GPU has room for two clusters of 8 CTAs, or one of 16.
+  if constexpr (QT == 1) {
+    int64_t tiles = most_tiles;
+    if (a.window != win::kNoWindow) {
+      const int64_t seen = (int64_t(a.window) + plan.PT + kBN - 1) / kBN + 1 + (int64_t(a.sinks) + kBN - 1) / kBN;
+      if (seen < tiles) tiles = seen;
+    }
+    const int64_t size = plan.n_items <= kClusters16 ? 16 : 8;
+    if (tiles <= 2 * size && plan.n_items <= (size == 16 ? kClusters16 : kClusters8)) {
+      p.cluster = 2;
+      while (p.cluster < size && p.cluster < tiles) p.cluster *= 2;
+      if (p.cluster > 8) e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kern), cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+      if (e == cudaSuccess)
+        e = launch_clusters(kern, dim3(unsigned(plan.n_items), unsigned(p.cluster)), unsigned(p.cluster), dim3(C::kThreads),
+                            C::kSmemBytes, a.stream, mq, mk, mv, static_cast<const __nv_bfloat16*>(a.q.p),
+                            static_cast<__nv_bfloat16*>(a.o.p), a.lse, part_o, part_ml, cuts, p);
+      if (e != cudaSuccess) {
+        snprintf(msg, msglen, "attention with a window: %s", cudaGetErrorString(e));
+        return 5;
+      }
+      return 0;
+    }
+  }
   // rows of an item that may be there
   const int64_t positions = a.N < plan.PT ? a.N : plan.PT, live = QT == 2 ? C::kRows : positions * plan.GC;
   e = launch_overlapped(kern, dim3(ctas), dim3(C::kThreads), C::kSmemBytes, a.stream, mq, mk, mv,
