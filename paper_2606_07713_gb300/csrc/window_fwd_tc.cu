@@ -55,7 +55,8 @@ using namespace tc;
 
 constexpr int kBM = 128;              // rows of a row tile (= TMEM lanes)
 constexpr int kBN = 128;              // tokens of a tile
-constexpr int kItemUnits = 4;         // what an item costs besides its tiles, in tiles
+// What an item costs besides its tiles, in tiles (48 sequences of one query with 0, 1, 2, 4: 204, 195, 189, 192 us).
+__host__ __device__ constexpr int item_units(int QT) { return QT == 2 ? 4 : 2; }
 constexpr float kRescaleLog2 = 8.f;   // the running maximum may lag by this: weights up to 2^8
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -279,9 +280,9 @@ __device__ __noinline__ void whole_rows_again(const __nv_bfloat16* Q, __nv_bfloa
   const int64_t first_unit = shares.start(blockIdx.x), stop = shares.start(blockIdx.x + 1);
   int64_t before = begin->unit;
   for (int item = int(begin->item); before < stop; ++item) {
-    const int64_t end = before + units_of<QT>(p, item, false) + kItemUnits;
+    const int64_t end = before + units_of<QT>(p, item, false) + item_units(QT);
     // its tiles, which come after its first units, are all in this share
-    if (before + kItemUnits >= first_unit && end <= stop) {
+    if (before + item_units(QT) >= first_unit && end <= stop) {
       const Where w = where_of<QT>(p, item);
       for (int r = warp; r < kBM * QT; r += 4 * QT) {
         const int tile = r / kBM, in_tile = r - tile * kBM, row_pos = in_tile / p.GC;
@@ -472,7 +473,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     };
     const bool one_pass = p.n_items <= C::kThreads;
     int64_t mine = 0;
-    for (int i = threadIdx.x; i < p.n_items; i += C::kThreads) mine += units_of<QT>(p, i, true) + kItemUnits;
+    for (int i = threadIdx.x; i < p.n_items; i += C::kThreads) mine += units_of<QT>(p, i, true) + item_units(QT);
     int64_t incl = block_scan(mine, &total);
     const Shares shares(total, gridDim.x);
     first_unit = blockIdx.x < shares.n ? shares.start(blockIdx.x) : total;
@@ -482,7 +483,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       const int i = base + threadIdx.x;
       if (!one_pass) {
         int64_t all;
-        mine = i < p.n_items ? units_of<QT>(p, i, false) + kItemUnits : 0;
+        mine = i < p.n_items ? units_of<QT>(p, i, false) + item_units(QT) : 0;
         incl = block_scan(mine, &all) + done;
         done += all;
       }
@@ -499,9 +500,11 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
   if (clustered) cluster_arrive();   // every thread waits for it once: the softmax threads before they write to other CTAs
   // A whole warp's wait: on expiry all its lanes leave together.
   auto wait_warp = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_bounded(bar, parity, wc)) != 0; };
-  // Item number i of the share, as every role sees it: valid until the role's release.
+  // Item number i of the share, as every role sees it: valid until the role's release.  The wait lasts as long as the item
+  // before the last one takes.
+  const WaitCtl wi{abort_flag, p.wait_limit_ns + uint64_t(p.max_len / kBN) * 10000u, 0u, &g_moa_window_tc_status};
   auto get_item = [&](uint32_t i, bool& ok) {
-    ok = ok && wait_warp(item_full(i & 1), i >> 1 & 1u);
+    ok = ok && __all_sync(0xffffffffu, wait_bounded(item_full(i & 1), i >> 1 & 1u, wi)) != 0;
     const volatile Item& x = items[i & 1];
     return ok ? Item{x.item, x.u0, x.u1, x.units, x.first, x.from, x.len} : Item{-1, 0, 0, 0, 0, 0, 0};
   };
@@ -649,7 +652,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         };
         bool ok = true;
         for (uint32_t seg = 0; ok; ++seg) {
-          ok = wait_bounded(item_full(seg & 1), seg >> 1 & 1u, wc);
+          ok = wait_bounded(item_full(seg & 1), seg >> 1 & 1u, wi);
           const volatile Item& xi = items[seg & 1];
           const int item = xi.item, n_kt = xi.u1 - xi.u0;
           if (!ok || item < 0) break;
@@ -711,8 +714,8 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
           len = length_of(p, w.b, false);
           list = win::tiles_of(p.mask, len, p.N, w.i0, w.i1, kBN);
           units = list.n < 1 ? 1 : list.n;
-          const int64_t end = before + units + kItemUnits, upto = end < stop ? end : stop;
-          u0 = max(0, int(at - before) - kItemUnits), u1 = max(0, int(upto - before) - kItemUnits);
+          const int64_t end = before + units + item_units(QT), upto = end < stop ? end : stop;
+          u0 = max(0, int(at - before) - item_units(QT)), u1 = max(0, int(upto - before) - item_units(QT));
           if (u0 < u1) which = item;
           if (u0 == 0 && u1 > 0 && u1 < units) {   // begun here, ended by a later CTA
             uint32_t c = blockIdx.x;
@@ -723,7 +726,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
           before = end;
           ++item;
         }
-        if (seg >= 2 && !wait_bounded(item_empty(seg & 1), ((seg >> 1) - 1) & 1u, wc)) break;
+        if (seg >= 2 && !wait_bounded(item_empty(seg & 1), ((seg >> 1) - 1) & 1u, wi)) break;
         volatile Item& x = items[seg & 1];
         x.item = which, x.u0 = u0, x.u1 = u1, x.units = units;
         x.first = list.first, x.from = list.from, x.len = len;

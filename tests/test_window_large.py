@@ -1,0 +1,257 @@
+"""Attention with a window, its gradients and the 16- and 32-bit cache at sizes where work is divided: many
+work items, items cut between CTAs, clusters, long contexts, places past 32 bits.  The references are 64-bit
+sums in torch operations on the GPU; the bounds are those of window_reference.py, with the magnitudes that
+they are made of computed beside the outputs."""
+import math
+
+import pytest
+
+import paper_2606_07713_gb300 as pkg
+from paper_2606_07713_gb300 import _lib
+from window_reference import HALF, SUMS, WEIGHT
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+TORCH = {"bf16": torch.bfloat16, "fp32": torch.float32}
+
+
+def rand(g, *shape, dtype, scale=1.0):
+    return (torch.randn(*shape, generator=g, device="cuda") * scale).to(TORCH[dtype])
+
+
+def seen(N, T, length, window, sinks, causal=True):
+    p = length - N + torch.arange(N, device="cuda")[:, None]
+    j = torch.arange(T, device="cuda")[None]
+    see = (j <= p) if causal else (j < length) & (p == p)
+    return see & ((j > p - window) | (j < sinks)) if window else see
+
+
+def reference(q, k, v, see, dtype):
+    """(o, its bound, lse and its bound) of one head in 64 bits: q [N, d], k [T, d], v [T, dv]."""
+    q, k, v = q.double(), k.double(), v.double()
+    scale, u = q.shape[1] ** -0.5, HALF[dtype]
+    s = (q @ k.T * scale).masked_fill(~see, -math.inf)
+    size = (q.abs() @ k.abs().T * scale).masked_fill(~see, 0).amax(1)
+    lse = torch.logsumexp(s, 1)
+    p = torch.nan_to_num(torch.softmax(s, 1), nan=0.0)
+    o, av = p @ v, p @ v.abs()
+    e = (q.shape[1] + 8) * 2.0 ** -24 * size[:, None]
+    bound = (2 * e + WEIGHT + SUMS + (u if dtype == "bf16" else 0.0)) * av * 1.02 + u * o.abs() * 1.02 + 1e-30
+    return o, bound, lse, e[:, 0] + 2.0 ** -17 + 2.0 ** -20 * lse.abs()
+
+
+def check(o, lse, q, k, v, see, dtype):
+    ro, bound, rl, slack = reference(q, k, v, see, dtype)
+    assert bool(((o.double() - ro).abs() <= bound).all())
+    if lse is not None:
+        live = see.any(1)
+        assert bool((torch.isfinite(lse) == live).all())
+        assert bool(((lse.double() - rl).abs() <= slack)[live].all())
+
+
+@pytest.mark.parametrize("dtype,B,Hq,Hk,N,M,dk,dv,window,sinks", [
+    ("bf16", 1, 8, 2, 4000, 4000, 128, 128, 700, 4),        # more items than CTAs, cut between them
+    ("bf16", 3, 16, 16, 1025, 1025, 64, 64, 0, 0),
+    ("bf16", 1, 3, 1, 6000, 6100, 64, 128, 0, 0),
+    ("bf16", 2, 4, 4, 3001, 3001, 128, 64, 50, 200),
+    ("bf16", 1, 2, 2, 40, 9000, 128, 128, 0, 0),            # few rows, many pieces
+    ("fp32", 2, 4, 2, 1500, 1500, 64, 64, 300, 3),
+    ("fp32", 1, 2, 1, 3, 5000, 128, 128, 0, 0),
+])
+def test_window(dtype, B, Hq, Hk, N, M, dk, dv, window, sinks):
+    g = torch.Generator(device="cuda").manual_seed(N + M)
+    q, k, v = (rand(g, B, Hq, N, dk, dtype=dtype, scale=1.5), rand(g, B, Hk, M, dk, dtype=dtype), rand(g, B, Hk, M, dv, dtype=dtype))
+    o, lse = pkg.window_attn_lse(q, k, v, window=window or None, sinks=sinks)
+    assert pkg.get_device_status() == _lib.MOA_OK
+    see = seen(N, M, M, window, sinks)
+    for b in range(B):
+        for h in (0, Hq // 2, Hq - 1):
+            check(o[b, h], lse[b, h], q[b, h], k[b, h // (Hq // Hk)], v[b, h // (Hq // Hk)], see, dtype)
+
+
+@pytest.mark.parametrize("dtype,B,Hq,Hk,N,M,dk,dv,window,sinks", [
+    ("bf16", 1, 8, 2, 3000, 3000, 128, 128, 400, 4),        # sinks in pieces
+    ("bf16", 1, 2, 1, 2500, 2500, 64, 64, 0, 0),            # every token tile in pieces
+    ("bf16", 4, 12, 12, 1100, 1100, 64, 64, 0, 0),          # more items than CTAs
+    ("bf16", 1, 6, 2, 1500, 2000, 128, 64, 100, 300),       # sinks over several tiles
+    ("bf16", 1, 4, 4, 700, 700, 64, 128, 9, 700),           # every token a sink
+    ("fp32", 1, 4, 2, 1400, 1400, 64, 64, 200, 3),
+    ("fp32", 1, 1, 1, 1200, 1200, 128, 128, 0, 0),
+])
+def test_gradients(dtype, B, Hq, Hk, N, M, dk, dv, window, sinks):
+    g = torch.Generator(device="cuda").manual_seed(N + M + 1)
+    q, k, v = (rand(g, B, Hq, N, dk, dtype=dtype, scale=1.5), rand(g, B, Hk, M, dk, dtype=dtype), rand(g, B, Hk, M, dv, dtype=dtype))
+    do = rand(g, B, Hq, N, dv, dtype=dtype, scale=0.1)
+    o, lse = pkg.window_attn_lse(q, k, v, window=window or None, sinks=sinks)
+    got = pkg.window_attn_bwd(q, k, v, o, lse, do, window=window or None, sinks=sinks)
+    assert pkg.get_device_status() == _lib.MOA_OK
+    see, scale, G = seen(N, M, M, window, sinks), dk ** -0.5, Hq // Hk
+    u = HALF[dtype]
+    ub = u if dtype == "bf16" else 0.0
+    for b in range(B):
+        for hk in {0, Hk - 1}:
+            dk_, dv_ = torch.zeros(M, dk, dtype=torch.float64, device="cuda"), torch.zeros(M, dv, dtype=torch.float64, device="cuda")
+            ek, ev = torch.zeros_like(dk_), torch.zeros_like(dv_)
+            kk, vv = k[b, hk].double(), v[b, hk].double()
+            for h in range(hk * G, hk * G + G):
+                qq, gg, oo, ll = q[b, h].double(), do[b, h].double(), o[b, h].double(), lse[b, h].double()
+                base = torch.where(torch.isfinite(ll), ll, 0.0)[:, None]
+                p = torch.exp((qq @ kk.T * scale - base).masked_fill(~see, -math.inf))
+                size = (qq.abs() @ kk.abs().T * scale).masked_fill(~see, 0).amax(1, keepdim=True)
+                w = 2 * (dk + 8) * 2.0 ** -24 * size + WEIGHT + 2.0 ** -22 * base.abs()
+                ds = p * (gg @ vv.T - (gg * oo).sum(1, keepdim=True))
+                dot = (dv + 8) * 2.0 ** -24 * (gg.abs() @ vv.abs().T + (gg * oo).abs().sum(1, keepdim=True))
+                eds = (w + ub + SUMS) * ds.abs() + p * dot * 1.02
+                want = scale * ds @ kk
+                bound = scale * (eds @ kk.abs()) * 1.02 + u * want.abs() * 1.02 + 1e-30
+                assert bool(((got[0][b, h].double() - want).abs() <= bound).all()), "dq"
+                dk_ += scale * ds.T @ qq
+                ek += scale * eds.T @ qq.abs()
+                dv_ += p.T @ gg
+                ev += ((w + ub + SUMS) * p).T @ gg.abs()
+            assert bool(((got[1][b, hk].double() - dk_).abs() <= 1.02 * (ek + u * dk_.abs()) + 1e-30).all()), "dk"
+            assert bool(((got[2][b, hk].double() - dv_).abs() <= 1.02 * (ev + u * dv_.abs()) + 1e-30).all()), "dv"
+
+
+def cache(g, lens, Hk, page, dk, dv, dtype, n_pages=None, first=0):
+    """(pool, table, rows by sequence [Hk, n, dk + dv]); pages from `first` on, in any order; junk past the ends."""
+    per = [-(-n // page) for n in lens]
+    order = (torch.randperm(sum(per), generator=g, device="cuda") + first).to(torch.int32)
+    pool = torch.empty(n_pages or sum(per), Hk, page, dk + dv, dtype=TORCH[dtype], device="cuda")
+    table = torch.full((len(lens), max(per) or 1), -1, dtype=torch.int32, device="cuda")
+    rows, at = [], 0
+    for b, n in enumerate(lens):
+        mine = order[at:at + per[b]].long()
+        at += per[b]
+        x = rand(g, Hk, per[b] * page, dk + dv, dtype=dtype)
+        x[:, n:] = float("nan")
+        pool[mine] = x.view(Hk, per[b], page, dk + dv).transpose(0, 1)
+        table[b, :per[b]] = mine.to(torch.int32)
+        rows.append(x[:, :n])
+    return pool, table, rows
+
+
+def check_cache(o, lse, q, rows, lens, dk, window, sinks, causal, dtype):
+    Hq, N = q.shape[1:3]
+    for b, n in enumerate(lens):
+        if n == 0:
+            assert bool((o[b] == 0).all())
+            continue
+        see = seen(N, n, n, window, sinks, causal)
+        for h in {0, Hq - 1}:
+            x = rows[b][h // (Hq // rows[b].shape[0])]
+            check(o[b, h], lse[b, h], q[b, h], x[:, :dk], x[:, dk:], see, dtype)
+
+
+@pytest.mark.parametrize("lens,Hq,Hk,N,dk,dv,page,window,sinks,causal,dtype", [
+    ([20000], 8, 1, 1, 128, 128, 64, 0, 0, True, "bf16"),                    # one sequence on all SMs
+    ([30000, 7, 12345], 4, 2, 3, 64, 64, 16, 0, 0, False, "bf16"),
+    ([900 + 37 * i for i in range(40)] + [0, 1], 16, 8, 1, 128, 64, 32, 0, 0, True, "bf16"),   # more items than CTAs
+    ([5000, 4000], 8, 2, 1, 128, 128, 16, 1024, 4, True, "bf16"),             # clusters
+    ([300, 250, 1], 4, 2, 60, 64, 128, 48, 0, 0, True, "bf16"),               # clusters, many rows
+    ([130], 2, 1, 1, 64, 64, 64, 0, 0, True, "bf16"),
+    ([3000, 2000, 100], 32, 8, 700, 128, 128, 64, 0, 0, True, "bf16"),         # chunks
+    ([9000, 500], 8, 2, 333, 64, 64, 32, 2000, 130, True, "bf16"),
+    ([20000, 3], 4, 1, 1, 128, 128, 64, 0, 0, True, "fp32"),
+    ([3000, 2500], 6, 2, 5, 128, 64, 48, 1000, 4, True, "fp32"),              # clusters of 16
+    ([1200], 4, 2, 300, 64, 64, 16, 0, 0, True, "fp32"),
+])
+def test_cache(lens, Hq, Hk, N, dk, dv, page, window, sinks, causal, dtype):
+    g = torch.Generator(device="cuda").manual_seed(sum(lens))
+    pool, table, rows = cache(g, lens, Hk, page, dk, dv, dtype)
+    q = rand(g, len(lens), Hq, N, dk, dtype=dtype, scale=1.5)
+    ln = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    o, lse = pkg.kv_attn_lse(q, pool, table, ln, max_len=max(lens), window=window or None, sinks=sinks, causal=causal)
+    assert pkg.get_device_status() == _lib.MOA_OK
+    check_cache(o, lse, q, rows, lens, dk, window, sinks, causal, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_a_pool_of_more_than_2_31_elements(dtype):
+    """Rows appended to, and read from, the last pages of a pool of 2.4 * 10^9 elements."""
+    Hk, page, d, n_pages = 8, 128, 128, 9200
+    g = torch.Generator(device="cuda").manual_seed(1)
+    pool = torch.empty(n_pages, Hk, page, 2 * d, dtype=TORCH[dtype], device="cuda")
+    assert pool.numel() > 2 ** 31
+    lens, N = [300, 140], 300
+    table = torch.tensor([[n_pages - 1, n_pages - 3, 8300], [n_pages - 2, 8301, 0]], dtype=torch.int32, device="cuda")
+    k, v = rand(g, 2, Hk, N, d, dtype=dtype), rand(g, 2, Hk, N, d, dtype=dtype)
+    pos = torch.arange(N, dtype=torch.int32, device="cuda").repeat(2, 1)
+    pos[1, 140:] = -1
+    pkg.kv_append(k, v, pool, table, pos)
+    q = rand(g, 2, 16, 2, d, dtype=dtype, scale=1.5)
+    o, lse = pkg.kv_attn_lse(q, pool, table, torch.tensor(lens, dtype=torch.int32, device="cuda"))
+    assert pkg.get_device_status() == _lib.MOA_OK
+    rows = [torch.cat([k[b, :, :n], v[b, :, :n]], -1) for b, n in enumerate(lens)]
+    check_cache(o, lse, q, rows, lens, d, 0, 0, True, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_dense_strides_past_32_bits(dtype):
+    """A sequence's keys and values 2^31 elements apart from the next one's."""
+    N, d, B = 70, 64, 2
+    g = torch.Generator(device="cuda").manual_seed(4)
+    step = 2 ** 31 + 4096
+    big = torch.empty(step + 4 * N * d, dtype=TORCH[dtype], device="cuda")
+    q = rand(g, B, 2, N, d, dtype=dtype)
+    k, v = (big.as_strided((B, 1, N, d), (step, N * d, d, 1), at) for at in (0, 2 * N * d))
+    k.copy_(rand(g, B, 1, N, d, dtype=dtype))
+    v.copy_(rand(g, B, 1, N, d, dtype=dtype))
+    o, lse = pkg.window_attn_lse(q, k, v, window=20, sinks=1)
+    grads = pkg.window_attn_bwd(q, k, v, o, lse, q, window=20, sinks=1)
+    kc, vc = k.contiguous(), v.contiguous()
+    want = pkg.window_attn_lse(q, kc, vc, window=20, sinks=1)
+    assert torch.equal(o, want[0]) and torch.equal(lse, want[1])
+    assert all(torch.equal(a, b) for a, b in zip(grads, pkg.window_attn_bwd(q, kc, vc, o, lse, q, window=20, sinks=1)))
+    assert pkg.get_device_status() == _lib.MOA_OK
+
+
+@pytest.mark.parametrize("N", [1, 2, 50, 400])
+def test_values_that_are_not_numbers_in_whole_and_cut_items(N):
+    """A value that is not finite in each tile, seen and not seen, with items on one CTA, cut, and in clusters: the
+    rows that do not see it are bit for bit what they are without it, or within the bound where they are computed
+    again."""
+    Hq, Hk, d, page, L, window = 8, 4, 64, 32, 5000, 600
+    g = torch.Generator(device="cuda").manual_seed(N)
+    for w in (window, 0):
+        pool, table, rows = cache(g, [L, 900], Hk, page, d, d, "bf16")
+        q = rand(g, 2, Hq, N, d, dtype="bf16")
+        ln = torch.tensor([L, 900], dtype=torch.int32, device="cuda")
+        t = L - N // 2 - 1                                # seen by half of the queries
+        pool[table[0, t // page].long(), 1, t % page, d + 3] = float("inf")
+        o, lse = pkg.kv_attn_lse(q, pool, table, ln, window=w or None)
+        assert pkg.get_device_status() == _lib.MOA_OK
+        see = seen(N, L, L, w, 0)
+        hit = see[:, t]
+        for h in range(Hq):
+            x = rows[0][h // 2]
+            ro, bound, _, _ = reference(q[0, h], x[:, :d], x[:, d:], see, "bf16")
+            ok = (o[0, h].double() - ro).abs() <= bound
+            if h // 2 == 1:
+                assert bool(torch.isinf(o[0, h, hit, 3]).all())
+                ok[hit, 3] = True
+            assert bool(ok.all())
+
+
+def test_two_streams_at_once():
+    """Calls under way at the same time, each with its own outputs and workspaces."""
+    g = torch.Generator(device="cuda").manual_seed(8)
+    sets = []
+    for i in range(2):
+        q, k, v = rand(g, 1, 8, 2000, 64, dtype="bf16"), rand(g, 1, 2, 2000, 64, dtype="bf16"), rand(g, 1, 2, 2000, 64, dtype="bf16")
+        sets.append((q, k, v))
+
+    def both(t, stream=None):
+        o, lse = pkg.window_attn_lse(*t, window=300, sinks=2, stream=stream)
+        return [o, lse, *pkg.window_attn_bwd(*t, o, lse, t[0], window=300, sinks=2, stream=stream)]
+
+    want = [both(t) for t in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    got = [[both(t, s) for t, s in zip(sets, streams)] for _ in range(4)]
+    torch.cuda.synchronize()
+    for r in got:
+        for x, y in zip(r, want):
+            assert all(torch.equal(a, b) for a, b in zip(x, y))
