@@ -44,6 +44,7 @@ struct Params {
   float* nl;      // [B * Hk][N * G] -LSE log2 e, rows of a key head in their order
   float* delta;   // alike
   float* part;    // [piece item][64][DK + DV], null: no pieces
+  float* part_q;  // [dQ tile][piece][64][DK], if dQ's tiles come in pieces
   int Hk, N, G, Nk;
   win::Mask mask;
   float c_log2, scale;
@@ -52,6 +53,7 @@ struct Params {
   int pieces;
   int64_t piece_rows;
   int n_rt;       // tiles of rows
+  int q_pieces;   // pieces of a dQ tile's tokens
 };
 
 template <typename T>
@@ -375,18 +377,21 @@ __device__ __forceinline__ void dq_tile(const Params& p, unsigned index, float* 
   float* sTokens = sG + kRowsQ * (DV + 4);
   float* sS = sTokens + kBuf * S::kTokens;   // [tokens][rows]
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int bh = int(index / unsigned(p.n_rt)), b = bh / p.Hk, h = bh - b * p.Hk;
+  const unsigned tile = index / unsigned(p.q_pieces), piece = index - tile * unsigned(p.q_pieces);
+  const int bh = int(tile / unsigned(p.n_rt)), b = bh / p.Hk, h = bh - b * p.Hk;
   // the last rows, which see the most without a window, come first
-  const int r0 = (p.n_rt - 1 - int(index - unsigned(bh) * unsigned(p.n_rt))) * kRowsQ;
+  const int rt = p.n_rt - 1 - int(tile - unsigned(bh) * unsigned(p.n_rt)), r0 = rt * kRowsQ;
   const int64_t rows = int64_t(p.N) * p.G;
   const int live = int(rows - r0 < kRowsQ ? rows - r0 : kRowsQ);
   const int off = p.Nk - p.N;
   const int i0 = r0 / p.G, i1 = (r0 + live - 1) / p.G;
   // the tokens that they visit, 32 at a time, the sinks and the window's next to each other
   const win::Run run = win::run_of(p.mask, p.Nk, p.N, i0, i1);
-  const int steps = (run.n + kKeysQ - 1) / kKeysQ;
+  const int all = (run.n + kKeysQ - 1) / kKeysQ;
+  const int begin = int(int64_t(all) * piece / p.q_pieces), steps = int(int64_t(all) * (piece + 1) / p.q_pieces);   // this piece's
   fill_rows<T, DK, DV, kRowsQ>(p.q, p.go, sQ, sG, b, h, p.G, r0, int(rows));
-  if (steps > 0) fill_tokens<T, DK, DV, kKeysQ>(p.k, p.v, sTokens, sTokens + kKeysQ * (DK + 4), b, h, 0, run);
+  float* buffer0 = sTokens + (begin % kBuf) * S::kTokens;
+  if (begin < steps) fill_tokens<T, DK, DV, kKeysQ>(p.k, p.v, buffer0, buffer0 + kKeysQ * (DK + 4), b, h, begin * kKeysQ, run);
   fill_commit();
   float nl[4], d[4], dq[4][DK / 16];
   int pos[4];
@@ -403,7 +408,7 @@ __device__ __forceinline__ void dq_tile(const Params& p, unsigned index, float* 
   // positions of the warp's rows
   const int wr = r0 + 8 * (threadIdx.x >> 5), wz = r0 + live < wr + 8 ? r0 + live : wr + 8;
   const int warp_first = wr / p.G + off, warp_last = wz > wr ? (wz - 1) / p.G + off : -1;
-  for (int t = 0; t < steps; ++t) {
+  for (int t = begin; t < steps; ++t) {
     const float* sK = sTokens + (t % kBuf) * S::kTokens;
     const float* sV = sK + kKeysQ * (DK + 4);
     float* next = sTokens + ((t + 1) % kBuf) * S::kTokens;
@@ -477,6 +482,13 @@ __device__ __forceinline__ void dq_tile(const Params& p, unsigned index, float* 
   for (int a = 0; a < 4; ++a) {
     const int r = r0 + 4 * ty + a;
     if (r >= rows) continue;
+    if (p.q_pieces > 1) {
+      float* dst = p.part_q + (((int64_t(bh) * p.n_rt + rt) * p.q_pieces + piece) * kRowsQ + 4 * ty + a) * DK;
+#pragma unroll
+      for (int c = 0; c < DK / 64; ++c)
+        store4(dst + 64 * c + 4 * tx, make_float4(dq[a][4 * c], dq[a][4 * c + 1], dq[a][4 * c + 2], dq[a][4 * c + 3]));
+      continue;
+    }
     const int i = r / p.G;
     const int64_t hq = int64_t(h) * p.G + (r - i * p.G);
     T* dst = const_cast<T*>(row_of<T>(p.dq, b, hq, i));
@@ -485,6 +497,27 @@ __device__ __forceinline__ void dq_tile(const Params& p, unsigned index, float* 
       store4(dst + 64 * c + 4 * tx, make_float4(dq[a][4 * c] * p.scale, dq[a][4 * c + 1] * p.scale, dq[a][4 * c + 2] * p.scale,
                                                 dq[a][4 * c + 3] * p.scale));
   }
+}
+
+// Adds the pieces of dQ's tiles: four features of a row a thread.
+template <typename T, int DK>
+__global__ void __launch_bounds__(kThreads)
+window_dq_join_kernel(const Params p, int64_t n) {
+  wait_for_previous();
+  const int64_t x = int64_t(blockIdx.x) * kThreads + threadIdx.x;
+  if (x >= n) return;
+  const int64_t row = x / (DK / 4), tile = row / kRowsQ, bh = tile / p.n_rt;   // row: (tile, row of the tile)
+  const int c = int(x - row * (DK / 4)) * 4;
+  const int64_t r = (tile - bh * p.n_rt) * kRowsQ + (row - tile * kRowsQ);
+  if (r >= int64_t(p.N) * p.G) return;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i = 0; i < p.q_pieces; ++i) {
+    const float4 v = load4(p.part_q + ((tile * p.q_pieces + i) * kRowsQ + (row - tile * kRowsQ)) * DK + c);
+    s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+  }
+  const int64_t b = bh / p.Hk, h = bh - b * p.Hk, i = r / p.G;
+  store4(const_cast<T*>(row_of<T>(p.dq, b, h * p.G + (r - i * p.G), i)) + c,
+         make_float4(s.x * p.scale, s.y * p.scale, s.z * p.scale, s.w * p.scale));
 }
 
 // CTAs below n_q: dQ; the others, whose pieces are shorter: dK and dV.
@@ -503,6 +536,7 @@ window_bwd_cc_kernel(const Params p, unsigned n_q) {
 // for each SM; the first `cut` tiles then come in up to `pieces` pieces.
 struct Cut {
   int64_t n_kt, cut, pieces, piece_rows;
+  int64_t q_tiles, q_pieces;   // dQ's tiles, and pieces of each one's tokens where there are few
 };
 Cut cut_of(const WindowBwdArgs& a) {
   const int64_t G = a.Hq / a.Hk, bh = a.B * a.Hk, rows = a.Nq * G;
@@ -530,6 +564,13 @@ Cut cut_of(const WindowBwdArgs& a) {
   if ((rows + c.piece_rows - 1) / c.piece_rows > most) c.piece_rows = ((rows + most - 1) / most + kRowsKv - 1) / kRowsKv * kRowsKv;
   c.pieces = (rows + c.piece_rows - 1) / c.piece_rows;
   if (c.pieces == 1) c.cut = 0;
+  c.q_tiles = bh * ((rows + kRowsQ - 1) / kRowsQ);
+  int64_t tokens = windowed ? int64_t(a.window) + kRowsQ / G + a.sinks : a.Nk;
+  if (tokens > a.Nk) tokens = a.Nk;
+  c.q_pieces = c.q_tiles < kMostPieces / 8 ? (kMostPieces / 4 + c.q_tiles - 1) / c.q_tiles : 1;
+  // (pieces of eight steps at least: with two of three, the case above takes 71 us instead of 61)
+  if (c.q_pieces > tokens / (8 * kKeysQ)) c.q_pieces = tokens / (8 * kKeysQ);
+  if (c.q_pieces < 1) c.q_pieces = 1;
   return c;
 }
 
@@ -547,6 +588,8 @@ int launch(const WindowBwdArgs& a, char* msg, size_t msglen) {
   p.nl = reinterpret_cast<float*>(ws);
   p.delta = reinterpret_cast<float*>(ws + rows_bytes(a));
   p.part = reinterpret_cast<float*>(ws + 2 * rows_bytes(a));
+  p.part_q = p.part + bh * cut.cut * cut.pieces * kKeysKv * (DK + DV);
+  p.q_pieces = int(cut.q_pieces);
   p.Hk = int(a.Hk), p.N = int(a.Nq), p.G = int(G), p.Nk = int(a.Nk);
   p.mask = win::Mask{a.window, a.sinks, true};
   p.c_log2 = a.scale * kLog2e, p.scale = a.scale;
@@ -560,11 +603,16 @@ int launch(const WindowBwdArgs& a, char* msg, size_t msglen) {
     e = launch_overlapped(window_delta_kernel<T, DV>, dim3(unsigned((rows + 7) / 8)), dim3(kThreads), 0, a.stream, p, rows);
   const int64_t items = bh * (cut.cut * cut.pieces + cut.n_kt - cut.cut);
   if (e == cudaSuccess)
-    e = launch_overlapped(kern, dim3(unsigned(items + bh * p.n_rt)), dim3(kThreads), size_t(kSmem), a.stream, p, unsigned(bh * p.n_rt));
+    e = launch_overlapped(kern, dim3(unsigned(items + cut.q_tiles * cut.q_pieces)), dim3(kThreads), size_t(kSmem), a.stream, p,
+                          unsigned(cut.q_tiles * cut.q_pieces));
   const int64_t joined = bh * cut.cut * kKeysKv * ((DK + DV) / 4);
   if (e == cudaSuccess && joined > 0)
     e = launch_overlapped(window_dkdv_join_kernel<T, DK, DV>, dim3(unsigned((joined + kThreads - 1) / kThreads)), dim3(kThreads),
                           0, a.stream, p, joined);
+  const int64_t q_joined = cut.q_tiles * kRowsQ * (DK / 4);
+  if (e == cudaSuccess && cut.q_pieces > 1)
+    e = launch_overlapped(window_dq_join_kernel<T, DK>, dim3(unsigned((q_joined + kThreads - 1) / kThreads)), dim3(kThreads), 0,
+                          a.stream, p, q_joined);
   if (e != cudaSuccess) {
     snprintf(msg, msglen, "gradients of attention with a window: %s", cudaGetErrorString(e));
     return 5;
@@ -582,7 +630,8 @@ int launch_sizes(const WindowBwdArgs& a, char* msg, size_t msglen) {
 
 size_t window_bwd_cc_workspace(const WindowBwdArgs& a) {
   const Cut c = cut_of(a);
-  return size_t(2 * rows_bytes(a) + a.B * a.Hk * c.cut * c.pieces * kKeysKv * (a.dk + a.dv) * 4);
+  return size_t(2 * rows_bytes(a) + a.B * a.Hk * c.cut * c.pieces * kKeysKv * (a.dk + a.dv) * 4 +
+                (c.q_pieces > 1 ? c.q_tiles * c.q_pieces * kRowsQ * a.dk * 4 : 0));
 }
 
 int launch_window_bwd_cc(const WindowBwdArgs& a, char* msg, size_t msglen) {

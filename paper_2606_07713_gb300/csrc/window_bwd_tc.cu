@@ -13,7 +13,7 @@
 //            S^T = K Q^T, dP^T = V dO^T, P^T and dS^T back into TMEM as bf16, dV += P^T dO, dK += dS^T Q;
 //          dQ: 128 rows, over the token tiles that they see,
 //            S = Q K^T, dP = dO V^T, dS = P (dP - D), dQ += dS K;
-//   join   adds the pieces of cut token tiles, in order.
+//   join   adds the pieces of cut tiles, in order.
 // dQ apart from dK and dV: seven tile products in place of five, but every sum stays within one CTA (no
 // atomics, the same bits every time).
 //
@@ -27,7 +27,7 @@
 //
 // Pieces.  A token's rows are those of a window; a sink's are all later ones, which one CTA would walk over while the
 // others are done: token tiles with more row tiles than `piece` are cut.  `piece` is a window's row tiles, or less
-// where there are too few CTAs for the machine.
+// where there are too few CTAs for the machine.  With few rows and many tokens dQ's tiles have their tokens cut alike.
 //
 // CTA organisation of both kinds: 8 compute warps (warp w: TMEM lanes 32 (w % 4) .., columns N / 2 (w / 4) .. of the score
 // tiles; its bf16 values go back into the first half of its own columns), one warp for TMEM and the products, one for the
@@ -65,11 +65,13 @@ struct Params {
   float* nl;      // [half][64] -LSE log2 e; -infinity for rows that are not there or see nothing
   float* delta;   // alike: D
   float* part;    // [cut tile][piece][128][DK + DV]
+  float* part_q;  // [pair of halves][piece][128][DK], if dQ's tiles come in pieces
   int B, Hk, G, N, Nk;
   int GC, chunks, PT;   // heads of a half, chunks of heads, positions of a half
   int n_ht;             // halves along the positions, an even number
   int n_kt;             // token tiles
   int cut, pieces, piece;   // the first `cut` token tiles come in up to `pieces` pieces of `piece` row tiles (of N rows)
+  int q_pieces;         // pieces of a dQ tile's tokens
   int group;            // key heads whose token tiles are handed out in turn, longest first
   win::Mask mask;
   float c_log2, scale;
@@ -654,12 +656,16 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
   const WaitCtl wc{abort_flag, p.wait_limit_ns, 0u, &g_moa_window_bwd_status};
 
   // the last positions, which see the most without a window, come first
-  const int64_t per = int64_t(p.chunks) * (p.n_ht / 2), group = index / per;
-  const int64_t tile_id = group * per + (per - 1 - (index - group * per));
+  const unsigned which = index / unsigned(p.q_pieces), piece = index - which * unsigned(p.q_pieces);
+  const int64_t per = int64_t(p.chunks) * (p.n_ht / 2), group = which / per;
+  const int64_t tile_id = group * per + (per - 1 - (which - group * per));
   const RowTile t = row_tile(p, tile_id);
   // (a pair's positions may all lie past the end)
   const int i1 = t.i0 + 2 * p.PT - 1 < p.N ? t.i0 + 2 * p.PT - 1 : p.N - 1;
   const win::Tiles list = win::tiles_of(p.mask, p.Nk, p.N, t.i0, i1, C::kN);
+  // this piece's tiles of the list
+  const int j0 = int(int64_t(list.n) * piece / p.q_pieces), n_kt = int(int64_t(list.n) * (piece + 1) / p.q_pieces) - j0;
+  if (n_kt == 0 && p.q_pieces > 1) return;   // the join adds what pieces there are
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::kStages; ++s) {
@@ -692,7 +698,7 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
 
   if (warp == kLoadWarp) {
     // ---------------------------------------------------------------- TMA producer
-    if (lane == 0 && list.n > 0) {
+    if (lane == 0 && n_kt > 0) {
       tma_prefetch_desc(&tmQ);
       tma_prefetch_desc(&tmK);
       tma_prefetch_desc(&tmV);
@@ -710,7 +716,7 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
       int slot = 0;
       uint32_t phase = 0, issued = 0, issued_phase = 0;
       bool aborted = false;
-      for (int j = 0; j < list.n; ++j) {
+      for (int j = 0; j < n_kt; ++j) {
         if (!wait_bounded(empty_bar(slot), phase ^ 1u, wc)) {
           aborted = true;
           break;
@@ -719,7 +725,7 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
         issued_phase = (issued_phase & ~(1u << slot)) | (phase << slot);
         const uint32_t st = sStage + slot * C::kStageBytes;
         mbar_arrive_expect_tx(full_bar(slot), C::kStageBytes);
-        const int n0 = list.at(j) * C::kN;
+        const int n0 = list.at(j0 + j) * C::kN;
 #pragma unroll
         for (int q = 0; q < DK / 64; ++q) tma_load_4d(st + q * C::kTokenPanel, &tmK, full_bar(slot), q * 64, n0, t.h, t.b);
 #pragma unroll
@@ -763,20 +769,20 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
       };
       // S(0) dP(0) | S(1) dQ(0) dP(1) | S(2) dQ(1) dP(2) | ...: S(j + 1) goes as soon as the compute warps hold S(j)
       // in registers (s_free); dP(j + 1) overwrites the columns of dS(j) only after dQ(j), issued earlier.
-      bool ok = list.n > 0 && wait_bounded(q_full, 0, wc) && wait_bounded(full_bar(0), 0, wc);
+      bool ok = n_kt > 0 && wait_bounded(q_full, 0, wc) && wait_bounded(full_bar(0), 0, wc);
       if (ok) {
         tc_fence_after_sync();
         issue_s(stage(0));
         issue_dp(stage(0) + C::kKBytes);
       }
-      for (int j = 0; ok && j < list.n; ++j) {
+      for (int j = 0; ok && j < n_kt; ++j) {
         const int st = slot;
         if (++slot == C::kStages) {
           slot = 0;
           phase ^= 1u;
         }
         const uint32_t par = uint32_t(j) & 1u;
-        const bool more = j + 1 < list.n;
+        const bool more = j + 1 < n_kt;
         if (more) {
           ok = wait_bounded(full_bar(slot), phase, wc) && wait_bounded(s_free, par, wc);
           if (!ok) break;
@@ -813,7 +819,7 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
     const int lim = live ? win::row_end(p.mask, p.Nk, p.N, i) : 0x7fffffff, low = live ? win::row_low(p.mask, p.Nk, p.N, i) : 0;
     bool ok = true;
     auto wait_warp = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_bounded(bar, parity, wc)) != 0; };
-    for (int j = 0; j < list.n; ++j) {
+    for (int j = 0; j < n_kt; ++j) {
       const uint32_t par = uint32_t(j) & 1u;
       ok = wait_warp(s_full, par);
       if (!ok) break;
@@ -822,7 +828,7 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
       tmem_load_part<kCols>(tS, r);
       tc_fence_before_sync();
       mbar_arrive(s_free);
-      const int n0 = list.at(j) * C::kN + part * kCols;
+      const int n0 = list.at(j0 + j) * C::kN + part * kCols;
       float w[kCols];
 #pragma unroll
       for (int k = 0; k < kCols; k += 2) ffma2(w[k], w[k + 1], __uint_as_float(r[k]), __uint_as_float(r[k + 1]), cc, nn);
@@ -853,12 +859,13 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
     constexpr int wq = DK / kParts;
     {
       __nv_bfloat16* dst = row_of(p.dq, t.b, t.h * p.G + (live ? g : 0), live ? i : 0) + part * wq;
-      if (list.n == 0) {
+      if (n_kt == 0) {
         if (live)
           for (int e = 0; e < wq / 8; ++e) reinterpret_cast<uint4*>(dst)[e] = make_uint4(0, 0, 0, 0);
       } else if (ok && wait_warp(acc_done, 0)) {
         tc_fence_after_sync();
-        store_row<wq>(tmem + lanes + C::kTmemDQ + part * wq, p.scale, dst, nullptr, live);
+        store_row<wq>(tmem + lanes + C::kTmemDQ + part * wq, p.scale, dst,
+                      p.q_pieces > 1 ? p.part_q + ((tile_id * p.q_pieces + piece) * kBlk + row) * DK + part * wq : nullptr, live);
       }
     }
   }
@@ -870,6 +877,30 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
     tc_fence_after_sync();
     tmem_dealloc(tmem, C::kTmemCols);
   }
+}
+
+// Adds the pieces of dQ's tiles: four features of a row a thread.
+template <int DK, int DV>
+__global__ void __launch_bounds__(256)
+window_dq_tc_join_kernel(const Params p, int64_t n) {
+  wait_for_previous();
+  const int64_t x = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  if (x >= n) return;
+  const int64_t row = x / (DK / 4), pair = row / kBlk;
+  const int c = int(x - row * (DK / 4)) * 4, r = int(row - pair * kBlk);
+  const RowTile t = row_tile(p, pair);
+  const RowAt at = row_at(p, t, r);
+  if (!at.real) return;
+  const int i1 = t.i0 + 2 * p.PT - 1 < p.N ? t.i0 + 2 * p.PT - 1 : p.N - 1;
+  const int tiles = win::tiles_of(p.mask, p.Nk, p.N, t.i0, i1, width_of(DK, DV)).n;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i = 0; i < p.q_pieces; ++i) {
+    if (int64_t(tiles) * i / p.q_pieces == int64_t(tiles) * (i + 1) / p.q_pieces) continue;   // an empty piece
+    const float4 v = *reinterpret_cast<const float4*>(p.part_q + ((pair * p.q_pieces + i) * kBlk + r) * DK + c);
+    s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+  }
+  *reinterpret_cast<uint2*>(row_of(p.dq, t.b, t.h * p.G + at.g, at.i) + c) =
+      make_uint2(pack_bf16x2(s.x * p.scale, s.y * p.scale), pack_bf16x2(s.z * p.scale, s.w * p.scale));
 }
 
 // CTAs below n_kv: dK and dV; the others: dQ, which are shorter and fill the SMs that run out of the former.
@@ -891,7 +922,7 @@ constexpr int kSms = 152;   // the pieces aim at two CTAs for each SM; results d
 
 struct Plan {
   int64_t GC, chunks, PT, n_ht, n_kt, pairs;   // pairs of halves
-  int64_t cut, pieces, piece, items;
+  int64_t cut, pieces, piece, items, q_pieces;
   explicit Plan(const WindowBwdArgs& a) {
     const int64_t G = a.Hq / a.Hk, bh = a.B * a.Hk;
     chunks = (G + kHalf - 1) / kHalf;
@@ -930,17 +961,28 @@ struct Plan {
     pieces = (chunks * n_pt + piece - 1) / piece;
     if (pieces <= 1) cut = 0, pieces = 1;
     items = bh * (cut * pieces + n_kt - cut);
+    // dQ's tiles: pieces of four token tiles at least, until there are two CTAs for each SM
+    const int64_t width = width_of(a.dk, a.dv);
+    int64_t tiles = (a.Nk + width - 1) / width;
+    if (a.window != win::kNoWindow) {
+      const int64_t seen = (int64_t(a.window) + 2 * PT + a.sinks + 3 * width) / width;
+      if (seen < tiles) tiles = seen;
+    }
+    q_pieces = (2 * kSms + pairs - 1) / pairs;
+    if (q_pieces > tiles / 4) q_pieces = tiles / 4;
+    if (q_pieces < 1 || pairs >= kSms) q_pieces = 1;
   }
 };
 
 // The workspace: -LSE log2 e and D of every row of every half, then the pieces.
 struct Work {
-  int64_t nl, delta, part, bytes;
+  int64_t nl, delta, part, part_q, bytes;
   Work(const WindowBwdArgs& a, const Plan& p) {
     nl = 0;
     delta = p.pairs * kBlk * 4;
     part = 2 * delta;
-    bytes = part + a.B * a.Hk * p.cut * p.pieces * kBlk * (a.dk + a.dv) * 4;
+    part_q = part + a.B * a.Hk * p.cut * p.pieces * kBlk * (a.dk + a.dv) * 4;
+    bytes = part_q + (p.q_pieces > 1 ? p.pairs * p.q_pieces * kBlk * a.dk * 4 : 0);
   }
 };
 
@@ -964,6 +1006,8 @@ int launch(const WindowBwdArgs& a, char* msg, size_t msglen) {
   p.nl = reinterpret_cast<float*>(ws + w.nl);
   p.delta = reinterpret_cast<float*>(ws + w.delta);
   p.part = reinterpret_cast<float*>(ws + w.part);
+  p.part_q = reinterpret_cast<float*>(ws + w.part_q);
+  p.q_pieces = int(plan.q_pieces);
   p.B = int(a.B), p.Hk = int(a.Hk), p.G = int(G), p.N = int(a.Nq), p.Nk = int(a.Nk);
   p.GC = int(plan.GC), p.chunks = int(plan.chunks), p.PT = int(plan.PT);
   p.n_ht = int(plan.n_ht), p.n_kt = int(plan.n_kt);
@@ -994,12 +1038,15 @@ int launch(const WindowBwdArgs& a, char* msg, size_t msglen) {
   if (e == cudaSuccess)
     e = launch_overlapped(window_delta_tc_kernel<DV>, dim3(unsigned(plan.pairs)), dim3(256), 0, a.stream, p);
   if (e == cudaSuccess)
-    e = launch_overlapped(kern, dim3(unsigned(plan.items + plan.pairs)), dim3(kThreads), kSmem, a.stream, mq, mk, mv, mg, p,
+    e = launch_overlapped(kern, dim3(unsigned(plan.items + plan.pairs * plan.q_pieces)), dim3(kThreads), kSmem, a.stream, mq, mk, mv, mg, p,
                           unsigned(plan.items));
   const int64_t joined = bh * plan.cut * kBlk * ((DK + DV) / 4);
   if (e == cudaSuccess && joined > 0)
     e = launch_overlapped(window_dkdv_tc_join_kernel<DK, DV>, dim3(unsigned((joined + 255) / 256)), dim3(256), 0, a.stream, p,
                           joined);
+  const int64_t q_joined = plan.pairs * kBlk * (DK / 4);
+  if (e == cudaSuccess && plan.q_pieces > 1)
+    e = launch_overlapped(window_dq_tc_join_kernel<DK, DV>, dim3(unsigned((q_joined + 255) / 256)), dim3(256), 0, a.stream, p, q_joined);
   if (e != cudaSuccess) {
     snprintf(msg, msglen, "gradients of attention with a window: %s", cudaGetErrorString(e));
     return 5;

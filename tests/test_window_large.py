@@ -77,6 +77,10 @@ def test_window(dtype, B, Hq, Hk, N, M, dk, dv, window, sinks):
     ("bf16", 4, 12, 12, 1100, 1100, 64, 64, 0, 0),          # more items than CTAs
     ("bf16", 1, 6, 2, 1500, 2000, 128, 64, 100, 300),       # sinks over several tiles
     ("bf16", 1, 4, 4, 700, 700, 64, 128, 9, 700),           # every token a sink
+    ("bf16", 1, 4, 2, 30, 3000, 128, 128, 0, 0),            # few rows: their tokens in pieces
+    ("bf16", 2, 2, 2, 5, 2500, 64, 64, 2000, 100),
+    ("fp32", 1, 2, 1, 30, 1900, 128, 64, 0, 0),
+    ("fp32", 2, 6, 2, 3, 1000, 64, 128, 700, 5),
     ("fp32", 1, 4, 2, 1400, 1400, 64, 64, 200, 3),
     ("fp32", 1, 1, 1, 1200, 1200, 128, 128, 0, 0),
 ])
