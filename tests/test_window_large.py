@@ -259,3 +259,22 @@ def test_two_streams_at_once():
     for r in got:
         for x, y in zip(r, want):
             assert all(torch.equal(a, b) for a, b in zip(x, y))
+
+
+@pytest.mark.parametrize("N,M,window,sinks", [(27000, 27000, 3000, 4), (5000, 26000, 0, 0)])
+def test_more_keys_and_values_than_l2_holds(N, M, window, sinks):
+    """Work items are then taken in another order; rows at the beginning, the end and in between."""
+    Hq, Hk, d = 16, 8, 128
+    g = torch.Generator(device="cuda").manual_seed(N)
+    q, k, v = (rand(g, 1, h, n, d, dtype="bf16") for h, n in ((Hq, N), (Hk, M), (Hk, M)))
+    o, lse = pkg.window_attn_lse(q, k, v, window=window or None, sinks=sinks)
+    assert pkg.get_device_status() == _lib.MOA_OK
+    rows = torch.cat([torch.arange(70, device="cuda"), torch.randint(0, N, (200,), generator=g, device="cuda"),
+                      torch.arange(N - 70, N, device="cuda")])
+    p, j = (M - N + rows)[:, None], torch.arange(M, device="cuda")[None]
+    see = (j <= p) & ((j > p - window) | (j < sinks)) if window else j <= p
+    for h in range(Hq):
+        check(o[0, h, rows], lse[0, h, rows], q[0, h, rows], k[0, h // 2], v[0, h // 2], see, "bf16")
+    # every row was written: values of one give the sum of its weights, each rounded by 2^-8 at most, and the output once
+    ones = pkg.window_attn(q, k, torch.ones_like(v), window=window or None, sinks=sinks)
+    assert bool(((ones.float() - 1).abs() <= 2.0 ** -7 * 1.02).all())
