@@ -73,17 +73,25 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v) {
   __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
   *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<uint32_t*>(&a), *reinterpret_cast<uint32_t*>(&b));
 }
-__device__ __forceinline__ float dot4(float4 a, float4 b, float s) {
-  s = fmaf(a.x, b.x, s);
-  s = fmaf(a.y, b.y, s);
-  s = fmaf(a.z, b.z, s);
-  return fmaf(a.w, b.w, s);
+// d += a b for pairs: one instruction.
+__device__ __forceinline__ void fma2(float& d0, float& d1, float a0, float a1, float b0, float b1) {
+  asm("{\n\t.reg .b64 ra, rb, rd;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\tmov.b64 rd, {%0, %1};\n\t"
+      "fma.rn.f32x2 rd, ra, rb, rd;\n\tmov.b64 {%0, %1}, rd;\n\t}"
+      : "+f"(d0), "+f"(d1)
+      : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
+}
+// A sum of products in two halves, which are added at the end.
+struct Sum2 {
+  float a, b;
+  __device__ __forceinline__ float all() const { return a + b; }
+};
+__device__ __forceinline__ void dot4(float4 x, float4 y, Sum2& s) {
+  fma2(s.a, s.b, x.x, x.y, y.x, y.y);
+  fma2(s.a, s.b, x.z, x.w, y.z, y.w);
 }
 __device__ __forceinline__ void axpy4(float w, float4 v, float* acc) {
-  acc[0] = fmaf(w, v.x, acc[0]);
-  acc[1] = fmaf(w, v.y, acc[1]);
-  acc[2] = fmaf(w, v.z, acc[2]);
-  acc[3] = fmaf(w, v.w, acc[3]);
+  fma2(acc[0], acc[1], w, w, v.x, v.y);
+  fma2(acc[2], acc[3], w, w, v.z, v.w);
 }
 
 template <typename T>
@@ -101,7 +109,10 @@ window_delta_kernel(Params p, int64_t rows) {
   const int64_t per = int64_t(p.N) * p.G, bh = r / per, b = bh / p.Hk, h = bh - b * p.Hk;
   const int64_t at = r - bh * per, i = at / p.G, g = at - i * p.G, hq = h * p.G + g;
   float s = 0.f;
-  if (lane * 4 < DV) s = dot4(load4(row_of<T>(p.o, b, hq, i) + lane * 4), load4(row_of<T>(p.go, b, hq, i) + lane * 4), 0.f);
+  if (lane * 4 < DV) {
+    const float4 x = load4(row_of<T>(p.o, b, hq, i) + lane * 4), y = load4(row_of<T>(p.go, b, hq, i) + lane * 4);
+    s = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, x.w * y.w)));
+  }
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
   if (lane == 0) {
@@ -177,7 +188,7 @@ __device__ __forceinline__ bool rows_of_piece(const Params& p, int kt, int piece
 }
 
 // Buffers of a step's rows or tokens: two where two CTAs still fit on an SM (8 warps alone left it waiting for shared memory
-// half of the time: gradients of 2 x (6 / 3) heads x 517 x (128 / 64), window 100: 77 us, with all that is below 61).
+// half of the time: gradients of 2 x (6 / 3) heads x 517 x (128 / 64), window 100: 77 us, with all that is below 61, and with products in pairs 54).
 __host__ __device__ constexpr int buffers(int dk, int dv) { return dk + dv <= 192 ? 2 : 1; }
 
 template <int DK, int DV>
@@ -233,9 +244,9 @@ __device__ __forceinline__ void dkdv_tile(const Params& p, unsigned index, float
     const int p1 = int(unsigned(r1 - 1) / unsigned(p.G)) + off, j0 = k0 + 8 * (threadIdx.x >> 5);
     if (j0 <= p1 && (p0 - (j0 + 7) < p.mask.window || j0 < p.mask.sinks)) {
       // rows tx, tx + 16 against tokens 4 ty + a
-      float s[4][2], e[4][2];
+      Sum2 s2[4][2], e2[4][2];
 #pragma unroll
-      for (int a = 0; a < 4; ++a) s[a][0] = s[a][1] = e[a][0] = e[a][1] = 0.f;
+      for (int a = 0; a < 4; ++a) s2[a][0] = s2[a][1] = e2[a][0] = e2[a][1] = Sum2{0.f, 0.f};
 #pragma unroll 4
       for (int c = 0; c < DK; c += 4) {
         const float4 q0 = *reinterpret_cast<const float4*>(sQ + tx * (DK + 4) + c);
@@ -243,8 +254,8 @@ __device__ __forceinline__ void dkdv_tile(const Params& p, unsigned index, float
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
           const float4 kk = *reinterpret_cast<const float4*>(sK + (4 * ty + a) * (DK + 4) + c);
-          s[a][0] = dot4(q0, kk, s[a][0]);
-          s[a][1] = dot4(q1, kk, s[a][1]);
+          dot4(q0, kk, s2[a][0]);
+          dot4(q1, kk, s2[a][1]);
         }
       }
 #pragma unroll 4
@@ -254,10 +265,15 @@ __device__ __forceinline__ void dkdv_tile(const Params& p, unsigned index, float
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
           const float4 vv = *reinterpret_cast<const float4*>(sV + (4 * ty + a) * (DV + 4) + c);
-          e[a][0] = dot4(g0, vv, e[a][0]);
-          e[a][1] = dot4(g1, vv, e[a][1]);
+          dot4(g0, vv, e2[a][0]);
+          dot4(g1, vv, e2[a][1]);
         }
       }
+      float s[4][2], e[4][2];
+#pragma unroll
+      for (int a = 0; a < 4; ++a)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) s[a][x] = s2[a][x].all(), e[a][x] = e2[a][x].all();
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         const int r = r0 + tx + 16 * x;
@@ -422,9 +438,9 @@ __device__ __forceinline__ void dq_tile(const Params& p, unsigned index, float* 
     const int first = run.at(t * kKeysQ), last = run.at(x1);   // tokens
     if (first <= warp_last && (warp_first - last < p.mask.window || first < p.mask.sinks)) {
       // tokens tx, tx + 16 against rows 4 ty + a
-      float s[4][2], e[4][2];
+      Sum2 s2[4][2], e2[4][2];
 #pragma unroll
-      for (int a = 0; a < 4; ++a) s[a][0] = s[a][1] = e[a][0] = e[a][1] = 0.f;
+      for (int a = 0; a < 4; ++a) s2[a][0] = s2[a][1] = e2[a][0] = e2[a][1] = Sum2{0.f, 0.f};
 #pragma unroll 4
       for (int c = 0; c < DK; c += 4) {
         const float4 k0 = *reinterpret_cast<const float4*>(sK + tx * (DK + 4) + c);
@@ -432,8 +448,8 @@ __device__ __forceinline__ void dq_tile(const Params& p, unsigned index, float* 
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
           const float4 q = *reinterpret_cast<const float4*>(sQ + (4 * ty + a) * (DK + 4) + c);
-          s[a][0] = dot4(q, k0, s[a][0]);
-          s[a][1] = dot4(q, k1, s[a][1]);
+          dot4(q, k0, s2[a][0]);
+          dot4(q, k1, s2[a][1]);
         }
       }
 #pragma unroll 4
@@ -443,8 +459,8 @@ __device__ __forceinline__ void dq_tile(const Params& p, unsigned index, float* 
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
           const float4 g = *reinterpret_cast<const float4*>(sG + (4 * ty + a) * (DV + 4) + c);
-          e[a][0] = dot4(g, v0, e[a][0]);
-          e[a][1] = dot4(g, v1, e[a][1]);
+          dot4(g, v0, e2[a][0]);
+          dot4(g, v1, e2[a][1]);
         }
       }
 #pragma unroll
@@ -455,7 +471,7 @@ __device__ __forceinline__ void dq_tile(const Params& p, unsigned index, float* 
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
           const bool seen = j <= pos[a] && (pos[a] - j < p.mask.window || j < p.mask.sinks);
-          fs[a] = seen ? exp2f(fmaf(s[a][x], p.c_log2, nl[a])) * (e[a][x] - d[a]) : 0.f;
+          fs[a] = seen ? exp2f(fmaf(s2[a][x].all(), p.c_log2, nl[a])) * (e2[a][x].all() - d[a]) : 0.f;
         }
         *reinterpret_cast<float4*>(sS + (tx + 16 * x) * kLdW + 4 * ty) = ws;
       }

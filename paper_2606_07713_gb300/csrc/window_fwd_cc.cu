@@ -67,6 +67,14 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v) {
   *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<uint32_t*>(&a), *reinterpret_cast<uint32_t*>(&b));
 }
 
+// d += a b for pairs: one instruction.
+__device__ __forceinline__ void fma2(float& d0, float& d1, float a0, float a1, float b0, float b1) {
+  asm("{\n\t.reg .b64 ra, rb, rd;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\tmov.b64 rd, {%0, %1};\n\t"
+      "fma.rn.f32x2 rd, ra, rb, rd;\n\tmov.b64 {%0, %1}, rd;\n\t}"
+      : "+f"(d0), "+f"(d1)
+      : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
+}
+
 __device__ __forceinline__ int length_of(const Params& p, int64_t b) {
   if (p.lens == nullptr) return p.max_len;
   const int len = p.lens[b];
@@ -198,11 +206,11 @@ window_cc_kernel(const Params p) {
     fill_wait<1>();
     __syncthreads();
     // scores of tokens tx, tx + 16, ... : a quarter warp's rows of sK then lie in all banks
-    float s[RM][4];
+    float2 s[RM][4];   // in two halves
 #pragma unroll
     for (int a = 0; a < RM; ++a)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) s[a][k] = 0.f;
+      for (int k = 0; k < 4; ++k) s[a][k] = make_float2(0.f, 0.f);
 #pragma unroll 4
     for (int c = 0; c < DK; c += 4) {
       float4 q[RM], kk[4];
@@ -214,10 +222,8 @@ window_cc_kernel(const Params p) {
       for (int a = 0; a < RM; ++a)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          s[a][k] = fmaf(q[a].x, kk[k].x, s[a][k]);
-          s[a][k] = fmaf(q[a].y, kk[k].y, s[a][k]);
-          s[a][k] = fmaf(q[a].z, kk[k].z, s[a][k]);
-          s[a][k] = fmaf(q[a].w, kk[k].w, s[a][k]);
+          fma2(s[a][k].x, s[a][k].y, q[a].x, q[a].y, kk[k].x, kk[k].y);
+          fma2(s[a][k].x, s[a][k].y, q[a].z, q[a].w, kk[k].z, kk[k].w);
         }
     }
     float w[RM][4];
@@ -231,7 +237,7 @@ window_cc_kernel(const Params p) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         seen[k] = token[k] < end[a] && (token[k] >= low[a] || token[k] < p.mask.sinks);
-        w[a][k] = s[a][k] * p.c_log2;
+        w[a][k] = (s[a][k].x + s[a][k].y) * p.c_log2;
         if (seen[k]) top = fmaxf(top, w[a][k]);
       }
 #pragma unroll
@@ -270,10 +276,8 @@ window_cc_kernel(const Params p) {
 #pragma unroll
         for (int a = 0; a < RM; ++a) {
           if (pw[a] >= 0.f || pw[a] != pw[a]) {
-            acc[a][4 * c] = fmaf(pw[a], v.x, acc[a][4 * c]);
-            acc[a][4 * c + 1] = fmaf(pw[a], v.y, acc[a][4 * c + 1]);
-            acc[a][4 * c + 2] = fmaf(pw[a], v.z, acc[a][4 * c + 2]);
-            acc[a][4 * c + 3] = fmaf(pw[a], v.w, acc[a][4 * c + 3]);
+            fma2(acc[a][4 * c], acc[a][4 * c + 1], pw[a], pw[a], v.x, v.y);
+            fma2(acc[a][4 * c + 2], acc[a][4 * c + 3], pw[a], pw[a], v.z, v.w);
           }
         }
       }
