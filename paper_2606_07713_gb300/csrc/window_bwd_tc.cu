@@ -29,6 +29,10 @@
 // others are done: token tiles with more row tiles than `piece` are cut.  `piece` is a window's row tiles, or less
 // where there are too few CTAs for the machine.  With few rows and many tokens dQ's tiles have their tokens cut alike.
 //
+// What bounds it: the same chain; 2 x (32 / 8) heads x 8192 x 128, window 1024: 1005 us = 0.64 PFLOP/s of what the five products need,
+// tensor pipe 48 %, no other unit half busy.  (16 compute warps: 1026 us in place of 996; score tiles of 64 columns in two
+// buffers: 1364 in place of 1000.)
+//
 // CTA organisation of both kinds: 8 compute warps (warp w: TMEM lanes 32 (w % 4) .., columns N / 2 (w / 4) .. of the score
 // tiles; its bf16 values go back into the first half of its own columns), one warp for TMEM and the products, one for the
 // copies.  Waits are bounded; on expiry MOA_ERR_DEVICE_TIMEOUT is recorded and
@@ -183,39 +187,44 @@ window_delta_tc_kernel(const Params p) {
   wait_for_previous();
   const RowTile t = row_tile(p, blockIdx.x);
   const int gl = threadIdx.x % L, first = threadIdx.x / L;
-  uint4 ov[kIts], gv[kIts];
-  float lse[kIts];
-  bool real[kIts];
+  // four rows a thread on their way at a time (eight leave room for two CTAs an SM)
+  constexpr int kBatch = kIts < 4 ? kIts : 4;
+#pragma unroll 1
+  for (int k0 = 0; k0 < kIts; k0 += kBatch) {
+    uint4 ov[kBatch], gv[kBatch];
+    float lse[kBatch];
+    bool real[kBatch];
 #pragma unroll
-  for (int k = 0; k < kIts; ++k) {
-    const RowAt at = row_at(p, t, first + k * kStep);
-    const int hq = t.h * p.G + at.g, i = at.i;
-    real[k] = at.real;
-    ov[k] = gv[k] = make_uint4(0, 0, 0, 0);
-    lse[k] = -INFINITY;
-    if (real[k]) {
-      ov[k] = *reinterpret_cast<const uint4*>(row_of(p.o, t.b, hq, i) + gl * 8);
-      gv[k] = *reinterpret_cast<const uint4*>(row_of(p.go, t.b, hq, i) + gl * 8);
-      if (gl == 0) lse[k] = p.lse[(int64_t(t.b) * p.Hk * p.G + hq) * p.N + i];
-    }
-  }
-#pragma unroll
-  for (int k = 0; k < kIts; ++k) {
-    const __nv_bfloat162* o2 = reinterpret_cast<const __nv_bfloat162*>(&ov[k]);
-    const __nv_bfloat162* g2 = reinterpret_cast<const __nv_bfloat162*>(&gv[k]);
-    float acc = 0.f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float2 of = __bfloat1622float2(o2[e]), gf = __bfloat1622float2(g2[e]);
-      acc = fmaf(of.x, gf.x, acc);
-      acc = fmaf(of.y, gf.y, acc);
+    for (int k = 0; k < kBatch; ++k) {
+      const RowAt at = row_at(p, t, first + (k0 + k) * kStep);
+      const int hq = t.h * p.G + at.g, i = at.i;
+      real[k] = at.real;
+      ov[k] = gv[k] = make_uint4(0, 0, 0, 0);
+      lse[k] = -INFINITY;
+      if (real[k]) {
+        ov[k] = *reinterpret_cast<const uint4*>(row_of(p.o, t.b, hq, i) + gl * 8);
+        gv[k] = *reinterpret_cast<const uint4*>(row_of(p.go, t.b, hq, i) + gl * 8);
+        if (gl == 0) lse[k] = p.lse[(int64_t(t.b) * p.Hk * p.G + hq) * p.N + i];
+      }
     }
 #pragma unroll
-    for (int d = L / 2; d > 0; d >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, d);
-    if (gl == 0) {
-      const int64_t r = int64_t(blockIdx.x) * kBlk + first + k * kStep;
-      p.nl[r] = lse[k] == -INFINITY ? -INFINITY : -lse[k] * kLog2e;
-      p.delta[r] = acc;
+    for (int k = 0; k < kBatch; ++k) {
+      const __nv_bfloat162* o2 = reinterpret_cast<const __nv_bfloat162*>(&ov[k]);
+      const __nv_bfloat162* g2 = reinterpret_cast<const __nv_bfloat162*>(&gv[k]);
+      float acc = 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float2 of = __bfloat1622float2(o2[e]), gf = __bfloat1622float2(g2[e]);
+        acc = fmaf(of.x, gf.x, acc);
+        acc = fmaf(of.y, gf.y, acc);
+      }
+#pragma unroll
+      for (int d = L / 2; d > 0; d >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, d);
+      if (gl == 0) {
+        const int64_t r = int64_t(blockIdx.x) * kBlk + first + (k0 + k) * kStep;
+        p.nl[r] = lse[k] == -INFINITY ? -INFINITY : -lse[k] * kLog2e;
+        p.delta[r] = acc;
+      }
     }
   }
 }
