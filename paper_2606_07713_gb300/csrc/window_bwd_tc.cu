@@ -342,7 +342,6 @@ __device__ __forceinline__ void dkdv_tile(const CUtensorMap& tmQ, const CUtensor
       reinterpret_cast<uint4*>(smem + C::kOffStage)[x] = make_uint4(0, 0, 0, 0);
     fence_proxy_async_smem();
   }
-  wait_for_previous();
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
@@ -699,7 +698,6 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
       reinterpret_cast<uint4*>(smem)[x] = make_uint4(0, 0, 0, 0);
     fence_proxy_async_smem();
   }
-  wait_for_previous();
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
@@ -918,6 +916,7 @@ __global__ void __launch_bounds__(kThreads, ctas_of(DK, DV))
 window_bwd_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                      const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmG, const Params p,
                      unsigned n_kv) {
+  wait_for_previous();
   if (blockIdx.x < n_kv)
     dkdv_tile<DK, DV>(tmQ, tmK, tmV, tmG, p, blockIdx.x);
   else
