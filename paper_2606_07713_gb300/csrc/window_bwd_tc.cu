@@ -497,16 +497,16 @@ __device__ __forceinline__ void dkdv_tile(const CUtensorMap& tmQ, const CUtensor
     bool ok = true;
     int pt = n_t > 0 ? range.first + t0 % range.n : 0;
     auto wait_warp = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_bounded(bar, parity, wc)) != 0; };
-    for (int i = 0; i < n_t; ++i) {
+    for (int i = 0; ok && i < n_t; ++i) {
       const int st = slot;
       const uint32_t par = uint32_t(i) & 1u;
       // -L and D came with the tiles: the wait for the stage makes them visible to this thread
-      ok = wait_warp(full_bar(st), phase) && wait_warp(s_full, par);
+      // Waits that run out leave the loop together, at its end: until then what they would have brought is used as it is.
+      ok = wait_bounded(full_bar(st), phase, wc) && wait_bounded(s_full, par, wc);
       if (++slot == C::kStages) {
         slot = 0;
         phase ^= 1u;
       }
-      if (!ok) break;
       tc_fence_after_sync();
       const uint32_t nl4 = sStage + st * C::kStageBytes + C::kQBytes + C::kGBytes + part * kCols * 4;
       const uint32_t d4 = nl4 + C::kVecBytes;
@@ -549,8 +549,7 @@ __device__ __forceinline__ void dkdv_tile(const CUtensorMap& tmQ, const CUtensor
       tmem_wait_st();
       tc_fence_before_sync();
       mbar_arrive(p_ready);
-      ok = wait_warp(dp_full, par);
-      if (!ok) break;
+      ok = wait_bounded(dp_full, par, wc) && ok;
       tc_fence_after_sync();
       tmem_load_part<kCols>(tDP, r);
 #pragma unroll
@@ -567,6 +566,7 @@ __device__ __forceinline__ void dkdv_tile(const CUtensorMap& tmQ, const CUtensor
       tmem_wait_st();
       tc_fence_before_sync();
       mbar_arrive(ds_ready);
+      ok = __all_sync(0xffffffffu, ok);
     }
     // The first part writes dV, the second scale dK.
     const bool valid = key < p.Nk;
@@ -826,10 +826,9 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
     const int lim = live ? win::row_end(p.mask, p.Nk, p.N, i) : 0x7fffffff, low = live ? win::row_low(p.mask, p.Nk, p.N, i) : 0;
     bool ok = true;
     auto wait_warp = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_bounded(bar, parity, wc)) != 0; };
-    for (int j = 0; j < n_kt; ++j) {
+    for (int j = 0; ok && j < n_kt; ++j) {
       const uint32_t par = uint32_t(j) & 1u;
-      ok = wait_warp(s_full, par);
-      if (!ok) break;
+      ok = wait_bounded(s_full, par, wc);
       tc_fence_after_sync();
       uint32_t r[kCols];
       tmem_load_part<kCols>(tS, r);
@@ -849,8 +848,7 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
       }
 #pragma unroll
       for (int k = 0; k < kCols; ++k) w[k] = ex2_approx(w[k]);
-      ok = wait_warp(dp_full, par);
-      if (!ok) break;
+      ok = wait_bounded(dp_full, par, wc) && ok;
       tc_fence_after_sync();
       tmem_load_part<kCols>(tDP, r);
       uint32_t pk[kCols / 2];
@@ -861,6 +859,7 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
       tmem_wait_st();
       tc_fence_before_sync();
       mbar_arrive(ds_ready);
+      ok = __all_sync(0xffffffffu, ok);
     }
     // part q writes columns [wq q, wq q + wq)
     constexpr int wq = DK / kParts;

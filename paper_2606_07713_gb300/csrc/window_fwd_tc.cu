@@ -89,7 +89,9 @@ struct Cfg {
   static constexpr int kOffItems = (kOffMisc + 12 + 15) / 16 * 16;   // two items, then scan[12] and the share's beginning
   static constexpr int kOffSums = (kOffItems + 2 * 32 + 15 * 8 + 15) / 16 * 16;   // m and l of a row, for the cluster (QT = 1)
   static constexpr int kSmemBytes = kOffSums + (QT == 1 ? kBM * 8 : 0) + 1024;
-  static constexpr int kEarlyChunks = DV == 64 ? 2 : 4;   // of 32 tokens, exponentials before the wait for P's buffer
+  // Exponentials, in chunks of 32 tokens, before the wait for P's buffer (2, 3, 4 of 4 at d_v = 128: 1566, 1525, 1545 us of 32768
+  // tokens; 1 to 4 at d_v = 64: 65.2, 64.5, 65.1, 67.0 us of 4 x 16 heads x 2048, causal).
+  static constexpr int kEarlyChunks = DV == 64 ? 2 : 3;
   static constexpr uint32_t kTmemCols = 512;
   static constexpr uint32_t kTmemS0 = 0, kTmemS1 = kSharedS ? 0 : 128;
   static constexpr uint32_t kTmemP0 = kSharedS ? 128 : 256, kTmemP1 = kSharedS ? 192 : 320;
@@ -812,7 +814,8 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
           ok = zero_rows<DV>(smem + C::kOffKV + at % C::kStages * C::kStageBytes, zero_row, zero_step, gone - n0,
                              full_bar(at % C::kStages), at / C::kStages & 1, wc) && ok;
         }
-        if (!live_warp) {   // rows that are not there: in step with the others, and no more
+        // (with two row tiles such warps are few, and the branch alone cost the loop 5 %: 16384 tokens in 357 us, 341 without)
+        if (QT == 1 && !live_warp) {   // rows that are not there: in step with the others, and no more
           tc_fence_before_sync();
           mbar_arrive(s_free(j));
           if (t > 0) ok = wait_bounded(p_free(j), (t - 1) & 1u, wc) && ok;
