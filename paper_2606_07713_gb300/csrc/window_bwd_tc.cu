@@ -101,6 +101,18 @@ __device__ __forceinline__ void tmem_load_part(uint32_t taddr, uint32_t* r) {
 #pragma unroll
   for (int c = 0; c < COLS; c += 32) reg_anchor_x32(r + c);
 }
+// The same in steps of 32 columns: while one is worked on, the next is on its way.
+template <int COLS, typename F>
+__device__ __forceinline__ void tmem_each_32(uint32_t taddr, uint32_t* r, F&& work) {
+  tmem_ld_32x32b_x32(taddr, r);
+#pragma unroll
+  for (int c = 0; c < COLS; c += 32) {
+    tmem_wait_ld();
+    reg_anchor_x32(r + c);
+    if (c + 32 < COLS) tmem_ld_32x32b_x32(taddr + c + 32, r + c + 32);
+    work(c);
+  }
+}
 template <int COLS>
 __device__ __forceinline__ void tmem_store_part(uint32_t taddr, const uint32_t* pk) {
   if constexpr (COLS == 64)
@@ -522,46 +534,45 @@ __device__ __forceinline__ void dkdv_tile(const CUtensorMap& tmQ, const CUtensor
       from -= part * kCols % kHalf, upto -= part * kCols % kHalf;
       const bool full = __all_sync(0xffffffffu, from <= 0 && upto >= kCols);
       uint32_t r[kCols];
-      tmem_load_part<kCols>(tS, r);
       float w[kCols];
-#pragma unroll
-      for (int q = 0; q < kCols; q += 4) {
-        const float4 l = lds_f32x4(nl4 + q * 4);
-        ffma2(w[q], w[q + 1], __uint_as_float(r[q]), __uint_as_float(r[q + 1]), cc, pack_f32x2(l.x, l.y));
-        ffma2(w[q + 2], w[q + 3], __uint_as_float(r[q + 2]), __uint_as_float(r[q + 3]), cc, pack_f32x2(l.z, l.w));
-      }
-      if (!full) {
-#pragma unroll
-        for (int k = 0; k < kCols / 32; ++k) {
-          const uint32_t bits = below(upto, k) & ~below(from, k);
-#pragma unroll
-          for (int e = 0; e < 32; ++e) w[32 * k + e] = bits >> e & 1u ? w[32 * k + e] : -INFINITY;
-        }
-      }
       uint32_t pk[kCols / 2];
+      tmem_each_32<kCols>(tS, r, [&](int c) {
 #pragma unroll
-      for (int q = 0; q < kCols; q += 2) {
-        w[q] = ex2_approx(w[q]);
-        w[q + 1] = ex2_approx(w[q + 1]);
-        pk[q >> 1] = pack_bf16x2(w[q], w[q + 1]);
-      }
+        for (int q = c; q < c + 32; q += 4) {
+          const float4 l = lds_f32x4(nl4 + q * 4);
+          ffma2(w[q], w[q + 1], __uint_as_float(r[q]), __uint_as_float(r[q + 1]), cc, pack_f32x2(l.x, l.y));
+          ffma2(w[q + 2], w[q + 3], __uint_as_float(r[q + 2]), __uint_as_float(r[q + 3]), cc, pack_f32x2(l.z, l.w));
+        }
+        if (!full) {
+          const uint32_t bits = below(upto, c / 32) & ~below(from, c / 32);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) w[c + e] = bits >> e & 1u ? w[c + e] : -INFINITY;
+        }
+#pragma unroll
+        for (int q = c; q < c + 32; q += 2) {
+          w[q] = ex2_approx(w[q]);
+          w[q + 1] = ex2_approx(w[q + 1]);
+          pk[q >> 1] = pack_bf16x2(w[q], w[q + 1]);
+        }
+      });
       tmem_store_part<kCols>(tS, pk);
       tmem_wait_st();
       tc_fence_before_sync();
       mbar_arrive(p_ready);
       ok = wait_bounded(dp_full, par, wc) && ok;
       tc_fence_after_sync();
-      tmem_load_part<kCols>(tDP, r);
+      tmem_each_32<kCols>(tDP, r, [&](int c) {
 #pragma unroll
-      for (int q = 0; q < kCols; q += 4) {
-        const float4 d = lds_f32x4(d4 + q * 4);
-        const float s0 = w[q] * (__uint_as_float(r[q]) - d.x);
-        const float s1 = w[q + 1] * (__uint_as_float(r[q + 1]) - d.y);
-        const float s2 = w[q + 2] * (__uint_as_float(r[q + 2]) - d.z);
-        const float s3 = w[q + 3] * (__uint_as_float(r[q + 3]) - d.w);
-        pk[q >> 1] = pack_bf16x2(s0, s1);
-        pk[(q >> 1) + 1] = pack_bf16x2(s2, s3);
-      }
+        for (int q = c; q < c + 32; q += 4) {
+          const float4 d = lds_f32x4(d4 + q * 4);
+          const float s0 = w[q] * (__uint_as_float(r[q]) - d.x);
+          const float s1 = w[q + 1] * (__uint_as_float(r[q + 1]) - d.y);
+          const float s2 = w[q + 2] * (__uint_as_float(r[q + 2]) - d.z);
+          const float s3 = w[q + 3] * (__uint_as_float(r[q + 3]) - d.w);
+          pk[q >> 1] = pack_bf16x2(s0, s1);
+          pk[(q >> 1) + 1] = pack_bf16x2(s2, s3);
+        }
+      });
       tmem_store_part<kCols>(tDP, pk);
       tmem_wait_st();
       tc_fence_before_sync();
@@ -850,11 +861,12 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
       for (int k = 0; k < kCols; ++k) w[k] = ex2_approx(w[k]);
       ok = wait_bounded(dp_full, par, wc) && ok;
       tc_fence_after_sync();
-      tmem_load_part<kCols>(tDP, r);
       uint32_t pk[kCols / 2];
+      tmem_each_32<kCols>(tDP, r, [&](int c) {
 #pragma unroll
-      for (int k = 0; k < kCols; k += 2)
-        pk[k >> 1] = pack_bf16x2(w[k] * (__uint_as_float(r[k]) - dd), w[k + 1] * (__uint_as_float(r[k + 1]) - dd));
+        for (int k = c; k < c + 32; k += 2)
+          pk[k >> 1] = pack_bf16x2(w[k] * (__uint_as_float(r[k]) - dd), w[k + 1] * (__uint_as_float(r[k + 1]) - dd));
+      });
       tmem_store_part<kCols>(tDP, pk);
       tmem_wait_st();
       tc_fence_before_sync();
