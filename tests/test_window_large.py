@@ -278,3 +278,24 @@ def test_more_keys_and_values_than_l2_holds(N, M, window, sinks):
     # every row was written: values of one give the sum of its weights, each rounded by 2^-8 at most, and the output once
     ones = pkg.window_attn(q, k, torch.ones_like(v), window=window or None, sinks=sinks)
     assert bool(((ones.float() - 1).abs() <= 2.0 ** -7 * 1.02).all())
+
+
+def test_kernels_longer_than_the_limit_of_a_wait():
+    """Forward and gradients of 40000 tokens and 32 heads take some 20 and 100 ms; with waits limited to 5 ms no wait runs out: each is for
+    one tile, or lasts with the length of the context."""
+    import os
+    import subprocess
+    import sys
+    code = (
+        "import torch, paper_2606_07713_gb300 as p\n"
+        "q = torch.randn(1, 32, 40000, 128, device='cuda').bfloat16()\n"
+        "k, v = (torch.randn(1, 4, 40000, 128, device='cuda').bfloat16() for _ in range(2))\n"
+        "o, lse = p.window_attn_lse(q, k, v)\n"
+        "g = p.window_attn_bwd(q, k, v, o, lse, q)\n"
+        "v[:, :, 5, 7] = float('inf')\n"
+        "p.window_attn(q[:, :, :300], k[:, :, :300].contiguous(), v[:, :, :300].contiguous())\n"
+        "print('status', p.get_device_status(), all(bool(torch.isfinite(x).all()) for x in (o, *g)))\n")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300,
+                       env=dict(os.environ, MOA_WAIT_LIMIT_NS="5000000", PYTHONPATH=root))
+    assert r.returncode == 0 and "status 0 True" in r.stdout, r.stdout + r.stderr
