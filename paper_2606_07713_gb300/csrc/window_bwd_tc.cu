@@ -29,8 +29,8 @@
 // others are done: token tiles with more row tiles than `piece` are cut.  `piece` is a window's row tiles, or less
 // where there are too few CTAs for the machine.  With few rows and many tokens dQ's tiles have their tokens cut alike.
 //
-// What bounds it: the same chain; 2 x (32 / 8) heads x 8192 x 128, window 1024: 1005 us = 0.64 PFLOP/s of what the five products need,
-// tensor pipe 48 %, no other unit half busy.  (16 compute warps: 1026 us in place of 996; score tiles of 64 columns in two
+// What bounds it: the same chain; 2 x (32 / 8) heads x 8192 x 128, window 1024: 993 us = 0.65 PFLOP/s of what the five products need,
+// tensor pipe 49 %, no other unit half busy.  (16 compute warps: 1026 us in place of 996 at the time; score tiles of 64 columns in two
 // buffers: 1364 in place of 1000.)
 //
 // CTA organisation of both kinds: 8 compute warps (warp w: TMEM lanes 32 (w % 4) .., columns N / 2 (w / 4) .. of the score

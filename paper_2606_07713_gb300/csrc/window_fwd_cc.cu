@@ -13,7 +13,7 @@
 // then DV / 16 features of their outputs.
 //
 // What bounds it: shared memory's data path and multiply-adds about equally (2 x (6 / 3) heads x 517 queries x 700 keys x (128 / 64),
-// window 100: 18.6 us, 51 % and 49 % of the issue slots); few rows: the latency of a tile (5 sequences of 5 queries, window 1000:
+// window 100: 18.6 us, 52 %, and 39 % of the issue slots); few rows: the latency of a tile (5 sequences of 5 queries, window 1000:
 // 13.7 us).  The next tile's keys are on their way during the second product, its values during the next first one.
 //
 // Hidden tokens get the weight -1, which the second product skips: what their values hold (not numbers,

@@ -26,8 +26,8 @@
 // (exact_row).  That costs nothing where all values are finite.
 //
 // What bounds it.  Many rows: a softmax warp's chain of score load, maximum, 128 exponentials and stores beside the products
-// (32768 tokens, 32 / 8 heads of 128, window 4096: 1653 us = 1.24 PFLOP/s of what is seen, tensor pipe 57 %; 2048 queries against 16384 cached
-// tokens: 368 us = 1.40 PFLOP/s).  Few rows: memory (48 sequences, 1.2 GB of keys and values: 190 us, 6.3 TB/s), or latency (one
+// (32768 tokens, 32 / 8 heads of 128, window 4096: 1545 us = 1.33 PFLOP/s of what is seen, tensor pipe 62 %; 2048 queries against 16384 cached
+// tokens: 353 us = 1.46 PFLOP/s).  Few rows: memory (48 sequences, 1.2 GB of keys and values: 190 us, 6.3 TB/s), or latency (one
 // token, window 1024: 10.9 us).
 //
 // CTA organisation (QT = 2): warps 0-3 and 4-7 softmax and epilogue of row tiles 0 and 1 (thread = row), then the
@@ -132,8 +132,8 @@ struct Where {
 // Items in the order of the shares: what the CTAs work on at one time is neighbouring items (positions of one key head),
 // whose tokens they share in L2.  The order is that of a table read column by column, a column a CTA; the first `tall` columns
 // have height + 1 items.  Where all CTAs' tokens fit into L2 the items are taken in order of place (columns = 0).  32768 tokens of 8
-// key heads of 128, window 4096: in order of place the tokens come 12 times from memory, 5.1 GB, and the call takes 1717 us
-// instead of 1653; 4 x 16 heads x 2048 x 64, causal: 66 us instead of 68.
+// key heads of 128, window 4096: in order of place the tokens come 12 times from memory, 5.1 GB, and the call takes 4 % longer
+// (1717 us instead of 1653 before the softmax loop's last steps); 4 x 16 heads x 2048 x 64, causal: 66 us instead of 68.
 template <int QT>
 __device__ __forceinline__ Where where_of(const Params& p, int item) {
   Where w;
