@@ -495,11 +495,11 @@ size_t moa_kv4_attn_workspace_bytes(int64_t B, int64_t H_q, int64_t H_k, int64_t
  *   Q [B, H_q, N_q, d_k], K [B, H_k, N_k, d_k], V [B, H_k, N_k, d_v] inputs, O [B, H_q, N_q, d_v] output;
  *   strides 12 values: Q, K, V, O
  *   LSE       float32 [B, H_q, N_q] contiguous, or null: ln of the sum of exp of the row's scaled scores
- *   scale     any finite value;  dtype MOA_BF16 or MOA_FP32
+ *   scale     from -2e38 to 2e38;  dtype MOA_BF16 or MOA_FP32
  *   workspace device, 16-byte aligned, moa_window_attn_workspace_bytes(...) bytes
  * A batch padded at the end needs no lengths: later tokens are hidden from earlier ones.  What a token
  * that a query does not see holds, not numbers included, has no influence on that query.
- * B H_q N_q and B H_k N_k below 2^31.  fp32 accumulation, maxima and sums; bf16: weights are rounded to
+ * B H_q N_q and B H_k N_k at most 2^31 - 1025.  fp32 accumulation, maxima and sums; bf16: weights are rounded to
  * bf16 once.  Bounded waits as moa_attn_fwd.  Bitwise reproducible.
  */
 int moa_window_attn(const void* Q, const void* K, const void* V, void* O, float* LSE, int64_t B,
@@ -524,7 +524,8 @@ size_t moa_window_attn_workspace_bytes(int64_t B, int64_t H_q, int64_t H_k, int6
  * Tokens that no query sees get zeros, and so do queries that see nothing.  Inputs are finite: one that
  * is not can make the gradients of its neighbours (128 rows, 128 tokens) NaN that it does not reach by the
  * formula.  Accumulation in fp32; bf16: weights and dS are rounded to bf16 once.  dQ, dK and dV may be
- * slices of one buffer.  Bitwise reproducible.
+ * slices of one buffer where d_k = d_v and N_q = N_k.  Bounded waits as moa_attn_fwd.  Bitwise
+ * reproducible.
  */
 int moa_window_attn_bwd(const void* Q, const void* K, const void* V, const void* O, const void* dO,
                         const float* LSE, void* dQ, void* dK, void* dV, int64_t B, int64_t H_q,
@@ -573,7 +574,7 @@ int moa_kv_append(const void* Q, const void* K, const void* V, const float* cos,
  *   Q  [B, H_q, N, d_k] input, O  [B, H_q, N, d_v] output;  strides  6 values: Q, O
  *   lens     int32 [B] on the device: L of each sequence, 0 <= lens[b] <= max_len
  *   max_len  what the host knows of the lengths: it decides how the work is divided
- *            (1 <= max_len <= max_pages * page_tokens, below 2^31 - 64)
+ *            (1 <= max_len <= max_pages * page_tokens, at most 2^31 - 1025)
  *   causal   0: queries see later tokens too (those before their window are hidden all the same)
  *   LSE, scale, dtype (the pool's), workspace  as moa_window_attn
  * What the pool holds past lens[b], and at tokens that a query does not see, has no influence on it.

@@ -397,6 +397,10 @@ int attn_call(const void* Q, const void* pool, const int32_t* pages, const int32
 // ---------------------------------------------------------------------------------------------
 // Attention with a window, its gradients, and the 16- and 32-bit cache
 // ---------------------------------------------------------------------------------------------
+// Rows and tokens stay this far below 2^31: the kernels look ahead by a tile or two in 32 bits.
+constexpr int64_t kMostRows = kMax31 - 1024;
+constexpr float kMostScale = 2e38f;   // times log2 e still finite
+
 // Two tensors that may share a buffer without sharing an element.
 bool apart(const View& a, const Shape& sa, const View& b, const Shape& sb, int64_t elt) {
   return sa.d == sb.d && sa.N == sb.N && sa.B == sb.B && disjoint_slices(a, sa, b, sb, elt);
@@ -463,10 +467,10 @@ int check_window(int64_t B, int64_t Hq, int64_t Hk, int64_t N, int64_t dk, int64
   if ((dk != 64 && dk != 128) || (dv != 64 && dv != 128))
     return api_fail(MOA_ERR_UNSUPPORTED_SHAPE, "d_k, d_v must be 64 or 128; got %lld, %lld", (long long)dk, (long long)dv);
   int64_t rows;
-  if (!mul(B, Hq, &rows) || !mul(rows, N, &rows) || rows > kMax31)
-    return api_fail(MOA_ERR_UNSUPPORTED_SHAPE, "B * H_q * N must be below 2^31");
+  if (!mul(B, Hq, &rows) || !mul(rows, N, &rows) || rows > kMostRows)
+    return api_fail(MOA_ERR_UNSUPPORTED_SHAPE, "B * H_q * N must be at most 2^31 - 1025");
   if (window < 0 || sinks < 0) return api_fail(MOA_ERR_INVALID_ARG, "window and sinks must not be negative");
-  if (!std::isfinite(scale)) return api_fail(MOA_ERR_INVALID_ARG, "scale must be finite");
+  if (!(std::fabs(scale) <= kMostScale)) return api_fail(MOA_ERR_INVALID_ARG, "scale must be finite, and 2e38 at most");
   return MOA_OK;
 }
 
@@ -522,8 +526,8 @@ int run_window(WindowArgs& a, const Span* in, int n_in, const Span& out, void* w
 int check_keys(int64_t B, int64_t Hk, int64_t Nk) {
   if (Nk < 1) return api_fail(MOA_ERR_INVALID_ARG, "sizes must be >= 1");
   int64_t rows;
-  if (Nk > kMax31 - 64 || !mul(B, Hk, &rows) || !mul(rows, Nk, &rows) || rows > kMax31)
-    return api_fail(MOA_ERR_UNSUPPORTED_SHAPE, "B * H_k * N_k must be below 2^31");
+  if (!mul(B, Hk, &rows) || !mul(rows, Nk, &rows) || rows > kMostRows)
+    return api_fail(MOA_ERR_UNSUPPORTED_SHAPE, "B * H_k * N_k must be at most 2^31 - 1025");
   return MOA_OK;
 }
 
@@ -595,7 +599,7 @@ int cache_call(const void* Q, const void* pool, const int32_t* pages, const int3
   if (!lens || !strides) return api_fail(MOA_ERR_INVALID_ARG, "null lens or strides pointer");
   if (reinterpret_cast<uintptr_t>(lens) % 4 != 0) return api_fail(MOA_ERR_MISALIGNED, "lens is not 4-byte aligned");
   if (max_len < 1) return api_fail(MOA_ERR_INVALID_ARG, "sizes must be >= 1");
-  if (max_len > max_pages * page_tokens || max_len > kMax31 - 64)
+  if (max_len > max_pages * page_tokens || max_len > kMostRows)
     return api_fail(MOA_ERR_INVALID_ARG, "max_len %lld is more than the page table or the kernels take", (long long)max_len);
   WindowArgs a{};
   a.q = view(Q, strides), a.o = view(O, strides + 3);
@@ -843,8 +847,8 @@ size_t moa_window_attn_bwd_workspace_bytes(int64_t B, int64_t H_q, int64_t H_k, 
   if ((dtype != MOA_BF16 && dtype != MOA_FP32) || B < 1 || H_q < 1 || H_k < 1 || N_q < 1 || N_k < 1) return 0;
   if (H_q % H_k != 0 || (d_k != 64 && d_k != 128) || (d_v != 64 && d_v != 128) || window < 0 || sinks < 0) return 0;
   int64_t rows;
-  if (!moa::mul(B, H_q, &rows) || !moa::mul(rows, N_q, &rows) || rows > moa::kMax31) return 0;
-  if (!moa::mul(B, H_k, &rows) || !moa::mul(rows, N_k, &rows) || rows > moa::kMax31 || N_k > moa::kMax31 - 64) return 0;
+  if (!moa::mul(B, H_q, &rows) || !moa::mul(rows, N_q, &rows) || rows > moa::kMostRows) return 0;
+  if (!moa::mul(B, H_k, &rows) || !moa::mul(rows, N_k, &rows) || rows > moa::kMostRows) return 0;
   moa::WindowBwdArgs a{};
   a.B = B, a.Hq = H_q, a.Hk = H_k, a.Nq = N_q, a.Nk = N_k, a.dk = int(d_k), a.dv = int(d_v);
   a.f32 = dtype == MOA_FP32;
@@ -891,9 +895,9 @@ int moa_kv_attn(const void* Q, const void* pool, const int32_t* pages, const int
 size_t moa_kv_attn_workspace_bytes(int64_t B, int64_t H_q, int64_t H_k, int64_t N, int64_t d_k, int64_t d_v,
                                    int64_t max_len, int64_t window, int64_t sinks, int dtype) {
   if ((dtype != MOA_BF16 && dtype != MOA_FP32) || B < 1 || H_q < 1 || H_k < 1 || N < 1 || max_len < 1) return 0;
-  if (H_q % H_k != 0 || (d_k != 64 && d_k != 128) || (d_v != 64 && d_v != 128) || max_len > moa::kMax31 - 64) return 0;
+  if (H_q % H_k != 0 || (d_k != 64 && d_k != 128) || (d_v != 64 && d_v != 128) || max_len > moa::kMostRows) return 0;
   int64_t rows;
-  if (window < 0 || sinks < 0 || !moa::mul(B, H_q, &rows) || !moa::mul(rows, N, &rows) || rows > moa::kMax31) return 0;
+  if (window < 0 || sinks < 0 || !moa::mul(B, H_q, &rows) || !moa::mul(rows, N, &rows) || rows > moa::kMostRows) return 0;
   int sms = 0;
   if (moa::device_sm_count(&sms) != cudaSuccess) return 0;
   moa::WindowArgs a{};

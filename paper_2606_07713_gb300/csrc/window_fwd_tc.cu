@@ -558,7 +558,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             return s;
           }
           s.page = int(p.kv.n_pages);   // past the pool: zeros
-          if (t0 < end && (t0 + p.box > low || t0 < p.mask.sinks)) {
+          if (t0 < end && (t0 > low - p.box || t0 < p.mask.sinks)) {
             const int at = int(unsigned(t0) / unsigned(p.kv.page));
             const int pg = p.kv.table[w.b * p.kv.max_pages + at];
             s.token = t0 - at * p.kv.page;

@@ -468,3 +468,9 @@ def test_binding_refusals():
         pkg.kv_attn(x[:, :1].expand(1, 3, 8, 64), pool, pages, lens)
     with pytest.raises(TypeError):
         pkg.kv_attn(x, pool, pages.long(), lens)
+
+
+def test_attention_refuses_lengths_past_the_last_tile():
+    """max_len 2^31 - 1024 of 2^17 pages of 2^14 tokens: one more than the kernels take."""
+    a = dict(ATTEND, page_tokens=2 ** 14, max_pages=2 ** 17, max_len=2 ** 31 - 1024, window=0, sinks=0)
+    assert pkg.moa_kv_attn(**a) == INVALID and "max_len" in pkg.moa_last_error()

@@ -395,3 +395,14 @@ def test_binding_refusals_on_the_device():
         pkg.window_attn_bwd(x, x, x, o, lse, x, out=(x, x))
     with pytest.raises(ValueError):
         pkg.window_attn(x.transpose(2, 3), x, x)
+
+
+@pytest.mark.parametrize("call", [forward, backward], ids=["forward", "backward"])
+@pytest.mark.parametrize("changes,status", [
+    (dict(N_q=2 ** 29 - 256), _lib.MOA_ERR_UNSUPPORTED_SHAPE), (dict(N_k=2 ** 30 - 512), _lib.MOA_ERR_UNSUPPORTED_SHAPE),
+    (dict(scale=2.5e38), _lib.MOA_ERR_INVALID_ARG), (dict(scale=-3.4e38), _lib.MOA_ERR_INVALID_ARG),
+], ids=lambda x: str(x)[:40])
+def test_refusals_at_the_ends_of_ranges(call, changes, status):
+    """Rows and tokens one step past 2^31 - 1025 (4 and 2 heads), and scales that overflow times log2 e."""
+    assert call(**changes) == status
+    assert pkg.moa_last_error()
