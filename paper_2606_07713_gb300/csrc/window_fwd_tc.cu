@@ -11,7 +11,9 @@
 // tiles of tokens, and a decoding step's heads share one tile.  TMA puts them in that order itself (a
 // five-dimensional map: feature, head of the group, position, key head, sequence); heads and positions past the
 // end are zeros.  Keys and values come by TMA as well, a page (or the part of it that divides 128) a copy, straight from
-// the pool.  A page that no row of the work item sees is asked for past the pool's end, which fills zeros: its
+// the pool: a row's 128-byte panels lie side by side for every eight tokens, so that one copy brings all of them (with a
+// copy for each panel, 2048 queries against 16384 tokens in pages of 16 took 460 us instead of 345, 48 single tokens against
+// 8192 each 327 instead of 288).  A page that no row of the work item sees is asked for past the pool's end, which fills zeros: its
 // entry in the table may be anything.
 //
 // Work items (key head, chunk of heads, 128 QT rows) count in 128-token tiles; all items' tiles are cut into equal
@@ -26,7 +28,7 @@
 // (exact_row).  That costs nothing where all values are finite.
 //
 // What bounds it.  Many rows: a softmax warp's chain of score load, maximum, 128 exponentials and stores beside the products
-// (32768 tokens, 32 / 8 heads of 128, window 4096: 1545 us = 1.33 PFLOP/s of what is seen, tensor pipe 62 %; 2048 queries against 16384 cached
+// (32768 tokens, 32 / 8 heads of 128, window 4096: 1500 us = 1.37 PFLOP/s of what is seen, tensor pipe 62 %; 2048 queries against 16384 cached
 // tokens: 353 us = 1.46 PFLOP/s).  Few rows: memory (48 sequences, 1.2 GB of keys and values: 190 us, 6.3 TB/s), or latency (one
 // token, window 1024: 10.9 us).
 //
@@ -101,6 +103,13 @@ struct Cfg {
   static_assert(kSmemBytes <= 232448, "shared memory budget");
 };
 
+// Where a tile's panels of 64 columns and its groups of eight tokens lie in shared memory, in bytes from one to the next.  (A
+// template's constants: as variables of the products' descriptors, 32768 tokens take 4 % longer.)
+template <int D, bool PAGED>
+struct Layout {
+  static constexpr uint32_t kPanel = PAGED ? 1024 : 128 * 128, kGroup = PAGED ? D / 64 * 1024 : 1024;
+};
+
 struct Params {
   int64_t q_sb, q_sh, q_sn, o_sb, o_sh, o_sn;
   KvSource kv;
@@ -111,6 +120,8 @@ struct Params {
   int n_items;
   int columns, tall, height;   // the items' order in the shares (where_of)
   int box;               // tokens of a TMA copy
+  int page_groups;       // groups of eight tokens of a page and head
+  int all_groups;        // of the pool
   int cluster;           // CTAs for each work item, joined in the same launch; 0: equal shares of all items
   win::Mask mask;
   float c_log2;          // scale log2 e, >= 0
@@ -268,18 +279,20 @@ __device__ __noinline__ void exact_row(const __nv_bfloat16* q, __nv_bfloat16* o,
   for (int e = 0; e < NV; ++e) o[lane * NV + e] = __float2bfloat16(acc[e] * inv);
 }
 
-// Zeros in rows `row`, row + step, ... of a values' tile that has arrived, from row `gone` on; false if it has not.  (A
+// Zeros in rows `row`, row + step, ... of a values' tile (of pages) that has arrived, from row `gone` on; false if it has not.  (A
 // function of its own: an item's last tile only.)
 template <int DV>
 __device__ __noinline__ bool zero_rows(uint8_t* tile, int row, int step, int gone, uint32_t full, uint32_t parity,
                                        const WaitCtl& wc) {
+  using L = Layout<DV, true>;
   const bool ok = wait_bounded(full, parity, wc);
   for (; row < kBN; row += step) {
     if (row < gone) continue;
 #pragma unroll
     for (int q = 0; q < DV / 64; ++q)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) reinterpret_cast<uint4*>(tile + q * 128 * 128 + row * 128)[e] = make_uint4(0, 0, 0, 0);
+      for (int e = 0; e < 8; ++e)
+        reinterpret_cast<uint4*>(tile + q * L::kPanel + (row >> 3) * L::kGroup + (row & 7) * 128)[e] = make_uint4(0, 0, 0, 0);
   }
   fence_proxy_async_smem();
   return ok;
@@ -390,12 +403,14 @@ __device__ __noinline__ void cluster_rows(const __nv_bfloat16* Q, __nv_bfloat16*
 // ------------------------------------------------------------------------------------------------
 // Attention
 // ------------------------------------------------------------------------------------------------
-template <int DK, int DV, int QT>
+template <int DK, int DV, int QT, bool PAGED>
 __global__ void __launch_bounds__(Cfg<DK, DV, QT>::kThreads, 1)
 window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                  const __grid_constant__ CUtensorMap tmV, const __nv_bfloat16* Q, __nv_bfloat16* O, float* lse, float* part_o,
                  float2* part_ml, Cut* cuts, const Params p) {
   using C = Cfg<DK, DV, QT>;
+  using KL = Layout<DK, PAGED>;
+  using VL = Layout<DV, PAGED>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const uint32_t sQ = smem_u32(smem), sKV = smem_u32(smem + C::kOffKV), bar0 = smem_u32(smem + C::kOffBar);
@@ -545,31 +560,24 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         const win::Tiles list{x.first, x.from, x.units};
         const int end = win::row_end(p.mask, x.len, p.N, w.i1), low = win::row_low(p.mask, x.len, p.N, w.i0);
         const int n_kt = x.u1 - x.u0;
-        // the lane's copy of tile u0 + n: its first token, and the page (of a dense tensor the sequence)
-        struct Source {
-          int token, page;
-        };
+        // the lane's copy of tile u0 + n: its first token, or its first group of eight tokens of the pool
         auto source = [&](int n) {
-          Source s{0, w.b};
+          int s = 0;
           if (n >= n_kt || lane >= boxes) return s;
           const int t0 = list.at(x.u0 + n) * kBN + lane * p.box;
-          if (p.kv.table == nullptr) {
-            s.token = t0;
-            return s;
-          }
-          s.page = int(p.kv.n_pages);   // past the pool: zeros
+          if (!PAGED) return t0;
+          s = p.all_groups;   // past the pool: zeros
           if (t0 < end && (t0 > low - p.box || t0 < p.mask.sinks)) {
             const int at = int(unsigned(t0) / unsigned(p.kv.page));
             const int pg = p.kv.table[w.b * p.kv.max_pages + at];
-            s.token = t0 - at * p.kv.page;
             if (pg >= 0 && pg < p.kv.n_pages)
-              s.page = pg;
+              s = (pg * p.Hk + w.h) * p.page_groups + ((t0 - at * p.kv.page) >> 3);
             else
               atomicExch(&g_moa_window_tc_status, win::kErrIndex);
           }
           return s;
         };
-        Source cur = source(0), next = cur, after = source(1);
+        int cur = source(0), next = cur, after = source(1);
         for (int t = 0; t < 2 * n_kt; ++t) {
           // K0 K1 V0 K2 V1 ... (tile n + 1's scores come before tile n's P V)
           const int u = t - 1, nn = u >> 1;
@@ -585,19 +593,21 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
           }
           issued |= 1u << slot;
           issued_phase = (issued_phase & ~(1u << slot)) | (phase << slot);
-          const uint32_t dst = sKV + slot * C::kStageBytes + lane * p.box * 128;
+          const uint32_t dst = sKV + slot * C::kStageBytes + lane * p.box / 8 * (is_k ? KL::kGroup : VL::kGroup);
           if (lane == 0) mbar_arrive_expect_tx(full_bar(slot), is_k ? C::kKTileBytes : C::kVTileBytes);
           __syncwarp();
           if (lane < boxes) {
-            if (is_k) {
-              const Source& s = n == 0 ? cur : next;
+            const int s = is_k && n > 0 ? next : cur;
+            if constexpr (PAGED) {
+              tma_load_4d(dst, is_k ? &tmK : &tmV, full_bar(slot), 0, 0, 0, s);
+            } else if (is_k) {
 #pragma unroll
               for (int q = 0; q < DK / 64; ++q)
-                tma_load_4d(dst + q * C::kPanelBytes, &tmK, full_bar(slot), q * 64, s.token, w.h, s.page);
+                tma_load_4d(dst + q * C::kPanelBytes, &tmK, full_bar(slot), q * 64, s, w.h, w.b);
             } else {
 #pragma unroll
               for (int q = 0; q < DV / 64; ++q)
-                tma_load_4d(dst + q * C::kPanelBytes, &tmV, full_bar(slot), q * 64, cur.token, w.h, cur.page);
+                tma_load_4d(dst + q * C::kPanelBytes, &tmV, full_bar(slot), q * 64, s, w.h, w.b);
             }
           }
           if (!is_k) cur = next;
@@ -650,16 +660,15 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         };
         auto issue_qk = [&](uint32_t kb) {
 #pragma unroll
-          for (int kk = 0; kk < DK / 16; ++kk) {
-            const uint32_t off = (kk >> 2) * C::kPanelBytes + (kk & 3) * 32;
-            mma_f16_ss(tS, make_sdesc_sw128(sQj + off, 16, 1024), make_sdesc_sw128(kb + off, 16, 1024), kIdescQK,
+          for (int kk = 0; kk < DK / 16; ++kk)
+            mma_f16_ss(tS, make_sdesc_sw128(sQj + (kk >> 2) * C::kPanelBytes + (kk & 3) * 32, 16, 1024),
+                       make_sdesc_sw128(kb + (kk >> 2) * KL::kPanel + (kk & 3) * 32, 16, KL::kGroup), kIdescQK,
                        kk > 0 ? 1u : 0u);
-          }
         };
         auto issue_pv = [&](uint32_t vb, uint32_t acc_first) {
 #pragma unroll
           for (int kk = 0; kk < kBN / 16; ++kk)
-            mma_f16_ts(tO, tP + kk * 8, make_sdesc_sw128(vb + kk * 2048, C::kPanelBytes, 1024), kIdescPV,
+            mma_f16_ts(tO, tP + kk * 8, make_sdesc_sw128(vb + 2 * kk * VL::kGroup, VL::kPanel, VL::kGroup), kIdescPV,
                        kk > 0 ? 1u : acc_first);
         };
         // The S buffer may take tile u's scores once its last reader holds what it has: this row
@@ -793,7 +802,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       }
       // past the sequence's end a page holds whatever it held: the first such token, of a cache.  Its rows of values are
       // zeroed by the warps that have no rows of queries, or else by all, each its own rows.
-      const int gone = p.kv.table != nullptr ? x.len : 0x7fffffff;
+      const int gone = PAGED ? x.len : 0x7fffffff;
       int zero_row = row, zero_step = kBN;
       if (QT == 1) {
         const int warps = (p.N * p.GC + 31) / 32;   // those with rows
@@ -809,7 +818,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         // as it is.
         ok = wait_bounded(s_full(j), t & 1u, wc);
         tc_fence_after_sync();
-        if (gone - n0 < kBN && zero_step > 0) {   // the item's last tile
+        if (PAGED && gone - n0 < kBN && zero_step > 0) {   // the item's last tile
           const int k = n - x.u0, at = int(ring) + (n + 1 < x.u1 ? 2 * k + 2 : 2 * k + 1);
           ok = zero_rows<DV>(smem + C::kOffKV + at % C::kStages * C::kStageBytes, zero_row, zero_step, gone - n0,
                              full_bar(at % C::kStages), at / C::kStages & 1, wc) && ok;
@@ -1108,10 +1117,10 @@ struct Work {
 bool describable(int64_t stride, int64_t size) { return size == 1 || (stride > 0 && stride < (int64_t(1) << 39)); }
 uint64_t map_stride(int64_t stride, int64_t size) { return size == 1 ? 16 : uint64_t(stride) * 2; }
 
-template <int DK, int DV, int QT>
+template <int DK, int DV, int QT, bool PAGED>
 int launch(const WindowArgs& a, const Plan& plan, int sms, char* msg, size_t msglen) {
   using C = Cfg<DK, DV, QT>;
-  auto kern = window_tc_kernel<DK, DV, QT>;
+  auto kern = window_tc_kernel<DK, DV, QT, PAGED>;
   cudaError_t e = ensure_smem_limit(reinterpret_cast<const void*>(kern), C::kSmemBytes);
   if constexpr (QT == 2) {
     static std::atomic<int> regs{-1};
@@ -1145,23 +1154,32 @@ int launch(const WindowArgs& a, const Plan& plan, int sms, char* msg, size_t msg
   p.mask = win::Mask{a.window, a.sinks, a.causal};
   p.c_log2 = a.scale * kLog2e;
   p.wait_limit_ns = wait_limit_ns();
-  const bool paged = a.kv.table != nullptr;
   p.box = kBN;
-  if (paged)
+  if (PAGED)
     while (a.kv.page % p.box != 0) p.box /= 2;
   CUtensorMap mq, mk, mv;
   const uint64_t q_dims[5] = {DK, uint64_t(G), uint64_t(a.N), uint64_t(a.Hk), uint64_t(a.B)};
   const uint64_t q_str[4] = {map_stride(a.q.sh, G), map_stride(a.q.sn, a.N), map_stride(G * a.q.sh, a.Hk),
                              map_stride(a.q.sb, a.B)};
   const uint32_t q_box[5] = {64, uint32_t(plan.GC), uint32_t(plan.PT), 1, 1};
-  const uint64_t rows = uint64_t(paged ? a.kv.page : a.max_len), outer = uint64_t(paged ? a.kv.n_pages : a.B);
-  const uint64_t k_dims[4] = {DK, rows, uint64_t(a.Hk), outer}, v_dims[4] = {DV, rows, uint64_t(a.Hk), outer};
-  const uint64_t k_str[3] = {map_stride(a.kv.k_sn, int64_t(rows)), map_stride(a.kv.k_sh, a.Hk), map_stride(a.kv.k_sb, int64_t(outer))};
-  const uint64_t v_str[3] = {map_stride(a.kv.v_sn, int64_t(rows)), map_stride(a.kv.v_sh, a.Hk), map_stride(a.kv.v_sb, int64_t(outer))};
-  const uint32_t kv_box[4] = {64, uint32_t(p.box), 1, 1};
+  // Keys and values.  Dense: feature, token, head, sequence, a panel of 64 features a copy.  Pages: feature of a panel, token of a
+  // group of eight, panel, group of the pool (its pages and heads lie one after the other).
+  p.page_groups = PAGED ? a.kv.page / 8 : 0;
+  p.all_groups = PAGED ? int(a.kv.n_pages * a.Hk * p.page_groups) : 0;
+  const uint64_t len = uint64_t(a.max_len), row_bytes = (DK + DV) * 2;
+  uint64_t k_dims[4] = {DK, len, uint64_t(a.Hk), uint64_t(a.B)}, v_dims[4] = {DV, len, uint64_t(a.Hk), uint64_t(a.B)};
+  uint64_t k_str[3] = {map_stride(a.kv.k_sn, a.max_len), map_stride(a.kv.k_sh, a.Hk), map_stride(a.kv.k_sb, a.B)};
+  uint64_t v_str[3] = {map_stride(a.kv.v_sn, a.max_len), map_stride(a.kv.v_sh, a.Hk), map_stride(a.kv.v_sb, a.B)};
+  uint32_t k_box[4] = {64, uint32_t(p.box), 1, 1}, v_box[4] = {64, uint32_t(p.box), 1, 1};
+  auto by_groups = [&](uint32_t panels, uint64_t* dims, uint64_t* str, uint32_t* box) {
+    dims[0] = 64, dims[1] = 8, dims[2] = panels, dims[3] = uint64_t(p.all_groups);
+    str[0] = row_bytes, str[1] = 128, str[2] = 8 * row_bytes;
+    box[1] = 8, box[2] = panels, box[3] = uint32_t(p.box) / 8;
+  };
+  if (PAGED) by_groups(DK / 64, k_dims, k_str, k_box), by_groups(DV / 64, v_dims, v_str, v_box);
   if (!encode_bf16_map_nd(&mq, a.q.p, 5, q_dims, q_str, q_box, msg, msglen) ||
-      !encode_bf16_map_nd(&mk, a.kv.k, 4, k_dims, k_str, kv_box, msg, msglen) ||
-      !encode_bf16_map_nd(&mv, a.kv.v, 4, v_dims, v_str, kv_box, msg, msglen))
+      !encode_bf16_map_nd(&mk, a.kv.k, 4, k_dims, k_str, k_box, msg, msglen) ||
+      !encode_bf16_map_nd(&mv, a.kv.v, 4, v_dims, v_str, v_box, msg, msglen))
     return 5;
   // tiles of tokens, if every sequence is as long as max_len and no window hides any
   const int64_t most_tiles = (a.max_len + kBN - 1) / kBN, most = plan.n_items * most_tiles;
@@ -1219,7 +1237,9 @@ int launch(const WindowArgs& a, const Plan& plan, int sms, char* msg, size_t msg
 template <int DK, int DV>
 int launch_rows(const WindowArgs& a, int sms, char* msg, size_t msglen) {
   const Plan plan(a);
-  return plan.QT == 2 ? launch<DK, DV, 2>(a, plan, sms, msg, msglen) : launch<DK, DV, 1>(a, plan, sms, msg, msglen);
+  if (a.kv.table != nullptr)
+    return plan.QT == 2 ? launch<DK, DV, 2, true>(a, plan, sms, msg, msglen) : launch<DK, DV, 1, true>(a, plan, sms, msg, msglen);
+  return plan.QT == 2 ? launch<DK, DV, 2, false>(a, plan, sms, msg, msglen) : launch<DK, DV, 1, false>(a, plan, sms, msg, msglen);
 }
 
 }  // namespace
@@ -1227,6 +1247,7 @@ int launch_rows(const WindowArgs& a, int sms, char* msg, size_t msglen) {
 bool window_tc_takes(const WindowArgs& a) {
   const int64_t G = a.Hq / a.Hk, rows = a.kv.table != nullptr ? a.kv.page : a.max_len;
   const int64_t outer = a.kv.table != nullptr ? a.kv.n_pages : a.B;
+  if (a.kv.table != nullptr && a.kv.n_pages * a.Hk * (a.kv.page / 8) >= int64_t(1) << 31) return false;   // groups of a pool
   return !a.f32 && a.scale >= 0.f && describable(a.q.sh, G) && describable(G * a.q.sh, a.Hk) && describable(a.q.sn, a.N) &&
          describable(a.q.sb, a.B) && describable(a.kv.k_sn, rows) && describable(a.kv.k_sh, a.Hk) &&
          describable(a.kv.k_sb, outer) && describable(a.kv.v_sn, rows) && describable(a.kv.v_sh, a.Hk) &&
