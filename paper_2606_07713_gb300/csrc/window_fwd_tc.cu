@@ -18,7 +18,7 @@
 //
 // Work items (key head, chunk of heads, 128 QT rows) count in 128-token tiles; all items' tiles are cut into equal
 // shares, one for each SM (one CTA fills an SM), and a CTA walks over its share.  Cut items are joined by a
-// second kernel.  QT = 2 where there are more rows than a tile holds: keys and values in shared memory then serve
+// second kernel.  Few items of one row tile go to a cluster each, whose CTAs join them in the same launch.  QT = 2 where there are more rows than a tile holds: keys and values in shared memory then serve
 // twice the rows.
 //
 // Hidden tokens: a tile that some row sees only in part is masked by words of bits, -infinity in place of the
@@ -346,7 +346,7 @@ __device__ __forceinline__ void rows_again(const __nv_bfloat16* Q, __nv_bfloat16
 }
 
 // A cluster's item: CTA (r / 4) % size joins row r.  Every CTA leaves its part of the row there, in the last two stages of the
-// ring, which an item of two tiles does not use: [CTA][row of the owner][DV], and m and l.  (Parts fetched by the owner instead
+// ring, which a cluster does not use for tiles: [CTA][row of the owner][DV], and m and l.  (Parts fetched by the owner instead
 // took 3 us more: two round trips and a second barrier.)
 struct Owner {
   int rank, row;
@@ -531,6 +531,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
   tc_fence_after_sync();
   const uint32_t tmem = *tmem_slot;
   const bool clustered = QT == 1 && p.cluster != 0;
+  const int stages = clustered ? C::kStages - 2 : C::kStages;   // the last two receive a cluster's parts
   if (clustered) cluster_arrive();   // every thread waits for it once: the softmax threads before they write to other CTAs
   // A whole warp's wait: on expiry all its lanes leave together.
   auto wait_warp = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_bounded(bar, parity, wc)) != 0; };
@@ -626,7 +627,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             if (!ok) break;
             ++q_issued;
           }
-          if (++slot == C::kStages) {
+          if (++slot == stages) {
             slot = 0;
             phase ^= 1u;
           }
@@ -653,7 +654,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         uint32_t phase = 0;
         uint32_t t = 0;   // tiles so far: the phases of the barriers between the roles
         auto next = [&]() {
-          if (++slot == C::kStages) {
+          if (++slot == stages) {
             slot = 0;
             phase ^= 1u;
           }
@@ -820,8 +821,8 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         tc_fence_after_sync();
         if (PAGED && gone - n0 < kBN && zero_step > 0) {   // the item's last tile
           const int k = n - x.u0, at = int(ring) + (n + 1 < x.u1 ? 2 * k + 2 : 2 * k + 1);
-          ok = zero_rows<DV>(smem + C::kOffKV + at % C::kStages * C::kStageBytes, zero_row, zero_step, gone - n0,
-                             full_bar(at % C::kStages), at / C::kStages & 1, wc) && ok;
+          ok = zero_rows<DV>(smem + C::kOffKV + at % stages * C::kStageBytes, zero_row, zero_step, gone - n0,
+                             full_bar(at % stages), at / stages & 1, wc) && ok;
         }
         // (with two row tiles such warps are few, and the branch alone cost the loop 5 %: 16384 tokens in 357 us, 341 without)
         if (QT == 1 && !live_warp) {   // rows that are not there: in step with the others, and no more
@@ -1085,7 +1086,8 @@ window_tc_join_kernel(const __nv_bfloat16* Q, __nv_bfloat16* O, float* lse, cons
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 constexpr int64_t kMostInL2 = int64_t(100) << 20;   // of 129 MB
-constexpr int64_t kClusters16 = 7, kClusters8 = 14;   // clusters of this many CTAs at a time, one less a kind than there is room for
+// Clusters of 16, 8, 4, 2 CTAs at a time, a little less than there was room for (7, 15, 36, 76; one more took twice as long).
+constexpr int64_t kClusters16 = 7, kClusters8 = 14, kClusters4 = 34, kClusters2 = 72;
 
 // How the rows of a key head are divided.
 struct Plan {
@@ -1184,17 +1186,20 @@ int launch(const WindowArgs& a, const Plan& plan, int sms, char* msg, size_t msg
   // tiles of tokens, if every sequence is as long as max_len and no window hides any
   const int64_t most_tiles = (a.max_len + kBN - 1) / kBN, most = plan.n_items * most_tiles;
   const unsigned ctas = unsigned(most < sms ? most : sms);
-  // Few items of few tiles: a cluster for each, joined in the same launch, where that is no more than two tiles a CTA.  A
-  // processing cluster of the GPU has room for two clusters of 8 CTAs, or one of 16.
+  // Few items: a cluster for each, the largest that all fit into the GPU at the same time, joined in the same launch, where that is
+  // no more than eight tiles a CTA (equal shares and the cluster, bf16, d = 128: 1 item of 128 tiles 23.9 and 18.2 us; 8 of 64:
+  // 20.2 and 17.8, of 128, sixteen a CTA: 24.0 and 26.2; 32 of 32: 24.9 and 19.2; 64 of 16: 23.9 and 19.2).
   if constexpr (QT == 1) {
     int64_t tiles = most_tiles;
     if (a.window != win::kNoWindow) {
       const int64_t seen = (int64_t(a.window) + plan.PT + kBN - 1) / kBN + 1 + (int64_t(a.sinks) + kBN - 1) / kBN;
       if (seen < tiles) tiles = seen;
     }
-    const int64_t size = plan.n_items <= kClusters16 ? 16 : 8;
-    if (tiles <= 2 * size && plan.n_items <= (size == 16 ? kClusters16 : kClusters8)) {
-      p.cluster = 2;
+    int64_t size = 16;
+    for (int64_t room : {kClusters16, kClusters8, kClusters4, kClusters2})
+      if (plan.n_items > room) size /= 2;
+    if (tiles <= 8 * size && plan.n_items <= sms) {
+      p.cluster = 1;
       while (p.cluster < size && p.cluster < tiles) p.cluster *= 2;
       if (p.cluster > 8) e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kern), cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
       if (e == cudaSuccess)

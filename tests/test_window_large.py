@@ -299,3 +299,44 @@ def test_kernels_longer_than_the_limit_of_a_wait():
     r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300,
                        env=dict(os.environ, MOA_WAIT_LIMIT_NS="5000000", PYTHONPATH=root))
     assert r.returncode == 0 and "status 0 True" in r.stdout, r.stdout + r.stderr
+
+
+@pytest.mark.parametrize("lens,Hq,Hk,N,dk,dv,page,window,sinks,causal", [
+    ([16384], 8, 2, 1, 128, 128, 64, 0, 0, True),                    # 16 CTAs, eight tiles each
+    ([5000, 16300], 2, 2, 3, 64, 128, 16, 0, 0, True),               # 16, lengths apart
+    ([8100], 32, 8, 4, 128, 128, 16, 0, 0, True),                    # 8
+    ([7000, 8192], 12, 6, 2, 128, 64, 48, 0, 0, False),              # 8, later tokens seen
+    ([100000], 32, 8, 1, 128, 128, 128, 7500, 130, True),            # 8, a window
+    ([2100], 32, 2, 8, 64, 64, 32, 0, 0, True),                      # 16, all 128 rows
+    ([4096, 1, 0, 3000], 32, 8, 1, 128, 128, 16, 0, 0, True),        # 4
+    ([1800, 2000, 5, 1999, 129, 2048], 16, 8, 5, 64, 64, 48, 0, 0, True),          # 2
+    ([1000, 512, 900, 3, 128, 0, 640, 1024] * 2, 16, 8, 2, 128, 128, 16, 0, 0, True),   # 1: no clusters
+    ([1000, 512, 900, 3, 128, 0, 640, 1025] * 2, 16, 8, 2, 128, 128, 16, 0, 0, True),   # more tiles: equal shares
+    ([700] * 20, 16, 8, 2, 128, 64, 16, 200, 3, True),               # more items than SMs: equal shares
+])
+def test_few_query_rows(lens, Hq, Hk, N, dk, dv, page, window, sinks, causal):
+    """Every size of a cluster and its neighbours, at the most tiles a CTA."""
+    test_cache(lens, Hq, Hk, N, dk, dv, page, window, sinks, causal, "bf16")
+
+
+@pytest.mark.parametrize("B,L", [(1, 8000), (4, 4000), (8, 2000), (16, 1000), (10, 4000)])
+def test_hidden_values_that_are_not_numbers_in_clusters_and_shares(B, L):
+    """The last token's values: not numbers, seen by the second of two queries only."""
+    Hq, Hk, N, d, page = 16, 8, 2, 128, 16
+    g = torch.Generator(device="cuda").manual_seed(B)
+    pool, table, rows = cache(g, [L] * B, Hk, page, d, d, "bf16")
+    q = rand(g, B, Hq, N, d, dtype="bf16", scale=1.5)
+    ln = torch.full((B,), L, dtype=torch.int32, device="cuda")
+    t = L - 1
+    pool[table[B - 1, t // page].long(), 2, t % page, d:] = float("nan")
+    o, lse = pkg.kv_attn_lse(q, pool, table, ln)
+    assert pkg.get_device_status() == _lib.MOA_OK
+    assert bool(torch.isnan(o[B - 1, 4:6, 1]).all()) and int(torch.isnan(o).sum()) == 2 * d
+    see = seen(N, L, L, 0, 0)
+    for b, h in ((B - 1, 4), (B - 1, 5), (B - 1, 6), (0, 0)):
+        x = rows[b][h // 2]
+        clean = torch.nan_to_num(x[:, d:].double())
+        ro, bound, rl, _ = reference(q[b, h], x[:, :d], clean, see, "bf16")
+        assert bool(((o[b, h, :1].double() - ro[:1]).abs() <= bound[:1]).all())
+        if h != 4 and h != 5:
+            assert bool(((o[b, h].double() - ro).abs() <= bound).all())
