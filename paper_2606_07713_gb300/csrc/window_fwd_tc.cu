@@ -374,7 +374,7 @@ __device__ __noinline__ void cluster_rows(const __nv_bfloat16* Q, __nv_bfloat16*
 #pragma unroll 2
       for (int k = 0; k < p.cluster; ++k) {
         const float2 ml = stat[k * rows + at];
-        if (ml.x == -INFINITY) continue;   // its tiles held nothing that the row sees, or it had none
+        if (ml.x == -INFINITY && ml.y == 0.f) continue;   // its tiles held nothing that the row sees, or it had none
         const float f = ex2_approx(ml.x - M);
         L += f * ml.y;
 #pragma unroll

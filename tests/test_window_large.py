@@ -340,3 +340,21 @@ def test_hidden_values_that_are_not_numbers_in_clusters_and_shares(B, L):
         assert bool(((o[b, h, :1].double() - ro[:1]).abs() <= bound[:1]).all())
         if h != 4 and h != 5:
             assert bool(((o[b, h].double() - ro).abs() <= bound).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("lens", [[100], [300, 100], [1500, 40, 129], [200] * 20])
+def test_queries_that_are_not_numbers(lens, dtype):
+    """One such query of a head: its output and log-sum-exp are not numbers, in tiles that it sees in part too (their maximum
+    is then that of the hidden scores), and no other row changes."""
+    Hq, Hk, N, d = 8, 4, 3, 64
+    g = torch.Generator(device="cuda").manual_seed(len(lens))
+    pool, table, _ = cache(g, lens, Hk, 32, d, d, dtype)
+    q = rand(g, len(lens), Hq, N, d, dtype=dtype)
+    ln = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    good, good_lse = pkg.kv_attn_lse(q, pool, table, ln, window=50, sinks=2)
+    q[-1, 5, 1, 7] = float("nan")
+    o, lse = pkg.kv_attn_lse(q, pool, table, ln, window=50, sinks=2)
+    assert bool(torch.isnan(o[-1, 5, 1]).all()) and bool(torch.isnan(lse[-1, 5, 1]))
+    o[-1, 5, 1], lse[-1, 5, 1] = good[-1, 5, 1], good_lse[-1, 5, 1]
+    assert torch.equal(o, good) and torch.equal(lse, good_lse)
