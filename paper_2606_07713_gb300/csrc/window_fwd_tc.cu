@@ -18,7 +18,7 @@
 //
 // Work items (key head, chunk of heads, 128 QT rows) count in 128-token tiles; all items' tiles are cut into equal
 // shares, one for each SM (one CTA fills an SM), and a CTA walks over its share.  Cut items are joined by a
-// second kernel.  Few items of one row tile go to a cluster each, whose CTAs join them in the same launch.  QT = 2 where there are more rows than a tile holds: keys and values in shared memory then serve
+// second kernel.  Few items (of one row tile then) go to a cluster each, whose CTAs join them in the same launch.  QT = 2 where there are more rows than a tile holds (and no clusters): keys and values in shared memory then serve
 // twice the rows.
 //
 // Hidden tokens: a tile that some row sees only in part is masked by words of bits, -infinity in place of the
@@ -303,30 +303,34 @@ struct Begin {
   int64_t item, unit, total;
 };
 
-// Rows of a CTA's whole items whose output is not finite, again: a softmax warp a row.  (A function of its own: what it holds
+// Rows of an item whose output is not finite, again: a softmax warp a row.  (Functions of their own: what they hold
 // would cost the softmax loop registers.)
 template <int DK, int DV, int QT>
-__device__ __noinline__ void whole_rows_again(const __nv_bfloat16* Q, __nv_bfloat16* O, const Params& p, const Begin* begin) {
+__device__ __noinline__ void item_rows_again(const __nv_bfloat16* Q, __nv_bfloat16* O, const Params& p, int item) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const Where w = where_of<QT>(p, item);
+  for (int r = warp; r < kBM * QT; r += 4 * QT) {
+    const int tile = r / kBM, in_tile = r - tile * kBM, row_pos = in_tile / p.GC;
+    const int g = w.chunk * p.GC + in_tile - row_pos * p.GC, hq = w.h * p.G + g, i = w.i0 + tile * p.PT + row_pos;
+    if (row_pos >= p.PT || g >= p.G || i >= p.N) continue;
+    __nv_bfloat16* o = O + int64_t(w.b) * p.o_sb + int64_t(hq) * p.o_sh + int64_t(i) * p.o_sn;
+    bool bad = false;
+    for (int e = lane; e < DV; e += 32) bad |= not_finite(__bfloat162float(o[e]));
+    if (__any_sync(0xffffffffu, bad))
+      exact_row<DK, DV>(Q + int64_t(w.b) * p.q_sb + int64_t(hq) * p.q_sh + int64_t(i) * p.q_sn, o, p, w.b, w.h, i);
+  }
+}
+
+// The same for a share's whole items.
+template <int DK, int DV, int QT>
+__device__ __noinline__ void whole_rows_again(const __nv_bfloat16* Q, __nv_bfloat16* O, const Params& p, const Begin* begin) {
   const Shares shares(begin->total, gridDim.x);
   const int64_t first_unit = shares.start(blockIdx.x), stop = shares.start(blockIdx.x + 1);
   int64_t before = begin->unit;
   for (int item = int(begin->item); before < stop; ++item) {
     const int64_t end = before + units_of<QT>(p, item, false) + item_units(QT);
     // its tiles, which come after its first units, are all in this share
-    if (before + item_units(QT) >= first_unit && end <= stop) {
-      const Where w = where_of<QT>(p, item);
-      for (int r = warp; r < kBM * QT; r += 4 * QT) {
-        const int tile = r / kBM, in_tile = r - tile * kBM, row_pos = in_tile / p.GC;
-        const int g = w.chunk * p.GC + in_tile - row_pos * p.GC, hq = w.h * p.G + g, i = w.i0 + tile * p.PT + row_pos;
-        if (row_pos >= p.PT || g >= p.G || i >= p.N) continue;
-        __nv_bfloat16* o = O + int64_t(w.b) * p.o_sb + int64_t(hq) * p.o_sh + int64_t(i) * p.o_sn;
-        bool bad = false;
-        for (int e = lane; e < DV; e += 32) bad |= not_finite(__bfloat162float(o[e]));
-        if (__any_sync(0xffffffffu, bad))
-          exact_row<DK, DV>(Q + int64_t(w.b) * p.q_sb + int64_t(hq) * p.q_sh + int64_t(i) * p.q_sn, o, p, w.b, w.h, i);
-      }
-    }
+    if (before + item_units(QT) >= first_unit && end <= stop) item_rows_again<DK, DV, QT>(Q, O, p, item);
     before = end;
   }
 }
@@ -530,7 +534,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = *tmem_slot;
-  const bool clustered = QT == 1 && p.cluster != 0;
+  const bool clustered = QT == 1 && p.cluster > 1;
   const int stages = clustered ? C::kStages - 2 : C::kStages;   // the last two receive a cluster's parts
   if (clustered) cluster_arrive();   // every thread waits for it once: the softmax threads before they write to other CTAs
   // A whole warp's wait: on expiry all its lanes leave together.
@@ -1001,7 +1005,12 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       return;
     }
   }
-  if (*any_odd != 0 && warp < C::kMmaWarp0) whole_rows_again<DK, DV, QT>(Q, O, p, found);
+  if (*any_odd != 0 && warp < C::kMmaWarp0) {
+    if (p.cluster != 0)
+      item_rows_again<DK, DV, QT>(Q, O, p, int(blockIdx.x));
+    else
+      whole_rows_again<DK, DV, QT>(Q, O, p, found);
+  }
 }
 
 // Joins the pieces of cut items: CTA (x, y) 32 / WS rows of CTA x's cut, four for every WS warps, eight lanes a row (a row a
@@ -1092,14 +1101,37 @@ constexpr int64_t kClusters16 = 7, kClusters8 = 14, kClusters4 = 34, kClusters2 
 // How the rows of a key head are divided.
 struct Plan {
   int64_t GC, chunks, PT, QT, n_tiles, n_items;
-  explicit Plan(const WindowArgs& a) {
+  int cluster;   // CTAs for each item; 0: equal shares
+  Plan(const WindowArgs& a, int sms) {
     const int64_t G = a.Hq / a.Hk;
     GC = G < kBM ? G : kBM;
     chunks = (G + GC - 1) / GC;
     PT = kBM / GC;
-    QT = a.N > PT ? 2 : 1;
-    n_tiles = chunks * ((a.N + QT * PT - 1) / (QT * PT));
+    // Few items: a cluster for each, the largest that all fit into the GPU at the same time, joined in the same launch, where that is
+    // no more than eight tiles a CTA (equal shares and the cluster, bf16, d = 128: 1 item of 128 tiles 23.9 and 18.2 us; 8 of 64:
+    // 20.2 and 17.8, of 128, sixteen a CTA: 24.0 and 26.2; 32 of 32: 24.9 and 19.2; 64 of 16: 23.9 and 19.2).  Where there are more
+    // rows than one tile's, sixteen: shares then come in two row tiles, whose items are longer (16 heads x 512 tokens 21.8 and
+    // 14.5; 64 queries of 32 / 8 heads against 8192 tokens 34.6 and 29.5).
+    int64_t tiles = (a.max_len + kBN - 1) / kBN;   // of tokens that an item of one row tile visits, at most
+    if (a.window != win::kNoWindow) {
+      const int64_t seen = (int64_t(a.window) + PT + kBN - 1) / kBN + 1 + (int64_t(a.sinks) + kBN - 1) / kBN;
+      if (seen < tiles) tiles = seen;
+    }
+    QT = 1;
+    n_tiles = chunks * ((a.N + PT - 1) / PT);
     n_items = a.B * a.Hk * n_tiles;
+    int64_t size = 16;
+    for (int64_t room : {kClusters16, kClusters8, kClusters4, kClusters2})
+      if (n_items > room) size /= 2;
+    cluster = 0;
+    if (n_items <= sms && tiles <= (a.N > PT ? 16 : 8) * size) {
+      cluster = 1;
+      while (cluster < size && cluster < tiles) cluster *= 2;
+    } else if (a.N > PT) {
+      QT = 2;
+      n_tiles = chunks * ((a.N + 2 * PT - 1) / (2 * PT));
+      n_items = a.B * a.Hk * n_tiles;
+    }
   }
 };
 
@@ -1186,21 +1218,9 @@ int launch(const WindowArgs& a, const Plan& plan, int sms, char* msg, size_t msg
   // tiles of tokens, if every sequence is as long as max_len and no window hides any
   const int64_t most_tiles = (a.max_len + kBN - 1) / kBN, most = plan.n_items * most_tiles;
   const unsigned ctas = unsigned(most < sms ? most : sms);
-  // Few items: a cluster for each, the largest that all fit into the GPU at the same time, joined in the same launch, where that is
-  // no more than eight tiles a CTA (equal shares and the cluster, bf16, d = 128: 1 item of 128 tiles 23.9 and 18.2 us; 8 of 64:
-  // 20.2 and 17.8, of 128, sixteen a CTA: 24.0 and 26.2; 32 of 32: 24.9 and 19.2; 64 of 16: 23.9 and 19.2).
   if constexpr (QT == 1) {
-    int64_t tiles = most_tiles;
-    if (a.window != win::kNoWindow) {
-      const int64_t seen = (int64_t(a.window) + plan.PT + kBN - 1) / kBN + 1 + (int64_t(a.sinks) + kBN - 1) / kBN;
-      if (seen < tiles) tiles = seen;
-    }
-    int64_t size = 16;
-    for (int64_t room : {kClusters16, kClusters8, kClusters4, kClusters2})
-      if (plan.n_items > room) size /= 2;
-    if (tiles <= 8 * size && plan.n_items <= sms) {
-      p.cluster = 1;
-      while (p.cluster < size && p.cluster < tiles) p.cluster *= 2;
+    if (plan.cluster != 0) {
+      p.cluster = plan.cluster;
       if (p.cluster > 8) e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kern), cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
       if (e == cudaSuccess)
         e = launch_clusters(kern, dim3(unsigned(plan.n_items), unsigned(p.cluster)), unsigned(p.cluster), dim3(C::kThreads),
@@ -1241,7 +1261,7 @@ int launch(const WindowArgs& a, const Plan& plan, int sms, char* msg, size_t msg
 
 template <int DK, int DV>
 int launch_rows(const WindowArgs& a, int sms, char* msg, size_t msglen) {
-  const Plan plan(a);
+  const Plan plan(a, sms);
   if (a.kv.table != nullptr)
     return plan.QT == 2 ? launch<DK, DV, 2, true>(a, plan, sms, msg, msglen) : launch<DK, DV, 1, true>(a, plan, sms, msg, msglen);
   return plan.QT == 2 ? launch<DK, DV, 2, false>(a, plan, sms, msg, msglen) : launch<DK, DV, 1, false>(a, plan, sms, msg, msglen);
@@ -1259,7 +1279,7 @@ bool window_tc_takes(const WindowArgs& a) {
          describable(a.kv.v_sb, outer);
 }
 
-size_t window_tc_workspace(const WindowArgs& a, int sms) { return size_t(Work(a, Plan(a), sms).bytes); }
+size_t window_tc_workspace(const WindowArgs& a, int sms) { return size_t(Work(a, Plan(a, sms), sms).bytes); }
 
 int launch_window_tc(const WindowArgs& a, int sms, char* msg, size_t msglen) {
   if (a.dk == 64) return a.dv == 64 ? launch_rows<64, 64>(a, sms, msg, msglen) : launch_rows<64, 128>(a, sms, msg, msglen);

@@ -358,3 +358,49 @@ def test_queries_that_are_not_numbers(lens, dtype):
     assert bool(torch.isnan(o[-1, 5, 1]).all()) and bool(torch.isnan(lse[-1, 5, 1]))
     o[-1, 5, 1], lse[-1, 5, 1] = good[-1, 5, 1], good_lse[-1, 5, 1]
     assert torch.equal(o, good) and torch.equal(lse, good_lse)
+
+
+@pytest.mark.parametrize("lens,Hq,Hk,N,dk,dv,page,window,sinks,causal", [
+    ([8192], 32, 8, 64, 128, 128, 16, 0, 0, True),           # clusters: 4 CTAs, 16 tiles each
+    ([16000], 4, 1, 100, 64, 128, 48, 0, 0, True),           # 16
+    ([4096, 70, 64, 3000], 32, 8, 64, 128, 64, 64, 0, 0, True),   # 2, lengths apart
+    ([300, 200, 130], 9, 3, 130, 64, 64, 16, 90, 5, False),  # rows that no head fills, later tokens seen
+    ([260], 200, 1, 3, 64, 64, 32, 0, 0, True),              # two chunks of heads
+    ([40, 10], 6, 3, 130, 128, 128, 16, 0, 0, True),         # more queries than tokens
+    ([8192 + 2048] * 2, 32, 8, 64, 128, 128, 16, 0, 0, True),     # one step more: equal shares
+])
+def test_more_rows_than_a_tile(lens, Hq, Hk, N, dk, dv, page, window, sinks, causal):
+    test_cache(lens, Hq, Hk, N, dk, dv, page, window, sinks, causal, "bf16")
+
+
+@pytest.mark.parametrize("B,Hq,Hk,N,M,dk,dv,window,sinks", [
+    (3, 9, 3, 1500, 1700, 64, 64, 0, 0),      # heads that leave rows of a tile empty
+    (3, 9, 3, 1501, 1501, 128, 64, 77, 5),
+    (1, 200, 1, 203, 190, 64, 128, 33, 2),    # two chunks of heads, more queries than keys
+    (7, 5, 5, 777, 901, 128, 128, 130, 1),
+    (40, 4, 2, 300, 300, 64, 64, 0, 0),
+])
+def test_two_row_tiles(B, Hq, Hk, N, M, dk, dv, window, sinks):
+    """Odd shapes with more work items than SMs, which take two row tiles each."""
+    test_window("bf16", B, Hq, Hk, N, M, dk, dv, window, sinks)
+
+
+@pytest.mark.parametrize("B,N", [(4, 1500), (1, 200)])
+def test_hidden_values_that_are_not_numbers_without_pages(B, N):
+    """Whole items of two row tiles and of one: a token's values that are not finite change only the rows that see it."""
+    Hq, Hk, d, window = 8, 4, 64, 100
+    g = torch.Generator(device="cuda").manual_seed(N)
+    q, k, v = (rand(g, B, h, N, d, dtype="bf16", scale=1.5) for h in (Hq, Hk, Hk))
+    clean = v.clone()
+    t = N // 2
+    v[-1, 1, t] = float("inf")
+    o, lse = pkg.window_attn_lse(q, k, v, window=window)
+    assert pkg.get_device_status() == _lib.MOA_OK
+    assert bool(torch.isinf(o[-1, 2:4, t:t + window]).all()) and int(torch.isfinite(o).logical_not().sum()) == 2 * window * d
+    see = seen(N, N, N, window, 0)
+    for b, h in ((B - 1, 2), (B - 1, 3), (B - 1, 0), (0, 7)):
+        ro, bound, _, _ = reference(q[b, h], k[b, h // 2], clean[b, h // 2], see, "bf16")
+        ok = (o[b, h].double() - ro).abs() <= bound
+        if b == B - 1 and h // 2 == 1:
+            ok[t:t + window] = True
+        assert bool(ok.all())
