@@ -1111,7 +1111,7 @@ struct Plan {
     // no more than eight tiles a CTA (equal shares and the cluster, bf16, d = 128: 1 item of 128 tiles 23.9 and 18.2 us; 8 of 64:
     // 20.2 and 17.8, of 128, sixteen a CTA: 24.0 and 26.2; 32 of 32: 24.9 and 19.2; 64 of 16: 23.9 and 19.2).  Where there are more
     // rows than one tile's, sixteen: shares then come in two row tiles, whose items are longer (16 heads x 512 tokens 21.8 and
-    // 14.5; 64 queries of 32 / 8 heads against 8192 tokens 34.6 and 29.5).
+    // 10.7; 64 queries of 32 / 8 heads against 8192 tokens 34.6 and 29.5).
     int64_t tiles = (a.max_len + kBN - 1) / kBN;   // of tokens that an item of one row tile visits, at most
     if (a.window != win::kNoWindow) {
       const int64_t seen = (int64_t(a.window) + PT + kBN - 1) / kBN + 1 + (int64_t(a.sinks) + kBN - 1) / kBN;
@@ -1126,7 +1126,10 @@ struct Plan {
     cluster = 0;
     if (n_items <= sms && tiles <= (a.N > PT ? 16 : 8) * size) {
       cluster = 1;
-      while (cluster < size && cluster < tiles) cluster *= 2;
+      // Many rows cost the join about what three tiles do: those then stay together (16 heads x 512 tokens of 128 rows a tile 14.5 us in
+      // pairs and 10.7 alone; 64 rows against 1024 tokens 10.3 in eights and 13.6 in pairs).
+      const int64_t rows = (a.N < PT ? a.N : PT) * GC, least = rows > 64 ? 4 : 1;
+      while (cluster < size && cluster * least < tiles) cluster *= 2;
     } else if (a.N > PT) {
       QT = 2;
       n_tiles = chunks * ((a.N + 2 * PT - 1) / (2 * PT));
