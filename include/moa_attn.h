@@ -524,7 +524,7 @@ size_t moa_window_attn_workspace_bytes(int64_t B, int64_t H_q, int64_t H_k, int6
  * Tokens that no query sees get zeros, and so do queries that see nothing.  Inputs are finite: one that
  * is not can make the gradients of its neighbours (128 rows, 128 tokens) NaN that it does not reach by the
  * formula.  Accumulation in fp32; bf16: weights and dS are rounded to bf16 once.  dQ, dK and dV may be
- * slices of one buffer where d_k = d_v and N_q = N_k.  Bounded waits as moa_attn_fwd.  Bitwise
+ * slices of one buffer where N_q = N_k (dK and dV always).  Bounded waits as moa_attn_fwd.  Bitwise
  * reproducible.
  */
 int moa_window_attn_bwd(const void* Q, const void* K, const void* V, const void* O, const void* dO,
@@ -553,7 +553,8 @@ size_t moa_kv_pool_bytes(int64_t n_pages, int64_t H, int64_t page_tokens, int64_
  * moa_kv_append -- writes rows of keys and values into the pool, keys rotated by their positions' angles
  * on the way, and rotates the queries beside them.
  *   K [B, H_k, N, d_k], V [B, H_k, N, d_v]  inputs, the pool's element type
- *   Q, Qo     [B, H_q, N, d_k] input and output, or both null.  Qo may be Q with the same strides (in place)
+ *   Q, Qo     [B, H_q, N, d_k] input and output, or both null.  Qo may be Q with the same strides (in place),
+ *             and may be a slice of one buffer with K and V
  *   cos, sin  float32 [n_pos, d_rot / 2], contiguous, 16-byte aligned, or both null (nothing is rotated; Q
  *             must be null then).  Pairs and formula of moa_qk_norm_rope; d_rot a multiple of 16 up to d_k
  *   pages     int32 [B, max_pages];  pos  int32 [B, N], the tokens' positions; negative: nothing is

@@ -93,11 +93,11 @@ bool same_view(const View& a, const View& b) {
   return a.p == b.p && a.sb == b.sb && a.sh == b.sh && a.sn == b.sn;
 }
 
-// Whether two tensors of the same B, N and d whose spans meet are slices of one buffer that share no
+// Whether two tensors of the same B and N whose spans meet are slices of one buffer that share no
 // element: equal strides along B and N, and heads that lie apart.  The buffer's dimensions may be in any
-// order: with k of B and N (those of the smaller strides) inside a head, a head is a piece of `inner`
-// elements; the two tensors' pieces must lie apart, one tensor's after the other's or in turn, and all of
-// them within the strides of the dimensions outside.
+// order: with k of B and N (those of the smaller strides) inside a head, a head is a piece of `in_a` or
+// `in_b` elements (rows may differ in length); the two tensors' pieces must lie apart, one tensor's after the
+// other's or in turn, and all of them within the strides of the dimensions outside.
 bool disjoint_slices(const View& a, const Shape& sa, const View& b, const Shape& sb, int64_t elt) {
   if ((sa.B > 1 && a.sb != b.sb) || (sa.N > 1 && a.sn != b.sn)) return false;
   if (a.sh < 0 || b.sh < 0 || a.sn < 0 || a.sb < 0) return false;
@@ -109,18 +109,19 @@ bool disjoint_slices(const View& a, const Shape& sa, const View& b, const Shape&
     std::swap(stride[0], stride[1]);
     std::swap(size[0], size[1]);
   }
-  int64_t inner = sa.d;
+  int64_t in_a = sa.d, in_b = sb.d;
   for (int k = 0; k <= 2; ++k) {
     if (k > 0) {
-      if (size[k - 1] > 1 && stride[k - 1] < inner) return false;   // rows on one another
-      inner += (size[k - 1] - 1) * stride[k - 1];
+      if (size[k - 1] > 1 && (stride[k - 1] < in_a || stride[k - 1] < in_b)) return false;   // rows on one another
+      in_a += (size[k - 1] - 1) * stride[k - 1];
+      in_b += (size[k - 1] - 1) * stride[k - 1];
     }
-    if ((sa.H > 1 && a.sh < inner) || (sb.H > 1 && b.sh < inner)) continue;
-    const int64_t end_a = (sa.H - 1) * a.sh + inner, end_b = off + (sb.H - 1) * b.sh + inner;
+    if ((sa.H > 1 && a.sh < in_a) || (sb.H > 1 && b.sh < in_b)) continue;
+    const int64_t end_a = (sa.H - 1) * a.sh + in_a, end_b = off + (sb.H - 1) * b.sh + in_b;
     bool apart = end_a <= off || end_b <= 0;
     if (!apart && sa.H > 1 && sb.H > 1 && a.sh == b.sh) {
       const int64_t turn = (off % a.sh + a.sh) % a.sh;   // where b's pieces lie between a's
-      apart = turn >= inner && turn + inner <= a.sh;
+      apart = turn >= in_a && turn + in_b <= a.sh;
     }
     if (!apart) continue;
     int64_t whole = (end_a > end_b ? end_a : end_b) - (off < 0 ? off : 0);
@@ -403,7 +404,7 @@ constexpr float kMostScale = 2e38f;   // times log2 e still finite
 
 // Two tensors that may share a buffer without sharing an element.
 bool apart(const View& a, const Shape& sa, const View& b, const Shape& sb, int64_t elt) {
-  return sa.d == sb.d && sa.N == sb.N && sa.B == sb.B && disjoint_slices(a, sa, b, sb, elt);
+  return sa.N == sb.N && sa.B == sb.B && disjoint_slices(a, sa, b, sb, elt);
 }
 
 struct Tensor {
