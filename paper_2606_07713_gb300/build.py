@@ -23,12 +23,12 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(BUILD, "libmoa_attn.so")
 SOURCES = ["moa_attn_api.cu", "attn_fwd_f32_cc.cu", "attn_fwd_bf16_tc.cu", "attn_bwd_bf16_tc.cu",
            "attn_bwd_f32_cc.cu", "qkv_proj_bf16_tc.cu", "moa_ops_api.cu", "qk_norm_rope.cu",
-           "kv4_cache.cu", "kv4_attn.cu", "kv4_attn_tc.cu", "kv_append.cu", "window_fwd_cc.cu", "window_fwd_tc.cu",
-           "window_bwd_cc.cu", "window_bwd_tc.cu"]
+           "kv4_cache.cu", "kv4_attn.cu", "kv4_attn_tc.cu", "kv_append.cu", "window_map.cu", "window_fwd_cc.cu",
+           "window_fwd_tc.cu", "window_bwd_cc.cu", "window_bwd_tc.cu"]
 BINDING = os.path.join(BUILD, "moa_torch.so")
 BINDING_SOURCE = "torch_binding.cpp"
 BINDING_TORCH = BINDING + ".torch"   # which PyTorch it was built against
-HEADERS = ["internal.h", "ops_internal.h", "kv4.cuh", "window.cuh", "ptx.cuh", "tc_common.cuh"]
+HEADERS = ["internal.h", "ops_internal.h", "kv4.cuh", "window.cuh", "window_tc.cuh", "ptx.cuh", "tc_common.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
 

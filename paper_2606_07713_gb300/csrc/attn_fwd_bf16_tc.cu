@@ -694,24 +694,6 @@ bool encode_bf16_map_box(CUtensorMap* map, const void* base, int64_t BH, int64_t
   return true;
 }
 
-bool encode_bf16_map_nd(CUtensorMap* map, const void* base, int rank, const uint64_t* dims, const uint64_t* strides,
-                        const uint32_t* box, char* msg, size_t msglen) {
-  EncodeTiledFn enc = get_encode_fn(msg, msglen);
-  if (!enc) return false;
-  cuuint64_t d[5], st[4];
-  cuuint32_t bx[5], es[5];
-  for (int i = 0; i < rank; ++i) d[i] = dims[i], bx[i] = box[i], es[i] = 1;
-  for (int i = 0; i + 1 < rank; ++i) st[i] = strides[i];
-  const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, cuuint32_t(rank), const_cast<void*>(base), d, st, bx, es,
-                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r != CUDA_SUCCESS) {
-    snprintf(msg, msglen, "cuTensorMapEncodeTiled failed (%d) for a tensor of %d dimensions", int(r), rank);
-    return false;
-  }
-  return true;
-}
-
 // 3-D map over a contiguous fp32 [BH, N, d] tensor; box = box_cols columns (32: one 128-byte
 // swizzle row) x box_rows rows x 1 slice, 128-byte swizzle.
 bool encode_f32_map_sw128(CUtensorMap* map, const void* base, int64_t BH, int64_t N, int64_t d,

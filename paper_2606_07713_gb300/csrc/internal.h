@@ -74,11 +74,6 @@ bool encode_f32_map_sw128(CUtensorMap* map, const void* base, int64_t BH, int64_
 bool encode_bf16_map_box(CUtensorMap* map, const void* base, int64_t BH, int64_t N, int64_t d,
                          int box_rows, char* msg, size_t msglen);
 
-// Map over a bf16 tensor of 2 to 5 dimensions, the innermost contiguous; sizes and the box from the
-// innermost on, strides in bytes from the second on.  128-byte swizzle, zeros past the end.
-bool encode_bf16_map_nd(CUtensorMap* map, const void* base, int rank, const uint64_t* dims, const uint64_t* strides,
-                        const uint32_t* box, char* msg, size_t msglen);
-
 // Validated arguments of one projection call (see include/moa_attn.h, moa_qkv_proj).
 struct ProjArgs {
   const void* X;  // [B, N, d]

@@ -48,6 +48,7 @@
 #include "ptx.cuh"
 #include "tc_common.cuh"
 #include "window.cuh"
+#include "window_tc.cuh"
 
 namespace moa {
 
@@ -57,6 +58,7 @@ namespace {
 
 using namespace ptx;
 using namespace tc;
+using win::below, win::describable, win::map_stride, win::tma_load_4d, win::tma_load_5d;
 
 constexpr int kBlk = 128;                // tokens of dK's and dV's tiles, rows of dQ's
 constexpr int kHalf = 64;                // rows of half a row tile
@@ -125,12 +127,6 @@ __device__ __forceinline__ float4 lds_f32x4(uint32_t addr) {
   asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
   return v;
 }
-// Bits 32 w .. 32 w + 31 of the number with the lowest x bits set.
-__device__ __forceinline__ uint32_t below(int x, int w) {
-  const int n = x - 32 * w;
-  return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u;
-}
-
 // NCOLS fp32 TMEM columns of this thread's lane, times mul: as bf16 to dst, or as they are to part.
 template <int NCOLS>
 __device__ __forceinline__ void store_row(uint32_t taddr, float mul, __nv_bfloat16* dst, float* part, bool valid) {
@@ -1004,9 +1000,6 @@ struct Work {
     bytes = part_q + (p.q_pieces > 1 ? p.pairs * p.q_pieces * kBlk * a.dk * 4 : 0);
   }
 };
-
-bool describable(int64_t stride, int64_t size) { return size == 1 || (stride > 0 && stride < (int64_t(1) << 39)); }
-uint64_t map_stride(int64_t stride, int64_t size) { return size == 1 ? 16 : uint64_t(stride) * 2; }
 
 template <int DK, int DV>
 int launch(const WindowBwdArgs& a, char* msg, size_t msglen) {

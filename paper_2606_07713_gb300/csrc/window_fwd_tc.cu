@@ -50,6 +50,7 @@
 #include "ptx.cuh"
 #include "tc_common.cuh"
 #include "window.cuh"
+#include "window_tc.cuh"
 
 namespace moa {
 
@@ -59,6 +60,7 @@ namespace {
 
 using namespace ptx;
 using namespace tc;
+using win::below, win::describable, win::map_stride, win::tma_load_4d, win::tma_load_5d;
 
 constexpr int kBM = 128;              // rows of a row tile (= TMEM lanes)
 constexpr int kBN = 128;              // tokens of a tile
@@ -223,12 +225,6 @@ __device__ __forceinline__ void tmem_scale_row(uint32_t taddr, float alpha) {
     tmem_st_32x32b_x32(taddr + c, o);
   }
   tmem_wait_st();
-}
-
-// Bits 32 w .. 32 w + 31 of the number with the lowest x bits set.
-__device__ __forceinline__ uint32_t below(int x, int w) {
-  const int n = x - 32 * w;
-  return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u;
 }
 
 __device__ __forceinline__ bool not_finite(float x) { return !(fabsf(x) < INFINITY); }
@@ -1149,10 +1145,6 @@ struct Work {
     bytes = cuts + round_up(int64_t(sms) * sizeof(Cut), 256);
   }
 };
-
-// A tensor's stride as a tensor map has it: positive, whole 16 bytes, below 2^40 bytes.
-bool describable(int64_t stride, int64_t size) { return size == 1 || (stride > 0 && stride < (int64_t(1) << 39)); }
-uint64_t map_stride(int64_t stride, int64_t size) { return size == 1 ? 16 : uint64_t(stride) * 2; }
 
 template <int DK, int DV, int QT, bool PAGED>
 int launch(const WindowArgs& a, const Plan& plan, int sms, char* msg, size_t msglen) {
