@@ -23,9 +23,11 @@
 //
 // Hidden tokens: a tile that some row sees only in part is masked by words of bits, -infinity in place of the
 // score.  Past a sequence's end the cache may hold anything: the softmax threads zero the values' rows there in
-// shared memory before the product.  Any other hidden value that is not finite (0 * NaN) makes the output NaN;
-// rows whose output is not finite are computed again at the end, token by token, from what they do see
-// (exact_row).  That costs nothing where all values are finite.
+// shared memory before the product.  Any other hidden value that is not finite reaches all rows of the product (0 * NaN).  So an
+// item with an output that is not finite, though its row's sum of weights is a number, is computed once more when the CTA is done
+// with the others (redo_piece): tile after tile without overlap, with the values of its partly hidden tiles looked through in shared
+// memory; those that are not finite are taken out before the product, and added at the end to the rows that do see them.  A call all of
+// whose values are infinite or NaN takes some five times as long as one without; other calls pay nothing.
 //
 // What bounds it.  Many rows: a softmax warp's chain of score load, maximum, 128 exponentials and stores beside the products
 // (32768 tokens, 32 / 8 heads of 128, window 4096: 1500 us = 1.37 PFLOP/s of what is seen, tensor pipe 64 %; 2048 queries against 16384 cached
@@ -67,6 +69,7 @@ constexpr int kBN = 128;              // tokens of a tile
 // What an item costs besides its tiles, in tiles (48 sequences of one query with 0, 1, 2, 4: 204, 195, 189, 192 us; 4 x 16 heads x
 // 2048 x 64, causal, with 1, 2, 3, 4: 66.7, 64.7, 65.2, 66.7, a chunk of 2048 queries 363, 364, 361, 363).
 __host__ __device__ constexpr int item_units(int QT) { return QT == 2 ? 3 : 2; }
+constexpr int kAgain = 256;           // pieces of a share that are marked one by one; the last bit is for all that follow
 constexpr float kRescaleLog2 = 8.f;   // the running maximum may lag by this: weights up to 2^8
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -87,11 +90,12 @@ struct Cfg {
   static constexpr int kStages = (229376 - kOffKV) / kStageBytes < 8 ? (229376 - kOffKV) / kStageBytes : 8;
   static constexpr int kOffBar = kOffKV + kStages * kStageBytes;
   // barriers: full[NS], empty[NS], q_full, q_empty, drain, s_full[2], p_ready[2], o_done[2], s_free[2], p_free[2],
-  // item_full[2], item_empty[2]
-  static constexpr int kNumBars = 2 * kStages + 17;
+  // item_full[2], item_empty[2], redo_loaded, redo_done
+  static constexpr int kNumBars = 2 * kStages + 19;
   static constexpr int kOffMisc = kOffBar + kNumBars * 8;
-  static constexpr int kOffItems = (kOffMisc + 12 + 15) / 16 * 16;   // two items, then scan[12] and the share's beginning
-  static constexpr int kOffSums = (kOffItems + 2 * 32 + 15 * 8 + 15) / 16 * 16;   // m and l of a row, for the cluster (QT = 1)
+  static constexpr int kOffItems = (kOffMisc + 16 + 15) / 16 * 16;   // two items, then scan[12] and the share's beginning
+  static constexpr int kOffAgain = kOffItems + 2 * 32 + 15 * 8;      // kAgain bits: pieces of the share to compute once more
+  static constexpr int kOffSums = (kOffAgain + kAgain / 8 + 15) / 16 * 16;   // m and l of a row, for the cluster (QT = 1)
   static constexpr int kSmemBytes = kOffSums + (QT == 1 ? kBM * 8 : 0) + 1024;
   // Exponentials, in chunks of 32 tokens, before the wait for P's buffer (2, 3, 4 of 4 at d_v = 128: 1566, 1525, 1545 us of 32768
   // tokens; 1 to 4 at d_v = 64: 65.2, 64.5, 65.1, 67.0 us of 4 x 16 heads x 2048, causal).
@@ -113,7 +117,7 @@ struct Layout {
 };
 
 struct Params {
-  int64_t q_sb, q_sh, q_sn, o_sb, o_sh, o_sn;
+  int64_t o_sb, o_sh, o_sn;
   KvSource kv;
   const int32_t* lens;   // null: every sequence has max_len tokens
   int N, max_len, Hk, G;
@@ -227,54 +231,6 @@ __device__ __forceinline__ void tmem_scale_row(uint32_t taddr, float alpha) {
   tmem_wait_st();
 }
 
-__device__ __forceinline__ bool not_finite(float x) { return !(fabsf(x) < INFINITY); }
-
-// One row again, token by token over what it sees: a warp, 4 features a lane.
-template <int DK, int DV>
-__device__ __noinline__ void exact_row(const __nv_bfloat16* q, __nv_bfloat16* o, const Params& p, int b, int h, int i) {
-  const int lane = threadIdx.x & 31;
-  constexpr int NK = DK / 32, NV = DV / 32;
-  float x[NK], acc[NV];
-#pragma unroll
-  for (int e = 0; e < NK; ++e) x[e] = __bfloat162float(q[lane * NK + e]);
-#pragma unroll
-  for (int e = 0; e < NV; ++e) acc[e] = 0.f;
-  const int len = length_of(p, b, false);
-  const int end = win::row_end(p.mask, len, p.N, i), low = win::row_low(p.mask, len, p.N, i);
-  float m = -INFINITY, l = 0.f;
-  for (int t = 0; t < end; ++t) {
-    if (t >= p.mask.sinks && t < low) {
-      t = low;
-      if (t >= end) break;
-    }
-    int64_t at = b, place = t;
-    bool there = true;
-    if (p.kv.table != nullptr) {
-      const int slot = t / p.kv.page;
-      at = p.kv.table[b * p.kv.max_pages + slot];
-      place = t - slot * p.kv.page;
-      there = at >= 0 && at < p.kv.n_pages;
-    }
-    const __nv_bfloat16* k = static_cast<const __nv_bfloat16*>(p.kv.k) + at * p.kv.k_sb + h * p.kv.k_sh + place * p.kv.k_sn;
-    const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(p.kv.v) + at * p.kv.v_sb + h * p.kv.v_sh + place * p.kv.v_sn;
-    float s = 0.f;
-#pragma unroll
-    for (int e = 0; e < NK; ++e) s = fmaf(x[e], there ? __bfloat162float(k[lane * NK + e]) : 0.f, s);
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-    s *= p.c_log2;
-    const float m_new = fmaxf(m, s), base = m_new == -INFINITY ? 0.f : m_new;
-    const float alpha = exp2f(m - base), w = exp2f(s - base);
-    l = l * alpha + w;
-    m = m_new;
-#pragma unroll
-    for (int e = 0; e < NV; ++e) acc[e] = acc[e] * alpha + w * (there ? __bfloat162float(v[lane * NV + e]) : 0.f);
-  }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-  for (int e = 0; e < NV; ++e) o[lane * NV + e] = __float2bfloat16(acc[e] * inv);
-}
-
 // Zeros in rows `row`, row + step, ... of a values' tile (of pages) that has arrived, from row `gone` on; false if it has not.  (A
 // function of its own: an item's last tile only.)
 template <int DV>
@@ -299,52 +255,6 @@ struct Begin {
   int64_t item, unit, total;
 };
 
-// Rows of an item whose output is not finite, again: a softmax warp a row.  (Functions of their own: what they hold
-// would cost the softmax loop registers.)
-template <int DK, int DV, int QT>
-__device__ __noinline__ void item_rows_again(const __nv_bfloat16* Q, __nv_bfloat16* O, const Params& p, int item) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const Where w = where_of<QT>(p, item);
-  for (int r = warp; r < kBM * QT; r += 4 * QT) {
-    const int tile = r / kBM, in_tile = r - tile * kBM, row_pos = in_tile / p.GC;
-    const int g = w.chunk * p.GC + in_tile - row_pos * p.GC, hq = w.h * p.G + g, i = w.i0 + tile * p.PT + row_pos;
-    if (row_pos >= p.PT || g >= p.G || i >= p.N) continue;
-    __nv_bfloat16* o = O + int64_t(w.b) * p.o_sb + int64_t(hq) * p.o_sh + int64_t(i) * p.o_sn;
-    bool bad = false;
-    for (int e = lane; e < DV; e += 32) bad |= not_finite(__bfloat162float(o[e]));
-    if (__any_sync(0xffffffffu, bad))
-      exact_row<DK, DV>(Q + int64_t(w.b) * p.q_sb + int64_t(hq) * p.q_sh + int64_t(i) * p.q_sn, o, p, w.b, w.h, i);
-  }
-}
-
-// The same for a share's whole items.
-template <int DK, int DV, int QT>
-__device__ __noinline__ void whole_rows_again(const __nv_bfloat16* Q, __nv_bfloat16* O, const Params& p, const Begin* begin) {
-  const Shares shares(begin->total, gridDim.x);
-  const int64_t first_unit = shares.start(blockIdx.x), stop = shares.start(blockIdx.x + 1);
-  int64_t before = begin->unit;
-  for (int item = int(begin->item); before < stop; ++item) {
-    const int64_t end = before + units_of<QT>(p, item, false) + item_units(QT);
-    // its tiles, which come after its first units, are all in this share
-    if (before + item_units(QT) >= first_unit && end <= stop) item_rows_again<DK, DV, QT>(Q, O, p, item);
-    before = end;
-  }
-}
-
-// Of the four rows that a warp's groups of eight lanes hold, those with a member that is `bad`, again.
-template <int DK, int DV>
-__device__ __forceinline__ void rows_again(const __nv_bfloat16* Q, __nv_bfloat16* O, const Params& p, const Where& w, bool bad,
-                                           int hq, int i) {
-  uint32_t again = __ballot_sync(0xffffffffu, bad);
-  while (again != 0) {
-    const int from = __ffs(again) - 1;
-    again &= ~(0xffu << (from & ~7));
-    const int h = __shfl_sync(0xffffffffu, hq, from), n = __shfl_sync(0xffffffffu, i, from);
-    exact_row<DK, DV>(Q + int64_t(w.b) * p.q_sb + int64_t(h) * p.q_sh + int64_t(n) * p.q_sn,
-                      O + int64_t(w.b) * p.o_sb + int64_t(h) * p.o_sh + int64_t(n) * p.o_sn, p, w.b, w.h, n);
-  }
-}
-
 // A cluster's item: CTA (r / 4) % size joins row r.  Every CTA leaves its part of the row there, in the last two stages of the
 // ring, which a cluster does not use for tiles: [CTA][row of the owner][DV], and m and l.  (Parts fetched by the owner instead
 // took 3 us more: two round trips and a second barrier.)
@@ -353,8 +263,8 @@ struct Owner {
 };
 __device__ __forceinline__ Owner owner_of(int r, int size) { return Owner{(r >> 2) % size, (r >> 2) / size * 4 + (r & 3)}; }
 
-template <int DK, int DV>
-__device__ __noinline__ void cluster_rows(const __nv_bfloat16* Q, __nv_bfloat16* O, float* lse, const Params& p, const float* sum,
+template <int DV>
+__device__ __noinline__ void cluster_rows(__nv_bfloat16* O, float* lse, const Params& p, const float* sum,
                                           const float2* stat) {
   // eight lanes a row
   constexpr int kQuads = DV / 32;
@@ -386,17 +296,468 @@ __device__ __noinline__ void cluster_rows(const __nv_bfloat16* Q, __nv_bfloat16*
     }
     const float inv = L == 0.f ? 0.f : 1.f / L;
     __nv_bfloat16* o = O + int64_t(w.b) * p.o_sb + int64_t(hq) * p.o_sh + int64_t(i) * p.o_sn;
-    bool bad = false;
 #pragma unroll
     for (int q = 0; q < kQuads; ++q) {
       x[q].x *= inv, x[q].y *= inv, x[q].z *= inv, x[q].w *= inv;
-      bad |= not_finite(x[q].x) || not_finite(x[q].y) || not_finite(x[q].z) || not_finite(x[q].w);
       if (live)
         *reinterpret_cast<uint2*>(o + (sub + 8 * q) * 4) = make_uint2(pack_bf16x2(x[q].x, x[q].y), pack_bf16x2(x[q].z, x[q].w));
     }
     if (lse != nullptr && live && sub == 0)
       lse[(int64_t(w.b) * p.Hk * p.G + hq) * p.N + i] = L == 0.f ? -INFINITY : (M + lg2_approx(L)) * kLn2;
-    rows_again<DK, DV>(Q, O, p, w, bad && live, hq, i);
+  }
+}
+
+// Looks through rows `row`, row + step, ... of a values' tile that has arrived.  From row `gone` on they become zeros; values
+// of the others that are not finite become zeros and set *odd to `mark`.  False if the tile has not arrived.  (In the softmax loop this
+// would cost 4 to 10 % of long calls; it is for redo_piece.)
+template <int DV, bool PAGED>
+__device__ __noinline__ bool look_through(uint8_t* tile, int row, int step, int gone, uint32_t full, uint32_t parity, volatile int* odd,
+                                          int mark, const WaitCtl& wc) {
+  using L = Layout<DV, PAGED>;
+  const bool ok = wait_bounded(full, parity, wc);
+  for (; row < kBN; row += step) {
+    // the row's 16-byte words, eight lanes in eight banks at a time
+    uint8_t* at = tile + (row >> 3) * L::kGroup + (row & 7) * 128;
+    auto word = [&](int q, int e) { return reinterpret_cast<uint4*>(at + q * L::kPanel + ((e ^ row) & 7) * 16); };
+    if (row >= gone) {
+#pragma unroll
+      for (int q = 0; q < DV / 64; ++q)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) *word(q, e) = make_uint4(0, 0, 0, 0);
+      continue;
+    }
+    // x * 0 + sum is NaN from the first x on that is not finite
+    const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
+    __nv_bfloat162 sum[4] = {zero, zero, zero, zero};
+#pragma unroll
+    for (int q = 0; q < DV / 64; ++q)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint4 x = *word(q, e);
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&w[i]), zero, sum[i]);
+      }
+    const __nv_bfloat162 all = __hadd2(__hadd2(sum[0], sum[1]), __hadd2(sum[2], sum[3]));
+    if (__low2float(all) == 0.f && __high2float(all) == 0.f) continue;
+    *odd = mark;
+    __threadfence_block();   // (the other row tile's warps may find the zeros)
+#pragma unroll 1
+    for (int e = 0; e < DV / 8; ++e) {
+      uint32_t* w = reinterpret_cast<uint32_t*>(word(e >> 3, e));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if ((w[i] & 0x7f80u) == 0x7f80u) w[i] &= 0xffff0000u;
+        if ((w[i] & 0x7f800000u) == 0x7f800000u) w[i] &= 0xffffu;
+      }
+    }
+  }
+  fence_proxy_async_smem();
+  return ok;
+}
+
+// Tiles of an item in which a token is hidden from one of its rows: end0 the end of its first row, low1 the beginning of its last one's
+// window.
+struct Partly {
+  int end0, low1;
+  __device__ __forceinline__ Partly(const win::Mask& m, int len, int N, int i0, int i1)
+      : end0(win::row_end(m, len, N, i0)), low1(win::row_low(m, len, N, i1)) {}
+  __device__ __forceinline__ bool operator()(int n0, int sinks) const {
+    return end0 - n0 < kBN || (n0 < low1 && n0 + kBN > sinks);
+  }
+};
+
+// Where token t's values lie; null: a page outside the pool.
+__device__ __forceinline__ const __nv_bfloat16* values_of(const Params& p, int b, int h, int t) {
+  int64_t at = b, place = t;
+  if (p.kv.table != nullptr) {
+    const int slot = int(unsigned(t) / unsigned(p.kv.page));
+    at = p.kv.table[b * p.kv.max_pages + slot];
+    place = t - slot * p.kv.page;
+    if (at < 0 || at >= p.kv.n_pages) return nullptr;
+  }
+  return static_cast<const __nv_bfloat16*>(p.kv.v) + at * p.kv.v_sb + h * p.kv.v_sh + place * p.kv.v_sn;
+}
+__device__ __forceinline__ bool odd_pair(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
+
+// Adds, to the sums in TMEM of a warp's rows, the values that look_through took out of tiles [u0, u1) and that the rows see: tokens below
+// lim from low on, or below the sinks.  Rows that are not `live` are left.  A row that has nothing but NaN is done.
+template <int DV>
+__device__ __noinline__ void add_odd_values(uint32_t tO, const Params& p, int b, int h, int len, int i0, int i1, const win::Tiles& list, int u0,
+                                            int u1, int lim, int low, bool live) {
+  const int lane = threadIdx.x & 31;
+  const Partly partly(p.mask, len, p.N, i0, i1);
+#pragma unroll 1
+  for (int c = 0; c < DV; c += 32) {
+    uint32_t o[32];
+    tmem_ld_32x32b_x32(tO + c, o);
+    tmem_wait_ld();
+    reg_anchor_x32(o);
+    auto open = [&]() {
+      bool any = false;
+#pragma unroll
+      for (int e = 0; e < 32; ++e) any |= __uint_as_float(o[e]) == __uint_as_float(o[e]);
+      return __any_sync(0xffffffffu, any && live);
+    };
+#pragma unroll 1
+    for (int n = u0; n < u1 && open(); ++n) {
+      const int n0 = list.at(n) * kBN;
+      if (!partly(n0, p.mask.sinks)) continue;
+#pragma unroll 1
+      for (int t0 = n0; t0 < n0 + kBN && t0 < len; t0 += 32) {
+        // a token a lane
+        const __nv_bfloat16* v = t0 + lane < len ? values_of(p, b, h, t0 + lane) : nullptr;
+        bool odd = false;
+        if (v != nullptr) {
+          v += c;
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) odd |= odd_pair(*reinterpret_cast<const uint32_t*>(v + e));
+        }
+        uint32_t rest = __ballot_sync(0xffffffffu, odd);
+        while (rest != 0) {
+          const int from = __ffs(rest) - 1, token = t0 + from;
+          rest &= rest - 1;
+          const __nv_bfloat16* x = reinterpret_cast<const __nv_bfloat16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(v), from));
+          if (live && token < lim && (token >= low || token < p.mask.sinks)) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              const float y = __bfloat162float(x[e]);
+              if (!(fabsf(y) < INFINITY)) o[e] = __float_as_uint(__uint_as_float(o[e]) + y);
+            }
+          }
+        }
+      }
+    }
+    tmem_st_32x32b_x32(tO + c, o);
+    tmem_wait_st();
+  }
+}
+
+// A row's place.
+struct Place {
+  int b, hq, i;
+  bool live;
+};
+template <int QT>
+__device__ __forceinline__ Place place_of(const Params& p, int item, int j, int row_pos, int row_head) {
+  const Where w = where_of<QT>(p, item);
+  const int g = w.chunk * p.GC + row_head, i = w.i0 + j * p.PT + row_pos;
+  return Place{w.b, w.h * p.G + g, i, row_pos < p.PT && g < p.G && i < p.N};
+}
+
+// Where an item's rows go.
+struct Out {
+  __nv_bfloat16* O;
+  float* lse;
+  float* part_o;
+  float2* part_ml;
+};
+// Writes a warp's rows of an item: the output, or this CTA's piece, or to the CTA of the cluster that joins the row.  Returns whether some
+// row has a sum that is not finite though its weights are numbers.
+template <int DK, int DV, int QT, bool ROLLED>
+__device__ __forceinline__ bool write_rows(const Params& p, const Out& out, const Place& w, uint32_t tO, uint32_t parts, int j, int row, float m,
+                                           float l, bool first_piece, bool whole) {
+  using C = Cfg<DK, DV, QT>;
+  constexpr int kUnroll = ROLLED ? 1 : DV / 16;
+  float top[4] = {0.f, 0.f, 0.f, 0.f};   // x * 0 + top is NaN from the first x on that is not finite
+  if (QT == 1 && p.cluster > 1) {   // the row's sums, to the CTA that joins it
+    const Owner own = owner_of(row, p.cluster);
+    const uint32_t sum = smem_of_cta(parts + ((int(blockIdx.y) * (kBM / p.cluster) + own.row) * DV) * 4, own.rank);
+#pragma unroll(kUnroll)
+    for (int d = 0; d < DV; d += 16) {
+      uint32_t o[16];
+      tmem_ld_32x32b_x16(tO + d, o);
+      tmem_wait_ld();
+      reg_anchor_x16(o);
+      if (w.live) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) store4_to_cta(sum + (d + 4 * e) * 4, o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top[e & 3] = fmaf(__uint_as_float(o[e]), 0.f, top[e & 3]);
+    }
+  } else if (!whole) {
+    const int64_t at = (int64_t(blockIdx.x) * 2 + first_piece) * C::kRows + j * kBM + row;
+#pragma unroll(kUnroll)
+    for (int d = 0; d < DV; d += 16) {
+      uint32_t o[16];
+      tmem_ld_32x32b_x16(tO + d, o);
+      tmem_wait_ld();
+      reg_anchor_x16(o);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top[e & 3] = fmaf(__uint_as_float(o[e]), 0.f, top[e & 3]);
+      if (w.live) {
+        float4* dst = reinterpret_cast<float4*>(out.part_o + at * DV + d);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          dst[e] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]),
+                               __uint_as_float(o[4 * e + 3]));
+      }
+    }
+    if (w.live) out.part_ml[at] = make_float2(m, l);
+  } else {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    __nv_bfloat16* orow = out.O + int64_t(w.b) * p.o_sb + int64_t(w.hq) * p.o_sh + int64_t(w.i) * p.o_sn;
+    if (out.lse != nullptr && w.live)
+      out.lse[(int64_t(w.b) * p.Hk * p.G + w.hq) * p.N + w.i] = l == 0.f ? -INFINITY : (m + lg2_approx(l)) * kLn2;
+#pragma unroll(kUnroll)
+    for (int d = 0; d < DV; d += 16) {
+      uint32_t o[16];
+      tmem_ld_32x32b_x16(tO + d, o);
+      tmem_wait_ld();
+      reg_anchor_x16(o);
+      uint32_t z[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float y0 = __uint_as_float(o[2 * e]) * inv, y1 = __uint_as_float(o[2 * e + 1]) * inv;
+        top[2 * e & 3] = fmaf(y0, 0.f, top[2 * e & 3]);
+        top[(2 * e + 1) & 3] = fmaf(y1, 0.f, top[(2 * e + 1) & 3]);
+        z[e] = pack_bf16x2(y0, y1);
+      }
+      if (w.live) {
+        reinterpret_cast<uint4*>(orow + d)[0] = make_uint4(z[0], z[1], z[2], z[3]);
+        reinterpret_cast<uint4*>(orow + d)[1] = make_uint4(z[4], z[5], z[6], z[7]);
+      }
+    }
+  }
+  return __any_sync(0xffffffffu, w.live && (top[0] + top[1]) + (top[2] + top[3]) != 0.f && l == l);
+}
+
+// The lane's copy of the tile of tokens from t0 (its own first token) on of a paged item: the first group of eight tokens of the pool.
+__device__ __forceinline__ int page_source(const Params& p, const Where& w, int t0, int end, int low) {
+  if (t0 < end && (t0 > low - p.box || t0 < p.mask.sinks)) {
+    const int at = int(unsigned(t0) / unsigned(p.kv.page));
+    const int pg = p.kv.table[w.b * p.kv.max_pages + at];
+    if (pg >= 0 && pg < p.kv.n_pages) return (pg * p.Hk + w.h) * p.page_groups + ((t0 - at * p.kv.page) >> 3);
+    atomicExch(&g_moa_window_tc_status, win::kErrIndex);
+  }
+  return p.all_groups;   // past the pool: zeros
+}
+
+// The products of a row tile: S = Q K^T, O (+)= P V.
+template <int DK, bool PAGED>
+__device__ __forceinline__ void issue_scores(uint32_t tS, uint32_t q, uint32_t k) {
+  using L = Layout<DK, PAGED>;
+  constexpr uint32_t kIdesc = make_idesc(kBM, kBN, false);
+#pragma unroll
+  for (int kk = 0; kk < DK / 16; ++kk)
+    mma_f16_ss(tS, make_sdesc_sw128(q + (kk >> 2) * (128 * 128) + (kk & 3) * 32, 16, 1024),
+               make_sdesc_sw128(k + (kk >> 2) * L::kPanel + (kk & 3) * 32, 16, L::kGroup), kIdesc, kk > 0 ? 1u : 0u);
+}
+template <int DV, bool PAGED>
+__device__ __forceinline__ void issue_outputs(uint32_t tO, uint32_t tP, uint32_t v, uint32_t acc_first) {
+  using L = Layout<DV, PAGED>;
+  constexpr uint32_t kIdesc = make_idesc(kBM, DV, true);
+#pragma unroll
+  for (int kk = 0; kk < kBN / 16; ++kk)
+    mma_f16_ts(tO, tP + kk * 8, make_sdesc_sw128(v + 2 * kk * L::kGroup, L::kPanel, L::kGroup), kIdesc, kk > 0 ? 1u : acc_first);
+}
+
+// What redo_piece works with.
+struct Again {
+  const CUtensorMap *q, *k, *v;
+  uint8_t* kv;             // the ring: a tile of keys in its first stage, of values in its second
+  uint32_t tmem, sQ;
+  uint32_t loaded, done;   // barriers: copies, products
+  volatile int* odd;
+  uint32_t loads, products;   // so far
+};
+
+// Tiles [u0, u1) of an item once more, by the softmax warps alone, with values that are not finite taken out of the tiles that
+// some row does not see all of, if there are any.  False if a wait ran out.
+template <int DK, int DV, int QT, bool PAGED>
+__device__ __forceinline__ bool redo_piece(Again& a, const Params& p, const Out& out, int item, int u0, int u1, const WaitCtl& wc) {
+  using C = Cfg<DK, DV, QT>;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, j = warp >> 2, row = (warp & 3) * 32 + lane;
+  const uint32_t lanes = a.tmem + (uint32_t((warp & 3) * 32) << 16);
+  const uint32_t tS = lanes + (j ? C::kTmemS1 : C::kTmemS0), tP = lanes + (j ? C::kTmemP1 : C::kTmemP0);
+  const uint32_t tO = lanes + (j ? C::kTmemO1 : C::kTmemO0), sK = smem_u32(a.kv), sV = sK + C::kStageBytes;
+  const bool first = threadIdx.x == 0;
+  // all softmax threads; whether all of them say so
+  auto meet = [](bool yes) {
+    uint32_t all;
+    asm volatile("{\n\t.reg .pred a, b;\n\tsetp.ne.u32 a, %1, 0;\n\tbar.red.and.pred b, 1, %2, a;\n\tselp.u32 %0, 1, 0, b;\n\t}"
+                 : "=r"(all)
+                 : "r"(uint32_t(yes)), "n"(C::kSoftmax)
+                 : "memory");
+    return all != 0;
+  };
+  const Where w = where_of<QT>(p, item);
+  const int len = length_of(p, w.b, false);
+  const win::Tiles list = win::tiles_of(p.mask, len, p.N, w.i0, w.i1, kBN);
+  const int end = win::row_end(p.mask, len, p.N, w.i1), begin = win::row_low(p.mask, len, p.N, w.i0);
+  const Partly partly(p.mask, len, p.N, w.i0, w.i1);
+  const int row_pos = int(unsigned(row) / unsigned(p.GC));
+  const Place at = place_of<QT>(p, item, j, row_pos, row - row_pos * p.GC);
+  const int lim = at.live ? win::row_end(p.mask, len, p.N, at.i) : 0, low = at.live ? win::row_low(p.mask, len, p.N, at.i) : 0;
+  const float c = fmaxf(p.c_log2, FLT_MIN);
+  const int gone = PAGED ? len : 0x7fffffff;
+  // nothing to take out: what is not finite is what the rows see
+  bool odd = false;
+#pragma unroll 1
+  for (int n = u0; n < u1; ++n) {
+    const int n0 = list.at(n) * kBN;
+    if (!partly(n0, p.mask.sinks)) continue;
+    for (int x = threadIdx.x; x < kBN * (DV / 8); x += C::kSoftmax) {
+      const int t = n0 + x / (DV / 8);
+      const __nv_bfloat16* v = t < len ? values_of(p, w.b, w.h, t) : nullptr;
+      if (v == nullptr) continue;
+      const uint4 y = *reinterpret_cast<const uint4*>(v + x % (DV / 8) * 8);
+      odd |= odd_pair(y.x) || odd_pair(y.y) || odd_pair(y.z) || odd_pair(y.w);
+    }
+  }
+  if (meet(!odd)) return true;
+  float m = -INFINITY, l = 0.f;
+  if (first) {
+    *a.odd = 0;
+    mbar_arrive_expect_tx(a.loaded, QT * DK * 2 * p.GC * p.PT);
+#pragma unroll 1
+    for (int x = 0; x < QT * (DK / 64); ++x) {
+      const int t = x / (DK / 64), q = x % (DK / 64);
+      tma_load_5d(a.sQ + t * C::kQTileBytes + q * C::kPanelBytes, a.q, a.loaded, q * 64, w.chunk * p.GC, w.i0 + t * p.PT, w.h, w.b);
+    }
+  }
+  bool ok = wait_bounded(a.loaded, a.loads++ & 1u, wc);
+#pragma unroll 1
+  for (int n = u0; n < u1; ++n) {
+    const int n0 = list.at(n) * kBN;
+    ok = meet(ok);   // the tile before is done with
+    if (!ok) break;
+    if (first) {
+      mbar_arrive_expect_tx(a.loaded, C::kKTileBytes + C::kVTileBytes);
+      if constexpr (PAGED) {
+#pragma unroll 1
+        for (int t = 0; t < kBN; t += p.box) {
+          const int s = page_source(p, w, n0 + t, end, begin);
+          tma_load_4d(sK + t / 8 * Layout<DK, true>::kGroup, a.k, a.loaded, 0, 0, 0, s);
+          tma_load_4d(sV + t / 8 * Layout<DV, true>::kGroup, a.v, a.loaded, 0, 0, 0, s);
+        }
+      } else {
+#pragma unroll 1
+        for (int q = 0; q < DK / 64; ++q) tma_load_4d(sK + q * C::kPanelBytes, a.k, a.loaded, q * 64, n0, w.h, w.b);
+#pragma unroll 1
+        for (int q = 0; q < DV / 64; ++q) tma_load_4d(sV + q * C::kPanelBytes, a.v, a.loaded, q * 64, n0, w.h, w.b);
+      }
+    }
+    const uint32_t arrived = a.loads++ & 1u;
+    ok = wait_bounded(a.loaded, arrived, wc);
+#pragma unroll 1
+    for (int t = 0; t < QT; ++t) {   // (both row tiles may have one buffer of scores)
+      if (first) {
+        tc_fence_after_sync();
+        issue_scores<DK, PAGED>(a.tmem + (t ? C::kTmemS1 : C::kTmemS0), a.sQ + t * C::kQTileBytes, sK);
+        mma_commit(a.done);
+      }
+      ok = wait_bounded(a.done, a.products++ & 1u, wc) && ok;
+      tc_fence_after_sync();
+      if (j == t) {
+        // 32 tokens at a time, twice: their scores, -infinity for those that the row does not see
+        uint32_t sr[32];
+        auto scores = [&](int k) {
+          tmem_ld_32x32b_x32(tS + 32 * k, sr);
+          tmem_wait_ld();
+          reg_anchor_x32(sr);
+          const uint32_t bits = below(lim - n0, k) & (~below(low - n0, k) | below(p.mask.sinks - n0, k));
+#pragma unroll
+          for (int e = 0; e < 32; ++e) sr[e] = bits >> e & 1u ? sr[e] : 0xff800000u;
+        };
+        float top = -INFINITY;
+#pragma unroll 1
+        for (int k = 0; k < 4; ++k) {
+          scores(k);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) top = fmaxf(top, __uint_as_float(sr[e]));
+        }
+        top *= c;
+        if (__any_sync(0xffffffffu, top > m)) {
+          const float m_new = fmaxf(m, top), alpha = m == -INFINITY ? 0.f : ex2_approx(m - m_new);
+          l *= alpha;
+          m = m_new;
+          if (n > u0) tmem_scale_row<DV>(tO, alpha);
+        }
+        const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll 1
+        for (int k = 0; k < 4; ++k) {
+          scores(k);
+          uint32_t pk[16];
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) {
+            const float p0 = ex2_approx(fmaf(__uint_as_float(sr[e]), c, -base)), p1 = ex2_approx(fmaf(__uint_as_float(sr[e + 1]), c, -base));
+            l += p0 + p1;
+            pk[e >> 1] = pack_bf16x2(p0, p1);
+          }
+          tmem_st_32x32b_x16(tP + 16 * k, pk);
+        }
+        tmem_wait_st();
+      }
+      tc_fence_before_sync();
+      ok = meet(ok);
+    }
+    if (partly(n0, p.mask.sinks))
+      ok = look_through<DV, PAGED>(a.kv + C::kStageBytes, int(threadIdx.x), C::kSoftmax, gone - n0, a.loaded, arrived, a.odd, 1, wc) && ok;
+    ok = meet(ok);
+    if (first) {
+      tc_fence_after_sync();
+#pragma unroll 1
+      for (int t = 0; t < QT; ++t)
+        issue_outputs<DV, PAGED>(a.tmem + (t ? C::kTmemO1 : C::kTmemO0), a.tmem + (t ? C::kTmemP1 : C::kTmemP0), sV, n > u0 ? 1u : 0u);
+      mma_commit(a.done);
+    }
+    ok = wait_bounded(a.done, a.products++ & 1u, wc) && ok;
+    tc_fence_after_sync();
+  }
+  ok = meet(ok);
+  if (!ok) {   // the last copies and products end before the CTA does
+    if (first) {
+      wait_quiesce(a.loaded, (a.loads - 1) & 1u, wc.limit_ns, wc.status);
+      if (a.products > 0) wait_quiesce(a.done, (a.products - 1) & 1u, wc.limit_ns, wc.status);
+    }
+    return false;
+  }
+  if (*a.odd != 0) add_odd_values<DV>(tO, p, w.b, w.h, len, w.i0, w.i1, list, u0, u1, lim, low, at.live && l == l);
+  const int units = list.n < 1 ? 1 : list.n;
+  write_rows<DK, DV, QT, true>(p, out, at, tO, sK + (C::kStages - 2) * C::kStageBytes, j, row, m, l, u0 == 0, u0 == 0 && u1 == units);
+  if (QT == 1 && p.cluster > 1) {
+    const Owner own = owner_of(row, p.cluster);
+    store2_to_cta(smem_of_cta(sK - C::kOffKV + C::kOffSums + (int(blockIdx.y) * (kBM / p.cluster) + own.row) * 8, own.rank),
+                  at.live ? m : -INFINITY, at.live ? l : 0.f);
+  }
+  tc_fence_before_sync();
+  return meet(true);
+}
+
+// The marked pieces of a CTA's share, as the walk had them, or its part of a cluster's item.  (All that it needs it finds again: what
+// a call kept for it would cost the softmax loop registers.)
+template <int DK, int DV, int QT, bool PAGED>
+__device__ __noinline__ void redo_share(const CUtensorMap* tmQ, const CUtensorMap* tmK, const CUtensorMap* tmV, const Params& p, const Out& out,
+                                        uint8_t* smem, uint32_t tmem) {
+  using C = Cfg<DK, DV, QT>;
+  const volatile Item* items = reinterpret_cast<const volatile Item*>(smem + C::kOffItems);
+  const uint32_t* again = reinterpret_cast<const uint32_t*>(smem + C::kOffAgain);
+  const Begin* found = reinterpret_cast<const Begin*>(smem + C::kOffItems + 64 + 12 * 8);
+  const uint32_t bars = smem_u32(smem + C::kOffBar) + 8u * (2 * C::kStages + 17);
+  const WaitCtl wc{reinterpret_cast<volatile int*>(smem + C::kOffMisc + 4), p.wait_limit_ns, 0u, &g_moa_window_tc_status};
+  Again a{tmQ, tmK, tmV, smem + C::kOffKV, tmem, smem_u32(smem), bars, bars + 8, reinterpret_cast<volatile int*>(smem + C::kOffMisc + 12), 0, 0};
+  int64_t at = 0, stop = 0, before = 0;
+  int item = 0;
+  if (p.cluster == 0) {
+    const Shares shares(found->total, gridDim.x);
+    at = shares.start(blockIdx.x), stop = shares.start(blockIdx.x + 1);
+    item = int(found->item), before = found->unit;
+  }
+  for (uint32_t seg = 0; p.cluster != 0 ? seg == 0 : at < stop; ++item) {
+    int u0 = items[0].u0, u1 = items[0].u1, which = items[0].item;   // of a cluster
+    if (p.cluster == 0) {
+      which = item;
+      const int64_t end = before + units_of<QT>(p, item, false) + item_units(QT), upto = end < stop ? end : stop;
+      u0 = max(0, int(at - before) - item_units(QT)), u1 = max(0, int(upto - before) - item_units(QT));
+      at = upto;
+      before = end;
+      if (u0 >= u1) continue;
+    }
+    const uint32_t bit = seg < kAgain - 1 ? seg : kAgain - 1;
+    if ((again[bit / 32] >> (bit & 31) & 1u) != 0 && !redo_piece<DK, DV, QT, PAGED>(a, p, out, which, u0, u1, wc)) return;
+    ++seg;
   }
 }
 
@@ -406,8 +767,8 @@ __device__ __noinline__ void cluster_rows(const __nv_bfloat16* Q, __nv_bfloat16*
 template <int DK, int DV, int QT, bool PAGED>
 __global__ void __launch_bounds__(Cfg<DK, DV, QT>::kThreads, 1)
 window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
-                 const __grid_constant__ CUtensorMap tmV, const __nv_bfloat16* Q, __nv_bfloat16* O, float* lse, float* part_o,
-                 float2* part_ml, Cut* cuts, const Params p) {
+                 const __grid_constant__ CUtensorMap tmV, const __grid_constant__ Out out, Cut* cuts,
+                 const __grid_constant__ Params p) {
   using C = Cfg<DK, DV, QT>;
   using KL = Layout<DK, PAGED>;
   using VL = Layout<DV, PAGED>;
@@ -424,9 +785,11 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
   auto p_free = [&](int j) { return q_full + 8u * (11 + j); };
   auto item_full = [&](int i) { return q_full + 8u * (13 + i); };
   auto item_empty = [&](int i) { return q_full + 8u * (15 + i); };
+  const uint32_t redo_loaded = q_full + 8u * 17, redo_done = q_full + 8u * 18;   // (redo_share)
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::kOffMisc);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::kOffMisc + 4);
-  volatile int* any_odd = reinterpret_cast<volatile int*>(smem + C::kOffMisc + 8);   // an item's row is to be computed again
+  volatile int* any_again = reinterpret_cast<volatile int*>(smem + C::kOffMisc + 8);   // a piece is to be computed once more
+  uint32_t* again = reinterpret_cast<uint32_t*>(smem + C::kOffAgain);
   volatile Item* items = reinterpret_cast<volatile Item*>(smem + C::kOffItems);
   int64_t* scan = reinterpret_cast<int64_t*>(smem + C::kOffItems + 64);   // warp sums
   Begin* found = reinterpret_cast<Begin*>(scan + 12);
@@ -454,9 +817,10 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       mbar_init(p_free(j), 1);
     }
     *abort_flag = 0;
-    *any_odd = 0;
+    *any_again = 0;
     fence_barrier_init();
   }
+  if (threadIdx.x < kAgain / 32) again[threadIdx.x] = 0;
   if (warp == C::kLoadWarp && lane == 0) {
     tma_prefetch_desc(&tmQ);
     tma_prefetch_desc(&tmK);
@@ -567,15 +931,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
           if (n >= n_kt || lane >= boxes) return s;
           const int t0 = list.at(x.u0 + n) * kBN + lane * p.box;
           if (!PAGED) return t0;
-          s = p.all_groups;   // past the pool: zeros
-          if (t0 < end && (t0 > low - p.box || t0 < p.mask.sinks)) {
-            const int at = int(unsigned(t0) / unsigned(p.kv.page));
-            const int pg = p.kv.table[w.b * p.kv.max_pages + at];
-            if (pg >= 0 && pg < p.kv.n_pages)
-              s = (pg * p.Hk + w.h) * p.page_groups + ((t0 - at * p.kv.page) >> 3);
-            else
-              atomicExch(&g_moa_window_tc_status, win::kErrIndex);
-          }
+          s = page_source(p, w, t0, end, low);
           return s;
         };
         int cur = source(0), next = cur, after = source(1);
@@ -644,8 +1000,6 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       // ------------------------------------------------------------ MMA issuers, one for each row tile
       if (lane == 0) {
         const int j = warp == C::kMmaWarp0 ? 0 : 1;
-        constexpr uint32_t kIdescQK = make_idesc(kBM, kBN, false);
-        constexpr uint32_t kIdescPV = make_idesc(kBM, DV, true);
         const uint32_t tS = tmem + (j ? C::kTmemS1 : C::kTmemS0);
         const uint32_t tP = tmem + (j ? C::kTmemP1 : C::kTmemP0);
         const uint32_t tO = tmem + (j ? C::kTmemO1 : C::kTmemO0);
@@ -658,19 +1012,6 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             slot = 0;
             phase ^= 1u;
           }
-        };
-        auto issue_qk = [&](uint32_t kb) {
-#pragma unroll
-          for (int kk = 0; kk < DK / 16; ++kk)
-            mma_f16_ss(tS, make_sdesc_sw128(sQj + (kk >> 2) * C::kPanelBytes + (kk & 3) * 32, 16, 1024),
-                       make_sdesc_sw128(kb + (kk >> 2) * KL::kPanel + (kk & 3) * 32, 16, KL::kGroup), kIdescQK,
-                       kk > 0 ? 1u : 0u);
-        };
-        auto issue_pv = [&](uint32_t vb, uint32_t acc_first) {
-#pragma unroll
-          for (int kk = 0; kk < kBN / 16; ++kk)
-            mma_f16_ts(tO, tP + kk * 8, make_sdesc_sw128(vb + 2 * kk * VL::kGroup, VL::kPanel, VL::kGroup), kIdescPV,
-                       kk > 0 ? 1u : acc_first);
         };
         // The S buffer may take tile u's scores once its last reader holds what it has: this row
         // tile's softmax (tile u - 1), or with one buffer for both, the other one's (tile u - 1 for
@@ -691,7 +1032,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             tc_fence_after_sync();
             const int ks = slot;
             next();
-            issue_qk(sKV + ks * C::kStageBytes);
+            issue_scores<DK, PAGED>(tS, sQj, sKV + ks * C::kStageBytes);
             mma_commit(s_full(j));
             mma_commit(empty_bar(ks));
             if (n_kt == 1) mma_commit(q_empty);
@@ -703,7 +1044,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
               next();
               if (!ok) break;
               tc_fence_after_sync();
-              issue_qk(sKV + ks * C::kStageBytes);
+              issue_scores<DK, PAGED>(tS, sQj, sKV + ks * C::kStageBytes);
               mma_commit(s_full(j));
               mma_commit(empty_bar(ks));
               if (n + 2 == n_kt) mma_commit(q_empty);
@@ -713,7 +1054,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             next();
             if (!ok) break;
             tc_fence_after_sync();
-            issue_pv(sKV + vs * C::kStageBytes, n > 0 ? 1u : 0u);
+            issue_outputs<DV, PAGED>(tO, tP, sKV + vs * C::kStageBytes, n > 0 ? 1u : 0u);
             mma_commit(p_free(j));
             mma_commit(empty_bar(vs));
           }
@@ -781,16 +1122,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       const Item x = get_item(seg, ok);
       if (x.item < 0) break;
       const win::Tiles list{x.first, x.from, 0};
-      // where the thread's row lies
-      struct Place {
-        int b, hq, i;
-        bool live;
-      };
-      auto place = [&](int item) {
-        const Where w = where_of<QT>(p, item);
-        const int g = w.chunk * p.GC + row_head, i = w.i0 + j * p.PT + row_pos;
-        return Place{w.b, w.h * p.G + g, i, row_pos < p.PT && g < p.G && i < p.N};
-      };
+      auto place = [&](int which) { return place_of<QT>(p, which, j, row_pos, row_head); };   // where the thread's row lies
       int lim = 0x7fffffff, low = 0;
       bool live_warp;
       {
@@ -907,68 +1239,12 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       const bool first_piece = xi.u0 == 0, whole = first_piece && xi.u1 == xi.units;
       if (live_warp) {
         const Place w = place(xi.item);
-        bool bad = false;
-        if (clustered) {   // the row's sums, to the CTA that joins it
-          const Owner own = owner_of(row, p.cluster);
-          const uint32_t sum = smem_of_cta(sKV + (C::kStages - 2) * C::kStageBytes +
-                                           ((int(blockIdx.y) * (kBM / p.cluster) + own.row) * DV) * 4, own.rank);
-#pragma unroll
-          for (int d = 0; d < DV; d += 16) {
-            uint32_t o[16];
-            tmem_ld_32x32b_x16(tO + d, o);
-            tmem_wait_ld();
-            reg_anchor_x16(o);
-            if (w.live) {
-#pragma unroll
-              for (int e = 0; e < 4; ++e) store4_to_cta(sum + (d + 4 * e) * 4, o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
-            }
-          }
-          cluster_m = m, cluster_l = l;
-        } else if (!whole) {
-          const int64_t at = (int64_t(blockIdx.x) * 2 + first_piece) * C::kRows + j * kBM + row;
-#pragma unroll
-          for (int d = 0; d < DV; d += 16) {
-            uint32_t o[16];
-            tmem_ld_32x32b_x16(tO + d, o);
-            tmem_wait_ld();
-            reg_anchor_x16(o);
-            if (w.live) {
-              float4* dst = reinterpret_cast<float4*>(part_o + at * DV + d);
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                dst[e] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]),
-                                     __uint_as_float(o[4 * e + 3]));
-            }
-          }
-          if (w.live) part_ml[at] = make_float2(m, l);
-        } else {
-          const float inv = l == 0.f ? 0.f : 1.f / l;
-          __nv_bfloat16* orow = O + int64_t(w.b) * p.o_sb + int64_t(w.hq) * p.o_sh + int64_t(w.i) * p.o_sn;
-          if (lse != nullptr && w.live)
-            lse[(int64_t(w.b) * p.Hk * p.G + w.hq) * p.N + w.i] = l == 0.f ? -INFINITY : (m + lg2_approx(l)) * kLn2;
-          float top = 0.f;
-#pragma unroll
-          for (int d = 0; d < DV; d += 16) {
-            uint32_t o[16];
-            tmem_ld_32x32b_x16(tO + d, o);
-            tmem_wait_ld();
-            reg_anchor_x16(o);
-            uint32_t z[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float y0 = __uint_as_float(o[2 * e]) * inv, y1 = __uint_as_float(o[2 * e + 1]) * inv;
-              top = fmaf(y0, 0.f, top);   // not zero if one is not finite
-              top = fmaf(y1, 0.f, top);
-              z[e] = pack_bf16x2(y0, y1);
-            }
-            if (w.live) {
-              reinterpret_cast<uint4*>(orow + d)[0] = make_uint4(z[0], z[1], z[2], z[3]);
-              reinterpret_cast<uint4*>(orow + d)[1] = make_uint4(z[4], z[5], z[6], z[7]);
-            }
-          }
-          bad = __any_sync(0xffffffffu, w.live && top != 0.f);
+        if (write_rows<DK, DV, QT, false>(p, out, w, tO, sKV + (C::kStages - 2) * C::kStageBytes, j, row, m, l, first_piece, whole) && lane == 0) {
+          const uint32_t bit = seg < kAgain - 1 ? seg : kAgain - 1;
+          atomicOr(again + bit / 32, 1u << (bit & 31));
+          *any_again = 1;
         }
-        if (bad && lane == 0) *any_odd = 1;   // (a cut item's rows are looked at when joined)
+        cluster_m = m, cluster_l = l;
       }
       tc_fence_before_sync();   // O is read: the next item's first product (after p_ready) may write it
       __syncwarp();
@@ -986,6 +1262,21 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
   if (warp == C::kMmaWarp0 && lane == 0) wait_quiesce(drain, 0, p.wait_limit_ns, &g_moa_window_tc_status);
   tc_fence_before_sync();
   __syncthreads();
+  if (*any_again != 0) {
+    const bool dead = *abort_flag != 0;
+    if (threadIdx.x == 0) {
+      mbar_init(redo_loaded, 1);
+      mbar_init(redo_done, 1);
+      fence_barrier_init();
+    }
+    __syncthreads();
+    if (!dead && warp < C::kMmaWarp0) {
+      tc_fence_after_sync();
+      redo_share<DK, DV, QT, PAGED>(&tmQ, &tmK, &tmV, p, out, smem, tmem);
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+  }
   if (warp == C::kMmaWarp0) {
     tc_fence_after_sync();
     tmem_dealloc(tmem, C::kTmemCols);
@@ -996,27 +1287,19 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       __syncwarp();
       cluster_sync();
       if (warp < C::kMmaWarp0)
-        cluster_rows<DK, DV>(Q, O, lse, p, reinterpret_cast<const float*>(smem + C::kOffKV + (C::kStages - 2) * C::kStageBytes),
+        cluster_rows<DV>(out.O, out.lse, p, reinterpret_cast<const float*>(smem + C::kOffKV + (C::kStages - 2) * C::kStageBytes),
                              reinterpret_cast<const float2*>(smem + C::kOffSums));
-      return;
     }
-  }
-  if (*any_odd != 0 && warp < C::kMmaWarp0) {
-    if (p.cluster != 0)
-      item_rows_again<DK, DV, QT>(Q, O, p, int(blockIdx.x));
-    else
-      whole_rows_again<DK, DV, QT>(Q, O, p, found);
   }
 }
 
 // Joins the pieces of cut items: CTA (x, y) 32 / WS rows of CTA x's cut, four for every WS warps, eight lanes a row (a row a
 // warp spent most of its instructions on places: the call of 4 x 16 heads x 2048 x 64 took 78 us in place of 67); each of the WS warps takes
-// every WS-th piece, where items have many.  Rows whose output is not finite are computed again.
+// every WS-th piece, where items have many.
 constexpr int kJoinRows = 4;
-template <int DK, int DV, int QT>
+template <int DV, int QT>
 __global__ void __launch_bounds__(256)
-window_tc_join_kernel(const __nv_bfloat16* Q, __nv_bfloat16* O, float* lse, const float* part_o, const float2* part_ml,
-                      const Cut* cuts, const Params p, int WS) {
+window_tc_join_kernel(const Out out, const Cut* cuts, const Params p, int WS) {
   constexpr int kRows = kBM * QT, kQuads = DV / 32;
   __shared__ float4 s_x[8][32][kQuads];
   __shared__ float s_l[8][kJoinRows];
@@ -1037,7 +1320,7 @@ window_tc_join_kernel(const __nv_bfloat16* Q, __nv_bfloat16* O, float* lse, cons
 #pragma unroll
   for (int q = 0; q < kQuads; ++q) x[q] = make_float4(0.f, 0.f, 0.f, 0.f);
   if (live)
-    for (int k = sub; k < cut.pieces; k += 8) M = fmaxf(M, part_ml[place(k)].x);
+    for (int k = sub; k < cut.pieces; k += 8) M = fmaxf(M, out.part_ml[place(k)].x);
 #pragma unroll
   for (int d = 4; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
   const float base = M == -INFINITY ? 0.f : M;
@@ -1045,12 +1328,12 @@ window_tc_join_kernel(const __nv_bfloat16* Q, __nv_bfloat16* O, float* lse, cons
 #pragma unroll 2
     for (int k = turn; k < cut.pieces; k += WS) {
       const int64_t at = place(k);
-      const float2 ml = part_ml[at];
+      const float2 ml = out.part_ml[at];
       const float f = ex2_approx(ml.x - base);
       L += f * ml.y;
 #pragma unroll
       for (int q = 0; q < kQuads; ++q) {
-        const float4 v = *reinterpret_cast<const float4*>(part_o + at * DV + (sub + 8 * q) * 4);
+        const float4 v = *reinterpret_cast<const float4*>(out.part_o + at * DV + (sub + 8 * q) * 4);
         x[q].x += f * v.x, x[q].y += f * v.y, x[q].z += f * v.z, x[q].w += f * v.w;
       }
     }
@@ -1071,18 +1354,15 @@ window_tc_join_kernel(const __nv_bfloat16* Q, __nv_bfloat16* O, float* lse, cons
     }
   }
   const float inv = L == 0.f ? 0.f : 1.f / L;
-  __nv_bfloat16* o = O + int64_t(w.b) * p.o_sb + int64_t(hq) * p.o_sh + int64_t(i) * p.o_sn;
-  bool bad = false;
+  __nv_bfloat16* o = out.O + int64_t(w.b) * p.o_sb + int64_t(hq) * p.o_sh + int64_t(i) * p.o_sn;
 #pragma unroll
   for (int q = 0; q < kQuads; ++q) {
     x[q].x *= inv, x[q].y *= inv, x[q].z *= inv, x[q].w *= inv;
-    bad |= not_finite(x[q].x) || not_finite(x[q].y) || not_finite(x[q].z) || not_finite(x[q].w);
     if (live)
       *reinterpret_cast<uint2*>(o + (sub + 8 * q) * 4) = make_uint2(pack_bf16x2(x[q].x, x[q].y), pack_bf16x2(x[q].z, x[q].w));
   }
-  if (lse != nullptr && live && sub == 0)
-    lse[(int64_t(w.b) * p.Hk * p.G + hq) * p.N + i] = L == 0.f ? -INFINITY : (M + lg2_approx(L)) * kLn2;
-  rows_again<DK, DV>(Q, O, p, w, bad && live, hq, i);
+  if (out.lse != nullptr && live && sub == 0)
+    out.lse[(int64_t(w.b) * p.Hk * p.G + hq) * p.N + i] = L == 0.f ? -INFINITY : (M + lg2_approx(L)) * kLn2;
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -1169,12 +1449,10 @@ int launch(const WindowArgs& a, const Plan& plan, int sms, char* msg, size_t msg
   }
   const Work w(a, plan, sms);
   uint8_t* ws = static_cast<uint8_t*>(a.ws);
-  float* part_o = reinterpret_cast<float*>(ws + w.part_o);
-  float2* part_ml = reinterpret_cast<float2*>(ws + w.part_ml);
+  const Out out{static_cast<__nv_bfloat16*>(a.o.p), a.lse, reinterpret_cast<float*>(ws + w.part_o), reinterpret_cast<float2*>(ws + w.part_ml)};
   Cut* cuts = reinterpret_cast<Cut*>(ws + w.cuts);
   const int64_t G = a.Hq / a.Hk;
   Params p{};
-  p.q_sb = a.q.sb, p.q_sh = a.q.sh, p.q_sn = a.q.sn;
   p.o_sb = a.o.sb, p.o_sh = a.o.sh, p.o_sn = a.o.sn;
   p.kv = a.kv, p.lens = a.lens;
   p.N = int(a.N), p.max_len = int(a.max_len), p.Hk = int(a.Hk), p.G = int(G);
@@ -1219,8 +1497,7 @@ int launch(const WindowArgs& a, const Plan& plan, int sms, char* msg, size_t msg
       if (p.cluster > 8) e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kern), cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
       if (e == cudaSuccess)
         e = launch_clusters(kern, dim3(unsigned(plan.n_items), unsigned(p.cluster)), unsigned(p.cluster), dim3(C::kThreads),
-                            C::kSmemBytes, a.stream, mq, mk, mv, static_cast<const __nv_bfloat16*>(a.q.p),
-                            static_cast<__nv_bfloat16*>(a.o.p), a.lse, part_o, part_ml, cuts, p);
+                            C::kSmemBytes, a.stream, mq, mk, mv, out, cuts, p);
       if (e != cudaSuccess) {
         snprintf(msg, msglen, "attention with a window: %s", cudaGetErrorString(e));
         return 5;
@@ -1236,17 +1513,14 @@ int launch(const WindowArgs& a, const Plan& plan, int sms, char* msg, size_t msg
   }
   // rows of an item that may be there
   const int64_t positions = a.N < plan.PT ? a.N : plan.PT, live = QT == 2 ? C::kRows : positions * plan.GC;
-  e = launch_overlapped(kern, dim3(ctas), dim3(C::kThreads), C::kSmemBytes, a.stream, mq, mk, mv,
-                        static_cast<const __nv_bfloat16*>(a.q.p), static_cast<__nv_bfloat16*>(a.o.p), a.lse, part_o, part_ml,
-                        cuts, p);
+  e = launch_overlapped(kern, dim3(ctas), dim3(C::kThreads), C::kSmemBytes, a.stream, mq, mk, mv, out, cuts, p);
   // warps for a row's pieces: about a quarter of the pieces that an item may have
   const int64_t pieces = ctas / plan.n_items + 1;
   const int split = pieces <= 4 ? 1 : pieces <= 8 ? 2 : pieces <= 16 ? 4 : 8;
   const int64_t per = 32 / split;
   if (e == cudaSuccess)
-    e = launch_overlapped(window_tc_join_kernel<DK, DV, QT>, dim3(ctas, unsigned((live + per - 1) / per)), dim3(256), 0, a.stream,
-                          static_cast<const __nv_bfloat16*>(a.q.p), static_cast<__nv_bfloat16*>(a.o.p), a.lse, part_o, part_ml,
-                          cuts, p, split);
+    e = launch_overlapped(window_tc_join_kernel<DV, QT>, dim3(ctas, unsigned((live + per - 1) / per)), dim3(256), 0, a.stream, out, cuts, p,
+                          split);
   if (e != cudaSuccess) {
     snprintf(msg, msglen, "attention with a window: %s", cudaGetErrorString(e));
     return 5;
