@@ -626,6 +626,13 @@ int moa_get_device_status(void* stream);
 int moa_selftest_wait_timeout(uint64_t limit_ns, void* stream);
 
 /*
+ * moa_selftest_cluster_limit -- for tests: the calls that follow, on any thread, divide their work as if no
+ * cluster of more than `most` CTAs (1, 2, 4, 8 or 16; 0: no limit) had room on the device, as it is where a
+ * context has a part of its SMs.  Workspaces are to be asked for anew.  MOA_ERR_INVALID_ARG for other numbers.
+ */
+int moa_selftest_cluster_limit(int most);
+
+/*
  * moa_attn_flops -- floating-point operations of the two contractions,
  * 2*B*H*N_q*N_k*(d_k + d_v): the two matrix products of Eq. (attention),
  * Q K^T and the product of the weights with V (exponentials, maxima and the

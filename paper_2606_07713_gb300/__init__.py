@@ -15,7 +15,7 @@ import math
 
 from ._lib import (MOA_BF16, MOA_FP32, MoaError, check, lib, moa_attn_dnf_bytes,  # noqa: F401
                    moa_attn_flops, moa_attn_fwd, moa_attn_fwd_staged, moa_attn_version,
-                   moa_get_device_status, moa_last_error, moa_selftest_wait_timeout,
+                   moa_get_device_status, moa_last_error, moa_selftest_cluster_limit, moa_selftest_wait_timeout,
                    moa_attn_fwd_splitkv, moa_attn_splitkv_workspace_bytes, moa_attn_fwd_lse,
                    moa_attn_bwd, moa_attn_bwd_workspace_bytes, moa_qkv_proj,
                    moa_attn_split_plan, MOA_SPLITS_AUTO, moa_attn_bwd_fused,
@@ -33,7 +33,7 @@ from .ops import (kv4_attn, kv4_attn_lse, kv4_pool, kv4_read, kv4_write, kv_appe
 __all__ = ["attn_fwd", "attn_fwd_staged", "get_device_status", "attn_flops", "dnf_bytes",
            "MOA_FP32", "MOA_BF16", "MoaError", "moa_attn_fwd", "moa_attn_fwd_staged",
            "moa_last_error", "moa_get_device_status", "moa_attn_flops", "moa_attn_dnf_bytes",
-           "moa_attn_version", "moa_selftest_wait_timeout", "attn_fwd_splitkv",
+           "moa_attn_version", "moa_selftest_wait_timeout", "moa_selftest_cluster_limit", "attn_fwd_splitkv",
            "moa_attn_fwd_splitkv", "moa_attn_splitkv_workspace_bytes", "attn_fwd_lse",
            "moa_attn_fwd_lse", "attn_bwd", "moa_attn_bwd", "moa_attn_bwd_workspace_bytes",
            "qkv_proj", "moa_qkv_proj", "moa_attn_split_plan", "MOA_SPLITS_AUTO",

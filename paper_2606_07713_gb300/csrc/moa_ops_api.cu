@@ -2,6 +2,7 @@
 // entry point is documented in include/moa_attn.h.
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cmath>
 #include <cstdint>
 #include <exception>
@@ -13,6 +14,44 @@
 #include "window.cuh"
 
 namespace moa {
+namespace {
+std::atomic<int> g_most_cluster{0};
+}  // namespace
+
+void limit_clusters(int most) { g_most_cluster.store(most, std::memory_order_relaxed); }
+
+int ClusterRoom::operator()(const void* kernel, int threads, int bytes, int size) {
+  const int most = g_most_cluster.load(std::memory_order_relaxed);
+  int dev = -1, at = 0;
+  if ((most > 0 && size > most) || cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+  while ((1 << at) < size) ++at;
+  const int known = known_[dev][at].load(std::memory_order_relaxed);
+  if (known > 0) return known - 1;
+  int n = 0;
+  cudaError_t e = ensure_smem_limit(kernel, bytes);
+  if (e == cudaSuccess && size > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e == cudaSuccess) {
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 1;
+    attr.val.clusterDim.y = unsigned(size);
+    attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t c{};
+    c.gridDim = dim3(1, unsigned(size));
+    c.blockDim = dim3(unsigned(threads));
+    c.dynamicSmemBytes = size_t(bytes);
+    c.attrs = &attr;
+    c.numAttrs = 1;
+    e = cudaOccupancyMaxActiveClusters(&n, kernel, &c);
+  }
+  if (e != cudaSuccess) {   // no error of the call, which takes smaller clusters or none
+    cudaGetLastError();
+    n = 0;
+  }
+  known_[dev][at].store(n + 1, std::memory_order_relaxed);
+  return n;
+}
+
 namespace {
 
 constexpr int64_t kMax31 = 0x7fffffffLL;
@@ -855,6 +894,14 @@ size_t moa_window_attn_bwd_workspace_bytes(int64_t B, int64_t H_q, int64_t H_k, 
   a.f32 = dtype == MOA_FP32;
   moa::set_bwd_window(a, window, sinks);
   return moa::window_bwd_workspace(a);
+}
+
+int moa_selftest_cluster_limit(int most) {
+  if (most != 0 && most != 1 && most != 2 && most != 4 && most != 8 && most != 16)
+    return moa::api_fail(MOA_ERR_INVALID_ARG, "the limit must be 0, 1, 2, 4, 8 or 16; got %d", most);
+  moa::limit_clusters(most);
+  moa::api_clear();
+  return MOA_OK;
 }
 
 size_t moa_kv_pool_bytes(int64_t n_pages, int64_t H, int64_t page_tokens, int64_t d_k, int64_t d_v, int dtype) {

@@ -1,6 +1,7 @@
 // Declarations shared by the translation units of the operators around attention: per-head norms
 // with rotation, the 4-bit cache and attention over it.
 #pragma once
+#include <atomic>
 #include <cstddef>
 #include <cstdint>
 #include <cuda_runtime.h>
@@ -44,6 +45,17 @@ cudaError_t launch_clusters(void (*kernel)(P...), dim3 grid, unsigned cluster, d
   c.numAttrs = 2;
   return cudaLaunchKernelEx(&c, kernel, P(std::forward<A>(args))...);
 }
+// Clusters of `size` CTAs (1, 2, 4, 8, 16) of a kernel that the current device, or what the context has of it, takes at the same
+// time: 0 if a launch of one would fail.  Asked once for each device and size.
+class ClusterRoom {
+ public:
+  int operator()(const void* kernel, int threads, int bytes, int size);
+
+ private:
+  std::atomic<int> known_[64][5]{};   // [device][log2 size]: what was asked, and 1
+};
+void limit_clusters(int most);   // as if no cluster of more than `most` CTAs fitted (0: as it is)
+
 #ifdef __CUDACC__
 // The cluster's barrier in two halves: a CTA's shared memory may be written from others once all have arrived.
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory"); }
@@ -185,7 +197,7 @@ struct WindowCcPlan {
   int64_t splits;        // shares of a tile's tokens, joined at the end
   bool cluster;          // by the CTAs of a cluster, in the same launch
 };
-WindowCcPlan window_cc_plan(const WindowArgs& a, int sms);
+WindowCcPlan window_cc_plan(const WindowArgs& a, int sms);   // (on the current device)
 size_t window_cc_workspace(const WindowArgs& a, const WindowCcPlan& p);
 int launch_window_cc(const WindowArgs& a, const WindowCcPlan& p, char* msg, size_t msglen);
 

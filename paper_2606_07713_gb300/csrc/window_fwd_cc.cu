@@ -435,6 +435,25 @@ int launch_sizes(const WindowArgs& a, const WindowCcPlan& plan, char* msg, size_
   return a.dv == 64 ? launch_rows<T, 128, 64>(a, plan, msg, msglen) : launch_rows<T, 128, 128>(a, plan, msg, msglen);
 }
 
+// The most CTAs of a cluster that has room on the device: 1, where no cluster has.
+template <typename T, int DK, int DV, int RM, int NT>
+int most_cluster() {
+  static ClusterRoom room;
+  int size = kMostCluster;
+  while (size > 1 && room(reinterpret_cast<const void*>(window_cc_kernel<T, DK, DV, RM, NT>), NT, Cfg<DK, DV, RM, NT>::kSmem, size) < 1)
+    size /= 2;
+  return size;
+}
+template <typename T, int DK, int DV>
+int most_cluster(int64_t rows) {
+  return rows == 16 ? most_cluster<T, DK, DV, 2, 128>() : most_cluster<T, DK, DV, 4, 256>();
+}
+template <typename T>
+int most_cluster(const WindowArgs& a, int64_t rows) {
+  if (a.dk == 64) return a.dv == 64 ? most_cluster<T, 64, 64>(rows) : most_cluster<T, 64, 128>(rows);
+  return a.dv == 64 ? most_cluster<T, 128, 64>(rows) : most_cluster<T, 128, 128>(rows);
+}
+
 }  // namespace
 
 // Tiles of 16 rows where 64 would be mostly empty, or too few for the machine; shares of a tile's
@@ -455,9 +474,13 @@ WindowCcPlan window_cc_plan(const WindowArgs& a, int sms) {
   p.splits = p.items >= 2 * sms ? 1 : (2 * sms + p.items - 1) / p.items;
   if (p.splits > most) p.splits = most;
   if (p.splits < 1) p.splits = 1;
-  // joined by clusters where sixteen CTAs have no more than three tiles each
-  p.cluster = p.splits > 1 && (p.splits <= kMostCluster || most <= 3 * kMostCluster);
-  if (p.cluster && p.splits > kMostCluster) p.splits = kMostCluster;
+  // joined by clusters where a cluster's CTAs have no more than three tiles each
+  p.cluster = false;
+  if (p.splits > 1) {
+    const int64_t size = a.f32 ? most_cluster<float>(a, p.rows) : most_cluster<__nv_bfloat16>(a, p.rows);
+    p.cluster = size > 1 && (p.splits <= size || most <= 3 * size);
+    if (p.cluster && p.splits > size) p.splits = size;
+  }
   return p;
 }
 

@@ -1371,8 +1371,21 @@ window_tc_join_kernel(const Out out, const Cut* cuts, const Params p, int WS) {
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 constexpr int64_t kMostInL2 = int64_t(100) << 20;   // of 129 MB
-// Clusters of 16, 8, 4, 2 CTAs at a time, a little less than there was room for (7, 15, 36, 76; one more took twice as long).
+// Clusters of 16, 8, 4, 2 CTAs at a time on a whole GPU: what there was room for, or a little less (7, 15, 36, 76; one more took twice
+// as long).  Where the context has fewer SMs, what there is room for.
 constexpr int64_t kClusters16 = 7, kClusters8 = 14, kClusters4 = 34, kClusters2 = 72;
+template <int DK, int DV>
+int room_of(int size) {
+  static ClusterRoom dense, paged;
+  using C = Cfg<DK, DV, 1>;
+  const int a = dense(reinterpret_cast<const void*>(window_tc_kernel<DK, DV, 1, false>), C::kThreads, C::kSmemBytes, size);
+  const int b = paged(reinterpret_cast<const void*>(window_tc_kernel<DK, DV, 1, true>), C::kThreads, C::kSmemBytes, size);
+  return a < b ? a : b;
+}
+int room(int64_t dk, int64_t dv, int size) {
+  if (dk == 64) return dv == 64 ? room_of<64, 64>(size) : room_of<64, 128>(size);
+  return dv == 64 ? room_of<128, 64>(size) : room_of<128, 128>(size);
+}
 
 // How the rows of a key head are divided.
 struct Plan {
@@ -1397,8 +1410,10 @@ struct Plan {
     n_tiles = chunks * ((a.N + PT - 1) / PT);
     n_items = a.B * a.Hk * n_tiles;
     int64_t size = 16;
-    for (int64_t room : {kClusters16, kClusters8, kClusters4, kClusters2})
-      if (n_items > room) size /= 2;
+    for (int64_t most : {kClusters16, kClusters8, kClusters4, kClusters2}) {
+      if (n_items <= most && n_items <= room(a.dk, a.dv, int(size))) break;
+      size /= 2;
+    }
     cluster = 0;
     if (n_items <= sms && tiles <= (a.N > PT ? 16 : 8) * size) {
       cluster = 1;
