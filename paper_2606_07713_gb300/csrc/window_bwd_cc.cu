@@ -19,7 +19,8 @@
 // Rows of a key head are counted position by position (row r: position r / G, head r % G of the group).
 // No atomics: results do not depend on the order in which CTAs run.
 //
-// What bounds it: multiply-adds, at 40 % of their rate, and the last CTAs' steps (2 x (6 / 3) heads x 517 x (128 / 64), window 100: 54 us).
+// What bounds it: shared memory's data path (47 %) and issue slots (40 %) about equally, with the barriers of a step as the largest
+// wait; multiply-adds are at 23 % of their rate (2 x (6 / 3) heads x 517 x (128 / 64), window 100: 54 us, in three launches).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 

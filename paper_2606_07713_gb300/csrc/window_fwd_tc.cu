@@ -30,9 +30,9 @@
 // whose values are infinite or NaN takes some five times as long as one without; other calls pay nothing.
 //
 // What bounds it.  Many rows: a softmax warp's chain of score load, maximum, 128 exponentials and stores beside the products
-// (32768 tokens, 32 / 8 heads of 128, window 4096: 1500 us = 1.37 PFLOP/s of what is seen, tensor pipe 64 %; 2048 queries against 16384 cached
+// (32768 tokens, 32 / 8 heads of 128, window 4096: 1515 us = 1.36 PFLOP/s of what is seen, tensor pipe 64 %; 2048 queries against 16384 cached
 // tokens: 352 us = 1.46 PFLOP/s).  Few rows: memory (48 sequences, 1.2 GB of keys and values: 190 us, 6.3 TB/s), or latency (one
-// token, window 1024: 10.6 us).
+// token, window 1024: 10.7 us).
 //
 // CTA organisation (QT = 2): warps 0-3 and 4-7 softmax and epilogue of row tiles 0 and 1 (thread = row), then the
 // products of tile 0 (and TMEM allocation), TMA, the products of tile 1, the share's items for the other roles.

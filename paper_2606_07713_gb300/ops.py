@@ -138,7 +138,9 @@ def window_attn(q, k, v, window: int | None = None, sinks: int = 0, scale: float
 
     The queries stand at the last N_q of the N_k positions.  A query at position p sees the tokens
     j <= p with j > p - window or j < sinks (window None: all j <= p); one that sees nothing gives
-    zeros.  Query head h reads key head h // (H_q / H_k).  scale defaults to 1 / sqrt(d_k)."""
+    zeros.  Query head h reads key head h // (H_q / H_k).  scale defaults to 1 / sqrt(d_k).
+    A batch padded at the end needs no lengths; what a query does not see, not numbers included, has no
+    influence on it (the gradients are stricter: window_attn_bwd)."""
     return _b.window_attn(q, k, v, window, sinks, scale, out, None, workspace, stream)
 
 
@@ -152,7 +154,10 @@ def window_attn_lse(q, k, v, window: int | None = None, sinks: int = 0, scale: f
 def window_attn_bwd(q, k, v, o, lse, do, window: int | None = None, sinks: int = 0, scale: float | None = None,
                     out=None, workspace=None, stream=None):
     """(dq, dk, dv): the gradients of window_attn for the gradient do of its output, from the o and lse
-    of window_attn_lse.  out: three tensors of the shapes of q, k and v."""
+    of window_attn_lse.  out: three tensors of the shapes of q, k and v.
+
+    q, k, v, o and do have to be finite, in a batch's padding too (there do is zero, and q, k and v are anything finite): the weights of
+    a padded query that is not a number are none, and reach the tokens before it."""
     return _b.window_attn_bwd(q, k, v, o, lse, do, window, sinks, scale, out, workspace, stream)
 
 
