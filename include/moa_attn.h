@@ -498,8 +498,7 @@ size_t moa_kv4_attn_workspace_bytes(int64_t B, int64_t H_q, int64_t H_k, int64_t
  *   scale     from -2e38 to 2e38;  dtype MOA_BF16 or MOA_FP32
  *   workspace device, 16-byte aligned, moa_window_attn_workspace_bytes(...) bytes
  * A batch padded at the end needs no lengths: later tokens are hidden from earlier ones.  What a token
- * that a query does not see holds, not numbers included, has no influence on that query.  (Gradients: padding has to
- * be finite, see moa_window_attn_bwd.)
+ * that a query does not see holds, not numbers included, has no influence on that query.
  * B H_q N_q and B H_k N_k at most 2^31 - 1025.  fp32 accumulation, maxima and sums; bf16: weights are rounded to
  * bf16 once.  Bounded waits as moa_attn_fwd.  Bitwise reproducible.
  */
@@ -522,10 +521,10 @@ size_t moa_window_attn_workspace_bytes(int64_t B, int64_t H_q, int64_t H_k, int6
  *   strides     24 values: Q, K, V, O, dO, dQ, dK, dV
  *   LSE         float32 [B, H_q, N_q] contiguous, as moa_window_attn wrote it
  *   workspace   device, 16-byte aligned, moa_window_attn_bwd_workspace_bytes(...) bytes
- * Tokens that no query sees get zeros, and so do queries that see nothing.  Inputs are finite, padding
- * included: by the formula a query that is not a number reaches every token that it sees, whatever its
- * dO, and so does one that sees such a key; beyond that, an input that is not finite can make the
- * gradients of its neighbours (128 rows, 128 tokens) NaN that it does not reach by the formula.
+ * Tokens that no query sees get zeros, and so do queries that see nothing.  A query and a token
+ * that it does not see have no influence on one another's gradients, not numbers included.  (By the formula
+ * a query that is not a number reaches every token that it sees, whatever its dO, and so does one that
+ * sees such a key: of a batch's padding only finite values leave the tokens before it their gradients.)
  * Accumulation in fp32; bf16: weights and dS are rounded to bf16 once.  dQ, dK and dV may be slices of one
  * buffer where N_q = N_k (dK and dV always).  Bounded waits as moa_attn_fwd.  Bitwise reproducible.
  */

@@ -28,7 +28,7 @@ SOURCES = ["moa_attn_api.cu", "attn_fwd_f32_cc.cu", "attn_fwd_bf16_tc.cu", "attn
 BINDING = os.path.join(BUILD, "moa_torch.so")
 BINDING_SOURCE = "torch_binding.cpp"
 BINDING_TORCH = BINDING + ".torch"   # which PyTorch it was built against
-HEADERS = ["internal.h", "ops_internal.h", "kv4.cuh", "window.cuh", "window_tc.cuh", "ptx.cuh", "tc_common.cuh"]
+HEADERS = ["internal.h", "ops_internal.h", "kv4.cuh", "window.cuh", "window_tc.cuh", "window_again.cuh", "ptx.cuh", "tc_common.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
 

@@ -29,6 +29,7 @@
 #include "internal.h"
 #include "ops_internal.h"
 #include "window.cuh"
+#include "window_again.cuh"
 
 namespace moa {
 namespace {
@@ -199,6 +200,63 @@ struct KvSmem {
   static constexpr int kFloats = kKeysKv * (DK + 4 + DV + 4) + buffers(DK, DV) * kRows + kRowsKv * kLdW;
 };
 
+// Which of a warp's eight tokens (rows) have a sum that is not finite: thread (ty, tx) holds N features of each of four, 4 ty + a.
+template <int N>
+__device__ __forceinline__ uint32_t odd_sums(const float (&sum)[4][N]) {
+  float any = 0.f;
+#pragma unroll
+  for (int c = 0; c < N; ++c) any += (sum[0][c] * 0.f + sum[1][c] * 0.f) + (sum[2][c] * 0.f + sum[3][c] * 0.f);
+  uint32_t bad = 0;
+  if (!__any_sync(0xffffffffu, any != 0.f)) return bad;
+#pragma unroll
+  for (int a = 0; a < 4; ++a) {
+    float odd = 0.f;   // x * 0 + odd is NaN from the first x on that is not finite
+#pragma unroll
+    for (int c = 0; c < N; ++c) odd = fmaf(sum[a][c], 0.f, odd);
+    const uint32_t which = __ballot_sync(0xffffffffu, odd != 0.f);
+    bad |= uint32_t((which & 0xffffu) != 0) << a | uint32_t(which >> 16 != 0) << (a + 4);
+  }
+  return bad;
+}
+
+// dK (KEY) or dV of a warp's tokens `bad` once more, from what their rows see (window_again.cuh): sums that are not finite, as hidden
+// pairs' may not be (0 * NaN).
+template <typename T, int DK, int DV, bool KEY>
+__device__ __noinline__ void tokens_again(const Params& p, unsigned index, uint32_t bad) {
+  const unsigned per = unsigned(p.cut * p.pieces + p.n_kt - p.cut);
+  const int bh = int(index / per), item = int(index - unsigned(bh) * per);
+  const bool whole = item >= p.cut * p.pieces;
+  const int kt = whole ? item - p.cut * p.pieces + p.cut : item / p.pieces, piece = whole ? 0 : item - kt * p.pieces;
+  const int b = bh / p.Hk, h = bh - b * p.Hk, k0 = kt * kKeysKv, off = p.Nk - p.N;
+  const int keys = p.Nk - k0 < kKeysKv ? p.Nk - k0 : kKeysKv, first = 8 * (threadIdx.x >> 5);
+  const int64_t rows = int64_t(p.N) * p.G;
+  int ra, rz;
+  rows_of_piece(p, kt, whole ? -1 : piece, &ra, &rz);
+  if (keys - first < 8) bad &= keys > first ? (1u << (keys - first)) - 1 : 0u;
+  const int G = p.G;
+  const int64_t q_sh = p.q.sh, q_sn = p.q.sn, go_sh = p.go.sh, go_sn = p.go.sn;
+  const T *q = row_of<T>(p.q, b, int64_t(h) * G, 0), *go = row_of<T>(p.go, b, int64_t(h) * G, 0);
+  const float *nl = p.nl + bh * rows + ra, *delta = p.delta + bh * rows + ra;
+  win::tokens_again<T, DK, DV, KEY>(
+      bad, k0 + first, k0, k0 + keys - 1, rz - ra, p.mask, p.c_log2,
+      win::Tokens<T>{row_of<T>(p.k, b, h, 0), row_of<T>(p.v, b, h, 0), p.k.sn, p.v.sn},
+      [=](int x) {
+        const int r = ra + x, i = int(unsigned(r) / unsigned(G)), g = r - i * G;
+        return win::RowOf<T>{q + g * q_sh + i * q_sn, go + g * go_sh + i * go_sn, nl[x], delta[x], i + off};
+      },
+      [&](int j, int f, const float(&sum)[(KEY ? DK : DV) / 32]) {
+        float* to = p.part + (((int64_t(bh) * p.cut + kt) * p.pieces + piece) * kKeysKv + (j - k0)) * (DK + DV) + (KEY ? 0 : DK) + f;
+        T* dst = const_cast<T*>(row_of<T>(KEY ? p.dk : p.dv, b, h, j)) + f;
+        const float mul = KEY ? p.scale : 1.f;
+#pragma unroll
+        for (int e = 0; e < (KEY ? DK : DV) / 32; ++e)
+          if (whole)
+            dst[e] = T(sum[e] * mul);
+          else
+            to[e] = sum[e];
+      });
+}
+
 template <typename T, int DK, int DV>
 __device__ __forceinline__ void dkdv_tile(const Params& p, unsigned index, float* smem) {
   using S = KvSmem<DK, DV>;
@@ -351,6 +409,9 @@ __device__ __forceinline__ void dkdv_tile(const Params& p, unsigned index, float
     for (int c = 0; c < DV / 64; ++c)
       store4(ov + 64 * c + 4 * tx, make_float4(dv[a][4 * c], dv[a][4 * c + 1], dv[a][4 * c + 2], dv[a][4 * c + 3]));
   }
+  const uint32_t bad_k = odd_sums(dk), bad_v = odd_sums(dv);
+  if (bad_k != 0) tokens_again<T, DK, DV, true>(p, index, bad_k);
+  if (bad_v != 0) tokens_again<T, DK, DV, false>(p, index, bad_v);
 }
 
 // Adds the pieces of cut tiles: four features of a token a thread.
@@ -384,6 +445,41 @@ struct QSmem {
   static constexpr int kTokens = kKeysQ * (DK + 4 + DV + 4);   // a step's keys and values
   static constexpr int kFloats = kRowsQ * (DK + 4 + DV + 4) + buffers(DK, DV) * kTokens + kKeysQ * kLdW;
 };
+
+// dQ of a warp's rows `bad` once more, from the tokens that they see.
+template <typename T, int DK, int DV>
+__device__ __noinline__ void rows_again(const Params& p, unsigned index, uint32_t bad) {
+  const unsigned tile = index / unsigned(p.q_pieces), piece = index - tile * unsigned(p.q_pieces);
+  const int bh = int(tile / unsigned(p.n_rt)), rt = p.n_rt - 1 - int(tile - unsigned(bh) * unsigned(p.n_rt));
+  const int b = bh / p.Hk, h = bh - b * p.Hk, r0 = rt * kRowsQ, off = p.Nk - p.N, first = r0 + 8 * int(threadIdx.x >> 5);
+  const int64_t rows = int64_t(p.N) * p.G;
+  const int live = int(rows - r0 < kRowsQ ? rows - r0 : kRowsQ), i0 = r0 / p.G, i1 = (r0 + live - 1) / p.G;
+  const win::Run run = win::run_of(p.mask, p.Nk, p.N, i0, i1);
+  const int all = (run.n + kKeysQ - 1) / kKeysQ;
+  const int begin = int(int64_t(all) * piece / p.q_pieces) * kKeysQ, steps = int(int64_t(all) * (piece + 1) / p.q_pieces);
+  const int end = int64_t(steps) * kKeysQ < run.n ? steps * kKeysQ : run.n;
+  if (rows - first < 8) bad &= rows > first ? (1u << (rows - first)) - 1 : 0u;
+  win::rows_again<T, DK, DV>(
+      bad, i0 + off, i1 + off, end - begin, p.mask, p.c_log2,
+      win::Tokens<T>{row_of<T>(p.k, b, h, 0), row_of<T>(p.v, b, h, 0), p.k.sn, p.v.sn},
+      [&](int t) {
+        const int r = first + t, i = r / p.G;
+        const int64_t hq = int64_t(h) * p.G + (r - i * p.G);
+        return win::RowOf<T>{row_of<T>(p.q, b, hq, i), row_of<T>(p.go, b, hq, i), p.nl[bh * rows + r], p.delta[bh * rows + r], i + off};
+      },
+      [=](int x) { return run.at(begin + x); },
+      [&](int t, int f, const float(&sum)[DK / 32]) {
+        const int r = first + t, i = r / p.G;
+        float* to = p.part_q + (((int64_t(bh) * p.n_rt + rt) * p.q_pieces + piece) * kRowsQ + (r - r0)) * DK + f;
+        T* dst = const_cast<T*>(row_of<T>(p.dq, b, int64_t(h) * p.G + (r - i * p.G), i)) + f;
+#pragma unroll
+        for (int e = 0; e < DK / 32; ++e)
+          if (p.q_pieces > 1)
+            to[e] = sum[e];
+          else
+            dst[e] = T(sum[e] * p.scale);
+      });
+}
 
 template <typename T, int DK, int DV>
 __device__ __forceinline__ void dq_tile(const Params& p, unsigned index, float* smem) {
@@ -514,6 +610,8 @@ __device__ __forceinline__ void dq_tile(const Params& p, unsigned index, float* 
       store4(dst + 64 * c + 4 * tx, make_float4(dq[a][4 * c] * p.scale, dq[a][4 * c + 1] * p.scale, dq[a][4 * c + 2] * p.scale,
                                                 dq[a][4 * c + 3] * p.scale));
   }
+  const uint32_t bad = odd_sums(dq);
+  if (bad != 0) rows_again<T, DK, DV>(p, index, bad);
 }
 
 // Adds the pieces of dQ's tiles: four features of a row a thread.
@@ -540,7 +638,7 @@ window_dq_join_kernel(const Params p, int64_t n) {
 // CTAs below n_q: dQ; the others, whose pieces are shorter: dK and dV.
 template <typename T, int DK, int DV>
 __global__ void __launch_bounds__(kThreads, 2)
-window_bwd_cc_kernel(const Params p, unsigned n_q) {
+window_bwd_cc_kernel(const __grid_constant__ Params p, unsigned n_q) {
   extern __shared__ float smem[];
   wait_for_previous();
   if (blockIdx.x < n_q)

@@ -33,6 +33,11 @@
 // tensor pipe 49 %, no other unit half busy.  (16 compute warps: 1026 us in place of 996 at the time; score tiles of 64 columns in two
 // buffers: 1364 in place of 1000.)
 //
+// What is not finite.  Hidden pairs have the weight zero, and zero times what is not finite reaches every output of a product.  So
+// a tile with an output that is not finite is computed once more by its CTA at the end, unless nothing that is not finite is hidden from a
+// part of it: step after step without overlap, hidden dS set to zero, what is not finite taken out of the operand in steps that are seen
+// in part, and added at the end where it is seen.  (dq_again, dkdv_again.  That takes some five times as long; other calls pay nothing.)
+//
 // CTA organisation of both kinds: 8 compute warps (warp w: TMEM lanes 32 (w % 4) .., columns N / 2 (w / 4) .. of the score
 // tiles; its bf16 values go back into the first half of its own columns), one warp for TMEM and the products, one for the
 // copies.  Waits are bounded; on expiry MOA_ERR_DEVICE_TIMEOUT is recorded and
@@ -127,16 +132,22 @@ __device__ __forceinline__ float4 lds_f32x4(uint32_t addr) {
   asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
   return v;
 }
-// NCOLS fp32 TMEM columns of this thread's lane, times mul: as bf16 to dst, or as they are to part.
-template <int NCOLS>
-__device__ __forceinline__ void store_row(uint32_t taddr, float mul, __nv_bfloat16* dst, float* part, bool valid) {
-#pragma unroll
+// NCOLS fp32 TMEM columns of this thread's lane, times mul: as bf16 to dst, or as they are to part.  Whether all are finite.
+template <int NCOLS, bool ROLLED = false>
+__device__ __forceinline__ bool store_row(uint32_t taddr, float mul, __nv_bfloat16* dst, float* part, bool valid) {
+  constexpr int kUnroll = ROLLED ? 1 : NCOLS / 32;
+  float odd[4] = {0.f, 0.f, 0.f, 0.f};   // x * 0 + odd is NaN from the first x on that is not finite
+  const uint64_t none = pack_f32x2(0.f, 0.f);
+#pragma unroll(kUnroll)
   for (int c = 0; c < NCOLS; c += 32) {
     uint32_t o[32];
     tmem_ld_32x32b_x32(taddr + c, o);
     tmem_wait_ld();
     reg_anchor_x32(o);
     if (!valid) continue;
+#pragma unroll
+    for (int i = 0; i < 32; i += 2)
+      ffma2(odd[i & 2], odd[(i & 2) + 1], __uint_as_float(o[i]), __uint_as_float(o[i + 1]), none, pack_f32x2(odd[i & 2], odd[(i & 2) + 1]));
     if (part != nullptr) {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
@@ -151,7 +162,78 @@ __device__ __forceinline__ void store_row(uint32_t taddr, float mul, __nv_bfloat
         reinterpret_cast<uint4*>(dst + c)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
     }
   }
+  return (odd[0] + odd[1]) + (odd[2] + odd[3]) == 0.f;
 }
+
+// ------------------------------------------------------------------------------------------------
+// What dkdv_again and dq_again share
+// ------------------------------------------------------------------------------------------------
+__device__ __forceinline__ bool odd_word(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
+template <int D>
+__device__ __forceinline__ bool odd_row(const __nv_bfloat16* x) {
+  bool odd = false;
+#pragma unroll 4
+  for (int c = 0; c < D; c += 8) {
+    const uint4 w = *reinterpret_cast<const uint4*>(x + c);
+    odd |= odd_word(w.x) || odd_word(w.y) || odd_word(w.z) || odd_word(w.w);
+  }
+  return odd;
+}
+// All compute threads; whether all of them say so.
+__device__ __forceinline__ bool meet(bool yes) {
+  uint32_t all;
+  asm volatile("{\n\t.reg .pred a, b;\n\tsetp.ne.u32 a, %1, 0;\n\tbar.red.and.pred b, 1, %2, a;\n\tselp.u32 %0, 1, 0, b;\n\t}"
+               : "=r"(all)
+               : "r"(uint32_t(yes)), "n"(256)
+               : "memory");
+  return all != 0;
+}
+// Sets what is not finite in `rows` rows of D columns in shared memory, 64 a panel, to zero (all compute threads).
+template <int D>
+__device__ __forceinline__ void take_out(uint8_t* tile, int rows, int panel) {
+#pragma unroll 1
+  for (int x = threadIdx.x; x < rows * (D / 64); x += 256) {
+    const int q = x / rows, r = x - q * rows;
+#pragma unroll 2
+    for (int e = 0; e < 8; ++e) {   // eight lanes in eight banks
+      uint4* at = reinterpret_cast<uint4*>(tile + q * panel + r * 128 + ((e ^ r) & 7) * 16);
+      const uint4 v = *at;
+      if (!(odd_word(v.x) || odd_word(v.y) || odd_word(v.z) || odd_word(v.w))) continue;
+      uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if ((w[i] & 0x7f80u) == 0x7f80u) w[i] &= 0xffff0000u;
+        if ((w[i] & 0x7f800000u) == 0x7f800000u) w[i] &= 0xffffu;
+      }
+      *at = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+}
+// Whether some of a warp's 32 sums each, of outputs that are there, are numbers.
+__device__ __forceinline__ bool any_number(const uint32_t (&o)[32], bool there) {
+  bool any = false;
+#pragma unroll
+  for (int e = 0; e < 32; ++e) any |= __uint_as_float(o[e]) == __uint_as_float(o[e]);
+  return __any_sync(0xffffffffu, any && there);
+}
+// Adds to 32 sums the members of the rows `odd` (a lane each, its row at x) that are not finite, where sees(lane) says that the
+// thread's output sees the row; NAN_ONLY: as NaN, whatever they are.
+template <bool NAN_ONLY, typename Sees>
+__device__ __forceinline__ void add_odd(uint32_t (&o)[32], uint32_t odd, const __nv_bfloat16* x, Sees&& sees) {
+  while (odd != 0) {
+    const int b = __ffs(odd) - 1;
+    odd &= odd - 1;
+    const __nv_bfloat16* row =
+        reinterpret_cast<const __nv_bfloat16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(x), b));
+    if (!sees(b)) continue;
+#pragma unroll
+    for (int e = 0; e < 32; ++e) {
+      const float y = __bfloat162float(row[e]);
+      if (!(fabsf(y) < INFINITY)) o[e] = __float_as_uint(__uint_as_float(o[e]) + (NAN_ONLY ? __int_as_float(0x7fffffff) : y));
+    }
+  }
+}
+__device__ __forceinline__ bool sees(const win::Mask& m, int pos, int j) { return j <= pos && (pos - j < m.window || j < m.sinks); }
 
 __device__ __forceinline__ __nv_bfloat16* row_of(const View& x, int b, int h, int n) {
   return static_cast<__nv_bfloat16*>(x.p) + b * x.sb + h * x.sh + n * x.sn;
@@ -268,8 +350,8 @@ struct KvCfg {
   static constexpr int kStageBytes = (kQBytes + kGBytes + 2 * kVecBytes + 1023) / 1024 * 1024;
   static constexpr int kStages = ring_stages(DK, DV);
   static constexpr int kOffK = 0, kOffV = kKBytes, kOffStage = kKBytes + kVBytes;
-  // barriers: full[NS], empty[NS], kv_full, s_full, dp_full, p_ready, ds_ready, acc_done
-  static constexpr int kNumBars = 2 * kStages + 6;
+  // barriers: full[NS], empty[NS], kv_full, s_full, dp_full, p_ready, ds_ready, acc_done, again_loaded, again_done
+  static constexpr int kNumBars = 2 * kStages + 8;
   static constexpr int kOffBar = kOffStage + kStages * kStageBytes;
   static constexpr int kOffMisc = kOffBar + kNumBars * 8;
   static constexpr int kSmemBytes = kOffMisc + 16 + 1024;
@@ -297,6 +379,232 @@ __host__ __device__ __forceinline__ KvItem kv_item(const Params& p, int64_t x) {
   k.kt = k.whole ? int(item - n_cut) + p.cut : int(item / p.pieces);
   k.piece = k.whole ? 0 : int(item - int64_t(k.kt) * p.pieces);
   return k;
+}
+
+// The products of a step: S^T = K Q^T (M = 128 tokens, N rows, both operands K-major), dP^T = V dO^T,
+// dV += P^T dO and dK += dS^T Q (A from TMEM, B MN-major).
+template <int DK, int DV>
+__device__ __forceinline__ void issue_scores(uint32_t tS, uint32_t sK, uint32_t sQ) {
+  using C = KvCfg<DK, DV>;
+  constexpr uint32_t kIdesc = make_idesc(kBlk, C::kN, false);
+#pragma unroll
+  for (int kk = 0; kk < DK / 16; ++kk) {
+    const uint32_t k = (kk >> 2) * kPanelBytes + (kk & 3) * 32, r = (kk >> 2) * C::kRowPanel + (kk & 3) * 32;
+    mma_f16_ss(tS, make_sdesc_sw128(sK + k, 16, 1024), make_sdesc_sw128(sQ + r, 16, 1024), kIdesc, kk > 0 ? 1u : 0u);
+  }
+}
+template <int DK, int DV>
+__device__ __forceinline__ void issue_changes(uint32_t tDP, uint32_t sV, uint32_t sG) {
+  using C = KvCfg<DK, DV>;
+  constexpr uint32_t kIdesc = make_idesc(kBlk, C::kN, false);
+#pragma unroll
+  for (int kk = 0; kk < DV / 16; ++kk) {
+    const uint32_t k = (kk >> 2) * kPanelBytes + (kk & 3) * 32, r = (kk >> 2) * C::kRowPanel + (kk & 3) * 32;
+    mma_f16_ss(tDP, make_sdesc_sw128(sV + k, 16, 1024), make_sdesc_sw128(sG + r, 16, 1024), kIdesc, kk > 0 ? 1u : 0u);
+  }
+}
+template <int DK, int DV>
+__device__ __forceinline__ void issue_dv(uint32_t tDV, uint32_t tS, uint32_t sG, bool more) {
+  using C = KvCfg<DK, DV>;
+  constexpr uint32_t kIdesc = make_idesc(kBlk, DV, true);
+#pragma unroll
+  for (int kk = 0; kk < C::kN / 16; ++kk)
+    mma_f16_ts(tDV, tS + part_col<C::kCols>(kk), make_sdesc_sw128(sG + kk * 2048, C::kRowPanel, 1024), kIdesc, (kk > 0 || more) ? 1u : 0u);
+}
+template <int DK, int DV>
+__device__ __forceinline__ void issue_dk(uint32_t tDK, uint32_t tDP, uint32_t sQ, bool more) {
+  using C = KvCfg<DK, DV>;
+  constexpr uint32_t kIdesc = make_idesc(kBlk, DK, true);
+#pragma unroll
+  for (int kk = 0; kk < C::kN / 16; ++kk)
+    mma_f16_ts(tDK, tDP + part_col<C::kCols>(kk), make_sdesc_sw128(sQ + kk * 2048, C::kRowPanel, 1024), kIdesc, (kk > 0 || more) ? 1u : 0u);
+}
+
+// A dK and dV tile once more, by the compute warps alone, if what is not finite may have come through a product.
+template <int DK, int DV>
+__device__ __noinline__ void dkdv_again(const CUtensorMap* tmQ, const CUtensorMap* tmG, const Params& p, unsigned index, uint8_t* smem, uint32_t tmem) {
+  using C = KvCfg<DK, DV>;
+  constexpr int kCols = C::kCols;
+  const uint32_t sK = smem_u32(smem + C::kOffK), sV = smem_u32(smem + C::kOffV), sQ = smem_u32(smem + C::kOffStage), sG = sQ + C::kQBytes;
+  const uint32_t loaded = smem_u32(smem + C::kOffBar) + 8u * (2 * C::kStages + 6), done = loaded + 8;
+  const WaitCtl wc{reinterpret_cast<volatile int*>(smem + C::kOffMisc + 4), p.wait_limit_ns, 0u, &g_moa_window_bwd_status};
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp >> 2, lane_base = (warp & 3) * 32, row = lane_base + lane;
+  const uint32_t lanes = uint32_t(lane_base) << 16;
+  const uint32_t tS = tmem + C::kTmemS, tDP = tmem + C::kTmemDP, tDV = tmem + C::kTmemDV, tDK = tmem + C::kTmemDK;
+  const KvItem it = kv_item(p, index);
+  const int k0 = it.kt * kBlk, k1 = (k0 + kBlk < p.Nk ? k0 + kBlk : p.Nk) - 1, off = p.Nk - p.N, key = k0 + row;
+  const Range range = rows_of_tokens(p.mask, it.kt, p.N, p.Nk, C::kHalves * p.PT);
+  const int all = range.n * p.chunks, t0 = it.whole ? 0 : it.piece * p.piece;
+  const int n_t = it.whole ? all : all - t0 < p.piece ? all - t0 : p.piece;
+  const int64_t bh = int64_t(it.b) * p.Hk + it.h;
+  struct Row {
+    int hq, i;
+    int64_t at;
+    bool real;
+  };
+  auto tile_of = [&](int t, int* chunk) {   // the first half of row tile number t of the piece
+    *chunk = (t0 + t) / range.n;
+    return (range.first + (t0 + t) - *chunk * range.n) * C::kHalves;
+  };
+  auto row_of_tile = [&](int t, int r) {
+    int chunk;
+    const int half = tile_of(t, &chunk) + r / kHalf, in_half = r % kHalf, pos = in_half / p.GC, g = chunk * p.GC + in_half - pos * p.GC;
+    const int i = half * p.PT + pos;
+    return Row{it.h * p.G + g, i, (int64_t(bh * p.chunks + chunk) * p.n_ht + half) * kHalf + in_half, pos < p.PT && g < p.G && i < p.N};
+  };
+  // whether a token of the tile does not see some row of a row tile
+  auto partly = [&](int t) {
+    int chunk;
+    const int half = tile_of(t, &chunk), p0 = half * p.PT + off, p1 = p0 + C::kHalves * p.PT - 1;
+    return p0 < k1 || (p1 - k0 >= p.mask.window && k1 >= p.mask.sinks);
+  };
+  {
+    bool odd = false;
+    if (part == 0 && key < p.Nk) odd = odd_row<DK>(row_of(p.k, it.b, it.h, key)) || odd_row<DV>(row_of(p.v, it.b, it.h, key));
+#pragma unroll 1
+    for (int t = 0; t < n_t; ++t) {
+      if (!partly(t) || int(threadIdx.x) >= C::kN) continue;
+      const Row r = row_of_tile(t, threadIdx.x);
+      if (!r.real) continue;
+      odd |= !(p.nl[r.at] < INFINITY) || !(fabsf(p.delta[r.at]) < INFINITY) || odd_row<DK>(row_of(p.q, it.b, r.hq, r.i)) ||
+             odd_row<DV>(row_of(p.go, it.b, r.hq, r.i));
+    }
+    if (meet(!odd)) return;
+  }
+  const bool first = threadIdx.x == 0, bounded = p.mask.window != win::kNoWindow && key >= p.mask.sinks;
+  bool ok = true;
+  uint32_t products = 0;
+#pragma unroll 1
+  for (int t = 0; t < n_t; ++t) {
+    int chunk;
+    const int half = tile_of(t, &chunk);
+    ok = meet(ok);   // the row tile before is done with
+    if (!ok) break;
+    if (first) {
+      mbar_arrive_expect_tx(loaded, C::kHalves * (DK + DV) * 2 * p.GC * p.PT + 2 * C::kVecBytes);
+#pragma unroll 1
+      for (int f = 0; f < C::kHalves; ++f) {
+        const int i0 = (half + f) * p.PT;
+#pragma unroll 1
+        for (int q = 0; q < DK / 64; ++q)
+          tma_load_5d(sQ + q * C::kRowPanel + f * kHalf * 128, tmQ, loaded, q * 64, chunk * p.GC, i0, it.h, it.b);
+#pragma unroll 1
+        for (int q = 0; q < DV / 64; ++q)
+          tma_load_5d(sG + q * C::kRowPanel + f * kHalf * 128, tmG, loaded, q * 64, chunk * p.GC, i0, it.h, it.b);
+      }
+      const int64_t vrow = ((bh * p.chunks + chunk) * p.n_ht + half) * kHalf;
+      bulk_load(sG + C::kGBytes, p.nl + vrow, C::kVecBytes, loaded);
+      bulk_load(sG + C::kGBytes + C::kVecBytes, p.delta + vrow, C::kVecBytes, loaded);
+    }
+    ok = wait_bounded(loaded, uint32_t(t) & 1u, wc);
+    if (first) {
+      tc_fence_after_sync();
+      issue_scores<DK, DV>(tS, sK, sQ);
+      issue_changes<DK, DV>(tDP, sV, sG);
+      mma_commit(done);
+    }
+    ok = wait_bounded(done, products++ & 1u, wc) && ok;
+    tc_fence_after_sync();
+    const int p0 = half * p.PT + part * kCols / kHalf * p.PT + off, ahead = key - p0;
+    int from = ahead <= 0 ? 0 : ahead >= p.PT ? kHalf : ahead * p.GC, upto = kHalf;
+    if (bounded) {
+      const int64_t left = int64_t(ahead) + p.mask.window;
+      upto = left <= 0 ? 0 : left >= p.PT ? kHalf : int(left) * p.GC;
+    }
+    from -= part * kCols % kHalf, upto -= part * kCols % kHalf;
+    const uint32_t nl4 = sG + C::kGBytes + part * kCols * 4, d4 = nl4 + C::kVecBytes;
+#pragma unroll 1
+    for (int c = 0; c < kCols; c += 32) {
+      const uint32_t bits = below(upto, c / 32) & ~below(from, c / 32);
+      uint32_t r[32], pk[16];
+      float w[32];
+      tmem_ld_32x32b_x32(tS + lanes + part * kCols + c, r);
+      tmem_wait_ld();
+      reg_anchor_x32(r);
+#pragma unroll
+      for (int e = 0; e < 32; e += 4) {
+        const float4 l = lds_f32x4(nl4 + (c + e) * 4);
+        const float x[4] = {l.x, l.y, l.z, l.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          w[e + i] = bits >> (e + i) & 1u ? ex2_approx(fmaf(__uint_as_float(r[e + i]), p.c_log2, x[i])) : 0.f;
+      }
+#pragma unroll
+      for (int e = 0; e < 32; e += 2) pk[e >> 1] = pack_bf16x2(w[e], w[e + 1]);
+      tmem_st_32x32b_x16(tS + lanes + part * kCols + c / 2, pk);
+      tmem_ld_32x32b_x32(tDP + lanes + part * kCols + c, r);
+      tmem_wait_ld();
+      reg_anchor_x32(r);
+#pragma unroll
+      for (int e = 0; e < 32; e += 4) {
+        const float4 d = lds_f32x4(d4 + (c + e) * 4);
+        const float x[4] = {d.x, d.y, d.z, d.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[e + i] = bits >> (e + i) & 1u ? w[e + i] * (__uint_as_float(r[e + i]) - x[i]) : 0.f;
+      }
+#pragma unroll
+      for (int e = 0; e < 32; e += 2) pk[e >> 1] = pack_bf16x2(w[e], w[e + 1]);
+      tmem_st_32x32b_x16(tDP + lanes + part * kCols + c / 2, pk);
+      tmem_wait_st();
+    }
+    if (partly(t)) {
+      take_out<DK>(smem + C::kOffStage, C::kN, C::kRowPanel);
+      take_out<DV>(smem + C::kOffStage + C::kQBytes, C::kN, C::kRowPanel);
+      fence_proxy_async_smem();
+    }
+    tc_fence_before_sync();
+    ok = meet(ok);
+    if (first) {
+      tc_fence_after_sync();
+      issue_dv<DK, DV>(tDV, tS, sG, t > 0);
+      issue_dk<DK, DV>(tDK, tDP, sQ, t > 0);
+      mma_commit(done);
+    }
+    ok = wait_bounded(done, products++ & 1u, wc) && ok;
+    tc_fence_after_sync();
+  }
+  ok = meet(ok);
+  if (!ok) {   // the last copies and products end before the CTA does
+    if (first) {
+      wait_quiesce(loaded, uint32_t(n_t - 1) & 1u, wc.limit_ns, wc.status);
+      wait_quiesce(done, (products - 1) & 1u, wc.limit_ns, wc.status);
+    }
+    return;
+  }
+  // what was taken out, to the tokens that it reaches
+  const uint32_t acc = lanes + (part == 0 ? tDV : tDK);
+#pragma unroll 1
+  for (int c = 0; c < (part == 0 ? DV : DK); c += 32) {
+    uint32_t o[32];
+    tmem_ld_32x32b_x32(acc + c, o);
+    tmem_wait_ld();
+    reg_anchor_x32(o);
+#pragma unroll 1
+    for (int t = 0; t < n_t && any_number(o, key < p.Nk); ++t) {
+      if (!partly(t)) continue;
+#pragma unroll 1
+      for (int r0 = 0; r0 < C::kN; r0 += 32) {
+        const Row r = row_of_tile(t, r0 + lane);
+        const __nv_bfloat16* x = r.real ? row_of(part == 0 ? p.go : p.q, it.b, r.hq, r.i) + c : nullptr;
+        const uint32_t odd = __ballot_sync(0xffffffffu, x != nullptr && odd_row<32>(x));
+        if (odd == 0) continue;
+        auto seen = [&](int b) { return key < p.Nk && sees(p.mask, row_of_tile(t, r0 + b).i + off, key); };
+        if (part == 0)
+          add_odd<false>(o, odd, x, seen);
+        else
+          add_odd<true>(o, odd, x, seen);
+      }
+    }
+    tmem_st_32x32b_x32(acc + c, o);
+    tmem_wait_st();
+  }
+  const bool valid = key < p.Nk;
+  float* piece = it.whole ? nullptr : p.part + (((bh * p.cut + it.kt) * p.pieces + it.piece) * kBlk + row) * (DK + DV);
+  if (part == 0)
+    store_row<DV, true>(acc, 1.f, row_of(p.dv, it.b, it.h, valid ? key : 0), piece ? piece + DK : nullptr, valid);
+  else
+    store_row<DK, true>(acc, p.scale, row_of(p.dk, it.b, it.h, valid ? key : 0), piece, valid);
+  tc_fence_before_sync();
 }
 
 template <int DK, int DV>
@@ -354,6 +662,7 @@ __device__ __forceinline__ void dkdv_tile(const CUtensorMap& tmQ, const CUtensor
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = *tmem_slot;
+  bool bad = false;   // the thread's outputs are not all finite
 
   if (warp == kLoadWarp) {
     // ---------------------------------------------------------------- TMA producer
@@ -418,29 +727,16 @@ __device__ __forceinline__ void dkdv_tile(const CUtensorMap& tmQ, const CUtensor
   } else if (warp == kMmaWarp) {
     // ---------------------------------------------------------------- MMA issuer
     if (lane == 0) {
-      constexpr uint32_t kIdescS = make_idesc(kBlk, C::kN, false);
-      constexpr uint32_t kIdescDV = make_idesc(kBlk, DV, true);
-      constexpr uint32_t kIdescDK = make_idesc(kBlk, DK, true);
       const uint32_t tS = tmem + C::kTmemS, tDP = tmem + C::kTmemDP;
       const uint32_t tDV = tmem + C::kTmemDV, tDK = tmem + C::kTmemDK;
       int slot = 0;
       uint32_t phase = 0;
-      // S^T = K Q^T: M = 128 tokens, N rows, both operands K-major
       auto issue_s = [&](uint32_t sQ) {
-#pragma unroll
-        for (int kk = 0; kk < DK / 16; ++kk) {
-          const uint32_t k = (kk >> 2) * kPanelBytes + (kk & 3) * 32, r = (kk >> 2) * C::kRowPanel + (kk & 3) * 32;
-          mma_f16_ss(tS, make_sdesc_sw128(sK + k, 16, 1024), make_sdesc_sw128(sQ + r, 16, 1024), kIdescS, kk > 0 ? 1u : 0u);
-        }
+        issue_scores<DK, DV>(tS, sK, sQ);
         mma_commit(s_full);
       };
-      // dP^T = V dO^T
       auto issue_dp = [&](uint32_t sG) {
-#pragma unroll
-        for (int kk = 0; kk < DV / 16; ++kk) {
-          const uint32_t k = (kk >> 2) * kPanelBytes + (kk & 3) * 32, r = (kk >> 2) * C::kRowPanel + (kk & 3) * 32;
-          mma_f16_ss(tDP, make_sdesc_sw128(sV + k, 16, 1024), make_sdesc_sw128(sG + r, 16, 1024), kIdescS, kk > 0 ? 1u : 0u);
-        }
+        issue_changes<DK, DV>(tDP, sV, sG);
         mma_commit(dp_full);
       };
       auto stage = [&](int st) { return sStage + st * C::kStageBytes; };
@@ -465,10 +761,7 @@ __device__ __forceinline__ void dkdv_tile(const CUtensorMap& tmQ, const CUtensor
         ok = wait_bounded(p_ready, par, wc);
         if (!ok) break;
         tc_fence_after_sync();
-#pragma unroll
-        for (int kk = 0; kk < C::kN / 16; ++kk)
-          mma_f16_ts(tDV, tS + part_col<kCols>(kk), make_sdesc_sw128(sG + kk * 2048, C::kRowPanel, 1024), kIdescDV,
-                     (kk > 0 || i > 0) ? 1u : 0u);
+        issue_dv<DK, DV>(tDV, tS, sG, i > 0);
         const bool more = i + 1 < n_t;
         if (more) {
           ok = wait_bounded(full_bar(slot), phase, wc);
@@ -480,10 +773,7 @@ __device__ __forceinline__ void dkdv_tile(const CUtensorMap& tmQ, const CUtensor
         ok = wait_bounded(ds_ready, par, wc);
         if (!ok) break;
         tc_fence_after_sync();
-#pragma unroll
-        for (int kk = 0; kk < C::kN / 16; ++kk)
-          mma_f16_ts(tDK, tDP + part_col<kCols>(kk), make_sdesc_sw128(sQ + kk * 2048, C::kRowPanel, 1024), kIdescDK,
-                     (kk > 0 || i > 0) ? 1u : 0u);
+        issue_dk<DK, DV>(tDK, tDP, sQ, i > 0);
         mma_commit(empty_bar(st));
         if (more) issue_dp(stage(slot) + C::kQBytes);
       }
@@ -585,16 +875,28 @@ __device__ __forceinline__ void dkdv_tile(const CUtensorMap& tmQ, const CUtensor
     } else if (ok && wait_warp(acc_done, 0)) {
       tc_fence_after_sync();
       float* piece = it.whole ? nullptr : p.part + (((bh * p.cut + it.kt) * p.pieces + it.piece) * kBlk + row) * (DK + DV);
-      if (part == 0)
-        store_row<DV>(tmem + lanes + C::kTmemDV, 1.f, row_of(p.dv, it.b, it.h, valid ? key : 0), piece ? piece + DK : nullptr, valid);
-      else
-        store_row<DK>(tmem + lanes + C::kTmemDK, p.scale, row_of(p.dk, it.b, it.h, valid ? key : 0), piece, valid);
+      bad = !(part == 0 ? store_row<DV>(tmem + lanes + C::kTmemDV, 1.f, row_of(p.dv, it.b, it.h, valid ? key : 0), piece ? piece + DK : nullptr, valid)
+                        : store_row<DK>(tmem + lanes + C::kTmemDK, p.scale, row_of(p.dk, it.b, it.h, valid ? key : 0), piece, valid));
     }
   }
 
   if (warp == kMmaWarp && lane == 0) wait_quiesce(acc_done, 0, p.wait_limit_ns, &g_moa_window_bwd_status);
   tc_fence_before_sync();
-  __syncthreads();
+  if (__syncthreads_or(bad)) {
+    const bool dead = *abort_flag != 0;
+    if (threadIdx.x == 0) {
+      mbar_init(acc_done + 8, 1);
+      mbar_init(acc_done + 8 + 8, 1);
+      fence_barrier_init();
+    }
+    __syncthreads();
+    if (!dead && warp < kMmaWarp) {
+      tc_fence_after_sync();
+      dkdv_again<DK, DV>(&tmQ, &tmG, p, index, smem, tmem);
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+  }
   if (warp == kMmaWarp) {
     tc_fence_after_sync();
     tmem_dealloc(tmem, C::kTmemCols);
@@ -640,8 +942,8 @@ struct QCfg {
   static constexpr int kStageBytes = kKBytes + kVBytes;
   static constexpr int kStages = ring_stages(DK, DV);
   static constexpr int kOffQ = 0, kOffG = kQBytes, kOffStage = kQBytes + kGBytes;
-  // barriers: full[NS], empty[NS], q_full, s_full, dp_full, ds_ready, acc_done, s_free
-  static constexpr int kNumBars = 2 * kStages + 6;
+  // barriers: full[NS], empty[NS], q_full, s_full, dp_full, ds_ready, acc_done, s_free, again_loaded, again_done
+  static constexpr int kNumBars = 2 * kStages + 8;
   static constexpr int kOffBar = kOffStage + kStages * kStageBytes;
   static constexpr int kOffMisc = kOffBar + kNumBars * 8;
   static constexpr int kSmemBytes = kOffMisc + 16 + 1024;
@@ -650,6 +952,185 @@ struct QCfg {
   static_assert(kTmemDQ + DK <= kTmemCols, "TMEM budget");
   static_assert((kSmemBytes + 1024) * ctas_of(DK, DV) <= 233472, "shared memory budget");
 };
+
+// The products of a step: S = Q K^T, dP = dO V^T, dQ += dS K (A from TMEM, B MN-major).
+template <int DK, int DV>
+__device__ __forceinline__ void issue_row_scores(uint32_t tS, uint32_t sQ, uint32_t sK) {
+  using C = QCfg<DK, DV>;
+  constexpr uint32_t kIdesc = make_idesc(kBlk, C::kN, false);
+#pragma unroll
+  for (int kk = 0; kk < DK / 16; ++kk) {
+    const uint32_t r = (kk >> 2) * kPanelBytes + (kk & 3) * 32, k = (kk >> 2) * C::kTokenPanel + (kk & 3) * 32;
+    mma_f16_ss(tS, make_sdesc_sw128(sQ + r, 16, 1024), make_sdesc_sw128(sK + k, 16, 1024), kIdesc, kk > 0 ? 1u : 0u);
+  }
+}
+template <int DK, int DV>
+__device__ __forceinline__ void issue_row_changes(uint32_t tDP, uint32_t sG, uint32_t sV) {
+  using C = QCfg<DK, DV>;
+  constexpr uint32_t kIdesc = make_idesc(kBlk, C::kN, false);
+#pragma unroll
+  for (int kk = 0; kk < DV / 16; ++kk) {
+    const uint32_t r = (kk >> 2) * kPanelBytes + (kk & 3) * 32, k = (kk >> 2) * C::kTokenPanel + (kk & 3) * 32;
+    mma_f16_ss(tDP, make_sdesc_sw128(sG + r, 16, 1024), make_sdesc_sw128(sV + k, 16, 1024), kIdesc, kk > 0 ? 1u : 0u);
+  }
+}
+template <int DK, int DV>
+__device__ __forceinline__ void issue_dq(uint32_t tDQ, uint32_t tDP, uint32_t sK, bool more) {
+  using C = QCfg<DK, DV>;
+  constexpr uint32_t kIdesc = make_idesc(kBlk, DK, true);
+#pragma unroll
+  for (int kk = 0; kk < C::kN / 16; ++kk)
+    mma_f16_ts(tDQ, tDP + part_col<C::kCols>(kk), make_sdesc_sw128(sK + kk * 2048, C::kTokenPanel, 1024), kIdesc, (kk > 0 || more) ? 1u : 0u);
+}
+
+// A dQ tile's work: the pair of halves, this piece's token tiles [j0, j0 + n) of the list.
+struct QItem {
+  int64_t tile;
+  RowTile t;
+  win::Tiles list;
+  int piece, i1, j0, n;
+};
+template <int DK, int DV>
+__device__ __forceinline__ QItem q_item(const Params& p, unsigned index) {
+  QItem x;
+  // the last positions, which see the most without a window, come first
+  const unsigned which = index / unsigned(p.q_pieces);
+  x.piece = int(index - which * unsigned(p.q_pieces));
+  const int64_t per = int64_t(p.chunks) * (p.n_ht / 2), group = which / per;
+  x.tile = group * per + (per - 1 - (which - group * per));
+  x.t = row_tile(p, x.tile);
+  // (a pair's positions may all lie past the end)
+  x.i1 = x.t.i0 + 2 * p.PT - 1 < p.N ? x.t.i0 + 2 * p.PT - 1 : p.N - 1;
+  x.list = win::tiles_of(p.mask, p.Nk, p.N, x.t.i0, x.i1, QCfg<DK, DV>::kN);
+  x.j0 = int(int64_t(x.list.n) * x.piece / p.q_pieces);
+  x.n = int(int64_t(x.list.n) * (x.piece + 1) / p.q_pieces) - x.j0;
+  return x;
+}
+
+// A dQ tile once more, by the compute warps alone, if what is not finite may have come through a product.
+template <int DK, int DV>
+__device__ __noinline__ void dq_again(const CUtensorMap* tmK, const CUtensorMap* tmV, const Params& p, unsigned index, uint8_t* smem, uint32_t tmem) {
+  using C = QCfg<DK, DV>;
+  constexpr int kCols = C::kCols, wq = DK / kParts;
+  const uint32_t sQ = smem_u32(smem + C::kOffQ), sG = smem_u32(smem + C::kOffG), sK = smem_u32(smem + C::kOffStage), sV = sK + C::kKBytes;
+  const uint32_t loaded = smem_u32(smem + C::kOffBar) + 8u * (2 * C::kStages + 6), done = loaded + 8;
+  const WaitCtl wc{reinterpret_cast<volatile int*>(smem + C::kOffMisc + 4), p.wait_limit_ns, 0u, &g_moa_window_bwd_status};
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp >> 2, lane_base = (warp & 3) * 32, row = lane_base + lane;
+  const uint32_t lanes = uint32_t(lane_base) << 16;
+  const uint32_t tS = tmem + C::kTmemS, tDP = tmem + C::kTmemDP, tDQ = tmem + C::kTmemDQ;
+  const QItem x = q_item<DK, DV>(p, index);
+  const RowAt at = row_at(p, x.t, row);
+  const bool live = at.real;
+  const float nl = p.nl[x.tile * kBlk + row], dd = p.delta[x.tile * kBlk + row];
+  const int off = p.Nk - p.N, p0 = x.t.i0 + off, p1 = x.i1 + off, pos = at.i + off;
+  const int lim = live ? win::row_end(p.mask, p.Nk, p.N, at.i) : 0, low = live ? win::row_low(p.mask, p.Nk, p.N, at.i) : 0;
+  // whether a row of the tile does not see some token of the tile from n0 on
+  auto partly = [&](int n0) { return n0 + C::kN - 1 > p0 || (p1 - n0 >= p.mask.window && n0 + C::kN > p.mask.sinks); };
+  {
+    // (a row that sees nothing, and is none, has what hidden tokens give only)
+    bool odd = live && pos < 0 && (!(nl < INFINITY) || !(fabsf(dd) < INFINITY) || odd_row<DK>(row_of(p.q, x.t.b, x.t.h * p.G + at.g, at.i)));
+#pragma unroll 1
+    for (int j = 0; j < x.n; ++j) {
+      const int n0 = x.list.at(x.j0 + j) * C::kN, token = n0 + int(threadIdx.x);
+      if (!partly(n0) || int(threadIdx.x) >= C::kN || token >= p.Nk) continue;
+      odd |= odd_row<DK>(row_of(p.k, x.t.b, x.t.h, token)) || odd_row<DV>(row_of(p.v, x.t.b, x.t.h, token));
+    }
+    if (meet(!odd)) return;
+  }
+  const bool first = threadIdx.x == 0;
+  bool ok = true;
+  uint32_t products = 0;
+#pragma unroll 1
+  for (int j = 0; j < x.n; ++j) {
+    const int n0 = x.list.at(x.j0 + j) * C::kN;
+    ok = meet(ok);   // the tile before is done with
+    if (!ok) break;
+    if (first) {
+      mbar_arrive_expect_tx(loaded, C::kStageBytes);
+#pragma unroll 1
+      for (int q = 0; q < DK / 64; ++q) tma_load_4d(sK + q * C::kTokenPanel, tmK, loaded, q * 64, n0, x.t.h, x.t.b);
+#pragma unroll 1
+      for (int q = 0; q < DV / 64; ++q) tma_load_4d(sV + q * C::kTokenPanel, tmV, loaded, q * 64, n0, x.t.h, x.t.b);
+    }
+    ok = wait_bounded(loaded, uint32_t(j) & 1u, wc);
+    if (first) {
+      tc_fence_after_sync();
+      issue_row_scores<DK, DV>(tS, sQ, sK);
+      issue_row_changes<DK, DV>(tDP, sG, sV);
+      mma_commit(done);
+    }
+    ok = wait_bounded(done, products++ & 1u, wc) && ok;
+    tc_fence_after_sync();
+#pragma unroll 1
+    for (int c = 0; c < kCols; c += 32) {
+      const int t0 = n0 + part * kCols + c;
+      const uint32_t bits = below(lim - t0, 0) & (~below(low - t0, 0) | below(p.mask.sinks - t0, 0));
+      uint32_t r[32], pk[16];
+      float w[32];
+      tmem_ld_32x32b_x32(tS + lanes + part * kCols + c, r);
+      tmem_wait_ld();
+      reg_anchor_x32(r);
+#pragma unroll
+      for (int e = 0; e < 32; ++e) w[e] = bits >> e & 1u ? ex2_approx(fmaf(__uint_as_float(r[e]), p.c_log2, nl)) : 0.f;
+      tmem_ld_32x32b_x32(tDP + lanes + part * kCols + c, r);
+      tmem_wait_ld();
+      reg_anchor_x32(r);
+#pragma unroll
+      for (int e = 0; e < 32; ++e) w[e] = bits >> e & 1u ? w[e] * (__uint_as_float(r[e]) - dd) : 0.f;
+#pragma unroll
+      for (int e = 0; e < 32; e += 2) pk[e >> 1] = pack_bf16x2(w[e], w[e + 1]);
+      tmem_st_32x32b_x16(tDP + lanes + part * kCols + c / 2, pk);
+      tmem_wait_st();
+    }
+    if (partly(n0)) {
+      take_out<DK>(smem + C::kOffStage, C::kN, C::kTokenPanel);
+      fence_proxy_async_smem();
+    }
+    tc_fence_before_sync();
+    ok = meet(ok);
+    if (first) {
+      tc_fence_after_sync();
+      issue_dq<DK, DV>(tDQ, tDP, sK, j > 0);
+      mma_commit(done);
+    }
+    ok = wait_bounded(done, products++ & 1u, wc) && ok;
+    tc_fence_after_sync();
+  }
+  ok = meet(ok);
+  if (!ok) {   // the last copies and products end before the CTA does
+    if (first) {
+      wait_quiesce(loaded, uint32_t(x.n - 1) & 1u, wc.limit_ns, wc.status);
+      wait_quiesce(done, (products - 1) & 1u, wc.limit_ns, wc.status);
+    }
+    return;
+  }
+  // what was taken out, to the rows that see it
+  const uint32_t acc = tDQ + lanes + part * wq;
+#pragma unroll 1
+  for (int c = 0; c < wq; c += 32) {
+    uint32_t o[32];
+    tmem_ld_32x32b_x32(acc + c, o);
+    tmem_wait_ld();
+    reg_anchor_x32(o);
+#pragma unroll 1
+    for (int j = 0; j < x.n && any_number(o, live); ++j) {
+      const int n0 = x.list.at(x.j0 + j) * C::kN;
+      if (!partly(n0)) continue;
+#pragma unroll 1
+      for (int r0 = 0; r0 < C::kN; r0 += 32) {
+        const int token = n0 + r0 + lane;
+        const __nv_bfloat16* k = token < p.Nk ? row_of(p.k, x.t.b, x.t.h, token) + part * wq + c : nullptr;
+        const uint32_t odd = __ballot_sync(0xffffffffu, k != nullptr && odd_row<32>(k));
+        if (odd != 0) add_odd<true>(o, odd, k, [&](int b) { return live && sees(p.mask, pos, n0 + r0 + b); });
+      }
+    }
+    tmem_st_32x32b_x32(acc + c, o);
+    tmem_wait_st();
+  }
+  store_row<wq, true>(acc, p.scale, row_of(p.dq, x.t.b, x.t.h * p.G + (live ? at.g : 0), live ? at.i : 0) + part * wq,
+                      p.q_pieces > 1 ? p.part_q + ((x.tile * p.q_pieces + x.piece) * kBlk + row) * DK + part * wq : nullptr, live);
+  tc_fence_before_sync();
+}
 
 template <int DK, int DV>
 __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV,
@@ -670,16 +1151,11 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const WaitCtl wc{abort_flag, p.wait_limit_ns, 0u, &g_moa_window_bwd_status};
 
-  // the last positions, which see the most without a window, come first
-  const unsigned which = index / unsigned(p.q_pieces), piece = index - which * unsigned(p.q_pieces);
-  const int64_t per = int64_t(p.chunks) * (p.n_ht / 2), group = which / per;
-  const int64_t tile_id = group * per + (per - 1 - (which - group * per));
-  const RowTile t = row_tile(p, tile_id);
-  // (a pair's positions may all lie past the end)
-  const int i1 = t.i0 + 2 * p.PT - 1 < p.N ? t.i0 + 2 * p.PT - 1 : p.N - 1;
-  const win::Tiles list = win::tiles_of(p.mask, p.Nk, p.N, t.i0, i1, C::kN);
-  // this piece's tiles of the list
-  const int j0 = int(int64_t(list.n) * piece / p.q_pieces), n_kt = int(int64_t(list.n) * (piece + 1) / p.q_pieces) - j0;
+  const QItem x = q_item<DK, DV>(p, index);
+  const RowTile& t = x.t;
+  const win::Tiles& list = x.list;
+  const int64_t tile_id = x.tile;
+  const int piece = x.piece, j0 = x.j0, n_kt = x.n;
   if (n_kt == 0 && p.q_pieces > 1) return;   // the join adds what pieces there are
 
   if (threadIdx.x == 0) {
@@ -709,6 +1185,7 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = *tmem_slot;
+  bool bad = false;   // the thread's outputs are not all finite
 
   if (warp == kLoadWarp) {
     // ---------------------------------------------------------------- TMA producer
@@ -759,26 +1236,16 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
   } else if (warp == kMmaWarp) {
     // ---------------------------------------------------------------- MMA issuer
     if (lane == 0) {
-      constexpr uint32_t kIdescS = make_idesc(kBlk, C::kN, false);
-      constexpr uint32_t kIdescDQ = make_idesc(kBlk, DK, true);
       const uint32_t tS = tmem + C::kTmemS, tDP = tmem + C::kTmemDP, tDQ = tmem + C::kTmemDQ;
       int slot = 0;
       uint32_t phase = 0;
       auto stage = [&](int st) { return sStage + st * C::kStageBytes; };
-      auto issue_s = [&](uint32_t sK) {   // S = Q K^T
-#pragma unroll
-        for (int kk = 0; kk < DK / 16; ++kk) {
-          const uint32_t r = (kk >> 2) * kPanelBytes + (kk & 3) * 32, k = (kk >> 2) * C::kTokenPanel + (kk & 3) * 32;
-          mma_f16_ss(tS, make_sdesc_sw128(sQ + r, 16, 1024), make_sdesc_sw128(sK + k, 16, 1024), kIdescS, kk > 0 ? 1u : 0u);
-        }
+      auto issue_s = [&](uint32_t sK) {
+        issue_row_scores<DK, DV>(tS, sQ, sK);
         mma_commit(s_full);
       };
-      auto issue_dp = [&](uint32_t sV) {   // dP = dO V^T
-#pragma unroll
-        for (int kk = 0; kk < DV / 16; ++kk) {
-          const uint32_t r = (kk >> 2) * kPanelBytes + (kk & 3) * 32, k = (kk >> 2) * C::kTokenPanel + (kk & 3) * 32;
-          mma_f16_ss(tDP, make_sdesc_sw128(sG + r, 16, 1024), make_sdesc_sw128(sV + k, 16, 1024), kIdescS, kk > 0 ? 1u : 0u);
-        }
+      auto issue_dp = [&](uint32_t sV) {
+        issue_row_changes<DK, DV>(tDP, sG, sV);
         mma_commit(dp_full);
       };
       // S(0) dP(0) | S(1) dQ(0) dP(1) | S(2) dQ(1) dP(2) | ...: S(j + 1) goes as soon as the compute warps hold S(j)
@@ -807,11 +1274,7 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
         ok = wait_bounded(ds_ready, par, wc);
         if (!ok) break;
         tc_fence_after_sync();
-        const uint32_t sK = stage(st);
-#pragma unroll
-        for (int kk = 0; kk < C::kN / 16; ++kk)
-          mma_f16_ts(tDQ, tDP + part_col<kCols>(kk), make_sdesc_sw128(sK + kk * 2048, C::kTokenPanel, 1024), kIdescDQ,
-                     (kk > 0 || j > 0) ? 1u : 0u);
+        issue_dq<DK, DV>(tDQ, tDP, stage(st), j > 0);
         mma_commit(empty_bar(st));
         if (more) issue_dp(stage(slot) + C::kKBytes);
       }
@@ -878,15 +1341,29 @@ __device__ __forceinline__ void dq_tile(const CUtensorMap& tmQ, const CUtensorMa
           for (int e = 0; e < wq / 8; ++e) reinterpret_cast<uint4*>(dst)[e] = make_uint4(0, 0, 0, 0);
       } else if (ok && wait_warp(acc_done, 0)) {
         tc_fence_after_sync();
-        store_row<wq>(tmem + lanes + C::kTmemDQ + part * wq, p.scale, dst,
-                      p.q_pieces > 1 ? p.part_q + ((tile_id * p.q_pieces + piece) * kBlk + row) * DK + part * wq : nullptr, live);
+        bad = !store_row<wq>(tmem + lanes + C::kTmemDQ + part * wq, p.scale, dst,
+                             p.q_pieces > 1 ? p.part_q + ((tile_id * p.q_pieces + piece) * kBlk + row) * DK + part * wq : nullptr, live);
       }
     }
   }
 
   if (warp == kMmaWarp && lane == 0) wait_quiesce(acc_done, 0, p.wait_limit_ns, &g_moa_window_bwd_status);
   tc_fence_before_sync();
-  __syncthreads();
+  if (__syncthreads_or(bad)) {
+    const bool dead = *abort_flag != 0;
+    if (threadIdx.x == 0) {
+      mbar_init(acc_done + 16, 1);
+      mbar_init(acc_done + 16 + 8, 1);
+      fence_barrier_init();
+    }
+    __syncthreads();
+    if (!dead && warp < kMmaWarp) {
+      tc_fence_after_sync();
+      dq_again<DK, DV>(&tmK, &tmV, p, index, smem, tmem);
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+  }
   if (warp == kMmaWarp) {
     tc_fence_after_sync();
     tmem_dealloc(tmem, C::kTmemCols);
@@ -921,8 +1398,8 @@ window_dq_tc_join_kernel(const Params p, int64_t n) {
 template <int DK, int DV>
 __global__ void __launch_bounds__(kThreads, ctas_of(DK, DV))
 window_bwd_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
-                     const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmG, const Params p,
-                     unsigned n_kv) {
+                     const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmG,
+                     const __grid_constant__ Params p, unsigned n_kv) {
   wait_for_previous();
   if (blockIdx.x < n_kv)
     dkdv_tile<DK, DV>(tmQ, tmK, tmV, tmG, p, blockIdx.x);

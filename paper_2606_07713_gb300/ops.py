@@ -140,7 +140,7 @@ def window_attn(q, k, v, window: int | None = None, sinks: int = 0, scale: float
     j <= p with j > p - window or j < sinks (window None: all j <= p); one that sees nothing gives
     zeros.  Query head h reads key head h // (H_q / H_k).  scale defaults to 1 / sqrt(d_k).
     A batch padded at the end needs no lengths; what a query does not see, not numbers included, has no
-    influence on it (the gradients are stricter: window_attn_bwd)."""
+    influence on it."""
     return _b.window_attn(q, k, v, window, sinks, scale, out, None, workspace, stream)
 
 
@@ -156,8 +156,8 @@ def window_attn_bwd(q, k, v, o, lse, do, window: int | None = None, sinks: int =
     """(dq, dk, dv): the gradients of window_attn for the gradient do of its output, from the o and lse
     of window_attn_lse.  out: three tensors of the shapes of q, k and v.
 
-    q, k, v, o and do have to be finite, in a batch's padding too (there do is zero, and q, k and v are anything finite): the weights of
-    a padded query that is not a number are none, and reach the tokens before it."""
+    What a query does not see, not numbers included, has no influence on its gradient, nor it on a hidden
+    token's.  A batch's padding is finite all the same: by the formula a query that is not a number reaches all tokens that it sees."""
     return _b.window_attn_bwd(q, k, v, o, lse, do, window, sinks, scale, out, workspace, stream)
 
 

@@ -207,3 +207,122 @@ def test_values_here_and_there_in_a_cache(lens, Hq, Hk, N, dk, dv, page, window,
         for h in range(0, Hq, max(1, Hq // 4)):
             hk = h // (Hq // Hk)
             assert agrees(o[b, h], *formula(q[b, h], k[b, hk, :n], v[b, hk, :n], see)), (b, h)
+
+
+# -- gradients ----------------------------------------------------------------------------------------
+TYPES = {"bf16": (torch.bfloat16, 2.0 ** -8), "fp32": (torch.float32, 2.0 ** -24)}
+
+
+def plant(x, seed, some, whole):
+    """`some` rows of x [B, H, N, d] get values that are not finite: single features, or (`whole`) all of them."""
+    g = torch.Generator().manual_seed(seed)
+    flat = x.view(-1, x.shape[-1])
+    for n in range(some):
+        r, f = int(torch.randint(flat.shape[0], (), generator=g)), int(torch.randint(x.shape[-1], (), generator=g))
+        flat[r, slice(None) if whole else f] = (NAN, INF, -INF)[n % 3]
+
+
+def gradients_agree(q, k, v, o, lse, do, got, window, sinks, dtype):
+    """Where the formula is finite, within its bound; elsewhere not finite.  One key head: q, o, do [G, N, .], k, v [M, .]."""
+    G, N, dk = q.shape
+    M, dv = v.shape
+    u, scale, see = TYPES[dtype][1], dk ** -0.5, sight(N, M, window, sinks)
+    ub = u if dtype == "bf16" else 0.0
+    k, v = k.double(), v.double()
+    num = lambda x: torch.where(torch.isfinite(x), x, 0.0)  # noqa: E731
+    odd = lambda x: (~torch.isfinite(x)).double()  # noqa: E731
+    sums = {n: torch.zeros(M, d, dtype=torch.float64, device="cuda") for n, d in (("k", dk), ("v", dv), ("ek", dk), ("ev", dv),
+                                                                                 ("bk", dk), ("bv", dv))}
+    for h in range(G):
+        qq, gg, oo, ll = q[h].double(), do[h].double(), o[h].double(), lse[h].double()
+        base = torch.where(ll == -INF, 0.0, ll)[:, None]
+        p = torch.where(see, torch.exp(qq @ k.T * scale - base), 0.0)
+        ds = torch.where(see, p * (gg @ v.T - (gg * oo).sum(1, keepdim=True)), 0.0)
+        badp, badds = odd(p), odd(ds)
+        seen = see.double()
+        fp, fds = num(p), num(ds)
+        size = (num(qq).abs() @ num(k).abs().T * scale).masked_fill(~see, 0).amax(1, keepdim=True)
+        w = 2 * (dk + 8) * 2.0 ** -24 * size + 2.0 ** -18 + 2.0 ** -22 * num(base).abs()
+        dot = (dv + 8) * 2.0 ** -24 * (num(gg).abs() @ num(v).abs().T + (num(gg) * num(oo)).abs().sum(1, keepdim=True))
+        eds = (w + ub + 2.0 ** -15) * fds.abs() + fp * dot * 1.02
+        want, bound = scale * fds @ num(k), scale * (eds @ num(k).abs())
+        none = (badds.sum(1, keepdim=True) + seen @ odd(k)) > 0
+        ok = torch.where(none, ~torch.isfinite(got[0][h]), (got[0][h].double() - want).abs() <= 1.02 * (bound + u * want.abs()) + 1e-30)
+        assert bool(ok.all()), ("dq", h, (~ok).nonzero()[:4].tolist())
+        sums["k"] += scale * fds.T @ num(qq)
+        sums["ek"] += scale * eds.T @ num(qq).abs()
+        sums["bk"] += badds.sum(0)[:, None] + seen.T @ odd(qq)
+        sums["v"] += fp.T @ num(gg)
+        sums["ev"] += ((w + ub + 2.0 ** -15) * fp).T @ num(gg).abs()
+        sums["bv"] += badp.sum(0)[:, None] + seen.T @ odd(gg)
+    for n, x in (("k", got[1]), ("v", got[2])):
+        want = sums[n]
+        ok = torch.where(sums["b" + n] > 0, ~torch.isfinite(x), (x.double() - want).abs() <= 1.02 * (sums["e" + n] + u * want.abs()) + 1e-30)
+        assert bool(ok.all()), ("d" + n, (~ok).nonzero()[:4].tolist())
+
+
+SHAPES = [  # B, H_q, H_k, N, M, d_k, d_v, window, sinks
+    (1, 4, 2, 300, 300, 64, 64, 50, 3), (1, 8, 2, 900, 900, 128, 128, 130, 5), (2, 6, 2, 400, 400, 64, 128, 0, 0),
+    (1, 4, 1, 500, 1700, 128, 64, 200, 0),      # tokens that no query sees
+    (1, 6, 2, 700, 430, 64, 64, 90, 2),         # queries that see nothing
+    (1, 2, 2, 40, 3000, 128, 128, 0, 0),        # few rows: tokens in pieces
+    (1, 2, 1, 3000, 3000, 64, 64, 260, 70),     # sinks' rows in pieces
+    (1, 130, 1, 90, 90, 64, 64, 20, 0),         # chunks of heads
+]
+
+
+@pytest.mark.parametrize("what", ["q", "k", "v", "do", "rows", "tokens", "all"])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_gradients(shape, dtype, what):
+    """Queries, keys, values and output gradients that are not finite reach what they see, and nothing else."""
+    B, Hq, Hk, N, M, dk, dv, window, sinks = shape
+    x = {n: rand(i, *s).to(TYPES[dtype][0]) for i, (n, s) in enumerate(
+        dict(q=(B, Hq, N, dk), k=(B, Hk, M, dk), v=(B, Hk, M, dv), do=(B, Hq, N, dv)).items())}
+    sight_ = dict(window=window or None, sinks=sinks)
+    for n in dict(rows=("q", "do"), tokens=("k", "v"), all=x).get(what, (what,)):
+        plant(x[n], N + len(n), 2 * B, what in ("rows", "tokens"))
+    hidden = M - N - window + 1                # tokens before every window
+    if window and hidden > sinks and what in ("k", "v", "tokens", "all"):
+        for n in "kv":
+            x[n][:, :, sinks:hidden] = NAN
+    if N > M and what in ("q", "do", "rows", "all"):
+        for n in ("q", "do"):
+            x[n][:, :, :N - M] = NAN
+    o, lse = pkg.window_attn_lse(x["q"], x["k"], x["v"], **sight_)
+    got = pkg.window_attn_bwd(x["q"], x["k"], x["v"], o, lse, x["do"], **sight_)
+    again = pkg.window_attn_bwd(x["q"], x["k"], x["v"], o, lse, x["do"], **sight_)
+    assert pkg.get_device_status() == _lib.MOA_OK
+    assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(got, again))
+    G = Hq // Hk
+    for b in range(B):
+        for hk in range(Hk):
+            of = lambda t: t[b, hk * G:hk * G + G]  # noqa: E731
+            gradients_agree(of(x["q"]), x["k"][b, hk], x["v"][b, hk], of(o), of(lse), of(x["do"]),
+                            (of(got[0]), got[1][b, hk], got[2][b, hk]), window, sinks, dtype)
+
+
+@pytest.mark.parametrize("what", ["q", "k", "v", "do", "all", "one k", "one v", "one q", "one do", "padding"])
+@pytest.mark.parametrize("window", [None, 1024])
+def test_gradients_take_no_longer(what, window):
+    """Diverged steps, single values, and padding that is anything: in about a call's time."""
+    N, Hq, Hk, d = 8192, 8, 2, 128
+    x = {n: rand(i, 1, h, N, d) for i, (n, h) in enumerate((("q", Hq), ("k", Hk), ("v", Hk), ("do", Hq)))}
+    o, lse = pkg.window_attn_lse(x["q"], x["k"], x["v"], window=window)
+    clean, _ = fastest(lambda: pkg.window_attn_bwd(x["q"], x["k"], x["v"], o, lse, x["do"], window=window))
+    if what == "padding":
+        for n in x:
+            x[n][:, :, 5000:] = NAN if n != "do" else 0
+    elif what.startswith("one"):
+        x[what[4:]][0, 1, 4000, 5] = NAN
+    else:
+        for n in x if what == "all" else [what]:
+            x[n].fill_(NAN)
+    o, lse = pkg.window_attn_lse(x["q"], x["k"], x["v"], window=window)
+    ms, got = fastest(lambda: pkg.window_attn_bwd(x["q"], x["k"], x["v"], o, lse, x["do"], window=window))
+    assert pkg.get_device_status() == _lib.MOA_OK
+    if what == "padding" and window:
+        assert bool(torch.isfinite(got[0][:, :, :5000]).all())      # real queries see real tokens only
+        assert all(bool(torch.isfinite(g[:, :, :5000 - window + 1]).all()) for g in got[1:])
+    # a tile once more: each step's copies, products and exponentials one after the other, five times as long at most, beside the call itself
+    assert ms <= 8 * clean + 1.0, (ms, clean)
