@@ -15,12 +15,14 @@
 //           tiles with more rows than a piece are cut, a piece being a window's rows, or less where there are too
 //           few CTAs for the machine.  dQ: 64 rows, 32 tokens at a time.  The next step's rows (tokens) are on their
 //           way while a step is computed;
+//   again   sums that are not finite, once more from the pairs that see one another (window_again.cuh), if there are any: 1.4 us of
+//           a call that has none (its code as a branch of the tiles, called or inlined, cost their loops 2 to 18 %);
 //   join    adds the pieces, in order.
 // Rows of a key head are counted position by position (row r: position r / G, head r % G of the group).
 // No atomics: results do not depend on the order in which CTAs run.
 //
 // What bounds it: shared memory's data path (47 %) and issue slots (40 %) about equally, with the barriers of a step as the largest
-// wait; multiply-adds are at 23 % of their rate (2 x (6 / 3) heads x 517 x (128 / 64), window 100: 54 us, in three launches).
+// wait; multiply-adds are at 23 % of their rate (2 x (6 / 3) heads x 517 x (128 / 64), window 100: 55.6 us, in four launches).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -39,6 +41,7 @@ constexpr int kKeysKv = 64, kRowsKv = 32;   // dkdv: tokens of a CTA, rows of a 
 constexpr int kRowsQ = 64, kKeysQ = 32;     // dq: rows of a CTA, tokens of a step
 constexpr int kThreads = 256;
 constexpr int64_t kMostPieces = 1216;       // of cut token tiles: eight for each SM
+constexpr int64_t kMostAgain = 304;         // CTAs that look for sums to compute once more: two for each SM
 
 struct Params {
   View q, k, v, o, go, dq, dk, dv;
@@ -47,6 +50,7 @@ struct Params {
   float* delta;   // alike
   float* part;    // [piece item][64][DK + DV], null: no pieces
   float* part_q;  // [dQ tile][piece][64][DK], if dQ's tiles come in pieces
+  uint32_t* odd;  // [CTA of the tiles][warp] which of its eight rows (tokens: dK, and dV in the second byte) have sums that are not finite
   int Hk, N, G, Nk;
   win::Mask mask;
   float c_log2, scale;
@@ -222,13 +226,13 @@ __device__ __forceinline__ uint32_t odd_sums(const float (&sum)[4][N]) {
 // dK (KEY) or dV of a warp's tokens `bad` once more, from what their rows see (window_again.cuh): sums that are not finite, as hidden
 // pairs' may not be (0 * NaN).
 template <typename T, int DK, int DV, bool KEY>
-__device__ __noinline__ void tokens_again(const Params& p, unsigned index, uint32_t bad) {
+__device__ __forceinline__ void tokens_again(const Params& p, unsigned index, int warp, uint32_t bad) {
   const unsigned per = unsigned(p.cut * p.pieces + p.n_kt - p.cut);
   const int bh = int(index / per), item = int(index - unsigned(bh) * per);
   const bool whole = item >= p.cut * p.pieces;
   const int kt = whole ? item - p.cut * p.pieces + p.cut : item / p.pieces, piece = whole ? 0 : item - kt * p.pieces;
   const int b = bh / p.Hk, h = bh - b * p.Hk, k0 = kt * kKeysKv, off = p.Nk - p.N;
-  const int keys = p.Nk - k0 < kKeysKv ? p.Nk - k0 : kKeysKv, first = 8 * (threadIdx.x >> 5);
+  const int keys = p.Nk - k0 < kKeysKv ? p.Nk - k0 : kKeysKv, first = 8 * warp;
   const int64_t rows = int64_t(p.N) * p.G;
   int ra, rz;
   rows_of_piece(p, kt, whole ? -1 : piece, &ra, &rz);
@@ -242,7 +246,7 @@ __device__ __noinline__ void tokens_again(const Params& p, unsigned index, uint3
       win::Tokens<T>{row_of<T>(p.k, b, h, 0), row_of<T>(p.v, b, h, 0), p.k.sn, p.v.sn},
       [=](int x) {
         const int r = ra + x, i = int(unsigned(r) / unsigned(G)), g = r - i * G;
-        return win::RowOf<T>{q + g * q_sh + i * q_sn, go + g * go_sh + i * go_sn, nl[x], delta[x], i + off};
+        return win::RowOf<T>{q + g * q_sh + i * q_sn, go + g * go_sh + i * go_sn, nl[x], delta[x], i + off, true};
       },
       [&](int j, int f, const float(&sum)[(KEY ? DK : DV) / 32]) {
         float* to = p.part + (((int64_t(bh) * p.cut + kt) * p.pieces + piece) * kKeysKv + (j - k0)) * (DK + DV) + (KEY ? 0 : DK) + f;
@@ -258,7 +262,7 @@ __device__ __noinline__ void tokens_again(const Params& p, unsigned index, uint3
 }
 
 template <typename T, int DK, int DV>
-__device__ __forceinline__ void dkdv_tile(const Params& p, unsigned index, float* smem) {
+__device__ __forceinline__ uint32_t dkdv_tile(const Params& p, unsigned index, float* smem) {
   using S = KvSmem<DK, DV>;
   constexpr int kLdW = S::kLdW, kBuf = buffers(DK, DV);
   float* sK = smem;
@@ -276,7 +280,7 @@ __device__ __forceinline__ void dkdv_tile(const Params& p, unsigned index, float
   const int keys = p.Nk - k0 < kKeysKv ? p.Nk - k0 : kKeysKv;
   const int64_t rows = int64_t(p.N) * p.G;
   int ra, rz;
-  if (!rows_of_piece(p, kt, whole ? -1 : piece, &ra, &rz)) return;   // the join adds what pieces there are
+  if (!rows_of_piece(p, kt, whole ? -1 : piece, &ra, &rz)) return 0;   // the join adds what pieces there are
   fill_tokens<T, DK, DV, kKeysKv>(p.k, p.v, sK, sV, b, h, k0, win::Run{p.Nk, p.Nk, p.Nk});
   if (ra < rz) fill_rows<T, DK, DV, kRowsKv>(p.q, p.go, sRows, sRows + kRowsKv * (DK + 4), b, h, p.G, ra, rz);
   fill_commit();
@@ -409,9 +413,7 @@ __device__ __forceinline__ void dkdv_tile(const Params& p, unsigned index, float
     for (int c = 0; c < DV / 64; ++c)
       store4(ov + 64 * c + 4 * tx, make_float4(dv[a][4 * c], dv[a][4 * c + 1], dv[a][4 * c + 2], dv[a][4 * c + 3]));
   }
-  const uint32_t bad_k = odd_sums(dk), bad_v = odd_sums(dv);
-  if (bad_k != 0) tokens_again<T, DK, DV, true>(p, index, bad_k);
-  if (bad_v != 0) tokens_again<T, DK, DV, false>(p, index, bad_v);
+  return odd_sums(dk) | odd_sums(dv) << 8;
 }
 
 // Adds the pieces of cut tiles: four features of a token a thread.
@@ -448,10 +450,10 @@ struct QSmem {
 
 // dQ of a warp's rows `bad` once more, from the tokens that they see.
 template <typename T, int DK, int DV>
-__device__ __noinline__ void rows_again(const Params& p, unsigned index, uint32_t bad) {
+__device__ __forceinline__ void rows_again(const Params& p, unsigned index, int warp, uint32_t bad) {
   const unsigned tile = index / unsigned(p.q_pieces), piece = index - tile * unsigned(p.q_pieces);
   const int bh = int(tile / unsigned(p.n_rt)), rt = p.n_rt - 1 - int(tile - unsigned(bh) * unsigned(p.n_rt));
-  const int b = bh / p.Hk, h = bh - b * p.Hk, r0 = rt * kRowsQ, off = p.Nk - p.N, first = r0 + 8 * int(threadIdx.x >> 5);
+  const int b = bh / p.Hk, h = bh - b * p.Hk, r0 = rt * kRowsQ, off = p.Nk - p.N, first = r0 + 8 * warp;
   const int64_t rows = int64_t(p.N) * p.G;
   const int live = int(rows - r0 < kRowsQ ? rows - r0 : kRowsQ), i0 = r0 / p.G, i1 = (r0 + live - 1) / p.G;
   const win::Run run = win::run_of(p.mask, p.Nk, p.N, i0, i1);
@@ -465,7 +467,7 @@ __device__ __noinline__ void rows_again(const Params& p, unsigned index, uint32_
       [&](int t) {
         const int r = first + t, i = r / p.G;
         const int64_t hq = int64_t(h) * p.G + (r - i * p.G);
-        return win::RowOf<T>{row_of<T>(p.q, b, hq, i), row_of<T>(p.go, b, hq, i), p.nl[bh * rows + r], p.delta[bh * rows + r], i + off};
+        return win::RowOf<T>{row_of<T>(p.q, b, hq, i), row_of<T>(p.go, b, hq, i), p.nl[bh * rows + r], p.delta[bh * rows + r], i + off, true};
       },
       [=](int x) { return run.at(begin + x); },
       [&](int t, int f, const float(&sum)[DK / 32]) {
@@ -482,7 +484,7 @@ __device__ __noinline__ void rows_again(const Params& p, unsigned index, uint32_
 }
 
 template <typename T, int DK, int DV>
-__device__ __forceinline__ void dq_tile(const Params& p, unsigned index, float* smem) {
+__device__ __forceinline__ uint32_t dq_tile(const Params& p, unsigned index, float* smem) {
   using S = QSmem<DK, DV>;
   constexpr int kLdW = S::kLdW, kBuf = buffers(DK, DV);
   float* sQ = smem;
@@ -610,8 +612,7 @@ __device__ __forceinline__ void dq_tile(const Params& p, unsigned index, float* 
       store4(dst + 64 * c + 4 * tx, make_float4(dq[a][4 * c] * p.scale, dq[a][4 * c + 1] * p.scale, dq[a][4 * c + 2] * p.scale,
                                                 dq[a][4 * c + 3] * p.scale));
   }
-  const uint32_t bad = odd_sums(dq);
-  if (bad != 0) rows_again<T, DK, DV>(p, index, bad);
+  return odd_sums(dq);
 }
 
 // Adds the pieces of dQ's tiles: four features of a row a thread.
@@ -638,13 +639,37 @@ window_dq_join_kernel(const Params p, int64_t n) {
 // CTAs below n_q: dQ; the others, whose pieces are shorter: dK and dV.
 template <typename T, int DK, int DV>
 __global__ void __launch_bounds__(kThreads, 2)
-window_bwd_cc_kernel(const __grid_constant__ Params p, unsigned n_q) {
+window_bwd_cc_kernel(const Params p, unsigned n_q) {
   extern __shared__ float smem[];
   wait_for_previous();
-  if (blockIdx.x < n_q)
-    dq_tile<T, DK, DV>(p, blockIdx.x, smem);
-  else
-    dkdv_tile<T, DK, DV>(p, blockIdx.x - n_q, smem);
+  const uint32_t odd = blockIdx.x < n_q ? dq_tile<T, DK, DV>(p, blockIdx.x, smem) : dkdv_tile<T, DK, DV>(p, blockIdx.x - n_q, smem);
+  if (threadIdx.x % 32 == 0) p.odd[blockIdx.x * (kThreads / 32) + threadIdx.x / 32] = odd;
+}
+
+// The marked sums of all CTAs' warps, of which there are n, once more: neighbours by different warps.
+template <typename T, int DK, int DV>
+__global__ void __launch_bounds__(kThreads)
+window_again_kernel(const Params p, unsigned n, unsigned n_q) {
+  wait_for_previous();
+  const unsigned lane = threadIdx.x % 32, warps = gridDim.x * (kThreads / 32), mine = blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
+  for (unsigned base = mine; base < n; base += 32 * warps) {
+    const uint64_t at = base + uint64_t(lane) * warps;
+    const uint32_t odd = at < n ? p.odd[at] : 0u;
+    uint32_t marked = __ballot_sync(0xffffffffu, odd != 0);
+    while (marked != 0) {
+      const int from = __ffs(marked) - 1;
+      marked &= marked - 1;
+      const uint32_t bad = __shfl_sync(0xffffffffu, odd, from);
+      const unsigned which = base + unsigned(from) * warps, cta = which / (kThreads / 32);
+      const int warp = int(which % (kThreads / 32));
+      if (cta < n_q) {
+        rows_again<T, DK, DV>(p, cta, warp, bad);
+      } else {
+        if ((bad & 0xffu) != 0) tokens_again<T, DK, DV, true>(p, cta - n_q, warp, bad & 0xffu);
+        if (bad >> 8 != 0) tokens_again<T, DK, DV, false>(p, cta - n_q, warp, bad >> 8);
+      }
+    }
+  }
 }
 
 // How token tiles are cut: pieces of a window's rows (of all rows without one), or of so few that there are two CTAs
@@ -689,7 +714,7 @@ Cut cut_of(const WindowBwdArgs& a) {
   return c;
 }
 
-// The workspace: -LSE log2 e and D of every row, then the pieces.
+// The workspace: -LSE log2 e and D of every row, the pieces, and the marks of sums that are not finite.
 int64_t rows_bytes(const WindowBwdArgs& a) { return (a.B * a.Hq * a.Nq * 4 + 255) / 256 * 256; }
 
 template <typename T, int DK, int DV>
@@ -704,6 +729,8 @@ int launch(const WindowBwdArgs& a, char* msg, size_t msglen) {
   p.delta = reinterpret_cast<float*>(ws + rows_bytes(a));
   p.part = reinterpret_cast<float*>(ws + 2 * rows_bytes(a));
   p.part_q = p.part + bh * cut.cut * cut.pieces * kKeysKv * (DK + DV);
+  const int64_t items = bh * (cut.cut * cut.pieces + cut.n_kt - cut.cut), ctas = items + cut.q_tiles * cut.q_pieces;
+  p.odd = reinterpret_cast<uint32_t*>(p.part_q + (cut.q_pieces > 1 ? cut.q_tiles * cut.q_pieces * kRowsQ * DK : 0));
   p.q_pieces = int(cut.q_pieces);
   p.Hk = int(a.Hk), p.N = int(a.Nq), p.G = int(G), p.Nk = int(a.Nk);
   p.mask = win::Mask{a.window, a.sinks, true};
@@ -716,10 +743,13 @@ int launch(const WindowBwdArgs& a, char* msg, size_t msglen) {
   cudaError_t e = ensure_smem_limit(reinterpret_cast<const void*>(kern), kSmem);
   if (e == cudaSuccess)
     e = launch_overlapped(window_delta_kernel<T, DV>, dim3(unsigned((rows + 7) / 8)), dim3(kThreads), 0, a.stream, p, rows);
-  const int64_t items = bh * (cut.cut * cut.pieces + cut.n_kt - cut.cut);
   if (e == cudaSuccess)
-    e = launch_overlapped(kern, dim3(unsigned(items + cut.q_tiles * cut.q_pieces)), dim3(kThreads), size_t(kSmem), a.stream, p,
+    e = launch_overlapped(kern, dim3(unsigned(ctas)), dim3(kThreads), size_t(kSmem), a.stream, p,
                           unsigned(cut.q_tiles * cut.q_pieces));
+  const int64_t marks = ctas * (kThreads / 32), again = (marks + kThreads - 1) / kThreads;
+  if (e == cudaSuccess)
+    e = launch_overlapped(window_again_kernel<T, DK, DV>, dim3(unsigned(again < kMostAgain ? again : kMostAgain)), dim3(kThreads), 0,
+                          a.stream, p, unsigned(marks), unsigned(cut.q_tiles * cut.q_pieces));
   const int64_t joined = bh * cut.cut * kKeysKv * ((DK + DV) / 4);
   if (e == cudaSuccess && joined > 0)
     e = launch_overlapped(window_dkdv_join_kernel<T, DK, DV>, dim3(unsigned((joined + kThreads - 1) / kThreads)), dim3(kThreads),
@@ -745,8 +775,9 @@ int launch_sizes(const WindowBwdArgs& a, char* msg, size_t msglen) {
 
 size_t window_bwd_cc_workspace(const WindowBwdArgs& a) {
   const Cut c = cut_of(a);
+  const int64_t ctas = a.B * a.Hk * (c.cut * c.pieces + c.n_kt - c.cut) + c.q_tiles * c.q_pieces;
   return size_t(2 * rows_bytes(a) + a.B * a.Hk * c.cut * c.pieces * kKeysKv * (a.dk + a.dv) * 4 +
-                (c.q_pieces > 1 ? c.q_tiles * c.q_pieces * kRowsQ * a.dk * 4 : 0));
+                (c.q_pieces > 1 ? c.q_tiles * c.q_pieces * kRowsQ * a.dk * 4 : 0) + ctas * (kThreads / 32) * 4);
 }
 
 int launch_window_bwd_cc(const WindowBwdArgs& a, char* msg, size_t msglen) {
