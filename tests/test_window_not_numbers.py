@@ -326,3 +326,26 @@ def test_gradients_take_no_longer(what, window):
         assert all(bool(torch.isfinite(g[:, :, :5000 - window + 1]).all()) for g in got[1:])
     # a tile once more: each step's copies, products and exponentials one after the other, five times as long at most, beside the call itself
     assert ms <= 8 * clean + 1.0, (ms, clean)
+
+
+@pytest.mark.parametrize("what", ["q", "k", "do", "rows", "tokens"])
+def test_gradients_of_tokens_that_sequences_share(what):
+    """bf16 on CUDA cores: one sequence's keys and values, expanded over the batch."""
+    B, Hq, Hk, N, M, dk, dv, window, sinks = 2, 6, 2, 300, 420, 64, 128, 70, 3
+    x = {n: rand(i, *s) for i, (n, s) in enumerate(
+        dict(q=(B, Hq, N, dk), k=(1, Hk, M, dk), v=(1, Hk, M, dv), do=(B, Hq, N, dv)).items())}
+    for n in dict(rows=("q", "do"), tokens=("k", "v")).get(what, (what,)):
+        plant(x[n], N + len(n), 4, what in ("rows", "tokens"))
+    for n in "kv":
+        if what in ("k", "tokens"):
+            x[n][:, :, sinks:M - N - window + 1] = NAN
+        x[n] = x[n].expand(B, -1, -1, -1)
+    o, lse = pkg.window_attn_lse(x["q"], x["k"], x["v"], window=window, sinks=sinks)
+    got = pkg.window_attn_bwd(x["q"], x["k"], x["v"], o, lse, x["do"], window=window, sinks=sinks)
+    assert pkg.get_device_status() == _lib.MOA_OK
+    G = Hq // Hk
+    for b in range(B):
+        for hk in range(Hk):
+            of = lambda t: t[b, hk * G:hk * G + G]  # noqa: E731
+            gradients_agree(of(x["q"]), x["k"][b, hk], x["v"][b, hk], of(o), of(lse), of(x["do"]),
+                            (of(got[0]), got[1][b, hk], got[2][b, hk]), window, sinks, "bf16")
